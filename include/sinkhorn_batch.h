@@ -59,7 +59,8 @@ typedef enum {
                         /* kernel that can skip lanes.  Results are bit-identical to MASKED.        */
 } skb_mode;
 
-typedef enum { SKB_F32 = 0, SKB_BF16 = 1 } skb_dtype;           /* storage type of x and y only */
+/* Storage type of x and y only.  The 4-bit types are those of sinkhorn_cloud4_pack. */
+typedef enum { SKB_F32 = 0, SKB_BF16 = 1, SKB_MX4 = 2, SKB_NV4 = 3 } skb_dtype;
 /* Arithmetic of the pair terms log2 pi_ij and their exponentials. */
 typedef enum {
     SKB_COMPUTE_AUTO = 0,  /* F32 (TENSOR where eligible), or MIXED when some lane's cost/eps  */
@@ -406,6 +407,37 @@ skb_status sinkhorn_row_residual_static(const float *x, const float *y, const fl
                                         const double *f, const double *g, const float *eps,
                                         int W, int n, int m, int d, float *r_row, void *stream);
 const char *sinkhorn_row_residual_static_last_error(void);
+
+/*
+ * Clouds held in microscaled 4-bit floating point: a quarter of bf16's memory for embedding banks.
+ * The points of a cloud [W, npts, d], 1 <= d <= 1024, become one buffer of sinkhorn_cloud4_bytes(W, npts, d,
+ * format) bytes (0: a bad argument), device memory of the caller, 256-byte aligned, of these parts, each padded to 256 bytes:
+ *   codes   [W npts][16 ceil(d/32)] bytes; two e2m1 codes to a byte (0, .5, 1, 1.5, 2, 3, 4, 6, and 8 added for the sign),
+ *           the even dimension in the low half; code 0 past the last dimension
+ *   scales  [W npts][s] bytes.  SKB_MX4: e8m0, one for 32 dimensions, s = 4 ceil(d/128).  SKB_NV4: e4m3, one for
+ *           16 dimensions, s = 4 ceil(d/64).  Unused bytes are 0
+ *   points  SKB_NV4 only: [W npts] floats, powers of two
+ * and stand for code * scale (* the point's power of two), which fp32 holds exactly, and bf16 from 2^-126 on.
+ *
+ * sinkhorn_cloud4_pack rounds v [W, npts, d] (SKB_F32 or SKB_BF16):
+ *   SKB_MX4   scale 2^(floor(log2 of the block's largest magnitude) - 2), at least 2^-127 (also for a block of zeros)
+ *   SKB_NV4   point 2^(floor(log2 of the point's largest magnitude) - 10), at least 2^-126, 1 for a point of zeros;
+ *             scale = largest magnitude of the block / 6 / point, to nearest even (320 at most where point is 2^117:
+ *             no value passes fp32's range)
+ *   codes are magnitude / scale to the nearest of the eight, halves to the even code, at most 6.
+ * A point with an infinite or NaN value becomes NaN as a whole (all of its scales).
+ *   values   may be null; else [W, npts, d] of values_dtype (SKB_F32 or SKB_BF16): what the buffer stands for,
+ *            written by the same launch (for costs of the rounded points, or a training step's forward values)
+ * sinkhorn_cloud4_unpack writes the values of a buffer.  Both enqueue one kernel on `stream` of the current device.
+ */
+size_t sinkhorn_cloud4_bytes(int W, int npts, int d, int format);
+skb_status sinkhorn_cloud4_pack(const void *v, int v_dtype, int W, int npts, int d, int format, void *cloud,
+                                void *values, int values_dtype, void *stream);
+skb_status sinkhorn_cloud4_unpack(const void *cloud, int W, int npts, int d, int format, void *values, int values_dtype,
+                                  void *stream);
+
+/* Text of the calling thread's last failed sinkhorn_cloud4_* call (empty after a successful one). */
+const char *sinkhorn_operator_last_error(void);
 
 /* Host string describing the last error on this handle (or, when h is null, of the calling
  * thread's last failed create or host-buffer solve).  Valid until the next call on the same

@@ -34,7 +34,10 @@ EXPORTS = (
 )
 PHASES = ("create", "f_leg", "column_check", "plan", "emit_move", "g_leg")
 # entry points outside the sinkhorn_batch_* family
-EXTRA_EXPORTS = ("sinkhorn_row_residual_static", "sinkhorn_row_residual_static_last_error")
+EXTRA_EXPORTS = ("sinkhorn_row_residual_static", "sinkhorn_row_residual_static_last_error",
+                 "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_operator_last_error")
+DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+FORMATS = {"mx4": 2, "nv4": 3}
 
 
 class SkbConfig(ctypes.Structure):
@@ -97,6 +100,12 @@ def _load():
                                                  ctypes.c_int, ctypes.c_int, vp, vp]
     lib.sinkhorn_row_residual_static.restype = ctypes.c_int
     lib.sinkhorn_row_residual_static_last_error.restype = ctypes.c_char_p
+    ci = ctypes.c_int
+    lib.sinkhorn_cloud4_bytes.restype = ctypes.c_size_t
+    lib.sinkhorn_cloud4_bytes.argtypes = [ci, ci, ci, ci]
+    lib.sinkhorn_cloud4_pack.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, ci, vp]
+    lib.sinkhorn_cloud4_unpack.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp]
+    lib.sinkhorn_operator_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("sinkhorn_batch_workspace_bytes", "sinkhorn_batch_host_workspace_bytes",
                         "sinkhorn_batch_destroy", "sinkhorn_batch_last_error"):
@@ -186,6 +195,72 @@ def unit_rates(device=None):
     with torch.cuda.device(dev):
         _check(lib.sinkhorn_batch_selftest_unit_rates(out, _ptr(sink), torch.cuda.current_stream(dev).cuda_stream))
     return dict(zip(("ffma", "ffma2", "dfma", "ex2"), list(out)))
+
+
+# ---- operators beside the solver --------------------------------------------------------
+
+def _check_op(code):
+    if code != SKB_OK:
+        raise SkbError(code, lib.sinkhorn_operator_last_error().decode())
+
+
+def _stream(device, stream):
+    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+
+
+class Cloud4:
+    """A cloud [W, npts, d] held in 4 bits: `buffer` as sinkhorn_cloud4_pack lays it out (a uint8 CUDA tensor)."""
+
+    def __init__(self, buffer, W, npts, d, format):
+        need = lib.sinkhorn_cloud4_bytes(W, npts, d, FORMATS[format])
+        if need == 0:
+            raise ValueError("W, npts and d must be >= 1, d at most 1024")
+        if buffer.dtype != torch.uint8 or not buffer.is_cuda or not buffer.is_contiguous() or buffer.numel() < need:
+            raise ValueError(f"buffer must be a contiguous uint8 CUDA tensor of at least {need} bytes")
+        if buffer.data_ptr() % 256:
+            raise ValueError("buffer must be 256-byte aligned")
+        self.buffer, self.W, self.npts, self.d, self.format = buffer, W, npts, d, format
+
+    @property
+    def shape(self):
+        return (self.W, self.npts, self.d)
+
+    @property
+    def device(self):
+        return self.buffer.device
+
+    def values(self, dtype=torch.float32, stream=None):
+        """What the cloud stands for, [W, npts, d] float32 or bfloat16."""
+        if dtype not in DTYPES:
+            raise ValueError("dtype must be float32 or bfloat16")
+        with torch.cuda.device(self.device):
+            out = torch.empty(self.shape, dtype=dtype, device=self.device)
+            _check_op(lib.sinkhorn_cloud4_unpack(_ptr(self.buffer), self.W, self.npts, self.d, FORMATS[self.format], _ptr(out),
+                                                 DTYPES[dtype], _stream(self.device, stream)))
+        return out
+
+
+def cloud4_pack(v, format="mx4", values=None, stream=None):
+    """Rounds v [W, npts, d] (float32 or bfloat16, CUDA) to 4 bits, format "mx4" or "nv4"; returns a Cloud4, or with
+    `values` (torch.float32 or torch.bfloat16) the pair of it and the values that it stands for."""
+    if v.dim() != 3 or not v.is_cuda or v.dtype not in DTYPES:
+        raise ValueError("v must be a float32 or bfloat16 CUDA tensor [W, npts, d]")
+    if format not in FORMATS:
+        raise ValueError(f"format must be one of {tuple(FORMATS)}")
+    if values is not None and values not in DTYPES:
+        raise ValueError("values must be torch.float32 or torch.bfloat16")
+    v = v.contiguous()
+    W, npts, d = v.shape
+    need = lib.sinkhorn_cloud4_bytes(W, npts, d, FORMATS[format])
+    if need == 0:
+        raise ValueError("W, npts and d must be >= 1, d at most 1024")
+    with torch.cuda.device(v.device):
+        buffer = torch.empty(need, dtype=torch.uint8, device=v.device)
+        out = None if values is None else torch.empty(v.shape, dtype=values, device=v.device)
+        _check_op(lib.sinkhorn_cloud4_pack(_ptr(v), DTYPES[v.dtype], W, npts, d, FORMATS[format], _ptr(buffer), _ptr(out),
+                                           DTYPES.get(values, 0), _stream(v.device, stream)))
+    cloud = Cloud4(buffer, W, npts, d, format)
+    return cloud if values is None else (cloud, out)
 
 
 class SinkhornBatch:

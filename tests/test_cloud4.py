@@ -1,0 +1,238 @@
+"""Clouds in microscaled 4-bit floating point: rounding, layout, values and refusals.
+
+The reference is the definition of the header in float64, by comparison with every value of the grid.  Codes, scales and
+values are exact numbers, so nothing here has a tolerance."""
+import numpy as np
+import pytest
+
+GRID = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2607_24741_b200 import build
+    build.build()
+    from paper_2607_24741_b200 import binding
+    return binding
+
+
+def floor_log2(v):
+    return np.frexp(v)[1] - 1
+
+
+def nearest_code(a):
+    """Index of the nearest grid value, halves to the even index."""
+    a = np.minimum(a, 6.0)
+    hi = np.clip(np.searchsorted(GRID, a, side="left"), 1, 7)
+    lo = hi - 1
+    dl, dh = a - GRID[lo], GRID[hi] - a
+    return np.where(dl < dh, lo, np.where(dh < dl, hi, np.where(lo % 2 == 0, lo, hi)))
+
+
+def e4m3_round(q):
+    """Nearest e4m3 value of q in [0, 448], halves to even."""
+    step = 2.0 ** (np.maximum(np.where(q > 0, floor_log2(np.where(q > 0, q, 1.0)), -6), -6) - 3)
+    return np.rint(q / step) * step
+
+
+def e4m3_byte(v):
+    e = np.maximum(np.where(v > 0, floor_log2(np.where(v > 0, v, 1.0)), -6), -6)
+    frac = v / 2.0 ** (e - 3)                                    # 0 .. 15 eighths
+    return np.where(frac >= 8, (e + 7) * 8 + frac - 8, frac).astype(np.uint8)
+
+
+def reference(x, fmt):
+    """codes [r, 32 ceil(d/32)], scale bytes [r, words], points [r], values [r, d] of x [r, d] (float64 holding the input's values)."""
+    r, d = x.shape
+    size = 32 if fmt == "mx4" else 16
+    nb = -(-d // 32) * (32 // size)
+    v = np.zeros((r, nb * size))
+    v[:, :d] = x
+    bad = ~np.isfinite(v).all(1)
+    v[bad] = 0.0
+    block = np.abs(v.reshape(r, nb, size))
+    top = block.max(2)
+    point = np.ones(r)
+    if fmt == "mx4":
+        e = np.where(top > 0, floor_log2(np.where(top > 0, top, 1.0)) - 2, -127)
+        e = np.maximum(e, -127)
+        scale, byte = 2.0 ** e.astype(np.float64), (e + 127).astype(np.uint8)
+    else:
+        whole = top.max(1)
+        pe = np.where(whole > 0, np.maximum(floor_log2(np.where(whole > 0, whole, 1.0)) - 10, -126), 0)
+        point = 2.0 ** pe.astype(np.float64)
+        s = e4m3_round(top / 6.0 / point[:, None])
+        s = np.where((point == 2.0 ** 117)[:, None], np.minimum(s, 320.0), s)
+        scale, byte = s * point[:, None], e4m3_byte(s)
+    q = np.divide(block, scale[:, :, None], out=np.zeros_like(block), where=scale[:, :, None] > 0)
+    code = nearest_code(q)
+    values = (GRID[code] * scale[:, :, None]).reshape(r, -1) * np.where(v < 0, -1.0, 1.0)
+    code = (code.reshape(r, -1) + 8 * np.signbit(v)).astype(np.uint8)
+    if bad.any():
+        code[bad], values[bad] = 0, np.nan
+        byte[bad] = 255 if fmt == "mx4" else 127
+    words = np.zeros((r, -(-nb // 4) * 4), np.uint8)
+    words[:, :nb] = byte
+    return code, words, point, values[:, :d]
+
+
+def split(buf, rows, d, fmt):
+    pad = lambda b: -(-b // 256) * 256
+    cb, nb = -(-d // 32) * 16, -(-d // 32) * (1 if fmt == "mx4" else 2)
+    sb = -(-nb // 4) * 4
+    codes = buf[:rows * cb].reshape(rows, cb)
+    code = np.stack((codes & 15, codes >> 4), 2).reshape(rows, -1)
+    at = pad(rows * cb)
+    scales = buf[at:at + rows * sb].reshape(rows, sb)
+    at += pad(rows * sb)
+    points = buf[at:at + 4 * rows].copy().view(np.float32) if fmt == "nv4" else np.ones(rows, np.float32)
+    at += pad(4 * rows) if fmt == "nv4" else 0
+    return code, scales, points, at
+
+
+def check(B, x, fmt, values=None):
+    """x: a CPU tensor [W, npts, d]."""
+    import torch
+    W, npts, d = x.shape
+    v = x.cuda()
+    got = B.cloud4_pack(v, fmt, values=values)
+    cloud, vals = got if values is not None else (got, None)
+    code, words, point, want = reference(x.double().numpy().reshape(W * npts, d), fmt)
+    gcode, gwords, gpoint, total = split(cloud.buffer.cpu().numpy(), W * npts, d, fmt)
+    assert total == cloud.buffer.numel()
+    np.testing.assert_array_equal(gwords, words)
+    np.testing.assert_array_equal(gpoint, point.astype(np.float32))
+    np.testing.assert_array_equal(gcode, code)
+    want = want.reshape(W, npts, d)
+    np.testing.assert_array_equal(cloud.values().cpu().double().numpy(), want)
+    if vals is not None:
+        assert vals.dtype == values
+        np.testing.assert_array_equal(vals.cpu().double().numpy(), want)
+        np.testing.assert_array_equal(cloud.values(values).cpu().double().numpy(), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+@pytest.mark.parametrize("d", [1, 2, 15, 16, 17, 32, 33, 48, 64, 100, 128, 129, 200, 256, 333, 512, 520, 640, 1000, 1024])
+def test_codes_scales_and_values_of_every_depth(B, fmt, d):
+    import torch
+    gen = torch.Generator().manual_seed(d)
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn(3, 37, d, generator=gen) * torch.exp(3.0 * torch.randn(3, 37, 1, generator=gen))
+        check(B, x.to(dtype), fmt, values=torch.bfloat16 if d % 2 else torch.float32)
+        check(B, (x * torch.exp(2.0 * torch.randn(3, 37, d, generator=gen))).to(dtype), fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+def test_halves_go_to_the_even_code_and_their_neighbours_do_not(B, fmt):
+    # values at scale * (halfway between two grid values), one step of fp32 below and above, for every e4m3 mantissa
+    import torch
+    rows = []
+    for eighths in range(8, 16):
+        s = np.float32(eighths / 8.0) if fmt == "nv4" else np.float32(1.0)
+        ties = np.float32([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]) * s
+        block = np.concatenate([np.nextafter(ties, np.float32(0)), ties, np.nextafter(ties, np.float32(9)), [6 * s]])
+        for part in (block[:15], block[7:]):
+            row = np.zeros(32, np.float32)
+            row[:len(part)] = part
+            row[15] = 6 * s                                      # the block's largest: the scale is s
+            row[16:] = -row[:16]
+            rows.append(row)
+    check(B, torch.from_numpy(np.stack(rows))[None], fmt, values=torch.float32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+def test_scales_at_their_borders(B, fmt):
+    # e4m3 scales exactly between two values, blocks far below their point's largest value, zeros, the ends of fp32
+    import torch
+    rng = np.random.default_rng(5)
+    x = np.zeros((96, 64), np.float32)
+    for i in range(64):
+        q = np.float32((17 + 2 * (i % 8)) / 16.0) * np.float32(2.0 ** -(i // 8))      # halfway between two e4m3 values of its binade
+        x[i, :16] = 6 * 8.0 / 8 * 32                             # fixes the point's power of two
+        x[i, 16:32] = 6 * q
+        x[i, 40] = 2.0 ** -(i // 2) * rng.uniform(1, 2)
+    x[64:72] = rng.standard_normal((8, 64)) * 2.0 ** -120
+    x[72:76] = rng.standard_normal((4, 64)) * 2.0 ** -140
+    x[76, 3] = 2.0 ** -149
+    x[77] = 3.4028235e38
+    x[78, ::2] = -3.4028235e38
+    x[79] = -0.0
+    x[80:] = rng.standard_normal((16, 64)) * 10.0 ** rng.integers(-30, 30, (16, 1))
+    check(B, torch.from_numpy(x)[None], fmt, values=torch.float32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_point_with_a_value_that_is_not_finite_is_nan_as_a_whole(B, fmt, bad):
+    import torch
+    for d in (24, 200, 600):
+        x = torch.randn(2, 9, d, generator=torch.Generator().manual_seed(1))
+        x[0, 3, d - 1] = bad
+        x[1, 8, 0] = bad
+        check(B, x, fmt, values=torch.float32)
+        check(B, x.bfloat16(), fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+def test_unaligned_and_strided_inputs_and_another_stream(B, fmt):
+    import torch
+    base = torch.randn(4 * 50 * 64 + 1, generator=torch.Generator().manual_seed(2)).cuda()
+    x = base[1:].view(4, 50, 64)                                 # contiguous, 4-byte aligned only
+    want = B.cloud4_pack(x.clone(), fmt)
+    np.testing.assert_array_equal(split(B.cloud4_pack(x, fmt).buffer.cpu().numpy(), 200, 64, fmt)[0],
+                                  split(want.buffer.cpu().numpy(), 200, 64, fmt)[0])
+    t = torch.randn(4, 64, 50, generator=torch.Generator().manual_seed(3)).cuda().transpose(1, 2)   # strided view
+    a, b = B.cloud4_pack(t, fmt), B.cloud4_pack(t.contiguous(), fmt)
+    assert torch.equal(a.values(), b.values())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c = B.cloud4_pack(x, fmt, values=torch.float32)[1]
+    side.synchronize()
+    assert torch.equal(c, want.values())
+
+
+@pytest.mark.gpu
+def test_packing_is_captured_and_replayed_on_new_values(B):
+    import torch
+    x = torch.randn(2, 100, 96).cuda()
+    B.cloud4_pack(x, "nv4", values=torch.float32)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cloud, vals = B.cloud4_pack(x, "nv4", values=torch.float32)
+    for _ in range(2):
+        x.copy_(torch.randn(2, 100, 96))
+        graph.replay()
+        assert torch.equal(vals, B.cloud4_pack(x.clone(), "nv4").values())
+        assert torch.equal(vals, cloud.values())
+
+
+def test_refusals_of_pack_and_unpack(B):
+    import ctypes
+    import torch
+    L, one = B.lib, ctypes.c_void_p(4096)
+    assert L.sinkhorn_cloud4_bytes(1, 1, 1, 2) == 512 and L.sinkhorn_cloud4_bytes(1, 1, 1, 3) == 768
+    assert L.sinkhorn_cloud4_bytes(64, 1024, 512, 2) == 64 * 1024 * (256 + 16)
+    for bad in ((0, 1, 1, 2), (1, 0, 1, 2), (1, 1, 0, 2), (1, 1, 1025, 2), (1, 1, 8, 1), (1, 1, 8, 4), (-1, 1, 8, 2), (1 << 16, 1 << 16, 8, 2)):
+        assert L.sinkhorn_cloud4_bytes(*bad) == 0
+        assert L.sinkhorn_cloud4_pack(one, 0, *bad, one, None, 0, None) == 2 and L.sinkhorn_operator_last_error()
+        assert L.sinkhorn_cloud4_unpack(one, *bad, one, 0, None) == 2
+    assert L.sinkhorn_cloud4_pack(None, 0, 1, 4, 8, 2, one, None, 0, None) == 1
+    assert L.sinkhorn_cloud4_pack(one, 0, 1, 4, 8, 2, None, None, 0, None) == 1
+    assert L.sinkhorn_cloud4_unpack(one, 1, 4, 8, 2, None, 0, None) == 1
+    assert L.sinkhorn_cloud4_pack(one, 2, 1, 4, 8, 2, one, None, 0, None) == 3
+    assert L.sinkhorn_cloud4_pack(one, 0, 1, 4, 8, 2, one, one, 5, None) == 3
+    assert L.sinkhorn_cloud4_pack(one, 0, 1, 4, 8, 2, ctypes.c_void_p(4096 + 16), None, 0, None) == 4
+    assert b"aligned" in L.sinkhorn_operator_last_error()
+    with pytest.raises(ValueError):
+        B.cloud4_pack(torch.zeros(2, 3, 4))                      # not on a GPU
+    with pytest.raises(ValueError):
+        B.Cloud4(torch.zeros(1024, dtype=torch.uint8), 1, 1, 8, "mx4")
+    with pytest.raises(ValueError):
+        B.Cloud4(torch.zeros(1024, dtype=torch.uint8), 1, 1, 2000, "mx4")
