@@ -435,6 +435,15 @@ skb_status sinkhorn_cloud4_pack(const void *v, int v_dtype, int W, int npts, int
                                 void *values, int values_dtype, void *stream);
 skb_status sinkhorn_cloud4_unpack(const void *cloud, int W, int npts, int d, int format, void *values, int values_dtype,
                                   void *stream);
+/*
+ * Products of two 4-bit clouds of the same format, out[t, i, j] = x_ti . y_tj of the values they stand for: x [W, n, d],
+ * y [W, m, d] buffers of sinkhorn_cloud4_pack, out [W, n, m] fp32.  The contraction of deep lanes' costs,
+ * |x_i|^2 + |y_j|^2 - 2 x_i . y_j, on the block-scaled tensor cores with fp32 accumulation.  A point that is NaN gives NaN
+ * in its row or column.  One kernel on `stream` of the current device; out is written 16 bytes at a time where
+ * m is a multiple of 4 and out 16-byte aligned.
+ */
+skb_status sinkhorn_cloud4_dots(const void *x, const void *y, int W, int n, int m, int d, int format, float *out,
+                                void *stream);
 
 /* Text of the calling thread's last failed sinkhorn_cloud4_* call (empty after a successful one). */
 const char *sinkhorn_operator_last_error(void);

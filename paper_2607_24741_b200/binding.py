@@ -35,7 +35,8 @@ EXPORTS = (
 PHASES = ("create", "f_leg", "column_check", "plan", "emit_move", "g_leg")
 # entry points outside the sinkhorn_batch_* family
 EXTRA_EXPORTS = ("sinkhorn_row_residual_static", "sinkhorn_row_residual_static_last_error",
-                 "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_operator_last_error")
+                 "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_cloud4_dots",
+                 "sinkhorn_operator_last_error")
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 FORMATS = {"mx4": 2, "nv4": 3}
 
@@ -105,6 +106,7 @@ def _load():
     lib.sinkhorn_cloud4_bytes.argtypes = [ci, ci, ci, ci]
     lib.sinkhorn_cloud4_pack.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, ci, vp]
     lib.sinkhorn_cloud4_unpack.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp]
+    lib.sinkhorn_cloud4_dots.argtypes = [vp, vp, ci, ci, ci, ci, ci, vp, vp]
     lib.sinkhorn_operator_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("sinkhorn_batch_workspace_bytes", "sinkhorn_batch_host_workspace_bytes",
@@ -261,6 +263,23 @@ def cloud4_pack(v, format="mx4", values=None, stream=None):
                                            DTYPES.get(values, 0), _stream(v.device, stream)))
     cloud = Cloud4(buffer, W, npts, d, format)
     return cloud if values is None else (cloud, out)
+
+
+def cloud4_dots(x, y, out=None, stream=None):
+    """x_ti . y_tj of two Cloud4 of one format, [W, n, d] and [W, m, d]: float32 [W, n, m]."""
+    if not isinstance(x, Cloud4) or not isinstance(y, Cloud4):
+        raise ValueError("x and y must be Cloud4")
+    if x.format != y.format or x.W != y.W or x.d != y.d or x.device != y.device:
+        raise ValueError("x and y must have one format, W, d and device")
+    shape = (x.W, x.npts, y.npts)
+    if out is not None and (out.dtype != torch.float32 or out.device != x.device or tuple(out.shape) != shape or not out.is_contiguous()):
+        raise ValueError("out must be a contiguous float32 tensor [W, n, m] on the clouds' device")
+    with torch.cuda.device(x.device):
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=x.device)
+        _check_op(lib.sinkhorn_cloud4_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, FORMATS[x.format], _ptr(out),
+                                           _stream(x.device, stream)))
+    return out
 
 
 class SinkhornBatch:

@@ -1,0 +1,384 @@
+// Products of two clouds, out[t, i, j] = x_ti . y_tj in fp32: 4-bit clouds by the block-scaled matrix instructions
+// (mx4: kind::mxf4, scales of 32 dimensions; nv4: kind::mxf4nvf4, scales of 16), bf16 clouds by kind::f16.
+//
+// The operands are small (a point of 512 dimensions in 4 bits is 272 bytes) and the result is not: 4 n m bytes a lane
+// bound the kernel (64 lanes of 1024 x 1024: 268 MB, 41 us at the measured copy rate; the 69 GFLOP would take 11 us at
+// four times the bf16 rate).  So the kernel is one persistent block an SM that always has a tile of results on its way out:
+//   warp 0     loads, by TMA: chunks of 128 bytes a point (256 dimensions in 4 bits, 64 in bf16), 128 points of x and of y,
+//              128-byte swizzle; points and dimensions past the end arrive as zeros
+//   warp 1     matrix instructions, one thread: four to a chunk into one of two accumulators of 128 x 128 in tensor memory
+//   warps 2-5  block scales (4-bit kinds): from the points' rows into the order that the matrix unit wants, through
+//              shared memory; they are a sixteenth of the codes and their rows too short for TMA.  Two warps to an operand, each
+//              takes every other chunk, so that a chunk's load latency has two chunks' time
+//   warps 6-9  results: tensor memory -> registers -> 32 x 32 boxes in shared memory -> TMA stores, which clip ragged edges.
+//              Rows that are no whole number of 16 bytes are stored by the threads, a warp to a row
+// In nv4 the points' powers of two multiply the results on their way out, which is exact.
+// Accumulation is the matrix unit's fp32.  Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and
+// the tiles that were not finished are NaN.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <string>
+
+#include "skb_cloud4.cuh"
+#include "skb_operators.h"
+#include "skb_tmem.cuh"
+
+namespace skb {
+namespace {
+
+constexpr int DT_BM = 128, DT_BN = 128;
+constexpr int DT_THREADS = 320, DT_STAGES = 4;
+constexpr uint32_t DT_TILE = 128 * 128;                  // bytes: 128 points, 128 bytes of each
+constexpr uint32_t DT_BOX = 32 * 32 * 4;                 // a box of results
+constexpr int DT_SF_COL = 2 * DT_BN, DT_SF_STRIDE = 32;  // tensor memory: accumulators, then the scales of each stage
+
+struct Dots {
+    const uint8_t *sx, *sy;                               // scales (4-bit kinds)
+    const float *px, *py;                                 // points' powers of two (nv4)
+    float *out;
+    long long ldo, lane_out;                              // floats from row to row, from lane to lane
+    int W, n, m, row_bytes, sb;                           // row_bytes: of a point's codes (or bf16 values)
+    int tma_out;
+};
+
+template <int KIND>
+__device__ __forceinline__ constexpr uint32_t dots_idesc()
+{
+    constexpr uint32_t shape = ((uint32_t)(DT_BN >> 3) << 17) | ((uint32_t)(DT_BM >> 4) << 24);
+    if (KIND == SKB_BF16) return (1u << 4) | (1u << 7) | (1u << 10) | shape;             // D fp32, A and B bf16
+    return (1u << 7) | (1u << 10) | shape | (KIND == SKB_MX4 ? 1u << 23 : 0u);           // A and B e2m1; scales e8m0 or e4m3
+}
+template <int KIND>
+__device__ __forceinline__ void dots_mma(uint32_t acc, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    if constexpr (KIND == SKB_BF16) tc_mma(acc, a, b, idesc, accumulate);
+    else if constexpr (KIND == SKB_MX4)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+}
+// 128 points' words of four scales, 512 bytes of shared memory, into four columns of tensor memory, the same for all four
+// quarters of the lanes.  Rows of 16 bytes, eight to a group of 128 bytes, no swizzle.
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr)
+{
+    const uint64_t desc = (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128u >> 4) << 32) | (1ull << 46);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void tma_load_points(uint32_t dst, const CUtensorMap *tm, int byte, int point, int lane, uint32_t mbar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(byte), "r"(point), "r"(lane), "r"(mbar) : "memory");
+}
+__device__ __forceinline__ void tma_store_box(const CUtensorMap *tm, uint32_t src, int col, int row, int lane)
+{
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(reinterpret_cast<uint64_t>(tm)), "r"(col), "r"(row), "r"(lane), "r"(src) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+
+template <int KIND>
+__global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmy,
+                                                             const __grid_constant__ CUtensorMap tmo, const Dots P)
+{
+    constexpr bool SCALED = KIND != SKB_BF16;
+    constexpr int WORDS = KIND == SKB_NV4 ? 4 : 2;               // words of scales that a point has in a chunk
+    constexpr uint32_t SF = SCALED ? WORDS * 512 : 0;            // bytes of an operand's scales in a stage
+    extern __shared__ __align__(1024) unsigned char smem_dyn[];
+    __shared__ __align__(8) unsigned long long bars[3 * DT_STAGES + 5];
+    __shared__ __align__(16) float col_points[2][DT_BN];     // read 16 bytes at a time
+    __shared__ uint32_t tmem_holder;
+    __shared__ int abort_flag;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+    unsigned char *gen = smem_dyn + (base - smem_u32(smem_dyn));
+    // operand tiles of all stages, then boxes of results (both want 1024 bytes), then scales
+    auto tile_a = [&](int s) { return base + (uint32_t)s * 2 * DT_TILE; };
+    const uint32_t boxes = base + DT_STAGES * 2 * DT_TILE, sfs = boxes + 8 * DT_BOX;
+    auto sf_a = [&](int s) { return sfs + (uint32_t)s * 2 * SF; };
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    constexpr int FULL = 0, EMPTY = DT_STAGES, SCALES = 2 * DT_STAGES, ACC = 3 * DT_STAGES, ACC_FREE = ACC + 2, LAST = ACC + 4;
+    if (tid == 0) {
+        for (int s = 0; s < DT_STAGES; ++s) {
+            mbar_init(bar(FULL + s), 1);
+            mbar_init(bar(EMPTY + s), 1);
+            mbar_init(bar(SCALES + s), 2);
+        }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar(ACC + b), 1); mbar_init(bar(ACC_FREE + b), 4); }
+        mbar_init(bar(LAST), 1);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tc_alloc<512>(&tmem_holder);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_holder;
+
+    const int nrt = (P.n + DT_BM - 1) / DT_BM, nct = (P.m + DT_BN - 1) / DT_BN;
+    const long long tiles = (long long)P.W * nrt * nct;
+    const int chunks = (P.row_bytes + 127) / 128;
+    auto where = [&](long long t, int &w, int &i0, int &j0) {
+        const int per_lane = nrt * nct, r = (int)(t % per_lane);
+        w = (int)(t / per_lane);
+        i0 = r / nct * DT_BM;
+        j0 = r % nct * DT_BN;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int s = 0, ph = 1;
+            unsigned issued = 0;                                  // stages with a load that may still be on its way
+            bool ok = true;
+            for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+                int w, i0, j0;
+                where(t, w, i0, j0);
+                for (int c = 0; c < chunks; ++c) {
+                    if (!(ok = mbar_wait(bar(EMPTY + s), ph, &abort_flag))) break;
+                    mbar_expect_tx(bar(FULL + s), 2 * DT_TILE);
+                    tma_load_points(tile_a(s), &tmx, c * 128, i0, w, bar(FULL + s));
+                    tma_load_points(tile_a(s) + DT_TILE, &tmy, c * 128, j0, w, bar(FULL + s));
+                    issued = (issued & ~(1u << (s + 16))) | (1u << s) | ((unsigned)(ph ^ 1) << (s + 16));
+                    if (++s == DT_STAGES) { s = 0; ph ^= 1; }
+                }
+            }
+            // nothing may land in shared memory after the block has gone: the last load of every stage, with a bound of its own
+            int unused = 0;
+            for (int q = 0; q < DT_STAGES; ++q)
+                if (issued >> q & 1u) mbar_wait(bar(FULL + q), issued >> (q + 16) & 1u, &unused);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int s = 0, ph = 0, b = 0, bph = 1;
+            bool ok = true;
+            for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+                if (!(ok = mbar_wait(bar(ACC_FREE + b), bph, &abort_flag))) break;
+                tc_fence_after();
+                const uint32_t acc = tmem + b * DT_BN;
+                for (int c = 0; c < chunks; ++c) {
+                    if (!(ok = mbar_wait(bar(FULL + s), ph, &abort_flag))) break;
+                    const uint32_t sf = tmem + DT_SF_COL + s * DT_SF_STRIDE;
+                    if constexpr (SCALED) {
+                        if (!(ok = mbar_wait(bar(SCALES + s), ph, &abort_flag))) break;
+                        tc_fence_after();
+#pragma unroll
+                        for (int q = 0; q < WORDS; ++q) {
+                            scales_to_tmem(sf + 4 * q, sf_a(s) + 512 * q);
+                            scales_to_tmem(sf + 16 + 4 * q, sf_a(s) + SF + 512 * q);
+                        }
+                    } else tc_fence_after();
+                    const uint64_t da = tc_desc(tile_a(s)), db = tc_desc(tile_a(s) + DT_TILE);
+                    const int left = P.row_bytes - c * 128;       // 32 bytes of a point to an instruction
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (32 * q >= left) break;
+                        const int word = KIND == SKB_NV4 ? q : q / 2;
+                        const uint32_t half = KIND == SKB_MX4 ? (uint32_t)(q & 1) * 2u : 0u;     // which two of a word's four scales
+                        dots_mma<KIND>(acc, da + 2 * q, db + 2 * q, dots_idesc<KIND>() | half << 29 | half << 4, sf + 4 * word, sf + 16 + 4 * word,
+                                       (c | q) != 0);
+                    }
+                    tc_commit(bar(EMPTY + s));
+                    if (++s == DT_STAGES) { s = 0; ph ^= 1; }
+                }
+                if (!ok) break;
+                tc_commit(bar(ACC + b));
+                b ^= 1;
+                if (b == 0) bph ^= 1;
+            }
+            // what was issued is over before tensor memory is given back
+            tc_commit(bar(LAST));
+            int unused = 0;
+            mbar_wait(bar(LAST), 0, &unused);
+        }
+    } else if (warp < 6) {
+        if constexpr (SCALED) {
+            const int op = (warp - 2) & 1, turn = (warp - 2) >> 1;     // operand; every other chunk
+            const uint8_t *src = op ? P.sy : P.sx;
+            const int npts = op ? P.m : P.n, words = P.sb / 4;
+            long long k = 0;                                          // chunks so far
+            bool ok = true;
+            for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+                int w, i0, j0;
+                where(t, w, i0, j0);
+                const int p0 = op ? j0 : i0;
+                for (int c = 0; c < chunks; ++c, ++k) {
+                    if ((int)(k & 1) != turn) continue;
+                    uint32_t v[4][WORDS];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int p = p0 + lane + 32 * q;
+                        const uint32_t *row = reinterpret_cast<const uint32_t *>(src + ((size_t)w * npts + min(p, npts - 1)) * P.sb);
+#pragma unroll
+                        for (int a = 0; a < WORDS; ++a) v[q][a] = p < npts && c * WORDS + a < words ? __ldg(row + c * WORDS + a) : 0u;
+                    }
+                    const int s = (int)(k % DT_STAGES);
+                    ok = mbar_wait(bar(EMPTY + s), (uint32_t)((k / DT_STAGES) & 1) ^ 1u, &abort_flag);
+                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                    // a word of scales of 128 points: row l of 32 holds the words of points l, l + 32, l + 64, l + 96
+                    uint4 *dst = reinterpret_cast<uint4 *>(gen + (sf_a(s) - base) + op * SF) + lane;
+#pragma unroll
+                    for (int a = 0; a < WORDS; ++a) dst[32 * a] = make_uint4(v[0][a], v[1][a], v[2][a], v[3][a]);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(SCALES + s));
+                }
+            }
+        }
+    } else {
+        const int quarter = warp & 3, e = (warp - 6) * 32 + lane;     // the lanes of tensor memory that this warp may read
+        const uint32_t box0 = boxes + (uint32_t)(warp - 6) * 2 * DT_BOX;
+        unsigned char *gbox0 = gen + (box0 - base);
+        int b = 0, ph = 0, turn = 0;
+        bool ok = true;
+        for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
+            int w, i0, j0;
+            where(t, w, i0, j0);
+            const int row = i0 + quarter * 32 + lane;
+            float rp = 1.f;
+            if constexpr (KIND == SKB_NV4) {
+                // (the buffer of two tiles ago: its readers have passed the barrier of the last tile)
+                col_points[b][e] = j0 + e < P.m ? P.py[(size_t)w * P.m + j0 + e] : 0.f;
+                rp = row < P.n ? P.px[(size_t)w * P.n + row] : 0.f;
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+            }
+            ok = ok && mbar_wait(bar(ACC + b), ph, &abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            for (int c0 = 0; c0 < DT_BN; c0 += 32) {
+                if (j0 + c0 >= P.m) break;
+                uint32_t r[32];
+                if (ok) {
+                    tc_ld32_issue(tmem + (uint32_t)(quarter << 21) + b * DT_BN + c0, r);
+                    tc_ld_wait(r);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 32; ++q) r[q] = 0x7fffffffu;
+                }
+                if constexpr (KIND == SKB_NV4) {
+#pragma unroll
+                    for (int q = 0; q < 32; q += 4) {
+                        const float4 p = *reinterpret_cast<const float4 *>(&col_points[b][c0 + q]);
+                        r[q] = __float_as_uint(__uint_as_float(r[q]) * rp * p.x);
+                        r[q + 1] = __float_as_uint(__uint_as_float(r[q + 1]) * rp * p.y);
+                        r[q + 2] = __float_as_uint(__uint_as_float(r[q + 2]) * rp * p.z);
+                        r[q + 3] = __float_as_uint(__uint_as_float(r[q + 3]) * rp * p.w);
+                    }
+                }
+                // the store before the last one has read its box
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                __syncwarp();
+                unsigned char *box = gbox0 + turn * DT_BOX;
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    *reinterpret_cast<uint4 *>(box + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+                if (P.tma_out) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && i0 + quarter * 32 < P.n) tma_store_box(&tmo, box0 + turn * DT_BOX, j0 + c0, i0 + quarter * 32, w);
+                } else {
+                    __syncwarp();
+                    const int rows = min(32, P.n - (i0 + quarter * 32));
+                    float *dst = P.out + (size_t)w * P.lane_out + (size_t)(i0 + quarter * 32) * P.ldo + j0 + c0 + lane;
+                    if (j0 + c0 + lane < P.m)
+                        for (int q = 0; q < rows; ++q)
+                            dst[(size_t)q * P.ldo] = *reinterpret_cast<const float *>(box + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
+                    __syncwarp();
+                }
+                turn ^= 1;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(ACC_FREE + b));
+            b ^= 1;
+            if (b == 0) ph ^= 1;
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) tc_dealloc<512>(tmem);
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encoder()
+{
+    static const EncodeTiledFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess ? (EncodeTiledFn)p : (EncodeTiledFn) nullptr;
+    }();
+    return fn;
+}
+bool make_map(CUtensorMap *tm, CUtensorMapDataType type, const void *base, cuuint64_t inner, cuuint64_t rows, cuuint64_t W, cuuint64_t pitch,
+              cuuint64_t lane_pitch, cuuint32_t box_inner, cuuint32_t box_rows)
+{
+    const cuuint64_t dims[3] = {inner, rows, W}, strides[2] = {pitch, lane_pitch};
+    const cuuint32_t box[3] = {box_inner, box_rows, 1}, step[3] = {1, 1, 1};
+    return encoder()(tm, type, 3, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                     CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int KIND>
+skb_status launch_kind(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &to, const Dots &P, int sms, cudaStream_t st)
+{
+    constexpr int sf = KIND == SKB_BF16 ? 0 : KIND == SKB_NV4 ? 2048 : 1024;
+    constexpr int smem = DT_STAGES * (2 * (int)DT_TILE + 2 * sf) + 8 * (int)DT_BOX + 1024;
+    cudaFuncSetAttribute(dots_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const long long tiles = (long long)P.W * ((P.n + DT_BM - 1) / DT_BM) * ((P.m + DT_BN - 1) / DT_BN);
+    dots_kernel<KIND><<<(unsigned)(tiles < sms ? tiles : sms), DT_THREADS, smem, st>>>(tx, ty, to, P);
+    return op_launched("products");
+}
+
+}  // namespace
+
+// Clouds of type `dtype` (bf16: d a multiple of 8, both 16-byte aligned), rows of ldo >= m floats, n rows to a lane.
+skb_status launch_dots(int dtype, const void *x, const void *y, int W, int n, int m, int d, float *out, long long ldo, cudaStream_t st)
+{
+    if (!encoder()) return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");
+    Dots P = {};
+    P.out = out; P.ldo = ldo; P.lane_out = ldo * n;
+    P.W = W; P.n = n; P.m = m;
+    const void *cx = x, *cy = y;
+    if (dtype == SKB_BF16) P.row_bytes = 2 * d;
+    else {
+        const Cloud4 a = cloud4_view(x, (size_t)W * n, d, dtype), b = cloud4_view(y, (size_t)W * m, d, dtype);
+        P.sx = a.scales; P.sy = b.scales; P.px = a.points; P.py = b.points;
+        P.row_bytes = a.cb; P.sb = a.sb;
+        cx = a.codes; cy = b.codes;
+    }
+    P.tma_out = ldo % 4 == 0 && (uintptr_t)out % 16 == 0;
+    CUtensorMap tx, ty, to = {};
+    const size_t rb = P.row_bytes;
+    if (!make_map(&tx, CU_TENSOR_MAP_DATA_TYPE_UINT8, cx, rb, n, W, rb, rb * n, 128, DT_BM) ||
+        !make_map(&ty, CU_TENSOR_MAP_DATA_TYPE_UINT8, cy, rb, m, W, rb, rb * m, 128, DT_BN) ||
+        (P.tma_out && !make_map(&to, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, out, m, n, W, ldo * 4, ldo * 4 * n, 32, 32)))
+        return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    if (dtype == SKB_BF16) return launch_kind<SKB_BF16>(tx, ty, to, P, sms, st);
+    if (dtype == SKB_MX4) return launch_kind<SKB_MX4>(tx, ty, to, P, sms, st);
+    return launch_kind<SKB_NV4>(tx, ty, to, P, sms, st);
+}
+
+}  // namespace skb
+
+using namespace skb;
+
+extern "C" skb_status sinkhorn_cloud4_dots(const void *x, const void *y, int W, int n, int m, int d, int format, float *out, void *stream)
+{
+    if (!x || !y || !out) return op_fail(SKB_ERR_NULL, "x, y and out are required");
+    if (const char *why = cloud4_refused(W, n, d, format)) return op_fail(SKB_ERR_SHAPE, why);
+    if (const char *why = cloud4_refused(W, m, d, format)) return op_fail(SKB_ERR_SHAPE, why);
+    if ((uintptr_t)x % 256 || (uintptr_t)y % 256) return op_fail(SKB_ERR_WORKSPACE, "x and y must be 256-byte aligned");
+    if ((uintptr_t)out % 4) return op_fail(SKB_ERR_WORKSPACE, "out must be 4-byte aligned");
+    return launch_dots(format, x, y, W, n, m, d, out, m, (cudaStream_t)stream);
+}

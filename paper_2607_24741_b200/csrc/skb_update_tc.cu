@@ -41,41 +41,7 @@ constexpr int TC_THREADS = TC_EPI_THREADS + 64;            // + producer warp + 
 constexpr int TC_MAX_STAGES = 4;
 constexpr int TC_BM = 128, TC_BK = 64;
 constexpr uint32_t TC_CHUNK = TC_BM * TC_BK * 2;          // 16 KB: 128 points x 64 bf16
-constexpr long long TC_WAIT_CLOCKS = 2000000000LL;        // ~1 s: budget of every bounded wait of the update kernels
 
-__device__ __forceinline__ void mbar_init(uint32_t a, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(a), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t a)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(a) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t a, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(a), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t a, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(ok) : "r"(a), "r"(parity) : "memory");
-    return ok != 0;
-}
-// Bounded wait: false if the budget ran out or another role already gave up.
-// The budget is an argument (the update kernels use the constant, the self-test its own short one):
-// a writable global would let a self-test on one stream shorten the waits of a solve on another.
-__device__ __forceinline__ bool mbar_wait(uint32_t a, uint32_t parity, volatile int *abort_flag,
-                                          const long long budget = TC_WAIT_CLOCKS)
-{
-    if (mbar_try_wait(a, parity)) return true;          // the common case costs no clock read
-    const long long t0 = clock64();
-    while (!mbar_try_wait(a, parity)) {
-        if (*abort_flag) return false;
-        if (clock64() - t0 > budget) { *abort_flag = 1; return false; }
-    }
-    return true;
-}
 // one pre-tiled chunk (128 points x 64 bf16, contiguous 16 KB in global memory) -> shared memory
 #ifdef SKB_TC_DEBUG
 #define TC_TIMED_WAIT(acc, call) ({ const long long _t = clock64(); const bool _r = (call); (acc) += clock64() - _t; _r; })
@@ -86,15 +52,6 @@ __device__ __forceinline__ void tma_load_chunk(uint32_t dst, const CUtensorMap *
 {
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(0), "r"(row), "r"(mbar) : "memory");
-}
-__device__ __forceinline__ void tc_commit(uint32_t mbar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(mbar) : "memory");
-}
-__device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
 // Online max / sum-of-exp2 over one 32-column chunk of a row: arg = 2 s S + ct_j, computed
 // on column pairs with packed fp32 instructions.  The running reference mx is NOT updated on
@@ -199,12 +156,6 @@ __device__ __forceinline__ void tc_merge_halves(const int e, const float mx, con
         row_s[row] = ok ? sd * (double)pow2i(mx - mn) + so * (double)pow2i(mo - mn) : __longlong_as_double(0x7ff8000000000000LL);
         row_h[row] = 0.f;
     }
-}
-// shared-memory matrix descriptor: K-major tile, rows of 64 bf16 (128 B), 128-byte swizzle,
-// 8-row groups 1024 B apart
-__device__ __forceinline__ uint64_t tc_desc(uint32_t saddr)
-{
-    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 // instruction descriptor: D fp32, A and B bf16, both K-major, M = 128, N = 128
 __host__ __device__ constexpr uint32_t tc_idesc(int bn) { return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(bn >> 3) << 17) | ((uint32_t)(TC_BM >> 4) << 24); }

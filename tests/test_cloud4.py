@@ -236,3 +236,112 @@ def test_refusals_of_pack_and_unpack(B):
         B.Cloud4(torch.zeros(1024, dtype=torch.uint8), 1, 1, 8, "mx4")
     with pytest.raises(ValueError):
         B.Cloud4(torch.zeros(1024, dtype=torch.uint8), 1, 1, 2000, "mx4")
+
+
+# ---- products
+
+def exact_dots(x, y):
+    """Float64 products of two Cloud4, and the sum of their terms' magnitudes."""
+    import torch
+    a, b = x.values().double(), y.values().double().transpose(1, 2)
+    return torch.bmm(a, b), torch.bmm(a.abs(), b.abs())
+
+
+def check_dots(B, x4, y4, out):
+    # A matrix instruction adds 64 exact products to an fp32 accumulator.  Each is allowed two units in the last place of the
+    # largest sum that can occur, the sum of the magnitudes; the powers of two of nv4 change nothing.
+    import torch
+    want, size = exact_dots(x4, y4)
+    steps = -(-x4.d // 64)
+    err = (out.double() - want).abs()
+    assert bool((err <= steps * 2.0 ** -22 * size + 1e-300).all()), float((err / (size + 1e-300)).max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (1, 128, 128, 64), (1, 128, 128, 256), (2, 128, 256, 512), (3, 37, 45, 20), (1, 129, 257, 96), (2, 300, 130, 200),
+                                   (5, 64, 33, 333), (2, 200, 100, 640), (1, 260, 516, 1024), (7, 1, 300, 48), (7, 300, 1, 48), (40, 130, 129, 160)])
+def test_products_of_every_shape(B, fmt, shape):
+    import torch
+    W, n, m, d = shape
+    gen = torch.Generator().manual_seed(sum(shape))
+    x = (torch.randn(W, n, d, generator=gen) * torch.exp(torch.randn(W, n, 1, generator=gen))).cuda()
+    y = (torch.randn(W, m, d, generator=gen) * torch.exp(torch.randn(W, m, d, generator=gen))).cuda()
+    x4, y4 = B.cloud4_pack(x, fmt), B.cloud4_pack(y, fmt)
+    # a result behind guards: rows past the last are left alone
+    room = torch.full((W * n * m + 256,), -7.0, device="cuda")
+    for at in (64, 65):                                          # 16-byte aligned, and not
+        room.fill_(-7.0)
+        out = room[at:at + W * n * m].view(W, n, m)
+        B.cloud4_dots(x4, y4, out=out)
+        check_dots(B, x4, y4, out)
+        assert bool((room[:at] == -7.0).all()) and bool((room[at + W * n * m:] == -7.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+def test_products_are_exact_where_sums_are_small_integers(B, fmt):
+    # every value a grid value with scale one or two: all sums are exact in fp32, so a scale or a code in the wrong place shows
+    import torch
+    gen = torch.Generator().manual_seed(11)
+    grid = torch.tensor(list(GRID) + list(-GRID), dtype=torch.float32)
+    for d in (64, 128, 192, 256, 500, 1024):
+        x, y = grid[torch.randint(16, (2, 150, d), generator=gen)], grid[torch.randint(16, (2, 140, d), generator=gen)]
+        x[:, :, ::16] = 6.0
+        y[:, :, ::16] = 6.0
+        x[:, :, : d // 2] *= 2.0
+        y[:, 70:, :] *= 0.25
+        x4, y4 = B.cloud4_pack(x.cuda(), fmt), B.cloud4_pack(y.cuda(), fmt)
+        want, _ = exact_dots(x4, y4)
+        assert torch.equal(B.cloud4_dots(x4, y4).double(), want), d
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+def test_a_nan_point_gives_nan_in_its_row_and_column_only(B, fmt):
+    import torch
+    x, y = torch.randn(2, 140, 200).cuda(), torch.randn(2, 133, 200).cuda()
+    x[1, 130, 199] = float("inf")
+    y[0, 132, 0] = float("nan")
+    x[0, 7] = 0.0
+    out = B.cloud4_dots(B.cloud4_pack(x, fmt), B.cloud4_pack(y, fmt))
+    bad = torch.zeros_like(out, dtype=torch.bool)
+    bad[1, 130] = True
+    bad[0, :, 132] = True
+    assert torch.equal(torch.isnan(out), bad)
+    assert bool((out[0, 7, :132] == 0).all())
+
+
+@pytest.mark.gpu
+def test_products_repeat_bit_for_bit_and_replay_from_a_graph(B):
+    import torch
+    x4, y4 = B.cloud4_pack(torch.randn(30, 200, 320).cuda(), "nv4"), B.cloud4_pack(torch.randn(30, 260, 320).cuda(), "nv4")
+    first = B.cloud4_dots(x4, y4)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = B.cloud4_dots(x4, y4)                            # at the same time as the next
+    again = B.cloud4_dots(x4, y4)
+    torch.cuda.synchronize()
+    assert torch.equal(first, again) and torch.equal(first, other)
+    out = torch.empty_like(first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.cloud4_dots(x4, y4, out=out)
+    y4.buffer.copy_(B.cloud4_pack(torch.randn(30, 260, 320).cuda(), "nv4").buffer)
+    graph.replay()
+    assert torch.equal(out, B.cloud4_dots(x4, y4)) and not torch.equal(out, first)
+
+
+def test_refusals_of_products(B):
+    import ctypes
+    L, one = B.lib, ctypes.c_void_p(4096)
+    assert L.sinkhorn_cloud4_dots(None, one, 1, 4, 4, 8, 2, one, None) == 1
+    assert L.sinkhorn_cloud4_dots(one, None, 1, 4, 4, 8, 2, one, None) == 1
+    assert L.sinkhorn_cloud4_dots(one, one, 1, 4, 4, 8, 2, None, None) == 1
+    for bad in ((0, 4, 4, 8, 2), (1, 0, 4, 8, 2), (1, 4, 0, 8, 2), (1, 4, 4, 0, 3), (1, 4, 4, 1025, 3), (1, 4, 4, 8, 0), (1, 4, 4, 8, 1)):
+        assert L.sinkhorn_cloud4_dots(one, one, *bad, one, None) == 2
+    assert L.sinkhorn_cloud4_dots(ctypes.c_void_p(4096 + 16), one, 1, 4, 4, 8, 2, one, None) == 4
+    assert L.sinkhorn_cloud4_dots(one, one, 1, 4, 4, 8, 2, ctypes.c_void_p(4098), None) == 4
+    with pytest.raises(ValueError):
+        B.cloud4_dots(None, None)
