@@ -444,8 +444,45 @@ skb_status sinkhorn_cloud4_unpack(const void *cloud, int W, int npts, int d, int
  */
 skb_status sinkhorn_cloud4_dots(const void *x, const void *y, int W, int n, int m, int d, int format, float *out,
                                 void *stream);
+/*
+ * Partners drawn from the rows of a coupling, from random numbers that the caller gives: training pairs, hypotheses for
+ * correspondences.  Row i of lane t is the distribution over the targets j with weights
+ *      w_ij = exp((g_j - |x_i - y_j|^2) / (eps T) - the largest of them),
+ * the plan's row i, normalised, where T = 1 (the row's own potential f_i drops out); sharper below, flatter above.  For
+ * partners of the targets exchange x and y and give f.  g_j = -inf masks a target whatever its coordinates hold.
+ * Settings by lane, device arrays [W] that may each be null:
+ *   temperature  fp32, T >= 0; 0: the largest weight alone (at T = 1)           null: 1
+ *   top_k        int, the k largest weights, 0: all                             null: 0
+ *   top_p        fp32, the shortest head of the weights in falling order whose sum is >= top_p times the sum of what
+ *                top_k left, at least one; 1 and more: all                      null: 1
+ *   min_p        fp32 in [0, 1], of what is left the weights >= min_p           null: 0
+ * Equal weights are in the order of their indices.  For each of the `draws` numbers u [W, n, draws] in [0, 1) of a row,
+ *   index [W, n, draws]  the smallest j whose kept weights up to and with j sum to more than u times all kept weights
+ *   logp  [W, n, draws]  fp32, may be null: log(w_ij / sum of the kept weights)
+ * Indices are those of float64 arithmetic (rows that fp32 cannot decide are decided again).  -1, and NaN for logp: a
+ * row without targets, with a NaN or an infinite exponent; a u outside [0, 1); every row of a lane whose settings or eps are not valid.
+ *   x [W, n, d], y [W, m, d]  of cfg->xy_dtype (4-bit clouds: the values they stand for), 16-byte aligned, 4-bit clouds 256
+ *   g [W, m] float64, eps [W] fp32, device
+ * d <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on cfg->stream of the current device and returns; the workspace (device,
+ * 256-byte aligned) is in use until they are done: calls that may overlap need one each.
+ */
+typedef struct {
+    int W, n, m, d;
+    int xy_dtype;              /* skb_dtype */
+    int draws;                 /* numbers, and so draws, per row, >= 1 */
+    const float *temperature;
+    const int *top_k;
+    const float *top_p;
+    const float *min_p;
+    void *stream;              /* cudaStream_t (0 = legacy default stream) */
+    void *workspace;
+    size_t workspace_bytes;
+} skb_draw_config;
+size_t sinkhorn_plan_draw_workspace_bytes(const skb_draw_config *cfg);     /* 0: a bad shape or type */
+skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u,
+                              const skb_draw_config *cfg, int *index, float *logp);
 
-/* Text of the calling thread's last failed sinkhorn_cloud4_* call (empty after a successful one). */
+/* Text of the calling thread's last failed sinkhorn_cloud4_* or sinkhorn_plan_draw call (empty after a successful one). */
 const char *sinkhorn_operator_last_error(void);
 
 /* Host string describing the last error on this handle (or, when h is null, of the calling

@@ -35,7 +35,7 @@ EXPORTS = (
 PHASES = ("create", "f_leg", "column_check", "plan", "emit_move", "g_leg")
 # entry points outside the sinkhorn_batch_* family
 EXTRA_EXPORTS = ("sinkhorn_row_residual_static", "sinkhorn_row_residual_static_last_error",
-                 "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_cloud4_dots",
+                 "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_cloud4_dots", "sinkhorn_plan_draw_workspace_bytes", "sinkhorn_plan_draw",
                  "sinkhorn_operator_last_error")
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 FORMATS = {"mx4": 2, "nv4": 3}
@@ -50,6 +50,14 @@ class SkbConfig(ctypes.Structure):
                 ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t), ("guard_band", ctypes.c_float),
                 ("lane_capacity", ctypes.c_int)]
+
+
+class SkbDrawConfig(ctypes.Structure):
+    _fields_ = [("W", ctypes.c_int), ("n", ctypes.c_int), ("m", ctypes.c_int), ("d", ctypes.c_int),
+                ("xy_dtype", ctypes.c_int), ("draws", ctypes.c_int),
+                ("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p), ("top_p", ctypes.c_void_p),
+                ("min_p", ctypes.c_void_p), ("stream", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 class SkbError(RuntimeError):
@@ -107,6 +115,10 @@ def _load():
     lib.sinkhorn_cloud4_pack.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, ci, vp]
     lib.sinkhorn_cloud4_unpack.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp]
     lib.sinkhorn_cloud4_dots.argtypes = [vp, vp, ci, ci, ci, ci, ci, vp, vp]
+    drawp = ctypes.POINTER(SkbDrawConfig)
+    lib.sinkhorn_plan_draw_workspace_bytes.restype = ctypes.c_size_t
+    lib.sinkhorn_plan_draw_workspace_bytes.argtypes = [drawp]
+    lib.sinkhorn_plan_draw.argtypes = [vp, vp, vp, vp, vp, drawp, vp, vp]
     lib.sinkhorn_operator_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("sinkhorn_batch_workspace_bytes", "sinkhorn_batch_host_workspace_bytes",
@@ -206,8 +218,9 @@ def _check_op(code):
         raise SkbError(code, lib.sinkhorn_operator_last_error().decode())
 
 
-def _stream(device, stream):
-    return (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
+# They run on the current stream of the tensors' device, and their outputs and workspaces belong to it.
+def _stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
 
 
 class Cloud4:
@@ -231,18 +244,18 @@ class Cloud4:
     def device(self):
         return self.buffer.device
 
-    def values(self, dtype=torch.float32, stream=None):
+    def values(self, dtype=torch.float32):
         """What the cloud stands for, [W, npts, d] float32 or bfloat16."""
         if dtype not in DTYPES:
             raise ValueError("dtype must be float32 or bfloat16")
         with torch.cuda.device(self.device):
             out = torch.empty(self.shape, dtype=dtype, device=self.device)
             _check_op(lib.sinkhorn_cloud4_unpack(_ptr(self.buffer), self.W, self.npts, self.d, FORMATS[self.format], _ptr(out),
-                                                 DTYPES[dtype], _stream(self.device, stream)))
+                                                 DTYPES[dtype], _stream(self.device)))
         return out
 
 
-def cloud4_pack(v, format="mx4", values=None, stream=None):
+def cloud4_pack(v, format="mx4", values=None):
     """Rounds v [W, npts, d] (float32 or bfloat16, CUDA) to 4 bits, format "mx4" or "nv4"; returns a Cloud4, or with
     `values` (torch.float32 or torch.bfloat16) the pair of it and the values that it stands for."""
     if v.dim() != 3 or not v.is_cuda or v.dtype not in DTYPES:
@@ -260,12 +273,12 @@ def cloud4_pack(v, format="mx4", values=None, stream=None):
         buffer = torch.empty(need, dtype=torch.uint8, device=v.device)
         out = None if values is None else torch.empty(v.shape, dtype=values, device=v.device)
         _check_op(lib.sinkhorn_cloud4_pack(_ptr(v), DTYPES[v.dtype], W, npts, d, FORMATS[format], _ptr(buffer), _ptr(out),
-                                           DTYPES.get(values, 0), _stream(v.device, stream)))
+                                           DTYPES.get(values, 0), _stream(v.device)))
     cloud = Cloud4(buffer, W, npts, d, format)
     return cloud if values is None else (cloud, out)
 
 
-def cloud4_dots(x, y, out=None, stream=None):
+def cloud4_dots(x, y, out=None):
     """x_ti . y_tj of two Cloud4 of one format, [W, n, d] and [W, m, d]: float32 [W, n, m]."""
     if not isinstance(x, Cloud4) or not isinstance(y, Cloud4):
         raise ValueError("x and y must be Cloud4")
@@ -278,8 +291,73 @@ def cloud4_dots(x, y, out=None, stream=None):
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=x.device)
         _check_op(lib.sinkhorn_cloud4_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, FORMATS[x.format], _ptr(out),
-                                           _stream(x.device, stream)))
+                                           _stream(x.device)))
     return out
+
+
+def _cloud(v, name):
+    """dtype, shape, pointer and the tensor to keep of a cloud: a tensor or a Cloud4."""
+    if isinstance(v, Cloud4):
+        return FORMATS[v.format], v.shape, v.buffer
+    if not torch.is_tensor(v) or not v.is_cuda or v.dim() != 3 or v.dtype not in DTYPES:
+        raise ValueError(f"{name} must be a float32 or bfloat16 CUDA tensor [W, points, d], or a Cloud4")
+    v = v.contiguous()
+    if v.data_ptr() % 16:
+        v = v.clone()
+    return DTYPES[v.dtype], tuple(v.shape), v
+
+
+def _draw_config(W, n, m, d, dtype, u, settings, stream):
+    """Configuration of a draw, with its settings checked; u [W, n] or [W, n, draws] is checked too."""
+    device = u.device
+    if not u.is_cuda or u.dtype != torch.float32 or u.dim() not in (2, 3) or tuple(u.shape[:2]) != (W, n):
+        raise ValueError("u must be a float32 CUDA tensor [W, n] or [W, n, draws]")
+    cfg = SkbDrawConfig(W, n, m, d, dtype, u.shape[2] if u.dim() == 3 else 1, stream=stream)
+    for name, t in settings.items():
+        if t is None:
+            continue
+        want = torch.int32 if name == "top_k" else torch.float32
+        if not torch.is_tensor(t) or t.dtype != want or t.device != device or tuple(t.shape) != (W,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {want} tensor [W] on the device of the clouds")
+        setattr(cfg, name, t.data_ptr())
+    return cfg
+
+
+def _draw_out(cfg, u, logp):
+    index = torch.empty(u.shape, dtype=torch.int32, device=u.device)
+    lp = torch.empty(u.shape, dtype=torch.float32, device=u.device) if logp else None
+    need = lib.sinkhorn_plan_draw_workspace_bytes(ctypes.byref(cfg))
+    if need == 0:
+        raise SkbError(2, "shape not supported: W, n, m, d, draws >= 1, d <= 1024, n and m <= 262143, W <= 65535")
+    ws = torch.empty(need, dtype=torch.uint8, device=u.device)
+    cfg.workspace, cfg.workspace_bytes = ws.data_ptr(), need
+    return index, lp, ws
+
+
+def plan_draw(x, y, g, eps, u, *, temperature=None, top_k=None, top_p=None, min_p=None, logp=False):
+    """Partners of x [W, n, d] among y [W, m, d] (tensors or Cloud4), drawn from the coupling's rows, softmax over j of
+    (g_j - |x_i - y_j|^2) / (eps T), one for each number of u [W, n] or [W, n, draws]; see sinkhorn_plan_draw in
+    the header.  Settings are tensors [W].  Returns the indices (int32, u's shape), with `logp` also their log
+    probabilities."""
+    dt, (W, n, d), xk = _cloud(x, "x")
+    dty, ys, yk = _cloud(y, "y")
+    m = ys[1]
+    if dty != dt or ys != (W, m, d):
+        raise ValueError("x and y must have one type, W and d")
+    device = xk.device
+    if yk.device != device or u.device != device:
+        raise ValueError("all tensors must be on one device")
+    if g.dtype != torch.float64 or g.device != device or tuple(g.shape) != (W, m):
+        raise ValueError("g must be a float64 tensor [W, m] on the device of the clouds")
+    if eps.dtype != torch.float32 or eps.device != device or tuple(eps.shape) != (W,):
+        raise ValueError("eps must be a float32 tensor [W] on the device of the clouds")
+    g, eps, u = g.contiguous(), eps.contiguous(), u.contiguous()
+    with torch.cuda.device(device):
+        cfg = _draw_config(W, n, m, d, dt, u, dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p),
+                           _stream(device))
+        index, lp, ws = _draw_out(cfg, u, logp)
+        _check_op(lib.sinkhorn_plan_draw(_ptr(xk), _ptr(yk), _ptr(g), _ptr(eps), _ptr(u), ctypes.byref(cfg), _ptr(index), _ptr(lp)))
+    return (index, lp) if logp else index
 
 
 class SinkhornBatch:

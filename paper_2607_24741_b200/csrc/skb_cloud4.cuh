@@ -42,15 +42,13 @@ inline Cloud4 cloud4_view(const void *buf, size_t rows, int d, int fmt)
 }
 
 #ifdef __CUDACC__
-// two e2m1 codes of a byte as floats (exact)
-__device__ __forceinline__ float2 e2m1_pair(uint32_t byte)
+// e2m1 codes as floats (exact): a code's exponent and mantissa are those of a float whose exponent counts from 126 less.
+__device__ __forceinline__ float e2m1_value(uint32_t code)
 {
-    uint32_t h;
-    asm("{\n\t.reg .b8 c, z1, z2, z3;\n\tmov.b32 {c, z1, z2, z3}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\t}" : "=r"(h) : "r"(byte));
-    float lo, hi;
-    asm("{\n\t.reg .f16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.f32.f16 %0, a;\n\tcvt.f32.f16 %1, b;\n\t}" : "=f"(lo), "=f"(hi) : "r"(h));
-    return make_float2(lo, hi);
+    return __uint_as_float((code & 7u) << 22 | (code & 8u) << 28) * 8.507059173023462e37f;
 }
+// the two of a byte
+__device__ __forceinline__ float2 e2m1_pair(uint32_t byte) { return make_float2(e2m1_value(byte), e2m1_value(byte >> 4)); }
 __device__ __forceinline__ float e8m0_value(uint32_t b)
 {
     return b == 255u ? __uint_as_float(0x7fffffffu) : b == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(b << 23);
@@ -71,8 +69,7 @@ __device__ __forceinline__ float cloud4_scale(const Cloud4 &c, size_t row, int k
 }
 __device__ __forceinline__ float cloud4_value(const Cloud4 &c, size_t row, int k)
 {
-    const float2 p = e2m1_pair(c.codes[row * c.cb + (k >> 1)]);
-    return ((k & 1) ? p.y : p.x) * cloud4_scale(c, row, k);
+    return e2m1_value((uint32_t)c.codes[row * c.cb + (k >> 1)] >> (4 * (k & 1))) * cloud4_scale(c, row, k);
 }
 #endif
 

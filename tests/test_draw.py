@@ -1,0 +1,278 @@
+"""Draws from the rows of a coupling: indices, log probabilities, masks, settings and refusals.
+
+The reference is the header's definition in float64 (numpy, distances by differences, one row at a time).  Indices have to be equal.
+logp: its error is that of the weights, of their sum and one rounding to fp32; the fp32 path of the kernel forms weights with
+a relative error below 1e-3 in every case here (rows it cannot decide go to float64), so |logp - reference| <= 1e-3 + 2^-23 |reference|."""
+import math
+
+import numpy as np
+import pytest
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2607_24741_b200 import build
+    build.build()
+    from paper_2607_24741_b200 import binding
+    return binding
+
+
+def row_reference(z, k, p, r, us):
+    """Indices and log probabilities of one row of exponents (natural units, -inf: masked)."""
+    m = len(z)
+    if np.isnan(z).any() or (z == np.inf).any() or (z == -np.inf).all():
+        return [-1] * len(us), [math.nan] * len(us)
+    w = np.exp(z - z.max())
+    order = np.lexsort((np.arange(m), -z))
+    keep = np.zeros(m, bool)
+    head = order[:k] if k > 0 else order
+    if p < 1.0:
+        cum = np.cumsum(w[head])
+        head = head[:1 + int((cum < p * cum[-1]).sum())]
+    keep[head] = True
+    keep &= (w >= r) & (w > 0)
+    cum = np.cumsum(np.where(keep, w, 0.0))
+    idx, lp = [], []
+    for u in us:
+        if not 0.0 <= u < 1.0:
+            idx.append(-1); lp.append(math.nan)
+            continue
+        j = int(np.searchsorted(cum, u * cum[-1], side="right"))
+        j = min(j, int(np.nonzero(keep)[0][-1]))
+        idx.append(j); lp.append(math.log(w[j] / cum[-1]))
+    return idx, lp
+
+
+def reference(x, y, g, eps, u, T=None, k=None, p=None, r=None):
+    W, n, S = u.shape
+    idx, lp = np.empty((W, n, S), np.int64), np.empty((W, n, S))
+    for t in range(W):
+        Tt, kt, pt, rt = 1.0 if T is None else float(T[t]), 0 if k is None else int(k[t]), 1.0 if p is None else float(p[t]), 0.0 if r is None else float(r[t])
+        if not (0 <= Tt < math.inf and kt >= 0 and pt > 0 and 0 <= rt <= 1 and 0 < float(eps[t]) < math.inf):
+            idx[t], lp[t] = -1, math.nan
+            continue
+        if Tt == 0:
+            Tt, kt = 1.0, 1
+        for i in range(n):
+            with np.errstate(all="ignore"):
+                c = ((x[t, i][None, :] - y[t]) ** 2).sum(1)
+                z = np.where(g[t] == -np.inf, -np.inf, (g[t] - c) / (float(eps[t]) * Tt))
+                idx[t, i], lp[t, i] = row_reference(z, kt, pt, rt, u[t, i])
+    return idx, lp
+
+
+def check(B, x, y, g, eps, u, T=None, k=None, p=None, r=None, fmt=None):
+    """x, y: CPU tensors of the storage type; the others numpy or None."""
+    import torch
+    dev = lambda v, dt: None if v is None else torch.as_tensor(np.asarray(v)).to(dt).cuda()
+    f32, i32 = torch.float32, torch.int32
+    xd, yd = x.cuda(), y.cuda()
+    xh, yh = x.double().numpy(), y.double().numpy()
+    if fmt is not None:
+        xd, yd = B.cloud4_pack(xd, fmt), B.cloud4_pack(yd, fmt)
+        xh, yh = xd.values().cpu().double().numpy(), yd.values().cpu().double().numpy()
+    if u.ndim == 2:
+        u = u[:, :, None]
+    u = np.asarray(u, np.float32)
+    eps = np.asarray(eps, np.float32)
+    T, p, r = (None if v is None else np.asarray(v, np.float32) for v in (T, p, r))
+    idx, lp = B.plan_draw(xd, yd, dev(g, torch.float64), dev(eps, f32), dev(u, f32), temperature=dev(T, f32), top_k=dev(k, i32),
+                          top_p=dev(p, f32), min_p=dev(r, f32), logp=True)
+    want, wlp = reference(xh, yh, np.asarray(g), eps, u.astype(np.float64), T, k, p, r)
+    idx, lp = idx.cpu().numpy(), lp.cpu().numpy()
+    np.testing.assert_array_equal(idx, want)
+    np.testing.assert_array_equal(np.isnan(lp), np.isnan(wlp))
+    fine = ~np.isnan(wlp)
+    assert (np.abs(lp - wlp)[fine] <= 1e-3 + 2.0 ** -23 * np.abs(wlp[fine])).all()
+    return idx
+
+
+def clouds(seed, W, n, m, d, dtype="f32", spread=1.0):
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    x, y = spread * torch.randn(W, n, d, generator=gen), spread * torch.randn(W, m, d, generator=gen)
+    if dtype == "bf16":
+        x, y = x.bfloat16(), y.bfloat16()
+    rng = np.random.default_rng(seed)
+    g = 0.1 * rng.standard_normal((W, m))
+    return x, y, g, rng
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (3, 5, 1, 2), (2, 9, 2, 3), (8, 64, 64, 2), (4, 33, 100, 3), (3, 40, 129, 5), (2, 50, 512, 15), (5, 17, 1000, 8),
+                                   (1, 12, 5000, 3), (1, 5, 20000, 2), (2, 30, 77, 33), (1, 20, 130, 200), (1, 9, 60, 1024)])
+@pytest.mark.parametrize("cut", ["none", "k", "p", "r", "all"])
+def test_draws_of_every_shape_and_cut(B, shape, cut):
+    W, n, m, d = shape
+    x, y, g, rng = clouds(sum(shape), *shape, spread=1.0 / math.sqrt(d))
+    eps = rng.uniform(0.02, 0.3, W)
+    kw = {}
+    if cut in ("k", "all"): kw["k"] = rng.integers(0, m + 3, W)
+    if cut in ("p", "all"): kw["p"] = rng.uniform(0.2, 1.1, W)
+    if cut in ("r", "all"): kw["r"] = rng.uniform(0.0, 0.3, W)
+    if cut == "all": kw["T"] = rng.uniform(0.3, 2.0, W) * (rng.random(W) > 0.2)
+    check(B, x, y, g, eps, rng.random((W, n, 3), np.float32), **kw)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "mx4", "nv4"])
+@pytest.mark.parametrize("shape", [(2, 20, 90, 8), (3, 30, 130, 40), (2, 70, 200, 64), (1, 140, 300, 128), (2, 33, 257, 200), (1, 50, 1100, 512), (1, 20, 64, 1024)])
+def test_draws_from_other_storage_types(B, dtype, shape):
+    W, n, m, d = shape
+    x, y, g, rng = clouds(7 + sum(shape), *shape, dtype=dtype, spread=1.0 / math.sqrt(d))
+    eps = rng.uniform(0.03, 0.2, W)
+    u = rng.random((W, n, 2), np.float32)
+    fmt = None if dtype == "bf16" else dtype
+    check(B, x, y, g, eps, u, fmt=fmt)
+    check(B, x, y, g, eps, u, k=np.full(W, 20), p=np.full(W, 0.9), r=np.full(W, 0.01), T=np.full(W, 0.8), fmt=fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [3, 64, 200])
+def test_masked_targets_and_their_coordinates(B, d):
+    # padding: -inf potentials with NaN and infinite coordinates behind them; a lane without any target
+    import torch
+    W, n, m = 6, 25, 150
+    for dtype in ("f32", "bf16"):
+        x, y, g, rng = clouds(3, W, n, m, d, dtype=dtype, spread=1.0 / math.sqrt(d))
+        real = [0, 1, 75, 128, 149, 150]
+        for t, c in enumerate(real):
+            g[t, c:] = -np.inf
+            y[t, c:] = float("nan") if t % 2 else float("inf")
+        g[3, 5:40] = -np.inf
+        u = rng.random((W, n, 2), np.float32)
+        for kw in ({}, dict(k=np.full(W, 7)), dict(p=np.full(W, 0.5)), dict(r=np.full(W, 0.05), T=np.full(W, 0.0))):
+            idx = check(B, x, y, g, np.full(W, 0.1), u, **kw)
+            assert (idx[0] == -1).all() and (idx[1] == 0).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [2, 64])
+def test_values_that_are_not_finite_give_no_draw(B, d):
+    W, n, m = 8, 6, 40
+    for dtype in ("f32", "bf16"):
+        x, y, g, rng = clouds(4, W, n, m, d, dtype=dtype, spread=1.0 / math.sqrt(d))
+        x[0, 2, 0] = float("nan")
+        x[1, 3, 1] = float("inf")
+        y[2, 5, 0] = float("nan")
+        y[3, 5, 0] = float("-inf")                               # infinitely far away: a weight of zero
+        g[4, 7] = np.nan
+        g[5, 7] = np.inf
+        g[6, 8] = -1e308                                         # finite, but no weight
+        idx = check(B, x, y, g, np.full(W, 0.1), rng.random((W, n), np.float32))
+        assert (idx[2] == -1).all() and (idx[4] == -1).all() and (idx[5] == -1).all() and (idx[3] >= 0).all() and (idx[6:] >= 0).all()
+        assert (idx[0, 2] == -1).all() and (idx[1, 3] == -1).all() and (idx[0, :2] >= 0).all()
+
+
+@pytest.mark.gpu
+def test_settings_that_are_not_valid_close_their_lane_only(B):
+    W, n, m, d = 16, 4, 30, 3
+    x, y, g, rng = clouds(5, W, n, m, d)
+    T, k, p, r, eps = np.ones(W), np.zeros(W, int), np.ones(W), np.zeros(W), np.full(W, 0.1)
+    T[1], T[2], T[3] = -0.5, np.nan, np.inf
+    k[4], p[5], p[6], p[7] = -1, 0.0, np.nan, -1.0
+    r[8], r[9], r[10] = -0.1, 1.5, np.nan
+    eps[11], eps[12], eps[13] = 0.0, -1.0, np.nan
+    p[14], r[15] = 7.0, 1.0
+    u = rng.random((W, n, 2), np.float32)
+    u[0, 0, 0], u[0, 1, 1], u[0, 2, 0], u[0, 3, 0] = 1.0, -0.25, np.nan, 0.0
+    idx = check(B, x, y, g, eps, u, T=T, k=k, p=p, r=r)
+    assert (idx[1:14] == -1).all() and (idx[14:] >= 0).all() and idx[0, 0, 0] == idx[0, 1, 1] == idx[0, 2, 0] == -1 and idx[0, 3, 0] >= 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [7, 64, 200, 1500])
+def test_equal_weights_are_taken_in_the_order_of_their_indices(B, m):
+    # all targets in one place, and in a few places
+    import torch
+    W, n, d = 5, 8, 3
+    rng = np.random.default_rng(m)
+    x = torch.zeros(W, n, d)
+    y = torch.ones(W, m, d)
+    place = torch.from_numpy(rng.integers(0, 4, (W, m)))
+    y[2:] = 0.25 * place[2:, :, None].float().expand(W - 2, m, d)
+    g = np.zeros((W, m))
+    u = rng.random((W, n, 4), np.float32)
+    u[:, 0] = [0.0, 0.25, 0.5, 0.75]
+    eps = np.full(W, 0.5)
+    for kw in ({}, dict(k=np.array([1, 3, 2, m // 2, m - 1])), dict(p=np.array([0.5, 0.25, 0.5, 0.9, 0.05])), dict(T=np.zeros(W)),
+               dict(k=np.full(W, m // 2 + 1), p=np.full(W, 0.75), r=np.full(W, 0.2))):
+        check(B, x, y, g, eps, u, **kw)
+
+
+@pytest.mark.gpu
+def test_near_ties_and_borders_are_those_of_float64(B):
+    # weights that differ in the tenth digit, shares and numbers that sit within 1e-7 of a border: fp32 cannot tell these
+    import torch
+    W, n, m, d = 4, 16, 300, 2
+    rng = np.random.default_rng(9)
+    x, y = torch.zeros(W, n, d), torch.from_numpy(rng.standard_normal((W, m, d)).astype(np.float32)) * 0.05
+    g = (y.double().numpy() ** 2).sum(2) + 1e-11 * rng.permutation(m)[None, :]       # exponents 1e-10 apart
+    eps = np.full(W, 0.1)
+    u = np.minimum((np.arange(n * 4).reshape(1, n, 4) * 37 % m + rng.choice([-1e-7, 0.0, 1e-7], (W, n, 4))) / m, 1 - 1e-7).clip(0).astype(np.float32)
+    check(B, x, y, g, eps, u)
+    check(B, x, y, g, eps, u, k=np.array([1, 10, 150, 299]))
+    check(B, x, y, g, eps, u, T=np.zeros(W))
+    check(B, x, y, g, eps, u, p=np.array([0.1, 0.5, 2 / 3, 0.99]))
+    check(B, x, y, g, eps, u, r=np.array([1.0, 1 - 1e-7, 0.999, 1.0]))
+
+
+@pytest.mark.gpu
+def test_far_and_large_exponents(B):
+    # potentials of a million eps, sources far from every target, weights that underflow
+    W, n, m, d = 4, 12, 260, 3
+    x, y, g, rng = clouds(12, W, n, m, d)
+    x = x + 50.0
+    g[1] += 1e4
+    g[2] *= 1e3
+    u = rng.random((W, n, 3), np.float32)
+    eps = np.array([0.01, 0.01, 0.05, 1e-3])
+    check(B, x, y, g, eps, u)
+    check(B, x, y, g, eps, u, k=np.array([5, 100, 200, 250]), p=np.full(W, 0.999))
+
+
+@pytest.mark.gpu
+def test_rows_and_outputs_of_a_call_stand_alone(B):
+    # two calls at once on two streams, a captured and replayed one, strided inputs, outputs without logp
+    import torch
+    W, n, m, d = 20, 60, 300, 4
+    x, y, g, rng = clouds(21, W, n, m, d)
+    dev = lambda v: torch.as_tensor(v).cuda()
+    xd, yd, gd, eps, u = x.cuda(), y.cuda(), dev(g), torch.full((W,), 0.1).cuda(), dev(rng.random((W, n, 2), np.float32))
+    first = B.plan_draw(xd, yd, gd, eps, u)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = B.plan_draw(xd, yd, gd, eps, u)
+    again, _ = B.plan_draw(xd, yd, gd, eps, u, logp=True)
+    torch.cuda.synchronize()
+    assert torch.equal(first, other) and torch.equal(first, again)
+    assert torch.equal(first[:, :, 0], B.plan_draw(xd, yd, gd, eps, u[:, :, 0]))
+    assert torch.equal(first, B.plan_draw(xd.transpose(1, 2).contiguous().transpose(1, 2), yd, gd, eps, u))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = B.plan_draw(xd, yd, gd, eps, u)
+    u.copy_(torch.rand(W, n, 2))
+    graph.replay()
+    assert torch.equal(held, B.plan_draw(xd, yd, gd, eps, u)) and not torch.equal(held, first)
+
+
+def test_refusals_of_draws(B):
+    import ctypes
+    import torch
+    L, one = B.lib, ctypes.c_void_p(4096)
+
+    def cfg(W=1, n=4, m=4, d=2, dt=0, draws=1, ws=4096, size=1 << 40):
+        return B.SkbDrawConfig(W, n, m, d, dt, draws, workspace=ws, workspace_bytes=size)
+
+    call = lambda c, x=one, y=one, g=one, e=one, u=one, i=one: L.sinkhorn_plan_draw(x, y, g, e, u, ctypes.byref(c), i, None)
+    assert L.sinkhorn_plan_draw_workspace_bytes(ctypes.byref(cfg())) > 0
+    for bad in (dict(W=0), dict(n=0), dict(m=0), dict(d=0), dict(d=1025), dict(draws=0), dict(dt=4), dict(dt=-1), dict(m=1 << 18), dict(n=1 << 18), dict(W=65536)):
+        assert L.sinkhorn_plan_draw_workspace_bytes(ctypes.byref(cfg(**bad))) == 0
+        assert call(cfg(**bad)) == 2 and L.sinkhorn_operator_last_error()
+    for name in ("x", "y", "g", "e", "u", "i"):
+        assert call(cfg(), **{name: None}) == 1
+    assert call(cfg(ws=None)) == 4 and call(cfg(ws=4096 + 8)) == 4 and call(cfg(size=100)) == 4
+    assert call(cfg(), x=ctypes.c_void_p(4096 + 4)) == 3 and call(cfg(dt=2), y=ctypes.c_void_p(4096 + 64)) == 3
+    with pytest.raises(ValueError):
+        B.plan_draw(torch.zeros(1, 4, 2), torch.zeros(1, 4, 2), None, None, None)
