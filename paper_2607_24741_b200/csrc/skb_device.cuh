@@ -16,6 +16,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "skb_f32x2.cuh"
+
 namespace skb {
 
 enum Leg : int { LEG_F = 0, LEG_G = 1, LEG_V = 2 };
@@ -339,12 +341,6 @@ __device__ __forceinline__ bool lane_needs_column_check(const Dev &P, const Ctl 
     return audited && live && !P.nonfinite[slot] && in_guard_band(P, (double)P.rsum_row[slot] * (1.0 / RSUM_SCALE));
 }
 
-__device__ __forceinline__ float ex2_fast(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ float ex2_t(float x) { return ex2_fast(x); }
 __device__ __forceinline__ double ex2_t(double x) { return exp2(x); }
 

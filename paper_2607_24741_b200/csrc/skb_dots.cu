@@ -339,8 +339,13 @@ skb_status launch_kind(const CUtensorMap &tx, const CUtensorMap &ty, const CUten
 
 }  // namespace
 
-// Clouds of type `dtype` (bf16: d a multiple of 8, both 16-byte aligned), rows of ldo >= m floats, n rows to a lane.
-skb_status launch_dots(int dtype, const void *x, const void *y, int W, int n, int m, int d, float *out, long long ldo, cudaStream_t st)
+DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t row)
+{
+    if (dtype == SKB_BF16) return {(const uint16_t *)base + row * d, nullptr, nullptr, 2 * d, 0};
+    return {c.codes + row * c.cb, c.scales + row * c.sb, c.points ? c.points + row : nullptr, c.cb, c.sb};
+}
+
+skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st)
 {
     if (!encoder()) return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
     int dev = 0, sms = 0;
@@ -349,14 +354,9 @@ skb_status launch_dots(int dtype, const void *x, const void *y, int W, int n, in
     Dots P = {};
     P.out = out; P.ldo = ldo; P.lane_out = ldo * n;
     P.W = W; P.n = n; P.m = m;
-    const void *cx = x, *cy = y;
-    if (dtype == SKB_BF16) P.row_bytes = 2 * d;
-    else {
-        const Cloud4 a = cloud4_view(x, (size_t)W * n, d, dtype), b = cloud4_view(y, (size_t)W * m, d, dtype);
-        P.sx = a.scales; P.sy = b.scales; P.px = a.points; P.py = b.points;
-        P.row_bytes = a.cb; P.sb = a.sb;
-        cx = a.codes; cy = b.codes;
-    }
+    P.sx = x.scales; P.sy = y.scales; P.px = x.points; P.py = y.points;
+    P.row_bytes = x.row_bytes; P.sb = x.sb;
+    const void *cx = x.data, *cy = y.data;
     P.tma_out = ldo % 4 == 0 && (uintptr_t)out % 16 == 0;
     CUtensorMap tx, ty, to = {};
     const size_t rb = P.row_bytes;
@@ -380,5 +380,6 @@ extern "C" skb_status sinkhorn_cloud4_dots(const void *x, const void *y, int W, 
     if (const char *why = cloud4_refused(W, m, d, format)) return op_fail(SKB_ERR_SHAPE, why);
     if ((uintptr_t)x % 256 || (uintptr_t)y % 256) return op_fail(SKB_ERR_WORKSPACE, "x and y must be 256-byte aligned");
     if ((uintptr_t)out % 4) return op_fail(SKB_ERR_WORKSPACE, "out must be 4-byte aligned");
-    return launch_dots(format, x, y, W, n, m, d, out, m, (cudaStream_t)stream);
+    const Cloud4 a = cloud4_view(x, (size_t)W * n, d, format), b = cloud4_view(y, (size_t)W * m, d, format);
+    return launch_dots(dots_cloud(x, a, format, d, 0), dots_cloud(y, b, format, d, 0), format, W, n, m, out, m, (cudaStream_t)stream);
 }

@@ -13,13 +13,15 @@
 //                 two columns to an instruction
 //   products      deep bf16 and 4-bit clouds: x . y from the tensor cores (skb_dots.cu) for as many rows at a time as stay in
 //                 the L2 cache, z = k (g - |y|^2) + 2 k x . y
-// Rows of more than DRAW_MAX_M entries do not fit shared memory: they are decided in float64 alone, weights in the workspace.
+// Rows that do not fit shared memory (from some 49 000 entries on) are decided in float64 alone, weights in the workspace.
 #include <cuda_runtime.h>
 #include <math_constants.h>
+#include <algorithm>
 #include <limits.h>
 
 #include "skb_cloud4.cuh"
 #include "skb_draw_row.cuh"
+#include "skb_f32x2.cuh"
 #include "skb_operators.h"
 
 namespace skb {
@@ -73,13 +75,6 @@ __device__ __forceinline__ float raw_value(const void *base, const Cloud4 &c, in
     if (dtype == SKB_BF16) return __uint_as_float((uint32_t)((const uint16_t *)base)[row * d + k] << 16);
     return cloud4_value(c, row, k);
 }
-__device__ __forceinline__ float ex2(float v)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
-
 // Transposed copy of y and k g, 32 points to a block.  Masked points get coordinates of zero, whatever theirs are.
 __global__ void __launch_bounds__(256) transpose_kernel(const Draw P)
 {
@@ -176,17 +171,18 @@ __device__ void draw_none(const Draw &P, size_t row, int t, int nt)
     for (int s = t; s < P.S; s += nt) put_draw(P, row * P.S + s, -1, CUDART_NAN_F);
 }
 
-// One row in float64 by the whole block.  wf, scale: the row's fp32 weights and a bound on their relative error; null: none.
-// xs: the point's coordinates, `step` floats apart.
-__device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int i, const float *xs, int step, const float *wf, double error,
+// One row in float64 by the whole block.  wf32, error: the row's fp32 weights, null if there are none, and a bound on their relative error.
+// xs: the point's coordinates times `sign`, `step` floats apart.
+__device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int i, const float *xs, int step, double sign, const float *wf32, double error,
                                         double *wd, double *tiles, RowScratch *sc, int *flag)
 {
     const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
     const RowGroup G = {tid, nt, 0, sc};
     const size_t row = (size_t)w * P.n + i;
     const double *hn = P.hn + (size_t)w * P.mp;
-    for (int tier = wf ? 0 : 1; tier < 2; ++tier) {
-        const float floor_ = tier == 0 ? 2.384185791015625e-7f : -1.f;      // 2^-22
+    for (int tier = wf32 && error < 0.01 ? 0 : 1; tier < 2; ++tier) {
+        const float floor_ = 2.384185791015625e-7f;                 // 2^-22
+        const float *wf = tier == 0 ? wf32 : nullptr;
         double top = -CUDART_INF;
         int bad = 0;
         if (P.yt) {
@@ -195,7 +191,7 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
                 if (wf && !(wf[j] > floor_)) continue;
                 double c = 0.0;
                 for (int k = 0; k < P.d; ++k) {
-                    const double e = (double)xs[k * step] - (double)yt[(size_t)k * P.mp + j];
+                    const double e = sign * (double)xs[k * step] - (double)yt[(size_t)k * P.mp + j];
                     c = fma(e, e, c);
                 }
                 const double z = hn[j] == -CUDART_INF ? -CUDART_INF : fma(-L.k2, c, hn[j]);
@@ -210,7 +206,7 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
                 if (hn[j] != -CUDART_INF) {
                     double c = 0.0;
                     for (int k = lane; k < P.d; k += 32) {
-                        const double e = (double)xs[k * step] - (double)raw_value(P.y, P.y4, P.dtype, (size_t)w * P.m + j, P.d, k);
+                        const double e = sign * (double)xs[k * step] - (double)raw_value(P.y, P.y4, P.dtype, (size_t)w * P.m + j, P.d, k);
                         c = fma(e, e, c);
                     }
 #pragma unroll
@@ -254,6 +250,215 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
     }
 }
 
+// R rows of a lane at a time, NT threads: weights in shared memory by all threads, then a group of NT / R threads to a row.
+//   w [R][mp], tiles [R][mp / 128], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
+//   (differences), or one row [d] (products, filled for rows that go to float64)
+// Error of an exponent t = log2 w of the entries above 2^-24 (those below weigh too little): with A = |max t| + 24,
+//   differences  h <= 0 and the scaled distance h - t are at most A; d + 2 roundings of the distance, three of the
+//                scale and t, one of h: (d + 6) A 2^-24
+//   products     B = 2 k |x| max |y| bounds 2 k |x . y|.  The matrix unit cuts off where it adds, up to a unit in the last place of
+//                the largest partial sum for each 16 products (and for their own sum): (d / 16 + 2) B 2^-23; the roundings of h,
+//                scale and t: (3 B + 3 A) 2^-24
+// ln 2 of that, 2^-22 of the exponential, and the additions of a thread's weights bound the relative error of a weight
+// and of a sum; a quotient of two has twice that.
+template <int R, int NT>
+struct DrawShape {
+    static size_t smem(int mp, int d, bool dots)
+    {
+        return (size_t)mp / ROW_TILE * 8 + (size_t)R * (mp + mp / ROW_TILE) * 4 + (size_t)mp * 4 + (dots ? (size_t)d * 4 : (size_t)R * d * 8);
+    }
+};
+
+// Exponents of the block's rows from coordinate differences, RPT rows and four columns to a thread.
+template <int R, int NT, int RPT>
+__device__ __forceinline__ void form_rows(const float *yt, const float *h, const u64 *xs, float *w, int mp, int d, float k2)
+{
+    constexpr int RG = R / RPT, CT = NT / RG;
+    const int ct = threadIdx.x % CT, r0 = threadIdx.x / CT * RPT;
+    const float ninf = -k2;
+    for (int j = 4 * ct; j < mp; j += 4 * CT) {
+        u64 acc[RPT][2];
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) acc[r][0] = acc[r][1] = 0ull;
+#pragma unroll 2
+        for (int k = 0; k < d; ++k) {
+            const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(yt + (size_t)k * mp + j);
+#pragma unroll
+            for (int r = 0; r < RPT; r += 2) {
+                ulonglong2 x = {0ull, 0ull};
+                if constexpr (RPT >= 2) x = *reinterpret_cast<const ulonglong2 *>(xs + k * R + r0 + r);
+                else x.x = xs[k * R + r0];
+#pragma unroll
+                for (int q = 0; q < (RPT >= 2 ? 2 : 1); ++q) {
+                    const u64 a = add2(y.x, q ? x.y : x.x), b = add2(y.y, q ? x.y : x.x);
+                    acc[r + q][0] = fma2(a, a, acc[r + q][0]);
+                    acc[r + q][1] = fma2(b, b, acc[r + q][1]);
+                }
+            }
+        }
+        const ulonglong2 hh = *reinterpret_cast<const ulonglong2 *>(h + j);
+        const u64 s = pack2(ninf, ninf);
+#pragma unroll
+        for (int r = 0; r < RPT; ++r) {
+            const ulonglong2 t = {fma2(s, acc[r][0], hh.x), fma2(s, acc[r][1], hh.y)};
+            *reinterpret_cast<ulonglong2 *>(w + (size_t)(r0 + r) * mp + j) = t;
+        }
+    }
+}
+
+template <int R, int NT, bool DOTS>
+__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1) draw_kernel(const Draw P)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowScratch sc[R];
+    __shared__ double error[R];
+    __shared__ int unsure[R], flag;
+    constexpr int NG = NT / R;                                   // threads of a row's group
+    const int mp = P.mp, ntiles = mp / ROW_TILE, tid = threadIdx.x, lane = tid & 31;
+    double *tiles64 = reinterpret_cast<double *>(smem);
+    float *w_all = reinterpret_cast<float *>(tiles64 + (ntiles + 1) / 2 * 2);
+    float *h = w_all + (size_t)R * mp;
+    u64 *xs = reinterpret_cast<u64 *>(h + mp);
+    float *x1 = reinterpret_cast<float *>(xs), *tiles_all = x1 + (DOTS ? (P.d + 3) / 4 * 4 : 2 * R * P.d);
+    const int g = tid / NG;
+    const RowGroup G = {tid % NG, NG, 1 + g, &sc[g]}, all = {tid, NT, 0, &sc[0]};
+    float *w = w_all + (size_t)g * mp, *tiles = tiles_all + (size_t)g * ntiles;
+
+    const int per_lane = (P.rows + R - 1) / R;
+    const long long total = (long long)P.lanes * per_lane, first = total * blockIdx.x / gridDim.x, last = total * (blockIdx.x + 1) / gridDim.x;
+    int at_lane = -1;
+    float y_max = 0.f;
+    bool some = false;
+    for (long long t = first; t < last; ++t) {
+        const int wl = (int)(t / per_lane), r0 = (int)(t % per_lane) * R, lanew = P.lane0 + wl, i0 = P.row0 + r0;
+        const int rows = min(R, P.rows - r0);
+        const size_t row0 = (size_t)lanew * P.n + i0;
+        const Lane L = lane_of(P, lanew);
+        if (!L.ok) {
+            for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, NT);
+            continue;
+        }
+        if (lanew != at_lane) {
+            // the lane's largest k g_j (- |y_j|^2), and the others less that
+            const double *hn = P.hn + (size_t)lanew * mp;
+            double top = -CUDART_INF;
+            float far = 0.f;
+            for (int j = tid; j < mp; j += NT) {
+                top = fmax(top, hn[j]);
+                if (DOTS) far = fmaxf(far, P.yn[(size_t)lanew * mp + j]);
+            }
+            top = all.largest(top);
+            if (DOTS) y_max = sqrtf(all.largest(far));
+            some = top != -CUDART_INF;
+            for (int j = tid; j < mp; j += NT) h[j] = some ? (float)(hn[j] - top) : 0.f;
+            at_lane = lanew;
+        }
+        if (!some) {
+            for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, NT);
+            continue;
+        }
+        if (!DOTS) {
+            for (int q = tid; q < R * P.d; q += NT) {
+                const int r = q / P.d, k = q % P.d;
+                const float v = r < rows ? -raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k) : 0.f;
+                xs[k * R + r] = pack2(v, v);
+            }
+        }
+        if (tid < R) unsure[tid] = 0;
+        __syncthreads();
+        const float k2 = (float)L.k2;
+        if (!DOTS) {
+            const float *yt = P.yt + (size_t)lanew * P.d * mp;
+            // rows too short for all threads to have four columns of them: fewer rows to a thread
+            if constexpr (R == 8) {
+                if (mp > 512) form_rows<R, NT, 8>(yt, h, xs, w_all, mp, P.d, k2);
+                else if (mp > 256) form_rows<R, NT, 4>(yt, h, xs, w_all, mp, P.d, k2);
+                else if (mp > 128) form_rows<R, NT, 2>(yt, h, xs, w_all, mp, P.d, k2);
+                else form_rows<R, NT, 1>(yt, h, xs, w_all, mp, P.d, k2);
+            } else form_rows<R, NT, R>(yt, h, xs, w_all, mp, P.d, k2);
+            __syncthreads();
+        }
+        if (g < rows) {
+            const size_t row = row0 + g;
+            float top = -CUDART_INF_F;
+            if (DOTS) {
+                const float *dots = P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo;
+                const float two_k = (float)(2.0 * L.k2);
+                for (int j = 4 * G.t; j < mp; j += 4 * NG) {
+                    float v[4], hh[4];
+                    load4(dots + j, v);
+                    load4(h + j, hh);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        v[i] = hh[i] == -CUDART_INF_F ? -CUDART_INF_F : fmaf(two_k, v[i], hh[i]);
+                        top = fmaxf(top, v[i]);
+                    }
+                    *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
+                }
+            } else {
+                for (int j = 4 * G.t; j < mp; j += 4 * NG) {
+                    float v[4];
+                    load4(w + j, v);
+                    top = fmaxf(fmaxf(top, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+                }
+            }
+            top = G.largest(top);
+            // nothing left in fp32's range, a NaN or an infinite exponent: float64 tells which
+            bool sure = false;
+            double delta = CUDART_INF;
+            if (top != -CUDART_INF_F) {
+                G.sync();
+                double mass = 0.0;
+                int count = 0;
+                for (int q = G.t >> 5; q < ntiles; q += NG >> 5) {
+                    float *p = w + q * ROW_TILE + 4 * lane, v[4];
+                    load4(p, v);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) { v[i] = ex2_fast(v[i] - top); count += v[i] > 0.f; }
+                    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+                    float s = (v[0] + v[1]) + (v[2] + v[3]);
+                    mass += (double)s;
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                    if (lane == 0) tiles[q] = s;
+                }
+                G.add(mass, count);
+                if (mass <= 3e38) {
+                    const float A = fabsf(top) + 24.f, u24 = 5.9604645e-8f;
+                    float e;
+                    if (DOTS) {
+                        const float b = 2.f * k2 * sqrtf(P.xn[row]) * y_max;
+                        e = ((float)(P.d / 16 + 2) * 2.f + 3.f) * u24 * b + 3.f * u24 * A;
+                    } else e = (float)(P.d + 6) * u24 * A;
+                    delta = 2.0 * (0.6932 * (double)e + 2.384e-7 + (double)u24 * (8 + mp / (4 * NG)));
+                    sure = true;
+                    RowCut<float> cut = {0.f, -1, mass, count, 1.f};
+                    if (L.cuts.k < count || L.cuts.p < 1.0 || L.cuts.r > 0.f) {
+                        G.sync();
+                        sure = row_cut(w, mp, G, L.cuts, mass, count, delta, cut, tiles);
+                    }
+                    if (sure) {
+                        G.sync();
+                        sure = draw_all(P, row, w, cut, tiles, delta, G.t >> 5, NG >> 5);
+                    }
+                }
+            }
+            if (!sure && lane == 0) { unsure[g] = 1; error[g] = delta; }
+        }
+        __syncthreads();
+        for (int r = 0; r < rows; ++r) {
+            if (!unsure[r]) continue;
+            if (DOTS) {
+                for (int k = tid; k < P.d; k += NT) x1[k] = raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k);
+                __syncthreads();
+            }
+            decide_row(P, L, lanew, i0 + r, DOTS ? x1 : x1 + 2 * r, DOTS ? 1 : 2 * R, DOTS ? 1.0 : -1.0, w_all + (size_t)r * mp, error[r],
+                       P.scratch + (size_t)blockIdx.x * mp, tiles64, &sc[0], &flag);
+        }
+        __syncthreads();
+    }
+}
+
 // Rows too long for shared memory: a block to a row, float64 throughout.
 __global__ void __launch_bounds__(512) draw_long_kernel(const Draw P)
 {
@@ -269,21 +474,73 @@ __global__ void __launch_bounds__(512) draw_long_kernel(const Draw P)
         if (!L.ok) { draw_none(P, (size_t)t, threadIdx.x, blockDim.x); continue; }
         for (int k = threadIdx.x; k < P.d; k += blockDim.x) xs[k] = raw_value(P.x, P.x4, P.dtype, (size_t)t, P.d, k);
         __syncthreads();
-        decide_row(P, L, w, i, xs, 1, nullptr, 0.0, P.scratch + (size_t)blockIdx.x * P.mp, tiles, &sc, &flag);
+        decide_row(P, L, w, i, xs, 1, 1.0, nullptr, 0.0, P.scratch + (size_t)blockIdx.x * P.mp, tiles, &sc, &flag);
     }
 }
 
 size_t long_smem(const Draw &P) { return (size_t)P.mp / ROW_TILE * 8 + (size_t)P.d * 4; }
 
+// How a problem is run: rows to a block, where the exponents come from, and the rows whose products are held at a time.
+struct Plan {
+    int R;                                                  // 8, 4, 1; 0: too long for shared memory
+    bool dots;
+    int lanes, rows;
+    size_t smem;
+};
+constexpr size_t DRAW_SMEM = 216 * 1024;                     // dynamic; a block has 8 KB more, an SM 227 KB
+Plan plan_of(const Draw &P)
+{
+    Plan p = {};
+    // Deep clouds whose rows TMA can take.  Below 64 dimensions the products are a small part of a pair's work.
+    p.dots = P.dtype == SKB_F32 ? false : P.d >= 64 && (P.dtype != SKB_BF16 || P.d % 8 == 0);
+    const size_t s8 = DrawShape<8, 256>::smem(P.mp, P.d, p.dots), s4 = DrawShape<4, 512>::smem(P.mp, P.d, p.dots),
+                 s1 = DrawShape<1, 512>::smem(P.mp, P.d, p.dots);
+    // eight rows while two blocks share an SM, four while one fits
+    if (s8 + 10 * 1024 <= DRAW_SMEM / 2) { p.R = 8; p.smem = s8; }
+    else if (s4 + 64 <= DRAW_SMEM) { p.R = 4; p.smem = s4; }
+    else if (s1 + 64 <= DRAW_SMEM) { p.R = 1; p.smem = s1; }
+    p.smem += 64;
+    p.lanes = P.W; p.rows = P.n;
+    if (p.dots && p.R) {
+        const size_t lane = (size_t)P.n * P.mp * 4;
+        if (lane <= DRAW_DOTS_BYTES) p.lanes = (int)std::min<size_t>(P.W, DRAW_DOTS_BYTES / lane);
+        else { p.lanes = 1; p.rows = (int)std::max<size_t>(128, DRAW_DOTS_BYTES / ((size_t)P.mp * 4) / 128 * 128); }
+        p.rows = std::min(p.rows, P.n);
+    }
+    return p;
+}
+
 // Where the parts of the workspace are; returns its size.
-size_t carve(Draw &P, char *base)
+size_t carve(Draw &P, const Plan &p, char *base)
 {
     size_t at = 0;
-    auto take = [&](size_t bytes) { char *p = base ? base + at : nullptr; at += (bytes + 255) / 256 * 256; return p; };
+    auto take = [&](size_t bytes) { char *q = base ? base + at : nullptr; at += (bytes + 255) / 256 * 256; return q; };
     P.hn = (double *)take((size_t)P.W * P.mp * 8);
-    P.yt = (float *)take((size_t)P.W * P.d * P.mp * 4);
-    P.scratch = (double *)take((size_t)DRAW_LONG_BLOCKS * P.mp * 8);
+    if (p.dots && p.R) {
+        P.yn = (float *)take((size_t)P.W * P.mp * 4);
+        P.xn = (float *)take((size_t)P.W * P.n * 4);
+        P.dots = (const float *)take((size_t)p.lanes * p.rows * P.mp * 4);
+    } else P.yt = (float *)take((size_t)P.W * P.d * P.mp * 4);
+    P.scratch = (double *)take((size_t)(p.R ? DRAW_MAX_BLOCKS : DRAW_LONG_BLOCKS) * P.mp * 8);
     return at;
+}
+
+template <int R, int NT, bool DOTS>
+void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
+{
+    // (the limit for any shape: another host thread may set it between this and the launch)
+    cudaFuncSetAttribute(draw_kernel<R, NT, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(R == 8 ? DRAW_SMEM / 2 : DRAW_SMEM));
+    const long long tiles = (long long)P.lanes * ((P.rows + R - 1) / R);
+    const size_t fit = NT > 256 ? 1 : std::min<size_t>(3, DRAW_SMEM / (p.smem + 10 * 1024));
+    const long long most = (long long)(DRAW_MAX_BLOCKS / 3 * fit);
+    draw_kernel<R, NT, DOTS><<<(unsigned)(tiles < most ? tiles : most), NT, p.smem, st>>>(P);
+}
+template <bool DOTS>
+void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
+{
+    if (p.R == 8) launch_draw<8, 256, DOTS>(P, p, st);
+    else if (p.R == 4) launch_draw<4, 512, DOTS>(P, p, st);
+    else launch_draw<1, 512, DOTS>(P, p, st);
 }
 
 const char *refused(const skb_draw_config *c)
@@ -315,7 +572,7 @@ extern "C" size_t sinkhorn_plan_draw_workspace_bytes(const skb_draw_config *cfg)
 {
     if (!cfg || refused(cfg)) return 0;
     Draw P = problem(cfg);
-    return carve(P, nullptr);
+    return carve(P, plan_of(P), nullptr);
 }
 
 extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u,
@@ -335,10 +592,31 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
         P.x4 = cloud4_view(x, (size_t)P.W * P.n, P.d, P.dtype);
         P.y4 = cloud4_view(y, (size_t)P.W * P.m, P.d, P.dtype);
     }
-    carve(P, (char *)cfg->workspace);
+    const Plan p = plan_of(P);
+    carve(P, p, (char *)cfg->workspace);
     cudaStream_t st = (cudaStream_t)cfg->stream;
-    transpose_kernel<<<dim3(P.mp / 32, P.W), 256, 0, st>>>(P);
-    const long long rows = (long long)P.W * P.n;
-    draw_long_kernel<<<(unsigned)(rows < DRAW_LONG_BLOCKS ? rows : DRAW_LONG_BLOCKS), 512, long_smem(P), st>>>(P);
+    if (!p.dots || !p.R) transpose_kernel<<<dim3(P.mp / 32, P.W), 256, 0, st>>>(P);
+    if (!p.R) {
+        const long long rows = (long long)P.W * P.n;
+        draw_long_kernel<<<(unsigned)(rows < DRAW_LONG_BLOCKS ? rows : DRAW_LONG_BLOCKS), 512, long_smem(P), st>>>(P);
+        return op_launched("plan_draw");
+    }
+    if (!p.dots) {
+        P.lanes = P.W; P.rows = P.n;
+        launch_draw<false>(P, p, st);
+        return op_launched("plan_draw");
+    }
+    norms_kernel<<<dim3((P.mp + P.n + 7) / 8, P.W), 256, 0, st>>>(P);
+    P.ldo = P.mp;
+    for (P.lane0 = 0; P.lane0 < P.W; P.lane0 += p.lanes)
+        for (P.row0 = 0; P.row0 < P.n; P.row0 += p.rows) {
+            P.lanes = std::min(p.lanes, P.W - P.lane0);
+            P.rows = std::min(p.rows, P.n - P.row0);
+            const skb_status s = launch_dots(dots_cloud(P.x, P.x4, P.dtype, P.d, (size_t)P.lane0 * P.n + P.row0),
+                                             dots_cloud(P.y, P.y4, P.dtype, P.d, (size_t)P.lane0 * P.m), P.dtype, P.lanes, P.rows, P.m,
+                                             const_cast<float *>(P.dots), P.ldo, st);
+            if (s != SKB_OK) return s;
+            launch_draw<true>(P, p, st);
+        }
     return op_launched("plan_draw");
 }

@@ -4,13 +4,22 @@
 #include <string>
 
 #include "../../include/sinkhorn_batch.h"
+#include "skb_cloud4.cuh"
 
 namespace skb {
 
 skb_status op_fail(skb_status st, const std::string &msg);     // sets the calling thread's text
 skb_status op_launched(const char *what);                       // the launch's status; clears the text where it went well
 const char *cloud4_refused(int W, int npts, int d, int format);   // null, or why there is no such cloud
-// x_i . y_j of clouds of type `dtype` (bf16: d a multiple of 8, both 16-byte aligned), n rows of ldo >= m floats to a lane
-skb_status launch_dots(int dtype, const void *x, const void *y, int W, int n, int m, int d, float *out, long long ldo, cudaStream_t st);
+// Points of a cloud from `row` on, as products take them: bf16 values, or codes, scales and powers of two.
+struct DotsCloud {
+    const void *data;
+    const uint8_t *scales;
+    const float *points;
+    int row_bytes, sb;
+};
+DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t row);
+// x_i . y_j of W lanes of n and m points (bf16: d a multiple of 8, rows 16-byte aligned), n rows of ldo >= m floats to a lane
+skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st);
 
 }  // namespace skb

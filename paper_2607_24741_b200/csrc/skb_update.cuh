@@ -35,10 +35,10 @@
 // (screen-positive) and the verdict, and the column-check leg reads the same flag predicate.
 #pragma once
 #include "skb_device.cuh"
+#include "skb_f32x2.cuh"
 
 namespace skb {
 
-typedef unsigned long long u64;
 
 // Register tile of one thread: R rows held for the whole kernel x CW adjacent columns per step.
 // More rows per thread means fewer shared-memory bytes per pair; the limit is the register file.
@@ -81,34 +81,6 @@ template <typename T, int DP, int CS> struct TileCols {
     static constexpr int value = (Tune<T, DP>::CW * CS * 2 > wish) ? Tune<T, DP>::CW * CS * 2 : wish;
 };
 
-__device__ __forceinline__ u64 pack2(float lo, float hi)
-{
-    u64 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(u64 v, float &lo, float &hi)
-{
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ u64 fma2(u64 a, u64 b, u64 c)
-{
-    u64 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ u64 add2(u64 a, u64 b)
-{
-    u64 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ u64 sub2(u64 a, u64 b)
-{
-    u64 d;
-    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 // 2^k for an integer-valued k <= 0 (exact; flushes to 0 below the normal range)
 __device__ __forceinline__ float pow2i(float k)
 {
