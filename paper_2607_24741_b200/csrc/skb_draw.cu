@@ -27,8 +27,9 @@
 namespace skb {
 namespace {
 
-constexpr int DRAW_MAX_BLOCKS = 444;                 // 148 SMs, three blocks each: rows of scratch in the workspace
+constexpr int DRAW_MAX_BLOCKS = 296;                 // 148 SMs, two blocks each: rows of scratch in the workspace
 constexpr int DRAW_LONG_BLOCKS = 148;
+constexpr float ROW_FLOOR = 2.384185791015625e-7f;   // 2^-22: weights that are formed again where fp32 does not do
 constexpr size_t DRAW_DOTS_BYTES = (size_t)64 << 20; // products that are held at a time: half of the L2 cache
 
 struct Draw {
@@ -43,7 +44,7 @@ struct Draw {
     // workspace
     double *hn;                                      // [W][mp] k g_j, or k (g_j - |y_j|^2); -inf: masked
     float *yt;                                       // [W][d][mp] (differences)
-    float *yn, *xn;                                  // [W][mp], [W][n] squared norms (products)
+    float2 *yn, *xn;                                 // [W][mp], [W][n] squared norms, and their means over prefixes (products)
     const float *dots;                               // rows row0 .. row0 + rows - 1 of lanes lane0 .. lane0 + lanes - 1
     double *scratch;                                 // [blocks][mp]
     long long ldo;
@@ -110,36 +111,43 @@ __global__ void __launch_bounds__(256) transpose_kernel(const Draw P)
     }
 }
 
-// |point|^2 in float64, by one warp
-__device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, int dtype, size_t row, int d)
+// |point|^2 in float64, by one warp; prefix: the mean of the squared norms of its first 16, 32, ... dimensions.
+__device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, int dtype, size_t row, int d, double &prefix)
 {
-    double s = 0.0;
+    double s = 0.0, p = 0.0;
+    const int steps = (d + 15) / 16;
     for (int k = threadIdx.x & 31; k < d; k += 32) {
         const double v = (double)raw_value(base, c, dtype, row, d, k);
         s = fma(v, v, s);
+        p = fma(v * v, (double)(steps - k / 16), p);
     }
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    for (int off = 16; off > 0; off >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, off);
+        p += __shfl_xor_sync(0xffffffffu, p, off);
+    }
+    prefix = p / steps;
     return s;
 }
-// Squared norms of both clouds and k (g - |y|^2), a warp to a point.
+// k (g - |y|^2), and what bounds the error of the products, a warp to a point.
 __global__ void __launch_bounds__(256) norms_kernel(const Draw P)
 {
     const int w = blockIdx.y, i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    double p = 0.0;
     if (i < P.mp) {
         const double g = i < P.m ? P.g[(size_t)w * P.m + i] : -CUDART_INF;
         const bool masked = g == -CUDART_INF;
-        const double s = masked ? 0.0 : square_of(P.y, P.y4, P.dtype, (size_t)w * P.m + i, P.d);
+        const double s = masked ? 0.0 : square_of(P.y, P.y4, P.dtype, (size_t)w * P.m + i, P.d, p);
         if (lane == 0) {
             P.hn[(size_t)w * P.mp + i] = masked ? g : lane_of(P, w).k2 * (g - s);
-            P.yn[(size_t)w * P.mp + i] = (float)s;
+            P.yn[(size_t)w * P.mp + i] = make_float2((float)s, (float)p);
         }
         return;
     }
     const int r = i - P.mp;
     if (r >= P.n) return;
-    const double s = square_of(P.x, P.x4, P.dtype, (size_t)w * P.n + r, P.d);
-    if (lane == 0) P.xn[(size_t)w * P.n + r] = (float)s;
+    const double s = square_of(P.x, P.x4, P.dtype, (size_t)w * P.n + r, P.d, p);
+    if (lane == 0) P.xn[(size_t)w * P.n + r] = make_float2((float)s, (float)p);
 }
 
 __device__ __forceinline__ void put_draw(const Draw &P, size_t at, int index, float logp)
@@ -150,7 +158,7 @@ __device__ __forceinline__ void put_draw(const Draw &P, size_t at, int index, fl
 
 // Draws of one row from weights and their cut, shared out to the group's warps.  True if all of this warp's were sure.
 template <typename Real>
-__device__ bool draw_all(const Draw &P, size_t row, const Real *w, const RowCut<Real> &cut, const Real *tiles, double delta, int warp, int warps)
+__device__ bool draw_all(const Draw &P, size_t row, const Real *w, const RowCut<Real> &cut, const Real *tiles, const RowError &err, int warp, int warps)
 {
     const double total = row_total(tiles, P.mp / ROW_TILE);
     bool sure = true;
@@ -159,7 +167,7 @@ __device__ bool draw_all(const Draw &P, size_t row, const Real *w, const RowCut<
         int j = -1;
         double wj = 0.0;
         if (u >= 0.f && u < 1.f) {
-            const bool good = row_draw(w, cut, tiles, P.mp / ROW_TILE, total, (double)u, delta, j, wj);
+            const bool good = row_draw(w, cut, tiles, P.mp / ROW_TILE, total, (double)u, err, j, wj);
             if (!good) { sure = false; continue; }
         }
         if ((threadIdx.x & 31) == 0) put_draw(P, row * P.S + s, j, j < 0 ? CUDART_NAN_F : (float)log(wj / total));
@@ -181,14 +189,13 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
     const size_t row = (size_t)w * P.n + i;
     const double *hn = P.hn + (size_t)w * P.mp;
     for (int tier = wf32 && error < 0.01 ? 0 : 1; tier < 2; ++tier) {
-        const float floor_ = 2.384185791015625e-7f;                 // 2^-22
         const float *wf = tier == 0 ? wf32 : nullptr;
         double top = -CUDART_INF;
         int bad = 0;
         if (P.yt) {
             const float *yt = P.yt + (size_t)w * P.d * P.mp;
             for (int j = tid; j < P.mp; j += nt) {
-                if (wf && !(wf[j] > floor_)) continue;
+                if (wf && !(wf[j] > ROW_FLOOR)) continue;
                 double c = 0.0;
                 for (int k = 0; k < P.d; ++k) {
                     const double e = sign * (double)xs[k * step] - (double)yt[(size_t)k * P.mp + j];
@@ -201,7 +208,7 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
             }
         } else {
             for (int j = warp; j < P.mp; j += nt >> 5) {
-                if (wf && !(wf[j] > floor_)) continue;
+                if (wf && !(wf[j] > ROW_FLOOR)) continue;
                 double z = -CUDART_INF;
                 if (hn[j] != -CUDART_INF) {
                     double c = 0.0;
@@ -226,7 +233,7 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
         int count = 0, unused = 0;
         for (int j = tid; j < P.mp; j += nt) {
             double v;
-            if (wf && !(wf[j] > floor_)) { v = (double)wf[j]; rest += v; }
+            if (wf && !(wf[j] > ROW_FLOOR)) { v = (double)wf[j]; rest += v; }
             else v = exp2(wd[j] - top);
             wd[j] = v;
             mass += v;
@@ -234,14 +241,15 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
         }
         G.add(mass, count);
         G.add(rest, unused);
-        const double delta = tier == 0 ? 4.0 * error * rest / mass + 1e-12 : 0.0;
+        RowError err = {0.0, 0.f, 0.f};
+        if (tier == 0) err = {4.0 * error * rest + 1e-12 * mass, 1e-12f, 0.f};
         RowCut<double> cut;
-        bool sure = row_cut(wd, P.mp, G, L.cuts, mass, count, delta, cut, tiles);
-        if (sure && tier == 0 && cut.lowest < 2.0 * floor_) sure = false;
+        bool sure = row_cut(wd, P.mp, G, L.cuts, 1.0, mass, count, err, cut, tiles);
+        if (sure && tier == 0 && cut.lowest < 2.f * ROW_FLOOR) sure = false;
         if (sure) {
             if (tid == 0) *flag = 0;
             __syncthreads();
-            if (!draw_all(P, row, wd, cut, tiles, delta, warp, nt >> 5) && lane == 0) *flag = 1;
+            if (!draw_all(P, row, wd, cut, tiles, err, warp, nt >> 5) && lane == 0) *flag = 1;
             __syncthreads();
             sure = *flag == 0;
         }
@@ -252,20 +260,21 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
 
 // R rows of a lane at a time, NT threads: weights in shared memory by all threads, then a group of NT / R threads to a row.
 //   w [R][mp], tiles [R][mp / 128], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
-//   (differences), or one row [d] (products, filled for rows that go to float64)
-// Error of an exponent t = log2 w of the entries above 2^-24 (those below weigh too little): with A = |max t| + 24,
-//   differences  h <= 0 and the scaled distance h - t are at most A; d + 2 roundings of the distance, three of the
-//                scale and t, one of h: (d + 6) A 2^-24
-//   products     B = 2 k |x| max |y| bounds 2 k |x . y|.  The matrix unit cuts off where it adds, up to a unit in the last place of
-//                the largest partial sum for each 16 products (and for their own sum): (d / 16 + 2) B 2^-23; the roundings of h,
-//                scale and t: (3 B + 3 A) 2^-24
-// ln 2 of that, 2^-22 of the exponential, and the additions of a thread's weights bound the relative error of a weight
-// and of a sum; a quotient of two has twice that.
+//   (differences), or x [R][xd] of rows that are formed again (products)
+// Error of an exponent t = log2 w at a depth q below the row's largest, A = |largest t|:
+//   differences  h <= 0 and the scaled distance h - t are at most A + q; d + 2 roundings of the distance, three of the
+//                scale and t, one of h: (d + 6) (A + q) 2^-24
+//   products     2 k |x . y| is at most B = 2 k |x| max |y|, and after each 16 dimensions at most the same of those
+//                prefixes, on average no more than B' (from the root mean squares of the prefixes' norms).  The matrix unit
+//                cuts off where it adds products to a sum: a unit in the last place of the sum, at most 2^-23 of it, for each 16, and
+//                two more: (d / 16) B' 2^-23 + 2 B 2^-23; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
+// The exponential adds 2^-22 and 2^-24 q of the difference that it is taken of, the additions of weights 2^-24 each.
+__host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
 template <int R, int NT>
 struct DrawShape {
     static size_t smem(int mp, int d, bool dots)
     {
-        return (size_t)mp / ROW_TILE * 8 + (size_t)R * (mp + mp / ROW_TILE) * 4 + (size_t)mp * 4 + (dots ? (size_t)d * 4 : (size_t)R * d * 8);
+        return (size_t)mp / ROW_TILE * 8 + (size_t)R * (mp + mp / ROW_TILE) * 4 + (size_t)mp * 4 + (dots ? (size_t)R * dots_xd(d) * 4 : (size_t)R * d * 8);
     }
 };
 
@@ -306,51 +315,186 @@ __device__ __forceinline__ void form_rows(const float *yt, const float *h, const
     }
 }
 
+// Tiles' sums, mass, number and largest of a row's weights, and the sum of w log2(1 / w).
+struct RowSums {
+    double mass, depth;
+    int count;
+    float top;
+};
+__device__ __forceinline__ RowSums sum_row(const RowGroup &G, const float *w, float *tiles, int ntiles)
+{
+    RowSums r = {0.0, 0.0, 0, 0.f};
+    const int lane = G.t & 31;
+    for (int q = G.t >> 5; q < ntiles; q += G.nt >> 5) {
+        float v[4];
+        load4(w + q * ROW_TILE + 4 * lane, v);
+        float s = (v[0] + v[1]) + (v[2] + v[3]);
+        r.mass += (double)s;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { r.count += v[i] > 0.f; r.top = fmaxf(r.top, v[i]); }
+#pragma unroll
+        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+        if (lane == 0) tiles[q] = s;
+    }
+    G.add(r.mass, r.count);
+    r.top = G.largest(r.top);
+    return r;
+}
+
+// Exact weights, to fp32's precision, for a row's entries above 2^-22, by a warp for its tiles' entries of the row
+// (tiles warp, warp + warps, ...).  `base`: what an exponent of h stands for in float64, the row's largest included.
+__device__ __forceinline__ void refine_differences(const Draw &P, double k2, const double *hn, const float *yt, const float *nx, int step, double base,
+                                                   float *w, int warp, int warps)
+{
+    const int lane = threadIdx.x & 31;
+    for (int q = warp; q < P.mp / ROW_TILE; q += warps) {
+        const int j = q * ROW_TILE + 4 * lane;
+        float v[4];
+        load4(w + j, v);
+        if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) > ROW_FLOOR)) continue;
+        double c[4] = {0.0, 0.0, 0.0, 0.0};
+        for (int k = 0; k < P.d; ++k) {
+            float y[4];
+            load4(yt + (size_t)k * P.mp + j, y);
+            const double x = (double)nx[k * step];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { const double e = (double)y[i] + x; c[i] = fma(e, e, c[i]); }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (v[i] > ROW_FLOOR) v[i] = ex2_fast((float)(fma(-k2, c[i], hn[j + i]) - base));
+        *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
+    }
+}
+// Eight dimensions of point `row` from k on, k a multiple of 8; zeros past the last (k < the padded depth).
+__device__ __forceinline__ void eight_values(const void *data, const Cloud4 &c, int dtype, size_t row, int d, int k, u64 (&v)[4])
+{
+    if (dtype == SKB_BF16) {
+        const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
+        const uint32_t b[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pack2(__uint_as_float(b[i] << 16), __uint_as_float(b[i] & 0xffff0000u));
+    } else {
+        const uint32_t b = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
+        const float s = cloud4_scale(c, row, k);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = pack2(e2m1_value(b >> (8 * i)) * s, e2m1_value(b >> (8 * i + 4)) * s);
+    }
+}
+// x . y of four points of y at a time, eight threads to a point.  Products are exact in fp32 (at most 16 bits).  They are
+// added to a large number M, whose last place is 2^-24 of a bound on the sum: what an addition cuts off is itself exact and is
+// added up apart, so that the result is good to 2^-40 of the bound.
+__device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl, const double *hn, const float *x, float magic, double base,
+                                                float *w, unsigned char *list, int warp, int warps)
+{
+    const int lane = threadIdx.x & 31, part = lane & 7, col = lane >> 3;
+    const int chunks = P.dtype == SKB_BF16 ? P.d / 8 : dots_xd(P.d) / 8;
+    for (int q = warp; q < P.mp / ROW_TILE; q += warps) {
+        float v[4];
+        load4(w + q * ROW_TILE + 4 * lane, v);
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned ball = __ballot_sync(0xffffffffu, v[i] > ROW_FLOOR);
+            if (v[i] > ROW_FLOOR) list[n + __popc(ball & ((1u << lane) - 1u))] = (unsigned char)(4 * lane + i);
+            n += __popc(ball);
+        }
+        __syncwarp();
+        for (int e0 = 0; e0 < n; e0 += 4) {
+            const int j = q * ROW_TILE + list[min(e0 + col, n - 1)];
+            const size_t row = (size_t)wl * P.m + j;
+            const u64 m2 = pack2(magic, magic);
+            u64 sum = m2, low = 0ull;
+            for (int c = part; c < chunks; c += 8) {
+                u64 y[4];
+                eight_values(P.y, P.y4, P.dtype, row, P.d, 8 * c, y);
+                const ulonglong2 xa = reinterpret_cast<const ulonglong2 *>(x + 8 * c)[0], xb = reinterpret_cast<const ulonglong2 *>(x + 8 * c)[1];
+                const u64 xv[4] = {xa.x, xa.y, xb.x, xb.y};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const u64 t = fma2(xv[i], y[i], sum);
+                    low = add2(low, fma2(xv[i], y[i], sub2(sum, t)));
+                    sum = t;
+                }
+            }
+            float a, b, la, lb;
+            unpack2(sub2(sum, m2), a, b);                            // exact
+            unpack2(low, la, lb);
+            double dot = ((double)a + (double)b) + ((double)la + (double)lb);
+#pragma unroll
+            for (int off = 1; off < 8; off *= 2) dot += __shfl_xor_sync(0xffffffffu, dot, off);
+            if (part == 0 && e0 + col < n) w[j] = ex2_fast((float)(fma(2.0 * k2, dot, hn[j]) - base));
+        }
+        __syncwarp();
+    }
+}
+
+// Cuts a row of fp32 weights and draws from it; false if something is unsure.  The bounds hold for weights above `floor_`.
+__device__ __forceinline__ bool decide_fast(const Draw &P, const RowGroup &G, const RowCuts &cuts, size_t row, const float *w, float *tiles,
+                                            const RowSums &sums, const RowError &err, float floor_)
+{
+    RowCut<float> cut = {0.f, -1, sums.mass, sums.count, 1.f};
+    G.sync();
+    if (cuts.k < sums.count || cuts.p < 1.0 || cuts.r > 0.f) {
+        if (!row_cut(w, P.mp, G, cuts, sums.top, sums.mass, sums.count, err, cut, tiles)) return false;
+        if (cut.lowest < floor_) return false;
+        G.sync();
+    }
+    return draw_all(P, row, w, cut, tiles, err, G.t >> 5, G.nt >> 5);
+}
+
 template <int R, int NT, bool DOTS>
-__global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1) draw_kernel(const Draw P)
+__global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc[R];
     __shared__ double error[R];
     __shared__ int unsure[R], flag;
+    __shared__ unsigned char lists[DOTS ? NT / 32 : 1][ROW_TILE];
     constexpr int NG = NT / R;                                   // threads of a row's group
-    const int mp = P.mp, ntiles = mp / ROW_TILE, tid = threadIdx.x, lane = tid & 31;
+    const int mp = P.mp, ntiles = mp / ROW_TILE, tid = threadIdx.x, lane = tid & 31, xd = dots_xd(P.d);
     double *tiles64 = reinterpret_cast<double *>(smem);
     float *w_all = reinterpret_cast<float *>(tiles64 + (ntiles + 1) / 2 * 2);
     float *h = w_all + (size_t)R * mp;
     u64 *xs = reinterpret_cast<u64 *>(h + mp);
-    float *x1 = reinterpret_cast<float *>(xs), *tiles_all = x1 + (DOTS ? (P.d + 3) / 4 * 4 : 2 * R * P.d);
+    float *x1 = reinterpret_cast<float *>(xs), *tiles_all = x1 + (DOTS ? R * xd : 2 * R * P.d);
     const int g = tid / NG;
     const RowGroup G = {tid % NG, NG, 1 + g, &sc[g]}, all = {tid, NT, 0, &sc[0]};
     float *w = w_all + (size_t)g * mp, *tiles = tiles_all + (size_t)g * ntiles;
+    constexpr float u24 = 5.9604645e-8f;
 
     const int per_lane = (P.rows + R - 1) / R;
     const long long total = (long long)P.lanes * per_lane, first = total * blockIdx.x / gridDim.x, last = total * (blockIdx.x + 1) / gridDim.x;
     int at_lane = -1;
-    float y_max = 0.f;
+    float y_max = 0.f, y_prefix = 0.f;
+    double h_top = 0.0;
     bool some = false;
     for (long long t = first; t < last; ++t) {
         const int wl = (int)(t / per_lane), r0 = (int)(t % per_lane) * R, lanew = P.lane0 + wl, i0 = P.row0 + r0;
         const int rows = min(R, P.rows - r0);
         const size_t row0 = (size_t)lanew * P.n + i0;
         const Lane L = lane_of(P, lanew);
+        const double *hn = P.hn + (size_t)lanew * mp;
         if (!L.ok) {
             for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, NT);
             continue;
         }
         if (lanew != at_lane) {
             // the lane's largest k g_j (- |y_j|^2), and the others less that
-            const double *hn = P.hn + (size_t)lanew * mp;
             double top = -CUDART_INF;
-            float far = 0.f;
+            float far = 0.f, prefix = 0.f;
             for (int j = tid; j < mp; j += NT) {
                 top = fmax(top, hn[j]);
-                if (DOTS) far = fmaxf(far, P.yn[(size_t)lanew * mp + j]);
+                if (DOTS) {
+                    const float2 s = P.yn[(size_t)lanew * mp + j];
+                    far = fmaxf(far, s.x);
+                    prefix = fmaxf(prefix, s.y);
+                }
             }
-            top = all.largest(top);
-            if (DOTS) y_max = sqrtf(all.largest(far));
-            some = top != -CUDART_INF;
-            for (int j = tid; j < mp; j += NT) h[j] = some ? (float)(hn[j] - top) : 0.f;
+            h_top = all.largest(top);
+            if (DOTS) { y_max = sqrtf(all.largest(far)); y_prefix = sqrtf(all.largest(prefix)); }
+            some = h_top != -CUDART_INF;
+            for (int j = tid; j < mp; j += NT) h[j] = some ? (float)(hn[j] - h_top) : 0.f;
             at_lane = lanew;
         }
         if (!some) {
@@ -367,8 +511,8 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1) draw_kernel(const Draw 
         if (tid < R) unsure[tid] = 0;
         __syncthreads();
         const float k2 = (float)L.k2;
+        const float *yt = P.yt + (size_t)lanew * P.d * mp;
         if (!DOTS) {
-            const float *yt = P.yt + (size_t)lanew * P.d * mp;
             // rows too short for all threads to have four columns of them: fewer rows to a thread
             if constexpr (R == 8) {
                 if (mp > 512) form_rows<R, NT, 8>(yt, h, xs, w_all, mp, P.d, k2);
@@ -405,45 +549,81 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 3 : 1) draw_kernel(const Draw 
             top = G.largest(top);
             // nothing left in fp32's range, a NaN or an infinite exponent: float64 tells which
             bool sure = false;
-            double delta = CUDART_INF;
+            double off = CUDART_INF;
             if (top != -CUDART_INF_F) {
                 G.sync();
-                double mass = 0.0;
-                int count = 0;
+                RowSums sums = {0.0, 0.0, 0, 1.f};
+                float depth = 0.f;
                 for (int q = G.t >> 5; q < ntiles; q += NG >> 5) {
                     float *p = w + q * ROW_TILE + 4 * lane, v[4];
                     load4(p, v);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) { v[i] = ex2_fast(v[i] - top); count += v[i] > 0.f; }
+                    for (int i = 0; i < 4; ++i) {
+                        const float below = top - v[i];
+                        v[i] = ex2_fast(-below);
+                        sums.count += v[i] > 0.f;
+                        depth += v[i] > 0.f ? v[i] * below : 0.f;
+                    }
                     *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
                     float s = (v[0] + v[1]) + (v[2] + v[3]);
-                    mass += (double)s;
+                    sums.mass += (double)s;
 #pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                     if (lane == 0) tiles[q] = s;
                 }
-                G.add(mass, count);
-                if (mass <= 3e38) {
-                    const float A = fabsf(top) + 24.f, u24 = 5.9604645e-8f;
-                    float e;
+                sums.depth = (double)depth;
+                int unused = 0;
+                G.add(sums.mass, sums.count);
+                G.add(sums.depth, unused);
+                if (sums.mass <= 3e38) {
+                    const float A = fabsf(top), adds = u24 * (float)(8 + mp / (4 * NG));
+                    float fixed, slope, x_norm = 0.f;               // of an exponent: fixed + slope q
                     if (DOTS) {
-                        const float b = 2.f * k2 * sqrtf(P.xn[row]) * y_max;
-                        e = ((float)(P.d / 16 + 2) * 2.f + 3.f) * u24 * b + 3.f * u24 * A;
-                    } else e = (float)(P.d + 6) * u24 * A;
-                    delta = 2.0 * (0.6932 * (double)e + 2.384e-7 + (double)u24 * (8 + mp / (4 * NG)));
-                    sure = true;
-                    RowCut<float> cut = {0.f, -1, mass, count, 1.f};
-                    if (L.cuts.k < count || L.cuts.p < 1.0 || L.cuts.r > 0.f) {
-                        G.sync();
-                        sure = row_cut(w, mp, G, L.cuts, mass, count, delta, cut, tiles);
+                        const float2 xn = P.xn[row];
+                        x_norm = sqrtf(xn.x);
+                        const float b = 2.f * k2 * x_norm * y_max, bp = 2.f * k2 * sqrtf(xn.y) * y_prefix;
+                        slope = 3.f * u24;
+                        fixed = u24 * (2.f * (float)((P.d + 15) / 16) * bp + 7.f * b + 3.f * A);
+                    } else {
+                        slope = (float)(P.d + 6) * u24;
+                        fixed = slope * A;
                     }
-                    if (sure) {
+                    fixed = 0.6932f * fixed + 2.4e-7f;
+                    slope = 0.6932f * (slope + u24);
+                    // (twice the single errors, see RowError)
+                    RowError err = {2.0 * ((double)(fixed + adds) * sums.mass + (double)slope * sums.depth), 2.f * fixed, 2.f * slope};
+                    sure = decide_fast(P, G, L.cuts, row, w, tiles, sums, err, 0.f);
+                    off = (double)fixed + 24.0 * (double)slope;
+                    sure = __all_sync(0xffffffffu, sure);
+                    if (NG > 32) {
+                        if (G.t == 0) G.sc->band[0] = 1;
                         G.sync();
-                        sure = draw_all(P, row, w, cut, tiles, delta, G.t >> 5, NG >> 5);
+                        if (!sure) G.sc->band[0] = 0;
+                        G.sync();
+                        sure = G.sc->band[0] != 0;
+                        G.sync();
+                    }
+                    if (!sure && off < 0.01) {
+                        // once more, with better weights for what counts
+                        const double base = h_top + (double)top;
+                        if (DOTS) {
+                            float *x = x1 + (size_t)g * xd;
+                            for (int k = G.t; k < xd; k += NG) x[k] = k < P.d ? raw_value(P.x, P.x4, P.dtype, row, P.d, k) : 0.f;
+                            // twice to four times the bound, and half as much again: sums within the bound stay in its binade
+                            const float magic = 1.5f * __uint_as_float((__float_as_uint(x_norm * y_max * 4.f) & 0x7f800000u) + 0x00800000u);
+                            G.sync();
+                            refine_products(P, L.k2, lanew, hn, x, magic, base, w, lists[tid >> 5], G.t >> 5, NG >> 5);
+                        } else refine_differences(P, L.k2, hn, yt, x1 + 2 * g, 2 * R, base, w, G.t >> 5, NG >> 5);
+                        G.sync();
+                        sums = sum_row(G, w, tiles, ntiles);
+                        // weights good to fp32's rounding and the exponential's; those below 2^-22 as they were
+                        const double rest = (double)ROW_FLOOR * (double)mp;
+                        err = {2.0 * (((double)adds + 2.4e-7 + 24.0 * u24) * sums.mass + rest * off), 2.f * (2.4e-7f + 24.f * u24), 0.f};
+                        if (sums.mass <= 3e38) sure = decide_fast(P, G, L.cuts, row, w, tiles, sums, err, 2.f * ROW_FLOOR);
                     }
                 }
             }
-            if (!sure && lane == 0) { unsure[g] = 1; error[g] = delta; }
+            if (!sure && lane == 0) { unsure[g] = 1; error[g] = off; }
         }
         __syncthreads();
         for (int r = 0; r < rows; ++r) {
@@ -517,8 +697,8 @@ size_t carve(Draw &P, const Plan &p, char *base)
     auto take = [&](size_t bytes) { char *q = base ? base + at : nullptr; at += (bytes + 255) / 256 * 256; return q; };
     P.hn = (double *)take((size_t)P.W * P.mp * 8);
     if (p.dots && p.R) {
-        P.yn = (float *)take((size_t)P.W * P.mp * 4);
-        P.xn = (float *)take((size_t)P.W * P.n * 4);
+        P.yn = (float2 *)take((size_t)P.W * P.mp * 8);
+        P.xn = (float2 *)take((size_t)P.W * P.n * 8);
         P.dots = (const float *)take((size_t)p.lanes * p.rows * P.mp * 4);
     } else P.yt = (float *)take((size_t)P.W * P.d * P.mp * 4);
     P.scratch = (double *)take((size_t)(p.R ? DRAW_MAX_BLOCKS : DRAW_LONG_BLOCKS) * P.mp * 8);
@@ -531,8 +711,8 @@ void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
     // (the limit for any shape: another host thread may set it between this and the launch)
     cudaFuncSetAttribute(draw_kernel<R, NT, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(R == 8 ? DRAW_SMEM / 2 : DRAW_SMEM));
     const long long tiles = (long long)P.lanes * ((P.rows + R - 1) / R);
-    const size_t fit = NT > 256 ? 1 : std::min<size_t>(3, DRAW_SMEM / (p.smem + 10 * 1024));
-    const long long most = (long long)(DRAW_MAX_BLOCKS / 3 * fit);
+    const size_t fit = NT > 256 ? 1 : std::min<size_t>(2, DRAW_SMEM / (p.smem + 10 * 1024));
+    const long long most = (long long)(DRAW_MAX_BLOCKS / 2 * fit);
     draw_kernel<R, NT, DOTS><<<(unsigned)(tiles < most ? tiles : most), NT, p.smem, st>>>(P);
 }
 template <bool DOTS>

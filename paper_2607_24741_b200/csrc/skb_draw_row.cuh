@@ -6,10 +6,9 @@
 // the pivots, which are sorted.  Draws look for the first entry whose cumulative kept weight, in the order of the indices,
 // exceeds u times the total: by sums of 128 entries, then inside one of them.
 //
-// `Real` is float where the weights come from fp32 arithmetic.  Every comparison that decides something is then
-// checked against the error `delta` of a sum relative to the row's mass (and of a weight relative to itself), and a row with
-// a comparison inside it is `unsure`: its caller decides it again with weights in double and a smaller delta, or with
-// delta = 0, which takes what it finds.  Sums are in double above the 128 entries of a warp's load, and always added in one
+// `Real` is float where the weights are fp32.  Every comparison that decides something is then checked against bounds on
+// the errors (RowError), and a row with a comparison inside them is `unsure`: its caller decides it again with better
+// weights, in the end with exact ones, which takes what it finds.  Sums are in double above the 128 entries of a warp's load, and always added in one
 // order: results do not depend on timing.
 #pragma once
 #include <cuda_runtime.h>
@@ -90,6 +89,14 @@ struct RowCuts {
     float r;
 };
 
+// Bounds on what is compared: two sums of a row's weights are off by `sums` between them, two weights at 2^-q of the
+// largest by `weight + slope q` of themselves.  All zero: exact.
+struct RowError {
+    double sums;
+    float weight, slope;
+    __device__ __forceinline__ bool any() const { return sums != 0.0; }     // (a bound that is NaN: nothing is sure)
+};
+
 template <typename Real>
 struct RowCut {
     Real tau;
@@ -104,10 +111,10 @@ struct RowCut {
 // present cut has more.
 template <typename Real>
 __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const bool by_mass, const double target, RowCut<Real> &cut,
-                         const double delta, bool &unsure)
+                         const RowError &err, bool &unsure)
 {
     const RowCut<Real> old = cut;
-    Real lo = old.tau > 0 ? old.tau : weight_of((decltype(weight_bits(Real(0))))1), hi = weight_of(weight_bits(Real(1)) + 1);
+    Real lo = old.tau > 0 ? old.tau : weight_of((decltype(weight_bits(Real(0))))1), hi = Real(2);
     int n_lo = old.count, n_hi = 0;
     double m_hi = 0.0;
     bool first = true;
@@ -138,7 +145,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
     const int have = n_lo - n_hi, lane = G.t & 31;
     if (have > ROW_CAND) {
         // more than a warp of entries that all weigh lo: the first so many of them by index
-        if (delta > 0.0) { unsure = true; return; }
+        if (err.any()) { unsure = true; return; }
         double need = by_mass ? ceil((target - m_hi) / (double)lo) : target - n_hi;
         need = fmin(fmax(need, 1.0), (double)have);
         const int r = (int)need;
@@ -199,7 +206,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
     const unsigned reach = __ballot_sync(0xffffffffu, lane < n && (by_mass ? m_hi + sum : (double)(n_hi + lane + 1)) >= target);
     const int at = reach ? __ffs(reach) - 1 : n - 1;
     const double w_at = __shfl_sync(0xffffffffu, mine, at), m_at = m_hi + __shfl_sync(0xffffffffu, sum, at);
-    if (by_mass && delta > 0.0 && (m_at - target <= delta * old.mass || target - (m_at - w_at) <= delta * old.mass)) unsure = true;
+    if (by_mass && err.any() && !(m_at - target > err.sums && target - (m_at - w_at) > err.sums)) unsure = true;
     cut.tau = (Real)w_at;
     cut.J = __shfl_sync(0xffffffffu, j, at);
     cut.mass = m_at;
@@ -207,39 +214,38 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
 }
 
 // Cuts a row and leaves the sums of its tiles' kept weights in `tiles`.  `count` entries are above zero and have the mass
-// `mass`.  Returns false where the row is unsure.
+// `mass`, `top` is the largest (1 up to errors).  Returns false where the row is unsure.
 template <typename Real>
-__device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const RowCuts &want, const double mass, const int count,
-                        const double delta, RowCut<Real> &cut, Real *tiles)
+__device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const RowCuts &want, const Real top, const double mass, const int count,
+                        const RowError &err, RowCut<Real> &cut, Real *tiles)
 {
     bool unsure = false;
     cut.tau = 0; cut.J = -1; cut.mass = mass; cut.count = count; cut.lowest = 1;
     Real border[3] = {0, 0, 0};                 // of each cut that was made
     if (want.k < cut.count) {
-        row_find(w, mp, G, false, (double)want.k, cut, delta, unsure);
+        row_find(w, mp, G, false, (double)want.k, cut, err, unsure);
         border[0] = cut.tau;
     }
     if (unsure) return false;
     if (want.p < 1.0) {
-        row_find(w, mp, G, true, want.p * cut.mass, cut, delta, unsure);
+        row_find(w, mp, G, true, want.p * cut.mass, cut, err, unsure);
         border[1] = cut.tau;
     }
     if (unsure) return false;
     if (want.r > 0.f) {
-        if ((Real)want.r > cut.tau) { cut.tau = (Real)want.r; cut.J = 0x7fffffff; }
-        border[2] = (Real)want.r;
+        border[2] = (Real)want.r * top;
+        if (border[2] > cut.tau) { cut.tau = border[2]; cut.J = 0x7fffffff; }
     }
 #pragma unroll
     for (int q = 0; q < 3; ++q)
         if (border[q] > 0 && border[q] < cut.lowest) cut.lowest = border[q];
-    const bool look = delta > 0.0 && (border[0] > 0 || border[1] > 0 || border[2] > 0);
+    const bool look = err.any() && (border[0] > 0 || border[1] > 0 || border[2] > 0);
     Real low[3], high[3];
     int near_[3] = {0, 0, 0};
     if (look) {
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
-            // a weight's own relative error grows with its exponent's size
-            const double e = border[q] > 0 ? delta * (1.0 - (double)log2f((float)border[q]) / 24.0) : 0.0;
+            const double e = border[q] > 0 ? (double)(err.weight - err.slope * fminf(log2f((float)border[q]), 0.f)) : 0.0;
             low[q] = (Real)(border[q] * (1.0 - e));
             high[q] = border[q] > 0 ? (Real)(border[q] * (1.0 + e)) : Real(-1);
         }
@@ -295,7 +301,7 @@ __device__ __forceinline__ double row_total(const Real *tiles, const int ntiles)
 // One draw, by one warp: the entry's index and weight.  Returns false where it is unsure.
 template <typename Real>
 __device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const Real *tiles, const int ntiles, const double total, const double u,
-                         const double delta, int &index, double &weight)
+                         const RowError &err, int &index, double &weight)
 {
     const int lane = threadIdx.x & 31;
     const double target = u * total;
@@ -319,6 +325,9 @@ __device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const Real *til
         base += __shfl_sync(0xffffffffu, s, 31);
         if (over) break;
     }
+    index = -1;
+    weight = 0.0;
+    if (tile < 0) return false;                      // no weight at all, or none that is a number
     const int j = tile * ROW_TILE + 4 * lane;
     Real v[4];
     load4(w + j, v);
@@ -347,7 +356,7 @@ __device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const Real *til
     index = __shfl_sync(0xffffffffu, at_j, who);
     weight = __shfl_sync(0xffffffffu, at_w, who);
     const double end = __shfl_sync(0xffffffffu, at_run, who);
-    return !(delta > 0.0) || (end - target > delta * total && target - (end - weight) > delta * total);
+    return !err.any() || (end - target > err.sums && target - (end - weight) > err.sums);
 }
 
 }  // namespace skb
