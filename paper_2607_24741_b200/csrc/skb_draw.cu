@@ -4,9 +4,10 @@
 // potential drops out.  The plan is not stored: a block forms the weights of a few rows in shared memory, cuts and draws, and
 // goes on to the next rows.
 //
-// The indices are those of the definition in float64.  The weights are formed in fp32, with a bound on their error; a row in
-// which some comparison falls inside the bound is decided again by the whole block in float64, first with exact weights
-// for the entries above 2^-22 of the largest alone, then, should that not do, for all.
+// The indices are those of the definition in float64.  The weights are formed in fp32, with bounds on their errors, cut and drawn
+// from (skb_draw_quick.cuh).  A row in which some comparison falls inside the bounds is formed again, to fp32's last place,
+// where it weighs more than 2^-22 of its largest entry, and decided again with sums in double (skb_draw_row.cuh); what that
+// leaves open goes on a list, for a kernel that decides in float64 throughout.
 //
 // Two ways to the exponents:
 //   differences   |x - y|^2 in fp32 from a transposed copy of y, R rows to a block: two operations a dimension and pair,
@@ -20,6 +21,7 @@
 #include <limits.h>
 
 #include "skb_cloud4.cuh"
+#include "skb_draw_quick.cuh"
 #include "skb_draw_row.cuh"
 #include "skb_f32x2.cuh"
 #include "skb_operators.h"
@@ -27,8 +29,8 @@
 namespace skb {
 namespace {
 
-constexpr int DRAW_MAX_BLOCKS = 296;                 // 148 SMs, two blocks each: rows of scratch in the workspace
-constexpr int DRAW_LONG_BLOCKS = 148;
+constexpr int DRAW_BLOCKS = 148;                     // SMs; the fp32 kernel has one or two blocks on each
+constexpr int DRAW_EXACT_BLOCKS = 148;               // rows of scratch in the workspace
 constexpr float ROW_FLOOR = 2.384185791015625e-7f;   // 2^-22: weights that are formed again where fp32 does not do
 constexpr size_t DRAW_DOTS_BYTES = (size_t)64 << 20; // products that are held at a time: half of the L2 cache
 
@@ -46,7 +48,8 @@ struct Draw {
     float *yt;                                       // [W][d][mp] (differences)
     float2 *yn, *xn;                                 // [W][mp], [W][n] squared norms, and their means over prefixes (products)
     const float *dots;                               // rows row0 .. row0 + rows - 1 of lanes lane0 .. lane0 + lanes - 1
-    double *scratch;                                 // [blocks][mp]
+    double *scratch;                                 // [blocks][mp] weights of rows in float64
+    long long *list;                                 // rows that are open: their number, then which; null: all rows
     long long ldo;
     int lane0, lanes, row0, rows;
 };
@@ -83,6 +86,7 @@ __global__ void __launch_bounds__(256) transpose_kernel(const Draw P)
     __shared__ int masked[32];
     const int w = blockIdx.y, j0 = blockIdx.x * 32, tid = threadIdx.x, col = tid & 31, part = tid >> 5;
     const Lane L = lane_of(P, w);
+    if (P.list && blockIdx.x == 0 && w == 0 && tid == 0) P.list[0] = 0;
     if (tid < 32) {
         const int j = j0 + tid;
         const double g = j < P.m ? P.g[(size_t)w * P.m + j] : -CUDART_INF;
@@ -134,6 +138,7 @@ __global__ void __launch_bounds__(256) norms_kernel(const Draw P)
 {
     const int w = blockIdx.y, i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     double p = 0.0;
+    if (blockIdx.x == 0 && w == 0 && threadIdx.x == 0) P.list[0] = 0;
     if (i < P.mp) {
         const double g = i < P.m ? P.g[(size_t)w * P.m + i] : -CUDART_INF;
         const bool masked = g == -CUDART_INF;
@@ -158,7 +163,7 @@ __device__ __forceinline__ void put_draw(const Draw &P, size_t at, int index, fl
 
 // Draws of one row from weights and their cut, shared out to the group's warps.  True if all of this warp's were sure.
 template <typename Real>
-__device__ bool draw_all(const Draw &P, size_t row, const Real *w, const RowCut<Real> &cut, const Real *tiles, const RowError &err, int warp, int warps)
+__device__ bool draw_all(const Draw &P, size_t row, const Real *w, const RowCut<Real> &cut, const double *tiles, const RowError &err, int warp, int warps)
 {
     const double total = row_total(tiles, P.mp / ROW_TILE);
     bool sure = true;
@@ -179,26 +184,50 @@ __device__ void draw_none(const Draw &P, size_t row, int t, int nt)
     for (int s = t; s < P.S; s += nt) put_draw(P, row * P.S + s, -1, CUDART_NAN_F);
 }
 
-// One row in float64 by the whole block.  wf32, error: the row's fp32 weights, null if there are none, and a bound on their relative error.
-// xs: the point's coordinates times `sign`, `step` floats apart.
-__device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int i, const float *xs, int step, double sign, const float *wf32, double error,
-                                        double *wd, double *tiles, RowScratch *sc, int *flag)
+// Eight dimensions of point `row` from k on, k a multiple of 8; zeros past the last (k < the padded depth).
+__device__ __forceinline__ void eight_values(const void *data, const Cloud4 &c, int dtype, size_t row, int d, int k, float (&v)[8])
 {
-    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5;
-    const RowGroup G = {tid, nt, 0, sc};
-    const size_t row = (size_t)w * P.n + i;
-    const double *hn = P.hn + (size_t)w * P.mp;
-    for (int tier = wf32 && error < 0.01 ? 0 : 1; tier < 2; ++tier) {
-        const float *wf = tier == 0 ? wf32 : nullptr;
+    if (dtype == SKB_BF16) {
+        const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
+        const uint32_t b[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(b[i] << 16); v[2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u); }
+    } else {
+        const uint32_t b = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
+        const float s = cloud4_scale(c, row, k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e2m1_value(b >> (4 * i)) * s;
+    }
+}
+__host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
+
+// Rows in float64, a block to a row: those of the list, or all (rows too long for shared memory).
+__global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowScratch sc;
+    double *tiles = reinterpret_cast<double *>(smem), *xs = tiles + P.mp / ROW_TILE, *wd = P.scratch + (size_t)blockIdx.x * P.mp;
+    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, xd = dots_xd(P.d);
+    const RowGroup G = {tid, nt, 0, &sc};
+    const long long rows = P.list ? P.list[0] : (long long)P.W * P.n;
+    for (long long t = blockIdx.x; t < rows; t += gridDim.x) {
+        const long long row = P.list ? P.list[1 + t] : t;
+        const int w = (int)(row / P.n);
+        const Lane L = lane_of(P, w);
+        const double *hn = P.hn + (size_t)w * P.mp;
+        __syncthreads();
+        if (!L.ok) { draw_none(P, (size_t)row, tid, nt); continue; }
+        for (int k = tid; k < xd; k += nt) xs[k] = k < P.d ? (double)raw_value(P.x, P.x4, P.dtype, (size_t)row, P.d, k) : 0.0;
+        __syncthreads();
         double top = -CUDART_INF;
         int bad = 0;
         if (P.yt) {
             const float *yt = P.yt + (size_t)w * P.d * P.mp;
             for (int j = tid; j < P.mp; j += nt) {
-                if (wf && !(wf[j] > ROW_FLOOR)) continue;
                 double c = 0.0;
+#pragma unroll 4
                 for (int k = 0; k < P.d; ++k) {
-                    const double e = sign * (double)xs[k * step] - (double)yt[(size_t)k * P.mp + j];
+                    const double e = xs[k] - (double)yt[(size_t)k * P.mp + j];
                     c = fma(e, e, c);
                 }
                 const double z = hn[j] == -CUDART_INF ? -CUDART_INF : fma(-L.k2, c, hn[j]);
@@ -207,59 +236,51 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
                 bad |= !(z <= 1.7e308);
             }
         } else {
-            for (int j = warp; j < P.mp; j += nt >> 5) {
-                if (wf && !(wf[j] > ROW_FLOOR)) continue;
-                double z = -CUDART_INF;
-                if (hn[j] != -CUDART_INF) {
-                    double c = 0.0;
-                    for (int k = lane; k < P.d; k += 32) {
-                        const double e = sign * (double)xs[k * step] - (double)raw_value(P.y, P.y4, P.dtype, (size_t)w * P.m + j, P.d, k);
-                        c = fma(e, e, c);
-                    }
+            // eight threads to a point, four points to a warp
+            const int part = lane & 7, chunks = P.dtype == SKB_BF16 ? P.d / 8 : xd / 8;
+            for (int j0 = 4 * warp; j0 < P.mp; j0 += 4 * (nt >> 5)) {
+                const int j = j0 + (lane >> 3);
+                const bool is = hn[j] != -CUDART_INF;
+                double c = 0.0;
+                if (is) {
+#pragma unroll 4
+                    for (int q = part; q < chunks; q += 8) {
+                        float y[8];
+                        eight_values(P.y, P.y4, P.dtype, (size_t)w * P.m + j, P.d, 8 * q, y);
 #pragma unroll
-                    for (int off = 16; off > 0; off >>= 1) c += __shfl_xor_sync(0xffffffffu, c, off);
-                    z = L.k2 * (P.g[(size_t)w * P.m + j] - c);
+                        for (int i = 0; i < 8; ++i) { const double e = xs[8 * q + i] - (double)y[i]; c = fma(e, e, c); }
+                    }
                 }
-                if (lane == 0) wd[j] = z;
+#pragma unroll
+                for (int off = 1; off < 8; off *= 2) c += __shfl_xor_sync(0xffffffffu, c, off);
+                const double z = is ? L.k2 * (P.g[(size_t)w * P.m + j] - c) : -CUDART_INF;
+                if (part == 0) wd[j] = z;
                 top = fmax(top, z);
                 bad |= !(z <= 1.7e308);
             }
         }
-        double some = 0.0;
+        double mass = 0.0;
+        int count = 0;
         top = G.largest(top);
-        G.add(some, bad);                                           // (a barrier: wd is written)
-        if (bad || top == -CUDART_INF) { draw_none(P, row, tid, nt); return; }
-        double mass = 0.0, rest = 0.0;
-        int count = 0, unused = 0;
+        G.add(mass, bad);                                           // (a barrier: wd is written)
+        if (bad || top == -CUDART_INF) { draw_none(P, (size_t)row, tid, nt); continue; }
         for (int j = tid; j < P.mp; j += nt) {
-            double v;
-            if (wf && !(wf[j] > ROW_FLOOR)) { v = (double)wf[j]; rest += v; }
-            else v = exp2(wd[j] - top);
+            const double v = exp2(wd[j] - top);
             wd[j] = v;
             mass += v;
             count += v > 0.0;
         }
         G.add(mass, count);
-        G.add(rest, unused);
-        RowError err = {0.0, 0.f, 0.f};
-        if (tier == 0) err = {4.0 * error * rest + 1e-12 * mass, 1e-12f, 0.f};
+        const RowError none = {0.0, 0.f, 0.f};
         RowCut<double> cut;
-        bool sure = row_cut(wd, P.mp, G, L.cuts, 1.0, mass, count, err, cut, tiles);
-        if (sure && tier == 0 && cut.lowest < 2.f * ROW_FLOOR) sure = false;
-        if (sure) {
-            if (tid == 0) *flag = 0;
-            __syncthreads();
-            if (!draw_all(P, row, wd, cut, tiles, err, warp, nt >> 5) && lane == 0) *flag = 1;
-            __syncthreads();
-            sure = *flag == 0;
-        }
+        row_cut(wd, P.mp, G, L.cuts, 1.0, mass, count, none, cut, tiles);
+        draw_all(P, (size_t)row, wd, cut, tiles, none, warp, nt >> 5);
         __syncthreads();
-        if (sure) return;
     }
 }
 
 // R rows of a lane at a time, NT threads: weights in shared memory by all threads, then a group of NT / R threads to a row.
-//   w [R][mp], tiles [R][mp / 128], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
+//   tiles [R][mp / 128], w [R][mp], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
 //   (differences), or x [R][xd] of rows that are formed again (products)
 // Error of an exponent t = log2 w at a depth q below the row's largest, A = |largest t|:
 //   differences  h <= 0 and the scaled distance h - t are at most A + q; d + 2 roundings of the distance, three of the
@@ -269,12 +290,11 @@ __device__ __noinline__ void decide_row(const Draw &P, const Lane &L, int w, int
 //                cuts off where it adds products to a sum: a unit in the last place of the sum, at most 2^-23 of it, for each 16, and
 //                two more: (d / 16) B' 2^-23 + 2 B 2^-23; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
 // The exponential adds 2^-22 and 2^-24 q of the difference that it is taken of, the additions of weights 2^-24 each.
-__host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
 template <int R, int NT>
 struct DrawShape {
     static size_t smem(int mp, int d, bool dots)
     {
-        return (size_t)mp / ROW_TILE * 8 + (size_t)R * (mp + mp / ROW_TILE) * 4 + (size_t)mp * 4 + (dots ? (size_t)R * dots_xd(d) * 4 : (size_t)R * d * 8);
+        return (size_t)R * (mp / ROW_TILE * 8 + (size_t)mp * 4) + (size_t)mp * 4 + (dots ? (size_t)R * dots_xd(d) * 4 : (size_t)R * d * 8);
     }
 };
 
@@ -315,28 +335,29 @@ __device__ __forceinline__ void form_rows(const float *yt, const float *h, const
     }
 }
 
-// Tiles' sums, mass, number and largest of a row's weights, and the sum of w log2(1 / w).
+// Mass, number and largest of a row's weights, and the mass of those at most ROW_FLOOR.
 struct RowSums {
-    double mass, depth;
+    double mass, rest;
     int count;
     float top;
 };
-__device__ __forceinline__ RowSums sum_row(const RowGroup &G, const float *w, float *tiles, int ntiles)
+__device__ __forceinline__ RowSums sum_row(const RowGroup &G, const float *w, int mp)
 {
     RowSums r = {0.0, 0.0, 0, 0.f};
-    const int lane = G.t & 31;
-    for (int q = G.t >> 5; q < ntiles; q += G.nt >> 5) {
+    for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
         float v[4];
-        load4(w + q * ROW_TILE + 4 * lane, v);
-        float s = (v[0] + v[1]) + (v[2] + v[3]);
-        r.mass += (double)s;
+        load4(w + j, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { r.count += v[i] > 0.f; r.top = fmaxf(r.top, v[i]); }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        if (lane == 0) tiles[q] = s;
+        for (int i = 0; i < 4; ++i) {
+            r.mass += (double)v[i];
+            r.rest += v[i] > ROW_FLOOR ? 0.0 : (double)v[i];
+            r.count += v[i] > 0.f;
+            r.top = fmaxf(r.top, v[i]);
+        }
     }
+    int unused = 0;
     G.add(r.mass, r.count);
+    G.add(r.rest, unused);
     r.top = G.largest(r.top);
     return r;
 }
@@ -362,23 +383,8 @@ __device__ __forceinline__ void refine_differences(const Draw &P, double k2, con
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (v[i] > ROW_FLOOR) v[i] = ex2_fast((float)(fma(-k2, c[i], hn[j + i]) - base));
+            if (v[i] > ROW_FLOOR) v[i] = (float)exp2(fma(-k2, c[i], hn[j + i]) - base);
         *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
-    }
-}
-// Eight dimensions of point `row` from k on, k a multiple of 8; zeros past the last (k < the padded depth).
-__device__ __forceinline__ void eight_values(const void *data, const Cloud4 &c, int dtype, size_t row, int d, int k, u64 (&v)[4])
-{
-    if (dtype == SKB_BF16) {
-        const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
-        const uint32_t b[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = pack2(__uint_as_float(b[i] << 16), __uint_as_float(b[i] & 0xffff0000u));
-    } else {
-        const uint32_t b = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
-        const float s = cloud4_scale(c, row, k);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = pack2(e2m1_value(b >> (8 * i)) * s, e2m1_value(b >> (8 * i + 4)) * s);
     }
 }
 // x . y of four points of y at a time, eight threads to a point.  Products are exact in fp32 (at most 16 bits).  They are
@@ -405,15 +411,16 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             const size_t row = (size_t)wl * P.m + j;
             const u64 m2 = pack2(magic, magic);
             u64 sum = m2, low = 0ull;
+#pragma unroll 4
             for (int c = part; c < chunks; c += 8) {
-                u64 y[4];
+                float y[8];
                 eight_values(P.y, P.y4, P.dtype, row, P.d, 8 * c, y);
                 const ulonglong2 xa = reinterpret_cast<const ulonglong2 *>(x + 8 * c)[0], xb = reinterpret_cast<const ulonglong2 *>(x + 8 * c)[1];
                 const u64 xv[4] = {xa.x, xa.y, xb.x, xb.y};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const u64 t = fma2(xv[i], y[i], sum);
-                    low = add2(low, fma2(xv[i], y[i], sub2(sum, t)));
+                    const u64 yv = pack2(y[2 * i], y[2 * i + 1]), t = fma2(xv[i], yv, sum);
+                    low = add2(low, fma2(xv[i], yv, sub2(sum, t)));
                     sum = t;
                 }
             }
@@ -423,24 +430,56 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             double dot = ((double)a + (double)b) + ((double)la + (double)lb);
 #pragma unroll
             for (int off = 1; off < 8; off *= 2) dot += __shfl_xor_sync(0xffffffffu, dot, off);
-            if (part == 0 && e0 + col < n) w[j] = ex2_fast((float)(fma(2.0 * k2, dot, hn[j]) - base));
+            if (part == 0 && e0 + col < n) w[j] = (float)exp2(fma(2.0 * k2, dot, hn[j]) - base);
         }
         __syncwarp();
     }
 }
 
-// Cuts a row of fp32 weights and draws from it; false if something is unsure.  The bounds hold for weights above `floor_`.
-__device__ __forceinline__ bool decide_fast(const Draw &P, const RowGroup &G, const RowCuts &cuts, size_t row, const float *w, float *tiles,
-                                            const RowSums &sums, const RowError &err, float floor_)
+// Sums of two floats and a count over the group, added in one order.
+__device__ __forceinline__ void group_sums(const RowGroup &G, float &a, float &b, unsigned &n, int &turn)
 {
-    RowCut<float> cut = {0.f, -1, sums.mass, sums.count, 1.f};
-    G.sync();
-    if (cuts.k < sums.count || cuts.p < 1.0 || cuts.r > 0.f) {
-        if (!row_cut(w, P.mp, G, cuts, sums.top, sums.mass, sums.count, err, cut, tiles)) return false;
-        if (cut.lowest < floor_) return false;
-        G.sync();
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+        a += __shfl_xor_sync(0xffffffffu, a, off);
+        b += __shfl_xor_sync(0xffffffffu, b, off);
     }
-    return draw_all(P, row, w, cut, tiles, err, G.t >> 5, G.nt >> 5);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (G.nt == 32) return;
+    turn ^= 1;
+    if ((G.t & 31) == 0) {
+        unsigned *p = G.sc->part[turn][G.t >> 5];
+        p[0] = __float_as_uint(a); p[1] = __float_as_uint(b); p[2] = n;
+    }
+    G.sync();
+    a = b = 0.f;
+    n = 0;
+    for (int q = 0; q < G.nt >> 5; ++q) {
+        const unsigned *p = G.sc->part[turn][q];
+        a += __uint_as_float(p[0]); b += __uint_as_float(p[1]); n += p[2];
+    }
+}
+__device__ __forceinline__ float group_largest(const RowGroup &G, float v, int &turn)
+{
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+    if (G.nt == 32) return v;
+    turn ^= 1;
+    if ((G.t & 31) == 0) G.sc->part[turn][G.t >> 5][0] = __float_as_uint(v);
+    G.sync();
+    for (int q = 0; q < G.nt >> 5; ++q) v = fmaxf(v, __uint_as_float(G.sc->part[turn][q][0]));
+    return v;
+}
+// Whether all warps of the group say so.
+__device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
+{
+    v = __all_sync(0xffffffffu, v);
+    if (G.nt == 32) return v;
+    turn ^= 1;
+    if ((G.t & 31) == 0) G.sc->part[turn][G.t >> 5][0] = v;
+    G.sync();
+    for (int q = 0; q < G.nt >> 5; ++q) v = v && G.sc->part[turn][q][0] != 0;
+    return v;
 }
 
 template <int R, int NT, bool DOTS>
@@ -448,24 +487,24 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc[R];
-    __shared__ double error[R];
-    __shared__ int unsure[R], flag;
     __shared__ unsigned char lists[DOTS ? NT / 32 : 1][ROW_TILE];
     constexpr int NG = NT / R;                                   // threads of a row's group
     const int mp = P.mp, ntiles = mp / ROW_TILE, tid = threadIdx.x, lane = tid & 31, xd = dots_xd(P.d);
-    double *tiles64 = reinterpret_cast<double *>(smem);
-    float *w_all = reinterpret_cast<float *>(tiles64 + (ntiles + 1) / 2 * 2);
+    double *tiles_all = reinterpret_cast<double *>(smem);
+    float *w_all = reinterpret_cast<float *>(tiles_all + (R * ntiles + 1) / 2 * 2);
     float *h = w_all + (size_t)R * mp;
     u64 *xs = reinterpret_cast<u64 *>(h + mp);
-    float *x1 = reinterpret_cast<float *>(xs), *tiles_all = x1 + (DOTS ? R * xd : 2 * R * P.d);
+    float *x1 = reinterpret_cast<float *>(xs);
     const int g = tid / NG;
     const RowGroup G = {tid % NG, NG, 1 + g, &sc[g]}, all = {tid, NT, 0, &sc[0]};
-    float *w = w_all + (size_t)g * mp, *tiles = tiles_all + (size_t)g * ntiles;
+    float *w = w_all + (size_t)g * mp;
+    double *tiles = tiles_all + (size_t)g * ntiles;
+    unsigned *units = reinterpret_cast<unsigned *>(tiles);       // (never at the same time)
     constexpr float u24 = 5.9604645e-8f;
 
     const int per_lane = (P.rows + R - 1) / R;
     const long long total = (long long)P.lanes * per_lane, first = total * blockIdx.x / gridDim.x, last = total * (blockIdx.x + 1) / gridDim.x;
-    int at_lane = -1;
+    int at_lane = -1, turn = 0;
     float y_max = 0.f, y_prefix = 0.f;
     double h_top = 0.0;
     bool some = false;
@@ -481,6 +520,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
         }
         if (lanew != at_lane) {
             // the lane's largest k g_j (- |y_j|^2), and the others less that
+            __syncthreads();
             double top = -CUDART_INF;
             float far = 0.f, prefix = 0.f;
             for (int j = tid; j < mp; j += NT) {
@@ -496,23 +536,21 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
             some = h_top != -CUDART_INF;
             for (int j = tid; j < mp; j += NT) h[j] = some ? (float)(hn[j] - h_top) : 0.f;
             at_lane = lanew;
+            __syncthreads();
         }
         if (!some) {
             for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, NT);
             continue;
         }
+        const float k2 = (float)L.k2;
+        const float *yt = P.yt + (size_t)lanew * P.d * mp;
         if (!DOTS) {
             for (int q = tid; q < R * P.d; q += NT) {
                 const int r = q / P.d, k = q % P.d;
                 const float v = r < rows ? -raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k) : 0.f;
                 xs[k * R + r] = pack2(v, v);
             }
-        }
-        if (tid < R) unsure[tid] = 0;
-        __syncthreads();
-        const float k2 = (float)L.k2;
-        const float *yt = P.yt + (size_t)lanew * P.d * mp;
-        if (!DOTS) {
+            __syncthreads();
             // rows too short for all threads to have four columns of them: fewer rows to a thread
             if constexpr (R == 8) {
                 if (mp > 512) form_rows<R, NT, 8>(yt, h, xs, w_all, mp, P.d, k2);
@@ -528,6 +566,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
             if (DOTS) {
                 const float *dots = P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo;
                 const float two_k = (float)(2.0 * L.k2);
+#pragma unroll 8
                 for (int j = 4 * G.t; j < mp; j += 4 * NG) {
                     float v[4], hh[4];
                     load4(dots + j, v);
@@ -540,43 +579,37 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
                     *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
                 }
             } else {
+#pragma unroll 4
                 for (int j = 4 * G.t; j < mp; j += 4 * NG) {
                     float v[4];
                     load4(w + j, v);
                     top = fmaxf(fmaxf(top, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
                 }
             }
-            top = G.largest(top);
+            top = group_largest(G, top, turn);
             // nothing left in fp32's range, a NaN or an infinite exponent: float64 tells which
             bool sure = false;
-            double off = CUDART_INF;
             if (top != -CUDART_INF_F) {
-                G.sync();
-                RowSums sums = {0.0, 0.0, 0, 1.f};
-                float depth = 0.f;
-                for (int q = G.t >> 5; q < ntiles; q += NG >> 5) {
-                    float *p = w + q * ROW_TILE + 4 * lane, v[4];
-                    load4(p, v);
+                float mass = 0.f, depth = 0.f;
+                unsigned count = 0;
+#pragma unroll 4
+                for (int j = 4 * G.t; j < mp; j += 4 * NG) {        // (each thread's own: no barrier yet)
+                    float v[4];
+                    load4(w + j, v);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const float below = top - v[i];
                         v[i] = ex2_fast(-below);
-                        sums.count += v[i] > 0.f;
+                        count += v[i] > 0.f;
                         depth += v[i] > 0.f ? v[i] * below : 0.f;
                     }
-                    *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-                    float s = (v[0] + v[1]) + (v[2] + v[3]);
-                    sums.mass += (double)s;
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                    if (lane == 0) tiles[q] = s;
+                    *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
+                    mass += (v[0] + v[1]) + (v[2] + v[3]);
                 }
-                sums.depth = (double)depth;
-                int unused = 0;
-                G.add(sums.mass, sums.count);
-                G.add(sums.depth, unused);
-                if (sums.mass <= 3e38) {
-                    const float A = fabsf(top), adds = u24 * (float)(8 + mp / (4 * NG));
+                group_sums(G, mass, depth, count, turn);
+                G.sync();
+                if (mass <= 3e38f) {
+                    const float A = fabsf(top), adds = u24 * (float)(12 + mp / (4 * NG));
                     float fixed, slope, x_norm = 0.f;               // of an exponent: fixed + slope q
                     if (DOTS) {
                         const float2 xn = P.xn[row];
@@ -590,75 +623,63 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
                     }
                     fixed = 0.6932f * fixed + 2.4e-7f;
                     slope = 0.6932f * (slope + u24);
-                    // (twice the single errors, see RowError)
-                    RowError err = {2.0 * ((double)(fixed + adds) * sums.mass + (double)slope * sums.depth), 2.f * fixed, 2.f * slope};
-                    sure = decide_fast(P, G, L.cuts, row, w, tiles, sums, err, 0.f);
-                    off = (double)fixed + 24.0 * (double)slope;
-                    sure = __all_sync(0xffffffffu, sure);
-                    if (NG > 32) {
-                        if (G.t == 0) G.sc->band[0] = 1;
-                        G.sync();
-                        if (!sure) G.sc->band[0] = 0;
-                        G.sync();
-                        sure = G.sc->band[0] != 0;
-                        G.sync();
-                    }
-                    if (!sure && off < 0.01) {
-                        // once more, with better weights for what counts
-                        const double base = h_top + (double)top;
-                        if (DOTS) {
-                            float *x = x1 + (size_t)g * xd;
-                            for (int k = G.t; k < xd; k += NG) x[k] = k < P.d ? raw_value(P.x, P.x4, P.dtype, row, P.d, k) : 0.f;
-                            // twice to four times the bound, and half as much again: sums within the bound stay in its binade
-                            const float magic = 1.5f * __uint_as_float((__float_as_uint(x_norm * y_max * 4.f) & 0x7f800000u) + 0x00800000u);
+                    // (twice the single errors, see RowError; the roundings to units)
+                    const float of_sums = 2.f * (fixed + adds + slope * depth / mass);
+                    const RowError err = {(double)of_sums, 2.f * fixed, 2.f * slope};
+                    const float off = fixed + 24.f * slope;
+                    if (off < 0.01f) {
+                        const float unit = QUICK_ONE / mass;
+                        const unsigned slack = (unsigned)(of_sums * QUICK_ONE) + 2 * NG + 32 * ntiles + 64;
+                        QuickCut cut;
+                        sure = quick_cut(w, mp, G, L.cuts, count, unit, slack, err, cut, turn);
+                        if (sure) {
+                            quick_tiles(w, ntiles, G, cut.tau, unit, units);
                             G.sync();
-                            refine_products(P, L.k2, lanew, hn, x, magic, base, w, lists[tid >> 5], G.t >> 5, NG >> 5);
-                        } else refine_differences(P, L.k2, hn, yt, x1 + 2 * g, 2 * R, base, w, G.t >> 5, NG >> 5);
-                        G.sync();
-                        sums = sum_row(G, w, tiles, ntiles);
-                        // weights good to fp32's rounding and the exponential's; those below 2^-22 as they were
-                        const double rest = (double)ROW_FLOOR * (double)mp;
-                        err = {2.0 * (((double)adds + 2.4e-7 + 24.0 * u24) * sums.mass + rest * off), 2.f * (2.4e-7f + 24.f * u24), 0.f};
-                        if (sums.mass <= 3e38) sure = decide_fast(P, G, L.cuts, row, w, tiles, sums, err, 2.f * ROW_FLOOR);
+                            const unsigned whole = quick_total(units, ntiles);
+                            for (int s = G.t >> 5; s < P.S; s += NG >> 5) {
+                                const float u = P.u[row * P.S + s];
+                                int j = -1;
+                                float wj = 0.f;
+                                if (u >= 0.f && u < 1.f && !quick_draw(w, ntiles, cut.tau, unit, units, whole, u, slack, j, wj)) { sure = false; continue; }
+                                if (lane == 0) put_draw(P, row * P.S + s, j, j < 0 ? CUDART_NAN_F : logf(wj * unit / (float)whole));
+                            }
+                        }
+                        sure = group_all(G, sure, turn);
+                        if (!sure) {
+                            // once more, with better weights for what counts
+                            const double base = h_top + (double)top;
+                            G.sync();
+                            if (DOTS) {
+                                float *x = x1 + (size_t)g * xd;
+                                for (int k = G.t; k < xd; k += NG) x[k] = k < P.d ? raw_value(P.x, P.x4, P.dtype, row, P.d, k) : 0.f;
+                                // twice to four times the bound, and half as much again: sums within the bound stay in its binade
+                                const float magic = 1.5f * __uint_as_float((__float_as_uint(x_norm * y_max * 4.f) & 0x7f800000u) + 0x00800000u);
+                                G.sync();
+                                refine_products(P, L.k2, lanew, hn, x, magic, base, w, lists[tid >> 5], G.t >> 5, NG >> 5);
+                            } else refine_differences(P, L.k2, hn, yt, x1 + 2 * g, 2 * R, base, w, G.t >> 5, NG >> 5);
+                            G.sync();
+                            const RowSums sums = sum_row(G, w, mp);
+                            if (sums.mass <= 3e38) {
+                                // weights rounded to fp32; those below 2^-22 as they were
+                                const RowError fine = {2.0 * ((double)u24 * sums.mass + sums.rest * off), 2.f * u24, 0.f};
+                                RowCut<float> rcut;
+                                sure = row_cut(w, mp, G, L.cuts, sums.top, sums.mass, sums.count, fine, rcut, tiles);
+                                if (rcut.lowest < 2.f * ROW_FLOOR) sure = false;
+                                if (sure) sure = draw_all(P, row, w, rcut, tiles, fine, G.t >> 5, NG >> 5);
+                                sure = group_all(G, sure, turn);
+                            }
+                        }
                     }
                 }
             }
-            if (!sure && lane == 0) { unsure[g] = 1; error[g] = off; }
+            if (!sure && G.t == 0) P.list[1 + (long long)atomicAdd((unsigned long long *)P.list, 1ull)] = (long long)row;
+            G.sync();
         }
-        __syncthreads();
-        for (int r = 0; r < rows; ++r) {
-            if (!unsure[r]) continue;
-            if (DOTS) {
-                for (int k = tid; k < P.d; k += NT) x1[k] = raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k);
-                __syncthreads();
-            }
-            decide_row(P, L, lanew, i0 + r, DOTS ? x1 : x1 + 2 * r, DOTS ? 1 : 2 * R, DOTS ? 1.0 : -1.0, w_all + (size_t)r * mp, error[r],
-                       P.scratch + (size_t)blockIdx.x * mp, tiles64, &sc[0], &flag);
-        }
-        __syncthreads();
+        if (!DOTS) __syncthreads();
     }
 }
 
-// Rows too long for shared memory: a block to a row, float64 throughout.
-__global__ void __launch_bounds__(512) draw_long_kernel(const Draw P)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ RowScratch sc;
-    __shared__ int flag;
-    double *tiles = reinterpret_cast<double *>(smem);
-    float *xs = reinterpret_cast<float *>(tiles + P.mp / ROW_TILE);
-    for (long long t = blockIdx.x; t < (long long)P.W * P.n; t += gridDim.x) {
-        const int w = (int)(t / P.n), i = (int)(t % P.n);
-        const Lane L = lane_of(P, w);
-        __syncthreads();
-        if (!L.ok) { draw_none(P, (size_t)t, threadIdx.x, blockDim.x); continue; }
-        for (int k = threadIdx.x; k < P.d; k += blockDim.x) xs[k] = raw_value(P.x, P.x4, P.dtype, (size_t)t, P.d, k);
-        __syncthreads();
-        decide_row(P, L, w, i, xs, 1, 1.0, nullptr, 0.0, P.scratch + (size_t)blockIdx.x * P.mp, tiles, &sc, &flag);
-    }
-}
-
-size_t long_smem(const Draw &P) { return (size_t)P.mp / ROW_TILE * 8 + (size_t)P.d * 4; }
+size_t exact_smem(const Draw &P) { return (size_t)P.mp / ROW_TILE * 8 + (size_t)dots_xd(P.d) * 8; }
 
 // How a problem is run: rows to a block, where the exponents come from, and the rows whose products are held at a time.
 struct Plan {
@@ -701,7 +722,8 @@ size_t carve(Draw &P, const Plan &p, char *base)
         P.xn = (float2 *)take((size_t)P.W * P.n * 8);
         P.dots = (const float *)take((size_t)p.lanes * p.rows * P.mp * 4);
     } else P.yt = (float *)take((size_t)P.W * P.d * P.mp * 4);
-    P.scratch = (double *)take((size_t)(p.R ? DRAW_MAX_BLOCKS : DRAW_LONG_BLOCKS) * P.mp * 8);
+    P.scratch = (double *)take((size_t)DRAW_EXACT_BLOCKS * P.mp * 8);
+    if (p.R) P.list = (long long *)take(((size_t)P.W * P.n + 1) * 8);
     return at;
 }
 
@@ -712,7 +734,7 @@ void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
     cudaFuncSetAttribute(draw_kernel<R, NT, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(R == 8 ? DRAW_SMEM / 2 : DRAW_SMEM));
     const long long tiles = (long long)P.lanes * ((P.rows + R - 1) / R);
     const size_t fit = NT > 256 ? 1 : std::min<size_t>(2, DRAW_SMEM / (p.smem + 10 * 1024));
-    const long long most = (long long)(DRAW_MAX_BLOCKS / 2 * fit);
+    const long long most = (long long)(DRAW_BLOCKS * fit);
     draw_kernel<R, NT, DOTS><<<(unsigned)(tiles < most ? tiles : most), NT, p.smem, st>>>(P);
 }
 template <bool DOTS>
@@ -776,15 +798,16 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
     carve(P, p, (char *)cfg->workspace);
     cudaStream_t st = (cudaStream_t)cfg->stream;
     if (!p.dots || !p.R) transpose_kernel<<<dim3(P.mp / 32, P.W), 256, 0, st>>>(P);
-    if (!p.R) {
+    auto exact_rows = [&] {
         const long long rows = (long long)P.W * P.n;
-        draw_long_kernel<<<(unsigned)(rows < DRAW_LONG_BLOCKS ? rows : DRAW_LONG_BLOCKS), 512, long_smem(P), st>>>(P);
+        draw_exact_kernel<<<(unsigned)(rows < DRAW_EXACT_BLOCKS ? rows : DRAW_EXACT_BLOCKS), 512, exact_smem(P), st>>>(P);
         return op_launched("plan_draw");
-    }
+    };
+    if (!p.R) return exact_rows();
     if (!p.dots) {
         P.lanes = P.W; P.rows = P.n;
         launch_draw<false>(P, p, st);
-        return op_launched("plan_draw");
+        return exact_rows();
     }
     norms_kernel<<<dim3((P.mp + P.n + 7) / 8, P.W), 256, 0, st>>>(P);
     P.ldo = P.mp;
@@ -798,5 +821,5 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
             if (s != SKB_OK) return s;
             launch_draw<true>(P, p, st);
         }
-    return op_launched("plan_draw");
+    return exact_rows();
 }

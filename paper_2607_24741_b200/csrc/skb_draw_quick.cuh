@@ -1,0 +1,230 @@
+// One row of fp32 weights cut and drawn from in a hurry: bounds on all errors known, sums as integers, no sorting.
+//
+// Sums are counted in units of 2^-30 of the row's mass: a thread adds its weights in fp32, rounds the sum to units, and the
+// warp's are added by one integer reduction, exactly and in no particular order.  A cut is found by three pivots at a time,
+// quarters of the bracket's bit patterns, until one weight is left in the bracket; two that are within their errors of each
+// other leave the row unsure, so no ties have to be ordered here.  skb_draw_row.cuh has the careful form of the same.
+#pragma once
+#include "skb_draw_row.cuh"
+
+namespace skb {
+
+constexpr float QUICK_ONE = 1073741824.f;                        // units of a row's mass
+
+// Sums over the group of N counts each thread has; the same in all threads.  `turn` alternates between two buffers, so that
+// one barrier does.
+template <int N>
+__device__ __forceinline__ void group_add(const RowGroup &G, unsigned (&v)[N], int &turn)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __reduce_add_sync(0xffffffffu, v[i]);
+    if (G.nt == 32) return;
+    turn ^= 1;
+    if ((G.t & 31) == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) G.sc->part[turn][G.t >> 5][i] = v[i];
+    G.sync();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        unsigned s = 0;
+        for (int q = 0; q < G.nt >> 5; ++q) s += G.sc->part[turn][q][i];
+        v[i] = s;
+    }
+}
+// Largest of a, b and smallest of c over the group, bit patterns of weights.
+__device__ __forceinline__ void group_extremes(const RowGroup &G, unsigned &a, unsigned &b, unsigned &c, int &turn)
+{
+    a = __reduce_max_sync(0xffffffffu, a);
+    b = __reduce_max_sync(0xffffffffu, b);
+    c = __reduce_min_sync(0xffffffffu, c);
+    if (G.nt == 32) return;
+    turn ^= 1;
+    if ((G.t & 31) == 0) { G.sc->part[turn][G.t >> 5][0] = a; G.sc->part[turn][G.t >> 5][1] = b; G.sc->part[turn][G.t >> 5][2] = c; }
+    G.sync();
+    for (int q = 0; q < G.nt >> 5; ++q) {
+        a = max(a, G.sc->part[turn][q][0]);
+        b = max(b, G.sc->part[turn][q][1]);
+        c = min(c, G.sc->part[turn][q][2]);
+    }
+}
+
+struct QuickCut {
+    float tau;                          // kept: weights from here on
+    unsigned count, mass;               // of what is kept; mass in units
+};
+
+// Shrinks the cut to the shortest head with `target` entries, or units of mass.  Returns false where it is unsure.
+__device__ __forceinline__ bool quick_find(const float *w, const int mp, const RowGroup &G, const bool by_mass, const unsigned target, const float unit,
+                                           const unsigned slack, const RowError &err, QuickCut &cut, int &turn)
+{
+    int lo = cut.tau > 0.f ? __float_as_int(cut.tau) : 1, hi = __float_as_int(2.f);
+    unsigned n_lo = cut.count, m_lo = cut.mass, n_hi = 0, m_hi = 0;
+    bool first = true;
+    while (n_lo - n_hi > 1) {
+        const int gap = hi - lo;
+        if (gap < 16) return false;                              // equal weights, or nearly
+        int p[3] = {lo + gap / 4, lo + gap / 2, lo + gap / 4 * 3};
+        if (first) {
+            // below (mass - target) / count there is less than mass - target: the border is above; and few rows need
+            // more than 2^-24 of their largest weight
+            const int b = by_mass ? __float_as_int((float)(m_lo - target) / ((float)n_lo * unit) * 0.999f) : __float_as_int(5.9604645e-8f);
+            if (b > lo && b < __float_as_int(0.25f)) {
+                const int gap1 = __float_as_int(1.f) - b;
+                p[0] = b; p[1] = b + gap1 / 3; p[2] = b + gap1 / 3 * 2;
+            }
+            first = false;
+        }
+        const float pv[3] = {__int_as_float(p[0]), __int_as_float(p[1]), __int_as_float(p[2])};
+        float s[3] = {0.f, 0.f, 0.f};
+        unsigned v[6] = {0, 0, 0, 0, 0, 0};
+#pragma unroll 4
+        for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+            float x[4];
+            load4(w + j, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int q = 0; q < 3; ++q)
+                    if (x[i] >= pv[q]) { s[q] += x[i]; ++v[q]; }
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) v[3 + q] = __float2uint_rn(s[q] * unit);
+        group_add(G, v, turn);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) {
+            const unsigned f = by_mass ? v[3 + q] : v[q];
+            if (f >= target) { if (p[q] > lo) { lo = p[q]; n_lo = v[q]; m_lo = v[3 + q]; } }
+            else if (p[q] < hi) { hi = p[q]; n_hi = v[q]; m_hi = v[3 + q]; }
+        }
+    }
+    // the entry that is left in [lo, hi), and its neighbours
+    unsigned at = 0, below = 0, above = 0x7f800000u;
+#pragma unroll 4
+    for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+        float x[4];
+        load4(w + j, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned b = __float_as_uint(x[i]);
+            if ((int)b >= hi) above = min(above, b);
+            else if ((int)b >= lo) at = max(at, b);
+            else below = max(below, b);
+        }
+    }
+    group_extremes(G, at, below, above, turn);
+    cut.tau = __uint_as_float(at);
+    cut.count = n_lo;
+    cut.mass = m_lo;
+    if (by_mass && !(m_lo > target + slack && target > m_hi + slack)) return false;
+    const float e = err.weight - err.slope * fminf(log2f(cut.tau), 0.f);
+    return cut.tau - __uint_as_float(below) > e * cut.tau && __uint_as_float(above) - cut.tau > e * cut.tau;
+}
+
+// Cuts the row.  `slack` is what two sums may be apart in units.
+__device__ __forceinline__ bool quick_cut(const float *w, const int mp, const RowGroup &G, const RowCuts &want, const unsigned count, const float unit,
+                                          const unsigned slack, const RowError &err, QuickCut &cut, int &turn)
+{
+    cut = {0.f, count, (unsigned)QUICK_ONE};
+    if ((unsigned)want.k < count && !quick_find(w, mp, G, false, (unsigned)want.k, unit, slack, err, cut, turn)) return false;
+    if (want.p < 1.0 && cut.count > 1) {
+        const unsigned target = (unsigned)(want.p * (double)cut.mass);
+        if (!quick_find(w, mp, G, true, target, unit, slack, err, cut, turn)) return false;
+    }
+    if (want.r > 0.f) {
+        const float e = err.weight - err.slope * log2f(want.r);
+        const float low = want.r * (1.f - e), high = want.r * (1.f + e);
+        unsigned near_[1] = {0};
+#pragma unroll 4
+        for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+            float x[4];
+            load4(w + j, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) near_[0] += x[i] >= low && x[i] <= high;
+        }
+        // (a smallest share of 1 keeps the largest weight, which is 1 itself)
+        group_add(G, near_, turn);
+        if (near_[0] != (want.r == 1.f ? 1u : 0u)) return false;
+        cut.tau = fmaxf(cut.tau, want.r);
+    }
+    return true;
+}
+
+__device__ __forceinline__ bool quick_kept(float v, float tau) { return tau > 0.f ? v >= tau : v > 0.f; }
+
+// Units of the kept weights by tile.
+__device__ __forceinline__ void quick_tiles(const float *w, const int ntiles, const RowGroup &G, const float tau, const float unit, unsigned *tiles)
+{
+    const int lane = G.t & 31;
+#pragma unroll 4
+    for (int q = G.t >> 5; q < ntiles; q += G.nt >> 5) {
+        float v[4], s = 0.f;
+        load4(w + q * ROW_TILE + 4 * lane, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s += quick_kept(v[i], tau) ? v[i] : 0.f;
+        const unsigned u = __reduce_add_sync(0xffffffffu, __float2uint_rn(s * unit));
+        if (lane == 0) tiles[q] = u;
+    }
+}
+__device__ __forceinline__ unsigned quick_total(const unsigned *tiles, const int ntiles)
+{
+    unsigned s = 0;
+    for (int q = threadIdx.x & 31; q < ntiles; q += 32) s += tiles[q];
+    return __reduce_add_sync(0xffffffffu, s);
+}
+__device__ __forceinline__ unsigned warp_scan(unsigned v)          // inclusive
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int off = 1; off < 32; off *= 2) {
+        const unsigned o = __shfl_up_sync(0xffffffffu, v, off);
+        if (lane >= off) v += o;
+    }
+    return v;
+}
+// One draw, by one warp; false where it is unsure.
+__device__ __forceinline__ bool quick_draw(const float *w, const int ntiles, const float tau, const float unit, const unsigned *tiles, const unsigned total,
+                                           const float u, const unsigned slack, int &index, float &weight)
+{
+    const int lane = threadIdx.x & 31;
+    const unsigned target = (unsigned)((double)u * (double)total);
+    unsigned before = 0;
+    int tile = -1;
+    for (int q0 = 0; q0 < ntiles; q0 += 32) {
+        const unsigned v = q0 + lane < ntiles ? tiles[q0 + lane] : 0u, s = before + warp_scan(v);
+        const unsigned over = __ballot_sync(0xffffffffu, s > target);
+        if (over) {
+            const int at = __ffs(over) - 1;
+            tile = q0 + at;
+            before = __shfl_sync(0xffffffffu, s - v, at);
+            break;
+        }
+        before = __shfl_sync(0xffffffffu, s, 31);
+    }
+    if (tile < 0) return false;
+    float v[4], s = 0.f;
+    load4(w + tile * ROW_TILE + 4 * lane, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = quick_kept(v[i], tau) ? v[i] : 0.f; s += v[i]; }
+    const unsigned own = __float2uint_rn(s * unit), run = before + warp_scan(own);
+    const unsigned over = __ballot_sync(0xffffffffu, run > target);
+    if (!over) return false;
+    const int who = __ffs(over) - 1;
+    // among the thread's four: the first at which the sum passes the target
+    const unsigned base = run - own;
+    float sum = 0.f, wi = 0.f;
+    int j = -1;
+    unsigned start = 0, end = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned a = base + __float2uint_rn(sum * unit);
+        sum += v[i];
+        const unsigned b = base + __float2uint_rn(sum * unit);
+        if (j < 0 && b > target) { j = tile * ROW_TILE + 4 * lane + i; wi = v[i]; start = a; end = b; }
+    }
+    const bool clear = j >= 0 && end > target + slack && target > start + slack;
+    index = __shfl_sync(0xffffffffu, j, who);
+    weight = __shfl_sync(0xffffffffu, wi, who);
+    return __shfl_sync(0xffffffffu, (int)clear, who) != 0;
+}
+
+}  // namespace skb

@@ -8,8 +8,7 @@
 //
 // `Real` is float where the weights are fp32.  Every comparison that decides something is then checked against bounds on
 // the errors (RowError), and a row with a comparison inside them is `unsure`: its caller decides it again with better
-// weights, in the end with exact ones, which takes what it finds.  Sums are in double above the 128 entries of a warp's load, and always added in one
-// order: results do not depend on timing.
+// weights, in the end with exact ones, which takes what it finds.  Sums are in double and always added in one order: results do not depend on timing.
 #pragma once
 #include <cuda_runtime.h>
 #include <math_constants.h>
@@ -24,10 +23,13 @@ constexpr int ROW_CAND = 32;
 struct RowScratch {
     double mass[16];
     int count[16];
-    double cand_w[ROW_CAND];
-    int cand_j[ROW_CAND];
-    double sort_w[ROW_CAND];
-    int sort_j[ROW_CAND];
+    union {
+        struct {
+            double cand_w[ROW_CAND], sort_w[ROW_CAND];
+            int cand_j[ROW_CAND], sort_j[ROW_CAND];
+        };
+        unsigned part[2][16][6];       // (skb_draw_quick.cuh)
+    };
     int n_cand, tie_j, band[3];
 };
 struct RowGroup {
@@ -128,16 +130,16 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
         if (bp <= bl) bp = bl + 1;
         if (bp >= bh) bp = bh - 1;
         const Real pivot = weight_of(bp);
-        Real s4[4] = {0, 0, 0, 0};
+        double s4[4] = {0, 0, 0, 0};
         int c = 0;
         for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
             Real v[4];
             load4(w + j, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (v[i] >= pivot) { s4[i] += v[i]; ++c; }
+                if (v[i] >= pivot) { s4[i] += (double)v[i]; ++c; }
         }
-        double s = ((double)s4[0] + (double)s4[1]) + ((double)s4[2] + (double)s4[3]);
+        double s = (s4[0] + s4[1]) + (s4[2] + s4[3]);
         G.add(s, c);
         if ((by_mass ? s : (double)c) >= target) { lo = pivot; n_lo = c; }
         else { hi = pivot; n_hi = c; m_hi = s; }
@@ -217,7 +219,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
 // `mass`, `top` is the largest (1 up to errors).  Returns false where the row is unsure.
 template <typename Real>
 __device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const RowCuts &want, const Real top, const double mass, const int count,
-                        const RowError &err, RowCut<Real> &cut, Real *tiles)
+                        const RowError &err, RowCut<Real> &cut, double *tiles)
 {
     bool unsure = false;
     cut.tau = 0; cut.J = -1; cut.mass = mass; cut.count = count; cut.lowest = 1;
@@ -255,11 +257,12 @@ __device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const Ro
     const int lane = G.t & 31;
     for (int q = G.t >> 5; q < mp / ROW_TILE; q += G.nt >> 5) {
         const int j = q * ROW_TILE + 4 * lane;
-        Real v[4], s = 0;
+        Real v[4];
+        double s = 0.0;
         load4(w + j, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (cut.kept(v[i], j + i)) s += v[i];
+            if (cut.kept(v[i], j + i)) s += (double)v[i];
             if (look) {
 #pragma unroll
                 for (int b = 0; b < 3; ++b) near_[b] += v[i] >= low[b] && v[i] <= high[b] ? 1 : 0;
@@ -288,11 +291,10 @@ __device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const Ro
 }
 
 // Total of the tiles' sums; by one warp.
-template <typename Real>
-__device__ __forceinline__ double row_total(const Real *tiles, const int ntiles)
+__device__ __forceinline__ double row_total(const double *tiles, const int ntiles)
 {
     double s = 0.0;
-    for (int q = threadIdx.x & 31; q < ntiles; q += 32) s += (double)tiles[q];
+    for (int q = threadIdx.x & 31; q < ntiles; q += 32) s += tiles[q];
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
     return s;
@@ -300,7 +302,7 @@ __device__ __forceinline__ double row_total(const Real *tiles, const int ntiles)
 
 // One draw, by one warp: the entry's index and weight.  Returns false where it is unsure.
 template <typename Real>
-__device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const Real *tiles, const int ntiles, const double total, const double u,
+__device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const double *tiles, const int ntiles, const double total, const double u,
                          const RowError &err, int &index, double &weight)
 {
     const int lane = threadIdx.x & 31;
@@ -309,7 +311,7 @@ __device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const Real *til
     double base = 0.0, before = 0.0;
     int tile = -1;
     for (int q0 = 0; q0 < ntiles; q0 += 32) {
-        const double v = q0 + lane < ntiles ? (double)tiles[q0 + lane] : 0.0;
+        const double v = q0 + lane < ntiles ? tiles[q0 + lane] : 0.0;
         double s = v;
 #pragma unroll
         for (int off = 1; off < 32; off *= 2) {
