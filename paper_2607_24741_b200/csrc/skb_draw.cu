@@ -29,7 +29,7 @@
 namespace skb {
 namespace {
 
-constexpr int DRAW_BLOCKS = 148;                     // SMs; the fp32 kernel has one or two blocks on each
+constexpr int DRAW_BLOCKS = 148;                     // SMs; the fp32 kernel has one to three blocks on each
 constexpr int DRAW_EXACT_BLOCKS = 148;               // rows of scratch in the workspace
 constexpr float ROW_FLOOR = 2.384185791015625e-7f;   // 2^-22: weights that are formed again where fp32 does not do
 constexpr size_t DRAW_DOTS_BYTES = (size_t)64 << 20; // products that are held at a time: half of the L2 cache
@@ -115,22 +115,45 @@ __global__ void __launch_bounds__(256) transpose_kernel(const Draw P)
     }
 }
 
+// Eight dimensions of point `row` from k on, k a multiple of 8; zeros past the last (k < the padded depth).
+__device__ __forceinline__ void eight_values(const void *data, const Cloud4 &c, int dtype, size_t row, int d, int k, float (&v)[8])
+{
+    if (dtype == SKB_BF16) {
+        const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
+        const uint32_t b[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(b[i] << 16); v[2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u); }
+    } else {
+        const uint32_t b = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
+        const float s = cloud4_scale(c, row, k);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = e2m1_value(b >> (4 * i)) * s;
+    }
+}
+__host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
 // |point|^2 in float64, by one warp; prefix: the mean of the squared norms of its first 16, 32, ... dimensions.
 __device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, int dtype, size_t row, int d, double &prefix)
 {
-    double s = 0.0, p = 0.0;
-    const int steps = (d + 15) / 16;
-    for (int k = threadIdx.x & 31; k < d; k += 32) {
-        const double v = (double)raw_value(base, c, dtype, row, d, k);
-        s = fma(v, v, s);
-        p = fma(v * v, (double)(steps - k / 16), p);
+    double s = 0.0;
+    float p = 0.f;
+    const int steps = (d + 15) / 16, chunks = dtype == SKB_BF16 ? d / 8 : dots_xd(d) / 8;
+    for (int q = threadIdx.x & 31; q < chunks; q += 32) {
+        float v[8], f = 0.f;
+        eight_values(base, c, dtype, row, d, 8 * q, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = v[i] * v[i];                             // exact: at most 16 bits
+            s += (double)a;
+            f += a;
+        }
+        p = fmaf(f, (float)max(steps - q / 2, 1), p);
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, off);
         p += __shfl_xor_sync(0xffffffffu, p, off);
     }
-    prefix = p / steps;
+    prefix = (double)(p / (float)steps) * 1.00001;                   // (the roundings of p)
     return s;
 }
 // k (g - |y|^2), and what bounds the error of the products, a warp to a point.
@@ -184,22 +207,6 @@ __device__ void draw_none(const Draw &P, size_t row, int t, int nt)
     for (int s = t; s < P.S; s += nt) put_draw(P, row * P.S + s, -1, CUDART_NAN_F);
 }
 
-// Eight dimensions of point `row` from k on, k a multiple of 8; zeros past the last (k < the padded depth).
-__device__ __forceinline__ void eight_values(const void *data, const Cloud4 &c, int dtype, size_t row, int d, int k, float (&v)[8])
-{
-    if (dtype == SKB_BF16) {
-        const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
-        const uint32_t b[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(b[i] << 16); v[2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u); }
-    } else {
-        const uint32_t b = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
-        const float s = cloud4_scale(c, row, k);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = e2m1_value(b >> (4 * i)) * s;
-    }
-}
-__host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
 
 // Rows in float64, a block to a row: those of the list, or all (rows too long for shared memory).
 __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
@@ -280,7 +287,7 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
 }
 
 // R rows of a lane at a time, NT threads: weights in shared memory by all threads, then a group of NT / R threads to a row.
-//   tiles [R][mp / 128], w [R][mp], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
+//   tiles [R][mp / 128], w [R][mp], lists [R][mp / 4], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
 //   (differences), or x [R][xd] of rows that are formed again (products)
 // Error of an exponent t = log2 w at a depth q below the row's largest, A = |largest t|:
 //   differences  h <= 0 and the scaled distance h - t are at most A + q; d + 2 roundings of the distance, three of the
@@ -294,7 +301,7 @@ template <int R, int NT>
 struct DrawShape {
     static size_t smem(int mp, int d, bool dots)
     {
-        return (size_t)R * (mp / ROW_TILE * 8 + (size_t)mp * 4) + (size_t)mp * 4 + (dots ? (size_t)R * dots_xd(d) * 4 : (size_t)R * d * 8);
+        return (size_t)R * (mp / ROW_TILE * 8 + (size_t)mp * 5) + (size_t)mp * 4 + (dots ? (size_t)R * dots_xd(d) * 4 : (size_t)R * d * 8);
     }
 };
 
@@ -482,8 +489,32 @@ __device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
     return v;
 }
 
+// A row once more: what weighs more than ROW_FLOOR to fp32's last place, what does not is `off` of itself off.  x: -x, `step`
+// apart (differences), or room for a row (products), whose bound is `bound`.
+template <bool DOTS>
+__device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t row, const RowGroup &G, double base, float off, float bound, float *x,
+                                   int step, float *w, double *tiles, unsigned char *list)
+{
+    const double *hn = P.hn + (size_t)wl * P.mp;
+    if (DOTS) {
+        const int xd = dots_xd(P.d);
+        for (int k = G.t; k < xd; k += G.nt) x[k] = k < P.d ? raw_value(P.x, P.x4, P.dtype, row, P.d, k) : 0.f;
+        // twice to four times the bound, and half as much again: sums within the bound stay in its binade
+        const float magic = 1.5f * __uint_as_float((__float_as_uint(bound * 4.f) & 0x7f800000u) + 0x00800000u);
+        G.sync();
+        refine_products(P, L.k2, wl, hn, x, magic, base, w, list, G.t >> 5, G.nt >> 5);
+    } else refine_differences(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, G.t >> 5, G.nt >> 5);
+    G.sync();
+    const RowSums sums = sum_row(G, w, P.mp);
+    if (!(sums.mass <= 3e38)) return false;
+    const RowError fine = {2.0 * (5.9604645e-8 * sums.mass + sums.rest * off), 2.f * 5.9604645e-8f, 0.f};
+    RowCut<float> cut;
+    if (!row_cut(w, P.mp, G, L.cuts, sums.top, sums.mass, sums.count, fine, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
+    return draw_all(P, row, w, cut, tiles, fine, G.t >> 5, G.nt >> 5);
+}
+
 template <int R, int NT, bool DOTS>
-__global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw P)
+__global__ void __launch_bounds__(NT, NT > 256 ? 1 : 3) draw_kernel(const Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc[R];
@@ -492,7 +523,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
     const int mp = P.mp, ntiles = mp / ROW_TILE, tid = threadIdx.x, lane = tid & 31, xd = dots_xd(P.d);
     double *tiles_all = reinterpret_cast<double *>(smem);
     float *w_all = reinterpret_cast<float *>(tiles_all + (R * ntiles + 1) / 2 * 2);
-    float *h = w_all + (size_t)R * mp;
+    float *h = w_all + (size_t)R * (mp + mp / 4);
     u64 *xs = reinterpret_cast<u64 *>(h + mp);
     float *x1 = reinterpret_cast<float *>(xs);
     const int g = tid / NG;
@@ -606,6 +637,7 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
                     *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
                     mass += (v[0] + v[1]) + (v[2] + v[3]);
                 }
+                const unsigned own = count;
                 group_sums(G, mass, depth, count, turn);
                 G.sync();
                 if (mass <= 3e38f) {
@@ -623,15 +655,15 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
                     }
                     fixed = 0.6932f * fixed + 2.4e-7f;
                     slope = 0.6932f * (slope + u24);
-                    // (twice the single errors, see RowError; the roundings to units)
-                    const float of_sums = 2.f * (fixed + adds + slope * depth / mass);
-                    const RowError err = {(double)of_sums, 2.f * fixed, 2.f * slope};
+                    // (of two weights: twice the error of one)
+                    const RowError err = {1.0, 2.f * fixed, 2.f * slope};
                     const float off = fixed + 24.f * slope;
                     if (off < 0.01f) {
                         const float unit = QUICK_ONE / mass;
-                        const unsigned slack = (unsigned)(of_sums * QUICK_ONE) + 2 * NG + 32 * ntiles + 64;
+                        // (roundings to units: half of one for each thread of a pass, and for each of 32 in a tile, twice)
+                        const QuickSlack slack = {1.02f * fixed * QUICK_ONE, (2.f * adds + slope * depth / mass) * QUICK_ONE + (float)(NG + 32 * ntiles)};
                         QuickCut cut;
-                        sure = quick_cut(w, mp, G, L.cuts, count, unit, slack, err, cut, turn);
+                        sure = quick_cut(w, mp, G, L.cuts, count, own, unit, slack, err, w_all + (size_t)R * mp + (size_t)g * (mp / 4), mp / 4, cut, turn);
                         if (sure) {
                             quick_tiles(w, ntiles, G, cut.tau, unit, units);
                             G.sync();
@@ -647,27 +679,10 @@ __global__ void __launch_bounds__(NT, NT == 256 ? 2 : 1) draw_kernel(const Draw 
                         sure = group_all(G, sure, turn);
                         if (!sure) {
                             // once more, with better weights for what counts
-                            const double base = h_top + (double)top;
                             G.sync();
-                            if (DOTS) {
-                                float *x = x1 + (size_t)g * xd;
-                                for (int k = G.t; k < xd; k += NG) x[k] = k < P.d ? raw_value(P.x, P.x4, P.dtype, row, P.d, k) : 0.f;
-                                // twice to four times the bound, and half as much again: sums within the bound stay in its binade
-                                const float magic = 1.5f * __uint_as_float((__float_as_uint(x_norm * y_max * 4.f) & 0x7f800000u) + 0x00800000u);
-                                G.sync();
-                                refine_products(P, L.k2, lanew, hn, x, magic, base, w, lists[tid >> 5], G.t >> 5, NG >> 5);
-                            } else refine_differences(P, L.k2, hn, yt, x1 + 2 * g, 2 * R, base, w, G.t >> 5, NG >> 5);
-                            G.sync();
-                            const RowSums sums = sum_row(G, w, mp);
-                            if (sums.mass <= 3e38) {
-                                // weights rounded to fp32; those below 2^-22 as they were
-                                const RowError fine = {2.0 * ((double)u24 * sums.mass + sums.rest * off), 2.f * u24, 0.f};
-                                RowCut<float> rcut;
-                                sure = row_cut(w, mp, G, L.cuts, sums.top, sums.mass, sums.count, fine, rcut, tiles);
-                                if (rcut.lowest < 2.f * ROW_FLOOR) sure = false;
-                                if (sure) sure = draw_all(P, row, w, rcut, tiles, fine, G.t >> 5, NG >> 5);
-                                sure = group_all(G, sure, turn);
-                            }
+                            sure = again<DOTS>(P, L, lanew, row, G, h_top + (double)top, off, x_norm * y_max, DOTS ? x1 + (size_t)g * xd : x1 + 2 * g,
+                                               2 * R, w, tiles, lists[DOTS ? tid >> 5 : 0]);
+                            sure = group_all(G, sure, turn);
                         }
                     }
                 }
@@ -733,7 +748,7 @@ void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
     // (the limit for any shape: another host thread may set it between this and the launch)
     cudaFuncSetAttribute(draw_kernel<R, NT, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(R == 8 ? DRAW_SMEM / 2 : DRAW_SMEM));
     const long long tiles = (long long)P.lanes * ((P.rows + R - 1) / R);
-    const size_t fit = NT > 256 ? 1 : std::min<size_t>(2, DRAW_SMEM / (p.smem + 10 * 1024));
+    const size_t fit = NT > 256 ? 1 : std::min<size_t>(3, 226 * 1024 / (p.smem + 10 * 1024));
     const long long most = (long long)(DRAW_BLOCKS * fit);
     draw_kernel<R, NT, DOTS><<<(unsigned)(tiles < most ? tiles : most), NT, p.smem, st>>>(P);
 }

@@ -2,8 +2,13 @@
 //
 // Sums are counted in units of 2^-30 of the row's mass: a thread adds its weights in fp32, rounds the sum to units, and the
 // warp's are added by one integer reduction, exactly and in no particular order.  A cut is found by three pivots at a time,
-// quarters of the bracket's bit patterns, until one weight is left in the bracket; two that are within their errors of each
-// other leave the row unsure, so no ties have to be ordered here.  skb_draw_row.cuh has the careful form of the same.
+// quarters of the bracket's bit patterns, until one weight is left in the bracket.  As soon as a quarter of the row is left,
+// the weights in the bracket move to a list, and later passes read that (a pass over the row is nine instructions a
+// weight, and some ten passes are needed).  Two weights within their errors of each other leave the row unsure, so no ties
+// have to be ordered here.  skb_draw_row.cuh has the careful form.
+//
+// Error of a comparison: a sum over a part of the row against a share f of its mass M, sum - f M = (1 - f) part - f rest.  Where
+// part is about f M, relative errors of the weights of at most e move that by 2 f (1 - f) e M, and no more.
 #pragma once
 #include "skb_draw_row.cuh"
 
@@ -48,19 +53,64 @@ __device__ __forceinline__ void group_extremes(const RowGroup &G, unsigned &a, u
     }
 }
 
+// What a sum and a share f of the row's mass may be apart, in units: errors of the weights, of additions and of rounding to units.
+struct QuickSlack {
+    float weights, rest;
+    __device__ __forceinline__ unsigned at(float f) const { return (unsigned)(2.f * f * (1.f - f) * weights + rest) + 1u; }
+};
+
 struct QuickCut {
     float tau;                          // kept: weights from here on
     unsigned count, mass;               // of what is kept; mass in units
+    unsigned own;                       // this thread's of `count`, where a thread has the entries 4 (t + i nt) ... + 3
 };
 
-// Shrinks the cut to the shortest head with `target` entries, or units of mass.  Returns false where it is unsure.
-__device__ __forceinline__ bool quick_find(const float *w, const int mp, const RowGroup &G, const bool by_mass, const unsigned target, const float unit,
-                                           const unsigned slack, const RowError &err, QuickCut &cut, int &turn)
+// Exclusive sum over the group's threads of a count each.
+__device__ __forceinline__ unsigned group_offset(const RowGroup &G, const unsigned v, int &turn)
+{
+    const int lane = G.t & 31;
+    unsigned s = v;
+#pragma unroll
+    for (int off = 1; off < 32; off *= 2) {
+        const unsigned o = __shfl_up_sync(0xffffffffu, s, off);
+        if (lane >= off) s += o;
+    }
+    unsigned before = s - v;
+    if (G.nt == 32) return before;
+    turn ^= 1;
+    if (lane == 31) G.sc->part[turn][G.t >> 5][0] = s;
+    G.sync();
+    for (int q = 0; q < G.t >> 5; ++q) before += G.sc->part[turn][q][0];
+    return before;
+}
+
+// Shrinks the cut to the shortest head with `target` entries, or units of mass.  `list` has room for `room` weights.
+// Returns false where it is unsure.
+__device__ __forceinline__ bool quick_find(const float *row, const int mp, const RowGroup &G, const bool by_mass, const unsigned target, const float unit,
+                                           const unsigned slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
     int lo = cut.tau > 0.f ? __float_as_int(cut.tau) : 1, hi = __float_as_int(2.f);
-    unsigned n_lo = cut.count, m_lo = cut.mass, n_hi = 0, m_hi = 0;
+    unsigned n_lo = cut.count, m_lo = cut.mass, n_hi = 0, m_hi = 0, own_lo = cut.own, own_hi = 0;
+    const float *w = row;
+    int n = mp, low_side = 0, high_side = hi;                    // the bracket of what w holds
+    unsigned n_out = 0, m_out = 0;                               // number and mass of what is above it
     bool first = true;
     while (n_lo - n_hi > 1) {
+        if (w == row && n_lo - n_hi <= room) {
+            // what is in the bracket to the list, zeros behind it up to whole quadruples
+            unsigned at = group_offset(G, own_lo - own_hi, turn);
+            for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+                float x[4];
+                load4(row + j, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (__float_as_int(x[i]) >= lo && __float_as_int(x[i]) < hi) list[at++] = x[i];
+            }
+            n = (int)((n_lo - n_hi + 3) / 4 * 4);
+            if (G.t < n - (int)(n_lo - n_hi)) list[n_lo - n_hi + G.t] = 0.f;
+            G.sync();
+            w = list; low_side = lo; high_side = hi; n_out = n_hi; m_out = m_hi;
+        }
         const int gap = hi - lo;
         if (gap < 16) return false;                              // equal weights, or nearly
         int p[3] = {lo + gap / 4, lo + gap / 2, lo + gap / 4 * 3};
@@ -77,8 +127,8 @@ __device__ __forceinline__ bool quick_find(const float *w, const int mp, const R
         const float pv[3] = {__int_as_float(p[0]), __int_as_float(p[1]), __int_as_float(p[2])};
         float s[3] = {0.f, 0.f, 0.f};
         unsigned v[6] = {0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-        for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+#pragma unroll 2
+        for (int j = 4 * G.t; j < n; j += 4 * G.nt) {
             float x[4];
             load4(w + j, x);
 #pragma unroll
@@ -87,20 +137,21 @@ __device__ __forceinline__ bool quick_find(const float *w, const int mp, const R
                 for (int q = 0; q < 3; ++q)
                     if (x[i] >= pv[q]) { s[q] += x[i]; ++v[q]; }
         }
+        const unsigned own[3] = {v[0], v[1], v[2]};
 #pragma unroll
         for (int q = 0; q < 3; ++q) v[3 + q] = __float2uint_rn(s[q] * unit);
         group_add(G, v, turn);
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
-            const unsigned f = by_mass ? v[3 + q] : v[q];
-            if (f >= target) { if (p[q] > lo) { lo = p[q]; n_lo = v[q]; m_lo = v[3 + q]; } }
-            else if (p[q] < hi) { hi = p[q]; n_hi = v[q]; m_hi = v[3 + q]; }
+            const unsigned c = n_out + v[q], m = m_out + v[3 + q];
+            if ((by_mass ? m : c) >= target) { if (p[q] > lo) { lo = p[q]; n_lo = c; m_lo = m; own_lo = own[q]; } }
+            else if (p[q] < hi) { hi = p[q]; n_hi = c; m_hi = m; own_hi = own[q]; }
         }
     }
-    // the entry that is left in [lo, hi), and its neighbours
-    unsigned at = 0, below = 0, above = 0x7f800000u;
-#pragma unroll 4
-    for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+    // the entry that is left in [lo, hi), and its neighbours; those outside of the list are outside of its bracket
+    unsigned at = 0, below = (unsigned)low_side, above = (unsigned)high_side, kept = 0;
+#pragma unroll 2
+    for (int j = 4 * G.t; j < n; j += 4 * G.nt) {
         float x[4];
         load4(w + j, x);
 #pragma unroll
@@ -115,20 +166,31 @@ __device__ __forceinline__ bool quick_find(const float *w, const int mp, const R
     cut.tau = __uint_as_float(at);
     cut.count = n_lo;
     cut.mass = m_lo;
+    if (!by_mass) {
+        // (a cut by mass may follow)
+        for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+            float x[4];
+            load4(row + j, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kept += x[i] >= cut.tau;
+        }
+    }
+    cut.own = kept;
+    G.sync();                                                    // the list is read
     if (by_mass && !(m_lo > target + slack && target > m_hi + slack)) return false;
     const float e = err.weight - err.slope * fminf(log2f(cut.tau), 0.f);
     return cut.tau - __uint_as_float(below) > e * cut.tau && __uint_as_float(above) - cut.tau > e * cut.tau;
 }
 
-// Cuts the row.  `slack` is what two sums may be apart in units.
-__device__ __forceinline__ bool quick_cut(const float *w, const int mp, const RowGroup &G, const RowCuts &want, const unsigned count, const float unit,
-                                          const unsigned slack, const RowError &err, QuickCut &cut, int &turn)
+// Cuts the row.
+__device__ __forceinline__ bool quick_cut(const float *w, const int mp, const RowGroup &G, const RowCuts &want, const unsigned count, const unsigned own,
+                                          const float unit, const QuickSlack &slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
-    cut = {0.f, count, (unsigned)QUICK_ONE};
-    if ((unsigned)want.k < count && !quick_find(w, mp, G, false, (unsigned)want.k, unit, slack, err, cut, turn)) return false;
+    cut = {0.f, count, (unsigned)QUICK_ONE, own};
+    if ((unsigned)want.k < count && !quick_find(w, mp, G, false, (unsigned)want.k, unit, 0u, err, list, room, cut, turn)) return false;
     if (want.p < 1.0 && cut.count > 1) {
         const unsigned target = (unsigned)(want.p * (double)cut.mass);
-        if (!quick_find(w, mp, G, true, target, unit, slack, err, cut, turn)) return false;
+        if (!quick_find(w, mp, G, true, target, unit, slack.at((float)want.p), err, list, room, cut, turn)) return false;
     }
     if (want.r > 0.f) {
         const float e = err.weight - err.slope * log2f(want.r);
@@ -183,10 +245,10 @@ __device__ __forceinline__ unsigned warp_scan(unsigned v)          // inclusive
 }
 // One draw, by one warp; false where it is unsure.
 __device__ __forceinline__ bool quick_draw(const float *w, const int ntiles, const float tau, const float unit, const unsigned *tiles, const unsigned total,
-                                           const float u, const unsigned slack, int &index, float &weight)
+                                           const float u, const QuickSlack &of, int &index, float &weight)
 {
     const int lane = threadIdx.x & 31;
-    const unsigned target = (unsigned)((double)u * (double)total);
+    const unsigned target = (unsigned)((double)u * (double)total), slack = of.at(u);
     unsigned before = 0;
     int tile = -1;
     for (int q0 = 0; q0 < ntiles; q0 += 32) {
