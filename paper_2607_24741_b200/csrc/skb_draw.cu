@@ -32,6 +32,7 @@ namespace {
 constexpr int DRAW_BLOCKS = 148;                     // SMs; the fp32 kernel has one to three blocks on each
 constexpr int DRAW_EXACT_BLOCKS = 148;               // rows of scratch in the workspace
 constexpr float ROW_FLOOR = 2.384185791015625e-7f;   // 2^-22: weights that are formed again where fp32 does not do
+constexpr float ROW_TAIL = 5.9604645e-8f;            // 2^-24: weights that a row of few heavy entries does without
 constexpr size_t DRAW_DOTS_BYTES = (size_t)64 << 20; // products that are held at a time: half of the L2 cache
 
 struct Draw {
@@ -115,31 +116,47 @@ __global__ void __launch_bounds__(256) transpose_kernel(const Draw P)
     }
 }
 
-// Eight dimensions of point `row` from k on, k a multiple of 8; zeros past the last (k < the padded depth).
-__device__ __forceinline__ void eight_values(const void *data, const Cloud4 &c, int dtype, size_t row, int d, int k, float (&v)[8])
+// Eight dimensions of a point from k on, k a multiple of 8, as they are held (loads of many of these are in flight
+// before the first is looked at): bf16, or codes and their scale's byte.
+struct Eight { uint4 a; };
+template <bool BF>
+__device__ __forceinline__ Eight load_eight(const void *data, const Cloud4 &c, size_t row, int d, int k)
 {
-    if (dtype == SKB_BF16) {
-        const uint4 a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
-        const uint32_t b[4] = {a.x, a.y, a.z, a.w};
+    Eight e;
+    if constexpr (BF) e.a = *reinterpret_cast<const uint4 *>((const uint16_t *)data + row * d + k);
+    else {
+        e.a.x = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
+        e.a.y = c.scales[row * c.sb + (c.points ? k >> 4 : k >> 5)];
+    }
+    return e;
+}
+// `point`: the point's power of two (nv4)
+template <bool BF>
+__device__ __forceinline__ void eight_values(const Eight &e, const Cloud4 &c, float point, float (&v)[8])
+{
+    if constexpr (BF) {
+        const uint32_t b[4] = {e.a.x, e.a.y, e.a.z, e.a.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(b[i] << 16); v[2 * i + 1] = __uint_as_float(b[i] & 0xffff0000u); }
     } else {
-        const uint32_t b = *reinterpret_cast<const uint32_t *>(c.codes + row * c.cb + k / 2);
-        const float s = cloud4_scale(c, row, k);
+        const float s = c.points ? e4m3_value(e.a.y) * point : e8m0_value(e.a.y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = e2m1_value(b >> (4 * i)) * s;
+        for (int i = 0; i < 8; ++i) v[i] = e2m1_value(e.a.x >> (4 * i)) * s;
     }
 }
 __host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
 // |point|^2 in float64, by one warp; prefix: the mean of the squared norms of its first 16, 32, ... dimensions.
-__device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, int dtype, size_t row, int d, double &prefix)
+template <bool BF>
+__device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, size_t row, int d, double &prefix)
 {
     double s = 0.0;
     float p = 0.f;
-    const int steps = (d + 15) / 16, chunks = dtype == SKB_BF16 ? d / 8 : dots_xd(d) / 8;
+    const int steps = (d + 15) / 16, chunks = BF ? d / 8 : dots_xd(d) / 8;
+    const float point = !BF && c.points ? c.points[row] : 1.f;
+#pragma unroll 2
     for (int q = threadIdx.x & 31; q < chunks; q += 32) {
         float v[8], f = 0.f;
-        eight_values(base, c, dtype, row, d, 8 * q, v);
+        eight_values<BF>(load_eight<BF>(base, c, row, d, 8 * q), c, point, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float a = v[i] * v[i];                             // exact: at most 16 bits
@@ -157,6 +174,7 @@ __device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, i
     return s;
 }
 // k (g - |y|^2), and what bounds the error of the products, a warp to a point.
+template <bool BF>
 __global__ void __launch_bounds__(256) norms_kernel(const Draw P)
 {
     const int w = blockIdx.y, i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -165,7 +183,7 @@ __global__ void __launch_bounds__(256) norms_kernel(const Draw P)
     if (i < P.mp) {
         const double g = i < P.m ? P.g[(size_t)w * P.m + i] : -CUDART_INF;
         const bool masked = g == -CUDART_INF;
-        const double s = masked ? 0.0 : square_of(P.y, P.y4, P.dtype, (size_t)w * P.m + i, P.d, p);
+        const double s = masked ? 0.0 : square_of<BF>(P.y, P.y4, (size_t)w * P.m + i, P.d, p);
         if (lane == 0) {
             P.hn[(size_t)w * P.mp + i] = masked ? g : lane_of(P, w).k2 * (g - s);
             P.yn[(size_t)w * P.mp + i] = make_float2((float)s, (float)p);
@@ -174,7 +192,7 @@ __global__ void __launch_bounds__(256) norms_kernel(const Draw P)
     }
     const int r = i - P.mp;
     if (r >= P.n) return;
-    const double s = square_of(P.x, P.x4, P.dtype, (size_t)w * P.n + r, P.d, p);
+    const double s = square_of<BF>(P.x, P.x4, (size_t)w * P.n + r, P.d, p);
     if (lane == 0) P.xn[(size_t)w * P.n + r] = make_float2((float)s, (float)p);
 }
 
@@ -208,13 +226,53 @@ __device__ void draw_none(const Draw &P, size_t row, int t, int nt)
 }
 
 
+// Exponents of a row from the points as they are held, eight threads to a point, four points to a warp.
+constexpr int BATCH = 8;                             // loads in flight
+template <bool BF>
+__device__ __forceinline__ void exact_rows(const Draw &P, const Lane &L, int w, const double *hn, const double *xs, double *wd, int warp, int warps,
+                                           double &top, int &bad)
+{
+    const int lane = threadIdx.x & 31, part = lane & 7, chunks = BF ? P.d / 8 : dots_xd(P.d) / 8;
+    for (int j0 = 4 * warp; j0 < P.mp; j0 += 4 * warps) {
+        const int j = j0 + (lane >> 3);
+        const bool is = hn[j] != -CUDART_INF;
+        double c = 0.0;
+        if (is) {
+            const size_t row = (size_t)w * P.m + j;
+            const float point = !BF && P.y4.points ? P.y4.points[row] : 1.f;
+            for (int q0 = part; q0 < chunks; q0 += 8 * BATCH) {
+                Eight e[BATCH];
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b)
+                    if (q0 + 8 * b < chunks) e[b] = load_eight<BF>(P.y, P.y4, row, P.d, 8 * (q0 + 8 * b));
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b)
+                    if (q0 + 8 * b < chunks) {
+                        float y[8];
+                        double part_c = 0.0;
+                        eight_values<BF>(e[b], P.y4, point, y);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) { const double f = xs[8 * (q0 + 8 * b) + i] - (double)y[i]; part_c = fma(f, f, part_c); }
+                        c += part_c;
+                    }
+            }
+        }
+#pragma unroll
+        for (int off = 1; off < 8; off *= 2) c += __shfl_xor_sync(0xffffffffu, c, off);
+        const double z = is ? L.k2 * (P.g[(size_t)w * P.m + j] - c) : -CUDART_INF;
+        if (part == 0) wd[j] = z;
+        top = fmax(top, z);
+        bad |= !(z <= 1.7e308);
+    }
+}
+
 // Rows in float64, a block to a row: those of the list, or all (rows too long for shared memory).
 __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc;
     double *tiles = reinterpret_cast<double *>(smem), *xs = tiles + P.mp / ROW_TILE, *wd = P.scratch + (size_t)blockIdx.x * P.mp;
-    const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31, warp = tid >> 5, xd = dots_xd(P.d);
+    const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, xd = dots_xd(P.d);
     const RowGroup G = {tid, nt, 0, &sc};
     const long long rows = P.list ? P.list[0] : (long long)P.W * P.n;
     for (long long t = blockIdx.x; t < rows; t += gridDim.x) {
@@ -243,28 +301,8 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
                 bad |= !(z <= 1.7e308);
             }
         } else {
-            // eight threads to a point, four points to a warp
-            const int part = lane & 7, chunks = P.dtype == SKB_BF16 ? P.d / 8 : xd / 8;
-            for (int j0 = 4 * warp; j0 < P.mp; j0 += 4 * (nt >> 5)) {
-                const int j = j0 + (lane >> 3);
-                const bool is = hn[j] != -CUDART_INF;
-                double c = 0.0;
-                if (is) {
-#pragma unroll 4
-                    for (int q = part; q < chunks; q += 8) {
-                        float y[8];
-                        eight_values(P.y, P.y4, P.dtype, (size_t)w * P.m + j, P.d, 8 * q, y);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) { const double e = xs[8 * q + i] - (double)y[i]; c = fma(e, e, c); }
-                    }
-                }
-#pragma unroll
-                for (int off = 1; off < 8; off *= 2) c += __shfl_xor_sync(0xffffffffu, c, off);
-                const double z = is ? L.k2 * (P.g[(size_t)w * P.m + j] - c) : -CUDART_INF;
-                if (part == 0) wd[j] = z;
-                top = fmax(top, z);
-                bad |= !(z <= 1.7e308);
-            }
+            if (P.dtype == SKB_BF16) exact_rows<true>(P, L, w, hn, xs, wd, warp, nt >> 5, top, bad);
+            else exact_rows<false>(P, L, w, hn, xs, wd, warp, nt >> 5, top, bad);
         }
         double mass = 0.0;
         int count = 0;
@@ -286,9 +324,8 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
     }
 }
 
-// R rows of a lane at a time, NT threads: weights in shared memory by all threads, then a group of NT / R threads to a row.
-//   tiles [R][mp / 128], w [R][mp], lists [R][mp / 4], h [mp]: the lane's hn less its largest, as fp32; xs: -x, twice each, [d][R] pairs
-//   (differences), or x [R][xd] of rows that are formed again (products)
+// Rows in fp32: a row's exponents, then weights, in shared memory, by a warp or a group of warps each.  h: the lane's hn less its
+// largest; xs: -x, twice each (differences), or x of a row that is formed again (products).
 // Error of an exponent t = log2 w at a depth q below the row's largest, A = |largest t|:
 //   differences  h <= 0 and the scaled distance h - t are at most A + q; d + 2 roundings of the distance, three of the
 //                scale and t, one of h: (d + 6) (A + q) 2^-24
@@ -297,51 +334,6 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
 //                cuts off where it adds products to a sum: a unit in the last place of the sum, at most 2^-23 of it, for each 16, and
 //                two more: (d / 16) B' 2^-23 + 2 B 2^-23; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
 // The exponential adds 2^-22 and 2^-24 q of the difference that it is taken of, the additions of weights 2^-24 each.
-template <int R, int NT>
-struct DrawShape {
-    static size_t smem(int mp, int d, bool dots)
-    {
-        return (size_t)R * (mp / ROW_TILE * 8 + (size_t)mp * 5) + (size_t)mp * 4 + (dots ? (size_t)R * dots_xd(d) * 4 : (size_t)R * d * 8);
-    }
-};
-
-// Exponents of the block's rows from coordinate differences, RPT rows and four columns to a thread.
-template <int R, int NT, int RPT>
-__device__ __forceinline__ void form_rows(const float *yt, const float *h, const u64 *xs, float *w, int mp, int d, float k2)
-{
-    constexpr int RG = R / RPT, CT = NT / RG;
-    const int ct = threadIdx.x % CT, r0 = threadIdx.x / CT * RPT;
-    const float ninf = -k2;
-    for (int j = 4 * ct; j < mp; j += 4 * CT) {
-        u64 acc[RPT][2];
-#pragma unroll
-        for (int r = 0; r < RPT; ++r) acc[r][0] = acc[r][1] = 0ull;
-#pragma unroll 2
-        for (int k = 0; k < d; ++k) {
-            const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(yt + (size_t)k * mp + j);
-#pragma unroll
-            for (int r = 0; r < RPT; r += 2) {
-                ulonglong2 x = {0ull, 0ull};
-                if constexpr (RPT >= 2) x = *reinterpret_cast<const ulonglong2 *>(xs + k * R + r0 + r);
-                else x.x = xs[k * R + r0];
-#pragma unroll
-                for (int q = 0; q < (RPT >= 2 ? 2 : 1); ++q) {
-                    const u64 a = add2(y.x, q ? x.y : x.x), b = add2(y.y, q ? x.y : x.x);
-                    acc[r + q][0] = fma2(a, a, acc[r + q][0]);
-                    acc[r + q][1] = fma2(b, b, acc[r + q][1]);
-                }
-            }
-        }
-        const ulonglong2 hh = *reinterpret_cast<const ulonglong2 *>(h + j);
-        const u64 s = pack2(ninf, ninf);
-#pragma unroll
-        for (int r = 0; r < RPT; ++r) {
-            const ulonglong2 t = {fma2(s, acc[r][0], hh.x), fma2(s, acc[r][1], hh.y)};
-            *reinterpret_cast<ulonglong2 *>(w + (size_t)(r0 + r) * mp + j) = t;
-        }
-    }
-}
-
 // Mass, number and largest of a row's weights, and the mass of those at most ROW_FLOOR.
 struct RowSums {
     double mass, rest;
@@ -397,11 +389,12 @@ __device__ __forceinline__ void refine_differences(const Draw &P, double k2, con
 // x . y of four points of y at a time, eight threads to a point.  Products are exact in fp32 (at most 16 bits).  They are
 // added to a large number M, whose last place is 2^-24 of a bound on the sum: what an addition cuts off is itself exact and is
 // added up apart, so that the result is good to 2^-40 of the bound.
+template <bool BF>
 __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl, const double *hn, const float *x, float magic, double base,
                                                 float *w, unsigned char *list, int warp, int warps)
 {
     const int lane = threadIdx.x & 31, part = lane & 7, col = lane >> 3;
-    const int chunks = P.dtype == SKB_BF16 ? P.d / 8 : dots_xd(P.d) / 8;
+    const int chunks = BF ? P.d / 8 : dots_xd(P.d) / 8;
     for (int q = warp; q < P.mp / ROW_TILE; q += warps) {
         float v[4];
         load4(w + q * ROW_TILE + 4 * lane, v);
@@ -416,20 +409,28 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
         for (int e0 = 0; e0 < n; e0 += 4) {
             const int j = q * ROW_TILE + list[min(e0 + col, n - 1)];
             const size_t row = (size_t)wl * P.m + j;
+            const float point = !BF && P.y4.points ? P.y4.points[row] : 1.f;
             const u64 m2 = pack2(magic, magic);
             u64 sum = m2, low = 0ull;
-#pragma unroll 4
-            for (int c = part; c < chunks; c += 8) {
-                float y[8];
-                eight_values(P.y, P.y4, P.dtype, row, P.d, 8 * c, y);
-                const ulonglong2 xa = reinterpret_cast<const ulonglong2 *>(x + 8 * c)[0], xb = reinterpret_cast<const ulonglong2 *>(x + 8 * c)[1];
-                const u64 xv[4] = {xa.x, xa.y, xb.x, xb.y};
+            for (int c0 = part; c0 < chunks; c0 += 8 * BATCH) {
+                Eight e[BATCH];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const u64 yv = pack2(y[2 * i], y[2 * i + 1]), t = fma2(xv[i], yv, sum);
-                    low = add2(low, fma2(xv[i], yv, sub2(sum, t)));
-                    sum = t;
-                }
+                for (int b = 0; b < BATCH; ++b)
+                    if (c0 + 8 * b < chunks) e[b] = load_eight<BF>(P.y, P.y4, row, P.d, 8 * (c0 + 8 * b));
+#pragma unroll
+                for (int b = 0; b < BATCH; ++b)
+                    if (c0 + 8 * b < chunks) {
+                        float y[8];
+                        eight_values<BF>(e[b], P.y4, point, y);
+                        const ulonglong2 *xp = reinterpret_cast<const ulonglong2 *>(x + 8 * (c0 + 8 * b));
+                        const u64 xv[4] = {xp[0].x, xp[0].y, xp[1].x, xp[1].y};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const u64 yv = pack2(y[2 * i], y[2 * i + 1]), t = fma2(xv[i], yv, sum);
+                            low = add2(low, fma2(xv[i], yv, sub2(sum, t)));
+                            sum = t;
+                        }
+                    }
             }
             float a, b, la, lb;
             unpack2(sub2(sum, m2), a, b);                            // exact
@@ -443,27 +444,33 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
     }
 }
 
-// Sums of two floats and a count over the group, added in one order.
-__device__ __forceinline__ void group_sums(const RowGroup &G, float &a, float &b, unsigned &n, int &turn)
+// Sums over the group of three floats and two counts, in one order; `before`: of the second count over the warps before this one.
+__device__ __forceinline__ void group_sums(const RowGroup &G, float (&f)[3], unsigned &n, unsigned &m, unsigned &before, int &turn)
 {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        a += __shfl_xor_sync(0xffffffffu, a, off);
-        b += __shfl_xor_sync(0xffffffffu, b, off);
-    }
+    for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+        for (int i = 0; i < 3; ++i) f[i] += __shfl_xor_sync(0xffffffffu, f[i], off);
     n = __reduce_add_sync(0xffffffffu, n);
+    m = __reduce_add_sync(0xffffffffu, m);
+    before = 0;
     if (G.nt == 32) return;
     turn ^= 1;
     if ((G.t & 31) == 0) {
         unsigned *p = G.sc->part[turn][G.t >> 5];
-        p[0] = __float_as_uint(a); p[1] = __float_as_uint(b); p[2] = n;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) p[i] = __float_as_uint(f[i]);
+        p[3] = n; p[4] = m;
     }
     G.sync();
-    a = b = 0.f;
-    n = 0;
+    f[0] = f[1] = f[2] = 0.f;
+    n = m = 0;
     for (int q = 0; q < G.nt >> 5; ++q) {
         const unsigned *p = G.sc->part[turn][q];
-        a += __uint_as_float(p[0]); b += __uint_as_float(p[1]); n += p[2];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) f[i] += __uint_as_float(p[i]);
+        if (q < G.t >> 5) before += p[4];
+        n += p[3]; m += p[4];
     }
 }
 __device__ __forceinline__ float group_largest(const RowGroup &G, float v, int &turn)
@@ -502,7 +509,8 @@ __device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t 
         // twice to four times the bound, and half as much again: sums within the bound stay in its binade
         const float magic = 1.5f * __uint_as_float((__float_as_uint(bound * 4.f) & 0x7f800000u) + 0x00800000u);
         G.sync();
-        refine_products(P, L.k2, wl, hn, x, magic, base, w, list, G.t >> 5, G.nt >> 5);
+        if (P.dtype == SKB_BF16) refine_products<true>(P, L.k2, wl, hn, x, magic, base, w, list, G.t >> 5, G.nt >> 5);
+        else refine_products<false>(P, L.k2, wl, hn, x, magic, base, w, list, G.t >> 5, G.nt >> 5);
     } else refine_differences(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, G.t >> 5, G.nt >> 5);
     G.sync();
     const RowSums sums = sum_row(G, w, P.mp);
@@ -513,211 +521,419 @@ __device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t 
     return draw_all(P, row, w, cut, tiles, fine, G.t >> 5, G.nt >> 5);
 }
 
-template <int R, int NT, bool DOTS>
-__global__ void __launch_bounds__(NT, NT > 256 ? 1 : 3) draw_kernel(const Draw P)
-{
-    extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ RowScratch sc[R];
-    __shared__ unsigned char lists[DOTS ? NT / 32 : 1][ROW_TILE];
-    constexpr int NG = NT / R;                                   // threads of a row's group
-    const int mp = P.mp, ntiles = mp / ROW_TILE, tid = threadIdx.x, lane = tid & 31, xd = dots_xd(P.d);
-    double *tiles_all = reinterpret_cast<double *>(smem);
-    float *w_all = reinterpret_cast<float *>(tiles_all + (R * ntiles + 1) / 2 * 2);
-    float *h = w_all + (size_t)R * (mp + mp / 4);
-    u64 *xs = reinterpret_cast<u64 *>(h + mp);
-    float *x1 = reinterpret_cast<float *>(xs);
-    const int g = tid / NG;
-    const RowGroup G = {tid % NG, NG, 1 + g, &sc[g]}, all = {tid, NT, 0, &sc[0]};
-    float *w = w_all + (size_t)g * mp;
-    double *tiles = tiles_all + (size_t)g * ntiles;
-    unsigned *units = reinterpret_cast<unsigned *>(tiles);       // (never at the same time)
-    constexpr float u24 = 5.9604645e-8f;
+// What the rows of a lane have in common, and a group's room in shared memory.
+struct LaneState {
+    Lane L;
+    int lane;
+    double h_top;
+    float y_max, y_prefix;
+    bool some;
+};
+struct RowRoom {
+    float *w;                    // [mp]
+    double *tiles;               // [mp / 128]
+    float *list;                 // [list_room(mp)] weights, and their columns
+    int *where;
+    float *x;                    // differences: -x, `step` apart; products: room for a row
+    int step;
+    unsigned char *bytes;        // of this warp, [128] (products)
+};
+__host__ __device__ inline int list_room(int mp) { return (mp / 4 + ROW_TILE - 1) / ROW_TILE * ROW_TILE; }
 
-    const int per_lane = (P.rows + R - 1) / R;
-    const long long total = (long long)P.lanes * per_lane, first = total * blockIdx.x / gridDim.x, last = total * (blockIdx.x + 1) / gridDim.x;
-    int at_lane = -1, turn = 0;
-    float y_max = 0.f, y_prefix = 0.f;
-    double h_top = 0.0;
-    bool some = false;
-    for (long long t = first; t < last; ++t) {
-        const int wl = (int)(t / per_lane), r0 = (int)(t % per_lane) * R, lanew = P.lane0 + wl, i0 = P.row0 + r0;
-        const int rows = min(R, P.rows - r0);
-        const size_t row0 = (size_t)lanew * P.n + i0;
-        const Lane L = lane_of(P, lanew);
-        const double *hn = P.hn + (size_t)lanew * mp;
-        if (!L.ok) {
-            for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, NT);
-            continue;
+// Settings of lane `lane`, its largest k g_j (- |y_j|^2), and the others less that; by all threads, NT of them.
+template <int NT, bool DOTS>
+__device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane, float *h, const RowGroup &all)
+{
+    __syncthreads();
+    S.lane = lane;
+    S.L = lane_of(P, lane);
+    const double *hn = P.hn + (size_t)lane * P.mp;
+    double top = -CUDART_INF;
+    float far = 0.f, prefix = 0.f;
+    for (int j = threadIdx.x; j < P.mp; j += NT) {
+        top = fmax(top, hn[j]);
+        if (DOTS) {
+            const float2 s = P.yn[(size_t)lane * P.mp + j];
+            far = fmaxf(far, s.x);
+            prefix = fmaxf(prefix, s.y);
         }
-        if (lanew != at_lane) {
-            // the lane's largest k g_j (- |y_j|^2), and the others less that
-            __syncthreads();
-            double top = -CUDART_INF;
-            float far = 0.f, prefix = 0.f;
-            for (int j = tid; j < mp; j += NT) {
-                top = fmax(top, hn[j]);
-                if (DOTS) {
-                    const float2 s = P.yn[(size_t)lanew * mp + j];
-                    far = fmaxf(far, s.x);
-                    prefix = fmaxf(prefix, s.y);
-                }
-            }
-            h_top = all.largest(top);
-            if (DOTS) { y_max = sqrtf(all.largest(far)); y_prefix = sqrtf(all.largest(prefix)); }
-            some = h_top != -CUDART_INF;
-            for (int j = tid; j < mp; j += NT) h[j] = some ? (float)(hn[j] - h_top) : 0.f;
-            at_lane = lanew;
-            __syncthreads();
-        }
-        if (!some) {
-            for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, NT);
-            continue;
-        }
-        const float k2 = (float)L.k2;
-        const float *yt = P.yt + (size_t)lanew * P.d * mp;
-        if (!DOTS) {
-            for (int q = tid; q < R * P.d; q += NT) {
-                const int r = q / P.d, k = q % P.d;
-                const float v = r < rows ? -raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k) : 0.f;
-                xs[k * R + r] = pack2(v, v);
-            }
-            __syncthreads();
-            // rows too short for all threads to have four columns of them: fewer rows to a thread
-            if constexpr (R == 8) {
-                if (mp > 512) form_rows<R, NT, 8>(yt, h, xs, w_all, mp, P.d, k2);
-                else if (mp > 256) form_rows<R, NT, 4>(yt, h, xs, w_all, mp, P.d, k2);
-                else if (mp > 128) form_rows<R, NT, 2>(yt, h, xs, w_all, mp, P.d, k2);
-                else form_rows<R, NT, 1>(yt, h, xs, w_all, mp, P.d, k2);
-            } else form_rows<R, NT, R>(yt, h, xs, w_all, mp, P.d, k2);
-            __syncthreads();
-        }
-        if (g < rows) {
-            const size_t row = row0 + g;
-            float top = -CUDART_INF_F;
-            if (DOTS) {
-                const float *dots = P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo;
-                const float two_k = (float)(2.0 * L.k2);
-#pragma unroll 8
-                for (int j = 4 * G.t; j < mp; j += 4 * NG) {
-                    float v[4], hh[4];
-                    load4(dots + j, v);
-                    load4(h + j, hh);
+    }
+    S.h_top = all.largest(top);
+    if (DOTS) { S.y_max = sqrtf(all.largest(far)); S.y_prefix = sqrtf(all.largest(prefix)); }
+    S.some = S.L.ok && S.h_top != -CUDART_INF;
+    for (int j = threadIdx.x; j < P.mp; j += NT) h[j] = S.some ? (float)(hn[j] - S.h_top) : 0.f;
+    __syncthreads();
+}
+
+// One row by its group: exponents (in w for differences, to be formed from `dots` for products) to weights, cut, draws.
+template <bool DOTS>
+__device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t row, const RowGroup &G, int &turn, const RowRoom &M, const float *h,
+                                       const float *dots)
+{
+    constexpr float u24 = 5.9604645e-8f;
+    const int mp = P.mp, ntiles = mp / ROW_TILE, lane = G.t & 31;
+    float *w = M.w;
+    unsigned *units = reinterpret_cast<unsigned *>(M.tiles);     // (never at the same time)
+    const Span span(G, mp);
+    const float u_first = P.u[row * P.S];
+    float2 xn = make_float2(0.f, 0.f);
+    float top = -CUDART_INF_F;
+    if (DOTS) {
+        xn = P.xn[row];
+        const float two_k = (float)(2.0 * S.L.k2);
+        for (int j0 = span.begin; j0 < span.end; j0 += 8 * span.step) {
+            float4 d[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (j0 + q * ROW_TILE < span.end) d[q] = *reinterpret_cast<const float4 *>(dots + j0 + q * ROW_TILE);
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                if (j0 + q * ROW_TILE < span.end) {
+                    float v[4] = {d[q].x, d[q].y, d[q].z, d[q].w}, hh[4];
+                    load4(h + j0 + q * ROW_TILE, hh);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         v[i] = hh[i] == -CUDART_INF_F ? -CUDART_INF_F : fmaf(two_k, v[i], hh[i]);
                         top = fmaxf(top, v[i]);
                     }
-                    *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4 *>(w + j0 + q * ROW_TILE) = make_float4(v[0], v[1], v[2], v[3]);
                 }
-            } else {
-#pragma unroll 4
-                for (int j = 4 * G.t; j < mp; j += 4 * NG) {
-                    float v[4];
-                    load4(w + j, v);
-                    top = fmaxf(fmaxf(top, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
-                }
-            }
-            top = group_largest(G, top, turn);
-            // nothing left in fp32's range, a NaN or an infinite exponent: float64 tells which
-            bool sure = false;
-            if (top != -CUDART_INF_F) {
-                float mass = 0.f, depth = 0.f;
-                unsigned count = 0;
-#pragma unroll 4
-                for (int j = 4 * G.t; j < mp; j += 4 * NG) {        // (each thread's own: no barrier yet)
-                    float v[4];
-                    load4(w + j, v);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float below = top - v[i];
-                        v[i] = ex2_fast(-below);
-                        count += v[i] > 0.f;
-                        depth += v[i] > 0.f ? v[i] * below : 0.f;
-                    }
-                    *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
-                    mass += (v[0] + v[1]) + (v[2] + v[3]);
-                }
-                const unsigned own = count;
-                group_sums(G, mass, depth, count, turn);
-                G.sync();
-                if (mass <= 3e38f) {
-                    const float A = fabsf(top), adds = u24 * (float)(12 + mp / (4 * NG));
-                    float fixed, slope, x_norm = 0.f;               // of an exponent: fixed + slope q
-                    if (DOTS) {
-                        const float2 xn = P.xn[row];
-                        x_norm = sqrtf(xn.x);
-                        const float b = 2.f * k2 * x_norm * y_max, bp = 2.f * k2 * sqrtf(xn.y) * y_prefix;
-                        slope = 3.f * u24;
-                        fixed = u24 * (2.f * (float)((P.d + 15) / 16) * bp + 7.f * b + 3.f * A);
-                    } else {
-                        slope = (float)(P.d + 6) * u24;
-                        fixed = slope * A;
-                    }
-                    fixed = 0.6932f * fixed + 2.4e-7f;
-                    slope = 0.6932f * (slope + u24);
-                    // (of two weights: twice the error of one)
-                    const RowError err = {1.0, 2.f * fixed, 2.f * slope};
-                    const float off = fixed + 24.f * slope;
-                    if (off < 0.01f) {
-                        const float unit = QUICK_ONE / mass;
-                        // (roundings to units: half of one for each thread of a pass, and for each of 32 in a tile, twice)
-                        const QuickSlack slack = {1.02f * fixed * QUICK_ONE, (2.f * adds + slope * depth / mass) * QUICK_ONE + (float)(NG + 32 * ntiles)};
-                        QuickCut cut;
-                        sure = quick_cut(w, mp, G, L.cuts, count, own, unit, slack, err, w_all + (size_t)R * mp + (size_t)g * (mp / 4), mp / 4, cut, turn);
-                        if (sure) {
-                            quick_tiles(w, ntiles, G, cut.tau, unit, units);
-                            G.sync();
-                            const unsigned whole = quick_total(units, ntiles);
-                            for (int s = G.t >> 5; s < P.S; s += NG >> 5) {
-                                const float u = P.u[row * P.S + s];
-                                int j = -1;
-                                float wj = 0.f;
-                                if (u >= 0.f && u < 1.f && !quick_draw(w, ntiles, cut.tau, unit, units, whole, u, slack, j, wj)) { sure = false; continue; }
-                                if (lane == 0) put_draw(P, row * P.S + s, j, j < 0 ? CUDART_NAN_F : logf(wj * unit / (float)whole));
-                            }
-                        }
-                        sure = group_all(G, sure, turn);
-                        if (!sure) {
-                            // once more, with better weights for what counts
-                            G.sync();
-                            sure = again<DOTS>(P, L, lanew, row, G, h_top + (double)top, off, x_norm * y_max, DOTS ? x1 + (size_t)g * xd : x1 + 2 * g,
-                                               2 * R, w, tiles, lists[DOTS ? tid >> 5 : 0]);
-                            sure = group_all(G, sure, turn);
-                        }
-                    }
-                }
-            }
-            if (!sure && G.t == 0) P.list[1 + (long long)atomicAdd((unsigned long long *)P.list, 1ull)] = (long long)row;
-            G.sync();
         }
+    } else {
+#pragma unroll 4
+        for (int j = span.begin; j < span.end; j += span.step) {
+            float v[4];
+            load4(w + j, v);
+            top = fmaxf(fmaxf(top, fmaxf(v[0], v[1])), fmaxf(v[2], v[3]));
+        }
+    }
+    top = group_largest(G, top, turn);
+    // nothing left in fp32's range, a NaN or an infinite exponent: float64 tells which
+    bool sure = false;
+    if (top != -CUDART_INF_F) {
+        float f[3] = {0.f, 0.f, 0.f};                            // mass, sum of w log2(1 / w), mass below ROW_TAIL
+        unsigned count = 0, heavy = 0, before;
+#pragma unroll 4
+        for (int j = span.begin; j < span.end; j += span.step) { // (each thread's own: no barrier yet)
+            float v[4];
+            load4(w + j, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float below = top - v[i];
+                v[i] = ex2_fast(-below);
+                count += v[i] > 0.f;
+                heavy += v[i] >= ROW_TAIL;
+                f[2] += v[i] >= ROW_TAIL ? 0.f : v[i];
+                f[1] += v[i] > 0.f ? v[i] * below : 0.f;
+            }
+            *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
+            f[0] += (v[0] + v[1]) + (v[2] + v[3]);
+        }
+        const unsigned own = count;
+        group_sums(G, f, count, heavy, before, turn);
+        G.sync();
+        const float mass = f[0];
+        if (mass <= 3e38f) {
+            const float k2 = (float)S.L.k2, A = fabsf(top), adds = u24 * (float)(12 + mp / (4 * G.nt));
+            float fixed, slope, bound = 0.f;                     // of an exponent: fixed + slope q
+            if (DOTS) {
+                bound = sqrtf(xn.x) * S.y_max;
+                slope = 3.f * u24;
+                fixed = u24 * (2.f * k2 * (2.f * (float)((P.d + 15) / 16) * sqrtf(xn.y) * S.y_prefix + 7.f * bound) + 3.f * A);
+            } else {
+                slope = (float)(P.d + 6) * u24;
+                fixed = slope * A;
+            }
+            fixed = 0.6932f * fixed + 2.4e-7f;
+            slope = 0.6932f * (slope + u24);
+            const RowError err = {1.0, 2.f * fixed, 2.f * slope};    // of two weights: twice the error of one
+            const float off = fixed + 24.f * slope;
+            if (off < 0.01f) {
+                const float unit = QUICK_ONE / mass;
+                // (roundings to units: half of one for each thread of a pass, and for each of 32 in a tile, twice)
+                QuickSlack slack = {1.02f * fixed * QUICK_ONE, (2.f * adds + slope * f[1] / mass) * QUICK_ONE + (float)(G.nt + 32 * ntiles)};
+                const bool sparse = ntiles >= 4 && heavy <= (unsigned)mp / 4 && f[2] * 1048576.f <= mass;
+                if (sparse) {
+                    // few entries weigh anything: they are the row, by one warp, the others an error of the sums
+                    slack.rest += 2.f * f[2] * unit;
+                    for (int j = span.begin; j < span.end; j += span.step) {
+                        float v[4];
+                        load4(w + j, v);
+                        unsigned ball[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) ball[i] = __ballot_sync(0xffffffffu, v[i] >= ROW_TAIL);
+                        if (!(ball[0] | ball[1] | ball[2] | ball[3])) continue;
+                        unsigned at = before;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { at += __popc(ball[i] & ((1u << lane) - 1u)); before += __popc(ball[i]); }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (v[i] >= ROW_TAIL) { M.list[at] = v[i]; M.where[at] = j + i; ++at; }
+                    }
+                    const int len = (int)(heavy + ROW_TILE - 1) / ROW_TILE * ROW_TILE;
+                    for (int j = (int)heavy + G.t; j < len; j += G.nt) M.list[j] = 0.f;
+                    G.sync();
+                }
+                const int len = sparse ? (int)(heavy + ROW_TILE - 1) / ROW_TILE * ROW_TILE : mp;
+                const float *r = sparse ? M.list : w;
+                const RowGroup A1 = {sparse ? lane : G.t, sparse ? 32 : G.nt, G.bar, G.sc};
+                sure = true;
+                if (!sparse || G.t < 32) {
+                    RowCuts cuts = S.L.cuts;
+                    QuickCut cut;
+                    sure = quick_cut(r, len, A1, cuts, sparse ? heavy : count, own, unit, slack, err, M.list, sparse ? 0u : (unsigned)mp / 4, cut, turn);
+                    if (sure) {
+                        quick_tiles(r, len / ROW_TILE, A1, cut.tau, unit, units);
+                        A1.sync();
+                        const unsigned whole = quick_total(units, len / ROW_TILE);
+                        for (int s = A1.t >> 5; s < P.S; s += A1.nt >> 5) {
+                            const float u = s ? P.u[row * P.S + s] : u_first;
+                            int j = -1;
+                            float wj = 0.f;
+                            if (u >= 0.f && u < 1.f && !quick_draw(r, len / ROW_TILE, cut.tau, unit, units, whole, u, slack, j, wj)) { sure = false; continue; }
+                            if (lane == 0) put_draw(P, row * P.S + s, sparse && j >= 0 ? M.where[j] : j, j < 0 ? CUDART_NAN_F : logf(wj * unit / (float)whole));
+                        }
+                    }
+                }
+                sure = group_all(G, sure, turn);
+                if (!sure) {
+                    // once more, with better weights for what counts
+                    G.sync();
+                    sure = again<DOTS>(P, S.L, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, w, M.tiles, M.bytes);
+                    sure = group_all(G, sure, turn);
+                }
+            }
+        }
+    }
+    if (!sure && G.t == 0) P.list[1 + (long long)atomicAdd((unsigned long long *)P.list, 1ull)] = (long long)row;
+    G.sync();
+}
+
+// Rows that a warp holds: each warp for itself, RW rows at a time where exponents are formed from differences (a column's
+// coordinates serve them all).  No barrier but where the lane changes, so warps need not wait for each other's rows.
+constexpr int WARPS = 8;
+template <int RW, bool DOTS>
+struct WarpShape {
+    int x, warp;                 // bytes: of a warp's points, and of all it has
+    size_t all;
+    __host__ __device__ WarpShape(int mp, int d)
+    {
+        x = DOTS ? dots_xd(d) * 4 : (RW * d * 8 + 15) / 16 * 16;
+        warp = RW * mp * 4 + list_room(mp) * 8 + (mp / ROW_TILE + 1) / 2 * 16 + x;
+        all = (size_t)mp * 4 + (size_t)WARPS * warp;
+    }
+};
+template <int RW>
+__device__ __forceinline__ void form_warp(const float *yt, const float *h, const u64 *xs, float *w, int mp, int d, float k2)
+{
+    for (int j = 4 * (threadIdx.x & 31); j < mp; j += ROW_TILE) {
+        u64 acc[RW][2];
+#pragma unroll
+        for (int r = 0; r < RW; ++r) acc[r][0] = acc[r][1] = 0ull;
+#pragma unroll 4
+        for (int k = 0; k < d; ++k) {
+            const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(yt + (size_t)k * mp + j);
+#pragma unroll
+            for (int r = 0; r < RW; ++r) {
+                const u64 x = xs[k * RW + r], a = add2(y.x, x), b = add2(y.y, x);
+                acc[r][0] = fma2(a, a, acc[r][0]);
+                acc[r][1] = fma2(b, b, acc[r][1]);
+            }
+        }
+        const ulonglong2 hh = *reinterpret_cast<const ulonglong2 *>(h + j);
+        const u64 s = pack2(-k2, -k2);
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+            const ulonglong2 t = {fma2(s, acc[r][0], hh.x), fma2(s, acc[r][1], hh.y)};
+            *reinterpret_cast<ulonglong2 *>(w + (size_t)r * mp + j) = t;
+        }
+    }
+}
+template <int RW, bool DOTS>
+__global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(const Draw P)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowScratch sc[WARPS];
+    __shared__ unsigned char bytes[DOTS ? WARPS : 1][ROW_TILE];
+    const int mp = P.mp, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const WarpShape<RW, DOTS> shape(mp, P.d);
+    float *h = reinterpret_cast<float *>(smem), *w = reinterpret_cast<float *>(smem + (size_t)mp * 4 + (size_t)warp * shape.warp);
+    RowRoom M;
+    M.list = w + RW * mp;
+    M.where = reinterpret_cast<int *>(M.list + list_room(mp));
+    M.tiles = reinterpret_cast<double *>(M.where + list_room(mp));
+    u64 *xs = reinterpret_cast<u64 *>(M.tiles + (mp / ROW_TILE + 1) / 2 * 2);
+    M.step = 2 * RW;
+    M.bytes = bytes[DOTS ? warp : 0];
+    const RowGroup G = {lane, 32, 0, &sc[warp]}, all = {(int)threadIdx.x, WARPS * 32, 0, &sc[0]};
+    int turn = 0;
+    // units of RW rows, the block's a range of all lanes'
+    const unsigned per_lane = (P.rows + RW - 1) / RW;
+    const unsigned long long total = (unsigned long long)P.lanes * per_lane;
+    const unsigned first = (unsigned)(total * blockIdx.x / gridDim.x), last = (unsigned)(total * (blockIdx.x + 1) / gridDim.x);
+    LaneState S;
+    unsigned at = first;
+    while (at < last) {
+        const unsigned wl = at / per_lane, lane_end = (wl + 1) * per_lane, end = last < lane_end ? last : lane_end;
+        enter_lane<WARPS * 32, DOTS>(P, S, P.lane0 + (int)wl, h, all);
+        const float *yt = P.yt + (size_t)S.lane * P.d * mp;
+        for (unsigned u = at + warp; u < end; u += WARPS) {
+            const int r0 = (int)(u - wl * per_lane) * RW, rows = min(RW, P.rows - r0);
+            const size_t row0 = (size_t)S.lane * P.n + P.row0 + r0;
+            if (!S.some) {
+                for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, lane, 32);
+                continue;
+            }
+            if (!DOTS) {
+                for (int q = lane; q < RW * P.d; q += 32) {
+                    const int r = q / P.d, k = q % P.d;
+                    const float v = r < rows ? -raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k) : 0.f;
+                    xs[k * RW + r] = pack2(v, v);
+                }
+                __syncwarp();
+                form_warp<RW>(yt, h, xs, w, mp, P.d, (float)S.L.k2);
+                __syncwarp();
+            }
+            for (int r = 0; r < rows; ++r) {
+                M.w = w + (size_t)r * mp;
+                M.x = reinterpret_cast<float *>(xs) + (DOTS ? 0 : 2 * r);
+                do_row<DOTS>(P, S, row0 + r, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + r) * P.ldo : nullptr);
+            }
+        }
+        at = end;
+    }
+}
+
+// Longer rows, R to a block: the block's 512 threads form them, then 512 / R threads have a row each.
+template <int R, bool DOTS>
+struct GroupShape {
+    int x;
+    size_t all;
+    __host__ __device__ GroupShape(int mp, int d)
+    {
+        x = DOTS ? R * dots_xd(d) * 4 : R * d * 8;
+        all = (size_t)mp * 4 + (size_t)R * (mp * 4 + list_room(mp) * 8 + (mp / ROW_TILE + 1) / 2 * 16) + x;
+    }
+};
+template <int R>
+__device__ __forceinline__ void form_rows(const float *yt, const float *h, const u64 *xs, float *w, int mp, int d, float k2)
+{
+    for (int j = 4 * threadIdx.x; j < mp; j += 4 * 512) {
+        u64 acc[R][2];
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[r][0] = acc[r][1] = 0ull;
+#pragma unroll 4
+        for (int k = 0; k < d; ++k) {
+            const ulonglong2 y = *reinterpret_cast<const ulonglong2 *>(yt + (size_t)k * mp + j);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const u64 x = xs[k * R + r], a = add2(y.x, x), b = add2(y.y, x);
+                acc[r][0] = fma2(a, a, acc[r][0]);
+                acc[r][1] = fma2(b, b, acc[r][1]);
+            }
+        }
+        const ulonglong2 hh = *reinterpret_cast<const ulonglong2 *>(h + j);
+        const u64 s = pack2(-k2, -k2);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const ulonglong2 t = {fma2(s, acc[r][0], hh.x), fma2(s, acc[r][1], hh.y)};
+            *reinterpret_cast<ulonglong2 *>(w + (size_t)r * mp + j) = t;
+        }
+    }
+}
+template <int R, bool DOTS>
+__global__ void __launch_bounds__(512, 1) draw_groups_kernel(const Draw P)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowScratch sc[R];
+    __shared__ unsigned char bytes[DOTS ? 16 : 1][ROW_TILE];
+    constexpr int NG = 512 / R;                                  // threads of a row's group
+    const int mp = P.mp, tid = threadIdx.x, g = tid / NG, room = list_room(mp), nt2 = (mp / ROW_TILE + 1) / 2 * 2;
+    float *h = reinterpret_cast<float *>(smem), *w = h + mp;
+    u64 *xs = reinterpret_cast<u64 *>(w + (size_t)R * (mp + 2 * room) + (size_t)R * nt2 * 2);
+    RowRoom M;
+    M.w = w + (size_t)g * mp;
+    M.list = w + (size_t)R * mp + (size_t)g * 2 * room;
+    M.where = reinterpret_cast<int *>(M.list + room);
+    M.tiles = reinterpret_cast<double *>(w + (size_t)R * (mp + 2 * room)) + (size_t)g * nt2;
+    M.x = reinterpret_cast<float *>(xs) + (DOTS ? g * dots_xd(P.d) : 2 * g);
+    M.step = 2 * R;
+    M.bytes = bytes[DOTS ? tid >> 5 : 0];
+    const RowGroup G = {tid % NG, NG, 1 + g, &sc[g]}, all = {tid, 512, 0, &sc[0]};
+    int turn = 0;
+    const unsigned per_lane = (P.rows + R - 1) / R;
+    const unsigned long long total = (unsigned long long)P.lanes * per_lane;
+    const unsigned first = (unsigned)(total * blockIdx.x / gridDim.x), last = (unsigned)(total * (blockIdx.x + 1) / gridDim.x);
+    LaneState S;
+    S.lane = -1;
+    for (unsigned t = first; t < last; ++t) {
+        const unsigned wl = t / per_lane;
+        const int r0 = (int)(t - wl * per_lane) * R, rows = min(R, P.rows - r0);
+        if (P.lane0 + (int)wl != S.lane) enter_lane<512, DOTS>(P, S, P.lane0 + (int)wl, h, all);
+        const size_t row0 = (size_t)S.lane * P.n + P.row0 + r0;
+        if (!S.some) {
+            for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, 512);
+            continue;
+        }
+        if (!DOTS) {
+            for (int q = tid; q < R * P.d; q += 512) {
+                const int r = q / P.d, k = q % P.d;
+                const float v = r < rows ? -raw_value(P.x, P.x4, P.dtype, row0 + r, P.d, k) : 0.f;
+                xs[k * R + r] = pack2(v, v);
+            }
+            __syncthreads();
+            form_rows<R>(P.yt + (size_t)S.lane * P.d * mp, h, xs, w, mp, P.d, (float)S.L.k2);
+            __syncthreads();
+        }
+        if (g < rows) do_row<DOTS>(P, S, row0 + g, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo : nullptr);
         if (!DOTS) __syncthreads();
     }
 }
 
 size_t exact_smem(const Draw &P) { return (size_t)P.mp / ROW_TILE * 8 + (size_t)dots_xd(P.d) * 8; }
 
-// How a problem is run: rows to a block, where the exponents come from, and the rows whose products are held at a time.
+// How a problem is run: the kernel and its rows to a warp or a block, where the exponents come from, and the rows whose
+// products are held at a time.
 struct Plan {
-    int R;                                                  // 8, 4, 1; 0: too long for shared memory
+    int warp_rows, block_rows;                              // one of them; neither: too long for shared memory
     bool dots;
-    int lanes, rows;
+    int lanes, rows, fit;                                   // fit: blocks to an SM
     size_t smem;
+    bool fp32() const { return warp_rows || block_rows; }
 };
-constexpr size_t DRAW_SMEM = 216 * 1024;                     // dynamic; a block has 8 KB more, an SM 227 KB
+constexpr size_t DRAW_SMEM = 216 * 1024;                    // dynamic; a block has up to 9 KB more, an SM 227 KB
+template <int RW, bool DOTS>
+bool warps_fit(Plan &p, int mp, int d, size_t most)
+{
+    p.smem = WarpShape<RW, DOTS>(mp, d).all;
+    if (p.smem > most) return false;
+    p.warp_rows = RW;
+    p.fit = (int)std::min<size_t>(DOTS ? 2 : 3, 226 * 1024 / (p.smem + 10 * 1024));
+    return true;
+}
+template <int R, bool DOTS>
+bool groups_fit(Plan &p, int mp, int d)
+{
+    p.smem = GroupShape<R, DOTS>(mp, d).all;
+    if (p.smem > DRAW_SMEM) return false;
+    p.block_rows = R;
+    p.fit = 1;
+    return true;
+}
 Plan plan_of(const Draw &P)
 {
     Plan p = {};
     // Deep clouds whose rows TMA can take.  Below 64 dimensions the products are a small part of a pair's work.
     p.dots = P.dtype == SKB_F32 ? false : P.d >= 64 && (P.dtype != SKB_BF16 || P.d % 8 == 0);
-    const size_t s8 = DrawShape<8, 256>::smem(P.mp, P.d, p.dots), s4 = DrawShape<4, 512>::smem(P.mp, P.d, p.dots),
-                 s1 = DrawShape<1, 512>::smem(P.mp, P.d, p.dots);
-    // eight rows while two blocks share an SM, four while one fits
-    if (s8 + 10 * 1024 <= DRAW_SMEM / 2) { p.R = 8; p.smem = s8; }
-    else if (s4 + 64 <= DRAW_SMEM) { p.R = 4; p.smem = s4; }
-    else if (s1 + 64 <= DRAW_SMEM) { p.R = 1; p.smem = s1; }
-    p.smem += 64;
+    // A row to a warp while two blocks share an SM, three where that leaves more rows to a warp; then a row to four warps,
+    // then to a block.
+    const size_t three = 65 * 1024, two = 103 * 1024;
+    if (p.dots) (void)(warps_fit<1, true>(p, P.mp, P.d, two) || groups_fit<4, true>(p, P.mp, P.d) || groups_fit<1, true>(p, P.mp, P.d));
+    else (void)(warps_fit<4, false>(p, P.mp, P.d, three) || warps_fit<2, false>(p, P.mp, P.d, three) || warps_fit<1, false>(p, P.mp, P.d, two) ||
+                groups_fit<4, false>(p, P.mp, P.d) || groups_fit<1, false>(p, P.mp, P.d));
     p.lanes = P.W; p.rows = P.n;
-    if (p.dots && p.R) {
+    if (!p.fp32()) p.dots = false;
+    if (p.dots) {
         const size_t lane = (size_t)P.n * P.mp * 4;
         if (lane <= DRAW_DOTS_BYTES) p.lanes = (int)std::min<size_t>(P.W, DRAW_DOTS_BYTES / lane);
         else { p.lanes = 1; p.rows = (int)std::max<size_t>(128, DRAW_DOTS_BYTES / ((size_t)P.mp * 4) / 128 * 128); }
@@ -732,32 +948,42 @@ size_t carve(Draw &P, const Plan &p, char *base)
     size_t at = 0;
     auto take = [&](size_t bytes) { char *q = base ? base + at : nullptr; at += (bytes + 255) / 256 * 256; return q; };
     P.hn = (double *)take((size_t)P.W * P.mp * 8);
-    if (p.dots && p.R) {
+    if (p.dots) {
         P.yn = (float2 *)take((size_t)P.W * P.mp * 8);
         P.xn = (float2 *)take((size_t)P.W * P.n * 8);
         P.dots = (const float *)take((size_t)p.lanes * p.rows * P.mp * 4);
     } else P.yt = (float *)take((size_t)P.W * P.d * P.mp * 4);
     P.scratch = (double *)take((size_t)DRAW_EXACT_BLOCKS * P.mp * 8);
-    if (p.R) P.list = (long long *)take(((size_t)P.W * P.n + 1) * 8);
+    if (p.fp32()) P.list = (long long *)take(((size_t)P.W * P.n + 1) * 8);
     return at;
 }
 
-template <int R, int NT, bool DOTS>
-void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
+// (limits for any shape: another host thread may set one between this and the launch)
+template <int RW, bool DOTS>
+void launch_warps(const Draw &P, const Plan &p, cudaStream_t st)
 {
-    // (the limit for any shape: another host thread may set it between this and the launch)
-    cudaFuncSetAttribute(draw_kernel<R, NT, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(R == 8 ? DRAW_SMEM / 2 : DRAW_SMEM));
-    const long long tiles = (long long)P.lanes * ((P.rows + R - 1) / R);
-    const size_t fit = NT > 256 ? 1 : std::min<size_t>(3, 226 * 1024 / (p.smem + 10 * 1024));
-    const long long most = (long long)(DRAW_BLOCKS * fit);
-    draw_kernel<R, NT, DOTS><<<(unsigned)(tiles < most ? tiles : most), NT, p.smem, st>>>(P);
+    cudaFuncSetAttribute(draw_warps_kernel<RW, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DRAW_SMEM / 2);
+    const long long units = (long long)P.lanes * ((P.rows + RW - 1) / RW), blocks = (units + WARPS - 1) / WARPS, most = DRAW_BLOCKS * p.fit;
+    draw_warps_kernel<RW, DOTS><<<(unsigned)(blocks < most ? blocks : most), WARPS * 32, p.smem, st>>>(P);
 }
-template <bool DOTS>
+template <int R, bool DOTS>
+void launch_groups(const Draw &P, const Plan &p, cudaStream_t st)
+{
+    cudaFuncSetAttribute(draw_groups_kernel<R, DOTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DRAW_SMEM);
+    const long long units = (long long)P.lanes * ((P.rows + R - 1) / R);
+    draw_groups_kernel<R, DOTS><<<(unsigned)(units < DRAW_BLOCKS ? units : DRAW_BLOCKS), 512, p.smem, st>>>(P);
+}
 void launch_draw(const Draw &P, const Plan &p, cudaStream_t st)
 {
-    if (p.R == 8) launch_draw<8, 256, DOTS>(P, p, st);
-    else if (p.R == 4) launch_draw<4, 512, DOTS>(P, p, st);
-    else launch_draw<1, 512, DOTS>(P, p, st);
+    if (p.dots) {
+        if (p.warp_rows) launch_warps<1, true>(P, p, st);
+        else if (p.block_rows == 4) launch_groups<4, true>(P, p, st);
+        else launch_groups<1, true>(P, p, st);
+    } else if (p.warp_rows == 4) launch_warps<4, false>(P, p, st);
+    else if (p.warp_rows == 2) launch_warps<2, false>(P, p, st);
+    else if (p.warp_rows == 1) launch_warps<1, false>(P, p, st);
+    else if (p.block_rows == 4) launch_groups<4, false>(P, p, st);
+    else launch_groups<1, false>(P, p, st);
 }
 
 const char *refused(const skb_draw_config *c)
@@ -812,19 +1038,21 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
     const Plan p = plan_of(P);
     carve(P, p, (char *)cfg->workspace);
     cudaStream_t st = (cudaStream_t)cfg->stream;
-    if (!p.dots || !p.R) transpose_kernel<<<dim3(P.mp / 32, P.W), 256, 0, st>>>(P);
-    auto exact_rows = [&] {
+    if (!p.dots) transpose_kernel<<<dim3(P.mp / 32, P.W), 256, 0, st>>>(P);
+    auto exact = [&] {
         const long long rows = (long long)P.W * P.n;
         draw_exact_kernel<<<(unsigned)(rows < DRAW_EXACT_BLOCKS ? rows : DRAW_EXACT_BLOCKS), 512, exact_smem(P), st>>>(P);
         return op_launched("plan_draw");
     };
-    if (!p.R) return exact_rows();
+    if (!p.fp32()) return exact();
     if (!p.dots) {
         P.lanes = P.W; P.rows = P.n;
-        launch_draw<false>(P, p, st);
-        return exact_rows();
+        launch_draw(P, p, st);
+        return exact();
     }
-    norms_kernel<<<dim3((P.mp + P.n + 7) / 8, P.W), 256, 0, st>>>(P);
+    const dim3 points((P.mp + P.n + 7) / 8, P.W);
+    if (P.dtype == SKB_BF16) norms_kernel<true><<<points, 256, 0, st>>>(P);
+    else norms_kernel<false><<<points, 256, 0, st>>>(P);
     P.ldo = P.mp;
     for (P.lane0 = 0; P.lane0 < P.W; P.lane0 += p.lanes)
         for (P.row0 = 0; P.row0 < P.n; P.row0 += p.rows) {
@@ -834,7 +1062,7 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
                                              dots_cloud(P.y, P.y4, P.dtype, P.d, (size_t)P.lane0 * P.m), P.dtype, P.lanes, P.rows, P.m,
                                              const_cast<float *>(P.dots), P.ldo, st);
             if (s != SKB_OK) return s;
-            launch_draw<true>(P, p, st);
+            launch_draw(P, p, st);
         }
-    return exact_rows();
+    return exact();
 }

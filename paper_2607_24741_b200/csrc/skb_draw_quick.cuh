@@ -62,7 +62,19 @@ struct QuickSlack {
 struct QuickCut {
     float tau;                          // kept: weights from here on
     unsigned count, mass;               // of what is kept; mass in units
-    unsigned own;                       // this thread's of `count`, where a thread has the entries 4 (t + i nt) ... + 3
+    unsigned own;                       // this thread's of `count`
+};
+
+// Quadruples of a row that a thread has: whole tiles to a warp, one after the other.
+struct Span {
+    int begin, end, step;
+    __device__ __forceinline__ Span(const RowGroup &G, int mp)
+    {
+        const int nw = G.nt >> 5, gw = G.t >> 5, tiles = mp / ROW_TILE;
+        begin = tiles * gw / nw * ROW_TILE + 4 * (G.t & 31);
+        end = tiles * (gw + 1) / nw * ROW_TILE;
+        step = ROW_TILE;
+    }
 };
 
 // Exclusive sum over the group's threads of a count each.
@@ -92,14 +104,16 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
     int lo = cut.tau > 0.f ? __float_as_int(cut.tau) : 1, hi = __float_as_int(2.f);
     unsigned n_lo = cut.count, m_lo = cut.mass, n_hi = 0, m_hi = 0, own_lo = cut.own, own_hi = 0;
     const float *w = row;
+    const Span all(G, mp);
+    Span span = all;
     int n = mp, low_side = 0, high_side = hi;                    // the bracket of what w holds
     unsigned n_out = 0, m_out = 0;                               // number and mass of what is above it
     bool first = true;
     while (n_lo - n_hi > 1) {
-        if (w == row && n_lo - n_hi <= room) {
+        if (w == row && n_lo - n_hi <= room) {                   // (room 0: never)
             // what is in the bracket to the list, zeros behind it up to whole quadruples
             unsigned at = group_offset(G, own_lo - own_hi, turn);
-            for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+            for (int j = all.begin; j < all.end; j += all.step) {
                 float x[4];
                 load4(row + j, x);
 #pragma unroll
@@ -110,6 +124,7 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
             if (G.t < n - (int)(n_lo - n_hi)) list[n_lo - n_hi + G.t] = 0.f;
             G.sync();
             w = list; low_side = lo; high_side = hi; n_out = n_hi; m_out = m_hi;
+            span.begin = 4 * G.t; span.end = n; span.step = 4 * G.nt;
         }
         const int gap = hi - lo;
         if (gap < 16) return false;                              // equal weights, or nearly
@@ -128,7 +143,7 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
         float s[3] = {0.f, 0.f, 0.f};
         unsigned v[6] = {0, 0, 0, 0, 0, 0};
 #pragma unroll 2
-        for (int j = 4 * G.t; j < n; j += 4 * G.nt) {
+        for (int j = span.begin; j < span.end; j += span.step) {
             float x[4];
             load4(w + j, x);
 #pragma unroll
@@ -151,7 +166,7 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
     // the entry that is left in [lo, hi), and its neighbours; those outside of the list are outside of its bracket
     unsigned at = 0, below = (unsigned)low_side, above = (unsigned)high_side, kept = 0;
 #pragma unroll 2
-    for (int j = 4 * G.t; j < n; j += 4 * G.nt) {
+    for (int j = span.begin; j < span.end; j += span.step) {
         float x[4];
         load4(w + j, x);
 #pragma unroll
@@ -166,9 +181,9 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
     cut.tau = __uint_as_float(at);
     cut.count = n_lo;
     cut.mass = m_lo;
-    if (!by_mass) {
+    if (!by_mass && room) {
         // (a cut by mass may follow)
-        for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+        for (int j = all.begin; j < all.end; j += all.step) {
             float x[4];
             load4(row + j, x);
 #pragma unroll
@@ -196,8 +211,9 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
         const float e = err.weight - err.slope * log2f(want.r);
         const float low = want.r * (1.f - e), high = want.r * (1.f + e);
         unsigned near_[1] = {0};
+        const Span all(G, mp);
 #pragma unroll 4
-        for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
+        for (int j = all.begin; j < all.end; j += all.step) {
             float x[4];
             load4(w + j, x);
 #pragma unroll
