@@ -81,7 +81,7 @@ __device__ __forceinline__ float raw_value(const void *base, const Cloud4 &c, in
     return cloud4_value(c, row, k);
 }
 // Transposed copy of y and k g, 32 points to a block.  Masked points get coordinates of zero, whatever theirs are.
-__global__ void __launch_bounds__(256) transpose_kernel(const Draw P)
+__global__ void __launch_bounds__(256) transpose_kernel(const __grid_constant__ Draw P)
 {
     __shared__ float tile[32][33];
     __shared__ int masked[32];
@@ -175,7 +175,7 @@ __device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, s
 }
 // k (g - |y|^2), and what bounds the error of the products, a warp to a point.
 template <bool BF>
-__global__ void __launch_bounds__(256) norms_kernel(const Draw P)
+__global__ void __launch_bounds__(256) norms_kernel(const __grid_constant__ Draw P)
 {
     const int w = blockIdx.y, i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     double p = 0.0;
@@ -202,21 +202,21 @@ __device__ __forceinline__ void put_draw(const Draw &P, size_t at, int index, fl
     if (P.logp) P.logp[at] = logp;
 }
 
-// Draws of one row from weights and their cut, shared out to the group's warps.  True if all of this warp's were sure.
+// Draws of one row from `len` weights, of columns `where` (null: their places), and their cut, shared out to the group's warps.  True if all of this warp's were sure.
 template <typename Real>
-__device__ bool draw_all(const Draw &P, size_t row, const Real *w, const RowCut<Real> &cut, const double *tiles, const RowError &err, int warp, int warps)
+__device__ bool draw_all(const Draw &P, size_t row, const Real *w, int len, const unsigned short *where, const RowCut<Real> &cut, const double *tiles, const RowError &err, int warp, int warps)
 {
-    const double total = row_total(tiles, P.mp / ROW_TILE);
+    const double total = row_total(tiles, len / ROW_TILE);
     bool sure = true;
     for (int s = warp; s < P.S; s += warps) {
         const float u = P.u[row * P.S + s];
         int j = -1;
         double wj = 0.0;
         if (u >= 0.f && u < 1.f) {
-            const bool good = row_draw(w, cut, tiles, P.mp / ROW_TILE, total, (double)u, err, j, wj);
+            const bool good = row_draw(w, cut, tiles, len / ROW_TILE, total, (double)u, err, j, wj);
             if (!good) { sure = false; continue; }
         }
-        if ((threadIdx.x & 31) == 0) put_draw(P, row * P.S + s, j, j < 0 ? CUDART_NAN_F : (float)log(wj / total));
+        if ((threadIdx.x & 31) == 0) put_draw(P, row * P.S + s, where && j >= 0 ? where[j] : j, j < 0 ? CUDART_NAN_F : (float)log(wj / total));
     }
     return sure;
 }
@@ -232,28 +232,31 @@ template <bool BF>
 __device__ __forceinline__ void exact_rows(const Draw &P, const Lane &L, int w, const double *hn, const double *xs, double *wd, int warp, int warps,
                                            double &top, int &bad)
 {
-    const int lane = threadIdx.x & 31, part = lane & 7, chunks = BF ? P.d / 8 : dots_xd(P.d) / 8;
+    const int lane = threadIdx.x & 31, part = lane & 7, chunks = BF ? P.d / 8 : dots_xd(P.d) / 8, rounds = (chunks + 7) / 8, d = P.d;
+    const void *y_data = P.y;
+    const Cloud4 y4 = P.y4;
     for (int j0 = 4 * warp; j0 < P.mp; j0 += 4 * warps) {
         const int j = j0 + (lane >> 3);
         const bool is = hn[j] != -CUDART_INF;
         double c = 0.0;
         if (is) {
             const size_t row = (size_t)w * P.m + j;
-            const float point = !BF && P.y4.points ? P.y4.points[row] : 1.f;
-            for (int q0 = part; q0 < chunks; q0 += 8 * BATCH) {
-                Eight e[BATCH];
+            const float point = !BF && y4.points ? y4.points[row] : 1.f;
+            for (int r0 = 0; r0 < rounds; r0 += BATCH) {
+                Eight y8[BATCH];
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b)
-                    if (q0 + 8 * b < chunks) e[b] = load_eight<BF>(P.y, P.y4, row, P.d, 8 * (q0 + 8 * b));
+                    if (r0 + b < rounds) y8[b] = load_eight<BF>(y_data, y4, row, d, 8 * min(8 * (r0 + b) + part, chunks - 1));
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b)
-                    if (q0 + 8 * b < chunks) {
+                    if (r0 + b < rounds) {
+                        const int q = 8 * (r0 + b) + part;
                         float y[8];
-                        double part_c = 0.0;
-                        eight_values<BF>(e[b], P.y4, point, y);
+                        double sum = 0.0;
+                        eight_values<BF>(y8[b], y4, point, y);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) { const double f = xs[8 * (q0 + 8 * b) + i] - (double)y[i]; part_c = fma(f, f, part_c); }
-                        c += part_c;
+                        for (int i = 0; i < 8; ++i) { const double f = xs[8 * min(q, chunks - 1) + i] - (double)y[i]; sum = fma(f, f, sum); }
+                        if (q < chunks) c += sum;
                     }
             }
         }
@@ -267,7 +270,7 @@ __device__ __forceinline__ void exact_rows(const Draw &P, const Lane &L, int w, 
 }
 
 // Rows in float64, a block to a row: those of the list, or all (rows too long for shared memory).
-__global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
+__global__ void __launch_bounds__(512) draw_exact_kernel(const __grid_constant__ Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc;
@@ -319,7 +322,7 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const Draw P)
         const RowError none = {0.0, 0.f, 0.f};
         RowCut<double> cut;
         row_cut(wd, P.mp, G, L.cuts, 1.0, mass, count, none, cut, tiles);
-        draw_all(P, (size_t)row, wd, cut, tiles, none, warp, nt >> 5);
+        draw_all(P, (size_t)row, wd, P.mp, nullptr, cut, tiles, none, warp, nt >> 5);
         __syncthreads();
     }
 }
@@ -390,40 +393,47 @@ __device__ __forceinline__ void refine_differences(const Draw &P, double k2, con
 // added to a large number M, whose last place is 2^-24 of a bound on the sum: what an addition cuts off is itself exact and is
 // added up apart, so that the result is good to 2^-40 of the bound.
 template <bool BF>
-__device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl, const double *hn, const float *x, float magic, double base,
-                                                float *w, unsigned char *list, int warp, int warps)
+__device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl, const double *hn, const float *x, float magic, double base, float *w,
+                                                int len, const unsigned short *where, int count, unsigned char *bytes, int warp, int warps)
 {
     const int lane = threadIdx.x & 31, part = lane & 7, col = lane >> 3;
-    const int chunks = BF ? P.d / 8 : dots_xd(P.d) / 8;
-    for (int q = warp; q < P.mp / ROW_TILE; q += warps) {
-        float v[4];
-        load4(w + q * ROW_TILE + 4 * lane, v);
+    const int chunks = BF ? P.d / 8 : dots_xd(P.d) / 8, rounds = (chunks + 7) / 8, m = P.m, d = P.d;
+    const void *y_data = P.y;
+    const Cloud4 y4 = P.y4;
+    for (int q = warp; q < len / ROW_TILE; q += warps) {
         int n = 0;
+        if (where) n = min(ROW_TILE, count - q * ROW_TILE);
+        else {
+            float v[4];
+            load4(w + q * ROW_TILE + 4 * lane, v);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned ball = __ballot_sync(0xffffffffu, v[i] > ROW_FLOOR);
-            if (v[i] > ROW_FLOOR) list[n + __popc(ball & ((1u << lane) - 1u))] = (unsigned char)(4 * lane + i);
-            n += __popc(ball);
+            for (int i = 0; i < 4; ++i) {
+                const unsigned ball = __ballot_sync(0xffffffffu, v[i] > ROW_FLOOR);
+                if (v[i] > ROW_FLOOR) bytes[n + __popc(ball & ((1u << lane) - 1u))] = (unsigned char)(4 * lane + i);
+                n += __popc(ball);
+            }
+            __syncwarp();
         }
-        __syncwarp();
         for (int e0 = 0; e0 < n; e0 += 4) {
-            const int j = q * ROW_TILE + list[min(e0 + col, n - 1)];
-            const size_t row = (size_t)wl * P.m + j;
-            const float point = !BF && P.y4.points ? P.y4.points[row] : 1.f;
+            const int e = min(e0 + col, n - 1), at = q * ROW_TILE + (where ? e : bytes[e]), j = where ? where[at] : at;
+            const size_t row = (size_t)wl * m + j;
+            const float point = !BF && y4.points ? y4.points[row] : 1.f;
             const u64 m2 = pack2(magic, magic);
             u64 sum = m2, low = 0ull;
-            for (int c0 = part; c0 < chunks; c0 += 8 * BATCH) {
-                Eight e[BATCH];
+            for (int r0 = 0; r0 < rounds; r0 += BATCH) {
+                Eight y8[BATCH];
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b)
-                    if (c0 + 8 * b < chunks) e[b] = load_eight<BF>(P.y, P.y4, row, P.d, 8 * (c0 + 8 * b));
+                    if (r0 + b < rounds) y8[b] = load_eight<BF>(y_data, y4, row, d, 8 * min(8 * (r0 + b) + part, chunks - 1));
 #pragma unroll
                 for (int b = 0; b < BATCH; ++b)
-                    if (c0 + 8 * b < chunks) {
+                    if (r0 + b < rounds) {
+                        const int c = 8 * (r0 + b) + part;
                         float y[8];
-                        eight_values<BF>(e[b], P.y4, point, y);
-                        const ulonglong2 *xp = reinterpret_cast<const ulonglong2 *>(x + 8 * (c0 + 8 * b));
-                        const u64 xv[4] = {xp[0].x, xp[0].y, xp[1].x, xp[1].y};
+                        eight_values<BF>(y8[b], y4, point, y);
+                        const ulonglong2 *xp = reinterpret_cast<const ulonglong2 *>(x + 8 * min(c, chunks - 1));
+                        u64 xv[4] = {xp[0].x, xp[0].y, xp[1].x, xp[1].y};
+                        if (c >= chunks) xv[0] = xv[1] = xv[2] = xv[3] = 0ull;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const u64 yv = pack2(y[2 * i], y[2 * i + 1]), t = fma2(xv[i], yv, sum);
@@ -438,21 +448,35 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             double dot = ((double)a + (double)b) + ((double)la + (double)lb);
 #pragma unroll
             for (int off = 1; off < 8; off *= 2) dot += __shfl_xor_sync(0xffffffffu, dot, off);
-            if (part == 0 && e0 + col < n) w[j] = (float)exp2(fma(2.0 * k2, dot, hn[j]) - base);
+            if (part == 0 && e0 + col < n) w[at] = (float)exp2(fma(2.0 * k2, dot, hn[j]) - base);
         }
         __syncwarp();
     }
 }
+// The same from differences, for a list of entries, one to a thread.
+__device__ __forceinline__ void refine_list(const Draw &P, double k2, const double *hn, const float *yt, const float *nx, int step, double base, float *w,
+                                            const unsigned short *where, int n, int t, int nt)
+{
+    for (int q = t; q < n; q += nt) {
+        const int j = where[q];
+        double c = 0.0;
+#pragma unroll 4
+        for (int k = 0; k < P.d; ++k) {
+            const double e = (double)yt[(size_t)k * P.mp + j] + (double)nx[k * step];
+            c = fma(e, e, c);
+        }
+        w[q] = (float)exp2(fma(-k2, c, hn[j]) - base);
+    }
+}
 
-// Sums over the group of three floats and two counts, in one order; `before`: of the second count over the warps before this one.
-__device__ __forceinline__ void group_sums(const RowGroup &G, float (&f)[3], unsigned &n, unsigned &m, unsigned &before, int &turn)
+// Sums over the group of three floats and a count, in one order; `before`: of the count over the warps before this one.
+__device__ __forceinline__ void group_sums(const RowGroup &G, float (&f)[3], unsigned &n, unsigned &before, int &turn)
 {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1)
 #pragma unroll
         for (int i = 0; i < 3; ++i) f[i] += __shfl_xor_sync(0xffffffffu, f[i], off);
     n = __reduce_add_sync(0xffffffffu, n);
-    m = __reduce_add_sync(0xffffffffu, m);
     before = 0;
     if (G.nt == 32) return;
     turn ^= 1;
@@ -460,17 +484,17 @@ __device__ __forceinline__ void group_sums(const RowGroup &G, float (&f)[3], uns
         unsigned *p = G.sc->part[turn][G.t >> 5];
 #pragma unroll
         for (int i = 0; i < 3; ++i) p[i] = __float_as_uint(f[i]);
-        p[3] = n; p[4] = m;
+        p[3] = n;
     }
     G.sync();
     f[0] = f[1] = f[2] = 0.f;
-    n = m = 0;
+    n = 0;
     for (int q = 0; q < G.nt >> 5; ++q) {
         const unsigned *p = G.sc->part[turn][q];
 #pragma unroll
         for (int i = 0; i < 3; ++i) f[i] += __uint_as_float(p[i]);
-        if (q < G.t >> 5) before += p[4];
-        n += p[3]; m += p[4];
+        if (q < G.t >> 5) before += p[3];
+        n += p[3];
     }
 }
 __device__ __forceinline__ float group_largest(const RowGroup &G, float v, int &turn)
@@ -497,10 +521,11 @@ __device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
 }
 
 // A row once more: what weighs more than ROW_FLOOR to fp32's last place, what does not is `off` of itself off.  x: -x, `step`
-// apart (differences), or room for a row (products), whose bound is `bound`.
+// apart (differences), or room for a row (products), whose bound is `bound`.  A row that is a list of n entries, columns
+// `where`, has a mass `tail` besides.
 template <bool DOTS>
 __device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t row, const RowGroup &G, double base, float off, float bound, float *x,
-                                   int step, float *w, double *tiles, unsigned char *list)
+                                   int step, float *w, int len, const unsigned short *where, int n, float tail, double *tiles, unsigned char *bytes)
 {
     const double *hn = P.hn + (size_t)wl * P.mp;
     if (DOTS) {
@@ -509,16 +534,18 @@ __device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t 
         // twice to four times the bound, and half as much again: sums within the bound stay in its binade
         const float magic = 1.5f * __uint_as_float((__float_as_uint(bound * 4.f) & 0x7f800000u) + 0x00800000u);
         G.sync();
-        if (P.dtype == SKB_BF16) refine_products<true>(P, L.k2, wl, hn, x, magic, base, w, list, G.t >> 5, G.nt >> 5);
-        else refine_products<false>(P, L.k2, wl, hn, x, magic, base, w, list, G.t >> 5, G.nt >> 5);
-    } else refine_differences(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, G.t >> 5, G.nt >> 5);
+        if (P.dtype == SKB_BF16) refine_products<true>(P, L.k2, wl, hn, x, magic, base, w, len, where, n, bytes, G.t >> 5, G.nt >> 5);
+        else refine_products<false>(P, L.k2, wl, hn, x, magic, base, w, len, where, n, bytes, G.t >> 5, G.nt >> 5);
+    } else if (where) refine_list(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, where, n, G.t, G.nt);
+    else refine_differences(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, G.t >> 5, G.nt >> 5);
     G.sync();
-    const RowSums sums = sum_row(G, w, P.mp);
+    const RowSums sums = sum_row(G, w, len);
     if (!(sums.mass <= 3e38)) return false;
-    const RowError fine = {2.0 * (5.9604645e-8 * sums.mass + sums.rest * off), 2.f * 5.9604645e-8f, 0.f};
+    // (a list's entries are all formed again; what is not in it is missing from the sums)
+    const RowError fine = {2.0 * (5.9604645e-8 * sums.mass + (where ? 1.02 * tail : sums.rest * off)), 2.f * 5.9604645e-8f, 0.f};
     RowCut<float> cut;
-    if (!row_cut(w, P.mp, G, L.cuts, sums.top, sums.mass, sums.count, fine, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
-    return draw_all(P, row, w, cut, tiles, fine, G.t >> 5, G.nt >> 5);
+    if (!row_cut(w, len, G, L.cuts, sums.top, sums.mass, sums.count, fine, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
+    return draw_all(P, row, w, len, where, cut, tiles, fine, G.t >> 5, G.nt >> 5);
 }
 
 // What the rows of a lane have in common, and a group's room in shared memory.
@@ -526,14 +553,14 @@ struct LaneState {
     Lane L;
     int lane;
     double h_top;
-    float y_max, y_prefix;
+    float k2, y_max, y_prefix;
     bool some;
 };
 struct RowRoom {
     float *w;                    // [mp]
     double *tiles;               // [mp / 128]
-    float *list;                 // [list_room(mp)] weights, and their columns
-    int *where;
+    float *list;                 // [list_room(mp) + ROW_TILE] weights, and their columns
+    unsigned short *where;
     float *x;                    // differences: -x, `step` apart; products: room for a row
     int step;
     unsigned char *bytes;        // of this warp, [128] (products)
@@ -547,6 +574,7 @@ __device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane
     __syncthreads();
     S.lane = lane;
     S.L = lane_of(P, lane);
+    S.k2 = (float)S.L.k2;
     const double *hn = P.hn + (size_t)lane * P.mp;
     double top = -CUDART_INF;
     float far = 0.f, prefix = 0.f;
@@ -580,7 +608,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
     float top = -CUDART_INF_F;
     if (DOTS) {
         xn = P.xn[row];
-        const float two_k = (float)(2.0 * S.L.k2);
+        const float two_k = 2.f * S.k2;
         for (int j0 = span.begin; j0 < span.end; j0 += 8 * span.step) {
             float4 d[8];
 #pragma unroll
@@ -612,29 +640,27 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
     bool sure = false;
     if (top != -CUDART_INF_F) {
         float f[3] = {0.f, 0.f, 0.f};                            // mass, sum of w log2(1 / w), mass below ROW_TAIL
-        unsigned count = 0, heavy = 0, before;
+        unsigned heavy = 0, before;
 #pragma unroll 4
         for (int j = span.begin; j < span.end; j += span.step) { // (each thread's own: no barrier yet)
             float v[4];
             load4(w + j, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float below = top - v[i];
-                v[i] = ex2_fast(-below);
-                count += v[i] > 0.f;
-                heavy += v[i] >= ROW_TAIL;
-                f[2] += v[i] >= ROW_TAIL ? 0.f : v[i];
-                f[1] += v[i] > 0.f ? v[i] * below : 0.f;
+                const float gap = v[i] - top, down = gap < -200.f ? -200.f : gap;    // (2^-200 is zero already; a NaN stays)
+                v[i] = ex2_fast(down);
+                f[1] = fmaf(-down, v[i], f[1]);
+                if (v[i] >= ROW_TAIL) ++heavy;
+                else f[2] += v[i];
             }
             *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
             f[0] += (v[0] + v[1]) + (v[2] + v[3]);
         }
-        const unsigned own = count;
-        group_sums(G, f, count, heavy, before, turn);
+        group_sums(G, f, heavy, before, turn);
         G.sync();
         const float mass = f[0];
         if (mass <= 3e38f) {
-            const float k2 = (float)S.L.k2, A = fabsf(top), adds = u24 * (float)(12 + mp / (4 * G.nt));
+            const float k2 = S.k2, A = fabsf(top), adds = u24 * (float)(12 + mp / (4 * G.nt));
             float fixed, slope, bound = 0.f;                     // of an exponent: fixed + slope q
             if (DOTS) {
                 bound = sqrtf(xn.x) * S.y_max;
@@ -659,16 +685,25 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                     for (int j = span.begin; j < span.end; j += span.step) {
                         float v[4];
                         load4(w + j, v);
-                        unsigned ball[4];
+                        int c = 0, i0 = 0;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) ball[i] = __ballot_sync(0xffffffffu, v[i] >= ROW_TAIL);
-                        if (!(ball[0] | ball[1] | ball[2] | ball[3])) continue;
-                        unsigned at = before;
+                        for (int i = 3; i >= 0; --i)
+                            if (v[i] >= ROW_TAIL) { ++c; i0 = i; }
+                        const unsigned one = __ballot_sync(0xffffffffu, c > 0);
+                        if (!one) continue;
+                        unsigned at = before + __popc(one & ((1u << lane) - 1u));
+                        if (__any_sync(0xffffffffu, c > 1)) {
+                            const unsigned two = __ballot_sync(0xffffffffu, c > 1), three = __ballot_sync(0xffffffffu, c > 2), four = __ballot_sync(0xffffffffu, c > 3);
+                            const unsigned less = (1u << lane) - 1u;
+                            at += __popc(two & less) + __popc(three & less) + __popc(four & less);
+                            before += __popc(two) + __popc(three) + __popc(four);
+                            unsigned to = at;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) { at += __popc(ball[i] & ((1u << lane) - 1u)); before += __popc(ball[i]); }
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (v[i] >= ROW_TAIL) { M.list[at] = v[i]; M.where[at] = j + i; ++at; }
+                            for (int i = 1; i < 4; ++i)
+                                if (i > i0 && v[i] >= ROW_TAIL) { ++to; M.list[to] = v[i]; M.where[to] = (unsigned short)(j + i); }
+                        }
+                        before += __popc(one);
+                        if (c) { M.list[at] = i0 == 0 ? v[0] : i0 == 1 ? v[1] : i0 == 2 ? v[2] : v[3]; M.where[at] = (unsigned short)(j + i0); }
                     }
                     const int len = (int)(heavy + ROW_TILE - 1) / ROW_TILE * ROW_TILE;
                     for (int j = (int)heavy + G.t; j < len; j += G.nt) M.list[j] = 0.f;
@@ -677,11 +712,26 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 const int len = sparse ? (int)(heavy + ROW_TILE - 1) / ROW_TILE * ROW_TILE : mp;
                 const float *r = sparse ? M.list : w;
                 const RowGroup A1 = {sparse ? lane : G.t, sparse ? 32 : G.nt, G.bar, G.sc};
+                unsigned count = heavy, own = 0;
+                if (sparse) {
+                    for (int j = 4 * lane; j < (int)heavy; j += ROW_TILE) own += (unsigned)min(4, (int)heavy - j);
+                } else if (S.L.cuts.k != INT_MAX || S.L.cuts.p < 1.0) {
+                    for (int j = span.begin; j < span.end; j += span.step) {
+                        float v[4];
+                        load4(w + j, v);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) own += v[i] > 0.f;
+                    }
+                    unsigned c[1] = {own};
+                    group_add(G, c, turn);
+                    count = c[0];
+                }
                 sure = true;
                 if (!sparse || G.t < 32) {
                     RowCuts cuts = S.L.cuts;
                     QuickCut cut;
-                    sure = quick_cut(r, len, A1, cuts, sparse ? heavy : count, own, unit, slack, err, M.list, sparse ? 0u : (unsigned)mp / 4, cut, turn);
+                    sure = quick_cut(r, len, A1, cuts, count, own, unit, slack, err, M.list + (sparse ? list_room(mp) : 0),
+                                     sparse ? 0u : (unsigned)list_room(mp), cut, turn);
                     if (sure) {
                         quick_tiles(r, len / ROW_TILE, A1, cut.tau, unit, units);
                         A1.sync();
@@ -699,7 +749,10 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 if (!sure) {
                     // once more, with better weights for what counts
                     G.sync();
-                    sure = again<DOTS>(P, S.L, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, w, M.tiles, M.bytes);
+                    if (!sparse || G.t < 32)
+                        sure = again<DOTS>(P, S.L, S.lane, row, A1, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
+                                           sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, M.tiles, M.bytes);
+                    else sure = true;
                     sure = group_all(G, sure, turn);
                 }
             }
@@ -719,7 +772,7 @@ struct WarpShape {
     __host__ __device__ WarpShape(int mp, int d)
     {
         x = DOTS ? dots_xd(d) * 4 : (RW * d * 8 + 15) / 16 * 16;
-        warp = RW * mp * 4 + list_room(mp) * 8 + (mp / ROW_TILE + 1) / 2 * 16 + x;
+        warp = RW * mp * 4 + list_room(mp) * 6 + 2 * ROW_TILE * 4 + (mp / ROW_TILE + 1) / 2 * 16 + x;
         all = (size_t)mp * 4 + (size_t)WARPS * warp;
     }
 };
@@ -750,7 +803,7 @@ __device__ __forceinline__ void form_warp(const float *yt, const float *h, const
     }
 }
 template <int RW, bool DOTS>
-__global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(const Draw P)
+__global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(const __grid_constant__ Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc[WARPS];
@@ -760,8 +813,8 @@ __global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(co
     float *h = reinterpret_cast<float *>(smem), *w = reinterpret_cast<float *>(smem + (size_t)mp * 4 + (size_t)warp * shape.warp);
     RowRoom M;
     M.list = w + RW * mp;
-    M.where = reinterpret_cast<int *>(M.list + list_room(mp));
-    M.tiles = reinterpret_cast<double *>(M.where + list_room(mp));
+    M.where = reinterpret_cast<unsigned short *>(M.list + list_room(mp) + ROW_TILE);
+    M.tiles = reinterpret_cast<double *>(M.where + list_room(mp) + 2 * ROW_TILE);
     u64 *xs = reinterpret_cast<u64 *>(M.tiles + (mp / ROW_TILE + 1) / 2 * 2);
     M.step = 2 * RW;
     M.bytes = bytes[DOTS ? warp : 0];
@@ -791,7 +844,7 @@ __global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(co
                     xs[k * RW + r] = pack2(v, v);
                 }
                 __syncwarp();
-                form_warp<RW>(yt, h, xs, w, mp, P.d, (float)S.L.k2);
+                form_warp<RW>(yt, h, xs, w, mp, P.d, S.k2);
                 __syncwarp();
             }
             for (int r = 0; r < rows; ++r) {
@@ -812,7 +865,7 @@ struct GroupShape {
     __host__ __device__ GroupShape(int mp, int d)
     {
         x = DOTS ? R * dots_xd(d) * 4 : R * d * 8;
-        all = (size_t)mp * 4 + (size_t)R * (mp * 4 + list_room(mp) * 8 + (mp / ROW_TILE + 1) / 2 * 16) + x;
+        all = (size_t)mp * 4 + (size_t)R * (mp * 4 + list_room(mp) * 6 + 2 * ROW_TILE * 4 + (mp / ROW_TILE + 1) / 2 * 16) + x;
     }
 };
 template <int R>
@@ -842,7 +895,7 @@ __device__ __forceinline__ void form_rows(const float *yt, const float *h, const
     }
 }
 template <int R, bool DOTS>
-__global__ void __launch_bounds__(512, 1) draw_groups_kernel(const Draw P)
+__global__ void __launch_bounds__(512, 1) draw_groups_kernel(const __grid_constant__ Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc[R];
@@ -850,12 +903,13 @@ __global__ void __launch_bounds__(512, 1) draw_groups_kernel(const Draw P)
     constexpr int NG = 512 / R;                                  // threads of a row's group
     const int mp = P.mp, tid = threadIdx.x, g = tid / NG, room = list_room(mp), nt2 = (mp / ROW_TILE + 1) / 2 * 2;
     float *h = reinterpret_cast<float *>(smem), *w = h + mp;
-    u64 *xs = reinterpret_cast<u64 *>(w + (size_t)R * (mp + 2 * room) + (size_t)R * nt2 * 2);
+    const int lists = room * 3 / 2 + 2 * ROW_TILE;               // floats: weights, and columns of half the size
+    u64 *xs = reinterpret_cast<u64 *>(w + (size_t)R * (mp + lists) + (size_t)R * nt2 * 2);
     RowRoom M;
     M.w = w + (size_t)g * mp;
-    M.list = w + (size_t)R * mp + (size_t)g * 2 * room;
-    M.where = reinterpret_cast<int *>(M.list + room);
-    M.tiles = reinterpret_cast<double *>(w + (size_t)R * (mp + 2 * room)) + (size_t)g * nt2;
+    M.list = w + (size_t)R * mp + (size_t)g * lists;
+    M.where = reinterpret_cast<unsigned short *>(M.list + room + ROW_TILE);
+    M.tiles = reinterpret_cast<double *>(w + (size_t)R * (mp + lists)) + (size_t)g * nt2;
     M.x = reinterpret_cast<float *>(xs) + (DOTS ? g * dots_xd(P.d) : 2 * g);
     M.step = 2 * R;
     M.bytes = bytes[DOTS ? tid >> 5 : 0];
@@ -882,7 +936,7 @@ __global__ void __launch_bounds__(512, 1) draw_groups_kernel(const Draw P)
                 xs[k * R + r] = pack2(v, v);
             }
             __syncthreads();
-            form_rows<R>(P.yt + (size_t)S.lane * P.d * mp, h, xs, w, mp, P.d, (float)S.L.k2);
+            form_rows<R>(P.yt + (size_t)S.lane * P.d * mp, h, xs, w, mp, P.d, S.k2);
             __syncthreads();
         }
         if (g < rows) do_row<DOTS>(P, S, row0 + g, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo : nullptr);

@@ -2,10 +2,10 @@
 //
 // Sums are counted in units of 2^-30 of the row's mass: a thread adds its weights in fp32, rounds the sum to units, and the
 // warp's are added by one integer reduction, exactly and in no particular order.  A cut is found by three pivots at a time,
-// quarters of the bracket's bit patterns, until one weight is left in the bracket.  As soon as a quarter of the row is left,
-// the weights in the bracket move to a list, and later passes read that (a pass over the row is nine instructions a
-// weight, and some ten passes are needed).  Two weights within their errors of each other leave the row unsure, so no ties
-// have to be ordered here.  skb_draw_row.cuh has the careful form.
+// quarters of the bracket's bit patterns.  As soon as a quarter of the row is left, the weights in the bracket move to a
+// list, which later passes read (a pass is nine instructions a weight); when 128 are left, each counts and adds up those
+// above it, which ends the search.  Two weights within their errors of each other leave the row unsure, so no ties have to be
+// ordered here.  skb_draw_row.cuh has the careful form.
 //
 // Error of a comparison: a sum over a part of the row against a share f of its mass M, sum - f M = (1 - f) part - f rest.  Where
 // part is about f M, relative errors of the weights of at most e move that by 2 f (1 - f) e M, and no more.
@@ -36,27 +36,10 @@ __device__ __forceinline__ void group_add(const RowGroup &G, unsigned (&v)[N], i
         v[i] = s;
     }
 }
-// Largest of a, b and smallest of c over the group, bit patterns of weights.
-__device__ __forceinline__ void group_extremes(const RowGroup &G, unsigned &a, unsigned &b, unsigned &c, int &turn)
-{
-    a = __reduce_max_sync(0xffffffffu, a);
-    b = __reduce_max_sync(0xffffffffu, b);
-    c = __reduce_min_sync(0xffffffffu, c);
-    if (G.nt == 32) return;
-    turn ^= 1;
-    if ((G.t & 31) == 0) { G.sc->part[turn][G.t >> 5][0] = a; G.sc->part[turn][G.t >> 5][1] = b; G.sc->part[turn][G.t >> 5][2] = c; }
-    G.sync();
-    for (int q = 0; q < G.nt >> 5; ++q) {
-        a = max(a, G.sc->part[turn][q][0]);
-        b = max(b, G.sc->part[turn][q][1]);
-        c = min(c, G.sc->part[turn][q][2]);
-    }
-}
-
 // What a sum and a share f of the row's mass may be apart, in units: errors of the weights, of additions and of rounding to units.
 struct QuickSlack {
-    float weights, rest;
-    __device__ __forceinline__ unsigned at(float f) const { return (unsigned)(2.f * f * (1.f - f) * weights + rest) + 1u; }
+    float weights, rest;                // (and 130 units, of a target's own rounding)
+    __device__ __forceinline__ unsigned at(float f) const { return (unsigned)(2.f * f * (1.f - f) * weights + rest) + 130u; }
 };
 
 struct QuickCut {
@@ -96,44 +79,123 @@ __device__ __forceinline__ unsigned group_offset(const RowGroup &G, const unsign
     return before;
 }
 
-// Shrinks the cut to the shortest head with `target` entries, or units of mass.  `list` has room for `room` weights.
-// Returns false where it is unsure.
+// Where a search has come to: the border is in [lo, hi), n weights and m units are from there on.
+struct QuickBracket {
+    int lo, hi;
+    unsigned n_lo, m_lo, n_hi, m_hi;
+};
+
+// The border among the n <= ROW_TILE weights w (zeros up to a whole quadruple), n_out weights and m_out units being above all
+// of them: every weight counts and adds up those above it, four weights to a thread, which is what eight pivots' passes
+// cost in instructions and one in latency.  By each warp of the group for itself.  Leaves the bracket around the border
+// and its weight, and the weights next to it in `below` and `above`.
+__device__ __forceinline__ bool quick_rank(const float *w, const int n, const bool by_mass, const unsigned target, const float unit, const unsigned n_out,
+                                           const unsigned m_out, QuickBracket &B, unsigned &at, unsigned &below, unsigned &above)
+{
+    const int lane = threadIdx.x & 31, per = (n + 31) / 32;
+    float x[4], s[4] = {0.f, 0.f, 0.f, 0.f};
+    unsigned c[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = lane + 32 * e < n ? w[lane + 32 * e] : 0.f;
+    if (per <= 2) {
+        for (int j = 0; j < n; j += 4) {
+            float v[4];
+            load4(w + j, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (v[i] > x[e]) { ++c[e]; s[e] += v[i]; }
+        }
+    } else {
+        for (int j = 0; j < n; j += 4) {
+            float v[4];
+            load4(w + j, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (v[i] > x[e]) { ++c[e]; s[e] += v[i]; }
+        }
+    }
+    bool found = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int b = __float_as_int(x[e]);
+        const unsigned m0 = m_out + __float2uint_rn(s[e] * unit), m1 = m_out + __float2uint_rn((s[e] + x[e]) * unit);
+        const bool is = b >= B.lo && b < B.hi && (by_mass ? m0 < target && m1 >= target : n_out + c[e] + 1 == target);
+        const unsigned ball = __ballot_sync(0xffffffffu, is);
+        if (ball && !found) {
+            const int who = __ffs(ball) - 1;
+            found = true;
+            at = __shfl_sync(0xffffffffu, (unsigned)b, who);
+            B.n_lo = n_out + __shfl_sync(0xffffffffu, c[e], who) + 1;
+            B.m_lo = __shfl_sync(0xffffffffu, m1, who);
+            B.m_hi = __shfl_sync(0xffffffffu, m0, who);
+        }
+    }
+    if (!found) return false;                                    // two that are equal, or a sum that was rounded past the target
+    unsigned same = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned b = __float_as_uint(x[e]);
+        if (b > at) above = min(above, b);
+        else if (b < at) below = max(below, b);
+        else ++same;
+    }
+    below = __reduce_max_sync(0xffffffffu, below);
+    above = __reduce_min_sync(0xffffffffu, above);
+    return __reduce_add_sync(0xffffffffu, same) == 1;
+}
+
+// Shrinks the cut to the shortest head with `target` entries, or units of mass.  `list` has room for `room` weights and
+// ROW_TILE more.  Returns false where it is unsure.
 __device__ __forceinline__ bool quick_find(const float *row, const int mp, const RowGroup &G, const bool by_mass, const unsigned target, const float unit,
                                            const unsigned slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
-    int lo = cut.tau > 0.f ? __float_as_int(cut.tau) : 1, hi = __float_as_int(2.f);
-    unsigned n_lo = cut.count, m_lo = cut.mass, n_hi = 0, m_hi = 0, own_lo = cut.own, own_hi = 0;
+    QuickBracket B = {cut.tau > 0.f ? __float_as_int(cut.tau) : 1, __float_as_int(2.f), cut.count, cut.mass, 0u, 0u};
+    unsigned own_lo = cut.own, own_hi = 0;
     const float *w = row;
     const Span all(G, mp);
     Span span = all;
-    int n = mp, low_side = 0, high_side = hi;                    // the bracket of what w holds
-    unsigned n_out = 0, m_out = 0;                               // number and mass of what is above it
+    int n = mp;
+    unsigned n_out = 0, m_out = 0;                               // number and mass of what is above all that w holds
+    unsigned at = 0, below = 0, above = (unsigned)B.hi;          // the border, and what is next to it (beyond a list: its bracket)
     bool first = true;
-    while (n_lo - n_hi > 1) {
-        if (w == row && n_lo - n_hi <= room) {                   // (room 0: never)
-            // what is in the bracket to the list, zeros behind it up to whole quadruples
-            unsigned at = group_offset(G, own_lo - own_hi, turn);
-            for (int j = all.begin; j < all.end; j += all.step) {
+    while (true) {
+        const unsigned left = B.n_lo - B.n_hi;
+        if (n > ROW_TILE && (left <= ROW_TILE || (w == row && left <= room))) {
+            // what is in the bracket to a list, zeros behind it up to whole quadruples
+            float *to = left <= ROW_TILE ? list + room : list;
+            unsigned next = group_offset(G, own_lo - own_hi, turn);
+            for (int j = span.begin; j < span.end; j += span.step) {
                 float x[4];
-                load4(row + j, x);
+                load4(w + j, x);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (__float_as_int(x[i]) >= lo && __float_as_int(x[i]) < hi) list[at++] = x[i];
+                    if (__float_as_int(x[i]) >= B.lo && __float_as_int(x[i]) < B.hi) to[next++] = x[i];
             }
-            n = (int)((n_lo - n_hi + 3) / 4 * 4);
-            if (G.t < n - (int)(n_lo - n_hi)) list[n_lo - n_hi + G.t] = 0.f;
+            n = (int)((left + 3) / 4 * 4);
+            if (G.t < n - (int)left) to[left + G.t] = 0.f;
             G.sync();
-            w = list; low_side = lo; high_side = hi; n_out = n_hi; m_out = m_hi;
+            w = to; below = (unsigned)B.lo - 1u; above = (unsigned)B.hi; n_out = B.n_hi; m_out = B.m_hi;
             span.begin = 4 * G.t; span.end = n; span.step = 4 * G.nt;
+            own_lo = own_hi = 0;
+            if (n > ROW_TILE)
+                for (int j = span.begin; j < span.end; j += span.step) own_lo += (unsigned)min(4, (int)left - j);
         }
-        const int gap = hi - lo;
+        if (n <= ROW_TILE) {
+            if (!quick_rank(w, n, by_mass, target, unit, n_out, m_out, B, at, below, above)) return false;
+            break;
+        }
+        const int gap = B.hi - B.lo;
         if (gap < 16) return false;                              // equal weights, or nearly
-        int p[3] = {lo + gap / 4, lo + gap / 2, lo + gap / 4 * 3};
+        int p[3] = {B.lo + gap / 4, B.lo + gap / 2, B.lo + gap / 4 * 3};
         if (first) {
             // below (mass - target) / count there is less than mass - target: the border is above; and few rows need
             // more than 2^-24 of their largest weight
-            const int b = by_mass ? __float_as_int((float)(m_lo - target) / ((float)n_lo * unit) * 0.999f) : __float_as_int(5.9604645e-8f);
-            if (b > lo && b < __float_as_int(0.25f)) {
+            const int b = by_mass ? __float_as_int((float)(B.m_lo - target) / ((float)B.n_lo * unit) * 0.999f) : __float_as_int(5.9604645e-8f);
+            if (b > B.lo && b < __float_as_int(0.25f)) {
                 const int gap1 = __float_as_int(1.f) - b;
                 p[0] = b; p[1] = b + gap1 / 3; p[2] = b + gap1 / 3 * 2;
             }
@@ -159,40 +221,16 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
 #pragma unroll
         for (int q = 0; q < 3; ++q) {
             const unsigned c = n_out + v[q], m = m_out + v[3 + q];
-            if ((by_mass ? m : c) >= target) { if (p[q] > lo) { lo = p[q]; n_lo = c; m_lo = m; own_lo = own[q]; } }
-            else if (p[q] < hi) { hi = p[q]; n_hi = c; m_hi = m; own_hi = own[q]; }
+            if ((by_mass ? m : c) >= target) { if (p[q] > B.lo) { B.lo = p[q]; B.n_lo = c; B.m_lo = m; own_lo = own[q]; } }
+            else if (p[q] < B.hi) { B.hi = p[q]; B.n_hi = c; B.m_hi = m; own_hi = own[q]; }
         }
     }
-    // the entry that is left in [lo, hi), and its neighbours; those outside of the list are outside of its bracket
-    unsigned at = 0, below = (unsigned)low_side, above = (unsigned)high_side, kept = 0;
-#pragma unroll 2
-    for (int j = span.begin; j < span.end; j += span.step) {
-        float x[4];
-        load4(w + j, x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned b = __float_as_uint(x[i]);
-            if ((int)b >= hi) above = min(above, b);
-            else if ((int)b >= lo) at = max(at, b);
-            else below = max(below, b);
-        }
-    }
-    group_extremes(G, at, below, above, turn);
     cut.tau = __uint_as_float(at);
-    cut.count = n_lo;
-    cut.mass = m_lo;
-    if (!by_mass && room) {
-        // (a cut by mass may follow)
-        for (int j = all.begin; j < all.end; j += all.step) {
-            float x[4];
-            load4(row + j, x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) kept += x[i] >= cut.tau;
-        }
-    }
-    cut.own = kept;
+    cut.count = B.n_lo;
+    cut.mass = B.m_lo;
+    cut.own = 0;
     G.sync();                                                    // the list is read
-    if (by_mass && !(m_lo > target + slack && target > m_hi + slack)) return false;
+    if (by_mass && !(B.m_lo > target + slack && target > B.m_hi + slack)) return false;
     const float e = err.weight - err.slope * fminf(log2f(cut.tau), 0.f);
     return cut.tau - __uint_as_float(below) > e * cut.tau && __uint_as_float(above) - cut.tau > e * cut.tau;
 }
@@ -204,7 +242,16 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
     cut = {0.f, count, (unsigned)QUICK_ONE, own};
     if ((unsigned)want.k < count && !quick_find(w, mp, G, false, (unsigned)want.k, unit, 0u, err, list, room, cut, turn)) return false;
     if (want.p < 1.0 && cut.count > 1) {
-        const unsigned target = (unsigned)(want.p * (double)cut.mass);
+        if (cut.tau > 0.f && mp > ROW_TILE) {
+            const Span all(G, mp);
+            for (int j = all.begin; j < all.end; j += all.step) {
+                float x[4];
+                load4(w + j, x);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) cut.own += x[i] >= cut.tau;
+            }
+        }
+        const unsigned target = (unsigned)((float)want.p * (float)cut.mass);        // (64 units: fp32's last place)
         if (!quick_find(w, mp, G, true, target, unit, slack.at((float)want.p), err, list, room, cut, turn)) return false;
     }
     if (want.r > 0.f) {
@@ -264,7 +311,8 @@ __device__ __forceinline__ bool quick_draw(const float *w, const int ntiles, con
                                            const float u, const QuickSlack &of, int &index, float &weight)
 {
     const int lane = threadIdx.x & 31;
-    const unsigned target = (unsigned)((double)u * (double)total), slack = of.at(u);
+    // (u in units of 2^-32: what that cuts off moves the target by less than a unit)
+    const unsigned target = __umulhi((unsigned)(u * 4294967296.f), total), slack = of.at(u);
     unsigned before = 0;
     int tile = -1;
     for (int q0 = 0; q0 < ntiles; q0 += 32) {

@@ -125,7 +125,8 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
         if (bh - bl <= 1) break;                                    // equal weights
         auto bp = bl + (bh - bl) / 2;
         // what is below (mass - target) / count adds up to less than mass - target: the border is above it
-        if (first && by_mass) bp = weight_bits((Real)((old.mass - target) / n_lo));
+        // (and few cuts by rank need what is below 2^-30)
+        if (first) bp = weight_bits((Real)(by_mass ? (old.mass - target) / n_lo : 9.3e-10));
         first = false;
         if (bp <= bl) bp = bl + 1;
         if (bp >= bh) bp = bh - 1;
