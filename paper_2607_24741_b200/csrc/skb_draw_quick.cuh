@@ -3,7 +3,7 @@
 // Sums are counted in units of 2^-30 of the row's mass: a thread adds its weights in fp32, rounds the sum to units, and the
 // warp's are added by one integer reduction, exactly and in no particular order.  A cut is found by three pivots at a time,
 // quarters of the bracket's bit patterns.  As soon as a quarter of the row is left, the weights in the bracket move to a
-// list, which later passes read (a pass is nine instructions a weight); when 128 are left, each counts and adds up those
+// list, which later passes read (a pass is nine instructions a weight); when 32 are left, each counts and adds up those
 // above it, which ends the search.  Two weights within their errors of each other leave the row unsure, so no ties have to be
 // ordered here.  skb_draw_row.cuh has the careful form.
 //
@@ -85,71 +85,41 @@ struct QuickBracket {
     unsigned n_lo, m_lo, n_hi, m_hi;
 };
 
-// The border among the n <= ROW_TILE weights w (zeros up to a whole quadruple), n_out weights and m_out units being above all
-// of them: every weight counts and adds up those above it, four weights to a thread, which is what eight pivots' passes
-// cost in instructions and one in latency.  By each warp of the group for itself.  Leaves the bracket around the border
-// and its weight, and the weights next to it in `below` and `above`.
+// The border among the n <= QUICK_FEW weights w (zeros up to a whole quadruple), n_out weights and m_out units being above all
+// of them: every thread counts and adds up what is above its weight.  By each warp of the group for itself.  Leaves the
+// bracket's sums around the border, its weight, and the weights next to it in `below` and `above`.
+constexpr int QUICK_FEW = 32;
 __device__ __forceinline__ bool quick_rank(const float *w, const int n, const bool by_mass, const unsigned target, const float unit, const unsigned n_out,
                                            const unsigned m_out, QuickBracket &B, unsigned &at, unsigned &below, unsigned &above)
 {
-    const int lane = threadIdx.x & 31, per = (n + 31) / 32;
-    float x[4], s[4] = {0.f, 0.f, 0.f, 0.f};
-    unsigned c[4] = {0, 0, 0, 0};
+    const int lane = threadIdx.x & 31;
+    const float x = lane < n ? w[lane] : 0.f;
+    float s = 0.f;
+    unsigned c = 0;
+#pragma unroll 2
+    for (int j = 0; j < n; j += 4) {
+        float v[4];
+        load4(w + j, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = lane + 32 * e < n ? w[lane + 32 * e] : 0.f;
-    if (per <= 2) {
-        for (int j = 0; j < n; j += 4) {
-            float v[4];
-            load4(w + j, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (v[i] > x[e]) { ++c[e]; s[e] += v[i]; }
-        }
-    } else {
-        for (int j = 0; j < n; j += 4) {
-            float v[4];
-            load4(w + j, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (v[i] > x[e]) { ++c[e]; s[e] += v[i]; }
-        }
+        for (int i = 0; i < 4; ++i)
+            if (v[i] > x) { ++c; s += v[i]; }
     }
-    bool found = false;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int b = __float_as_int(x[e]);
-        const unsigned m0 = m_out + __float2uint_rn(s[e] * unit), m1 = m_out + __float2uint_rn((s[e] + x[e]) * unit);
-        const bool is = b >= B.lo && b < B.hi && (by_mass ? m0 < target && m1 >= target : n_out + c[e] + 1 == target);
-        const unsigned ball = __ballot_sync(0xffffffffu, is);
-        if (ball && !found) {
-            const int who = __ffs(ball) - 1;
-            found = true;
-            at = __shfl_sync(0xffffffffu, (unsigned)b, who);
-            B.n_lo = n_out + __shfl_sync(0xffffffffu, c[e], who) + 1;
-            B.m_lo = __shfl_sync(0xffffffffu, m1, who);
-            B.m_hi = __shfl_sync(0xffffffffu, m0, who);
-        }
-    }
-    if (!found) return false;                                    // two that are equal, or a sum that was rounded past the target
-    unsigned same = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const unsigned b = __float_as_uint(x[e]);
-        if (b > at) above = min(above, b);
-        else if (b < at) below = max(below, b);
-        else ++same;
-    }
-    below = __reduce_max_sync(0xffffffffu, below);
-    above = __reduce_min_sync(0xffffffffu, above);
-    return __reduce_add_sync(0xffffffffu, same) == 1;
+    const unsigned b = __float_as_uint(x), m0 = m_out + __float2uint_rn(s * unit), m1 = m_out + __float2uint_rn((s + x) * unit);
+    const bool is = (int)b >= B.lo && (int)b < B.hi && (by_mass ? m0 < target && m1 >= target : n_out + c + 1 == target);
+    const unsigned ball = __ballot_sync(0xffffffffu, is);
+    if (!ball) return false;                                     // two that are equal, or a sum that was rounded past the target
+    const int who = __ffs(ball) - 1;
+    at = __shfl_sync(0xffffffffu, b, who);
+    B.n_lo = n_out + __shfl_sync(0xffffffffu, c, who) + 1;
+    B.m_lo = __shfl_sync(0xffffffffu, m1, who);
+    B.m_hi = __shfl_sync(0xffffffffu, m0, who);
+    below = max(below, __reduce_max_sync(0xffffffffu, b < at ? b : 0u));
+    above = min(above, __reduce_min_sync(0xffffffffu, b > at ? b : 0xffffffffu));
+    return __popc(__ballot_sync(0xffffffffu, b == at)) == 1;
 }
 
 // Shrinks the cut to the shortest head with `target` entries, or units of mass.  `list` has room for `room` weights and
-// ROW_TILE more.  Returns false where it is unsure.
+// QUICK_FEW more.  Returns false where it is unsure.
 __device__ __forceinline__ bool quick_find(const float *row, const int mp, const RowGroup &G, const bool by_mass, const unsigned target, const float unit,
                                            const unsigned slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
@@ -164,9 +134,9 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
     bool first = true;
     while (true) {
         const unsigned left = B.n_lo - B.n_hi;
-        if (n > ROW_TILE && (left <= ROW_TILE || (w == row && left <= room))) {
+        if (n > QUICK_FEW && (left <= QUICK_FEW || (w == row && left <= room))) {
             // what is in the bracket to a list, zeros behind it up to whole quadruples
-            float *to = left <= ROW_TILE ? list + room : list;
+            float *to = left <= QUICK_FEW ? list + room : list;
             unsigned next = group_offset(G, own_lo - own_hi, turn);
             for (int j = span.begin; j < span.end; j += span.step) {
                 float x[4];
@@ -181,10 +151,10 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
             w = to; below = (unsigned)B.lo - 1u; above = (unsigned)B.hi; n_out = B.n_hi; m_out = B.m_hi;
             span.begin = 4 * G.t; span.end = n; span.step = 4 * G.nt;
             own_lo = own_hi = 0;
-            if (n > ROW_TILE)
+            if (n > QUICK_FEW)
                 for (int j = span.begin; j < span.end; j += span.step) own_lo += (unsigned)min(4, (int)left - j);
         }
-        if (n <= ROW_TILE) {
+        if (n <= QUICK_FEW) {
             if (!quick_rank(w, n, by_mass, target, unit, n_out, m_out, B, at, below, above)) return false;
             break;
         }
@@ -242,7 +212,7 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
     cut = {0.f, count, (unsigned)QUICK_ONE, own};
     if ((unsigned)want.k < count && !quick_find(w, mp, G, false, (unsigned)want.k, unit, 0u, err, list, room, cut, turn)) return false;
     if (want.p < 1.0 && cut.count > 1) {
-        if (cut.tau > 0.f && mp > ROW_TILE) {
+        if (cut.tau > 0.f) {
             const Span all(G, mp);
             for (int j = all.begin; j < all.end; j += all.step) {
                 float x[4];
