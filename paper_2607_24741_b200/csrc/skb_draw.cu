@@ -51,6 +51,9 @@ struct Draw {
     const float *dots;                               // rows row0 .. row0 + rows - 1 of lanes lane0 .. lane0 + lanes - 1
     double *scratch;                                 // [blocks][mp] weights of rows in float64
     long long *list;                                 // rows that are open: their number, then which; null: all rows
+    unsigned *later_n;                               // products: rows of this launch that are formed again by a launch of
+    long long *later;                                // their own, their number and which; null: formed again at once
+    int launches;                                    // numbers that later_n has, one for each launch
     long long ldo;
     int lane0, lanes, row0, rows;
 };
@@ -179,7 +182,10 @@ __global__ void __launch_bounds__(256) norms_kernel(const __grid_constant__ Draw
 {
     const int w = blockIdx.y, i = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     double p = 0.0;
-    if (blockIdx.x == 0 && w == 0 && threadIdx.x == 0) P.list[0] = 0;
+    if (blockIdx.x == 0 && w == 0) {
+        if (threadIdx.x == 0) P.list[0] = 0;
+        for (int q = threadIdx.x; q < P.launches; q += 256) P.later_n[q] = 0u;
+    }
     if (i < P.mp) {
         const double g = i < P.m ? P.g[(size_t)w * P.m + i] : -CUDART_INF;
         const bool masked = g == -CUDART_INF;
@@ -400,7 +406,9 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
     const int chunks = BF ? P.d / 8 : dots_xd(P.d) / 8, rounds = (chunks + 7) / 8, m = P.m, d = P.d;
     const void *y_data = P.y;
     const Cloud4 y4 = P.y4;
-    for (int q = warp; q < len / ROW_TILE; q += warps) {
+    // (a list: its entries shared out among all warps; a row: its tiles)
+    const int first = where ? 4 * warp : 0, step = where ? 4 * warps : 4;
+    for (int q = where ? 0 : warp; q < len / ROW_TILE; q += where ? 1 : warps) {
         int n = 0;
         if (where) n = min(ROW_TILE, count - q * ROW_TILE);
         else {
@@ -414,11 +422,12 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             }
             __syncwarp();
         }
-        for (int e0 = 0; e0 < n; e0 += 4) {
+        for (int e0 = first; e0 < n; e0 += step) {
             const int e = min(e0 + col, n - 1), at = q * ROW_TILE + (where ? e : bytes[e]), j = where ? where[at] : at;
             const size_t row = (size_t)wl * m + j;
             const float point = !BF && y4.points ? y4.points[row] : 1.f;
             const u64 m2 = pack2(magic, magic);
+            const double hj = hn[j];
             u64 sum = m2, low = 0ull;
             for (int r0 = 0; r0 < rounds; r0 += BATCH) {
                 Eight y8[BATCH];
@@ -448,7 +457,7 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             double dot = ((double)a + (double)b) + ((double)la + (double)lb);
 #pragma unroll
             for (int off = 1; off < 8; off *= 2) dot += __shfl_xor_sync(0xffffffffu, dot, off);
-            if (part == 0 && e0 + col < n) w[at] = (float)exp2(fma(2.0 * k2, dot, hn[j]) - base);
+            if (part == 0 && e0 + col < n) w[at] = (float)exp2(fma(2.0 * k2, dot, hj) - base);
         }
         __syncwarp();
     }
@@ -594,7 +603,8 @@ __device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane
 }
 
 // One row by its group: exponents (in w for differences, to be formed from `dots` for products) to weights, cut, draws.
-template <bool DOTS>
+// LATER: a row that is to be formed again goes on a list.
+template <bool DOTS, bool LATER>
 __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t row, const RowGroup &G, int &turn, const RowRoom &M, const float *h,
                                        const float *dots)
 {
@@ -746,13 +756,14 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                     }
                 }
                 sure = group_all(G, sure, turn);
-                if (!sure) {
+                if (!sure && DOTS && LATER) {
+                    if (G.t == 0) P.later[atomicAdd(P.later_n, 1u)] = (long long)row;
+                    sure = true;
+                } else if (!sure) {
                     // once more, with better weights for what counts
                     G.sync();
-                    if (!sparse || G.t < 32)
-                        sure = again<DOTS>(P, S.L, S.lane, row, A1, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
-                                           sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, M.tiles, M.bytes);
-                    else sure = true;
+                    sure = again<DOTS>(P, S.L, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
+                                       sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, M.tiles, M.bytes);
                     sure = group_all(G, sure, turn);
                 }
             }
@@ -850,7 +861,7 @@ __global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(co
             for (int r = 0; r < rows; ++r) {
                 M.w = w + (size_t)r * mp;
                 M.x = reinterpret_cast<float *>(xs) + (DOTS ? 0 : 2 * r);
-                do_row<DOTS>(P, S, row0 + r, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + r) * P.ldo : nullptr);
+                do_row<DOTS, DOTS>(P, S, row0 + r, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + r) * P.ldo : nullptr);
             }
         }
         at = end;
@@ -939,8 +950,40 @@ __global__ void __launch_bounds__(512, 1) draw_groups_kernel(const __grid_consta
             form_rows<R>(P.yt + (size_t)S.lane * P.d * mp, h, xs, w, mp, P.d, S.k2);
             __syncthreads();
         }
-        if (g < rows) do_row<DOTS>(P, S, row0 + g, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo : nullptr);
+        if (g < rows) do_row<DOTS, false>(P, S, row0 + g, G, turn, M, h, DOTS ? P.dots + ((size_t)wl * P.rows + r0 + g) * P.ldo : nullptr);
         if (!DOTS) __syncthreads();
+    }
+}
+
+// Rows of products that are formed again, four warps to a row: among rows that are done in 10 us those that take a
+// warp 70 more would be what a launch waits for.
+constexpr int LATER_THREADS = 128;
+size_t later_smem(int mp, int d) { return GroupShape<1, true>(mp, d).all; }
+__global__ void __launch_bounds__(LATER_THREADS) draw_later_kernel(const __grid_constant__ Draw P)
+{
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ RowScratch sc;
+    __shared__ unsigned char bytes[LATER_THREADS / 32][ROW_TILE];
+    const int mp = P.mp, tid = threadIdx.x, room = list_room(mp), lists = room * 3 / 2 + 2 * ROW_TILE, nt2 = (mp / ROW_TILE + 1) / 2 * 2;
+    float *h = reinterpret_cast<float *>(smem);
+    RowRoom M;
+    M.w = h + mp;
+    M.list = M.w + mp;
+    M.where = reinterpret_cast<unsigned short *>(M.list + room + ROW_TILE);
+    M.tiles = reinterpret_cast<double *>(M.list + lists);
+    M.x = reinterpret_cast<float *>(M.tiles + nt2);
+    M.step = 0;
+    M.bytes = bytes[tid >> 5];
+    const RowGroup G = {tid, LATER_THREADS, 0, &sc};
+    int turn = 0;
+    LaneState S;
+    S.lane = -1;
+    const unsigned rows = *P.later_n;
+    for (unsigned t = blockIdx.x; t < rows; t += gridDim.x) {
+        const long long row = P.later[t];
+        const int w = (int)(row / P.n), i = (int)(row % P.n);
+        if (w != S.lane) enter_lane<LATER_THREADS, true>(P, S, w, h, G);
+        do_row<true, false>(P, S, (size_t)row, G, turn, M, h, P.dots + ((size_t)(w - P.lane0) * P.rows + (i - P.row0)) * P.ldo);
     }
 }
 
@@ -1007,6 +1050,11 @@ size_t carve(Draw &P, const Plan &p, char *base)
         P.xn = (float2 *)take((size_t)P.W * P.n * 8);
         P.dots = (const float *)take((size_t)p.lanes * p.rows * P.mp * 4);
     } else P.yt = (float *)take((size_t)P.W * P.d * P.mp * 4);
+    if (p.dots && p.warp_rows) {
+        P.launches = ((P.W + p.lanes - 1) / p.lanes) * ((P.n + p.rows - 1) / p.rows);
+        P.later_n = (unsigned *)take((size_t)P.launches * 4);
+        P.later = (long long *)take((size_t)p.lanes * p.rows * 8);
+    }
     P.scratch = (double *)take((size_t)DRAW_EXACT_BLOCKS * P.mp * 8);
     if (p.fp32()) P.list = (long long *)take(((size_t)P.W * P.n + 1) * 8);
     return at;
@@ -1117,6 +1165,11 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
                                              const_cast<float *>(P.dots), P.ldo, st);
             if (s != SKB_OK) return s;
             launch_draw(P, p, st);
+            if (p.warp_rows) {
+                cudaFuncSetAttribute(draw_later_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)DRAW_SMEM / 2);
+                draw_later_kernel<<<std::min(P.lanes * P.rows, DRAW_BLOCKS * 4), LATER_THREADS, later_smem(P.mp, P.d), st>>>(P);
+                ++P.later_n;
+            }
         }
     return exact();
 }
