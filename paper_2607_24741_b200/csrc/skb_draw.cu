@@ -77,7 +77,7 @@ __device__ __forceinline__ Lane lane_of(const Draw &P, int w)
     L.k2 = 1.4426950408889634 / ((double)eps * (double)T);
     return L;
 }
-__device__ __forceinline__ float raw_value(const void *base, const Cloud4 &c, int dtype, size_t row, int d, int k)
+__device__ __noinline__ float raw_value(const void *base, const Cloud4 &c, int dtype, size_t row, int d, int k)
 {
     if (dtype == SKB_F32) return ((const float *)base)[row * d + k];
     if (dtype == SKB_BF16) return __uint_as_float((uint32_t)((const uint16_t *)base)[row * d + k] << 16);
@@ -103,6 +103,7 @@ __global__ void __launch_bounds__(256) transpose_kernel(const __grid_constant__ 
         if (part < P.d) yt[(size_t)part * P.mp + j0 + col] = masked[col] ? 0.f : raw_value(P.y, P.y4, P.dtype, (size_t)w * P.m + j0 + col, P.d, part);
         return;
     }
+#pragma unroll 1
     for (int k0 = 0; k0 < P.d; k0 += 32) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -184,6 +185,7 @@ __global__ void __launch_bounds__(256) norms_kernel(const __grid_constant__ Draw
     double p = 0.0;
     if (blockIdx.x == 0 && w == 0) {
         if (threadIdx.x == 0) P.list[0] = 0;
+#pragma unroll 1
         for (int q = threadIdx.x; q < P.launches; q += 256) P.later_n[q] = 0u;
     }
     if (i < P.mp) {
@@ -210,10 +212,11 @@ __device__ __forceinline__ void put_draw(const Draw &P, size_t at, int index, fl
 
 // Draws of one row from `len` weights, of columns `where` (null: their places), and their cut, shared out to the group's warps.  True if all of this warp's were sure.
 template <typename Real>
-__device__ bool draw_all(const Draw &P, size_t row, const Real *w, int len, const unsigned short *where, const RowCut<Real> &cut, const double *tiles, const RowError &err, int warp, int warps)
+__device__ __noinline__ bool draw_all(const Draw &P, size_t row, const Real *w, int len, const unsigned short *where, const RowCut<Real> &cut, const double *tiles, const RowError &err, int warp, int warps)
 {
     const double total = row_total(tiles, len / ROW_TILE);
     bool sure = true;
+#pragma unroll 1
     for (int s = warp; s < P.S; s += warps) {
         const float u = P.u[row * P.S + s];
         int j = -1;
@@ -226,8 +229,9 @@ __device__ bool draw_all(const Draw &P, size_t row, const Real *w, int len, cons
     }
     return sure;
 }
-__device__ void draw_none(const Draw &P, size_t row, int t, int nt)
+__device__ __noinline__ void draw_none(const Draw &P, size_t row, int t, int nt)
 {
+#pragma unroll 1
     for (int s = t; s < P.S; s += nt) put_draw(P, row * P.S + s, -1, CUDART_NAN_F);
 }
 
@@ -241,6 +245,8 @@ __device__ __forceinline__ void exact_rows(const Draw &P, const Lane &L, int w, 
     const int lane = threadIdx.x & 31, part = lane & 7, chunks = BF ? P.d / 8 : dots_xd(P.d) / 8, rounds = (chunks + 7) / 8, d = P.d;
     const void *y_data = P.y;
     const Cloud4 y4 = P.y4;
+    const int eights = dots_xd(d) / 8;               // (x is kept as [8][d / 8]: threads next to each other read next to each other)
+#pragma unroll 1
     for (int j0 = 4 * warp; j0 < P.mp; j0 += 4 * warps) {
         const int j = j0 + (lane >> 3);
         const bool is = hn[j] != -CUDART_INF;
@@ -248,6 +254,7 @@ __device__ __forceinline__ void exact_rows(const Draw &P, const Lane &L, int w, 
         if (is) {
             const size_t row = (size_t)w * P.m + j;
             const float point = !BF && y4.points ? y4.points[row] : 1.f;
+#pragma unroll 1
             for (int r0 = 0; r0 < rounds; r0 += BATCH) {
                 Eight y8[BATCH];
 #pragma unroll
@@ -261,7 +268,7 @@ __device__ __forceinline__ void exact_rows(const Draw &P, const Lane &L, int w, 
                         double sum = 0.0;
                         eight_values<BF>(y8[b], y4, point, y);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) { const double f = xs[8 * min(q, chunks - 1) + i] - (double)y[i]; sum = fma(f, f, sum); }
+                        for (int i = 0; i < 8; ++i) { const double f = xs[i * eights + min(q, chunks - 1)] - (double)y[i]; sum = fma(f, f, sum); }
                         if (q < chunks) c += sum;
                     }
             }
@@ -284,6 +291,7 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const __grid_constant__
     const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, xd = dots_xd(P.d);
     const RowGroup G = {tid, nt, 0, &sc};
     const long long rows = P.list ? P.list[0] : (long long)P.W * P.n;
+#pragma unroll 1
     for (long long t = blockIdx.x; t < rows; t += gridDim.x) {
         const long long row = P.list ? P.list[1 + t] : t;
         const int w = (int)(row / P.n);
@@ -291,12 +299,15 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const __grid_constant__
         const double *hn = P.hn + (size_t)w * P.mp;
         __syncthreads();
         if (!L.ok) { draw_none(P, (size_t)row, tid, nt); continue; }
-        for (int k = tid; k < xd; k += nt) xs[k] = k < P.d ? (double)raw_value(P.x, P.x4, P.dtype, (size_t)row, P.d, k) : 0.0;
+#pragma unroll 1
+        for (int k = tid; k < xd; k += nt)
+            xs[P.yt ? k : (k & 7) * (xd / 8) + (k >> 3)] = k < P.d ? (double)raw_value(P.x, P.x4, P.dtype, (size_t)row, P.d, k) : 0.0;
         __syncthreads();
         double top = -CUDART_INF;
         int bad = 0;
         if (P.yt) {
             const float *yt = P.yt + (size_t)w * P.d * P.mp;
+#pragma unroll 1
             for (int j = tid; j < P.mp; j += nt) {
                 double c = 0.0;
 #pragma unroll 4
@@ -318,6 +329,7 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const __grid_constant__
         top = G.largest(top);
         G.add(mass, bad);                                           // (a barrier: wd is written)
         if (bad || top == -CUDART_INF) { draw_none(P, (size_t)row, tid, nt); continue; }
+#pragma unroll 1
         for (int j = tid; j < P.mp; j += nt) {
             const double v = exp2(wd[j] - top);
             wd[j] = v;
@@ -352,13 +364,15 @@ struct RowSums {
 __device__ __forceinline__ RowSums sum_row(const RowGroup &G, const float *w, int mp)
 {
     RowSums r = {0.0, 0.0, 0, 0.f};
+#pragma unroll 1
     for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
         float v[4];
         load4(w + j, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            r.mass += (double)v[i];
-            r.rest += v[i] > ROW_FLOOR ? 0.0 : (double)v[i];
+            const double d = (double)v[i];
+            r.mass += d;
+            r.rest += v[i] > ROW_FLOOR ? 0.0 : d;
             r.count += v[i] > 0.f;
             r.top = fmaxf(r.top, v[i]);
         }
@@ -376,12 +390,14 @@ __device__ __forceinline__ void refine_differences(const Draw &P, double k2, con
                                                    float *w, int warp, int warps)
 {
     const int lane = threadIdx.x & 31;
+#pragma unroll 1
     for (int q = warp; q < P.mp / ROW_TILE; q += warps) {
         const int j = q * ROW_TILE + 4 * lane;
         float v[4];
         load4(w + j, v);
         if (!(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])) > ROW_FLOOR)) continue;
         double c[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 1
         for (int k = 0; k < P.d; ++k) {
             float y[4];
             load4(yt + (size_t)k * P.mp + j, y);
@@ -408,6 +424,7 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
     const Cloud4 y4 = P.y4;
     // (a list: its entries shared out among all warps; a row: its tiles)
     const int first = where ? 4 * warp : 0, step = where ? 4 * warps : 4;
+#pragma unroll 1
     for (int q = where ? 0 : warp; q < len / ROW_TILE; q += where ? 1 : warps) {
         int n = 0;
         if (where) n = min(ROW_TILE, count - q * ROW_TILE);
@@ -422,6 +439,7 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             }
             __syncwarp();
         }
+#pragma unroll 1
         for (int e0 = first; e0 < n; e0 += step) {
             const int e = min(e0 + col, n - 1), at = q * ROW_TILE + (where ? e : bytes[e]), j = where ? where[at] : at;
             const size_t row = (size_t)wl * m + j;
@@ -429,6 +447,7 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
             const u64 m2 = pack2(magic, magic);
             const double hj = hn[j];
             u64 sum = m2, low = 0ull;
+#pragma unroll 1
             for (int r0 = 0; r0 < rounds; r0 += BATCH) {
                 Eight y8[BATCH];
 #pragma unroll
@@ -466,6 +485,7 @@ __device__ __forceinline__ void refine_products(const Draw &P, double k2, int wl
 __device__ __forceinline__ void refine_list(const Draw &P, double k2, const double *hn, const float *yt, const float *nx, int step, double base, float *w,
                                             const unsigned short *where, int n, int t, int nt)
 {
+#pragma unroll 1
     for (int q = t; q < n; q += nt) {
         const int j = where[q];
         double c = 0.0;
@@ -498,6 +518,7 @@ __device__ __forceinline__ void group_sums(const RowGroup &G, float (&f)[3], uns
     G.sync();
     f[0] = f[1] = f[2] = 0.f;
     n = 0;
+#pragma unroll 1
     for (int q = 0; q < G.nt >> 5; ++q) {
         const unsigned *p = G.sc->part[turn][q];
 #pragma unroll
@@ -514,6 +535,7 @@ __device__ __forceinline__ float group_largest(const RowGroup &G, float v, int &
     turn ^= 1;
     if ((G.t & 31) == 0) G.sc->part[turn][G.t >> 5][0] = __float_as_uint(v);
     G.sync();
+#pragma unroll 1
     for (int q = 0; q < G.nt >> 5; ++q) v = fmaxf(v, __uint_as_float(G.sc->part[turn][q][0]));
     return v;
 }
@@ -525,6 +547,7 @@ __device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
     turn ^= 1;
     if ((G.t & 31) == 0) G.sc->part[turn][G.t >> 5][0] = v;
     G.sync();
+#pragma unroll 1
     for (int q = 0; q < G.nt >> 5; ++q) v = v && G.sc->part[turn][q][0] != 0;
     return v;
 }
@@ -539,6 +562,7 @@ __device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t 
     const double *hn = P.hn + (size_t)wl * P.mp;
     if (DOTS) {
         const int xd = dots_xd(P.d);
+#pragma unroll 1
         for (int k = G.t; k < xd; k += G.nt) x[k] = k < P.d ? raw_value(P.x, P.x4, P.dtype, row, P.d, k) : 0.f;
         // twice to four times the bound, and half as much again: sums within the bound stay in its binade
         const float magic = 1.5f * __uint_as_float((__float_as_uint(bound * 4.f) & 0x7f800000u) + 0x00800000u);
@@ -587,6 +611,7 @@ __device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane
     const double *hn = P.hn + (size_t)lane * P.mp;
     double top = -CUDART_INF;
     float far = 0.f, prefix = 0.f;
+#pragma unroll 1
     for (int j = threadIdx.x; j < P.mp; j += NT) {
         top = fmax(top, hn[j]);
         if (DOTS) {
@@ -598,6 +623,7 @@ __device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane
     S.h_top = all.largest(top);
     if (DOTS) { S.y_max = sqrtf(all.largest(far)); S.y_prefix = sqrtf(all.largest(prefix)); }
     S.some = S.L.ok && S.h_top != -CUDART_INF;
+#pragma unroll 1
     for (int j = threadIdx.x; j < P.mp; j += NT) h[j] = S.some ? (float)(hn[j] - S.h_top) : 0.f;
     __syncthreads();
 }
@@ -619,6 +645,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
     if (DOTS) {
         xn = P.xn[row];
         const float two_k = 2.f * S.k2;
+#pragma unroll 1
         for (int j0 = span.begin; j0 < span.end; j0 += 8 * span.step) {
             float4 d[8];
 #pragma unroll
@@ -692,6 +719,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 if (sparse) {
                     // few entries weigh anything: they are the row, by one warp, the others an error of the sums
                     slack.rest += 2.f * f[2] * unit;
+#pragma unroll 1
                     for (int j = span.begin; j < span.end; j += span.step) {
                         float v[4];
                         load4(w + j, v);
@@ -716,6 +744,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                         if (c) { M.list[at] = i0 == 0 ? v[0] : i0 == 1 ? v[1] : i0 == 2 ? v[2] : v[3]; M.where[at] = (unsigned short)(j + i0); }
                     }
                     const int len = (int)(heavy + ROW_TILE - 1) / ROW_TILE * ROW_TILE;
+#pragma unroll 1
                     for (int j = (int)heavy + G.t; j < len; j += G.nt) M.list[j] = 0.f;
                     G.sync();
                 }
@@ -724,8 +753,10 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 const RowGroup A1 = {sparse ? lane : G.t, sparse ? 32 : G.nt, G.bar, G.sc};
                 unsigned count = heavy, own = 0;
                 if (sparse) {
+#pragma unroll 1
                     for (int j = 4 * lane; j < (int)heavy; j += ROW_TILE) own += (unsigned)min(4, (int)heavy - j);
                 } else if (S.L.cuts.k != INT_MAX || S.L.cuts.p < 1.0) {
+#pragma unroll 1
                     for (int j = span.begin; j < span.end; j += span.step) {
                         float v[4];
                         load4(w + j, v);
@@ -746,6 +777,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                         quick_tiles(r, len / ROW_TILE, A1, cut.tau, unit, units);
                         A1.sync();
                         const unsigned whole = quick_total(units, len / ROW_TILE);
+#pragma unroll 1
                         for (int s = A1.t >> 5; s < P.S; s += A1.nt >> 5) {
                             const float u = s ? P.u[row * P.S + s] : u_first;
                             int j = -1;
@@ -790,6 +822,7 @@ struct WarpShape {
 template <int RW>
 __device__ __forceinline__ void form_warp(const float *yt, const float *h, const u64 *xs, float *w, int mp, int d, float k2)
 {
+#pragma unroll 1
     for (int j = 4 * (threadIdx.x & 31); j < mp; j += ROW_TILE) {
         u64 acc[RW][2];
 #pragma unroll
@@ -837,14 +870,17 @@ __global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(co
     const unsigned first = (unsigned)(total * blockIdx.x / gridDim.x), last = (unsigned)(total * (blockIdx.x + 1) / gridDim.x);
     LaneState S;
     unsigned at = first;
+#pragma unroll 1
     while (at < last) {
         const unsigned wl = at / per_lane, lane_end = (wl + 1) * per_lane, end = last < lane_end ? last : lane_end;
         enter_lane<WARPS * 32, DOTS>(P, S, P.lane0 + (int)wl, h, all);
         const float *yt = P.yt + (size_t)S.lane * P.d * mp;
+#pragma unroll 1
         for (unsigned u = at + warp; u < end; u += WARPS) {
             const int r0 = (int)(u - wl * per_lane) * RW, rows = min(RW, P.rows - r0);
             const size_t row0 = (size_t)S.lane * P.n + P.row0 + r0;
             if (!S.some) {
+#pragma unroll 1
                 for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, lane, 32);
                 continue;
             }
@@ -858,6 +894,7 @@ __global__ void __launch_bounds__(WARPS * 32, DOTS ? 2 : 3) draw_warps_kernel(co
                 form_warp<RW>(yt, h, xs, w, mp, P.d, S.k2);
                 __syncwarp();
             }
+#pragma unroll 1
             for (int r = 0; r < rows; ++r) {
                 M.w = w + (size_t)r * mp;
                 M.x = reinterpret_cast<float *>(xs) + (DOTS ? 0 : 2 * r);
@@ -882,6 +919,7 @@ struct GroupShape {
 template <int R>
 __device__ __forceinline__ void form_rows(const float *yt, const float *h, const u64 *xs, float *w, int mp, int d, float k2)
 {
+#pragma unroll 1
     for (int j = 4 * threadIdx.x; j < mp; j += 4 * 512) {
         u64 acc[R][2];
 #pragma unroll
@@ -931,12 +969,14 @@ __global__ void __launch_bounds__(512, 1) draw_groups_kernel(const __grid_consta
     const unsigned first = (unsigned)(total * blockIdx.x / gridDim.x), last = (unsigned)(total * (blockIdx.x + 1) / gridDim.x);
     LaneState S;
     S.lane = -1;
+#pragma unroll 1
     for (unsigned t = first; t < last; ++t) {
         const unsigned wl = t / per_lane;
         const int r0 = (int)(t - wl * per_lane) * R, rows = min(R, P.rows - r0);
         if (P.lane0 + (int)wl != S.lane) enter_lane<512, DOTS>(P, S, P.lane0 + (int)wl, h, all);
         const size_t row0 = (size_t)S.lane * P.n + P.row0 + r0;
         if (!S.some) {
+#pragma unroll 1
             for (int r = 0; r < rows; ++r) draw_none(P, row0 + r, tid, 512);
             continue;
         }
@@ -959,7 +999,7 @@ __global__ void __launch_bounds__(512, 1) draw_groups_kernel(const __grid_consta
 // warp 70 more would be what a launch waits for.
 constexpr int LATER_THREADS = 128;
 size_t later_smem(int mp, int d) { return GroupShape<1, true>(mp, d).all; }
-__global__ void __launch_bounds__(LATER_THREADS) draw_later_kernel(const __grid_constant__ Draw P)
+__global__ void __launch_bounds__(LATER_THREADS, 4) draw_later_kernel(const __grid_constant__ Draw P)
 {
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ RowScratch sc;
@@ -979,6 +1019,7 @@ __global__ void __launch_bounds__(LATER_THREADS) draw_later_kernel(const __grid_
     LaneState S;
     S.lane = -1;
     const unsigned rows = *P.later_n;
+#pragma unroll 1
     for (unsigned t = blockIdx.x; t < rows; t += gridDim.x) {
         const long long row = P.later[t];
         const int w = (int)(row / P.n), i = (int)(row % P.n);

@@ -32,6 +32,7 @@ __device__ __forceinline__ void group_add(const RowGroup &G, unsigned (&v)[N], i
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         unsigned s = 0;
+#pragma unroll 1
         for (int q = 0; q < G.nt >> 5; ++q) s += G.sc->part[turn][q][i];
         v[i] = s;
     }
@@ -75,6 +76,7 @@ __device__ __forceinline__ unsigned group_offset(const RowGroup &G, const unsign
     turn ^= 1;
     if (lane == 31) G.sc->part[turn][G.t >> 5][0] = s;
     G.sync();
+#pragma unroll 1
     for (int q = 0; q < G.t >> 5; ++q) before += G.sc->part[turn][q][0];
     return before;
 }
@@ -132,12 +134,14 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
     unsigned n_out = 0, m_out = 0;                               // number and mass of what is above all that w holds
     unsigned at = 0, below = 0, above = (unsigned)B.hi;          // the border, and what is next to it (beyond a list: its bracket)
     bool first = true;
+#pragma unroll 1
     while (true) {
         const unsigned left = B.n_lo - B.n_hi;
         if (n > QUICK_FEW && (left <= QUICK_FEW || (w == row && left <= room))) {
             // what is in the bracket to a list, zeros behind it up to whole quadruples
             float *to = left <= QUICK_FEW ? list + room : list;
             unsigned next = group_offset(G, own_lo - own_hi, turn);
+#pragma unroll 1
             for (int j = span.begin; j < span.end; j += span.step) {
                 float x[4];
                 load4(w + j, x);
@@ -152,6 +156,7 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
             span.begin = 4 * G.t; span.end = n; span.step = 4 * G.nt;
             own_lo = own_hi = 0;
             if (n > QUICK_FEW)
+#pragma unroll 1
                 for (int j = span.begin; j < span.end; j += span.step) own_lo += (unsigned)min(4, (int)left - j);
         }
         if (n <= QUICK_FEW) {
@@ -210,10 +215,13 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
                                           const float unit, const QuickSlack &slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
     cut = {0.f, count, (unsigned)QUICK_ONE, own};
-    if ((unsigned)want.k < count && !quick_find(w, mp, G, false, (unsigned)want.k, unit, 0u, err, list, room, cut, turn)) return false;
-    if (want.p < 1.0 && cut.count > 1) {
-        if (cut.tau > 0.f) {
+    // by rank, then by mass (one body: the code has to stay in the instruction cache)
+#pragma unroll 1
+    for (int by_mass = 0; by_mass < 2; ++by_mass) {
+        if (by_mass ? want.p >= 1.0 || cut.count <= 1 : (unsigned)want.k >= count) continue;
+        if (by_mass && cut.tau > 0.f) {
             const Span all(G, mp);
+#pragma unroll 1
             for (int j = all.begin; j < all.end; j += all.step) {
                 float x[4];
                 load4(w + j, x);
@@ -221,15 +229,16 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
                 for (int i = 0; i < 4; ++i) cut.own += x[i] >= cut.tau;
             }
         }
-        const unsigned target = (unsigned)((float)want.p * (float)cut.mass);        // (64 units: fp32's last place)
-        if (!quick_find(w, mp, G, true, target, unit, slack.at((float)want.p), err, list, room, cut, turn)) return false;
+        // (a target by mass is off by 64 units: fp32's last place)
+        const unsigned target = by_mass ? (unsigned)((float)want.p * (float)cut.mass) : (unsigned)want.k;
+        if (!quick_find(w, mp, G, by_mass != 0, target, unit, slack.at((float)want.p), err, list, room, cut, turn)) return false;
     }
     if (want.r > 0.f) {
         const float e = err.weight - err.slope * log2f(want.r);
         const float low = want.r * (1.f - e), high = want.r * (1.f + e);
         unsigned near_[1] = {0};
         const Span all(G, mp);
-#pragma unroll 4
+#pragma unroll 2
         for (int j = all.begin; j < all.end; j += all.step) {
             float x[4];
             load4(w + j, x);
@@ -250,7 +259,7 @@ __device__ __forceinline__ bool quick_kept(float v, float tau) { return tau > 0.
 __device__ __forceinline__ void quick_tiles(const float *w, const int ntiles, const RowGroup &G, const float tau, const float unit, unsigned *tiles)
 {
     const int lane = G.t & 31;
-#pragma unroll 4
+#pragma unroll 2
     for (int q = G.t >> 5; q < ntiles; q += G.nt >> 5) {
         float v[4], s = 0.f;
         load4(w + q * ROW_TILE + 4 * lane, v);
@@ -263,6 +272,7 @@ __device__ __forceinline__ void quick_tiles(const float *w, const int ntiles, co
 __device__ __forceinline__ unsigned quick_total(const unsigned *tiles, const int ntiles)
 {
     unsigned s = 0;
+#pragma unroll 1
     for (int q = threadIdx.x & 31; q < ntiles; q += 32) s += tiles[q];
     return __reduce_add_sync(0xffffffffu, s);
 }
@@ -285,6 +295,7 @@ __device__ __forceinline__ bool quick_draw(const float *w, const int ntiles, con
     const unsigned target = __umulhi((unsigned)(u * 4294967296.f), total), slack = of.at(u);
     unsigned before = 0;
     int tile = -1;
+#pragma unroll 1
     for (int q0 = 0; q0 < ntiles; q0 += 32) {
         const unsigned v = q0 + lane < ntiles ? tiles[q0 + lane] : 0u, s = before + warp_scan(v);
         const unsigned over = __ballot_sync(0xffffffffu, s > target);

@@ -41,7 +41,7 @@ struct RowGroup {
         else asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(nt) : "memory");
     }
     // sums over the group, the same in every thread
-    __device__ __forceinline__ void add(double &mass, int &count) const
+    __device__ __noinline__ void add(double &mass, int &count) const
     {
 #pragma unroll
         for (int off = 16; off > 0; off >>= 1) {
@@ -52,6 +52,7 @@ struct RowGroup {
         if ((t & 31) == 0) { sc->mass[t >> 5] = mass; sc->count[t >> 5] = count; }
         sync();
         mass = 0.0; count = 0;
+#pragma unroll 1
         for (int i = 0; i < nt >> 5; ++i) { mass += sc->mass[i]; count += sc->count[i]; }
         sync();
     }
@@ -63,6 +64,7 @@ struct RowGroup {
         if (nt == 32) return v;
         if ((t & 31) == 0) sc->mass[t >> 5] = (double)v;
         sync();
+#pragma unroll 1
         for (int i = 0; i < nt >> 5; ++i) v = fmax(v, (Real)sc->mass[i]);
         sync();
         return v;
@@ -112,7 +114,7 @@ struct RowCut {
 // Shrinks the cut to the shortest head of the order that has `target` entries, or, by mass, a mass of `target`; the
 // present cut has more.
 template <typename Real>
-__device__ void row_find(const Real *w, const int mp, const RowGroup &G, const bool by_mass, const double target, RowCut<Real> &cut,
+__device__ __noinline__ void row_find(const Real *w, const int mp, const RowGroup &G, const bool by_mass, const double target, RowCut<Real> &cut,
                          const RowError &err, bool &unsure)
 {
     const RowCut<Real> old = cut;
@@ -120,6 +122,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
     int n_lo = old.count, n_hi = 0;
     double m_hi = 0.0;
     bool first = true;
+#pragma unroll 1
     while (n_lo - n_hi > ROW_CAND) {
         const auto bl = weight_bits(lo), bh = weight_bits(hi);
         if (bh - bl <= 1) break;                                    // equal weights
@@ -133,6 +136,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
         const Real pivot = weight_of(bp);
         double s4[4] = {0, 0, 0, 0};
         int c = 0;
+#pragma unroll 1
         for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
             Real v[4];
             load4(w + j, v);
@@ -154,11 +158,13 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
         const int r = (int)need;
         if (G.t < 32) {
             int seen = 0, at = -1;
+#pragma unroll 1
             for (int j = lane; j < mp && at < 0; j += 32) {
                 const bool is = w[j] == lo && (lo != old.tau || j <= old.J);
                 const unsigned ball = __ballot_sync(0xffffffffu, is);
                 if (seen + __popc(ball) >= r) {
                     unsigned left = ball;
+#pragma unroll 1
                     for (int q = r - seen; q > 1; --q) left &= left - 1;
                     at = j - lane + __ffs(left) - 1;
                 }
@@ -173,6 +179,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
     }
     if (G.t == 0) G.sc->n_cand = 0;
     G.sync();
+#pragma unroll 1
     for (int j = 4 * G.t; j < mp; j += 4 * G.nt) {
         Real v[4];
         load4(w + j, v);
@@ -189,6 +196,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
         const double mine = G.sc->cand_w[lane];
         const int j = G.sc->cand_j[lane];
         int rank = 0;
+#pragma unroll 1
         for (int q = 0; q < n; ++q) {
             const double o = G.sc->cand_w[q];
             rank += o > mine || (o == mine && G.sc->cand_j[q] < j) ? 1 : 0;
@@ -219,7 +227,7 @@ __device__ void row_find(const Real *w, const int mp, const RowGroup &G, const b
 // Cuts a row and leaves the sums of its tiles' kept weights in `tiles`.  `count` entries are above zero and have the mass
 // `mass`, `top` is the largest (1 up to errors).  Returns false where the row is unsure.
 template <typename Real>
-__device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const RowCuts &want, const Real top, const double mass, const int count,
+__device__ __noinline__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const RowCuts &want, const Real top, const double mass, const int count,
                         const RowError &err, RowCut<Real> &cut, double *tiles)
 {
     bool unsure = false;
@@ -256,6 +264,7 @@ __device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const Ro
         G.sync();
     }
     const int lane = G.t & 31;
+#pragma unroll 1
     for (int q = G.t >> 5; q < mp / ROW_TILE; q += G.nt >> 5) {
         const int j = q * ROW_TILE + 4 * lane;
         Real v[4];
@@ -295,6 +304,7 @@ __device__ bool row_cut(const Real *w, const int mp, const RowGroup &G, const Ro
 __device__ __forceinline__ double row_total(const double *tiles, const int ntiles)
 {
     double s = 0.0;
+#pragma unroll 1
     for (int q = threadIdx.x & 31; q < ntiles; q += 32) s += tiles[q];
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
@@ -303,7 +313,7 @@ __device__ __forceinline__ double row_total(const double *tiles, const int ntile
 
 // One draw, by one warp: the entry's index and weight.  Returns false where it is unsure.
 template <typename Real>
-__device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const double *tiles, const int ntiles, const double total, const double u,
+__device__ __noinline__ bool row_draw(const Real *w, const RowCut<Real> &cut, const double *tiles, const int ntiles, const double total, const double u,
                          const RowError &err, int &index, double &weight)
 {
     const int lane = threadIdx.x & 31;
@@ -311,6 +321,7 @@ __device__ bool row_draw(const Real *w, const RowCut<Real> &cut, const double *t
     // the first tile whose cumulative sum is above the target, or the last one that has something
     double base = 0.0, before = 0.0;
     int tile = -1;
+#pragma unroll 1
     for (int q0 = 0; q0 < ntiles; q0 += 32) {
         const double v = q0 + lane < ntiles ? tiles[q0 + lane] : 0.0;
         double s = v;
