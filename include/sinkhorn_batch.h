@@ -141,6 +141,9 @@ size_t sinkhorn_batch_workspace_bytes(const skb_config *cfg);
  * Create a batch (Eq. 1 inputs) and enqueue its set-up kernels.
  *   x   [W, n, d] row-major, fp32 or bf16 per cfg->xy_dtype      (device)
  *   y   [W, m, d]                                                (device)
+ *       or 4-bit clouds (SKB_MX4, SKB_NV4; d <= 1024): buffers of sinkhorn_cloud4_pack, 256-byte aligned.  The batch
+ *       runs on the values they stand for, as one of bf16 inputs (which holds them exactly) would, with 2 d bytes a point
+ *       more workspace; deep lanes that keep their products form them from the codes (sinkhorn_cloud4_dots)
  *   a   [W, n] fp32, > 0, each lane sums to 1                    (device)
  *   b   [W, m] fp32, > 0, each lane sums to 1                    (device)
  *   eps [W]    fp32, > 0, per-lane regularisation                (device)
@@ -481,6 +484,17 @@ typedef struct {
 size_t sinkhorn_plan_draw_workspace_bytes(const skb_draw_config *cfg);     /* 0: a bad shape or type */
 skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u,
                               const skb_draw_config *cfg, int *index, float *logp);
+
+/*
+ * Partners drawn from the plan of a finished batch: sinkhorn_plan_draw with the potentials that every lane finished with,
+ * partners of the sources (side 0, u and the outputs [W, n, draws]) or of the targets (side 1, [W, m, draws]).
+ *   x, y, eps: the arrays the batch was created from; cfg: W, n, m, d and xy_dtype of the batch, cfg->stream is not read
+ *   (the batch's is used), a workspace of sinkhorn_plan_draw_workspace_bytes(cfg), for side 1 with n and m exchanged.
+ * Valid once every lane has finished (SKB_ERR_STATE before that, and for batches whose lanes were replaced); synchronises
+ * to check that.  A lane that went non-finite gives no draws (-1).
+ */
+skb_status sinkhorn_batch_draw_plan(skb_batch *h, const void *x, const void *y, const float *eps, const float *u, int side,
+                                    const skb_draw_config *cfg, int *index, float *logp);
 
 /* Text of the calling thread's last failed sinkhorn_cloud4_* or sinkhorn_plan_draw call (empty after a successful one). */
 const char *sinkhorn_operator_last_error(void);

@@ -30,7 +30,7 @@ EXPORTS = (
     "sinkhorn_batch_launch_count", "sinkhorn_batch_profile_update", "sinkhorn_batch_arithmetic",
     "sinkhorn_batch_selftest_bounded_wait", "sinkhorn_batch_warm_start", "sinkhorn_batch_set_profiling",
     "sinkhorn_batch_cycle_trace", "sinkhorn_batch_selftest_unit_rates", "sinkhorn_batch_last_audit",
-    "sinkhorn_batch_refill", "sinkhorn_batch_apply_plan", "sinkhorn_batch_check_guards",
+    "sinkhorn_batch_refill", "sinkhorn_batch_apply_plan", "sinkhorn_batch_check_guards", "sinkhorn_batch_draw_plan",
 )
 PHASES = ("create", "f_leg", "column_check", "plan", "emit_move", "g_leg")
 # entry points outside the sinkhorn_batch_* family
@@ -119,6 +119,7 @@ def _load():
     lib.sinkhorn_plan_draw_workspace_bytes.restype = ctypes.c_size_t
     lib.sinkhorn_plan_draw_workspace_bytes.argtypes = [drawp]
     lib.sinkhorn_plan_draw.argtypes = [vp, vp, vp, vp, vp, drawp, vp, vp]
+    lib.sinkhorn_batch_draw_plan.argtypes = [vp, vp, vp, vp, vp, ci, drawp, vp, vp]
     lib.sinkhorn_operator_last_error.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("sinkhorn_batch_workspace_bytes", "sinkhorn_batch_host_workspace_bytes",
@@ -140,10 +141,10 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
-def make_config(W, n, m, d, *, bf16=False, mode="active", compute="auto", max_iter=5000,
+def make_config(W, n, m, d, *, bf16=False, format=None, mode="active", compute="auto", max_iter=5000,
                 audit_every=1, tol_screen=0.0, column_split=0, cost_form=0, stream=0, guard_band=0.0,
                 lane_capacity=0) -> SkbConfig:
-    return SkbConfig(W, n, m, d, 1 if bf16 else 0, MODES[mode] if isinstance(mode, str) else mode,
+    return SkbConfig(W, n, m, d, FORMATS[format] if format else 1 if bf16 else 0, MODES[mode] if isinstance(mode, str) else mode,
                      COMPUTE[compute] if isinstance(compute, str) else compute, max_iter, audit_every,
                      tol_screen, column_split, cost_form, stream, None, 0, guard_band, lane_capacity)
 
@@ -295,6 +296,10 @@ def cloud4_dots(x, y, out=None):
     return out
 
 
+def _raw(v):
+    return v.buffer if isinstance(v, Cloud4) else v
+
+
 def _cloud(v, name):
     """dtype, shape, pointer and the tensor to keep of a cloud: a tensor or a Cloud4."""
     if isinstance(v, Cloud4):
@@ -366,14 +371,22 @@ class SinkhornBatch:
     def __init__(self, x, y, a, b, eps, tol, *, mode="active", compute="auto", max_iter=5000,
                  audit_every=1, tol_screen=0.0, column_split=0, cost_form=0, stream=None, guard_band=0.0,
                  lane_capacity=0):
-        if not (x.is_cuda and y.is_cuda and a.is_cuda and b.is_cuda and eps.is_cuda):
-            raise ValueError("x, y, a, b, eps must be CUDA tensors")
-        if x.dtype not in (torch.float32, torch.bfloat16) or y.dtype != x.dtype:
-            raise ValueError("x and y must both be float32 or both be bfloat16")
+        self.format = x.format if isinstance(x, Cloud4) else None          # x and y may be clouds held in 4 bits
+        if self.format is None:
+            if isinstance(y, Cloud4):
+                raise ValueError("x and y must both be tensors or both be Cloud4")
+            if not (x.is_cuda and y.is_cuda and a.is_cuda and b.is_cuda and eps.is_cuda):
+                raise ValueError("x, y, a, b, eps must be CUDA tensors")
+            if x.dtype not in (torch.float32, torch.bfloat16) or y.dtype != x.dtype:
+                raise ValueError("x and y must both be float32 or both be bfloat16")
+        elif not isinstance(y, Cloud4) or y.format != x.format or not (a.is_cuda and b.is_cuda and eps.is_cuda):
+            raise ValueError("x and y must be Cloud4 of one format, a, b, eps CUDA tensors")
         for t in (a, b, eps):
             if t.dtype != torch.float32:
                 raise ValueError("a, b, eps must be float32")
-        x, y, a, b, eps = (t.contiguous() for t in (x, y, a, b, eps))
+        a, b, eps = (t.contiguous() for t in (a, b, eps))
+        if self.format is None:
+            x, y = x.contiguous(), y.contiguous()
         W, n, d = x.shape
         m = y.shape[1]
         if y.shape != (W, m, d) or a.shape != (W, n) or b.shape != (W, m) or eps.shape != (W,):
@@ -381,7 +394,7 @@ class SinkhornBatch:
         self.W, self.n, self.m, self.d = W, n, m, d
         self.device = x.device
         self.stream = stream if stream is not None else torch.cuda.current_stream(x.device)
-        self.cfg = make_config(W, n, m, d, bf16=x.dtype == torch.bfloat16, mode=mode, compute=compute,
+        self.cfg = make_config(W, n, m, d, bf16=self.format is None and x.dtype == torch.bfloat16, format=self.format, mode=mode, compute=compute,
                                max_iter=max_iter, audit_every=audit_every, tol_screen=tol_screen,
                                column_split=column_split, cost_form=cost_form, stream=self.stream.cuda_stream,
                                guard_band=guard_band, lane_capacity=lane_capacity)
@@ -395,7 +408,7 @@ class SinkhornBatch:
         self._keep = (x, y, a, b, eps)
         self.h = None
         with torch.cuda.device(x.device):
-            self.h = sinkhorn_batch_create(x, y, a, b, eps, float(tol), self.cfg)
+            self.h = sinkhorn_batch_create(_raw(x), _raw(y), a, b, eps, float(tol), self.cfg)
 
     def step(self, cycles=1):
         sinkhorn_batch_step(self.h, cycles)
@@ -450,13 +463,17 @@ class SinkhornBatch:
 
     def refill(self, x, y, a, b, eps) -> int:
         """New problems into the slots finished lanes have freed; returns their first lane number."""
-        x, y, a, b, eps = (t.contiguous() for t in (x, y, a, b, eps))
+        if (x.format if isinstance(x, Cloud4) else None) != self.format or (y.format if isinstance(y, Cloud4) else None) != self.format:
+            raise ValueError("x and y must be of the batch's storage type")
+        a, b, eps = (t.contiguous() for t in (a, b, eps))
+        if self.format is None:
+            x, y = x.contiguous(), y.contiguous()
         count = x.shape[0]
         if tuple(x.shape) != (count, self.n, self.d) or tuple(y.shape) != (count, self.m, self.d) or \
                 tuple(a.shape) != (count, self.n) or tuple(b.shape) != (count, self.m) or tuple(eps.shape) != (count,):
             raise ValueError("shapes must be x[c,n,d] y[c,m,d] a[c,n] b[c,m] eps[c]")
         first = ctypes.c_int(-1)
-        _check(lib.sinkhorn_batch_refill(self.h, _ptr(x), _ptr(y), _ptr(a), _ptr(b), _ptr(eps), count, ctypes.byref(first)), self.h)
+        _check(lib.sinkhorn_batch_refill(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(a), _ptr(b), _ptr(eps), count, ctypes.byref(first)), self.h)
         self._keep = self._keep + (x, y, a, b, eps)
         return first.value
 
@@ -467,8 +484,30 @@ class SinkhornBatch:
         if v.dtype != torch.float32 or v.dim() != 3 or tuple(v.shape[:2]) != (self.W, self.m):
             raise ValueError("v must be float32 [W, m, dv]")
         out = torch.empty(self.W, self.n, v.shape[2], dtype=torch.float32, device=self.device)
-        _check(lib.sinkhorn_batch_apply_plan(self.h, _ptr(x), _ptr(y), _ptr(eps), _ptr(v), v.shape[2], _ptr(out)), self.h)
+        _check(lib.sinkhorn_batch_apply_plan(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(eps), _ptr(v), v.shape[2], _ptr(out)), self.h)
         return out
+
+    def draw_plan(self, u, *, side="sources", temperature=None, top_k=None, top_p=None, min_p=None, logp=False):
+        """Partners of the sources (u [W, n] or [W, n, draws]) or of the targets (side "targets", u [W, m] or [W, m, draws])
+        drawn from the plan of the finished lanes; settings and outputs as those of plan_draw."""
+        if side not in ("sources", "targets"):
+            raise ValueError('side must be "sources" or "targets"')
+        x, y, _a, _b, eps = self._keep[:5]
+        if self.format is None:
+            x, y = (v if v.data_ptr() % 16 == 0 else v.clone() for v in (x, y))
+        other = side == "targets"
+        n, m = (self.m, self.n) if other else (self.n, self.m)
+        u = u.contiguous()
+        if u.device != self.device:
+            raise ValueError("u must be on the batch's device")
+        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            cfg = _draw_config(self.W, n, m, self.d, self.cfg.xy_dtype, u,
+                               dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p), self.stream.cuda_stream)
+            index, lp, ws = _draw_out(cfg, u, logp)
+            cfg.n, cfg.m = self.n, self.m
+            _check(lib.sinkhorn_batch_draw_plan(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(eps), _ptr(u), 1 if other else 0,
+                                                ctypes.byref(cfg), _ptr(index), _ptr(lp)), self.h)
+        return (index, lp) if logp else index
 
     def set_profiling(self, on=True):
         _check(lib.sinkhorn_batch_set_profiling(self.h, 1 if on else 0), self.h)

@@ -13,6 +13,7 @@
 
 #include "../../include/sinkhorn_batch.h"
 #include "skb_host.h"
+#include "skb_operators.h"
 
 using namespace skb;
 
@@ -44,6 +45,8 @@ struct skb_batch {
     std::vector<float> cycle_update_ms;   // per cycle: f-leg + g-leg
     alignas(64) unsigned char maps[2 * 128];   // CUtensorMap of x and of y
     GuardList guards;      // guard strips of the workspace in the layout the batch runs in
+    int packed;            // SKB_MX4 or SKB_NV4 where the caller's clouds are held in 4 bits, 0 otherwise
+    void *stage_x, *stage_y;   // their values (bf16)
     std::string err;
 };
 
@@ -143,11 +146,34 @@ static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 // Lanes that a batch can take in: its slots' and those that replace them.
 static int lanes_of(const skb_config *c) { return c->lane_capacity > c->W ? c->lane_capacity : c->W; }
 
+// 4-bit clouds (sinkhorn_cloud4_pack): a batch runs on their values, which bf16 holds exactly; they are staged at the start
+// of the workspace.  Where deep lanes keep their products, these come from the 4-bit codes.
+static bool packed4(const skb_config *c) { return c->xy_dtype == SKB_MX4 || c->xy_dtype == SKB_NV4; }
+static skb_config of_values(const skb_config *c)
+{
+    skb_config v = *c;
+    if (packed4(c)) v.xy_dtype = SKB_BF16;
+    return v;
+}
+static size_t stage_x_bytes(const skb_config *c) { return packed4(c) ? align_up((size_t)c->W * c->n * c->d * 2, 256) : 0; }
+static size_t stage_bytes(const skb_config *c) { return packed4(c) ? stage_x_bytes(c) + align_up((size_t)c->W * c->m * c->d * 2, 256) : 0; }
+// bytes of W clouds of npts points as the caller gives them
+static size_t cloud_bytes(const skb_config *c, size_t npts)
+{
+    if (packed4(c)) return cloud4_bytes((size_t)c->W * npts, c->d, c->xy_dtype);
+    return (size_t)c->W * npts * c->d * (c->xy_dtype == SKB_BF16 ? 2 : 4);
+}
+
 static bool config_ok(const skb_config *c, std::string &why)
 {
     if (!c) { why = "config is null"; return false; }
     if (c->W < 1 || c->n < 1 || c->m < 1 || c->d < 1) { why = "W, n, m, d must be >= 1"; return false; }
-    if (c->xy_dtype != SKB_F32 && c->xy_dtype != SKB_BF16) { why = "bad xy_dtype"; return false; }
+    if (c->xy_dtype < SKB_F32 || c->xy_dtype > SKB_NV4) { why = "bad xy_dtype"; return false; }
+    if (packed4(c)) {
+        const char *no = cloud4_refused(c->W, c->n, c->d, c->xy_dtype);
+        if (!no) no = cloud4_refused(c->W, c->m, c->d, c->xy_dtype);
+        if (no) { why = no; return false; }
+    }
     if (c->mode < SKB_ACTIVE || c->mode > SKB_MASKED_EXIT) { why = "bad mode"; return false; }
     if (c->compute < SKB_COMPUTE_AUTO || c->compute > SKB_COMPUTE_TENSOR) { why = "bad compute type"; return false; }
     if (c->max_iter < 1 || c->audit_every < 1) { why = "max_iter and audit_every must be >= 1"; return false; }
@@ -301,8 +327,9 @@ static const Variant *variant_for(const skb_config *c, int compute, bool spatial
 
 // room = false: the least that create takes (deep lanes then form their products in every leg, lanes in spatial order
 // choose their pairs in every leg)
-static size_t workspace_need(const skb_config *cfg, bool room)
+static size_t workspace_need(const skb_config *given, bool room)
 {
+    const skb_config values = of_values(given), *cfg = &values;
     // an automatic batch may end up with float64 coordinates: size for the larger layout
     if (cfg->compute == SKB_COMPUTE_TENSOR && !tc_eligible(cfg->d, cfg->xy_dtype == SKB_BF16)) return 0;
     const Variant *v = variant_for(cfg, cfg->compute == SKB_COMPUTE_AUTO ? SKB_COMPUTE_MIXED : cfg->compute, false);
@@ -319,7 +346,7 @@ static size_t workspace_need(const skb_config *cfg, bool room)
             if (t > need) need = t;
         }
     }
-    return need;
+    return need + stage_bytes(given);
 }
 
 extern "C" size_t sinkhorn_batch_workspace_bytes(const skb_config *cfg)
@@ -339,6 +366,27 @@ static skb_status cuda_fail(skb_batch *h, cudaError_t e, const char *where)
     return fail(h, SKB_ERR_CUDA, std::string(where) + ": " + cudaGetErrorString(e));
 }
 
+// Values of `count` lanes of 4-bit clouds, to the start of the workspace.
+static skb_status stage_values(skb_batch *h, const void *x4, const void *y4, int count)
+{
+    const skb_config &c = h->cfg;
+    skb_status st = sinkhorn_cloud4_unpack(x4, count, c.n, c.d, h->packed, h->stage_x, SKB_BF16, h->stream);
+    if (st == SKB_OK) st = sinkhorn_cloud4_unpack(y4, count, c.m, c.d, h->packed, h->stage_y, SKB_BF16, h->stream);
+    h->launches += 2;
+    return st == SKB_OK ? st : fail(h, st, sinkhorn_operator_last_error());
+}
+// The products of `count` lanes from slot0 on.
+static skb_status form_dots(skb_batch *h, const void *x4, const void *y4, int slot0, int count)
+{
+    const Dev &D = h->dev;
+    h->launches += 1;
+    if (!h->packed) { launch_gram(D, h->maps, slot0, count, h->stream); return SKB_OK; }
+    const Cloud4 x = cloud4_view(x4, (size_t)count * D.n, D.d, h->packed), y = cloud4_view(y4, (size_t)count * D.m, D.d, h->packed);
+    const skb_status st = launch_dots(dots_cloud(x4, x, h->packed, D.d, 0), dots_cloud(y4, y, h->packed, D.d, 0), h->packed, count, D.n, D.m,
+                                      D.dots + (size_t)slot0 * D.np * D.mp, D.mp, h->stream, D.np, D.mp);
+    return st == SKB_OK ? st : fail(h, st, sinkhorn_operator_last_error());
+}
+
 extern "C" skb_status sinkhorn_batch_create(const void *x, const void *y, const float *a, const float *b,
                                             const float *eps, float tol, const skb_config *cfg, skb_batch **out)
 {
@@ -352,6 +400,9 @@ extern "C" skb_status sinkhorn_batch_create(const void *x, const void *y, const 
         return fail(nullptr, shape ? SKB_ERR_SHAPE : SKB_ERR_VALUE, why);
     }
     if (!(tol > 0.0f) || !std::isfinite(tol)) return fail(nullptr, SKB_ERR_VALUE, "tol must be positive and finite");
+    const skb_config *given = cfg;
+    skb_config values = of_values(given);
+    cfg = &values;
     const bool automatic = cfg->compute == SKB_COMPUTE_AUTO;
     const Variant *var = variant_for(cfg, automatic ? SKB_COMPUTE_F32 : cfg->compute, false);
     const Variant *var_big = variant_for(cfg, automatic ? SKB_COMPUTE_MIXED : cfg->compute, false);
@@ -366,17 +417,22 @@ extern "C" skb_status sinkhorn_batch_create(const void *x, const void *y, const 
         return fail(nullptr, SKB_ERR_SHAPE, "the tensor-core path needs bf16 x, y and d a multiple of 64 with 64 <= d <= 512");
     size_t zero_end = 0;
     carve(cfg, var_big, false, false, false, nullptr, nullptr, &zero_end);
-    const size_t need = workspace_need(cfg, true);
+    const size_t need = workspace_need(given, true);
     const bool room = cfg->workspace_bytes >= need;
     if (!cfg->workspace) return fail(nullptr, SKB_ERR_WORKSPACE, "workspace is null");
     if (((uintptr_t)cfg->workspace & 255u) != 0) return fail(nullptr, SKB_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-    if (!room && cfg->workspace_bytes < workspace_need(cfg, false)) {
+    if (!room && cfg->workspace_bytes < workspace_need(given, false)) {
         char buf[128];
         snprintf(buf, sizeof(buf), "workspace too small: %zu bytes given, %zu needed", cfg->workspace_bytes, need);
         return fail(nullptr, SKB_ERR_WORKSPACE, buf);
     }
+    if (packed4(given) && (((uintptr_t)x | (uintptr_t)y) & 255u) != 0) return fail(nullptr, SKB_ERR_VALUE, "4-bit clouds must be 256-byte aligned");
+    values.workspace = (char *)given->workspace + stage_bytes(given);
+    values.workspace_bytes = given->workspace_bytes - stage_bytes(given);
     skb_batch *h = new (std::nothrow) skb_batch();
     if (!h) return fail(nullptr, SKB_ERR_CUDA, "host allocation failed");
+    h->packed = packed4(given) ? given->xy_dtype : 0;
+    h->stage_x = given->workspace; h->stage_y = (char *)given->workspace + stage_x_bytes(given);
     h->cfg = *cfg; h->var = var; h->stream = (cudaStream_t)cfg->stream;
     h->known_width = cfg->W; h->finished = false; h->enqueued = 0; h->launches = 0; h->h_ctl = nullptr;
     h->ev[0] = h->ev[1] = nullptr;
@@ -408,6 +464,12 @@ extern "C" skb_status sinkhorn_batch_create(const void *x, const void *y, const 
         skb_status st = cuda_fail(nullptr, e, "create");
         sinkhorn_batch_destroy(h);
         return st;
+    }
+    const void *x4 = x, *y4 = y;
+    if (h->packed) {
+        const skb_status st = stage_values(h, x4, y4, cfg->W);
+        if (st != SKB_OK) { fail(nullptr, st, h->err); sinkhorn_batch_destroy(h); return st; }
+        x = h->stage_x; y = h->stage_y;
     }
     launch_lane_stats(h->dev, x, y, eps, 0, 0, cfg->W, 0, h->stream);
     h->launches += 2;   // lane statistics + layout kernel
@@ -466,7 +528,10 @@ extern "C" skb_status sinkhorn_batch_create(const void *x, const void *y, const 
     }
     if (h->dev.permx) { launch_spatial_sort(h->dev, x, y, 0, cfg->W, h->stream); h->launches += 1; }
     launch_prep(h->dev, x, y, a, b, 0, cfg->W, h->stream);
-    if (h->dev.dots) { launch_gram(h->dev, h->maps, 0, cfg->W, h->stream); h->launches += 1; }
+    if (h->dev.dots) {
+        const skb_status st = form_dots(h, x4, y4, 0, cfg->W);
+        if (st != SKB_OK) { fail(nullptr, st, h->err); sinkhorn_batch_destroy(h); return st; }
+    }
     if (h->dev.guard > 0.0 && !h->dev.permx) {            // (lanes in spatial order: the layout kernel writes them)
         const size_t es = cfg->xy_dtype == SKB_BF16 ? 2 : 4;
         const size_t xb = (size_t)cfg->n * cfg->d * es, yb = (size_t)cfg->m * cfg->d * es;
@@ -533,6 +598,12 @@ extern "C" skb_status sinkhorn_batch_refill(skb_batch *h, const void *x, const v
     }
     const Dev &D = h->dev;
     const size_t es = h->cfg.xy_dtype == SKB_BF16 ? 2 : 4;
+    const void *x4 = x, *y4 = y;
+    if (h->packed) {
+        st0 = stage_values(h, x4, y4, count);        // (count <= W: the slots)
+        if (st0 != SKB_OK) return st0;
+        x = h->stage_x; y = h->stage_y;
+    }
     launch_lane_stats(D, x, y, eps, width, h->lanes_used, count, c.cycle, h->stream);
     cudaError_t e = cudaSuccess;
     if (h->tensor) {
@@ -543,7 +614,7 @@ extern "C" skb_status sinkhorn_batch_refill(skb_batch *h, const void *x, const v
     }
     if (D.permx) { launch_spatial_sort(D, x, y, width, count, h->stream); h->launches += 1; }
     launch_prep(D, x, y, a, b, width, count, h->stream);
-    if (D.dots) { launch_gram(D, h->maps, width, count, h->stream); h->launches += 1; }
+    if (D.dots && (st0 = form_dots(h, x4, y4, width, count)) != SKB_OK) return st0;
     if (D.guard > 0.0 && !D.permx) {
         const size_t xb = (size_t)h->cfg.n * h->cfg.d * es, yb = (size_t)h->cfg.m * h->cfg.d * es;
         e = cudaMemcpy2DAsync((char *)D.xraw + (size_t)width * D.xraw_stride, D.xraw_stride, x, xb, xb, count, cudaMemcpyDeviceToDevice, h->stream);
@@ -876,9 +947,30 @@ extern "C" skb_status sinkhorn_batch_apply_plan(skb_batch *h, const void *x, con
     skb_status st = read_ctl(h, &c);
     if (st != SKB_OK) return st;
     if (!c.done) return fail(h, SKB_ERR_STATE, "the plan is applied once every lane has finished (drain first)");
-    launch_apply_plan(h->dev, x, y, eps, v, dv, out, h->cfg.W, h->stream);
+    launch_apply_plan(h->dev, h->packed ? h->stage_x : x, h->packed ? h->stage_y : y, eps, v, dv, out, h->cfg.W, h->stream);
     cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? SKB_OK : cuda_fail(h, e, "apply_plan");
+}
+
+extern "C" skb_status sinkhorn_batch_draw_plan(skb_batch *h, const void *x, const void *y, const float *eps, const float *u, int side,
+                                               const skb_draw_config *cfg, int *index, float *logp)
+{
+    if (!h) return SKB_ERR_NULL;
+    if (!x || !y || !eps || !u || !cfg || !index) return fail(h, SKB_ERR_NULL, "x, y, eps, u, cfg and index are required");
+    if (side != 0 && side != 1) return fail(h, SKB_ERR_VALUE, "side must be 0 (partners of the sources) or 1 (of the targets)");
+    if (h->lanes_used > h->cfg.W) return fail(h, SKB_ERR_STATE, "not available for batches whose lanes were replaced (the inputs of all lanes are not in one array)");
+    const int dtype = h->packed ? h->packed : h->cfg.xy_dtype;
+    if (cfg->W != h->cfg.W || cfg->n != h->cfg.n || cfg->m != h->cfg.m || cfg->d != h->cfg.d || cfg->xy_dtype != dtype)
+        return fail(h, SKB_ERR_SHAPE, "W, n, m, d and xy_dtype of the configuration must be the batch's");
+    Ctl c;
+    skb_status st = read_ctl(h, &c);
+    if (st != SKB_OK) return st;
+    if (!c.done) return fail(h, SKB_ERR_STATE, "the plan is drawn from once every lane has finished (drain first)");
+    skb_draw_config mine = *cfg;
+    mine.stream = h->stream;
+    if (side) { mine.n = cfg->m; mine.m = cfg->n; }
+    st = sinkhorn_plan_draw(side ? y : x, side ? x : y, side ? h->dev.f_out : h->dev.g_out, eps, u, &mine, index, logp);
+    return st == SKB_OK ? st : fail(h, st, sinkhorn_operator_last_error());
 }
 
 extern "C" skb_status sinkhorn_batch_last_audit(skb_batch *h, float *r_row, float *r_col, int *flagged)
@@ -1008,8 +1100,8 @@ static HostStage host_stage(const skb_config *c, size_t base)
     HostStage s;
     size_t off = align_up(base, 256);
     auto take = [&](size_t b) { size_t o = off; off += align_up(b, 256); return o; };
-    const size_t W = c->W, n = c->n, m = c->m, d = c->d, es = c->xy_dtype == SKB_BF16 ? 2 : 4;
-    s.x = take(W * n * d * es); s.y = take(W * m * d * es);
+    const size_t W = c->W, n = c->n, m = c->m;
+    s.x = take(cloud_bytes(c, n)); s.y = take(cloud_bytes(c, m));
     s.a = take(W * n * 4); s.b = take(W * m * 4); s.eps = take(W * 4);
     s.f = take(W * n * 4); s.g = take(W * m * 4);
     s.depth = take(W * 4); s.status = take(W * 4); s.rrow = take(W * 4); s.rcol = take(W * 4);
@@ -1037,10 +1129,10 @@ extern "C" skb_status sinkhorn_batch_solve_host(const void *x, const void *y, co
     if (!cfg->workspace || cfg->workspace_bytes < s.end) return fail(nullptr, SKB_ERR_WORKSPACE, "workspace too small for the host-buffer call");
     char *base = (char *)cfg->workspace;
     cudaStream_t st = (cudaStream_t)cfg->stream;
-    const size_t W = cfg->W, n = cfg->n, m = cfg->m, d = cfg->d, es = cfg->xy_dtype == SKB_BF16 ? 2 : 4;
+    const size_t W = cfg->W, n = cfg->n, m = cfg->m;
     cudaError_t e;
-    if ((e = cudaMemcpyAsync(base + s.x, x, W * n * d * es, cudaMemcpyHostToDevice, st)) != cudaSuccess ||
-        (e = cudaMemcpyAsync(base + s.y, y, W * m * d * es, cudaMemcpyHostToDevice, st)) != cudaSuccess ||
+    if ((e = cudaMemcpyAsync(base + s.x, x, cloud_bytes(cfg, n), cudaMemcpyHostToDevice, st)) != cudaSuccess ||
+        (e = cudaMemcpyAsync(base + s.y, y, cloud_bytes(cfg, m), cudaMemcpyHostToDevice, st)) != cudaSuccess ||
         (e = cudaMemcpyAsync(base + s.a, a, W * n * 4, cudaMemcpyHostToDevice, st)) != cudaSuccess ||
         (e = cudaMemcpyAsync(base + s.b, b, W * m * 4, cudaMemcpyHostToDevice, st)) != cudaSuccess ||
         (e = cudaMemcpyAsync(base + s.eps, eps, W * 4, cudaMemcpyHostToDevice, st)) != cudaSuccess)

@@ -37,7 +37,7 @@ struct Dots {
     const float *px, *py;                                 // points' powers of two (nv4)
     float *out;
     long long ldo, lane_out;                              // floats from row to row, from lane to lane
-    int W, n, m, row_bytes, sb;                           // row_bytes: of a point's codes (or bf16 values)
+    int W, n, m, no, mo, row_bytes, sb;                   // no, mo: rows and columns of results; row_bytes: of a point's codes (or bf16 values)
     int tma_out;
 };
 
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
     tc_fence_after();
     const uint32_t tmem = tmem_holder;
 
-    const int nrt = (P.n + DT_BM - 1) / DT_BM, nct = (P.m + DT_BN - 1) / DT_BN;
+    const int nrt = (P.no + DT_BM - 1) / DT_BM, nct = (P.mo + DT_BN - 1) / DT_BN;
     const long long tiles = (long long)P.W * nrt * nct;
     const int chunks = (P.row_bytes + 127) / 128;
     auto where = [&](long long t, int &w, int &i0, int &j0) {
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             for (int c0 = 0; c0 < DT_BN; c0 += 32) {
-                if (j0 + c0 >= P.m) break;
+                if (j0 + c0 >= P.mo) break;
                 uint32_t r[32];
                 if (ok) {
                     tc_ld32_issue(tmem + (uint32_t)(quarter << 21) + b * DT_BN + c0, r);
@@ -279,12 +279,12 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 if (P.tma_out) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0 && i0 + quarter * 32 < P.n) tma_store_box(&tmo, box0 + turn * DT_BOX, j0 + c0, i0 + quarter * 32, w);
+                    if (lane == 0 && i0 + quarter * 32 < P.no) tma_store_box(&tmo, box0 + turn * DT_BOX, j0 + c0, i0 + quarter * 32, w);
                 } else {
                     __syncwarp();
-                    const int rows = min(32, P.n - (i0 + quarter * 32));
+                    const int rows = min(32, P.no - (i0 + quarter * 32));
                     float *dst = P.out + (size_t)w * P.lane_out + (size_t)(i0 + quarter * 32) * P.ldo + j0 + c0 + lane;
-                    if (j0 + c0 + lane < P.m)
+                    if (j0 + c0 + lane < P.mo)
                         for (int q = 0; q < rows; ++q)
                             dst[(size_t)q * P.ldo] = *reinterpret_cast<const float *>(box + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
                     __syncwarp();
@@ -332,7 +332,7 @@ skb_status launch_kind(const CUtensorMap &tx, const CUtensorMap &ty, const CUten
     constexpr int sf = KIND == SKB_BF16 ? 0 : KIND == SKB_NV4 ? 2048 : 1024;
     constexpr int smem = DT_STAGES * (2 * (int)DT_TILE + 2 * sf) + 8 * (int)DT_BOX + 1024;
     cudaFuncSetAttribute(dots_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    const long long tiles = (long long)P.W * ((P.n + DT_BM - 1) / DT_BM) * ((P.m + DT_BN - 1) / DT_BN);
+    const long long tiles = (long long)P.W * ((P.no + DT_BM - 1) / DT_BM) * ((P.mo + DT_BN - 1) / DT_BN);
     dots_kernel<KIND><<<(unsigned)(tiles < sms ? tiles : sms), DT_THREADS, smem, st>>>(tx, ty, to, P);
     return op_launched("products");
 }
@@ -345,15 +345,17 @@ DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t
     return {c.codes + row * c.cb, c.scales + row * c.sb, c.points ? c.points + row : nullptr, c.cb, c.sb};
 }
 
-skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st)
+skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st,
+                       int n_out, int m_out)
 {
     if (!encoder()) return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
     int dev = 0, sms = 0;
     cudaGetDevice(&dev);
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");
     Dots P = {};
-    P.out = out; P.ldo = ldo; P.lane_out = ldo * n;
     P.W = W; P.n = n; P.m = m;
+    P.no = n_out > n ? n_out : n; P.mo = m_out > m ? m_out : m;
+    P.out = out; P.ldo = ldo; P.lane_out = ldo * P.no;
     P.sx = x.scales; P.sy = y.scales; P.px = x.points; P.py = y.points;
     P.row_bytes = x.row_bytes; P.sb = x.sb;
     const void *cx = x.data, *cy = y.data;
@@ -362,7 +364,7 @@ skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W,
     const size_t rb = P.row_bytes;
     if (!make_map(&tx, CU_TENSOR_MAP_DATA_TYPE_UINT8, cx, rb, n, W, rb, rb * n, 128, DT_BM) ||
         !make_map(&ty, CU_TENSOR_MAP_DATA_TYPE_UINT8, cy, rb, m, W, rb, rb * m, 128, DT_BN) ||
-        (P.tma_out && !make_map(&to, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, out, m, n, W, ldo * 4, ldo * 4 * n, 32, 32)))
+        (P.tma_out && !make_map(&to, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, out, P.mo, P.no, W, ldo * 4, ldo * 4 * P.no, 32, 32)))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     if (dtype == SKB_BF16) return launch_kind<SKB_BF16>(tx, ty, to, P, sms, st);
     if (dtype == SKB_MX4) return launch_kind<SKB_MX4>(tx, ty, to, P, sms, st);

@@ -1,0 +1,179 @@
+"""Batches of clouds held in 4 bits, and draws from the plan of a finished batch: the operators as they are used together."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+from test_draw import reference
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2607_24741_b200 import build
+    build.build()
+    from paper_2607_24741_b200 import binding
+    return binding
+
+
+def problem(seed, W, n, m, d, fmt=None):
+    """Embeddings in a few clusters, uneven weights; on the GPU."""
+    import torch
+    gen = torch.Generator().manual_seed(seed)
+    mu = torch.randn(W, 4, d, generator=gen)
+    unit = lambda v: v / v.norm(dim=2, keepdim=True)
+    pick = lambda k: torch.gather(mu, 1, torch.randint(4, (W, k, 1), generator=gen).expand(W, k, d))
+    x, y = unit(torch.randn(W, n, d, generator=gen) + pick(n)), unit(torch.randn(W, m, d, generator=gen) + pick(m))
+    a, b = 0.5 + torch.rand(W, n, generator=gen).double(), 0.5 + torch.rand(W, m, generator=gen).double()
+    a, b = (a / a.sum(1, keepdim=True)).float(), (b / b.sum(1, keepdim=True)).float()
+    eps = torch.full((W,), 0.1)
+    return tuple(t.cuda() for t in (x, y, a, b, eps))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+@pytest.mark.parametrize("shape,compute", [((5, 40, 50, 20), "auto"), ((3, 70, 66, 40), "f32"), ((4, 130, 100, 64), "auto"), ((3, 333, 257, 192), "tensor"),
+                                           ((2, 1030, 300, 128), "auto"), ((6, 200, 210, 512), "auto"), ((2, 60, 90, 640), "auto")])
+def test_a_packed_batch_is_the_batch_of_its_values(B, fmt, shape, compute):
+    # The values are bf16 numbers.  Where no products are kept, the same kernels see the same inputs: equal bits.  Where they
+    # are, they differ by the matrix unit's roundings: two runs of the parity suite's acceptance, potentials to 1e-4.
+    import torch
+    W, n, m, d = shape
+    x, y, a, b, eps = problem(sum(shape), W, n, m, d)
+    x4, y4 = B.cloud4_pack(x, fmt), B.cloud4_pack(y, fmt)
+    kw = dict(compute=compute, max_iter=400)
+    p = B.SinkhornBatch(x4, y4, a, b, eps, 1e-3, **kw)
+    v = B.SinkhornBatch(x4.values(torch.bfloat16), y4.values(torch.bfloat16), a, b, eps, 1e-3, **kw)
+    assert p.arithmetic() == v.arithmetic()
+    p.drain(), v.drain()
+    products = p.arithmetic() == "tensor"
+    dp, dv = p.depths()[0], v.depths()[0]
+    (fp, gp), (fv, gv) = p.potentials(f64=True), v.potentials(f64=True)
+    img_p, img_v = p.apply_plan(y[:, :, :8]), v.apply_plan(y[:, :, :8])
+    if not products:
+        assert torch.equal(dp, dv) and torch.equal(fp, fv) and torch.equal(gp, gv) and torch.equal(img_p, img_v)
+    else:
+        assert bool(((dp - dv).abs() <= 1).all())
+        same = dp == dv
+        scale = max(float(fv.abs().max()), float(gv.abs().max()))
+        assert bool(same.any()) and float((fp - fv)[same].abs().max()) <= 1e-4 * scale and float((gp - gv)[same].abs().max()) <= 1e-4 * scale
+    assert bool((p.depths()[1] == B.LANE_DONE).all()) and float(torch.stack(p.residuals()).max()) <= 1e-3
+    assert p.check_guards() == -1
+    p.close(), v.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,shape", [(None, (3, 60, 45, 5)), ("nv4", (2, 130, 120, 128)), ("mx4", (3, 90, 100, 48))])
+def test_pack_solve_and_draw_both_ways(B, fmt, shape):
+    # the whole path, each draw the definition's with the potentials that the batch gives
+    import torch
+    W, n, m, d = shape
+    x, y, a, b, eps = problem(7, W, n, m, d)
+    if fmt:
+        x, y = B.cloud4_pack(x, fmt), B.cloud4_pack(y, fmt)
+    sb = B.SinkhornBatch(x, y, a, b, eps, 1e-3)
+    u, w = torch.rand(W, n, 2, generator=torch.Generator().manual_seed(1)).cuda(), torch.rand(W, m, generator=torch.Generator().manual_seed(2)).cuda()
+    with pytest.raises(B.SkbError) as e:
+        sb.draw_plan(u)
+    assert e.value.code == 5                                     # not finished
+    sb.drain()
+    f, g = sb.potentials(f64=True)
+    T, p = torch.full((W,), 0.8).cuda(), torch.full((W,), 0.9).cuda()
+    idx, lp = sb.draw_plan(u, temperature=T, top_p=p, logp=True)
+    assert torch.equal(idx, B.plan_draw(x, y, g, eps, u, temperature=T, top_p=p))
+    back = sb.draw_plan(w, side="targets")
+    assert back.shape == (W, m) and torch.equal(back, B.plan_draw(y, x, f, eps, w))
+    h = lambda t: (t.values() if fmt and isinstance(t, B.Cloud4) else t).cpu().double().numpy()
+    want, wlp = reference(h(x), h(y), g.cpu().numpy(), eps.cpu().numpy(), u.cpu().double().numpy(), T=T.cpu().numpy(), p=p.cpu().numpy())
+    np.testing.assert_array_equal(idx.cpu().numpy(), want)
+    assert np.abs(lp.cpu().numpy() - wlp).max() <= 1e-3
+    want, _ = reference(h(y), h(x), f.cpu().numpy(), eps.cpu().numpy(), w.cpu().double().numpy()[:, :, None])
+    np.testing.assert_array_equal(back.cpu().numpy(), want[:, :, 0])
+    # the plan's own marginal: with many numbers, partners come up as often as the plan says (five standard deviations)
+    many = torch.rand(W, n, 400, generator=torch.Generator().manual_seed(3)).cuda()
+    got = sb.draw_plan(many).cpu().numpy()
+    rows = sb.apply_plan(torch.eye(m, device="cuda")[None, :, :16].expand(W, m, 16).contiguous()).cpu().numpy()
+    share = rows / a.cpu().numpy()[:, :, None]
+    for j in range(16):
+        hits, q = (got == j).sum(2), np.clip(share[:, :, j], 0, 1)
+        total, expect, var = hits.sum(), 400 * q.sum(), 400 * (q * (1 - q)).sum()
+        assert abs(total - expect) <= 5 * math.sqrt(var) + 400 * 1e-3 * W * n * q.mean() + 5
+    sb.close()
+
+
+@pytest.mark.gpu
+def test_lanes_of_a_packed_batch_are_replaced(B):
+    import torch
+    W, n, m, d = 4, 150, 130, 128
+    x, y, a, b, eps = problem(3, 2 * W, n, m, d)
+    part = lambda t, s: t[s].contiguous()
+    first, second = slice(0, W), slice(W, 2 * W)
+    pk = lambda t, s: B.cloud4_pack(part(t, s), "nv4")
+    sb = B.SinkhornBatch(pk(x, first), pk(y, first), a[first], b[first], eps[first], 1e-3, lane_capacity=2 * W)
+    sb.drain()
+    assert sb.refill(pk(x, second), pk(y, second), a[second], b[second], eps[second]) == W
+    sb.drain()
+    f, g = sb.potentials(f64=True)
+    one = B.SinkhornBatch(pk(x, second), pk(y, second), a[second], b[second], eps[second], 1e-3)
+    one.drain()
+    f1, g1 = one.potentials(f64=True)
+    assert torch.equal(sb.depths()[0][W:], one.depths()[0]) and torch.equal(f[W:], f1) and torch.equal(g[W:], g1)
+    with pytest.raises(B.SkbError) as e:
+        sb.draw_plan(torch.rand(W, n).cuda())
+    assert e.value.code == 5                                     # the inputs of all lanes are not in one array
+    with pytest.raises(ValueError):
+        sb.refill(x[:1], y[:1], a[:1], b[:1], eps[:1])
+    assert sb.check_guards() == -1
+    sb.close(), one.close()
+
+
+@pytest.mark.gpu
+def test_packed_clouds_from_host_buffers(B):
+    import torch
+    W, n, m, d = 3, 100, 90, 200
+    x, y, a, b, eps = problem(5, W, n, m, d)
+    x4, y4 = B.cloud4_pack(x, "mx4"), B.cloud4_pack(y, "mx4")
+    sb = B.SinkhornBatch(x4, y4, a, b, eps, 1e-3)
+    sb.drain()
+    want = sb.potentials()
+    depth = sb.depths()[0].cpu()
+    sb.close()
+    cfg = B.make_config(W, n, m, d, format="mx4")
+    ws = torch.empty(B.sinkhorn_batch_host_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    cfg.workspace, cfg.workspace_bytes = ws.data_ptr(), ws.numel()
+    host = [t.cpu().contiguous() for t in (x4.buffer, y4.buffer, a, b, eps)]
+    f, g, dep = torch.zeros(W, n), torch.zeros(W, m), torch.zeros(W, dtype=torch.int32)
+    ptr = lambda t: ctypes.c_void_p(t.data_ptr())
+    rc = B.lib.sinkhorn_batch_solve_host(*(ptr(t) for t in host), 1e-3, ctypes.byref(cfg), ptr(f), ptr(g), ptr(dep), None, None, None, None, None)
+    assert rc == 0
+    assert torch.equal(dep, depth) and torch.equal(f, want[0].cpu()) and torch.equal(g, want[1].cpu())
+
+
+@pytest.mark.gpu
+def test_a_nan_point_of_a_packed_cloud_is_reported(B):
+    x, y, a, b, eps = problem(6, 2, 80, 70, 64)
+    x[1, 3, 5] = float("inf")
+    sb = B.SinkhornBatch(B.cloud4_pack(x, "nv4"), B.cloud4_pack(y, "nv4"), a, b, eps, 1e-3)
+    with pytest.raises(B.SkbError) as e:
+        sb.drain()
+    assert e.value.code == 3
+    sb.close()
+
+
+def test_refusals_of_packed_batches_and_their_draws(B):
+    ok = B.make_config(4, 64, 48, 128, format="nv4")
+    plain = B.make_config(4, 64, 48, 128, bf16=True)
+    staged = 4 * (64 + 48) * 128 * 2
+    assert B.sinkhorn_batch_workspace_bytes(ok) == B.sinkhorn_batch_workspace_bytes(plain) + staged
+    assert B.sinkhorn_batch_workspace_bytes(B.make_config(4, 64, 48, 1025, format="mx4")) == 0
+    bad = B.make_config(4, 64, 48, 128)
+    bad.xy_dtype = 4
+    assert B.sinkhorn_batch_workspace_bytes(bad) == 0
+    h, one, off = ctypes.c_void_p(), ctypes.c_void_p(4096), ctypes.c_void_p(4096 + 64)
+    ok.workspace, ok.workspace_bytes = 4096, 1 << 40
+    assert B.lib.sinkhorn_batch_create(off, one, one, one, one, 1e-3, ctypes.byref(ok), ctypes.byref(h)) == 3 and h.value is None
+    assert b"aligned" in B.lib.sinkhorn_batch_last_error(None)
+    ok.workspace_bytes = staged + 1000
+    assert B.lib.sinkhorn_batch_create(one, one, one, one, one, 1e-3, ctypes.byref(ok), ctypes.byref(h)) == 4
+    cfg = B.SkbDrawConfig(1, 4, 4, 2, 0, 1)
+    assert B.lib.sinkhorn_batch_draw_plan(None, one, one, one, one, 0, ctypes.byref(cfg), one, None) == 1
