@@ -10,8 +10,12 @@
 //   warps 2-5  block scales (4-bit kinds): from the points' rows into the order that the matrix unit wants, through
 //              shared memory; they are a sixteenth of the codes and their rows too short for TMA.  Two warps to an operand, each
 //              takes every other chunk, so that a chunk's load latency has two chunks' time
-//   warps 6-9  results: tensor memory -> registers -> 32 x 32 boxes in shared memory -> TMA stores, which clip ragged edges.
+//   warps 6-13 results: tensor memory -> registers -> 32 x 32 boxes in shared memory -> TMA stores, which clip ragged edges.
 //              Rows that are no whole number of 16 bytes are stored by the threads, a warp to a row
+// Tiles are dealt out to the blocks in turn, columns fastest: what is written at a time lies together.  A range of tiles to a block
+// with the rows' operand kept in shared memory reads half as much and takes longer (64 lanes of 1024 x 1024 x 512, mx4: 71 us,
+// pairs of tiles with their rows kept 61, this 56; a fill of the same results 39).  Four warps for the results instead
+// of eight: 73 us for 4 lanes of 4096 x 4096 x 512 in nv4, 68 so.
 // In nv4 the points' powers of two multiply the results on their way out, which is exact.
 // Accumulation is the matrix unit's fp32.  Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and
 // the tiles that were not finished are NaN.
@@ -27,7 +31,7 @@ namespace skb {
 namespace {
 
 constexpr int DT_BM = 128, DT_BN = 128;
-constexpr int DT_THREADS = 320, DT_STAGES = 4;
+constexpr int DT_EPI = 8, DT_THREADS = (6 + DT_EPI) * 32, DT_STAGES = 4;
 constexpr uint32_t DT_TILE = 128 * 128;                  // bytes: 128 points, 128 bytes of each
 constexpr uint32_t DT_BOX = 32 * 32 * 4;                 // a box of results
 constexpr int DT_SF_COL = 2 * DT_BN, DT_SF_STRIDE = 32;  // tensor memory: accumulators, then the scales of each stage
@@ -98,7 +102,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
     unsigned char *gen = smem_dyn + (base - smem_u32(smem_dyn));
     // operand tiles of all stages, then boxes of results (both want 1024 bytes), then scales
     auto tile_a = [&](int s) { return base + (uint32_t)s * 2 * DT_TILE; };
-    const uint32_t boxes = base + DT_STAGES * 2 * DT_TILE, sfs = boxes + 8 * DT_BOX;
+    const uint32_t boxes = base + DT_STAGES * 2 * DT_TILE, sfs = boxes + 2 * DT_EPI * DT_BOX;
     auto sf_a = [&](int s) { return sfs + (uint32_t)s * 2 * SF; };
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     constexpr int FULL = 0, EMPTY = DT_STAGES, SCALES = 2 * DT_STAGES, ACC = 3 * DT_STAGES, ACC_FREE = ACC + 2, LAST = ACC + 4;
@@ -108,7 +112,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             mbar_init(bar(EMPTY + s), 1);
             mbar_init(bar(SCALES + s), 2);
         }
-        for (int b = 0; b < 2; ++b) { mbar_init(bar(ACC + b), 1); mbar_init(bar(ACC_FREE + b), 4); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bar(ACC + b), 1); mbar_init(bar(ACC_FREE + b), DT_EPI); }
         mbar_init(bar(LAST), 1);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -230,7 +234,8 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             }
         }
     } else {
-        const int quarter = warp & 3, e = (warp - 6) * 32 + lane;     // the lanes of tensor memory that this warp may read
+        // the lanes of tensor memory that this warp may read, and its half of a tile's columns
+        const int quarter = warp & 3, half = (warp - 6) >> 2, e = (warp - 6) * 32 + lane;
         const uint32_t box0 = boxes + (uint32_t)(warp - 6) * 2 * DT_BOX;
         unsigned char *gbox0 = gen + (box0 - base);
         int b = 0, ph = 0, turn = 0;
@@ -242,14 +247,14 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             float rp = 1.f;
             if constexpr (KIND == SKB_NV4) {
                 // (the buffer of two tiles ago: its readers have passed the barrier of the last tile)
-                col_points[b][e] = j0 + e < P.m ? P.py[(size_t)w * P.m + j0 + e] : 0.f;
+                if (e < DT_BN) col_points[b][e] = j0 + e < P.m ? P.py[(size_t)w * P.m + j0 + e] : 0.f;
                 rp = row < P.n ? P.px[(size_t)w * P.n + row] : 0.f;
-                asm volatile("bar.sync 1, 128;" ::: "memory");
+                asm volatile("bar.sync 1, %0;" ::"n"(DT_EPI * 32) : "memory");
             }
             ok = ok && mbar_wait(bar(ACC + b), ph, &abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
-            for (int c0 = 0; c0 < DT_BN; c0 += 32) {
+            for (int c0 = half * (DT_BN / 2); c0 < (half + 1) * (DT_BN / 2); c0 += 32) {
                 if (j0 + c0 >= P.mo) break;
                 uint32_t r[32];
                 if (ok) {
@@ -330,7 +335,7 @@ template <int KIND>
 skb_status launch_kind(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &to, const Dots &P, int sms, cudaStream_t st)
 {
     constexpr int sf = KIND == SKB_BF16 ? 0 : KIND == SKB_NV4 ? 2048 : 1024;
-    constexpr int smem = DT_STAGES * (2 * (int)DT_TILE + 2 * sf) + 8 * (int)DT_BOX + 1024;
+    constexpr int smem = DT_STAGES * (2 * (int)DT_TILE + 2 * sf) + 2 * DT_EPI * (int)DT_BOX + 1024;
     cudaFuncSetAttribute(dots_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     const long long tiles = (long long)P.W * ((P.no + DT_BM - 1) / DT_BM) * ((P.mo + DT_BN - 1) / DT_BN);
     dots_kernel<KIND><<<(unsigned)(tiles < sms ? tiles : sms), DT_THREADS, smem, st>>>(tx, ty, to, P);
