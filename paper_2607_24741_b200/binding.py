@@ -6,6 +6,7 @@ missing or fails to load, importing this module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -220,15 +221,34 @@ def _check_op(code):
 
 
 # They run on the current stream of the tensors' device, and their outputs and workspaces belong to it.
+_HERE_ALREADY = contextlib.nullcontext()
+
+
+def _on(device):
+    """The device's context; none where it is the current one (a call of a few microseconds is worth that)."""
+    return _HERE_ALREADY if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
 def _stream(device):
     return torch.cuda.current_stream(device).cuda_stream
+
+
+def _cloud4_bytes(W, npts, d, format):
+    """sinkhorn_cloud4_bytes for a valid shape, 0 otherwise."""
+    if min(W, npts, d) < 1 or d > 1024 or W * npts > 0x7fffffff:
+        return 0
+    pad = lambda b: (b + 255) // 256 * 256
+    rows, blocks = W * npts, (d + 31) // 32 * (2 if format == "nv4" else 1)
+    return pad(rows * ((d + 31) // 32 * 16)) + pad(rows * ((blocks + 3) // 4 * 4)) + (pad(rows * 4) if format == "nv4" else 0)
 
 
 class Cloud4:
     """A cloud [W, npts, d] held in 4 bits: `buffer` as sinkhorn_cloud4_pack lays it out (a uint8 CUDA tensor)."""
 
     def __init__(self, buffer, W, npts, d, format):
-        need = lib.sinkhorn_cloud4_bytes(W, npts, d, FORMATS[format])
+        if format not in FORMATS:
+            raise ValueError(f"format must be one of {tuple(FORMATS)}")
+        need = _cloud4_bytes(W, npts, d, format)
         if need == 0:
             raise ValueError("W, npts and d must be >= 1, d at most 1024")
         if buffer.dtype != torch.uint8 or not buffer.is_cuda or not buffer.is_contiguous() or buffer.numel() < need:
@@ -249,7 +269,7 @@ class Cloud4:
         """What the cloud stands for, [W, npts, d] float32 or bfloat16."""
         if dtype not in DTYPES:
             raise ValueError("dtype must be float32 or bfloat16")
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             out = torch.empty(self.shape, dtype=dtype, device=self.device)
             _check_op(lib.sinkhorn_cloud4_unpack(_ptr(self.buffer), self.W, self.npts, self.d, FORMATS[self.format], _ptr(out),
                                                  DTYPES[dtype], _stream(self.device)))
@@ -267,10 +287,10 @@ def cloud4_pack(v, format="mx4", values=None):
         raise ValueError("values must be torch.float32 or torch.bfloat16")
     v = v.contiguous()
     W, npts, d = v.shape
-    need = lib.sinkhorn_cloud4_bytes(W, npts, d, FORMATS[format])
+    need = _cloud4_bytes(W, npts, d, format)
     if need == 0:
         raise ValueError("W, npts and d must be >= 1, d at most 1024")
-    with torch.cuda.device(v.device):
+    with _on(v.device):
         buffer = torch.empty(need, dtype=torch.uint8, device=v.device)
         out = None if values is None else torch.empty(v.shape, dtype=values, device=v.device)
         _check_op(lib.sinkhorn_cloud4_pack(_ptr(v), DTYPES[v.dtype], W, npts, d, FORMATS[format], _ptr(buffer), _ptr(out),
@@ -288,7 +308,7 @@ def cloud4_dots(x, y, out=None):
     shape = (x.W, x.npts, y.npts)
     if out is not None and (out.dtype != torch.float32 or out.device != x.device or tuple(out.shape) != shape or not out.is_contiguous()):
         raise ValueError("out must be a contiguous float32 tensor [W, n, m] on the clouds' device")
-    with torch.cuda.device(x.device):
+    with _on(x.device):
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=x.device)
         _check_op(lib.sinkhorn_cloud4_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, FORMATS[x.format], _ptr(out),
@@ -357,7 +377,7 @@ def plan_draw(x, y, g, eps, u, *, temperature=None, top_k=None, top_p=None, min_
     if eps.dtype != torch.float32 or eps.device != device or tuple(eps.shape) != (W,):
         raise ValueError("eps must be a float32 tensor [W] on the device of the clouds")
     g, eps, u = g.contiguous(), eps.contiguous(), u.contiguous()
-    with torch.cuda.device(device):
+    with _on(device):
         cfg = _draw_config(W, n, m, d, dt, u, dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p),
                            _stream(device))
         index, lp, ws = _draw_out(cfg, u, logp)

@@ -1067,8 +1067,13 @@ Plan plan_of(const Draw &P)
     // then to a block.
     const size_t three = 65 * 1024, two = 103 * 1024;
     if (p.dots) (void)(warps_fit<1, true>(p, P.mp, P.d, two) || groups_fit<4, true>(p, P.mp, P.d) || groups_fit<1, true>(p, P.mp, P.d));
-    else (void)(warps_fit<4, false>(p, P.mp, P.d, three) || warps_fit<2, false>(p, P.mp, P.d, three) || warps_fit<1, false>(p, P.mp, P.d, two) ||
-                groups_fit<4, false>(p, P.mp, P.d) || groups_fit<1, false>(p, P.mp, P.d));
+    else {
+        // (several rows to a warp only where every warp that the GPU holds still has two such units: 8 lanes of 64 rows of 64,
+        // 16 us with four rows to a warp, 6 with one)
+        const long long rows = (long long)P.W * P.n, warps = 2LL * 3 * WARPS * DRAW_BLOCKS;
+        (void)((rows >= 4 * warps && warps_fit<4, false>(p, P.mp, P.d, three)) || (rows >= 2 * warps && warps_fit<2, false>(p, P.mp, P.d, three)) ||
+               warps_fit<1, false>(p, P.mp, P.d, two) || groups_fit<4, false>(p, P.mp, P.d) || groups_fit<1, false>(p, P.mp, P.d));
+    }
     p.lanes = P.W; p.rows = P.n;
     if (!p.fp32()) p.dots = false;
     if (p.dots) {

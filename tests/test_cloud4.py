@@ -219,6 +219,9 @@ def test_refusals_of_pack_and_unpack(B):
     L, one = B.lib, ctypes.c_void_p(4096)
     assert L.sinkhorn_cloud4_bytes(1, 1, 1, 2) == 512 and L.sinkhorn_cloud4_bytes(1, 1, 1, 3) == 768
     assert L.sinkhorn_cloud4_bytes(64, 1024, 512, 2) == 64 * 1024 * (256 + 16)
+    for shape in ((1, 1, 1), (3, 37, 100), (2, 5, 64), (7, 333, 1000), (1, 1, 1024)):
+        for name, fmt in B.FORMATS.items():
+            assert B._cloud4_bytes(*shape, name) == L.sinkhorn_cloud4_bytes(*shape, fmt) > 0
     for bad in ((0, 1, 1, 2), (1, 0, 1, 2), (1, 1, 0, 2), (1, 1, 1025, 2), (1, 1, 8, 1), (1, 1, 8, 4), (-1, 1, 8, 2), (1 << 16, 1 << 16, 8, 2)):
         assert L.sinkhorn_cloud4_bytes(*bad) == 0
         assert L.sinkhorn_cloud4_pack(one, 0, *bad, one, None, 0, None) == 2 and L.sinkhorn_operator_last_error()
