@@ -12,8 +12,8 @@
 // Two ways to the exponents:
 //   differences   |x - y|^2 in fp32 from a transposed copy of y, R rows to a block: two operations a dimension and pair,
 //                 two columns to an instruction
-//   products      deep bf16 and 4-bit clouds: x . y from the tensor cores (skb_dots.cu) for as many rows at a time as stay in
-//                 the L2 cache, z = k (g - |y|^2) + 2 k x . y
+//   products      deep bf16 and 4-bit clouds: x . y from the tensor cores (skb_dots.cu), 512 MB at a time,
+//                 z = k (g - |y|^2) + 2 k x . y
 // Rows that do not fit shared memory (from some 49 000 entries on) are decided in float64 alone, weights in the workspace.
 #include <cuda_runtime.h>
 #include <math_constants.h>
@@ -33,7 +33,9 @@ constexpr int DRAW_BLOCKS = 148;                     // SMs; the fp32 kernel has
 constexpr int DRAW_EXACT_BLOCKS = 148;               // rows of scratch in the workspace
 constexpr float ROW_FLOOR = 2.384185791015625e-7f;   // 2^-22: weights that are formed again where fp32 does not do
 constexpr float ROW_TAIL = 5.9604645e-8f;            // 2^-24: weights that a row of few heavy entries does without
-constexpr size_t DRAW_DOTS_BYTES = (size_t)64 << 20; // products that are held at a time: half of the L2 cache
+// Products that are held at a time.  64 lanes of 1024 x 1024 x 512: 843 us by 64 MB, which stay in the L2 cache, 780 by 128 MB,
+// 743 all at once: the rows that are formed again are then one launch, too.
+constexpr size_t DRAW_DOTS_BYTES = (size_t)512 << 20;
 
 struct Draw {
     const void *x, *y;
@@ -554,10 +556,10 @@ __device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
 
 // A row once more: what weighs more than ROW_FLOOR to fp32's last place, what does not is `off` of itself off.  x: -x, `step`
 // apart (differences), or room for a row (products), whose bound is `bound`.  A row that is a list of n entries, columns
-// `where`, has a mass `tail` besides.
+// `where`, has a mass `tail` besides; `loose` is the mass of entries among which a cut was left out.
 template <bool DOTS>
-__device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t row, const RowGroup &G, double base, float off, float bound, float *x,
-                                   int step, float *w, int len, const unsigned short *where, int n, float tail, double *tiles, unsigned char *bytes)
+__device__ __noinline__ bool again(const Draw &P, double k2, RowCuts cuts, int wl, size_t row, const RowGroup &G, double base, float off, float bound, float *x,
+                                   int step, float *w, int len, const unsigned short *where, int n, float tail, float loose, double *tiles, unsigned char *bytes)
 {
     const double *hn = P.hn + (size_t)wl * P.mp;
     if (DOTS) {
@@ -567,17 +569,19 @@ __device__ __noinline__ bool again(const Draw &P, const Lane &L, int wl, size_t 
         // twice to four times the bound, and half as much again: sums within the bound stay in its binade
         const float magic = 1.5f * __uint_as_float((__float_as_uint(bound * 4.f) & 0x7f800000u) + 0x00800000u);
         G.sync();
-        if (P.dtype == SKB_BF16) refine_products<true>(P, L.k2, wl, hn, x, magic, base, w, len, where, n, bytes, G.t >> 5, G.nt >> 5);
-        else refine_products<false>(P, L.k2, wl, hn, x, magic, base, w, len, where, n, bytes, G.t >> 5, G.nt >> 5);
-    } else if (where) refine_list(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, where, n, G.t, G.nt);
-    else refine_differences(P, L.k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, G.t >> 5, G.nt >> 5);
+        if (P.dtype == SKB_BF16) refine_products<true>(P, k2, wl, hn, x, magic, base, w, len, where, n, bytes, G.t >> 5, G.nt >> 5);
+        else refine_products<false>(P, k2, wl, hn, x, magic, base, w, len, where, n, bytes, G.t >> 5, G.nt >> 5);
+    } else if (where) refine_list(P, k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, where, n, G.t, G.nt);
+    else refine_differences(P, k2, hn, P.yt + (size_t)wl * P.d * P.mp, x, step, base, w, G.t >> 5, G.nt >> 5);
     G.sync();
     const RowSums sums = sum_row(G, w, len);
     if (!(sums.mass <= 3e38)) return false;
-    // (a list's entries are all formed again; what is not in it is missing from the sums)
-    const RowError fine = {2.0 * (5.9604645e-8 * sums.mass + (where ? 1.02 * tail : sums.rest * off)), 2.f * 5.9604645e-8f, 0.f};
+    // (a list's entries are all formed again; what is not in it counts in the row's mass, of which a cut takes its share, and is
+    // missing from the sums that are drawn from where there is no cut)
+    RowError fine = {2.0 * (5.9604645e-8 * sums.mass + (where ? (double)tail : sums.rest) * off), 2.f * 5.9604645e-8f, 0.f};
     RowCut<float> cut;
-    if (!row_cut(w, len, G, L.cuts, sums.top, sums.mass, sums.count, fine, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
+    if (!row_cut(w, len, G, cuts, sums.top, sums.mass + (double)tail, sums.count, fine, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
+    fine.sums += 2.04 * (double)(cut.tau == 0.f ? fmaxf(tail, loose) : loose);
     return draw_all(P, row, w, len, where, cut, tiles, fine, G.t >> 5, G.nt >> 5);
 }
 
@@ -586,7 +590,7 @@ struct LaneState {
     Lane L;
     int lane;
     double h_top;
-    float k2, y_max, y_prefix;
+    float k2, p, y_max, y_prefix;
     bool some;
 };
 struct RowRoom {
@@ -608,6 +612,7 @@ __device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane
     S.lane = lane;
     S.L = lane_of(P, lane);
     S.k2 = (float)S.L.k2;
+    S.p = (float)S.L.cuts.p;
     const double *hn = P.hn + (size_t)lane * P.mp;
     double top = -CUDART_INF;
     float far = 0.f, prefix = 0.f;
@@ -677,7 +682,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
     bool sure = false;
     if (top != -CUDART_INF_F) {
         float f[3] = {0.f, 0.f, 0.f};                            // mass, sum of w log2(1 / w), mass below ROW_TAIL
-        unsigned heavy = 0, before;
+        unsigned heavy = 0, before, has = 0, bit = 1;            // has: this thread's tiles with a heavy entry (the first 32)
 #pragma unroll 4
         for (int j = span.begin; j < span.end; j += span.step) { // (each thread's own: no barrier yet)
             float v[4];
@@ -687,9 +692,10 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 const float gap = v[i] - top, down = gap < -200.f ? -200.f : gap;    // (2^-200 is zero already; a NaN stays)
                 v[i] = ex2_fast(down);
                 f[1] = fmaf(-down, v[i], f[1]);
-                if (v[i] >= ROW_TAIL) ++heavy;
+                if (v[i] >= ROW_TAIL) { ++heavy; has |= bit; }
                 else f[2] += v[i];
             }
+            bit <<= 1;
             *reinterpret_cast<float4 *>(w + j) = make_float4(v[0], v[1], v[2], v[3]);
             f[0] += (v[0] + v[1]) + (v[2] + v[3]);
         }
@@ -715,12 +721,24 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 const float unit = QUICK_ONE / mass;
                 // (roundings to units: half of one for each thread of a pass, and for each of 32 in a tile, twice)
                 QuickSlack slack = {1.02f * fixed * QUICK_ONE, (2.f * adds + slope * f[1] / mass) * QUICK_ONE + (float)(G.nt + 32 * ntiles)};
+                // Cuts among what weighs less than ROW_TAIL together make no difference that a draw could show but one inside
+                // of the bounds, to which that weight is added.
+                int k = S.L.cuts.k;
+                float r_min = S.L.cuts.r, loose = 0.f;
+                if (f[2] * 1048576.f <= mass && ((k != INT_MAX && (unsigned)k >= heavy) || (r_min > 0.f && r_min < ROW_TAIL))) {
+                    if ((unsigned)k >= heavy) k = INT_MAX;
+                    if (r_min < ROW_TAIL) r_min = 0.f;
+                    loose = f[2];
+                    slack.rest += 2.f * loose * unit;
+                }
                 const bool sparse = ntiles >= 4 && heavy <= (unsigned)mp / 4 && f[2] * 1048576.f <= mass;
                 if (sparse) {
                     // few entries weigh anything: they are the row, by one warp, the others an error of the sums
                     slack.rest += 2.f * f[2] * unit;
+                    has = (span.end - span.begin + span.step - 1) / span.step <= 32 ? __reduce_or_sync(0xffffffffu, has) : 0xffffffffu;
 #pragma unroll 1
-                    for (int j = span.begin; j < span.end; j += span.step) {
+                    for (int j = span.begin, q = 0; j < span.end; j += span.step, ++q) {
+                        if (!(has >> (q & 31) & 1u)) continue;
                         float v[4];
                         load4(w + j, v);
                         int c = 0, i0 = 0;
@@ -755,7 +773,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 if (sparse) {
 #pragma unroll 1
                     for (int j = 4 * lane; j < (int)heavy; j += ROW_TILE) own += (unsigned)min(4, (int)heavy - j);
-                } else if (S.L.cuts.k != INT_MAX || S.L.cuts.p < 1.0) {
+                } else if (k != INT_MAX || S.p < 1.f) {
 #pragma unroll 1
                     for (int j = span.begin; j < span.end; j += span.step) {
                         float v[4];
@@ -768,23 +786,29 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                     count = c[0];
                 }
                 sure = true;
+                QuickCut cut;
+                cut.tau = 0.f;
                 if (!sparse || G.t < 32) {
-                    RowCuts cuts = S.L.cuts;
-                    QuickCut cut;
-                    sure = quick_cut(r, len, A1, cuts, count, own, unit, slack, err, M.list + (sparse ? list_room(mp) : 0),
+                    sure = quick_cut(r, len, A1, k, S.p, r_min, count, own, unit, slack, err, M.list + (sparse ? list_room(mp) : 0),
                                      sparse ? 0u : (unsigned)list_room(mp), cut, turn);
-                    if (sure) {
-                        quick_tiles(r, len / ROW_TILE, A1, cut.tau, unit, units);
-                        A1.sync();
-                        const unsigned whole = quick_total(units, len / ROW_TILE);
+                    if (sure) quick_tiles(r, len / ROW_TILE, A1, cut.tau, unit, units);
+                }
+                if (sparse && G.nt > 32) {
+                    // the cut is the first warp's, the draws are everyone's
+                    if (G.t == 0) { G.sc->tie_j = __float_as_int(cut.tau); G.sc->n_cand = sure; }
+                    G.sync();
+                    cut.tau = __int_as_float(G.sc->tie_j);
+                    sure = G.sc->n_cand != 0;
+                } else A1.sync();
+                if (sure) {
+                    const unsigned whole = quick_total(units, len / ROW_TILE);
 #pragma unroll 1
-                        for (int s = A1.t >> 5; s < P.S; s += A1.nt >> 5) {
-                            const float u = s ? P.u[row * P.S + s] : u_first;
-                            int j = -1;
-                            float wj = 0.f;
-                            if (u >= 0.f && u < 1.f && !quick_draw(r, len / ROW_TILE, cut.tau, unit, units, whole, u, slack, j, wj)) { sure = false; continue; }
-                            if (lane == 0) put_draw(P, row * P.S + s, sparse && j >= 0 ? M.where[j] : j, j < 0 ? CUDART_NAN_F : logf(wj * unit / (float)whole));
-                        }
+                    for (int s = G.t >> 5; s < P.S; s += G.nt >> 5) {
+                        const float u = s ? P.u[row * P.S + s] : u_first;
+                        int j = -1;
+                        float wj = 0.f;
+                        if (u >= 0.f && u < 1.f && !quick_draw(r, len / ROW_TILE, cut.tau, unit, units, whole, u, slack, j, wj)) { sure = false; continue; }
+                        if (lane == 0) put_draw(P, row * P.S + s, sparse && j >= 0 ? M.where[j] : j, j < 0 ? CUDART_NAN_F : logf(wj * unit / (float)whole));
                     }
                 }
                 sure = group_all(G, sure, turn);
@@ -794,8 +818,8 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 } else if (!sure) {
                     // once more, with better weights for what counts
                     G.sync();
-                    sure = again<DOTS>(P, S.L, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
-                                       sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, M.tiles, M.bytes);
+                    sure = again<DOTS>(P, S.L.k2, {k, S.L.cuts.p, r_min}, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
+                                       sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, loose, M.tiles, M.bytes);
                     sure = group_all(G, sure, turn);
                 }
             }

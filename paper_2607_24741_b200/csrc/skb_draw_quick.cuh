@@ -211,14 +211,14 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
 }
 
 // Cuts the row.
-__device__ __forceinline__ bool quick_cut(const float *w, const int mp, const RowGroup &G, const RowCuts &want, const unsigned count, const unsigned own,
+__device__ __forceinline__ bool quick_cut(const float *w, const int mp, const RowGroup &G, const int k, const float p, const float smallest, const unsigned count, const unsigned own,
                                           const float unit, const QuickSlack &slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
     cut = {0.f, count, (unsigned)QUICK_ONE, own};
     // by rank, then by mass (one body: the code has to stay in the instruction cache)
 #pragma unroll 1
     for (int by_mass = 0; by_mass < 2; ++by_mass) {
-        if (by_mass ? want.p >= 1.0 || cut.count <= 1 : (unsigned)want.k >= count) continue;
+        if (by_mass ? p >= 1.f || cut.count <= 1 : (unsigned)k >= count) continue;
         if (by_mass && cut.tau > 0.f) {
             const Span all(G, mp);
 #pragma unroll 1
@@ -230,12 +230,12 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
             }
         }
         // (a target by mass is off by 64 units: fp32's last place)
-        const unsigned target = by_mass ? (unsigned)((float)want.p * (float)cut.mass) : (unsigned)want.k;
-        if (!quick_find(w, mp, G, by_mass != 0, target, unit, slack.at((float)want.p), err, list, room, cut, turn)) return false;
+        const unsigned target = by_mass ? (unsigned)(p * (float)cut.mass) : (unsigned)k;
+        if (!quick_find(w, mp, G, by_mass != 0, target, unit, slack.at(p), err, list, room, cut, turn)) return false;
     }
-    if (want.r > 0.f) {
-        const float e = err.weight - err.slope * log2f(want.r);
-        const float low = want.r * (1.f - e), high = want.r * (1.f + e);
+    if (smallest > 0.f) {
+        const float e = err.weight - err.slope * log2f(smallest);
+        const float low = smallest * (1.f - e), high = smallest * (1.f + e);
         unsigned near_[1] = {0};
         const Span all(G, mp);
 #pragma unroll 2
@@ -247,8 +247,8 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
         }
         // (a smallest share of 1 keeps the largest weight, which is 1 itself)
         group_add(G, near_, turn);
-        if (near_[0] != (want.r == 1.f ? 1u : 0u)) return false;
-        cut.tau = fmaxf(cut.tau, want.r);
+        if (near_[0] != (smallest == 1.f ? 1u : 0u)) return false;
+        cut.tau = fmaxf(cut.tau, smallest);
     }
     return true;
 }

@@ -100,7 +100,7 @@ def clouds(seed, W, n, m, d, dtype="f32", spread=1.0):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", [(1, 1, 1, 1), (3, 5, 1, 2), (2, 9, 2, 3), (8, 64, 64, 2), (4, 33, 100, 3), (3, 40, 129, 5), (2, 50, 512, 15), (5, 17, 1000, 8),
-                                   (1, 12, 5000, 3), (1, 5, 20000, 2), (2, 30, 77, 33), (1, 20, 130, 200), (1, 9, 60, 1024)])
+                                   (1, 12, 5000, 3), (1, 5, 20000, 2), (1, 4, 30000, 3), (2, 30, 77, 33), (1, 20, 130, 200), (1, 9, 60, 1024)])
 @pytest.mark.parametrize("cut", ["none", "k", "p", "r", "all"])
 def test_draws_of_every_shape_and_cut(B, shape, cut):
     W, n, m, d = shape
@@ -215,6 +215,25 @@ def test_near_ties_and_borders_are_those_of_float64(B):
     check(B, x, y, g, eps, u, T=np.zeros(W))
     check(B, x, y, g, eps, u, p=np.array([0.1, 0.5, 2 / 3, 0.99]))
     check(B, x, y, g, eps, u, r=np.array([1.0, 1 - 1e-7, 0.999, 1.0]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [100, 700, 3500, 9000])
+def test_cuts_far_below_the_heavy_entries(B, m):
+    # few entries carry the mass; ranks, shares and sizes that cut among those that weigh 2^-20 to 2^-200 of them
+    import torch
+    W, n, d = 4, 10, 3
+    rng = np.random.default_rng(m)
+    x, y = torch.from_numpy(0.05 * rng.standard_normal((W, n, d)).astype(np.float32)), torch.from_numpy(rng.standard_normal((W, m, d)).astype(np.float32))
+    y[:, ::50] *= 0.05
+    g, eps = np.zeros((W, m)), np.array([0.2, 0.05, 0.02, 0.01])
+    u = rng.random((W, n, 3), np.float32)
+    u[:, :, 0] = 1 - 2.0 ** -24                                  # the far end of the row
+    u[:, :, 1] = 0.0
+    check(B, x, y, g, eps, u, k=np.array([m // 2, m // 10 + 3, m - 1, m // 3]))
+    check(B, x, y, g, eps, u, p=np.array([0.9999999, 0.999999, 0.99999994, 0.9999]))
+    check(B, x, y, g, eps, u, r=np.array([1e-9, 1e-7, 1e-12, 1e-30]))
+    check(B, x, y, g, eps, u, k=np.full(W, m // 4), p=np.full(W, 0.999999), r=np.full(W, 1e-8))
 
 
 @pytest.mark.gpu
