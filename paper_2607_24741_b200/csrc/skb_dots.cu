@@ -255,7 +255,9 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             for (int c0 = half * (DT_BN / 2); c0 < (half + 1) * (DT_BN / 2); c0 += 32) {
-                if (j0 + c0 >= P.mo) break;
+                // (a box that is written is stored: the wait below counts stores, and one that were left out would let the next
+                // box but one be written while it is read)
+                if (j0 + c0 >= P.mo || i0 + quarter * 32 >= P.no) break;
                 uint32_t r[32];
                 if (ok) {
                     tc_ld32_issue(tmem + (uint32_t)(quarter << 21) + b * DT_BN + c0, r);
@@ -284,7 +286,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 if (P.tma_out) {
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0 && i0 + quarter * 32 < P.no) tma_store_box(&tmo, box0 + turn * DT_BOX, j0 + c0, i0 + quarter * 32, w);
+                    if (lane == 0) tma_store_box(&tmo, box0 + turn * DT_BOX, j0 + c0, i0 + quarter * 32, w);
                 } else {
                     __syncwarp();
                     const int rows = min(32, P.no - (i0 + quarter * 32));

@@ -348,3 +348,45 @@ def test_refusals_of_products(B):
     assert L.sinkhorn_cloud4_dots(one, one, 1, 4, 4, 8, 2, ctypes.c_void_p(4098), None) == 4
     with pytest.raises(ValueError):
         B.cloud4_dots(None, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+@pytest.mark.parametrize("n", [33, 129, 150, 200, 230, 1000])
+def test_last_rows_of_few_and_many_tiles(B, fmt, n):
+    # tiles of which some warps have no rows, next to whole ones, many to a block: results are stored before their room is
+    # written again.  Values are multiples of 1/4 and sums small: products are exact, and compared as a whole
+    import torch
+    gen = torch.Generator().manual_seed(n)
+    W, m, d = 3, 20000, 64
+    grid = torch.tensor(list(GRID) + list(-GRID), dtype=torch.float32)
+    x, y = grid[torch.randint(16, (W, n, d), generator=gen)], grid[torch.randint(16, (W, m, d), generator=gen)]
+    x[:, :, ::16] = 6.0
+    y[:, :, ::16] = 6.0
+    x4, y4 = B.cloud4_pack(x.cuda(), fmt), B.cloud4_pack(y.cuda(), fmt)
+    want = (x4.values().double() @ y4.values().double().transpose(1, 2)).float()
+    for _ in range(6):
+        out = torch.full((W, n, m), float("nan"), device="cuda")
+        B.cloud4_dots(x4, y4, out=out)
+        assert torch.equal(out, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["mx4", "nv4"])
+def test_offsets_past_32_bits(B, fmt):
+    # 2.3e9 values, and 2.2e9 products; the last points alone give the same
+    import torch
+    x = torch.zeros(9, 250000, 1024, dtype=torch.bfloat16, device="cuda")
+    x[8, -300:] = torch.randn(300, 1024, generator=torch.Generator().manual_seed(1)).cuda().bfloat16()
+    big, values = B.cloud4_pack(x, fmt, values=torch.bfloat16)
+    want = B.cloud4_pack(x[8:, -300:], fmt)
+    assert torch.equal(values[8:, -300:], want.values(torch.bfloat16)) and not bool(values[:8].any())
+    del values
+    assert torch.equal(big.values(torch.bfloat16)[8:, -300:], want.values(torch.bfloat16))
+    del big, x
+    gen = torch.Generator().manual_seed(2)
+    a, b = torch.randn(2, 33000, 64, generator=gen).cuda(), torch.randn(2, 33000, 64, generator=gen).cuda()
+    out = B.cloud4_dots(B.cloud4_pack(a, fmt), B.cloud4_pack(b, fmt))
+    part = B.cloud4_dots(B.cloud4_pack(a[1:, -200:], fmt), B.cloud4_pack(b[1:], fmt))
+    assert torch.equal(out[1:, -200:], part)
+    assert torch.equal(out[:1, 31000:31100], B.cloud4_dots(B.cloud4_pack(a[:1, 31000:31100], fmt), B.cloud4_pack(b[:1], fmt)))

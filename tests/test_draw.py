@@ -295,3 +295,34 @@ def test_refusals_of_draws(B):
     assert call(cfg(), x=ctypes.c_void_p(4096 + 4)) == 3 and call(cfg(dt=2), y=ctypes.c_void_p(4096 + 64)) == 3
     with pytest.raises(ValueError):
         B.plan_draw(torch.zeros(1, 4, 2), torch.zeros(1, 4, 2), None, None, None)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 20, 150, 65), (2, 30, 300, 100), (1, 25, 700, 333), (1, 10, 40, 1023)])
+def test_draws_of_deep_bf16_clouds_of_any_depth(B, shape):
+    # rows that are no multiple of 16 bytes
+    W, n, m, d = shape
+    x, y, g, rng = clouds(5 + sum(shape), *shape, dtype="bf16", spread=1.0 / math.sqrt(d))
+    eps, u = rng.uniform(0.03, 0.2, W), rng.random((W, n, 2), np.float32)
+    check(B, x, y, g, eps, u)
+    check(B, x, y, g, eps, u, k=np.full(W, 12), p=np.full(W, 0.9), r=np.full(W, 0.01))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [None, "nv4"])
+@pytest.mark.parametrize("shape", [(5, 5000, 6000, 64), (2, 14000, 12000, 64)])      # several lanes at a time, several rows of a lane
+def test_lanes_and_rows_of_large_problems_are_those_of_small_ones(B, fmt, shape):
+    import torch
+    W, n, m, d = shape
+    x, y, g, rng = clouds(9, W, n, m, d, dtype="bf16", spread=1.0 / math.sqrt(d))
+    x, y, g = x.cuda(), y.cuda(), torch.as_tensor(g).cuda()
+    g[:, m - 5:] = -math.inf
+    eps, p = torch.full((W,), 0.1).cuda(), torch.full((W,), 0.9).cuda()
+    u = torch.rand(W, n, generator=torch.Generator().manual_seed(4)).cuda()
+    cloud = (lambda v: v) if fmt is None else (lambda v: B.cloud4_pack(v, fmt))
+    whole = B.plan_draw(cloud(x), cloud(y), g, eps, u, top_p=p)
+    assert bool((whole >= 0).all()) and bool((whole < m - 5).all())
+    for t in range(W):
+        for rows in (slice(0, 40), slice(n // 2, n // 2 + 300), slice(n - 70, n)):
+            part = B.plan_draw(cloud(x[t:t + 1, rows]), cloud(y[t:t + 1]), g[t:t + 1], eps[:1], u[t:t + 1, rows], top_p=p[:1])
+            assert torch.equal(part[0], whole[t, rows])
