@@ -20,8 +20,8 @@
 // What bounds it: instructions of the searches and draws, not the exponentials.  256 lanes of 512 x 512, d = 15, top-p (131072
 // rows, 67 M pairs): 0.67 ms, some 2900 instructions of a warp a row, of which forming and exponentials are a fifth (15 us at
 // the rate of the exponentials); issue slots are used to 54 % and neither 16 nor 32 warps an SM instead of 24 change the time.
-// 2 lanes of 8192 x 8192, d = 3, top-k 16, four draws: 0.60 ms, a list of some 50 entries a row, latencies of one warp's search between
-// the block's barriers.  64 lanes of 1024 x 1024, d = 512 (bf16), top-p: 0.74 ms, of which products 0.12, rows 0.30, rows
+// 2 lanes of 8192 x 8192, d = 3, top-k 16, four draws: 0.77 ms, a list of some 50 entries a row, latencies of one warp's search between
+// the block's barriers, 0.15 of it log probabilities of large exponents.  64 lanes of 1024 x 1024, d = 512 (bf16), top-p: 0.74 ms, of which products 0.12, rows 0.30, rows
 // formed again 0.15 (2.8 % of them), norms 0.04, float64 0.09 (22 rows, a cold kernel's latency).
 #include <cuda_runtime.h>
 #include <math_constants.h>
@@ -41,6 +41,11 @@ constexpr int DRAW_BLOCKS = 148;                     // SMs; the fp32 kernel has
 constexpr int DRAW_EXACT_BLOCKS = 148;               // rows of scratch in the workspace
 constexpr float ROW_FLOOR = 2.384185791015625e-7f;   // 2^-22: weights that are formed again where fp32 does not do
 constexpr float ROW_TAIL = 5.9604645e-8f;            // 2^-24: weights that a row of few heavy entries does without
+// Rows whose largest exponent is at least this: fp32's last place of exponents shows in log probabilities, which are formed from the points
+// in double where they are wanted.  Their error (rms over rms), 96 lanes of 100 x 77, d = 8, eps from 0.01: 1e-5 without, 4e-7 from
+// 48 on (11 us more), 1e-7 from 16 on.  2 lanes of 8192 x 8192, d = 3: 613 us and 8e-7 without, 768 us and 4e-8 so.  From 16 on
+// rows of exponents of some tens take part, too: 256 lanes of 512 x 512, d = 15, threefold the time, for 2e-7 without.
+constexpr float DRAW_FAR = 48.f;
 // Products that are held at a time.  64 lanes of 1024 x 1024 x 512: 843 us by 64 MB, which stay in the L2 cache, 780 by 128 MB,
 // 743 all at once: the rows that are formed again are then one launch, too.
 constexpr size_t DRAW_DOTS_BYTES = (size_t)512 << 20;
@@ -508,6 +513,47 @@ __device__ __forceinline__ void refine_list(const Draw &P, double k2, const doub
     }
 }
 
+// log2 of an entry's weight where the row's largest has 2^base, from its points in double.
+__device__ __forceinline__ float exact_gap(const Draw &P, double k2, int wl, const float *nx, int step, double base, int j)
+{
+    const float *yt = P.yt + (size_t)wl * P.d * P.mp + j;
+    const double h = P.hn[(size_t)wl * P.mp + j];
+    double c = 0.0;
+#pragma unroll 4
+    for (int k = 0; k < P.d; ++k) {
+        const double e = (double)yt[(size_t)k * P.mp] + (double)nx[k * step];
+        c = fma(e, e, c);
+    }
+    return (float)(fma(-k2, c, h) - base);
+}
+// Log probabilities of a row's draws once more, entries above ROW_FLOOR from their points; w: weights, kept from tau on.  The
+// group's last threads have the draws, so that in a group of several warps they need not wait for the sum.
+__device__ __forceinline__ void exact_logs(const Draw &P, double k2, int wl, size_t row, const RowGroup &G, double base, const float *nx, int step, const float *w,
+                                           int len, const unsigned short *where, float tau)
+{
+    const int first = G.nt - 1 - G.t;
+    double mass = 0.0;
+    float gap = 0.f;
+    int j = first < P.S ? P.index[row * P.S + first] : -1, unused = 0;
+    if (j >= 0) gap = exact_gap(P, k2, wl, nx, step, base, j);
+#pragma unroll 1
+    for (int q = G.t; q < len; q += G.nt) {
+        float v = w[q];
+        if (!quick_kept(v, tau)) continue;
+        if (v > ROW_FLOOR) v = ex2_fast(exact_gap(P, k2, wl, nx, step, base, where ? where[q] : q));
+        mass += (double)v;
+    }
+    G.add(mass, unused);
+    const float whole = log2f((float)mass);
+#pragma unroll 1
+    for (int s = first; s < P.S;) {
+        if (j >= 0) P.logp[row * P.S + s] = 0.69314718f * (gap - whole);
+        if ((s += G.nt) >= P.S) break;
+        j = P.index[row * P.S + s];
+        if (j >= 0) gap = exact_gap(P, k2, wl, nx, step, base, j);
+    }
+}
+
 // Sums over the group of three floats and a count, in one order; `before`: of the count over the warps before this one.
 __device__ __forceinline__ void group_sums(const RowGroup &G, float (&f)[3], unsigned &n, unsigned &before, int &turn)
 {
@@ -564,12 +610,17 @@ __device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
 
 // A row once more: what weighs more than ROW_FLOOR to fp32's last place, what does not is `off` of itself off.  x: -x, `step`
 // apart (differences), or room for a row (products), whose bound is `bound`.  A row that is a list of n entries, columns
-// `where`, has a mass `tail` besides; `loose` is the mass of entries among which a cut was left out.
+// `where`, has a mass `tail` besides; `loose` is the mass of entries among which a cut was left out.  A row of which only the
+// logarithms are to be formed again has its cut in `tau`, the others a negative one.
 template <bool DOTS>
 __device__ __noinline__ bool again(const Draw &P, double k2, RowCuts cuts, int wl, size_t row, const RowGroup &G, double base, float off, float bound, float *x,
-                                   int step, float *w, int len, const unsigned short *where, int n, float tail, float loose, double *tiles, unsigned char *bytes)
+                                   int step, float *w, int len, const unsigned short *where, int n, float tail, float loose, double *tiles, unsigned char *bytes, float tau)
 {
     const double *hn = P.hn + (size_t)wl * P.mp;
+    if (!DOTS && tau >= 0.f) {
+        exact_logs(P, k2, wl, row, G, base, x, step, w, len, where, tau);
+        return true;
+    }
     if (DOTS) {
         const int xd = dots_xd(P.d);
 #pragma unroll 1
@@ -823,11 +874,11 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 if (!sure && DOTS && LATER) {
                     if (G.t == 0) P.later[atomicAdd(P.later_n, 1u)] = (long long)row;
                     sure = true;
-                } else if (!sure) {
+                } else if (!sure || (!DOTS && P.logp && A > DRAW_FAR)) {
                     // once more, with better weights for what counts
                     G.sync();
                     sure = again<DOTS>(P, S.L.k2, {k, S.L.cuts.p, r_min}, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
-                                       sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, loose, M.tiles, M.bytes);
+                                       sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, loose, M.tiles, M.bytes, sure ? cut.tau : -1.f);
                     sure = group_all(G, sure, turn);
                 }
             }

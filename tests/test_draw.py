@@ -326,3 +326,29 @@ def test_lanes_and_rows_of_large_problems_are_those_of_small_ones(B, fmt, shape)
         for rows in (slice(0, 40), slice(n // 2, n // 2 + 300), slice(n - 70, n)):
             part = B.plan_draw(cloud(x[t:t + 1, rows]), cloud(y[t:t + 1]), g[t:t + 1], eps[:1], u[t:t + 1, rows], top_p=p[:1])
             assert torch.equal(part[0], whole[t, rows])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(6, 40, 77, 8), (3, 30, 900, 3), (2, 20, 6000, 4)])      # rows to a warp, to a block; flat rows and lists
+def test_log_probabilities_of_large_exponents(B, shape):
+    # Exponents of hundreds and thousands.  Weights are formed to 2^-24 of at most 22 (times ln 2) and 2^-22 each, what weighs less than
+    # 2^-22 may be 1 % off (m 2^-22 / 100 of the sum) or, up to 2^-20 of the sum, missing; the drawn one's difference rounds to
+    # 2^-24 of itself.  Where the row's largest exponent is below 16 those within 22 of it are off by (d + 6) 2^-24 of 38, the
+    # drawn one's and those of the sum.
+    import torch
+    W, n, m, d = shape
+    x, y, g, rng = clouds(31, W, n, m, d)
+    eps = np.exp(rng.uniform(np.log(0.003), np.log(0.5), W))
+    u = rng.random((W, n, 3), np.float32)
+    bound = 22 * 2.0 ** -24 * 0.6932 + 2.0 ** -22 + m * 2.0 ** -22 / 100 + 2.0 ** -20 + 2 * 0.6932 * (d + 6) * 2.0 ** -24 * 38 + 2.0 ** -23
+    for kw in ({}, dict(k=np.full(W, 9), p=np.full(W, 0.9)), dict(r=np.full(W, 0.05)), dict(T=np.full(W, 0.3), p=np.full(W, 0.8))):
+        f = lambda v, dt: torch.as_tensor(v).to(dt).cuda()
+        args = dict(top_k=f(kw["k"], torch.int32) if "k" in kw else None, top_p=f(kw["p"], torch.float32) if "p" in kw else None,
+                    min_p=f(kw["r"], torch.float32) if "r" in kw else None, temperature=f(kw["T"], torch.float32) if "T" in kw else None)
+        idx, lp = B.plan_draw(x.cuda(), y.cuda(), f(g, torch.float64), f(eps, torch.float32), f(u, torch.float32), logp=True, **args)
+        cut = {key: np.asarray(v, np.float32) if key != "k" else v for key, v in kw.items()}
+        want, wlp = reference(x.double().numpy(), y.double().numpy(), g, eps.astype(np.float32), u.astype(np.float64),
+                              cut.get("T"), cut.get("k"), cut.get("p"), cut.get("r"))
+        np.testing.assert_array_equal(idx.cpu().numpy(), want)
+        off = np.abs(lp.cpu().numpy() - wlp)
+        assert (off <= bound + 2.0 ** -23 * np.abs(wlp)).all(), off.max()
