@@ -509,18 +509,19 @@ class SinkhornBatch:
 
     def draw_plan(self, u, *, side="sources", temperature=None, top_k=None, top_p=None, min_p=None, logp=False):
         """Partners of the sources (u [W, n] or [W, n, draws]) or of the targets (side "targets", u [W, m] or [W, m, draws])
-        drawn from the plan of the finished lanes; settings and outputs as those of plan_draw."""
+        drawn from the plan of the finished lanes; settings and outputs as those of plan_draw.  Runs on the batch's stream."""
         if side not in ("sources", "targets"):
             raise ValueError('side must be "sources" or "targets"')
         x, y, _a, _b, eps = self._keep[:5]
-        if self.format is None:
-            x, y = (v if v.data_ptr() % 16 == 0 else v.clone() for v in (x, y))
         other = side == "targets"
         n, m = (self.m, self.n) if other else (self.n, self.m)
-        u = u.contiguous()
         if u.device != self.device:
             raise ValueError("u must be on the batch's device")
         with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
+            # (copies, where they are needed, are made on the stream that reads them)
+            u = u.contiguous()
+            if self.format is None:
+                x, y = (v if v.data_ptr() % 16 == 0 else v.clone() for v in (x, y))
             cfg = _draw_config(self.W, n, m, self.d, self.cfg.xy_dtype, u,
                                dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p), self.stream.cuda_stream)
             index, lp, ws = _draw_out(cfg, u, logp)

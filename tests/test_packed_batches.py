@@ -177,3 +177,29 @@ def test_refusals_of_packed_batches_and_their_draws(B):
     assert B.lib.sinkhorn_batch_create(one, one, one, one, one, 1e-3, ctypes.byref(ok), ctypes.byref(h)) == 4
     cfg = B.SkbDrawConfig(1, 4, 4, 2, 0, 1)
     assert B.lib.sinkhorn_batch_draw_plan(None, one, one, one, one, 0, ctypes.byref(cfg), one, None) == 1
+
+
+@pytest.mark.gpu
+def test_draws_from_a_batch_on_a_stream_of_its_own(B):
+    # strided numbers and unaligned points are copied on the batch's stream, not behind what the current one is busy with
+    import torch
+    W, n, m, d = 2, 40, 50, 3
+    x, y, a, b, eps = problem(12, W, n, m, d)
+    room = torch.empty(W * n * d + 1, device="cuda")
+    x = room[1:].copy_(x.reshape(-1)).view(W, n, d)
+    u = torch.rand(4, n, W, generator=torch.Generator().manual_seed(5)).cuda().permute(2, 1, 0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    sb = B.SinkhornBatch(x, y, a, b, eps, 1e-3, stream=side)
+    sb.drain()
+    f, g = sb.potentials(f64=True)
+    side.synchronize()
+    want = B.plan_draw(x, y, g, eps, u)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(100_000_000)                               # some 50 ms
+    got = sb.draw_plan(u)
+    side.synchronize()
+    with torch.cuda.stream(side):
+        assert torch.equal(got, want)
+    torch.cuda.synchronize()
+    sb.close()
