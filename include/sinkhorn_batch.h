@@ -464,7 +464,7 @@ skb_status sinkhorn_cloud4_dots(const void *x, const void *y, int W, int n, int 
  *   logp  [W, n, draws]  fp32, may be null: log(w_ij / sum of the kept weights)
  *                        (rounded to fp32; besides, exponents z_ij below 48 are good to (d + 6) 2^-24 of themselves, larger ones to
  *                        fp32's last place of their distance from the row's largest; those from products, bf16 and 4-bit clouds
- *                        of d >= 64, to about 2^-23 of k |x_i| |y_j|)
+ *                        of d >= 64, to at most 40 2^-23 of 2 |x_i| |y_j| / (eps T), as a rule a tenth of that)
  * Indices are those of float64 arithmetic (rows that fp32 cannot decide are decided again).  -1, and NaN for logp: a
  * row without targets, with a NaN or an infinite exponent; a u outside [0, 1); every row of a lane whose settings or eps are not valid.
  *   x [W, n, d], y [W, m, d]  of cfg->xy_dtype (4-bit clouds: the values they stand for), 16-byte aligned, 4-bit clouds 256

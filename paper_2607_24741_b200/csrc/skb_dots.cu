@@ -17,7 +17,11 @@
 // pairs of tiles with their rows kept 61, this 56; a fill of the same results 39).  Four warps for the results instead
 // of eight: 73 us for 4 lanes of 4096 x 4096 x 512 in nv4, 68 so.
 // In nv4 the points' powers of two multiply the results on their way out, which is exact.
-// Accumulation is the matrix unit's fp32.  Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and
+// Accumulation is the matrix unit's fp32, which cuts off: measured with sums made for it, every product of an instruction (4-bit kinds: every
+// block of a common scale) and the sum so far are cut at 2^-25 of the power of two of the largest of them, and the result to its 24
+// bits.  Beside a sum that is there from the start 512 dimensions of bf16 can lose 127 units in its last place that way.  Draws
+// have to know their products' errors, and larger ones leave more rows to be formed again: bf16 products are summed 64 dimensions at a time, and
+// these sums added by the warps for the results, in fp32's rounding.  Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and
 // the tiles that were not finished are NaN.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -34,6 +38,8 @@ constexpr int DT_BM = 128, DT_BN = 128;
 constexpr int DT_EPI = 8, DT_THREADS = (6 + DT_EPI) * 32, DT_STAGES = 4;
 constexpr uint32_t DT_TILE = 128 * 128;                  // bytes: 128 points, 128 bytes of each
 constexpr uint32_t DT_BOX = 32 * 32 * 4;                 // a box of results
+// chunks of an accumulator (4-bit kinds have at most four)
+template <int KIND> constexpr int DT_PART = KIND == SKB_BF16 ? DOTS_BF16_PART / 64 : 4;
 constexpr int DT_SF_COL = 2 * DT_BN, DT_SF_STRIDE = 32;  // tensor memory: accumulators, then the scales of each stage
 
 struct Dots {
@@ -161,10 +167,13 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             int s = 0, ph = 0, b = 0, bph = 1;
             bool ok = true;
             for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-                if (!(ok = mbar_wait(bar(ACC_FREE + b), bph, &abort_flag))) break;
-                tc_fence_after();
-                const uint32_t acc = tmem + b * DT_BN;
                 for (int c = 0; c < chunks; ++c) {
+                    const bool starts = c % DT_PART<KIND> == 0, ends = (c + 1) % DT_PART<KIND> == 0 || c + 1 == chunks;
+                    if (starts) {
+                        if (!(ok = mbar_wait(bar(ACC_FREE + b), bph, &abort_flag))) break;
+                        tc_fence_after();
+                    }
+                    const uint32_t acc = tmem + b * DT_BN;
                     if (!(ok = mbar_wait(bar(FULL + s), ph, &abort_flag))) break;
                     const uint32_t sf = tmem + DT_SF_COL + s * DT_SF_STRIDE;
                     if constexpr (SCALED) {
@@ -184,15 +193,16 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                         const int word = KIND == SKB_NV4 ? q : q / 2;
                         const uint32_t half = KIND == SKB_MX4 ? (uint32_t)(q & 1) * 2u : 0u;     // which two of a word's four scales
                         dots_mma<KIND>(acc, da + 2 * q, db + 2 * q, dots_idesc<KIND>() | half << 29 | half << 4, sf + 4 * word, sf + 16 + 4 * word,
-                                       (c | q) != 0);
+                                       !starts || q != 0);
                     }
                     tc_commit(bar(EMPTY + s));
                     if (++s == DT_STAGES) { s = 0; ph ^= 1; }
+                    if (ends) {
+                        tc_commit(bar(ACC + b));
+                        b ^= 1;
+                        if (b == 0) bph ^= 1;
+                    }
                 }
-                if (!ok) break;
-                tc_commit(bar(ACC + b));
-                b ^= 1;
-                if (b == 0) bph ^= 1;
             }
             // what was issued is over before tensor memory is given back
             tc_commit(bar(LAST));
@@ -238,7 +248,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
         const int quarter = warp & 3, half = (warp - 6) >> 2, e = (warp - 6) * 32 + lane;
         const uint32_t box0 = boxes + (uint32_t)(warp - 6) * 2 * DT_BOX;
         unsigned char *gbox0 = gen + (box0 - base);
-        int b = 0, ph = 0, turn = 0;
+        int b = 0, ph = 0, turn = 0, even = 0;
         bool ok = true;
         for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
             int w, i0, j0;
@@ -247,29 +257,73 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             float rp = 1.f;
             if constexpr (KIND == SKB_NV4) {
                 // (the buffer of two tiles ago: its readers have passed the barrier of the last tile)
-                if (e < DT_BN) col_points[b][e] = j0 + e < P.m ? P.py[(size_t)w * P.m + j0 + e] : 0.f;
+                if (e < DT_BN) col_points[even][e] = j0 + e < P.m ? P.py[(size_t)w * P.m + j0 + e] : 0.f;
                 rp = row < P.n ? P.px[(size_t)w * P.n + row] : 0.f;
                 asm volatile("bar.sync 1, %0;" ::"n"(DT_EPI * 32) : "memory");
             }
-            ok = ok && mbar_wait(bar(ACC + b), ph, &abort_flag);
-            ok = __all_sync(0xffffffffu, ok);
-            tc_fence_after();
-            for (int c0 = half * (DT_BN / 2); c0 < (half + 1) * (DT_BN / 2); c0 += 32) {
+            const int c_first = half * (DT_BN / 2);
+            // (an accumulator that is written again goes back when it has been read)
+            auto wait_acc = [&] {
+                ok = ok && mbar_wait(bar(ACC + b), ph, &abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+                return tmem + (uint32_t)(quarter << 21) + b * DT_BN + c_first;
+            };
+            auto free_acc = [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(ACC_FREE + b));
+                b ^= 1;
+                if (b == 0) ph ^= 1;
+            };
+            uint32_t held[SCALED ? 1 : 2][32], src = 0;
+            if constexpr (SCALED) src = wait_acc();
+            else {
+                // sums of the parts, added; the 64 columns stay in registers (4-bit kinds, whose products are one part, are faster by
+                // boxes: 64 lanes of 1024 x 1024 x 512 56 us so, 75 this way)
+                for (int c = 0; c < chunks; c += DT_PART<KIND>) {
+                    src = wait_acc();
+                    if (!ok) {
+#pragma unroll
+                        for (int q = 0; q < 64; ++q) held[q / 32][q % 32] = 0x7fffffffu;
+                    } else if (c == 0) {
+                        tc_ld32_issue(src, held[0]);
+                        tc_ld32_issue(src + 32, held[1]);
+                        tc_ld_wait(held[0]);
+                        tc_ld_wait(held[1]);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            uint32_t v[32];
+                            tc_ld32_issue(src + 32 * h, v);
+                            tc_ld_wait(v);
+#pragma unroll
+                            for (int q = 0; q < 32; ++q) held[h][q] = __float_as_uint(__uint_as_float(held[h][q]) + __uint_as_float(v[q]));
+                        }
+                    }
+                    free_acc();
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c0 = c_first + 32 * h;
                 // (a box that is written is stored: the wait below counts stores, and one that were left out would let the next
                 // box but one be written while it is read)
                 if (j0 + c0 >= P.mo || i0 + quarter * 32 >= P.no) break;
-                uint32_t r[32];
-                if (ok) {
-                    tc_ld32_issue(tmem + (uint32_t)(quarter << 21) + b * DT_BN + c0, r);
-                    tc_ld_wait(r);
-                } else {
+                uint32_t (&r)[32] = held[SCALED ? 0 : h];
+                if constexpr (SCALED) {
+                    if (ok) {
+                        tc_ld32_issue(src + 32 * h, r);
+                        tc_ld_wait(r);
+                    } else {
 #pragma unroll
-                    for (int q = 0; q < 32; ++q) r[q] = 0x7fffffffu;
+                        for (int q = 0; q < 32; ++q) r[q] = 0x7fffffffu;
+                    }
                 }
                 if constexpr (KIND == SKB_NV4) {
 #pragma unroll
                     for (int q = 0; q < 32; q += 4) {
-                        const float4 p = *reinterpret_cast<const float4 *>(&col_points[b][c0 + q]);
+                        const float4 p = *reinterpret_cast<const float4 *>(&col_points[even][c0 + q]);
                         r[q] = __float_as_uint(__uint_as_float(r[q]) * rp * p.x);
                         r[q + 1] = __float_as_uint(__uint_as_float(r[q + 1]) * rp * p.y);
                         r[q + 2] = __float_as_uint(__uint_as_float(r[q + 2]) * rp * p.z);
@@ -298,11 +352,8 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 }
                 turn ^= 1;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(ACC_FREE + b));
-            b ^= 1;
-            if (b == 0) ph ^= 1;
+            if constexpr (SCALED) free_acc();
+            even ^= 1;
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }

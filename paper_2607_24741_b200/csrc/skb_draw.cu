@@ -164,7 +164,8 @@ __device__ __forceinline__ void eight_values(const Eight &e, const Cloud4 &c, fl
     }
 }
 __host__ __device__ inline int dots_xd(int d) { return (d + 31) / 32 * 32; }
-// |point|^2 in float64, by one warp; prefix: the mean of the squared norms of its first 16, 32, ... dimensions.
+// |point|^2 in float64, by one warp; prefix: the mean, over steps of 16 dimensions, of the squared norm of what the
+// accumulator has seen of the point by then (bf16: accumulators begin anew every DOTS_BF16_PART dimensions).
 template <bool BF>
 __device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, size_t row, int d, double &prefix)
 {
@@ -182,7 +183,8 @@ __device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, s
             s += (double)a;
             f += a;
         }
-        p = fmaf(f, (float)max(steps - q / 2, 1), p);
+        const int until = BF ? min(steps, (8 * q / DOTS_BF16_PART + 1) * (DOTS_BF16_PART / 16)) : steps;
+        p = fmaf(f, (float)max(until - q / 2, 1), p);
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
@@ -365,10 +367,12 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const __grid_constant__
 // Error of an exponent t = log2 w at a depth q below the row's largest, A = |largest t|:
 //   differences  h <= 0 and the scaled distance h - t are at most A + q; d + 2 roundings of the distance, three of the
 //                scale and t, one of h: (d + 6) (A + q) 2^-24
-//   products     2 k |x . y| is at most B = 2 k |x| max |y|, and after each 16 dimensions at most the same of those
-//                prefixes, on average no more than B' (from the root mean squares of the prefixes' norms).  The matrix unit
-//                cuts off where it adds products to a sum: a unit in the last place of the sum, at most 2^-23 of it, for each 16, and
-//                two more: (d / 16) B' 2^-23 + 2 B 2^-23; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
+//   products     2 k |x . y| is at most B = 2 k |x| max |y|, and what an accumulator has seen of it after each 16 dimensions at most the
+//                same of those dimensions, on average no more than B' (from the root mean squares of their norms).  The matrix unit
+//                cuts off (skb_dots.cu): bf16, for 16 dimensions, 16 products and the sum so far at 2^-25 of the largest and the
+//                result to 24 bits, 17 / 4 + 1 units of 2^-23 of that; 4-bit kinds, for 64 dimensions, four blocks of a scale
+//                and the sum, 5 / 4 + 1 units, counted as 4.  (d / 16) (5.25 or 1) B' 2^-23, the additions of bf16's parts
+//                B 2^-24 each, two units 2 B 2^-23 to spare; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
 // The exponential adds 2^-22 and 2^-24 q of the difference that it is taken of, the additions of weights 2^-24 each.
 // Mass, number and largest of a row's weights, and the mass of those at most ROW_FLOOR.
 struct RowSums {
@@ -767,7 +771,9 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
             if (DOTS) {
                 bound = sqrtf(xn.x) * S.y_max;
                 slope = 3.f * u24;
-                fixed = u24 * (2.f * k2 * (2.f * (float)((P.d + 15) / 16) * sqrtf(xn.y) * S.y_prefix + 7.f * bound) + 3.f * A);
+                const float steps = (float)((P.d + 15) / 16), cut_off = P.dtype == SKB_BF16 ? 10.5f : 2.f,
+                            joins = P.dtype == SKB_BF16 ? (float)((P.d - 1) / DOTS_BF16_PART) : 0.f;
+                fixed = u24 * (2.f * k2 * (cut_off * steps * sqrtf(xn.y) * S.y_prefix + (7.f + joins) * bound) + 3.f * A);
             } else {
                 slope = (float)(P.d + 6) * u24;
                 fixed = slope * A;

@@ -21,6 +21,8 @@ struct DotsCloud {
 DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t row);
 // x_i . y_j of W lanes of n and m points (bf16: d a multiple of 8, rows 16-byte aligned), rows of ldo >= m floats.  A lane has
 // n rows, or n_out >= n of m_out >= m columns, those past the points zero.
+// bf16: sums of DOTS_BF16_PART dimensions by the matrix unit, added in fp32.
+constexpr int DOTS_BF16_PART = 64;
 skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st,
                        int n_out = 0, int m_out = 0);
 

@@ -352,3 +352,26 @@ def test_log_probabilities_of_large_exponents(B, shape):
         np.testing.assert_array_equal(idx.cpu().numpy(), want)
         off = np.abs(lp.cpu().numpy() - wlp)
         assert (off <= bound + 2.0 ** -23 * np.abs(wlp)).all(), off.max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 256, 512, 1024])
+@pytest.mark.parametrize("fmt", [None, "mx4", "nv4"])
+def test_products_that_the_matrix_unit_cuts_off_one_by_one(B, d, fmt):
+    # One dimension carries a product of 1, each of the others one of just below 2^-25 (or a little more): beside the large sum
+    # they are cut off one by one, which is far more than a unit in the last place of the sum for 16 dimensions.  Half of
+    # the targets have only the first dimension.  Numbers around the border between the two halves' shares.
+    import torch
+    W, n, m = 8, 800, 4
+    x, y = torch.zeros(W, n, d), torch.zeros(W, m, d)
+    for t in range(W):
+        size = (1.9921875 if fmt is None else 1.5) * 2.0 ** -(11 + t / 2 if fmt is None else 11 + t // 2)
+        x[t], y[t, ::2] = size, size
+        if fmt is not None:
+            x[t, :, :32], y[t, :, :32] = 0.0, 0.0
+    x[:, :, 0], y[:, :, 0] = 1.0, 1.0
+    eps = np.full(W, 0.05)
+    u = np.linspace(0.25 - 4e-4, 0.25 + 4e-4, n // 2)
+    u = np.broadcast_to(np.concatenate((u, u + 0.25))[None, :], (W, n))
+    g = (y.bfloat16().double() ** 2).sum(2).numpy()
+    check(B, x.bfloat16(), y.bfloat16(), g, eps, u, fmt=fmt)
