@@ -642,8 +642,11 @@ __device__ __noinline__ bool again(const Draw &P, double k2, RowCuts cuts, int w
     // (a list's entries are all formed again; what is not in it counts in the row's mass, of which a cut takes its share, and is
     // missing from the sums that are drawn from where there is no cut)
     RowError fine = {2.0 * (5.9604645e-8 * sums.mass + (where ? (double)tail : sums.rest) * off), 2.f * 5.9604645e-8f, 0.f};
+    // a share is of what the ranks left: where their cut was left out, of up to `loose` less
+    RowError edge = fine;
+    if (cuts.p < 1.0) edge.sums += 1.04 * (double)loose;
     RowCut<float> cut;
-    if (!row_cut(w, len, G, cuts, sums.top, sums.mass + (double)tail, sums.count, fine, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
+    if (!row_cut(w, len, G, cuts, sums.top, sums.mass + (double)tail, sums.count, edge, cut, tiles) || cut.lowest < 2.f * ROW_FLOOR) return false;
     fine.sums += 2.04 * (double)(cut.tau == 0.f ? fmaxf(tail, loose) : loose);
     return draw_all(P, row, w, len, where, cut, tiles, fine, G.t >> 5, G.nt >> 5);
 }

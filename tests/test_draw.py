@@ -375,3 +375,25 @@ def test_products_that_the_matrix_unit_cuts_off_one_by_one(B, d, fmt):
     u = np.broadcast_to(np.concatenate((u, u + 0.25))[None, :], (W, n))
     g = (y.bfloat16().double() ** 2).sum(2).numpy()
     check(B, x.bfloat16(), y.bfloat16(), g, eps, u, fmt=fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [312, 600, 3000])                  # a whole row, lists
+def test_shares_behind_a_rank_that_cuts_among_negligible_weights(B, m):
+    # ten entries carry the mass, the others 2^-26 of the largest each, less than 2^-20 of the mass together; the rank cuts among
+    # those.  The share is of what the rank left: shares between a border of that mass and the same border of all mass.
+    import torch
+    heavy = np.array([1.0, 0.9, 0.8, 0.7, 0.6, 0.5, 0.4, 0.3, 0.2, 0.1])
+    tail = heavy.sum() * 0.9 * 2.0 ** -20 / (m - 10)
+    W, n = 14 * 7, 4
+    rng = np.random.default_rng(m)
+    w = np.full((W, m), tail)
+    p = np.empty(W, np.float32)
+    for t in range(W):
+        w[t, rng.choice(m, 10, replace=False)] = heavy
+        left = np.sort(w[t])[::-1][:12]
+        p[t] = left[:2 + t % 7].sum() / left.sum()
+        for _ in range(t // 7):                                  # 0 to 13 steps below the border
+            p[t] = np.nextafter(p[t], np.float32(0))
+    u = (0.9 * rng.random((W, n, 2))).astype(np.float32)
+    check(B, torch.zeros(W, n, 1), torch.zeros(W, m, 1), np.log(w), np.ones(W), u, k=np.full(W, 12), p=p)
