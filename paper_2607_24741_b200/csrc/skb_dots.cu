@@ -90,9 +90,45 @@ __device__ __forceinline__ void tma_store_box(const CUtensorMap *tm, uint32_t sr
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
+// A sum in units of two points' powers of two, rounded once.  It is 0 or between 2^-20 and 2^33, and powers within FAR_POINT of 1 can
+// multiply it in any order; for others sum * a may be infinite, or have lost bits, where sum * a * b is neither.
+constexpr float FAR_POINT = 1099511627776.f;             // 2^40
+__device__ __forceinline__ bool far_point(float p) { return p > FAR_POINT || p < 1.f / FAR_POINT; }
+__device__ __forceinline__ float times_points(float sum, float a, float b)
+{
+    if ((a > 1.f) != (b > 1.f)) return sum * (a * b);
+    // both above 1: infinite at the first step is infinite in the end; both below: bits are lost at the first where the end is 0
+    return sum * fmaxf(a, b) * fminf(a, b);
+}
+
+// A warp's 32 rows and 64 columns of a tile with points far from 1 (nv4), by way of one of its boxes.
+__device__ __noinline__ void far_tile(const Dots &P, unsigned char *box, uint32_t src, bool ok, int w, int row0, int col0, float rp, const float *cps, int lane)
+{
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+    __syncwarp();
+#pragma unroll 1
+    for (int h = 0; h < 2; ++h) {
+        const int col = col0 + 32 * h;
+        if (col >= P.mo || row0 >= P.no) break;
+        uint32_t r[32];
+        tc_ld32_issue(src + 32 * h, r);
+        tc_ld_wait(r);
+        // (threads next to each other to banks next to each other: element q of row l at 32 l + (q + l) % 32)
+#pragma unroll
+        for (int q = 0; q < 32; ++q)
+            reinterpret_cast<float *>(box)[32 * lane + ((q + lane) & 31)] = ok ? times_points(__uint_as_float(r[q]), rp, cps[32 * h + q]) : __uint_as_float(0x7fffffffu);
+        __syncwarp();
+        const int rows = min(32, P.no - row0);
+        float *dst = P.out + (size_t)w * P.lane_out + (size_t)row0 * P.ldo + col + lane;
+        if (col + lane < P.mo)
+            for (int q = 0; q < rows; ++q) dst[(size_t)q * P.ldo] = reinterpret_cast<const float *>(box)[32 * q + ((lane + q) & 31)];
+        __syncwarp();
+    }
+}
+
 template <int KIND>
 __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmy,
-                                                             const __grid_constant__ CUtensorMap tmo, const Dots P)
+                                                             const __grid_constant__ CUtensorMap tmo, const __grid_constant__ Dots P)
 {
     constexpr bool SCALED = KIND != SKB_BF16;
     constexpr int WORDS = KIND == SKB_NV4 ? 4 : 2;               // words of scales that a point has in a chunk
@@ -100,6 +136,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
     extern __shared__ __align__(1024) unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[3 * DT_STAGES + 5];
     __shared__ __align__(16) float col_points[2][DT_BN];     // read 16 bytes at a time
+    __shared__ __align__(16) int col_fars[2][DT_BN / 32];    // whether some of 32 columns' points are not near
     __shared__ uint32_t tmem_holder;
     __shared__ int abort_flag;
 
@@ -250,16 +287,33 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
         unsigned char *gbox0 = gen + (box0 - base);
         int b = 0, ph = 0, turn = 0, even = 0;
         bool ok = true;
+        // powers of two of this thread's row, and of a column for all, of the tile that comes next (1: none).  All warps want them at the
+        // start of a tile, to know whether it has far ones: loaded there 4 lanes of 4096 x 4096 x 512 take 72 us, a tile ahead 64
+        float rp_next = 1.f, cp_next = 1.f;
+        auto next_points = [&](long long t) {
+            if (t >= tiles) return;
+            int w, i0, j0;
+            where(t, w, i0, j0);
+            const int row = i0 + quarter * 32 + lane, col = j0 + e;
+            rp_next = row < P.n ? __ldg(P.px + (size_t)w * P.n + row) : 1.f;
+            cp_next = e < DT_BN && col < P.m ? __ldg(P.py + (size_t)w * P.m + col) : 1.f;
+        };
+        if constexpr (KIND == SKB_NV4) next_points(blockIdx.x);
         for (long long t = blockIdx.x; t < tiles; t += gridDim.x) {
             int w, i0, j0;
             where(t, w, i0, j0);
-            const int row = i0 + quarter * 32 + lane;
             float rp = 1.f;
+            bool far = false;
             if constexpr (KIND == SKB_NV4) {
                 // (the buffer of two tiles ago: its readers have passed the barrier of the last tile)
-                if (e < DT_BN) col_points[even][e] = j0 + e < P.m ? P.py[(size_t)w * P.m + j0 + e] : 0.f;
-                rp = row < P.n ? P.px[(size_t)w * P.n + row] : 0.f;
+                const float cp = cp_next;
+                rp = rp_next;
+                next_points(t + gridDim.x);
+                if (e < DT_BN) col_points[even][e] = cp;
+                const bool col_far = __any_sync(0xffffffffu, far_point(cp)), row_far = __any_sync(0xffffffffu, far_point(rp));
+                if (lane == 0 && warp < 10) col_fars[even][warp - 6] = col_far;
                 asm volatile("bar.sync 1, %0;" ::"n"(DT_EPI * 32) : "memory");
+                far = row_far || (col_fars[even][0] | col_fars[even][1] | col_fars[even][2] | col_fars[even][3]) != 0;
             }
             const int c_first = half * (DT_BN / 2);
             // (an accumulator that is written again goes back when it has been read)
@@ -277,8 +331,15 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 if (b == 0) ph ^= 1;
             };
             uint32_t held[SCALED ? 1 : 2][32], src = 0;
-            if constexpr (SCALED) src = wait_acc();
-            else {
+            if constexpr (SCALED) {
+                src = wait_acc();
+                if (KIND == SKB_NV4 && far) {
+                    far_tile(P, gbox0 + turn * DT_BOX, src, ok, w, i0 + quarter * 32, j0 + c_first, rp, &col_points[even][c_first], lane);
+                    free_acc();
+                    even ^= 1;
+                    continue;
+                }
+            } else {
                 // sums of the parts, added; the 64 columns stay in registers (4-bit kinds, whose products are one part, are faster by
                 // boxes: 64 lanes of 1024 x 1024 x 512 56 us so, 75 this way)
                 for (int c = 0; c < chunks; c += DT_PART<KIND>) {

@@ -390,3 +390,26 @@ def test_offsets_past_32_bits(B, fmt):
     part = B.cloud4_dots(B.cloud4_pack(a[1:, -200:], fmt), B.cloud4_pack(b[1:], fmt))
     assert torch.equal(out[1:, -200:], part)
     assert torch.equal(out[:1, 31000:31100], B.cloud4_dots(B.cloud4_pack(a[:1, 31000:31100], fmt), B.cloud4_pack(b[:1], fmt)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m", [64, 100, 131])
+def test_nv4_products_of_large_and_small_points(B, m):
+    # points of 1e-38 to 1e38: the sum, times one point's power of two, may be past fp32's range where the product is not
+    import torch
+    W, n, d = 4, 150, 64
+    gen = torch.Generator().manual_seed(m)
+    e = torch.linspace(-37, 37, n)[None, :, None].expand(W, n, 1)
+    f = torch.linspace(-37, 37, m)[None, :, None].expand(W, m, 1)
+    x, y = torch.randn(W, n, d, generator=gen).double() * 10.0 ** e.double(), torch.randn(W, m, d, generator=gen).double() * 10.0 ** f.double()
+    x4, y4 = B.cloud4_pack(x.float().cuda(), "nv4"), B.cloud4_pack(y.float().cuda(), "nv4")
+    want = torch.bmm(x4.values().double(), y4.values().double().transpose(1, 2))
+    size = torch.bmm(x4.values().double().abs(), y4.values().double().abs().transpose(1, 2))
+    out = B.cloud4_dots(x4, y4)
+    # one step of 64: two units in the last place of the magnitudes' sum, and fp32's smallest number
+    bound = 2.0 ** -22 * size + 2.0 ** -149
+    inside = want.abs() + bound < 3.4e38
+    assert bool(torch.isfinite(out[inside]).all()) and bool(((out.double() - want).abs() <= bound)[inside].all())
+    big = want.abs() - bound > 3.5e38
+    assert bool(torch.isinf(out[big]).all()) and bool((torch.sign(out) == torch.sign(want))[big].all())
+    assert bool(inside.any()) and bool(big.any())
