@@ -179,9 +179,9 @@ __device__ __forceinline__ double square_of(const void *base, const Cloud4 &c, s
         eight_values<BF>(load_eight<BF>(base, c, row, d, 8 * q), c, point, v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float a = v[i] * v[i];                             // exact: at most 16 bits
-            s += (double)a;
-            f += a;
+            // (in double: the square of a value beyond 2^64 is infinite in fp32, and a norm that is infinite would mask its target)
+            s = fma((double)v[i], (double)v[i], s);
+            f = fmaf(v[i], v[i], f);
         }
         const int until = BF ? min(steps, (8 * q / DOTS_BF16_PART + 1) * (DOTS_BF16_PART / 16)) : steps;
         p = fmaf(f, (float)max(until - q / 2, 1), p);

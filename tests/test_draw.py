@@ -397,3 +397,23 @@ def test_shares_behind_a_rank_that_cuts_among_negligible_weights(B, m):
             p[t] = np.nextafter(p[t], np.float32(0))
     u = (0.9 * rng.random((W, n, 2))).astype(np.float32)
     check(B, torch.zeros(W, n, 1), torch.zeros(W, m, 1), np.log(w), np.ones(W), u, k=np.full(W, 12), p=p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", [None, "mx4", "nv4"])
+@pytest.mark.parametrize("far", [2e19, 1e25, 1e36])
+def test_deep_points_whose_squares_pass_the_range_of_fp32(B, fmt, far):
+    # sources and targets at the same far place; some targets elsewhere (a weight of zero), some masked
+    import torch
+    W, n, m, d = 3, 12, 90, 64
+    x, y, g, rng = clouds(int(math.log(far)), W, n, m, d, dtype="bf16", spread=0.1)
+    x[0, :, 3] = far                                             # all targets there, but for three
+    y[0, :, 3] = far
+    y[0, 7:10, 3] = 0.0
+    x[1, 4, 3] = far                                             # one source and one target
+    y[1, 11, 3] = far
+    y[2, :, 3] = far                                             # targets that no source is near
+    x[2, 5, 3] = far
+    g[:, 20:24] = -np.inf
+    check(B, x, y, g, np.full(W, 0.1), rng.random((W, n, 4), np.float32), fmt=fmt)
+    check(B, x, y, g, np.full(W, 0.1), rng.random((W, n, 4), np.float32), k=np.full(W, 5), p=np.full(W, 0.8), fmt=fmt)
