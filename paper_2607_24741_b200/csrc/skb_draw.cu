@@ -677,7 +677,10 @@ __device__ __forceinline__ void enter_lane(const Draw &P, LaneState &S, int lane
     __syncthreads();
     S.lane = lane;
     S.L = lane_of(P, lane);
-    S.k2 = (float)S.L.k2;
+    // Distances past fp32's range are as good as infinite beside k from 1e-34 on (a row is decided in fp32 while its largest exponent is below
+    // 34000; 1e-34 times 3.4e38 is as much), and what is lost below the range is nothing up to 1e27 (2 k d 2^-126 < 2^-25 of an exponent).
+    // Other lanes' exponents are NaN in fp32, which leaves their rows to float64.
+    S.k2 = S.L.k2 >= 1e-34 && S.L.k2 <= 1e27 ? (float)S.L.k2 : CUDART_NAN_F;
     S.p = (float)S.L.cuts.p;
     const double *hn = P.hn + (size_t)lane * P.mp;
     double top = -CUDART_INF;

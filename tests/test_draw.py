@@ -417,3 +417,23 @@ def test_deep_points_whose_squares_pass_the_range_of_fp32(B, fmt, far):
     g[:, 20:24] = -np.inf
     check(B, x, y, g, np.full(W, 0.1), rng.random((W, n, 4), np.float32), fmt=fmt)
     check(B, x, y, g, np.full(W, 0.1), rng.random((W, n, 4), np.float32), k=np.full(W, 5), p=np.full(W, 0.8), fmt=fmt)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(2, 8, 50, 1), (2, 5, 700, 3), (1, 3, 9000, 2)])
+def test_distances_past_the_range_of_fp32_beside_an_eps_as_large(B, shape):
+    W, n, m, d = shape
+    x, y, g, rng = clouds(2, W, n, m, d)
+    x, y = x * 1.5e19, y * 1.5e19
+    check(B, x, y, g, np.full(W, 3e38), rng.random((W, n, 8), np.float32))
+    check(B, x, y, g, np.full(W, 3e38), rng.random((W, n, 8), np.float32), p=np.full(W, 0.9), T=np.full(W, 3.0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [1e-38, 2e-37, 1e-35, 1e-33, 1e-30])
+@pytest.mark.parametrize("shape,dtype,fmt", [((2, 800, 50, 64), "bf16", None), ((2, 800, 50, 64), "bf16", "mx4"), ((2, 800, 50, 128), "bf16", "nv4"), ((2, 800, 50, 3), "f32", None)])
+def test_distances_at_the_low_end_of_fp32_beside_an_eps_as_small(B, shape, dtype, fmt, eps):
+    W, n, m, d = shape
+    x, y, g, rng = clouds(2, W, n, m, d, dtype=dtype)
+    x, y = x * (eps / d) ** 0.5, y * (eps / d) ** 0.5
+    check(B, x, y, g * eps, np.full(W, eps), rng.random((W, n), np.float32), fmt=fmt)
