@@ -969,7 +969,7 @@ extern "C" skb_status sinkhorn_batch_draw_plan(skb_batch *h, const void *x, cons
     skb_draw_config mine = *cfg;
     mine.stream = h->stream;
     if (side) { mine.n = cfg->m; mine.m = cfg->n; }
-    st = sinkhorn_plan_draw(side ? y : x, side ? x : y, side ? h->dev.f_out : h->dev.g_out, eps, u, &mine, index, logp);
+    st = plan_draw(side ? y : x, side ? x : y, side ? h->dev.f_out : h->dev.g_out, eps, u, &mine, h->dev.status, index, logp);
     return st == SKB_OK ? st : fail(h, st, sinkhorn_operator_last_error());
 }
 

@@ -56,6 +56,7 @@ struct Draw {
     const double *g;
     const float *eps, *temperature, *top_p, *min_p, *u;
     const int *top_k;
+    const int *status;                               // of a batch's lanes, or null
     int *index;
     float *logp;
     int dtype, W, n, m, d, S, mp;
@@ -98,6 +99,9 @@ __device__ __noinline__ float raw_value(const void *base, const Cloud4 &c, int d
     if (dtype == SKB_BF16) return __uint_as_float((uint32_t)((const uint16_t *)base)[row * d + k] << 16);
     return cloud4_value(c, row, k);
 }
+// A lane that its batch gave up has potentials that mean nothing: NaN in the place of all k g, which closes its rows.  (The settings'
+// check would be the place to ask; there it costs the kernel of rows by warps 43 of 686 us.)
+__device__ __forceinline__ bool given_up(const Draw &P, int w) { return P.status && P.status[w] == SKB_LANE_NONFINITE; }
 // Transposed copy of y and k g, 32 points to a block.  Masked points get coordinates of zero, whatever theirs are.
 __global__ void __launch_bounds__(256) transpose_kernel(const __grid_constant__ Draw P)
 {
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(256) transpose_kernel(const __grid_constant__ 
         const int j = j0 + tid;
         const double g = j < P.m ? P.g[(size_t)w * P.m + j] : -CUDART_INF;
         masked[tid] = g == -CUDART_INF;
-        if (j < P.mp) P.hn[(size_t)w * P.mp + j] = g == -CUDART_INF ? g : L.k2 * g;
+        if (j < P.mp) P.hn[(size_t)w * P.mp + j] = given_up(P, w) ? CUDART_NAN : g == -CUDART_INF ? g : L.k2 * g;
     }
     __syncthreads();
     float *yt = P.yt + (size_t)w * P.d * P.mp;
@@ -210,7 +214,7 @@ __global__ void __launch_bounds__(256) norms_kernel(const __grid_constant__ Draw
         const bool masked = g == -CUDART_INF;
         const double s = masked ? 0.0 : square_of<BF>(P.y, P.y4, (size_t)w * P.m + i, P.d, p);
         if (lane == 0) {
-            P.hn[(size_t)w * P.mp + i] = masked ? g : lane_of(P, w).k2 * (g - s);
+            P.hn[(size_t)w * P.mp + i] = given_up(P, w) ? CUDART_NAN : masked ? g : lane_of(P, w).k2 * (g - s);
             P.yn[(size_t)w * P.mp + i] = make_float2((float)s, (float)p);
         }
         return;
@@ -1261,8 +1265,8 @@ extern "C" size_t sinkhorn_plan_draw_workspace_bytes(const skb_draw_config *cfg)
     return carve(P, plan_of(P), nullptr);
 }
 
-extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u,
-                                         const skb_draw_config *cfg, int *index, float *logp)
+skb_status skb::plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u, const skb_draw_config *cfg,
+                          const int *status, int *index, float *logp)
 {
     if (!x || !y || !g || !eps || !u || !cfg || !index) return op_fail(SKB_ERR_NULL, "x, y, g, eps, u, cfg and index are required");
     if (const char *why = refused(cfg)) return op_fail(SKB_ERR_SHAPE, why);
@@ -1273,7 +1277,7 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
     if ((uintptr_t)x % (packed ? 256 : 16) || (uintptr_t)y % (packed ? 256 : 16))
         return op_fail(SKB_ERR_VALUE, "x and y must be 16-byte aligned, 4-bit clouds 256-byte aligned");
     Draw P = problem(cfg);
-    P.x = x; P.y = y; P.g = g; P.eps = eps; P.u = u; P.index = index; P.logp = logp;
+    P.x = x; P.y = y; P.g = g; P.eps = eps; P.u = u; P.status = status; P.index = index; P.logp = logp;
     if (packed) {
         P.x4 = cloud4_view(x, (size_t)P.W * P.n, P.d, P.dtype);
         P.y4 = cloud4_view(y, (size_t)P.W * P.m, P.d, P.dtype);
@@ -1313,4 +1317,10 @@ extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const dou
             }
         }
     return exact();
+}
+
+extern "C" skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u,
+                                         const skb_draw_config *cfg, int *index, float *logp)
+{
+    return plan_draw(x, y, g, eps, u, cfg, nullptr, index, logp);
 }

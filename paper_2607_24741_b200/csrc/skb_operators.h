@@ -25,5 +25,8 @@ DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t
 constexpr int DOTS_BF16_PART = 64;
 skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st,
                        int n_out = 0, int m_out = 0);
+// sinkhorn_plan_draw; lanes whose `status` (null: none) is SKB_LANE_NONFINITE give no draws.
+skb_status plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u, const skb_draw_config *cfg,
+                     const int *status, int *index, float *logp);
 
 }  // namespace skb

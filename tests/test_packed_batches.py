@@ -203,3 +203,28 @@ def test_draws_from_a_batch_on_a_stream_of_its_own(B):
         assert torch.equal(got, want)
     torch.cuda.synchronize()
     sb.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,d", [(None, 3), ("bf16", 3), ("bf16", 64)])
+def test_a_lane_that_went_non_finite_is_not_drawn_from(B, fmt, d):
+    import torch
+    W, n, m = 3, 40, 50
+    x, y, a, b, eps = problem(8, W, n, m, d)
+    if fmt:
+        x, y = x.bfloat16(), y.bfloat16()
+    u, w = torch.rand(W, n, 2, generator=torch.Generator().manual_seed(1)).cuda(), torch.rand(W, m, generator=torch.Generator().manual_seed(2)).cuda()
+    out = []
+    for broken in (False, True):
+        if broken:
+            y = y.clone()
+            y[1, 5], y[1, 6] = 1e20, -1e20
+        sb = B.SinkhornBatch(x, y, a, b, eps, 1e-3, compute="f32")
+        sb.drain()
+        assert sb.depths()[1].tolist() == [B.LANE_DONE, B.LANE_NONFINITE if broken else B.LANE_DONE, B.LANE_DONE]
+        out.append(sb.draw_plan(u, logp=True) + sb.draw_plan(w, side="targets", logp=True))
+        sb.close()
+    for fine, part in zip(*out):
+        assert torch.equal(fine[::2], part[::2])
+        assert bool((part[1] == -1).all()) if part.dtype == torch.int32 else bool(torch.isnan(part[1]).all())
+        assert bool((fine != -1).all())
