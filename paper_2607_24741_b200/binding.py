@@ -430,6 +430,20 @@ class SinkhornBatch:
         with torch.cuda.device(x.device):
             self.h = sinkhorn_batch_create(_raw(x), _raw(y), a, b, eps, float(tol), self.cfg)
 
+    @contextlib.contextmanager
+    def _after_here(self):
+        """A call that reads or writes tensors of the current stream on the batch's: that waits for the current stream, which waits for
+        the call in turn, so that the tensors are the current stream's again when the call returns."""
+        here = torch.cuda.current_stream(self.device)
+        if here == self.stream:
+            yield
+            return
+        self.stream.wait_stream(here)
+        try:
+            yield
+        finally:
+            here.wait_stream(self.stream)
+
     def step(self, cycles=1):
         sinkhorn_batch_step(self.h, cycles)
 
@@ -509,7 +523,8 @@ class SinkhornBatch:
 
     def draw_plan(self, u, *, side="sources", temperature=None, top_k=None, top_p=None, min_p=None, logp=False):
         """Partners of the sources (u [W, n] or [W, n, draws]) or of the targets (side "targets", u [W, m] or [W, m, draws])
-        drawn from the plan of the finished lanes; settings and outputs as those of plan_draw.  Runs on the batch's stream."""
+        drawn from the plan of the finished lanes; settings and outputs as those of plan_draw.  Runs on the batch's stream, after what
+        the current one has been given and before what it is given next."""
         if side not in ("sources", "targets"):
             raise ValueError('side must be "sources" or "targets"')
         x, y, _a, _b, eps = self._keep[:5]
@@ -517,8 +532,7 @@ class SinkhornBatch:
         n, m = (self.m, self.n) if other else (self.n, self.m)
         if u.device != self.device:
             raise ValueError("u must be on the batch's device")
-        with torch.cuda.device(self.device), torch.cuda.stream(self.stream):
-            # (copies, where they are needed, are made on the stream that reads them)
+        with torch.cuda.device(self.device):
             u = u.contiguous()
             if self.format is None:
                 x, y = (v if v.data_ptr() % 16 == 0 else v.clone() for v in (x, y))
@@ -526,8 +540,9 @@ class SinkhornBatch:
                                dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p), self.stream.cuda_stream)
             index, lp, ws = _draw_out(cfg, u, logp)
             cfg.n, cfg.m = self.n, self.m
-            _check(lib.sinkhorn_batch_draw_plan(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(eps), _ptr(u), 1 if other else 0,
-                                                ctypes.byref(cfg), _ptr(index), _ptr(lp)), self.h)
+            with self._after_here():
+                _check(lib.sinkhorn_batch_draw_plan(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(eps), _ptr(u), 1 if other else 0,
+                                                    ctypes.byref(cfg), _ptr(index), _ptr(lp)), self.h)
         return (index, lp) if logp else index
 
     def set_profiling(self, on=True):

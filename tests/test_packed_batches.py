@@ -228,3 +228,35 @@ def test_a_lane_that_went_non_finite_is_not_drawn_from(B, fmt, d):
         assert torch.equal(fine[::2], part[::2])
         assert bool((part[1] == -1).all()) if part.dtype == torch.int32 else bool(torch.isnan(part[1]).all())
         assert bool((fine != -1).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mine", [False, True])
+def test_draws_from_a_batch_on_another_stream_wait_for_their_numbers(B, mine):
+    # the numbers and settings come from the caller's stream, which is busy, the draws are made on the batch's, the outputs are read on
+    # the caller's; what it allocates next is not what the draws still read
+    import torch
+    W, n, m, d = 2, 40, 50, 3
+    x, y, a, b, eps = problem(12, W, n, m, d)
+    side, own = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    sb = B.SinkhornBatch(x, y, a, b, eps, 1e-3, stream=side)
+    sb.drain()
+    g = sb.potentials(f64=True)[1]
+    torch.cuda.synchronize()
+    u0, T0 = torch.rand(W, n, generator=torch.Generator().manual_seed(5)).cuda(), torch.full((W,), 0.7, device="cuda")
+    want, wlp = B.plan_draw(x, y, g, eps, u0, temperature=T0, logp=True)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(own if mine else torch.cuda.current_stream()):
+        u, T = torch.zeros(W, n, device="cuda"), torch.zeros(W, device="cuda")
+        torch.cuda._sleep(100_000_000)                           # some 50 ms
+        u.copy_(u0), T.copy_(T0)
+        got, lp = sb.draw_plan(u, temperature=T, logp=True)
+        same = got.eq(want).all() & lp.eq(wlp).all()
+        del u, T
+        torch.full((W, n), 0.5, device="cuda")
+        torch.full((W,), 3.0, device="cuda")
+        assert bool(same)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(lp, wlp)
+    sb.close()
