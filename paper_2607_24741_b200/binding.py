@@ -385,6 +385,20 @@ def plan_draw(x, y, g, eps, u, *, temperature=None, top_k=None, top_p=None, min_
     return (index, lp) if logp else index
 
 
+class _Apart:
+    """A stream's work after what `here` has been given, and `here`'s after that: tensors that are made, cleared or freed on `here`
+    are read and written there in between."""
+
+    def __init__(self, here, there):
+        self.here, self.there = here, there
+
+    def __enter__(self):
+        self.there.wait_stream(self.here)
+
+    def __exit__(self, *_):
+        self.here.wait_stream(self.there)
+
+
 class SinkhornBatch:
     """One batch of W lanes on the current CUDA device (thin wrapper over the C calls)."""
 
@@ -427,22 +441,13 @@ class SinkhornBatch:
         self.cfg.workspace_bytes = need
         self._keep = (x, y, a, b, eps)
         self.h = None
-        with torch.cuda.device(x.device):
+        with torch.cuda.device(x.device), self._after_here():
             self.h = sinkhorn_batch_create(_raw(x), _raw(y), a, b, eps, float(tol), self.cfg)
 
-    @contextlib.contextmanager
     def _after_here(self):
-        """A call that reads or writes tensors of the current stream on the batch's: that waits for the current stream, which waits for
-        the call in turn, so that the tensors are the current stream's again when the call returns."""
+        """For calls that read or write tensors of the current stream on the batch's."""
         here = torch.cuda.current_stream(self.device)
-        if here == self.stream:
-            yield
-            return
-        self.stream.wait_stream(here)
-        try:
-            yield
-        finally:
-            here.wait_stream(self.stream)
+        return _HERE_ALREADY if here == self.stream else _Apart(here, self.stream)
 
     def step(self, cycles=1):
         sinkhorn_batch_step(self.h, cycles)
@@ -458,19 +463,22 @@ class SinkhornBatch:
         f = torch.zeros(self.L, self.n, dtype=dt, device=self.device)
         g = torch.zeros(self.L, self.m, dtype=dt, device=self.device)
         fn = lib.sinkhorn_batch_potentials_f64 if f64 else lib.sinkhorn_batch_potentials
-        _check(fn(self.h, _ptr(f), _ptr(g)), self.h)
+        with self._after_here():
+            _check(fn(self.h, _ptr(f), _ptr(g)), self.h)
         return f, g
 
     def depths(self):
         depth = torch.zeros(self.L, dtype=torch.int32, device=self.device)
         status = torch.zeros(self.L, dtype=torch.int32, device=self.device)
-        _check(lib.sinkhorn_batch_depths(self.h, _ptr(depth), _ptr(status)), self.h)
+        with self._after_here():
+            _check(lib.sinkhorn_batch_depths(self.h, _ptr(depth), _ptr(status)), self.h)
         return depth, status
 
     def residuals(self):
         rr = torch.zeros(self.L, dtype=torch.float32, device=self.device)
         rc = torch.zeros(self.L, dtype=torch.float32, device=self.device)
-        _check(lib.sinkhorn_batch_residuals(self.h, _ptr(rr), _ptr(rc)), self.h)
+        with self._after_here():
+            _check(lib.sinkhorn_batch_residuals(self.h, _ptr(rr), _ptr(rc)), self.h)
         return rr, rc
 
     def warm_start(self, f0=None, g0=None, audit_initial=False):
@@ -478,7 +486,8 @@ class SinkhornBatch:
             if t is not None and (t.dtype != torch.float64 or not t.is_cuda or tuple(t.shape) != shape
                                   or not t.is_contiguous()):
                 raise ValueError("f0 [W,n] and g0 [W,m] must be contiguous float64 CUDA tensors")
-        _check(lib.sinkhorn_batch_warm_start(self.h, _ptr(f0), _ptr(g0), 1 if audit_initial else 0), self.h)
+        with self._after_here():
+            _check(lib.sinkhorn_batch_warm_start(self.h, _ptr(f0), _ptr(g0), 1 if audit_initial else 0), self.h)
         self._warm = (f0, g0)
 
     def check_guards(self) -> int:
@@ -492,7 +501,8 @@ class SinkhornBatch:
         rr = torch.full((self.L,), float("nan"), dtype=torch.float32, device=self.device)
         rc = torch.full((self.L,), float("nan"), dtype=torch.float32, device=self.device)
         fl = torch.full((self.L,), -1, dtype=torch.int32, device=self.device)
-        _check(lib.sinkhorn_batch_last_audit(self.h, _ptr(rr), _ptr(rc), _ptr(fl)), self.h)
+        with self._after_here():
+            _check(lib.sinkhorn_batch_last_audit(self.h, _ptr(rr), _ptr(rc), _ptr(fl)), self.h)
         return rr, rc, fl
 
     def refill(self, x, y, a, b, eps) -> int:
@@ -507,7 +517,8 @@ class SinkhornBatch:
                 tuple(a.shape) != (count, self.n) or tuple(b.shape) != (count, self.m) or tuple(eps.shape) != (count,):
             raise ValueError("shapes must be x[c,n,d] y[c,m,d] a[c,n] b[c,m] eps[c]")
         first = ctypes.c_int(-1)
-        _check(lib.sinkhorn_batch_refill(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(a), _ptr(b), _ptr(eps), count, ctypes.byref(first)), self.h)
+        with self._after_here():
+            _check(lib.sinkhorn_batch_refill(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(a), _ptr(b), _ptr(eps), count, ctypes.byref(first)), self.h)
         self._keep = self._keep + (x, y, a, b, eps)
         return first.value
 
@@ -518,7 +529,8 @@ class SinkhornBatch:
         if v.dtype != torch.float32 or v.dim() != 3 or tuple(v.shape[:2]) != (self.W, self.m):
             raise ValueError("v must be float32 [W, m, dv]")
         out = torch.empty(self.W, self.n, v.shape[2], dtype=torch.float32, device=self.device)
-        _check(lib.sinkhorn_batch_apply_plan(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(eps), _ptr(v), v.shape[2], _ptr(out)), self.h)
+        with self._after_here():
+            _check(lib.sinkhorn_batch_apply_plan(self.h, _ptr(_raw(x)), _ptr(_raw(y)), _ptr(eps), _ptr(v), v.shape[2], _ptr(out)), self.h)
         return out
 
     def draw_plan(self, u, *, side="sources", temperature=None, top_k=None, top_p=None, min_p=None, logp=False):

@@ -260,3 +260,49 @@ def test_draws_from_a_batch_on_another_stream_wait_for_their_numbers(B, mine):
     torch.cuda.synchronize()
     assert torch.equal(got, want) and torch.equal(lp, wlp)
     sb.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("call", ["create", "potentials", "potentials64", "depths", "residuals", "apply_plan", "warm_start", "refill"])
+def test_what_a_batch_on_another_stream_reads_and_writes_is_the_callers(B, call):
+    # the caller's stream is busy with what the call reads, or has yet to clear what it writes
+    import torch
+    W, n, m, d = 3, 40, 50, 3
+    parts = problem(12, W, n, m, d)
+    side = torch.cuda.Stream()
+    busy = lambda: torch.cuda._sleep(100_000_000)                # some 50 ms
+    late = lambda t: torch.zeros_like(t).copy_(t)
+    f0 = torch.linspace(-0.01, 0.01, W * n, dtype=torch.float64, device="cuda").view(W, n)
+    v = torch.randn(W, m, 4, device="cuda")
+    out = []
+    for stream in (None, side):
+        torch.cuda.synchronize()
+        if call == "create":
+            busy()
+        sb = B.SinkhornBatch(*(late(t) if call == "create" else t for t in parts), 1e-3, stream=stream, lane_capacity=2 * W if call == "refill" else 0)
+        if call == "warm_start":
+            torch.cuda.synchronize()
+            busy()
+            sb.warm_start(late(f0))
+        sb.drain()
+        torch.cuda.synchronize()
+        if call == "refill":
+            busy()
+            sb.refill(*(late(t) for t in parts))
+            sb.drain()
+            torch.cuda.synchronize()
+        if call in ("potentials", "potentials64", "depths", "residuals"):
+            busy()
+            got = sb.potentials(f64=True) if call == "potentials64" else getattr(sb, call)()
+        elif call == "apply_plan":
+            busy()
+            got = (sb.apply_plan(late(v)),)
+        else:
+            got = sb.potentials(f64=True) + sb.depths()
+        got = [t.clone() for t in got]
+        torch.cuda.synchronize()
+        out.append(got)
+        sb.close()
+    assert bool((out[0][0] != 0).any())
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
