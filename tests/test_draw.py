@@ -437,3 +437,31 @@ def test_distances_at_the_low_end_of_fp32_beside_an_eps_as_small(B, shape, dtype
     x, y, g, rng = clouds(2, W, n, m, d, dtype=dtype)
     x, y = x * (eps / d) ** 0.5, y * (eps / d) ** 0.5
     check(B, x, y, g * eps, np.full(W, eps), rng.random((W, n), np.float32), fmt=fmt)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_32_bits_count(B):
+    # 4.3e9 rows, a row to a warp.  Most lanes are without targets, which takes no time; those that have some, at both ends and across
+    # the 2^32nd row, are drawn from like each for itself.  (The numbers, all within [0, 1), are the sources as well: 75 GB as a whole.)
+    import torch
+    W, n, m = 65535, 65540, 1000
+    u = torch.full((W, n), 0.25, device="cuda")
+    some = [0, 1, 32767, 65532, 65533, 65534]                    # 65532 has row 2^32
+    assert W * n > 1 << 32 and (1 << 32) // n == 65532
+    gen = torch.Generator("cuda").manual_seed(3)
+    for t in some:
+        u[t] = torch.rand(n, generator=gen, device="cuda")
+    y = torch.rand(W, m, 1, generator=gen, device="cuda")
+    g = torch.full((W, m), -math.inf, dtype=torch.float64, device="cuda")
+    g[some] = 0.0
+    eps = torch.full((W,), 0.01, device="cuda")
+    index = B.plan_draw(u[:, :, None], y, g, eps, u)
+    for lo in range(0, W, 8192):
+        part = index[lo:lo + 8192]
+        drawn = (part != -1).any(1).nonzero().reshape(-1).tolist()
+        assert [lo + t for t in drawn] == [t for t in some if lo <= t < lo + 8192]
+    for t in some:
+        one = slice(t, t + 1)
+        assert torch.equal(index[one], B.plan_draw(u[one, :, None], y[one], g[one], eps[one], u[one])) and bool((index[t] >= 0).all())
+    del u, y, g, index, part
+    torch.cuda.empty_cache()
