@@ -776,7 +776,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
         G.sync();
         const float mass = f[0];
         if (mass <= 3e38f) {
-            const float k2 = S.k2, A = fabsf(top), adds = u24 * (float)(12 + mp / (4 * G.nt));
+            const float k2 = S.k2, A = fabsf(top);
             float fixed, slope, bound = 0.f;                     // of an exponent: fixed + slope q
             if (DOTS) {
                 bound = sqrtf(xn.x) * S.y_max;
@@ -794,8 +794,14 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
             const float off = fixed + 24.f * slope;
             if (off < 0.01f) {
                 const float unit = QUICK_ONE / mass;
-                // (roundings to units: half of one for each thread of a pass, and for each of 32 in a tile, twice)
-                QuickSlack slack = {1.02f * fixed * QUICK_ONE, (2.f * adds + slope * f[1] / mass) * QUICK_ONE + (float)(G.nt + 32 * ntiles)};
+                // Additions, 2^-24 of a sum for each that a weight goes through.  Of the mass, which the unit is made from: a thread's
+                // quadruples, 2 in each, 5 in the warp, one a warp.  A part that a cut compares: one for each of a thread's
+                // weights, at most 32 in a list of the last; 3 for the unit, for its reciprocal and for the product.  A draw's
+                // sums, parts and whole, are of the same unit: 3 and the product, twice.  Roundings to units: half of one
+                // for each thread of a cut's passes, of which two are joined; for each of 32 in a draw's tiles, parts and whole.
+                const int warps = G.nt >> 5, quads = (ntiles + warps - 1) / warps;
+                const float cuts_sums = 64.f * (float)(quads + 7 + warps + 3 + max(4 * quads, 32)) + (float)G.nt;
+                QuickSlack slack = {1.02f * fixed * QUICK_ONE, slope * f[1] / mass * QUICK_ONE + (float)(64 * 8 + 32 * ntiles)};
                 // Cuts among what weighs less than ROW_TAIL together make no difference that a draw could show but one inside
                 // of the bounds, to which that weight is added.
                 int k = S.L.cuts.k;
@@ -864,7 +870,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 QuickCut cut;
                 cut.tau = 0.f;
                 if (!sparse || G.t < 32) {
-                    sure = quick_cut(r, len, A1, k, S.p, r_min, count, own, unit, slack, err, M.list + (sparse ? list_room(mp) : 0),
+                    sure = quick_cut(r, len, A1, k, S.p, r_min, count, own, unit, slack, sparse ? fmaxf(cuts_sums, 64.f * (float)(quads + 10 + warps + len / 32) + (float)G.nt) : cuts_sums, err, M.list + (sparse ? list_room(mp) : 0),
                                      sparse ? 0u : (unsigned)list_room(mp), cut, turn);
                     if (sure) quick_tiles(r, len / ROW_TILE, A1, cut.tau, unit, units);
                 }

@@ -212,7 +212,7 @@ __device__ __forceinline__ bool quick_find(const float *row, const int mp, const
 
 // Cuts the row.
 __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const RowGroup &G, const int k, const float p, const float smallest, const unsigned count, const unsigned own,
-                                          const float unit, const QuickSlack &slack, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
+                                          const float unit, const QuickSlack &slack, const float sums, const RowError &err, float *list, const unsigned room, QuickCut &cut, int &turn)
 {
     cut = {0.f, count, (unsigned)QUICK_ONE, own};
     // by rank, then by mass (one body: the code has to stay in the instruction cache)
@@ -231,7 +231,7 @@ __device__ __forceinline__ bool quick_cut(const float *w, const int mp, const Ro
         }
         // (a target by mass is off by 64 units: fp32's last place)
         const unsigned target = by_mass ? (unsigned)(p * (float)cut.mass) : (unsigned)k;
-        if (!quick_find(w, mp, G, by_mass != 0, target, unit, slack.at(p), err, list, room, cut, turn)) return false;
+        if (!quick_find(w, mp, G, by_mass != 0, target, unit, slack.at(p) + (unsigned)sums, err, list, room, cut, turn)) return false;
     }
     if (smallest > 0.f) {
         const float e = err.weight - err.slope * log2f(smallest);

@@ -465,3 +465,30 @@ def test_more_rows_than_32_bits_count(B):
         assert torch.equal(index[one], B.plan_draw(u[one, :, None], y[one], g[one], eps[one], u[one])) and bool((index[t] >= 0).all())
     del u, y, g, index, part
     torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,heavy", [(512, 512), (1024, 1024), (2000, 2000), (8192, 8192), (22000, 22000), (8000, 1900), (22900, 5700)])
+def test_shares_of_rows_whose_sums_all_round_one_way(B, m, heavy):
+    # Each thread's sum begins above 1 and every further weight is a whole number and 0.48 of its unit in the last place, which an
+    # addition in fp32 loses: up to 180 times.  Shares just below and at borders among the small weights, of rows and (where most
+    # entries are masked) of lists.
+    import torch
+    W, n = 12, 3
+    rng = np.random.default_rng(m)
+    w = np.zeros((W, m))
+    w[:, :heavy] = (np.floor(6.6e-4 * rng.uniform(1.04, 1.6, (W, heavy)) * 2 ** 23) + 0.48) * 2.0 ** -23
+    w[:, 0:128:4] = 1.0
+    order = np.sort(w, axis=1)[:, ::-1]
+    cum = np.cumsum(order, 1)
+    p = np.empty(W, np.float32)
+    for t in range(W):
+        j = 32 + int((heavy - 33) * (t + 1) / (W + 1))
+        p[t] = cum[t, j] / cum[t, -1]
+        for _ in range(t % 4):
+            p[t] = np.nextafter(p[t], np.float32(0))
+    with np.errstate(divide="ignore"):
+        g = np.log(w)
+    u = rng.random((W, n), np.float32)
+    u[:, 0] = 1 - 2.0 ** -24                                     # the last entry that is kept
+    check(B, torch.zeros(W, n, 1), torch.zeros(W, m, 1), g, np.ones(W), u, p=p)
