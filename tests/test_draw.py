@@ -492,3 +492,30 @@ def test_shares_of_rows_whose_sums_all_round_one_way(B, m, heavy):
     u = rng.random((W, n), np.float32)
     u[:, 0] = 1 - 2.0 ** -24                                     # the last entry that is kept
     check(B, torch.zeros(W, n, 1), torch.zeros(W, m, 1), g, np.ones(W), u, p=p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(6, 40, 77, 8), (3, 30, 900, 3), (2, 20, 6000, 4)])
+def test_log_probabilities_on_both_sides_of_the_border_of_large_exponents(B, shape):
+    # Rows whose largest exponent is A: from DRAW_FAR = 48 on weights above 2^-22 are formed from their points in double, and off by
+    # 2^-24 of at most 22 (times ln 2) and 2^-22 each; below that exponents are off by (d + 6) 2^-24 (A + 22), the drawn one's
+    # and those of the sum.  In both, what weighs less than 2^-22 may be 1 % off (m 2^-22 / 100 of the sum) or, up to 2^-20 of
+    # the sum, missing, and the result rounds to 2^-24 of itself (twice: it is formed as a difference).
+    import torch
+    W, n, m, d = shape
+    x, y, g, rng = clouds(31, W, n, m, d)
+    eps = np.exp(rng.uniform(np.log(0.003), np.log(0.5), W)).astype(np.float32)
+    u = rng.random((W, n, 3), np.float32)
+    f = lambda v, dt: torch.as_tensor(v).to(dt).cuda()
+    idx, lp = B.plan_draw(x.cuda(), y.cuda(), f(g, torch.float64), f(eps, torch.float32), f(u, torch.float32), logp=True)
+    xh, yh = x.double().numpy(), y.double().numpy()
+    want, wlp = reference(xh, yh, g, eps, u.astype(np.float64))
+    np.testing.assert_array_equal(idx.cpu().numpy(), want)
+    z = np.stack([(g[t] - g[t].max() - ((xh[t][:, None, :] - yh[t][None]) ** 2).sum(2)) / float(eps[t]) for t in range(W)]) / math.log(2)
+    A = -z.max(2)[:, :, None]
+    double = 22 * 2.0 ** -24 * 0.6932 + 2.0 ** -22 + m * 2.0 ** -22 / 100 + 2.0 ** -20 + 2.0 ** -23 * np.abs(wlp)
+    single = double + 2 * 0.6932 * (d + 6) * 2.0 ** -24 * (A + 22) + 2.0 ** -23
+    bound = np.where(A > 48.01, double, single)
+    off = np.abs(lp.cpu().numpy() - wlp)
+    assert (off <= bound).all(), (off / bound).max()
+    assert (A > 48.01).any() and (A < 48).any()
