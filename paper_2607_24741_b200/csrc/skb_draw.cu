@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(512) draw_exact_kernel(const __grid_constant__
 //                cuts off (skb_dots.cu): bf16, for 16 dimensions, 16 products and the sum so far at 2^-25 of the largest and the
 //                result to 24 bits, 17 / 4 + 1 units of 2^-23 of that; 4-bit kinds, for 64 dimensions, four blocks of a scale
 //                and the sum, 5 / 4 + 1 units, counted as 4.  (d / 16) (5.25 or 1) B' 2^-23, the additions of bf16's parts
-//                B 2^-24 each, two units 2 B 2^-23 to spare; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
+//                B 2^-24 each; the roundings of h, scale and t: (3 B + 3 (A + q)) 2^-24
 // The exponential adds 2^-22 and 2^-24 q of the difference that it is taken of, the additions of weights 2^-24 each.
 // Mass, number and largest of a row's weights, and the mass of those at most ROW_FLOOR.
 struct RowSums {
@@ -783,7 +783,7 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 slope = 3.f * u24;
                 const float steps = (float)((P.d + 15) / 16), cut_off = P.dtype == SKB_BF16 ? 10.5f : 2.f,
                             joins = P.dtype == SKB_BF16 ? (float)((P.d - 1) / DOTS_BF16_PART) : 0.f;
-                fixed = u24 * (2.f * k2 * (cut_off * steps * sqrtf(xn.y) * S.y_prefix + (7.f + joins) * bound) + 3.f * A);
+                fixed = u24 * (2.f * k2 * (cut_off * steps * sqrtf(xn.y) * S.y_prefix + (3.f + joins) * bound) + 3.f * A);
             } else {
                 slope = (float)(P.d + 6) * u24;
                 fixed = slope * A;
