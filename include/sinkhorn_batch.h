@@ -456,17 +456,21 @@ skb_status sinkhorn_cloud4_dots(const void *x, const void *y, int W, int n, int 
  * Settings by lane, device arrays [W] that may each be null:
  *   temperature  fp32, T >= 0; 0: the largest weight alone (at T = 1)           null: 1
  *   top_k        int, the k largest weights, 0: all                             null: 0
- *   top_p        fp32, the shortest head of the weights in falling order whose sum is >= top_p times the sum of what
+ *   top_p        fp32, > 0, the shortest head of the weights in falling order whose sum is >= top_p times the sum of what
  *                top_k left, at least one; 1 and more: all                      null: 1
  *   min_p        fp32 in [0, 1], of what is left the weights >= min_p           null: 0
  * Equal weights are in the order of their indices.  For each of the `draws` numbers u [W, n, draws] in [0, 1) of a row,
  *   index [W, n, draws]  the smallest j whose kept weights up to and with j sum to more than u times all kept weights
  *   logp  [W, n, draws]  fp32, may be null: log(w_ij / sum of the kept weights)
- *                        (rounded to fp32; besides, exponents z_ij below 48 are good to (d + 6) 2^-24 of themselves, larger ones to
- *                        fp32's last place of their distance from the row's largest; those from products, bf16 and 4-bit clouds
- *                        of d >= 64, to at most 40 2^-23 of 2 |x_i| |y_j| / (eps T), as a rule a tenth of that)
+ *                        (rounded to fp32; besides, with A the distance, in powers of two, of the row's largest weight from
+ *                        exp(max g / (eps T)): exponents are good to (d + 6) 2^-24 (A + 22) where A is below 48 and 4096 / (d + 6);
+ *                        from there on, those that weigh a sixteenth of the row and those drawn, and above 48 all that weigh 2^-22 of the
+ *                        largest, to fp32's last place of their distance from the largest.  Those from products, bf16 and 4-bit clouds of
+ *                        d >= 64, to at most 40 2^-23 of 2 |x_i| |y_j| / (eps T), as a rule a tenth of that.  Up to 2^-20
+ *                        of the weights, those below 2^-24 of the largest, may be missing from the sum)
  * Indices are those of float64 arithmetic (rows that fp32 cannot decide are decided again).  -1, and NaN for logp: a
- * row without targets, with a NaN or an infinite exponent; a u outside [0, 1); every row of a lane whose settings or eps are not valid.
+ * row without targets, with an exponent that is NaN or plus infinity (one of minus infinity is a weight of zero); a u outside
+ * [0, 1); every row of a lane whose settings or eps are not valid.
  *   x [W, n, d], y [W, m, d]  of cfg->xy_dtype (4-bit clouds: the values they stand for), 16-byte aligned, 4-bit clouds 256
  *   g [W, m] float64, eps [W] fp32, device
  * d <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on cfg->stream of the current device and returns; the workspace (device,

@@ -46,6 +46,10 @@ constexpr float ROW_TAIL = 5.9604645e-8f;            // 2^-24: weights that a ro
 // 48 on (11 us more), 1e-7 from 16 on.  2 lanes of 8192 x 8192, d = 3: 613 us and 8e-7 without, 768 us and 4e-8 so.  From 16 on
 // rows of exponents of some tens take part, too: 256 lanes of 512 x 512, d = 15, threefold the time, for 2e-7 without.
 constexpr float DRAW_FAR = 48.f;
+// Deep rows lose as much from smaller exponents on, (d + 6) 2^-24 of them.  Up to 48 only what counts is formed again, entries above a sixteenth of the
+// row and those drawn: 8 lanes of 144 x 739, d = 128, exponents of some 40: error 1.7e-6 without, 1.5e-7 so; 8 lanes of 1024 x 1024, d = 128,
+// exponents of some 29, of which those above 30 take part: 612 us, 524 without; half the limit 721, and with all entries 1950.
+constexpr float DRAW_FAR_SUMS = 4096.f;
 // Products that are held at a time.  64 lanes of 1024 x 1024 x 512: 843 us by 64 MB, which stay in the L2 cache, 780 by 128 MB,
 // 743 all at once: the rows that are formed again are then one launch, too.
 constexpr size_t DRAW_DOTS_BYTES = (size_t)512 << 20;
@@ -57,6 +61,7 @@ struct Draw {
     const float *eps, *temperature, *top_p, *min_p, *u;
     const int *top_k;
     const int *status;                               // of a batch's lanes, or null
+    float far;                                       // rows whose largest exponent is above have log probabilities from their points
     int *index;
     float *logp;
     int dtype, W, n, m, d, S, mp;
@@ -534,21 +539,29 @@ __device__ __forceinline__ float exact_gap(const Draw &P, double k2, int wl, con
     }
     return (float)(fma(-k2, c, h) - base);
 }
-// Log probabilities of a row's draws once more, entries above ROW_FLOOR from their points; w: weights, kept from tau on.  The
-// group's last threads have the draws, so that in a group of several warps they need not wait for the sum.
+// Log probabilities of a row's draws once more, heavy entries from their points; w: weights, kept from tau on; A: the largest exponent.  Heavy
+// are those above ROW_FLOOR, up to DRAW_FAR those above a sixteenth of the row (the others' errors add up to less than one's, being
+// independent).  The group's last threads have the draws, so that in a group of several warps they need not wait for the sum.
 __device__ __forceinline__ void exact_logs(const Draw &P, double k2, int wl, size_t row, const RowGroup &G, double base, const float *nx, int step, const float *w,
-                                           int len, const unsigned short *where, float tau)
+                                           int len, const unsigned short *where, float tau, float A)
 {
     const int first = G.nt - 1 - G.t;
     double mass = 0.0;
-    float gap = 0.f;
+    float gap = 0.f, heavy = ROW_FLOOR;
     int j = first < P.S ? P.index[row * P.S + first] : -1, unused = 0;
     if (j >= 0) gap = exact_gap(P, k2, wl, nx, step, base, j);
+    if (A <= DRAW_FAR) {
+        double all = 0.0;
+#pragma unroll 1
+        for (int q = G.t; q < len; q += G.nt) all += quick_kept(w[q], tau) ? (double)w[q] : 0.0;
+        G.add(all, unused);
+        heavy = fmaxf(heavy, (float)all * 0.0625f);
+    }
 #pragma unroll 1
     for (int q = G.t; q < len; q += G.nt) {
         float v = w[q];
         if (!quick_kept(v, tau)) continue;
-        if (v > ROW_FLOOR) v = ex2_fast(exact_gap(P, k2, wl, nx, step, base, where ? where[q] : q));
+        if (v > heavy) v = ex2_fast(exact_gap(P, k2, wl, nx, step, base, where ? where[q] : q));
         mass += (double)v;
     }
     G.add(mass, unused);
@@ -617,7 +630,7 @@ __device__ __forceinline__ bool group_all(const RowGroup &G, bool v, int &turn)
 }
 
 // A row once more: what weighs more than ROW_FLOOR to fp32's last place, what does not is `off` of itself off.  x: -x, `step`
-// apart (differences), or room for a row (products), whose bound is `bound`.  A row that is a list of n entries, columns
+// apart (differences), or room for a row (products), whose bound is `bound` (differences: the row's largest exponent).  A row that is a list of n entries, columns
 // `where`, has a mass `tail` besides; `loose` is the mass of entries among which a cut was left out.  A row of which only the
 // logarithms are to be formed again has its cut in `tau`, the others a negative one.
 template <bool DOTS>
@@ -626,7 +639,7 @@ __device__ __noinline__ bool again(const Draw &P, double k2, RowCuts cuts, int w
 {
     const double *hn = P.hn + (size_t)wl * P.mp;
     if (!DOTS && tau >= 0.f) {
-        exact_logs(P, k2, wl, row, G, base, x, step, w, len, where, tau);
+        exact_logs(P, k2, wl, row, G, base, x, step, w, len, where, tau, bound);
         return true;
     }
     if (DOTS) {
@@ -896,10 +909,10 @@ __device__ __forceinline__ void do_row(const Draw &P, const LaneState &S, size_t
                 if (!sure && DOTS && LATER) {
                     if (G.t == 0) P.later[atomicAdd(P.later_n, 1u)] = (long long)row;
                     sure = true;
-                } else if (!sure || (!DOTS && P.logp && A > DRAW_FAR)) {
+                } else if (!sure || (!DOTS && P.logp && A > P.far)) {
                     // once more, with better weights for what counts
                     G.sync();
-                    sure = again<DOTS>(P, S.L.k2, {k, S.L.cuts.p, r_min}, S.lane, row, G, S.h_top + (double)top, off, bound, M.x, M.step, const_cast<float *>(r), len,
+                    sure = again<DOTS>(P, S.L.k2, {k, S.L.cuts.p, r_min}, S.lane, row, G, S.h_top + (double)top, off, DOTS ? bound : A, M.x, M.step, const_cast<float *>(r), len,
                                        sparse ? M.where : nullptr, (int)heavy, sparse ? f[2] : 0.f, loose, M.tiles, M.bytes, sure ? cut.tau : -1.f);
                     sure = group_all(G, sure, turn);
                 }
@@ -1255,6 +1268,7 @@ Draw problem(const skb_draw_config *c)
     Draw P = {};
     P.dtype = c->xy_dtype; P.W = c->W; P.n = c->n; P.m = c->m; P.d = c->d; P.S = c->draws;
     P.mp = (c->m + ROW_TILE - 1) / ROW_TILE * ROW_TILE;
+    P.far = std::min(DRAW_FAR, DRAW_FAR_SUMS / (float)(c->d + 6));
     P.temperature = c->temperature; P.top_k = c->top_k; P.top_p = c->top_p; P.min_p = c->min_p;
     return P;
 }

@@ -519,3 +519,30 @@ def test_log_probabilities_on_both_sides_of_the_border_of_large_exponents(B, sha
     off = np.abs(lp.cpu().numpy() - wlp)
     assert (off <= bound).all(), (off / bound).max()
     assert (A > 48.01).any() and (A < 48).any()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [96, 128, 333, 1000])
+def test_log_probabilities_of_deep_fp32_clouds(B, d):
+    # Largest exponents between 4096 / (d + 6) and 48, a few targets of about the same weight: entries above a sixteenth and those drawn are
+    # formed from their points in double.  The drawn one's difference and the sum's logarithm are of a few units (below 8) and round to
+    # 2^-24 of that each, weights of the sum are good to 2^-22 and it to 2^-24; log2 and the product to three roundings of 8.
+    import torch
+    W, n, m = 6, 30, 8
+    rng = np.random.default_rng(d)
+    x = rng.standard_normal((W, n, d)) / math.sqrt(d)
+    y = (rng.standard_normal((W, 1, d)) + 0.01 * rng.standard_normal((W, m, d))) / math.sqrt(d)
+    x, y = x.astype(np.float32), y.astype(np.float32)
+    g, eps = np.zeros((W, m)), np.full(W, 0.072, np.float32)
+    u = rng.random((W, n, 2), np.float32)
+    f = lambda v: torch.as_tensor(v).cuda()
+    idx, lp = B.plan_draw(f(x), f(y), f(g), f(eps), f(u), logp=True)
+    want, wlp = reference(x.astype(np.float64), y.astype(np.float64), g, eps, u.astype(np.float64))
+    np.testing.assert_array_equal(idx.cpu().numpy(), want)
+    z = -((x[:, :, None, :].astype(np.float64) - y[:, None]) ** 2).sum(3) / 0.072 / math.log(2)
+    A = -z.max(2)
+    w = np.exp2(z - z.max(2, keepdims=True))
+    rows = (A > 4100 / (d + 6)) & (A < 48) & ((w / w.sum(2, keepdims=True)).min(2) > 0.07)
+    assert rows.sum() > 20
+    off = np.abs(lp.cpu().numpy() - wlp)[rows]
+    assert off.max() <= 2.0 ** -22 + 2.0 ** -24 + 5 * 8 * 2.0 ** -24, off.max()
