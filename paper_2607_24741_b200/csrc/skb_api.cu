@@ -579,6 +579,7 @@ extern "C" skb_status sinkhorn_batch_refill(skb_batch *h, const void *x, const v
     if (!h) return SKB_ERR_NULL;
     if (!x || !y || !a || !b || !eps) return fail(h, SKB_ERR_NULL, "x, y, a, b and eps are required");
     if (count < 1) return fail(h, SKB_ERR_VALUE, "count must be >= 1");
+    if (h->packed && (((uintptr_t)x | (uintptr_t)y) & 255u) != 0) return fail(h, SKB_ERR_VALUE, "4-bit clouds must be 256-byte aligned");
     if (h->cfg.mode != SKB_ACTIVE) return fail(h, SKB_ERR_STATE, "finished lanes can only be replaced in ACTIVE mode");
     if (h->lanes_used + count > h->dev.L) {
         char buf[128];

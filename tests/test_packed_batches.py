@@ -306,3 +306,25 @@ def test_what_a_batch_on_another_stream_reads_and_writes_is_the_callers(B, call)
     assert bool((out[0][0] != 0).any())
     for a, b in zip(*out):
         assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_a_refill_of_packed_clouds_that_is_refused_changes_nothing(B):
+    # a misaligned cloud is seen before the values of the other one take the place of those that the plan is applied with
+    import torch
+    W, n, m, d = 2, 60, 50, 40
+    x, y, a, b, eps = problem(9, 2 * W, n, m, d)
+    x4, y4 = B.cloud4_pack(x[:W], "mx4"), B.cloud4_pack(y[:W], "mx4")
+    sb = B.SinkhornBatch(x4, y4, a[:W], b[:W], eps[:W], 1e-3, lane_capacity=2 * W)
+    sb.drain()
+    v = torch.randn(W, m, 3, device="cuda")
+    want = sb.apply_plan(v)
+    other = B.cloud4_pack(x[W:], "mx4")
+    room = torch.zeros(y4.buffer.numel() + 256, dtype=torch.uint8, device="cuda")
+    first = ctypes.c_int(-1)
+    ptr = lambda t, off=0: ctypes.c_void_p(t.data_ptr() + off)
+    for bad in ((0, 64), (64, 0)):
+        clouds = (ptr(other.buffer if bad[0] == 0 else room, bad[0]), ptr(room, bad[1]))
+        assert B.lib.sinkhorn_batch_refill(sb.h, *clouds, ptr(a), ptr(b), ptr(eps), W, ctypes.byref(first)) == 3 and first.value == -1
+        assert torch.equal(sb.apply_plan(v), want)
+    sb.close()
