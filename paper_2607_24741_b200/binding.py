@@ -278,7 +278,8 @@ class Cloud4:
 
 def cloud4_pack(v, format="mx4", values=None):
     """Rounds v [W, npts, d] (float32 or bfloat16, CUDA) to 4 bits, format "mx4" or "nv4"; returns a Cloud4, or with
-    `values` (torch.float32 or torch.bfloat16) the pair of it and the values that it stands for."""
+    `values` (torch.float32 or torch.bfloat16) the pair of it and the values that it stands for.  No gradient is recorded: a training
+    step that wants one passes it through the rounding itself, v + (values - v).detach()."""
     if v.dim() != 3 or not v.is_cuda or v.dtype not in DTYPES:
         raise ValueError("v must be a float32 or bfloat16 CUDA tensor [W, npts, d]")
     if format not in FORMATS:

@@ -18,11 +18,12 @@
 // weight to a per cent, are decided in float64 alone, weights in the workspace.
 //
 // What bounds it: instructions of the searches and draws, not the exponentials.  256 lanes of 512 x 512, d = 15, top-p (131072
-// rows, 67 M pairs): 0.67 ms, some 2900 instructions of a warp a row, of which forming and exponentials are a fifth (15 us at
+// rows, 67 M pairs): 0.70 ms, some 2900 instructions of a warp a row, of which forming and exponentials are a fifth (15 us at
 // the rate of the exponentials); issue slots are used to 54 % and neither 16 nor 32 warps an SM instead of 24 change the time.
 // 2 lanes of 8192 x 8192, d = 3, top-k 16, four draws: 0.77 ms, a list of some 50 entries a row, latencies of one warp's search between
-// the block's barriers, 0.15 of it log probabilities of large exponents.  64 lanes of 1024 x 1024, d = 512 (bf16), top-p: 0.74 ms, of which products 0.12, rows 0.30, rows
-// formed again 0.15 (2.8 % of them), norms 0.04, float64 0.09 (22 rows, a cold kernel's latency).
+// the block's barriers, 0.15 of it log probabilities of large exponents.  64 lanes of 1024 x 1024, d = 512 (bf16), top-p: 0.75 ms, of which products 0.18, rows 0.28, rows
+// formed again 0.19 (2.7 % of them), norms 0.04, float64 0.09 (some ten rows, a cold kernel's latency).  Deep fp32 clouds, without tensor cores: 64 lanes of
+// 1024 x 1024, d = 512, 25 ms.
 #include <cuda_runtime.h>
 #include <math_constants.h>
 #include <algorithm>
@@ -44,14 +45,15 @@ constexpr float ROW_TAIL = 5.9604645e-8f;            // 2^-24: weights that a ro
 // Rows whose largest exponent is at least this: fp32's last place of exponents shows in log probabilities, which are formed from the points
 // in double where they are wanted.  Their error (rms over rms), 96 lanes of 100 x 77, d = 8, eps from 0.01: 1e-5 without, 4e-7 from
 // 48 on (11 us more), 1e-7 from 16 on.  2 lanes of 8192 x 8192, d = 3: 613 us and 8e-7 without, 768 us and 4e-8 so.  From 16 on
-// rows of exponents of some tens take part, too: 256 lanes of 512 x 512, d = 15, threefold the time, for 2e-7 without.
+// rows of exponents of some tens take part, too: 256 lanes of 512 x 512, d = 15, threefold the time (twofold with heavy entries alone, below), for
+// 2e-7 without.
 constexpr float DRAW_FAR = 48.f;
 // Deep rows lose as much from smaller exponents on, (d + 6) 2^-24 of them.  Up to 48 only what counts is formed again, entries above a sixteenth of the
 // row and those drawn: 8 lanes of 144 x 739, d = 128, exponents of some 40: error 1.7e-6 without, 1.5e-7 so; 8 lanes of 1024 x 1024, d = 128,
 // exponents of some 29, of which those above 30 take part: 612 us, 524 without; half the limit 721, and with all entries 1950.
 constexpr float DRAW_FAR_SUMS = 4096.f;
 // Products that are held at a time.  64 lanes of 1024 x 1024 x 512: 843 us by 64 MB, which stay in the L2 cache, 780 by 128 MB,
-// 743 all at once: the rows that are formed again are then one launch, too.
+// 743 all at once (with products of one accumulator; 751 so now): the rows that are formed again are then one launch, too.
 constexpr size_t DRAW_DOTS_BYTES = (size_t)512 << 20;
 
 struct Draw {
