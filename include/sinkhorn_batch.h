@@ -496,7 +496,8 @@ skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, con
  * Partners drawn from the plan of a finished batch: sinkhorn_plan_draw with the potentials that every lane finished with,
  * partners of the sources (side 0, u and the outputs [W, n, draws]) or of the targets (side 1, [W, m, draws]).
  *   x, y, eps: the arrays the batch was created from; cfg: W, n, m, d and xy_dtype of the batch, cfg->stream is not read
- *   (the batch's is used), a workspace of sinkhorn_plan_draw_workspace_bytes(cfg), for side 1 with n and m exchanged.
+ *   (the batch's is used: everything is read and written there), a workspace of sinkhorn_plan_draw_workspace_bytes(cfg), for
+ *   side 1 with n and m exchanged.
  * Valid once every lane has finished (SKB_ERR_STATE before that, and for batches whose lanes were replaced); synchronises
  * to check that.  A lane that went non-finite gives no draws (-1).
  */
