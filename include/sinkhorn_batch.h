@@ -504,7 +504,52 @@ skb_status sinkhorn_plan_draw(const void *x, const void *y, const double *g, con
 skb_status sinkhorn_batch_draw_plan(skb_batch *h, const void *x, const void *y, const float *eps, const float *u, int side,
                                     const skb_draw_config *cfg, int *index, float *logp);
 
-/* Text of the calling thread's last failed sinkhorn_cloud4_* or sinkhorn_plan_draw call (empty after a successful one). */
+/*
+ * Clouds held in 8-bit floating point with a power of two for each block of 128 dimensions of a point: half of bf16's memory, for
+ * banks of embeddings that are searched, scored and mapped to.  The points of a cloud [W, npts, d], 1 <= d <= 1024, become one buffer of
+ * sinkhorn_cloud8_bytes(W, npts, d) bytes (0: a bad argument), device memory of the caller, 256-byte aligned, of these parts, each
+ * padded to 256 bytes:
+ *   codes   [W npts][32 ceil(d/32)] bytes, e4m3; code 0 past the last dimension
+ *   scales  [W npts][4 ceil(d/512)] bytes, e8m0, one for 128 dimensions; unused bytes are 0
+ *   norms   [W npts] floats, the squared length of the point that codes and scales stand for
+ * and stand for code * scale, which fp32 and bf16 hold exactly.
+ *
+ * sinkhorn_cloud8_pack rounds v [W, npts, d] (SKB_F32 or SKB_BF16): a block's scale is the smallest power of two from 2^-100 on that
+ * its largest magnitude is at most 448 times of, a code v / scale to the nearest of e4m3, halves to the even code (240 at
+ * most where the scale is 2^120: no value passes fp32's range).  A point with an infinite or NaN value becomes NaN as a whole.  A norm is good to
+ * 17 2^-24 of itself, infinite past fp32's range.
+ *   values   may be null; else [W, npts, d] of values_dtype (SKB_F32 or SKB_BF16): what the buffer stands for, by the same launch
+ * sinkhorn_cloud8_unpack writes the values of a buffer.  Both enqueue one kernel on `stream` of the current device.
+ */
+size_t sinkhorn_cloud8_bytes(int W, int npts, int d);
+skb_status sinkhorn_cloud8_pack(const void *v, int v_dtype, int W, int npts, int d, void *cloud, void *values, int values_dtype, void *stream);
+skb_status sinkhorn_cloud8_unpack(const void *cloud, int W, int npts, int d, void *values, int values_dtype, void *stream);
+/*
+ * Products of two 8-bit clouds, out[t, i, j] = x_ti . y_tj of the values they stand for: x [W, n, d], y [W, m, d] buffers of
+ * sinkhorn_cloud8_pack, out [W, n, m] fp32, on the block-scaled tensor cores with fp32 accumulation.  A point that is NaN gives NaN in its row
+ * or column.  One kernel on `stream` of the current device; out is written 16 bytes at a time where m is a multiple of 4 and out
+ * 16-byte aligned.
+ */
+skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int m, int d, float *out, void *stream);
+/*
+ * The loss of scores against the rows of a coupling, and its gradient: what teaches a network to give the partners that the solver
+ * gives.  Row i of scores [rows, m] (dtype SKB_F32 or SKB_BF16, `ld` elements from row to row) has k named entries index [rows, k]:
+ * draws from the plan's row (sinkhorn_plan_draw's indices as they are), or a teacher's top entries with their logits [rows, k] fp32.
+ * With p = softmax(scores_i / T) over the row, q = softmax(logits_i / T) over the named entries (logits null: all alike),
+ *      loss_i = sum_k q_k (log q_k - log p_index(k))                                                       [rows] fp32
+ *      grad_ij = weight_i (p_ij - sum of the q_k with index(k) = j) / T, the gradient of sum_i weight_i loss_i     [rows, m]
+ * An index outside 0 .. m - 1 names nothing; an entry may be named more than once.  A row that names nothing, or whose logits are all
+ * minus infinity, has loss 0 and gradient 0 whatever its scores.  Scores of minus infinity have p = 0, and one that is named with
+ * q > 0 makes the loss infinite (the gradient stays finite); a NaN, plus infinity or a row of minus infinity makes them NaN.
+ *   weight  [rows] fp32, may be null: 1
+ *   grad    may be null, of the scores' type, `ldg` elements from row to row; may be scores itself
+ * T from 1e-30 to 1e30, k <= 256, m <= 262143, rows < 2^31.  Sums are fp32, in an order that does not change from call to call.  One kernel on `stream` of
+ * the current device, which reads a row once (longer ones than 131068 of fp32 or 262136 of bf16 twice).
+ */
+skb_status sinkhorn_plan_loss(const void *scores, int dtype, long long rows, int m, long long ld, const int *index, const float *logits, int k,
+                              float temperature, const float *weight, float *loss, void *grad, long long ldg, void *stream);
+
+/* Text of the calling thread's last failed sinkhorn_cloud4_*, sinkhorn_cloud8_*, sinkhorn_plan_draw or sinkhorn_plan_loss call (empty after a successful one). */
 const char *sinkhorn_operator_last_error(void);
 
 /* Host string describing the last error on this handle (or, when h is null, of the calling

@@ -37,6 +37,7 @@ PHASES = ("create", "f_leg", "column_check", "plan", "emit_move", "g_leg")
 # entry points outside the sinkhorn_batch_* family
 EXTRA_EXPORTS = ("sinkhorn_row_residual_static", "sinkhorn_row_residual_static_last_error",
                  "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_cloud4_dots", "sinkhorn_plan_draw_workspace_bytes", "sinkhorn_plan_draw",
+                 "sinkhorn_cloud8_bytes", "sinkhorn_cloud8_pack", "sinkhorn_cloud8_unpack", "sinkhorn_cloud8_dots", "sinkhorn_plan_loss",
                  "sinkhorn_operator_last_error")
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 FORMATS = {"mx4": 2, "nv4": 3}
@@ -116,6 +117,13 @@ def _load():
     lib.sinkhorn_cloud4_pack.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp, ci, vp]
     lib.sinkhorn_cloud4_unpack.argtypes = [vp, ci, ci, ci, ci, vp, ci, vp]
     lib.sinkhorn_cloud4_dots.argtypes = [vp, vp, ci, ci, ci, ci, ci, vp, vp]
+    cl = ctypes.c_longlong
+    lib.sinkhorn_cloud8_bytes.restype = ctypes.c_size_t
+    lib.sinkhorn_cloud8_bytes.argtypes = [ci, ci, ci]
+    lib.sinkhorn_cloud8_pack.argtypes = [vp, ci, ci, ci, ci, vp, vp, ci, vp]
+    lib.sinkhorn_cloud8_unpack.argtypes = [vp, ci, ci, ci, vp, ci, vp]
+    lib.sinkhorn_cloud8_dots.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp]
+    lib.sinkhorn_plan_loss.argtypes = [vp, ci, cl, ci, cl, vp, vp, ci, ctypes.c_float, vp, vp, vp, cl, vp]
     drawp = ctypes.POINTER(SkbDrawConfig)
     lib.sinkhorn_plan_draw_workspace_bytes.restype = ctypes.c_size_t
     lib.sinkhorn_plan_draw_workspace_bytes.argtypes = [drawp]
@@ -317,6 +325,143 @@ def cloud4_dots(x, y, out=None):
     return out
 
 
+def _cloud8_bytes(W, npts, d):
+    """sinkhorn_cloud8_bytes for a valid shape, 0 otherwise."""
+    if min(W, npts, d) < 1 or d > 1024 or W * npts > 0x7fffffff:
+        return 0
+    pad = lambda b: (b + 255) // 256 * 256
+    rows = W * npts
+    return pad(rows * ((d + 31) // 32 * 32)) + pad(rows * ((d + 511) // 512 * 4)) + pad(rows * 4)
+
+
+class Cloud8:
+    """A cloud [W, npts, d] held in 8 bits: `buffer` as sinkhorn_cloud8_pack lays it out (a uint8 CUDA tensor)."""
+
+    def __init__(self, buffer, W, npts, d):
+        need = _cloud8_bytes(W, npts, d)
+        if need == 0:
+            raise ValueError("W, npts and d must be >= 1, d at most 1024")
+        if buffer.dtype != torch.uint8 or not buffer.is_cuda or not buffer.is_contiguous() or buffer.numel() < need:
+            raise ValueError(f"buffer must be a contiguous uint8 CUDA tensor of at least {need} bytes")
+        if buffer.data_ptr() % 256:
+            raise ValueError("buffer must be 256-byte aligned")
+        self.buffer, self.W, self.npts, self.d = buffer, W, npts, d
+
+    @property
+    def shape(self):
+        return (self.W, self.npts, self.d)
+
+    @property
+    def device(self):
+        return self.buffer.device
+
+    def values(self, dtype=torch.float32):
+        """What the cloud stands for, [W, npts, d] float32 or bfloat16 (both exact)."""
+        if dtype not in DTYPES:
+            raise ValueError("dtype must be float32 or bfloat16")
+        with _on(self.device):
+            out = torch.empty(self.shape, dtype=dtype, device=self.device)
+            _check_op(lib.sinkhorn_cloud8_unpack(_ptr(self.buffer), self.W, self.npts, self.d, _ptr(out), DTYPES[dtype], _stream(self.device)))
+        return out
+
+
+def cloud8_pack(v, values=None):
+    """Rounds v [W, npts, d] (float32 or bfloat16, CUDA) to 8 bits with a power of two for each block of 128 dimensions of a point;
+    returns a Cloud8, or with `values` (torch.float32 or torch.bfloat16) the pair of it and the values that it stands for.  No gradient is
+    recorded: a training step that wants one passes it through the rounding itself, v + (values - v).detach()."""
+    if v.dim() != 3 or not v.is_cuda or v.dtype not in DTYPES:
+        raise ValueError("v must be a float32 or bfloat16 CUDA tensor [W, npts, d]")
+    if values is not None and values not in DTYPES:
+        raise ValueError("values must be torch.float32 or torch.bfloat16")
+    v = v.contiguous()
+    W, npts, d = v.shape
+    need = _cloud8_bytes(W, npts, d)
+    if need == 0:
+        raise ValueError("W, npts and d must be >= 1, d at most 1024")
+    with _on(v.device):
+        buffer = torch.empty(need, dtype=torch.uint8, device=v.device)
+        out = None if values is None else torch.empty(v.shape, dtype=values, device=v.device)
+        _check_op(lib.sinkhorn_cloud8_pack(_ptr(v), DTYPES[v.dtype], W, npts, d, _ptr(buffer), _ptr(out), DTYPES.get(values, 0), _stream(v.device)))
+    cloud = Cloud8(buffer, W, npts, d)
+    return cloud if values is None else (cloud, out)
+
+
+def cloud8_dots(x, y, out=None):
+    """x_ti . y_tj of two Cloud8, [W, n, d] and [W, m, d]: float32 [W, n, m]."""
+    if not isinstance(x, Cloud8) or not isinstance(y, Cloud8):
+        raise ValueError("x and y must be Cloud8")
+    if x.W != y.W or x.d != y.d or x.device != y.device:
+        raise ValueError("x and y must have one W, d and device")
+    shape = (x.W, x.npts, y.npts)
+    if out is not None and (out.dtype != torch.float32 or out.device != x.device or tuple(out.shape) != shape or not out.is_contiguous()):
+        raise ValueError("out must be a contiguous float32 tensor [W, n, m] on the clouds' device")
+    with _on(x.device):
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=x.device)
+        _check_op(lib.sinkhorn_cloud8_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, _ptr(out), _stream(x.device)))
+    return out
+
+
+def _rows_of(t):
+    """Row stride of a tensor [..., m] whose rows are evenly spaced and whose entries lie next to each other; None for others."""
+    m = t.shape[-1]
+    if t.numel() == 0 or (m > 1 and t.stride(-1) != 1):
+        return None
+    size, stride = 1, None                         # rows so far, elements from row to row
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if stride is None:
+            stride = s
+        elif s != stride * size:
+            return None
+        size *= n
+    stride = m if stride is None else stride
+    return stride if stride >= m else None
+
+
+def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=False):
+    """The loss of scores [..., m] (float32 or bfloat16, CUDA) against the rows of a coupling of which entries are named: index
+    [..., k] or [...] int32, draws as plan_draw gives them (-1 names nothing), or a teacher's top entries with their `logits` [..., k] float32.
+    A row's loss is sum_k q_k (log q_k - log p_index(k)), p the softmax of its scores over the temperature, q that of its logits (None: all
+    alike); see sinkhorn_plan_loss in the header.  Returns the rows' losses [...] float32; with `grad` also the gradient of the sum of
+    weight [...] float32 (None: 1) times loss, [..., m] of the scores' type.  grad=scores writes it in their place, another
+    tensor like them there.  Rows may be spaced out (a slice of wider ones); no autograd graph is recorded: scores.backward(gradient)
+    continues from it."""
+    if not torch.is_tensor(scores) or not scores.is_cuda or scores.dtype not in DTYPES or scores.dim() < 1:
+        raise ValueError("scores must be a float32 or bfloat16 CUDA tensor [..., m]")
+    lead, m, device = scores.shape[:-1], scores.shape[-1], scores.device
+    if torch.is_tensor(index) and index.shape == lead:              # one entry a row
+        index, logits = index.unsqueeze(-1), logits.unsqueeze(-1) if torch.is_tensor(logits) and logits.shape == lead else logits
+    if not torch.is_tensor(index) or index.dtype != torch.int32 or index.device != device or index.dim() != scores.dim() or index.shape[:-1] != lead:
+        raise ValueError("index must be an int32 tensor [..., k] on the scores' device")
+    if logits is not None and (not torch.is_tensor(logits) or logits.dtype != torch.float32 or logits.device != device or logits.shape != index.shape):
+        raise ValueError("logits must be a float32 tensor of index's shape on the scores' device")
+    if weight is not None and (not torch.is_tensor(weight) or weight.dtype != torch.float32 or weight.device != device or weight.shape != lead):
+        raise ValueError("weight must be a float32 tensor [...] on the scores' device")
+    k, rows = index.shape[-1], lead.numel()
+    if rows < 1 or not 1 <= m <= 262143 or not 1 <= k <= 256:
+        raise ValueError("at least one row, m from 1 to 262143 and k from 1 to 256 are supported")
+    in_place = torch.is_tensor(grad)
+    if in_place and (grad.dtype != scores.dtype or grad.device != device or grad.shape != scores.shape or _rows_of(grad) is None):
+        raise ValueError("grad must be a tensor like the scores with evenly spaced rows")
+    ld = _rows_of(scores)
+    if ld is None:
+        if in_place and grad.data_ptr() == scores.data_ptr():
+            raise ValueError("scores whose rows are not evenly spaced cannot take the gradient")
+        scores = scores.detach().contiguous()
+        ld = m
+    index = index.contiguous()
+    logits = None if logits is None else logits.contiguous()
+    weight = None if weight is None else weight.contiguous()
+    with _on(device):
+        loss = torch.empty(lead, dtype=torch.float32, device=device)
+        out = grad if in_place else torch.empty(scores.shape, dtype=scores.dtype, device=device) if grad else None
+        _check_op(lib.sinkhorn_plan_loss(_ptr(scores), DTYPES[scores.dtype], rows, m, ld, _ptr(index), _ptr(logits), k, float(temperature), _ptr(weight),
+                                         _ptr(loss), _ptr(out), m if out is None or not in_place else _rows_of(out), _stream(device)))
+    return loss if out is None else (loss, out)
+
+
 def _raw(v):
     return v.buffer if isinstance(v, Cloud4) else v
 
@@ -325,8 +470,10 @@ def _cloud(v, name):
     """dtype, shape, pointer and the tensor to keep of a cloud: a tensor or a Cloud4."""
     if isinstance(v, Cloud4):
         return FORMATS[v.format], v.shape, v.buffer
+    if isinstance(v, Cloud8):
+        v = v.values(torch.bfloat16)
     if not torch.is_tensor(v) or not v.is_cuda or v.dim() != 3 or v.dtype not in DTYPES:
-        raise ValueError(f"{name} must be a float32 or bfloat16 CUDA tensor [W, points, d], or a Cloud4")
+        raise ValueError(f"{name} must be a float32 or bfloat16 CUDA tensor [W, points, d], a Cloud4 or a Cloud8")
     v = v.contiguous()
     if v.data_ptr() % 16:
         v = v.clone()
@@ -361,7 +508,7 @@ def _draw_out(cfg, u, logp):
 
 
 def plan_draw(x, y, g, eps, u, *, temperature=None, top_k=None, top_p=None, min_p=None, logp=False):
-    """Partners of x [W, n, d] among y [W, m, d] (tensors or Cloud4), drawn from the coupling's rows, softmax over j of
+    """Partners of x [W, n, d] among y [W, m, d] (tensors, Cloud4 or Cloud8), drawn from the coupling's rows, softmax over j of
     (g_j - |x_i - y_j|^2) / (eps T), one for each number of u [W, n] or [W, n, draws]; see sinkhorn_plan_draw in
     the header.  Settings are tensors [W].  Returns the indices (int32, u's shape), with `logp` also their log
     probabilities."""
@@ -406,7 +553,12 @@ class SinkhornBatch:
     def __init__(self, x, y, a, b, eps, tol, *, mode="active", compute="auto", max_iter=5000,
                  audit_every=1, tol_screen=0.0, column_split=0, cost_form=0, stream=None, guard_band=0.0,
                  lane_capacity=0):
-        self.format = x.format if isinstance(x, Cloud4) else None          # x and y may be clouds held in 4 bits
+        # x and y may be clouds held in 4 bits, or in 8, whose bf16 values the batch then keeps
+        if isinstance(x, Cloud8) != isinstance(y, Cloud8):
+            raise ValueError("x and y must both be Cloud8 or neither")
+        if isinstance(x, Cloud8):
+            x, y = x.values(torch.bfloat16), y.values(torch.bfloat16)
+        self.format = x.format if isinstance(x, Cloud4) else None
         if self.format is None:
             if isinstance(y, Cloud4):
                 raise ValueError("x and y must both be tensors or both be Cloud4")
@@ -508,6 +660,10 @@ class SinkhornBatch:
 
     def refill(self, x, y, a, b, eps) -> int:
         """New problems into the slots finished lanes have freed; returns their first lane number."""
+        if self.format is None:
+            x, y = (v.values(torch.bfloat16 if self.cfg.xy_dtype == 1 else torch.float32) if isinstance(v, Cloud8) else v for v in (x, y))
+        elif isinstance(x, Cloud8) or isinstance(y, Cloud8):
+            raise ValueError("x and y must be of the batch's storage type")
         if (x.format if isinstance(x, Cloud4) else None) != self.format or (y.format if isinstance(y, Cloud4) else None) != self.format:
             raise ValueError("x and y must be of the batch's storage type")
         a, b, eps = (t.contiguous() for t in (a, b, eps))

@@ -1,13 +1,14 @@
 // Products of two clouds, out[t, i, j] = x_ti . y_tj in fp32: 4-bit clouds by the block-scaled matrix instructions
-// (mx4: kind::mxf4, scales of 32 dimensions; nv4: kind::mxf4nvf4, scales of 16), bf16 clouds by kind::f16.
+// (mx4: kind::mxf4, scales of 32 dimensions; nv4: kind::mxf4nvf4, scales of 16), 8-bit clouds by kind::mxf8f6f4 (a scale of 128 dimensions
+// serves four instructions), bf16 clouds by kind::f16.
 //
 // The operands are small (a point of 512 dimensions in 4 bits is 272 bytes) and the result is not: 4 n m bytes a lane
 // bound the kernel (64 lanes of 1024 x 1024: 268 MB, 41 us at the measured copy rate; the 69 GFLOP would take 11 us at
 // four times the bf16 rate).  So the kernel is one persistent block an SM that always has a tile of results on its way out:
-//   warp 0     loads, by TMA: chunks of 128 bytes a point (256 dimensions in 4 bits, 64 in bf16), 128 points of x and of y,
+//   warp 0     loads, by TMA: chunks of 128 bytes a point (256 dimensions in 4 bits, 128 in 8, 64 in bf16), 128 points of x and of y,
 //              128-byte swizzle; points and dimensions past the end arrive as zeros
 //   warp 1     matrix instructions, one thread: four to a chunk into one of two accumulators of 128 x 128 in tensor memory
-//   warps 2-5  block scales (4-bit kinds): from the points' rows into the order that the matrix unit wants, through
+//   warps 2-5  block scales (all but bf16): from the points' rows into the order that the matrix unit wants, through
 //              shared memory; they are a sixteenth of the codes and their rows too short for TMA.  Two warps to an operand, each
 //              takes every other chunk, so that a chunk's load latency has two chunks' time
 //   warps 6-13 results: tensor memory -> registers -> 32 x 32 boxes in shared memory -> TMA stores, which clip ragged edges.
@@ -27,7 +28,7 @@
 #include <cuda_runtime.h>
 #include <string>
 
-#include "skb_cloud4.cuh"
+#include "skb_cloud8.cuh"
 #include "skb_operators.h"
 #include "skb_tmem.cuh"
 
@@ -38,12 +39,12 @@ constexpr int DT_BM = 128, DT_BN = 128;
 constexpr int DT_EPI = 8, DT_THREADS = (6 + DT_EPI) * 32, DT_STAGES = 4;
 constexpr uint32_t DT_TILE = 128 * 128;                  // bytes: 128 points, 128 bytes of each
 constexpr uint32_t DT_BOX = 32 * 32 * 4;                 // a box of results
-// chunks of an accumulator (4-bit kinds have at most four)
-template <int KIND> constexpr int DT_PART = KIND == SKB_BF16 ? DOTS_BF16_PART / 64 : 4;
+// chunks of an accumulator (4-bit kinds have at most four, 8-bit clouds eight)
+template <int KIND> constexpr int DT_PART = KIND == SKB_BF16 ? DOTS_BF16_PART / 64 : 8;
 constexpr int DT_SF_COL = 2 * DT_BN, DT_SF_STRIDE = 32;  // tensor memory: accumulators, then the scales of each stage
 
 struct Dots {
-    const uint8_t *sx, *sy;                               // scales (4-bit kinds)
+    const uint8_t *sx, *sy;                               // scales (all but bf16)
     const float *px, *py;                                 // points' powers of two (nv4)
     float *out;
     long long ldo, lane_out;                              // floats from row to row, from lane to lane
@@ -56,6 +57,7 @@ __device__ __forceinline__ constexpr uint32_t dots_idesc()
 {
     constexpr uint32_t shape = ((uint32_t)(DT_BN >> 3) << 17) | ((uint32_t)(DT_BM >> 4) << 24);
     if (KIND == SKB_BF16) return (1u << 4) | (1u << 7) | (1u << 10) | shape;             // D fp32, A and B bf16
+    if (KIND == FMT_MX8) return shape | 1u << 23;                                        // A and B e4m3; scales e8m0
     return (1u << 7) | (1u << 10) | shape | (KIND == SKB_MX4 ? 1u << 23 : 0u);           // A and B e2m1; scales e8m0 or e4m3
 }
 template <int KIND>
@@ -65,6 +67,10 @@ __device__ __forceinline__ void dots_mma(uint32_t acc, uint64_t a, uint64_t b, u
     else if constexpr (KIND == SKB_MX4)
         asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
                      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                     ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+    else if constexpr (KIND == FMT_MX8)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
                      ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
     else
         asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -131,7 +137,8 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                                                              const __grid_constant__ CUtensorMap tmo, const __grid_constant__ Dots P)
 {
     constexpr bool SCALED = KIND != SKB_BF16;
-    constexpr int WORDS = KIND == SKB_NV4 ? 4 : 2;               // words of scales that a point has in a chunk
+    // words of scales that a point has in a chunk; an 8-bit cloud's word is that of four chunks
+    constexpr int WORDS = KIND == SKB_NV4 ? 4 : KIND == FMT_MX8 ? 1 : 2;
     constexpr uint32_t SF = SCALED ? WORDS * 512 : 0;            // bytes of an operand's scales in a stage
     extern __shared__ __align__(1024) unsigned char smem_dyn[];
     __shared__ __align__(8) unsigned long long bars[3 * DT_STAGES + 5];
@@ -227,9 +234,10 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         if (32 * q >= left) break;
-                        const int word = KIND == SKB_NV4 ? q : q / 2;
-                        const uint32_t half = KIND == SKB_MX4 ? (uint32_t)(q & 1) * 2u : 0u;     // which two of a word's four scales
-                        dots_mma<KIND>(acc, da + 2 * q, db + 2 * q, dots_idesc<KIND>() | half << 29 | half << 4, sf + 4 * word, sf + 16 + 4 * word,
+                        const int word = KIND == SKB_NV4 ? q : KIND == FMT_MX8 ? 0 : q / 2;
+                        // which of a word's four scales: the first or second two, or the chunk's
+                        const uint32_t part = KIND == SKB_MX4 ? (uint32_t)(q & 1) * 2u : KIND == FMT_MX8 ? (uint32_t)(c & 3) : 0u;
+                        dots_mma<KIND>(acc, da + 2 * q, db + 2 * q, dots_idesc<KIND>() | part << 29 | part << 4, sf + 4 * word, sf + 16 + 4 * word,
                                        !starts || q != 0);
                     }
                     tc_commit(bar(EMPTY + s));
@@ -259,13 +267,14 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 const int p0 = op ? j0 : i0;
                 for (int c = 0; c < chunks; ++c, ++k) {
                     if ((int)(k & 1) != turn) continue;
+                    const int c0 = KIND == FMT_MX8 ? c / 4 : c * WORDS;
                     uint32_t v[4][WORDS];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const int p = p0 + lane + 32 * q;
                         const uint32_t *row = reinterpret_cast<const uint32_t *>(src + ((size_t)w * npts + min(p, npts - 1)) * P.sb);
 #pragma unroll
-                        for (int a = 0; a < WORDS; ++a) v[q][a] = p < npts && c * WORDS + a < words ? __ldg(row + c * WORDS + a) : 0u;
+                        for (int a = 0; a < WORDS; ++a) v[q][a] = p < npts && c0 + a < words ? __ldg(row + c0 + a) : 0u;
                     }
                     const int s = (int)(k % DT_STAGES);
                     ok = mbar_wait(bar(EMPTY + s), (uint32_t)((k / DT_STAGES) & 1) ^ 1u, &abort_flag);
@@ -448,7 +457,7 @@ bool make_map(CUtensorMap *tm, CUtensorMapDataType type, const void *base, cuuin
 template <int KIND>
 skb_status launch_kind(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &to, const Dots &P, int sms, cudaStream_t st)
 {
-    constexpr int sf = KIND == SKB_BF16 ? 0 : KIND == SKB_NV4 ? 2048 : 1024;
+    constexpr int sf = KIND == SKB_BF16 ? 0 : KIND == SKB_NV4 ? 2048 : KIND == FMT_MX8 ? 512 : 1024;
     constexpr int smem = DT_STAGES * (2 * (int)DT_TILE + 2 * sf) + 2 * DT_EPI * (int)DT_BOX + 1024;
     cudaFuncSetAttribute(dots_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     const long long tiles = (long long)P.W * ((P.no + DT_BM - 1) / DT_BM) * ((P.mo + DT_BN - 1) / DT_BN);
@@ -487,6 +496,7 @@ skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W,
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     if (dtype == SKB_BF16) return launch_kind<SKB_BF16>(tx, ty, to, P, sms, st);
     if (dtype == SKB_MX4) return launch_kind<SKB_MX4>(tx, ty, to, P, sms, st);
+    if (dtype == FMT_MX8) return launch_kind<FMT_MX8>(tx, ty, to, P, sms, st);
     return launch_kind<SKB_NV4>(tx, ty, to, P, sms, st);
 }
 

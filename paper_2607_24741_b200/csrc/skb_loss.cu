@@ -1,0 +1,333 @@
+// The loss of scores against the rows of a coupling, and its gradient: distillation of the entries that a teacher names.
+//
+// Row i has scores s_ij, p = softmax(s / T), and k named entries (draws from the plan's row, or its top entries with logits t),
+//      q = softmax(t / T) over the named entries,   loss_i = sum_k q_k (log q_k - log p_{j(k)}),
+//      d loss_i / d s_ij = (p_ij - sum of q_k over the k with j(k) = j) / T.
+//
+// One pass: a row is read once, 16 bytes a thread and vector, and stays in registers (up to 64 scores of bf16 or 32 of fp32 a
+// thread, raw) until its maximum and sum are known; then the gradient is written.  So memory bounds it.  Exponentials are taken twice,
+// against the thread's own maximum for the sum and the row's for the gradient: that is one barrier a row instead of two, and no fp32
+// copies in registers.  What a row is given goes by its length: a warp, four warps, 16 warps, or a cluster of up to eight blocks of
+// 16 warps, whose maxima and sums meet in distributed shared memory; rows longer than what a cluster's registers hold are read twice, the second time
+// from L2 (a row is at most 1 MB).  A row is reduced in a fixed order, so results do not change from call to call.
+//
+// The named entries' gradients are written after all others of the row, by the first of the entries that name a column, which adds up
+// the q of all that do: no atomics, any entry may be named any number of times.
+#include <cuda_runtime.h>
+#include <string>
+
+#include "skb_operators.h"
+
+namespace skb {
+namespace {
+
+constexpr int LS_MAX_K = 256;
+
+struct Loss {
+    const void *scores;
+    const int *index;
+    const float *logits, *weight;
+    float *loss;
+    void *grad;
+    long long rows, ld, ldg;                  // ld, ldg: elements from row to row
+    int m, k;
+    float inv_t, c;                           // 1 / T and log2(e) / T
+};
+
+__device__ __forceinline__ float ex2f(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// element e of a vector
+template <bool BF16> __device__ __forceinline__ float element(const uint4 &v, int e)
+{
+    const uint32_t w = BF16 ? (e < 4 ? (e < 2 ? v.x : v.y) : (e < 6 ? v.z : v.w)) : (e < 2 ? (e < 1 ? v.x : v.y) : (e < 3 ? v.z : v.w));
+    if (!BF16) return __uint_as_float(w);
+    return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// (maximum, sum of exponentials against it), both of none: (-inf, 0)
+struct __align__(8) Part {                   // (written to other blocks in one 8-byte store)
+    float m, s;
+};
+__device__ __forceinline__ Part join(Part a, Part b, float c)
+{
+    const float m = fmaxf(a.m, b.m), at = m == -INFINITY ? 0.f : m;
+    // (a sum beside a maximum of minus infinity is 0, or NaN, which stays)
+    return {m, a.s * ex2f((a.m - at) * c) + b.s * ex2f((b.m - at) * c)};
+}
+
+// TPR threads of each of C blocks to a row, V vectors in each thread's registers; V = 0: the row is read twice.
+template <bool BF16, int TPR, int V, int C>
+__global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) loss_kernel(const __grid_constant__ Loss P)
+{
+    constexpr int THREADS = TPR <= 128 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR / 32;
+    constexpr int E = BF16 ? 8 : 4;
+    using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
+    __shared__ int s_index[GROUPS][LS_MAX_K];
+    __shared__ float s_q[GROUPS][LS_MAX_K], s_score[GROUPS][LS_MAX_K];
+    __shared__ float s_total[GROUPS];
+    __shared__ Part s_part[GROUPS][WARPS], s_rank[C];
+    const int tid = threadIdx.x, group = tid / TPR, t = tid % TPR, lane = tid & 31, warp = t >> 5;
+    const int rank = C > 1 ? (int)(blockIdx.x % C) : 0;
+    const long long row = (long long)(blockIdx.x / C) * GROUPS + group;
+    if (row >= P.rows) return;                                   // whole groups: barriers below are a group's
+    auto group_sync = [&] {
+        if constexpr (TPR == 32) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
+    };
+    // (a block's shared memory may be written by another of its cluster once it has started)
+    if constexpr (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const T *src = (const T *)P.scores + (size_t)row * P.ld;
+    const int head = (int)((uintptr_t)src % 16 / sizeof(T)), end = head + P.m;      // the row, in elements from a 16-byte boundary on
+    const T *base = src - head;
+    const int nvec = (end + E - 1) / E;
+    auto load = [&](int j) {
+        if (j * E >= head && (j + 1) * E <= end) return *reinterpret_cast<const uint4 *>(base + (size_t)j * E);
+        uint4 r = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                       : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+        uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int at = j * E + e;
+            if (at < head || at >= end) continue;
+            const uint32_t bits = base[at];
+            if (BF16) w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | bits << 16 : (w[e / 2] & 0xffff0000u) | bits;
+            else w[e] = bits;
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
+    uint4 held[V ? V : 1];
+    if constexpr (V > 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = (v * C + rank) * TPR + t;
+            held[v] = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                           : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+            if (j < nvec) held[v] = load(j);
+        }
+    }
+    // the teacher: the first warp's, meanwhile
+    float tk[LS_MAX_K / 32], top = -INFINITY, total = 0.f;
+    if (warp == 0) {
+#pragma unroll
+        for (int a = 0; a < LS_MAX_K / 32; ++a) {
+            const int k = a * 32 + lane;
+            tk[a] = -INFINITY;
+            if (a * 32 >= P.k) continue;
+            if (k < P.k) {
+                const int j = P.index[(size_t)row * P.k + k];
+                const bool named = j >= 0 && j < P.m;
+                if (named) tk[a] = P.logits ? P.logits[(size_t)row * P.k + k] * P.inv_t : 0.f;
+                float s = 0.f;
+                if (named) s = BF16 ? __uint_as_float((uint32_t)src[j] << 16) : __uint_as_float((uint32_t)src[j]);
+                s_index[group][k] = named ? j : -1;
+                s_score[group][k] = s;
+            }
+            top = fmaxf(top, tk[a]);
+        }
+#pragma unroll
+        for (int off = 16; off; off /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        const float at = top == -INFINITY ? 0.f : top;
+#pragma unroll
+        for (int a = 0; a < LS_MAX_K / 32; ++a)
+            if (a * 32 < P.k) total += expf(tk[a] - at);
+#pragma unroll
+        for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
+#pragma unroll
+        for (int a = 0; a < LS_MAX_K / 32; ++a) {
+            const int k = a * 32 + lane;
+            if (a * 32 >= P.k) continue;
+            if (k < P.k) s_q[group][k] = total == 0.f ? 0.f : expf(tk[a] - at) / total;
+            tk[a] -= at;
+        }
+        if (lane == 0) s_total[group] = total;
+    }
+    // maximum and sum of what this thread has seen
+    Part part = {-INFINITY, 0.f};
+    if constexpr (V > 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < E; ++e) part.m = fmaxf(part.m, element<BF16>(held[v], e));
+        const float at = part.m == -INFINITY ? 0.f : part.m;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < E; ++e) part.s += ex2f((element<BF16>(held[v], e) - at) * P.c);
+    } else {
+        for (int j = rank * TPR + t; j < nvec; j += C * TPR) {
+            const uint4 x = load(j);
+            Part one = {-INFINITY, 0.f};
+#pragma unroll
+            for (int e = 0; e < E; ++e) one.m = fmaxf(one.m, element<BF16>(x, e));
+            const float at = one.m == -INFINITY ? 0.f : one.m;
+#pragma unroll
+            for (int e = 0; e < E; ++e) one.s += ex2f((element<BF16>(x, e) - at) * P.c);
+            part = join(part, one, P.c);
+        }
+    }
+#pragma unroll
+    for (int off = 16; off; off /= 2)
+        part = join(part, {__shfl_xor_sync(0xffffffffu, part.m, off), __shfl_xor_sync(0xffffffffu, part.s, off)}, P.c);
+    if constexpr (WARPS > 1) {
+        if (lane == 0) s_part[group][warp] = part;
+        group_sync();
+        part = s_part[group][0];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) part = join(part, s_part[group][w], P.c);
+    } else __syncwarp();
+    if constexpr (C > 1) {
+        __syncwarp();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        if (t < C) {
+            uint32_t to;
+            const uint32_t mine = (uint32_t)__cvta_generic_to_shared(&s_rank[rank]);
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(mine), "r"(t));
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(part.m), "f"(part.s) : "memory");
+        }
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        part = s_rank[0];
+#pragma unroll
+        for (int r = 1; r < C; ++r) part = join(part, s_rank[r], P.c);
+    }
+    const bool live = s_total[group] != 0.f;                     // (NaN, too)
+    if (warp == 0 && rank == 0) {
+        const float log_total = logf(total), log_sum = logf(part.s);
+        float sum = 0.f;
+#pragma unroll
+        for (int a = 0; a < LS_MAX_K / 32; ++a) {
+            const int k = a * 32 + lane;
+            if (a * 32 >= P.k) continue;
+            const float q = k < P.k ? s_q[group][k] : 0.f;
+            if (q != 0.f) sum += q * ((tk[a] - log_total) - ((s_score[group][k] - part.m) * P.inv_t - log_sum));
+        }
+#pragma unroll
+        for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (lane == 0) P.loss[row] = live ? sum : 0.f;
+    }
+    if (!P.grad) return;
+    const float w = (P.weight ? P.weight[row] : 1.f) * P.inv_t, a = w / part.s;
+    T *out = (T *)P.grad + (size_t)row * P.ldg - head;
+    const bool wide = (uintptr_t)out % 16 == 0;
+    auto gradient = [&](float s) { return live ? ex2f((s - part.m) * P.c) * a : 0.f; };
+    auto store = [&](int j, const uint4 &x) {
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (BF16) r[i] = bf16x2(gradient(element<BF16>(x, 2 * i)), gradient(element<BF16>(x, 2 * i + 1)));
+            else r[i] = __float_as_uint(gradient(element<BF16>(x, i)));
+        }
+        if (wide && j * E >= head && (j + 1) * E <= end) {
+            *reinterpret_cast<uint4 *>(out + (size_t)j * E) = make_uint4(r[0], r[1], r[2], r[3]);
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int at = j * E + e;
+            if (at >= head && at < end) out[at] = (T)(BF16 ? r[e / 2] >> (16 * (e & 1)) : r[e]);
+        }
+    };
+    if constexpr (V > 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int j = (v * C + rank) * TPR + t;
+            if (j < nvec) store(j, held[v]);
+        }
+    } else {
+        for (int j = rank * TPR + t; j < nvec; j += C * TPR) store(j, load(j));
+    }
+    if (!live) return;
+    group_sync();
+    for (int k = t; k < P.k; k += TPR) {
+        const int j = s_index[group][k];
+        if (j < 0 || (C > 1 && (head + j) / E / TPR % C != rank)) continue;
+        float q = 0.f;
+        bool first = true;
+        for (int o = 0; o < P.k; ++o)
+            if (s_index[group][o] == j) {
+                first &= o >= k;
+                q += s_q[group][o];
+            }
+        if (!first) continue;
+        const float g = ex2f((s_score[group][k] - part.m) * P.c) / part.s * w - q * w;
+        out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+    }
+}
+
+template <bool BF16, int TPR, int V, int C>
+skb_status launch(const Loss &P, cudaStream_t st)
+{
+    constexpr int threads = TPR <= 128 ? 256 : TPR, groups = threads / TPR;
+    const long long blocks = (P.rows + groups - 1) / groups * C;
+    if (blocks > 0x7fffffffLL) return op_fail(SKB_ERR_SHAPE, "too many rows");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = C;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = C > 1 ? 1 : 0;
+    cudaLaunchKernelEx(&cfg, loss_kernel<BF16, TPR, V, C>, P);
+    return op_launched("plan_loss");
+}
+
+template <bool BF16>
+skb_status launch_by_length(const Loss &P, int sms, cudaStream_t st)
+{
+    constexpr int E = BF16 ? 8 : 4;
+    const long long vec = ((long long)P.m + 2 * E - 2) / E;      // vectors that a row may touch, wherever it starts
+    // more blocks to a row than it needs where there are too few rows to fill the device
+    const auto blocks = [&](int least) {
+        int c = least;
+        while (c < 8 && P.rows * c < 2 * sms && vec / (2 * c) >= 512) c *= 2;
+        return c;
+    };
+    if (vec <= 32 * 4) return launch<BF16, 32, 4, 1>(P, st);
+    if (vec <= 128 * 4) return launch<BF16, 128, 4, 1>(P, st);
+    if (vec <= 128 * 8 && P.rows >= sms) return launch<BF16, 128, 8, 1>(P, st);
+    if (vec <= 512 * 8 * 8) {
+        const int c = blocks(vec <= 512 * 8 ? 1 : vec <= 512 * 16 ? 2 : vec <= 512 * 32 ? 4 : 8);
+        if (c == 1) return launch<BF16, 512, 8, 1>(P, st);
+        if (c == 2) return launch<BF16, 512, 8, 2>(P, st);
+        if (c == 4) return launch<BF16, 512, 8, 4>(P, st);
+        return launch<BF16, 512, 8, 8>(P, st);
+    }
+    return launch<BF16, 512, 0, 8>(P, st);
+}
+
+}  // namespace
+}  // namespace skb
+
+using namespace skb;
+
+extern "C" skb_status sinkhorn_plan_loss(const void *scores, int dtype, long long rows, int m, long long ld, const int *index, const float *logits, int k,
+                                         float temperature, const float *weight, float *loss, void *grad, long long ldg, void *stream)
+{
+    if (!scores || !index || !loss) return op_fail(SKB_ERR_NULL, "scores, index and loss are required");
+    if (dtype != SKB_F32 && dtype != SKB_BF16) return op_fail(SKB_ERR_VALUE, "scores must be SKB_F32 or SKB_BF16");
+    if (rows < 1 || rows > 0x7fffffffLL || m < 1 || m > 262143 || k < 1 || k > LS_MAX_K)
+        return op_fail(SKB_ERR_SHAPE, "rows from 1 to 2^31 - 1, m from 1 to 262143 and k from 1 to 256 are supported");
+    if (ld < m || (grad && ldg < m)) return op_fail(SKB_ERR_SHAPE, "rows must not overlap: ld and ldg at least m");
+    if (!(temperature >= 1e-30f && temperature <= 1e30f)) return op_fail(SKB_ERR_VALUE, "temperature must be from 1e-30 to 1e30");
+    const uintptr_t size = dtype == SKB_BF16 ? 2 : 4;
+    if ((uintptr_t)scores % size || (uintptr_t)grad % size || (uintptr_t)index % 4 || (uintptr_t)logits % 4 || (uintptr_t)weight % 4 || (uintptr_t)loss % 4)
+        return op_fail(SKB_ERR_WORKSPACE, "arrays must be aligned to their types");
+    if (grad == scores && ldg != ld) return op_fail(SKB_ERR_SHAPE, "a gradient in the place of the scores has their row stride");
+    int dev = 0, sms = 0;
+    cudaGetDevice(&dev);
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");
+    const Loss P = {scores, index, logits, weight, loss, grad, rows, ld, ldg, m, k, 1.f / temperature, (float)(1.4426950408889634 / (double)temperature)};
+    return dtype == SKB_BF16 ? launch_by_length<true>(P, sms, (cudaStream_t)stream) : launch_by_length<false>(P, sms, (cudaStream_t)stream);
+}

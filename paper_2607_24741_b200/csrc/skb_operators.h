@@ -1,4 +1,5 @@
-// What the operators beside the solver (4-bit clouds, their products, draws from a coupling) share on the host.
+// What the operators beside the solver (clouds in 4 and 8 bits, their products, maps over them, draws from a coupling, the loss of scores
+// against its rows) share on the host.
 #pragma once
 #include <cuda_runtime.h>
 #include <string>
@@ -11,6 +12,7 @@ namespace skb {
 skb_status op_fail(skb_status st, const std::string &msg);     // sets the calling thread's text
 skb_status op_launched(const char *what);                       // the launch's status; clears the text where it went well
 const char *cloud4_refused(int W, int npts, int d, int format);   // null, or why there is no such cloud
+const char *cloud8_refused(int W, int npts, int d);
 // Points of a cloud from `row` on, as products take them: bf16 values, or codes, scales and powers of two.
 struct DotsCloud {
     const void *data;
