@@ -16,6 +16,7 @@
 #include <cuda_runtime.h>
 #include <string>
 
+#include "skb_f32x2.cuh"
 #include "skb_operators.h"
 
 namespace skb {
@@ -40,13 +41,47 @@ __device__ __forceinline__ float ex2f(float v)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// element e of a vector
-template <bool BF16> __device__ __forceinline__ float element(const uint4 &v, int e)
+// two scores of a vector
+template <bool BF16> __device__ __forceinline__ u64 two(const uint4 &v, int i)
 {
-    const uint32_t w = BF16 ? (e < 4 ? (e < 2 ? v.x : v.y) : (e < 6 ? v.z : v.w)) : (e < 2 ? (e < 1 ? v.x : v.y) : (e < 3 ? v.z : v.w));
-    if (!BF16) return __uint_as_float(w);
-    return __uint_as_float(e & 1 ? w & 0xffff0000u : w << 16);
+    if constexpr (BF16) {
+        const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+        return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    } else
+        return i == 0 ? pack2(__uint_as_float(v.x), __uint_as_float(v.y)) : pack2(__uint_as_float(v.z), __uint_as_float(v.w));
 }
+// the largest score of a vector; NaN counts as none
+template <bool BF16> __device__ __forceinline__ float largest(const uint4 &v)
+{
+    if constexpr (BF16) {
+        uint32_t a, b;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
+        asm("max.bf16x2 %0, %0, %1;" : "+r"(a) : "r"(b));
+        return fmaxf(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u));
+    } else
+        return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+}
+__device__ __forceinline__ float warp_max(float v)
+{
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ u64 mul2(u64 a, u64 b)
+{
+    u64 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// 2^((s - at) c) of two scores: the difference first, so that its rounding is of the distance, however large scores are
+__device__ __forceinline__ u64 exponentials(u64 s, u64 at2, u64 c2)
+{
+    float a, b;
+    unpack2(mul2(sub2(s, at2), c2), a, b);
+    return pack2(ex2f(a), ex2f(b));
+}
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
 {
     uint32_t r;
@@ -57,10 +92,19 @@ __device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
 struct __align__(8) Part {                   // (written to other blocks in one 8-byte store)
     float m, s;
 };
+// ... of COUNT threads next to each other (the others of a warp: of none)
+template <int COUNT> __device__ __forceinline__ Part join(Part p, float c)
+{
+    const float m = warp_max(p.m), at = finite_max(m);
+    // (a sum beside a maximum of minus infinity is 0, or NaN, which stays)
+    float s = p.s * ex2f((p.m - at) * c);
+#pragma unroll
+    for (int off = COUNT / 2; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
+    return {m, s};
+}
 __device__ __forceinline__ Part join(Part a, Part b, float c)
 {
-    const float m = fmaxf(a.m, b.m), at = m == -INFINITY ? 0.f : m;
-    // (a sum beside a maximum of minus infinity is 0, or NaN, which stays)
+    const float m = fmaxf(a.m, b.m), at = finite_max(m);
     return {m, a.s * ex2f((a.m - at) * c) + b.s * ex2f((b.m - at) * c)};
 }
 
@@ -72,7 +116,7 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
     constexpr int E = BF16 ? 8 : 4;
     using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
     __shared__ int s_index[GROUPS][LS_MAX_K];
-    __shared__ float s_q[GROUPS][LS_MAX_K], s_score[GROUPS][LS_MAX_K];
+    __shared__ float s_q[GROUPS][LS_MAX_K], s_log[GROUPS][LS_MAX_K], s_score[GROUPS][LS_MAX_K];
     __shared__ float s_total[GROUPS];
     __shared__ Part s_part[GROUPS][WARPS], s_rank[C];
     const int tid = threadIdx.x, group = tid / TPR, t = tid % TPR, lane = tid & 31, warp = t >> 5;
@@ -104,6 +148,16 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     };
+    // the first entries are on their way while the row is: what follows from them waits for neither
+    constexpr int AHEAD = 2;
+    int named_ahead[AHEAD];
+    float logit_ahead[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+        const int k = 32 * a + lane;
+        named_ahead[a] = warp == 0 && k < P.k ? P.index[(size_t)row * P.k + k] : -1;
+        logit_ahead[a] = warp == 0 && k < P.k && P.logits ? P.logits[(size_t)row * P.k + k] : 0.f;
+    }
     uint4 held[V ? V : 1];
     if constexpr (V > 0) {
 #pragma unroll
@@ -114,75 +168,77 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
             if (j < nvec) held[v] = load(j);
         }
     }
-    // the teacher: the first warp's, meanwhile
-    float tk[LS_MAX_K / 32], top = -INFINITY, total = 0.f;
-    if (warp == 0) {
-#pragma unroll
-        for (int a = 0; a < LS_MAX_K / 32; ++a) {
-            const int k = a * 32 + lane;
-            tk[a] = -INFINITY;
-            if (a * 32 >= P.k) continue;
-            if (k < P.k) {
-                const int j = P.index[(size_t)row * P.k + k];
-                const bool named = j >= 0 && j < P.m;
-                if (named) tk[a] = P.logits ? P.logits[(size_t)row * P.k + k] * P.inv_t : 0.f;
-                float s = 0.f;
-                if (named) s = BF16 ? __uint_as_float((uint32_t)src[j] << 16) : __uint_as_float((uint32_t)src[j]);
-                s_index[group][k] = named ? j : -1;
-                s_score[group][k] = s;
-            }
-            top = fmaxf(top, tk[a]);
-        }
-#pragma unroll
-        for (int off = 16; off; off /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-        const float at = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int a = 0; a < LS_MAX_K / 32; ++a)
-            if (a * 32 < P.k) total += expf(tk[a] - at);
-#pragma unroll
-        for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
-#pragma unroll
-        for (int a = 0; a < LS_MAX_K / 32; ++a) {
-            const int k = a * 32 + lane;
-            if (a * 32 >= P.k) continue;
-            if (k < P.k) s_q[group][k] = total == 0.f ? 0.f : expf(tk[a] - at) / total;
-            tk[a] -= at;
-        }
-        if (lane == 0) s_total[group] = total;
-    }
     // maximum and sum of what this thread has seen
+    constexpr bool KEEP = V > 0 && (!BF16 || V <= 4);            // exponentials stay in registers
     Part part = {-INFINITY, 0.f};
+    u64 kept[KEEP ? V : 1][E / 2];
+    const u64 c2 = pack2(P.c, P.c);
     if constexpr (V > 0) {
 #pragma unroll
+        for (int v = 0; v < V; ++v) part.m = fmaxf(part.m, largest<BF16>(held[v]));
+        const u64 at2 = pack2(finite_max(part.m), finite_max(part.m));
+        u64 sum[2] = {0ull, 0ull};
+#pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int e = 0; e < E; ++e) part.m = fmaxf(part.m, element<BF16>(held[v], e));
-        const float at = part.m == -INFINITY ? 0.f : part.m;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int e = 0; e < E; ++e) part.s += ex2f((element<BF16>(held[v], e) - at) * P.c);
+            for (int i = 0; i < E / 2; ++i) {
+                const u64 e = exponentials(two<BF16>(held[v], i), at2, c2);
+                if constexpr (KEEP) kept[v][i] = e;
+                sum[i & 1] = add2(sum[i & 1], e);
+            }
+        float a, b;
+        unpack2(add2(sum[0], sum[1]), a, b);
+        part.s = a + b;
     } else {
         for (int j = rank * TPR + t; j < nvec; j += C * TPR) {
             const uint4 x = load(j);
-            Part one = {-INFINITY, 0.f};
+            Part one = {largest<BF16>(x), 0.f};
+            const u64 at2 = pack2(finite_max(one.m), finite_max(one.m));
+            u64 sum = 0ull;
 #pragma unroll
-            for (int e = 0; e < E; ++e) one.m = fmaxf(one.m, element<BF16>(x, e));
-            const float at = one.m == -INFINITY ? 0.f : one.m;
-#pragma unroll
-            for (int e = 0; e < E; ++e) one.s += ex2f((element<BF16>(x, e) - at) * P.c);
+            for (int i = 0; i < E / 2; ++i) sum = add2(sum, exponentials(two<BF16>(x, i), at2, c2));
+            float a, b;
+            unpack2(sum, a, b);
+            one.s = a + b;
             part = join(part, one, P.c);
         }
     }
+    // the teacher: the first warp's; the scores that it names are in the first-level cache by now
+    if (warp == 0) {
+        float top = -INFINITY, total = 0.f;
+        auto entry = [&](int k, int j, float logit) {
+            const bool named = j >= 0 && j < P.m;
+            const float l = named ? logit * P.inv_t : -INFINITY;
+            s_index[group][k] = named ? j : -1;
+            s_score[group][k] = !named ? 0.f : BF16 ? __uint_as_float((uint32_t)src[j] << 16) : __uint_as_float((uint32_t)src[j]);
+            s_log[group][k] = l;
+            top = fmaxf(top, l);
+        };
 #pragma unroll
-    for (int off = 16; off; off /= 2)
-        part = join(part, {__shfl_xor_sync(0xffffffffu, part.m, off), __shfl_xor_sync(0xffffffffu, part.s, off)}, P.c);
+        for (int a = 0; a < AHEAD; ++a)
+            if (32 * a + lane < P.k) entry(32 * a + lane, named_ahead[a], logit_ahead[a]);
+        for (int k = 32 * AHEAD + lane; k < P.k; k += 32)
+            entry(k, P.index[(size_t)row * P.k + k], P.logits ? P.logits[(size_t)row * P.k + k] : 0.f);
+        const float at = finite_max(warp_max(top));
+        // (a thread reads back what it wrote)
+        for (int k = lane; k < P.k; k += 32) total += expf(s_log[group][k] - at);
+#pragma unroll
+        for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
+        const float log_total = logf(total);
+        for (int k = lane; k < P.k; k += 32) {
+            const float l = s_log[group][k] - at;
+            s_log[group][k] = l - log_total;
+            s_q[group][k] = total == 0.f ? 0.f : expf(l) / total;
+        }
+        if (lane == 0) s_total[group] = total;
+    }
+    const float own = part.m;
+    part = join<32>(part, P.c);
     if constexpr (WARPS > 1) {
         if (lane == 0) s_part[group][warp] = part;
         group_sync();
-        part = s_part[group][0];
-#pragma unroll
-        for (int w = 1; w < WARPS; ++w) part = join(part, s_part[group][w], P.c);
+        part = join<WARPS>(lane < WARPS ? s_part[group][lane] : Part{-INFINITY, 0.f}, P.c);
+        part.s = __shfl_sync(0xffffffffu, part.s, 0);
     } else __syncwarp();
     if constexpr (C > 1) {
         __syncwarp();
@@ -195,20 +251,16 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
         }
         __syncwarp();
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        part = s_rank[0];
-#pragma unroll
-        for (int r = 1; r < C; ++r) part = join(part, s_rank[r], P.c);
+        part = join<C>(lane < C ? s_rank[lane] : Part{-INFINITY, 0.f}, P.c);
+        part.s = __shfl_sync(0xffffffffu, part.s, 0);
     }
     const bool live = s_total[group] != 0.f;                     // (NaN, too)
     if (warp == 0 && rank == 0) {
-        const float log_total = logf(total), log_sum = logf(part.s);
+        const float log_sum = logf(part.s);
         float sum = 0.f;
-#pragma unroll
-        for (int a = 0; a < LS_MAX_K / 32; ++a) {
-            const int k = a * 32 + lane;
-            if (a * 32 >= P.k) continue;
-            const float q = k < P.k ? s_q[group][k] : 0.f;
-            if (q != 0.f) sum += q * ((tk[a] - log_total) - ((s_score[group][k] - part.m) * P.inv_t - log_sum));
+        for (int k = lane; k < P.k; k += 32) {
+            const float q = s_q[group][k];
+            if (q != 0.f) sum += q * (s_log[group][k] - ((s_score[group][k] - part.m) * P.inv_t - log_sum));
         }
 #pragma unroll
         for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
@@ -218,13 +270,22 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
     const float w = (P.weight ? P.weight[row] : 1.f) * P.inv_t, a = w / part.s;
     T *out = (T *)P.grad + (size_t)row * P.ldg - head;
     const bool wide = (uintptr_t)out % 16 == 0;
-    auto gradient = [&](float s) { return live ? ex2f((s - part.m) * P.c) * a : 0.f; };
-    auto store = [&](int j, const uint4 &x) {
+    // what an exponential is multiplied by: kept ones are against this thread's own maximum
+    const float factor = (KEEP ? ex2f((finite_max(own) - finite_max(part.m)) * P.c) : 1.f) * a;
+    const u64 at2 = pack2(part.m, part.m), f2 = pack2(factor, factor);
+    auto again = [&](const uint4 &x, u64 (&e)[E / 2]) {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) e[i] = exponentials(two<BF16>(x, i), at2, c2);
+    };
+    auto store = [&](int j, const u64 (&e)[E / 2]) {
         uint32_t r[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (BF16) r[i] = bf16x2(gradient(element<BF16>(x, 2 * i)), gradient(element<BF16>(x, 2 * i + 1)));
-            else r[i] = __float_as_uint(gradient(element<BF16>(x, i)));
+        for (int i = 0; i < E / 2; ++i) {
+            float p, q;
+            unpack2(mul2(e[i], f2), p, q);
+            if (!live) p = q = 0.f;
+            if constexpr (BF16) r[i] = bf16x2(p, q);
+            else { r[2 * i] = __float_as_uint(p); r[2 * i + 1] = __float_as_uint(q); }
         }
         if (wide && j * E >= head && (j + 1) * E <= end) {
             *reinterpret_cast<uint4 *>(out + (size_t)j * E) = make_uint4(r[0], r[1], r[2], r[3]);
@@ -240,10 +301,19 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int j = (v * C + rank) * TPR + t;
-            if (j < nvec) store(j, held[v]);
+            if (j >= nvec) continue;
+            if constexpr (!KEEP) {
+                // (unpacked anew: the compiler would keep what it unpacked before the barrier, and spill)
+                asm volatile("" : "+r"(held[v].x), "+r"(held[v].y), "+r"(held[v].z), "+r"(held[v].w));
+                again(held[v], kept[0]);
+            }
+            store(j, kept[KEEP ? v : 0]);
         }
     } else {
-        for (int j = rank * TPR + t; j < nvec; j += C * TPR) store(j, load(j));
+        for (int j = rank * TPR + t; j < nvec; j += C * TPR) {
+            again(load(j), kept[0]);
+            store(j, kept[0]);
+        }
     }
     if (!live) return;
     group_sync();
@@ -287,7 +357,9 @@ template <bool BF16>
 skb_status launch_by_length(const Loss &P, int sms, cudaStream_t st)
 {
     constexpr int E = BF16 ? 8 : 4;
-    const long long vec = ((long long)P.m + 2 * E - 2) / E;      // vectors that a row may touch, wherever it starts
+    // vectors that a row may touch: one more than it fills where rows do not all start on a 16-byte boundary
+    const bool even = (uintptr_t)P.scores % 16 == 0 && P.ld % E == 0;
+    const long long vec = ((long long)P.m + (even ? E - 1 : 2 * E - 2)) / E;
     // more blocks to a row than it needs where there are too few rows to fill the device
     const auto blocks = [&](int least) {
         int c = least;
