@@ -532,6 +532,27 @@ skb_status sinkhorn_cloud8_unpack(const void *cloud, int W, int npts, int d, voi
  */
 skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int m, int d, float *out, void *stream);
 /*
+ * Images of query points under the entropic map of a target cloud held in 8 bits: attention over a stored bank.  For x [W, n, d] bf16,
+ * a bank y [W, m, d] and its values v [W, m, dv] (buffers of sinkhorn_cloud8_pack; v null: the bank itself, dv = d and not read),
+ *      z_ij = (g_j - |x_i - y_j|^2) / eps,   lse_i = log sum_j exp z_ij,   out_i = sum_j exp(z_ij - lse_i) v_j.
+ * With the target's potential g [W, m] (float64, as the solver gives it; null: zeros) this is the plan's barycentric image of a source
+ * point, and of any other point its extension; -eps lse_i is the source's potential there, less eps log(1 / n).
+ *   g_j = -inf masks a target whatever its point and values hold; so does an index from lengths_t on
+ *   lengths  [W] int, may be null: targets of a lane that count, 0 .. m (others are cut to that)
+ *   out      [W, n, dv] bf16; lse [W, n] fp32, may be null
+ * A query without targets has an image of zeros and lse = -inf.  A query, an unmasked target or its value that is NaN, a potential that is
+ * NaN or plus infinity, and an eps that is not a positive number make the images they take part in NaN.
+ * Exponents are made of fp32 products of the bf16 query and the bank's values, good to (d / 32 + 8) 2^-24 (|x|^2 + |y|^2 + |g|) / eps; weights, for
+ * the product with the values, are rounded to 11 bits, sums are fp32.  A value below 2^-25 of the largest of its 128
+ * dimensions among 64 targets next to it may count as zero.
+ * d and dv <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on `stream` of the current device and returns; the workspace of
+ * sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv) bytes (0: a bad shape; dv = 0: d; device, 256-byte aligned) is in use until they are
+ * done: calls that may overlap need one each.
+ */
+size_t sinkhorn_cloud8_map_workspace_bytes(int W, int n, int m, int d, int dv);
+skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, const float *eps, const void *v, const int *lengths, int W, int n, int m,
+                               int d, int dv, void *out, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+/*
  * The loss of scores against the rows of a coupling, and its gradient: what teaches a network to give the partners that the solver
  * gives.  Row i of scores [rows, m] (dtype SKB_F32 or SKB_BF16, `ld` elements from row to row) has k named entries index [rows, k]:
  * draws from the plan's row (sinkhorn_plan_draw's indices as they are), or a teacher's top entries with their logits [rows, k] fp32.

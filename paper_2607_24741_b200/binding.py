@@ -38,6 +38,7 @@ PHASES = ("create", "f_leg", "column_check", "plan", "emit_move", "g_leg")
 EXTRA_EXPORTS = ("sinkhorn_row_residual_static", "sinkhorn_row_residual_static_last_error",
                  "sinkhorn_cloud4_bytes", "sinkhorn_cloud4_pack", "sinkhorn_cloud4_unpack", "sinkhorn_cloud4_dots", "sinkhorn_plan_draw_workspace_bytes", "sinkhorn_plan_draw",
                  "sinkhorn_cloud8_bytes", "sinkhorn_cloud8_pack", "sinkhorn_cloud8_unpack", "sinkhorn_cloud8_dots", "sinkhorn_plan_loss",
+                 "sinkhorn_cloud8_map", "sinkhorn_cloud8_map_workspace_bytes",
                  "sinkhorn_operator_last_error")
 DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 FORMATS = {"mx4": 2, "nv4": 3}
@@ -123,6 +124,9 @@ def _load():
     lib.sinkhorn_cloud8_pack.argtypes = [vp, ci, ci, ci, ci, vp, vp, ci, vp]
     lib.sinkhorn_cloud8_unpack.argtypes = [vp, ci, ci, ci, vp, ci, vp]
     lib.sinkhorn_cloud8_dots.argtypes = [vp, vp, ci, ci, ci, ci, vp, vp]
+    lib.sinkhorn_cloud8_map_workspace_bytes.restype = ctypes.c_size_t
+    lib.sinkhorn_cloud8_map_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    lib.sinkhorn_cloud8_map.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, ctypes.c_size_t, vp]
     lib.sinkhorn_plan_loss.argtypes = [vp, ci, cl, ci, cl, vp, vp, ci, ctypes.c_float, vp, vp, vp, cl, vp]
     drawp = ctypes.POINTER(SkbDrawConfig)
     lib.sinkhorn_plan_draw_workspace_bytes.restype = ctypes.c_size_t
@@ -400,6 +404,42 @@ def cloud8_dots(x, y, out=None):
             out = torch.empty(shape, dtype=torch.float32, device=x.device)
         _check_op(lib.sinkhorn_cloud8_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, _ptr(out), _stream(x.device)))
     return out
+
+
+def cloud8_map(x, y, g, eps, v=None, *, lengths=None, lse=False, out=None):
+    """Images of x [W, n, d] (bfloat16, CUDA) under the entropic map of the bank y [W, m, d], a Cloud8, with its potential g [W, m]
+    (float64, or None: zeros) and eps [W] float32: the values' mean by the softmax over j of (g_j - |x_i - y_j|^2) / eps, the values being
+    the bank's points or v [W, m, dv], a Cloud8.  lengths [W] int32: the targets of each lane that count; see sinkhorn_cloud8_map in
+    the header.  Returns [W, n, dv] bfloat16 (into `out`, if given), with `lse` also the logarithms of the sums [W, n] float32."""
+    if not isinstance(y, Cloud8) or not (v is None or isinstance(v, Cloud8)):
+        raise ValueError("y, and v if given, must be Cloud8")
+    if not torch.is_tensor(x) or not x.is_cuda or x.dtype != torch.bfloat16 or x.dim() != 3:
+        raise ValueError("x must be a bfloat16 CUDA tensor [W, n, d]")
+    (W, n, d), m, device = x.shape, y.npts, x.device
+    if (y.W, y.d) != (W, d) or y.device != device:
+        raise ValueError("x and y must have one W, d and device")
+    if v is not None and ((v.W, v.npts) != (W, m) or v.device != device):
+        raise ValueError("v must have the bank's W, points and device")
+    dv = d if v is None else v.d
+    for name, t, dtype, shape in (("g", g, torch.float64, (W, m)), ("eps", eps, torch.float32, (W,)), ("lengths", lengths, torch.int32, (W,))):
+        if t is None and name != "eps":
+            continue
+        if not torch.is_tensor(t) or t.dtype != dtype or t.device != device or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be a {dtype} tensor {list(shape)} on the queries' device")
+    if out is not None and (out.dtype != torch.bfloat16 or out.device != device or tuple(out.shape) != (W, n, dv) or not out.is_contiguous()):
+        raise ValueError("out must be a contiguous bfloat16 tensor [W, n, dv] on the queries' device")
+    x, eps = x.contiguous(), eps.contiguous()
+    g, lengths = (None if t is None else t.contiguous() for t in (g, lengths))
+    need = lib.sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv)
+    if need == 0:
+        raise SkbError(2, "shape not supported: W, n, m, d >= 1, d and dv <= 1024, n and m <= 262143, W <= 65535")
+    with _on(device):
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        out = torch.empty(W, n, dv, dtype=torch.bfloat16, device=device) if out is None else out
+        sums = torch.empty(W, n, dtype=torch.float32, device=device) if lse else None
+        _check_op(lib.sinkhorn_cloud8_map(_ptr(x), _ptr(y.buffer), _ptr(g), _ptr(eps), None if v is None else _ptr(v.buffer), _ptr(lengths), W, n, m, d, dv,
+                                          _ptr(out), _ptr(sums), _ptr(ws), need, _stream(device)))
+    return (out, sums) if lse else out
 
 
 def _rows_of(t):

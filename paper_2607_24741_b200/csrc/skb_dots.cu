@@ -467,6 +467,12 @@ skb_status launch_kind(const CUtensorMap &tx, const CUtensorMap &ty, const CUten
 
 }  // namespace
 
+bool points_map(CUtensorMap *tm, const void *codes, int row_bytes, int npts, int W, int box_points)
+{
+    const size_t rb = row_bytes;
+    return encoder() && make_map(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, rb, npts, W, rb, rb * npts, 128, box_points);
+}
+
 DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t row)
 {
     if (dtype == SKB_BF16) return {(const uint16_t *)base + row * d, nullptr, nullptr, 2 * d, 0};

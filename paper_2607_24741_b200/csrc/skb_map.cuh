@@ -1,0 +1,40 @@
+// Images under the entropic map of a stored cloud: what its kernels share.
+#pragma once
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "skb_cloud8.cuh"
+
+namespace skb {
+
+struct Map {
+    const uint16_t *x;                        // [W, n, d] bf16
+    Cloud8 y, v;                              // bank and its values (the same where there are none of their own)
+    const double *g;                          // [W, m], null: zeros
+    const float *eps;                         // [W]
+    const int *lengths;                       // [W], null: m
+    uint16_t *out;                            // [W, n, dv] bf16
+    float *lse;                               // [W, n], null: not wanted
+    float *part_ml, *part_out;                // splits > 1: [W, n, splits] pairs, [W, n, splits, dv]
+    int W, n, m, d, dv, splits;
+    int own_values;                           // v is not y
+};
+
+__device__ __forceinline__ int map_length(const Map &P, int w) { return P.lengths ? min(max(P.lengths[w], 0), P.m) : P.m; }
+// log2(e) / eps; NaN, and so are the lane's images, where eps is not a positive number
+__device__ __forceinline__ double map_scale(const Map &P, int w)
+{
+    const float eps = P.eps[w];
+    return eps > 0.f && eps <= 3.402823466e38f ? 1.4426950408889634 / (double)eps : __longlong_as_double(0x7ff8000000000000LL);
+}
+// What a target adds to the exponent of every query, in powers of two; minus infinity: it is masked, whatever its codes.
+__device__ __forceinline__ float map_term(double k, double g, float norm) { return g == -INFINITY ? -INFINITY : (float)(k * (g - (double)norm)); }
+// natural logarithm of the sum of exponentials, from the largest exponent and the sum against it (powers of two) and |x|^2
+__device__ __forceinline__ float map_lse(float top, float sum, double k, double xx)
+{
+    if (sum == 0.f) return -INFINITY;
+    return (float)(0.6931471805599453 * ((double)top + (double)log2f(sum) - k * xx));
+}
+
+}  // namespace skb

@@ -1,6 +1,7 @@
 // What the operators beside the solver (clouds in 4 and 8 bits, their products, maps over them, draws from a coupling, the loss of scores
 // against its rows) share on the host.
 #pragma once
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <string>
 
@@ -27,6 +28,9 @@ DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t
 constexpr int DOTS_BF16_PART = 64;
 skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W, int n, int m, float *out, long long ldo, cudaStream_t st,
                        int n_out = 0, int m_out = 0);
+// The tensor map of W lanes of npts points of row_bytes (a multiple of 16, 16-byte aligned): boxes of 128 bytes of box_points points, 128-byte swizzle.
+bool points_map(CUtensorMap *tm, const void *codes, int row_bytes, int npts, int W, int box_points);
+constexpr int MAP_MAX_SMS = 160;                                // multiprocessors that a map's workspace is sized for
 // sinkhorn_plan_draw; lanes whose `status` (null: none) is SKB_LANE_NONFINITE give no draws.
 skb_status plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u, const skb_draw_config *cfg,
                      const int *status, int *index, float *logp);
