@@ -449,6 +449,9 @@ skb_status launch_rows_by_depth(const CUtensorMap &ty, const CUtensorMap &tv, co
     return launch_rows<NG, 8>(ty, tv, P, st);
 }
 
+// queries up to which the matrix unit's tiles of 128 are too empty
+constexpr int MAP_ROWS_MAX = 32;
+
 const char *map_refused(int W, int n, int m, int d, int dv)
 {
     if (W < 1 || n < 1 || m < 1 || d < 1) return "W, n, m and d must be >= 1";
@@ -456,13 +459,21 @@ const char *map_refused(int W, int n, int m, int d, int dv)
     if (d > CLOUD8_MAX_D || dv > CLOUD8_MAX_D || dv < 0) return "d and dv must be at most 1024";
     return nullptr;
 }
-// Parts of a lane's bank: so many that four blocks come to an SM, of two tiles at least.
-int map_splits(int W, int n, int m, int sms)
+// Which kernel, and into how many parts a lane's bank goes: enough to fill the device, of a few tiles at least.
+struct MapPlan {
+    bool tiles;
+    int splits;
+};
+MapPlan map_plan(int W, int n, int m, int d, int dv, int sms)
 {
-    const long long blocks = (long long)W * ((n + 7) / 8), tiles = (m + MR_T - 1) / MR_T;
-    long long s = (2LL * sms + blocks - 1) / blocks;
+    MapPlan p;
+    p.tiles = n > MAP_ROWS_MAX && d <= MAP_TILES_MAX_D;
+    const long long blocks = p.tiles ? (long long)W * ((n + 127) / 128) * ((dv + 255) / 256) : (long long)W * ((n + 7) / 8);
+    const long long tiles = p.tiles ? (m + 127) / 128 : (m + MR_T - 1) / MR_T;
+    long long s = p.tiles ? sms / blocks : (2LL * sms + blocks - 1) / blocks;
     if (s > tiles / 2) s = tiles / 2;
-    return (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    return p;
 }
 size_t pad256(size_t b) { return (b + 255) / 256 * 256; }
 size_t map_workspace(int W, int n, int dv, int splits)
@@ -479,7 +490,7 @@ extern "C" size_t sinkhorn_cloud8_map_workspace_bytes(int W, int n, int m, int d
 {
     if (map_refused(W, n, m, d, dv)) return 0;
     // (what any device may split into: the workspace does not depend on the current one)
-    return map_workspace(W, n, dv ? dv : d, map_splits(W, n, m, MAP_MAX_SMS));
+    return map_workspace(W, n, dv ? dv : d, map_plan(W, n, m, d, dv ? dv : d, MAP_MAX_SMS).splits);
 }
 
 extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, const float *eps, const void *v, const int *lengths, int W, int n, int m,
@@ -503,13 +514,14 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     P.v = v ? cloud8_view(v, (size_t)W * m, dv) : P.y;
     P.g = g; P.eps = eps; P.lengths = lengths; P.out = (uint16_t *)out; P.lse = lse;
     P.W = W; P.n = n; P.m = m; P.d = d; P.dv = depth; P.own_values = v != nullptr;
-    P.splits = map_splits(W, n, m, sms < MAP_MAX_SMS ? sms : MAP_MAX_SMS);
+    const MapPlan plan = map_plan(W, n, m, d, depth, sms < MAP_MAX_SMS ? sms : MAP_MAX_SMS);
+    P.splits = plan.splits;
     P.part_ml = (float *)workspace;
     P.part_out = (float *)((char *)workspace + pad256((size_t)W * n * P.splits * 8));
     CUtensorMap ty, tv;
-    if (!points_map(&ty, P.y.codes, P.y.cb, m, W, MR_T) || !points_map(&tv, P.v.codes, P.v.cb, m, W, MR_T))
+    if (!plan.tiles && (!points_map(&ty, P.y.codes, P.y.cb, m, W, MR_T) || !points_map(&tv, P.v.codes, P.v.cb, m, W, MR_T)))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    const skb_status rc = n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
+    const skb_status rc = plan.tiles ? launch_map_tiles(P, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
     if (rc != SKB_OK || P.splits == 1) return rc;
     map_join_kernel<<<W * n, 128, 0, (cudaStream_t)stream>>>(P);
     return op_launched("map");

@@ -4,9 +4,13 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "../../include/sinkhorn_batch.h"
 #include "skb_cloud8.cuh"
 
 namespace skb {
+
+constexpr int MAP_TILES_MAX_D = 512;          // queries' depth up to which they stay in shared memory as tiles
+constexpr int MAP_TILES_SMEM = 232448;        // shared memory that a block may have
 
 struct Map {
     const uint16_t *x;                        // [W, n, d] bf16
@@ -20,6 +24,9 @@ struct Map {
     int W, n, m, d, dv, splits;
     int own_values;                           // v is not y
 };
+
+// Many queries (skb_map_tc.cu): d <= MAP_TILES_MAX_D, P.splits parts of a lane's bank.
+skb_status launch_map_tiles(const Map &P, cudaStream_t st);
 
 __device__ __forceinline__ int map_length(const Map &P, int w) { return P.lengths ? min(max(P.lengths[w], 0), P.m) : P.m; }
 // log2(e) / eps; NaN, and so are the lane's images, where eps is not a positive number

@@ -1,0 +1,472 @@
+// Images under the entropic map of a stored cloud for many queries (see skb_map.cu for the mathematics): both products on tcgen05.
+//
+// A block takes 128 queries, a part of the bank, and up to 256 dimensions of the values (deeper ones: further blocks, which form the scores again).
+// Per tile of 128 targets
+//      S = X . Y^T       bf16, fp32 in tensor memory, two buffers
+//      P = exp2(2k S + term - reference) in bf16, into S's place in tensor memory
+//      O += P . V        bf16, fp32 in tensor memory
+// so that the scores of the next tile are formed while this one's exponentials are.  Codes become bf16 on their way into shared memory: a value is four
+// bits times a power of two, which bf16 holds over all of the clouds' range, so products are those of the values, exactly; f16 would
+// round weights to 11 bits instead of 8, but cannot hold values of a bank whose scales differ.  Outputs are bf16.
+// The weights are summed in fp32 before they are rounded.
+//   warps 0-7    softmax: a thread to a query and half of a tile's targets; the two halves of a query exchange their maxima.  The reference is a
+//                whole number, raised only when a tile's maximum passes it by more than 8 (weights up to 2^8 are as good in bf16 as those
+//                below 1): O is then multiplied by a power of two, exactly
+//   warps 8-11   codes -> bf16 in the matrix unit's layout (128-byte swizzle), 128 targets by 128 dimensions a stage of 32 KB, the next stage's
+//                codes on their way to registers meanwhile.  The same layout is K-major for S and MN-major for O: values are not transposed
+//   warp 12      matrix instructions, one thread: S of tile t + 1 before O of tile t
+//   warp 13      the targets' terms
+// What bounds it: at 128 dimensions the exponentials (128 x 128 of a tile at 16 a clock take as long as its products), deeper the products.
+// Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and the block's images are NaN.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <string>
+
+#include "skb_f32x2.cuh"
+#include "skb_map.cuh"
+#include "skb_operators.h"
+#include "skb_tmem.cuh"
+
+namespace skb {
+namespace {
+
+constexpr int MT_SOFT = 8, MT_CONV = 4, MT_THREADS = (MT_SOFT + MT_CONV + 2) * 32;
+constexpr uint32_t MT_CHUNK = 128 * 128, MT_STAGE = 2 * MT_CHUNK;         // 128 points by 64, 128 dimensions of bf16
+constexpr int MT_MAX_STAGES = 5;
+constexpr uint32_t MT_MISC = 3072;
+constexpr float MT_SLACK = 8.f;
+
+constexpr uint32_t MT_IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);   // D fp32, A and B bf16, 128 x 128
+constexpr uint32_t MT_IDESC_V = MT_IDESC | (1u << 16);                    // B with its columns next to each other
+
+// D += A . B with A in tensor memory
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// rows of 64 columns (128 bytes), 8-row groups 1024 bytes apart, the next 64 columns a chunk further
+__device__ __forceinline__ uint64_t desc_columns(uint32_t saddr)
+{
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(MT_CHUNK >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Two codes, in the upper bytes of the halves of p, as bf16 of 2^-120 times their values: their four bits of exponent and three of mantissa are the
+// lowest of bf16's eight and the highest of its seven, subnormals among them.
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t p) { return ((p >> 4) & 0x07f007f0u) | (p & 0x80008000u); }
+
+// whether all 64 threads of a barrier say so
+__device__ __forceinline__ bool both(bool ok, int barrier)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(barrier), "r"((uint32_t)ok) : "memory");
+    return r != 0;
+}
+
+template <int DVC>
+__global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ Map P, const int nrt, const int stages)
+{
+    extern __shared__ __align__(1024) unsigned char smem_dyn[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rt = blockIdx.x % nrt, z = blockIdx.x / nrt, split = blockIdx.y, w = blockIdx.z;
+    const int i0 = rt * 128, dv0 = z * DVC;
+    const int nkc = (P.d + 63) / 64, nby = (P.d + 127) / 128, nbv = (min(DVC, P.dv - dv0) + 127) / 128;
+
+    // shared memory: the queries' chunks, the ring, and what is small
+    const uint32_t base = smem_u32(smem_dyn), sX = base, sR = base + (uint32_t)nkc * MT_CHUNK;
+    unsigned char *misc = smem_dyn + (size_t)nkc * MT_CHUNK + (size_t)stages * MT_STAGE;
+    float *terms = reinterpret_cast<float *>(misc);                        // [2][128]
+    float *tops = terms + 256;                                             // [2][128]: halves' maxima, and their sums at the end
+    unsigned long long *bars = reinterpret_cast<unsigned long long *>(tops + 256);
+    uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + 32);
+    int *abort_flag = reinterpret_cast<int *>(tmem_holder + 1);
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    constexpr int FULL = 0, EMPTY = MT_MAX_STAGES, SFULL = 2 * MT_MAX_STAGES, PFULL = SFULL + 2, ODONE = PFULL + 2, TFULL = ODONE + 1, TEMPTY = TFULL + 2,
+                  LAST = TEMPTY + 2;
+    static_assert(LAST < 32, "barriers");
+
+    const int len = map_length(P, w), tiles = (len + 127) / 128;
+    const int t0 = (int)((long long)tiles * split / P.splits), t1 = (int)((long long)tiles * (split + 1) / P.splits), nt = t1 - t0;
+    if (tid == 0) {
+        for (int s = 0; s < stages; ++s) { mbar_init(bar(FULL + s), MT_CONV); mbar_init(bar(EMPTY + s), 1); }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(bar(SFULL + b), 1);
+            mbar_init(bar(PFULL + b), MT_SOFT);
+            mbar_init(bar(TFULL + b), 1);
+            mbar_init(bar(TEMPTY + b), MT_SOFT + MT_CONV);
+        }
+        mbar_init(bar(ODONE), 1);
+        mbar_init(bar(LAST), 1);
+        *abort_flag = (base & 1023u) ? 1 : 0;                              // (the swizzle counts from 1024-byte boundaries)
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == MT_SOFT + MT_CONV) tc_alloc<512>(tmem_holder);
+    // the queries
+    {
+        const bool wide = P.d % 8 == 0 && (uintptr_t)P.x % 16 == 0;
+        for (int i = tid; i < 128 * 8 * nkc; i += MT_THREADS) {
+            const int r = i / (8 * nkc), ch = i % (8 * nkc), k0 = 8 * ch;
+            uint32_t v[4] = {0u, 0u, 0u, 0u};
+            if (i0 + r < P.n) {
+                const uint16_t *src = P.x + ((size_t)w * P.n + i0 + r) * P.d + k0;
+                if (wide && k0 < P.d) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(src);
+                    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+                } else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (k0 + e < P.d) v[e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
+            }
+            *reinterpret_cast<uint4 *>(smem_dyn + (size_t)(ch / 8) * MT_CHUNK + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder, tO = tmem + 256;
+    volatile int *ab = abort_flag;
+    const double k = map_scale(P, w);
+
+    if (warp < MT_SOFT) {
+        const int half = warp >> 2, q = (warp & 3) * 32 + lane;            // query; half of a tile's targets and of the image's dimensions
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const float kx = (float)(2.0 * k);
+        const u64 k2 = pack2(kx, kx);
+        float ref = -INFINITY;
+        double sum = 0.0;
+        bool ok = *ab == 0;
+        const bool starts = ok;
+        for (int t = 0; t < nt && starts; ++t) {
+            const int b = t & 1;
+            const uint32_t ph = (uint32_t)(t >> 1) & 1u;
+            ok = ok && mbar_wait(bar(TFULL + b), ph, ab) && mbar_wait(bar(SFULL + b), ph, ab);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            const uint32_t sS = tmem + lanes + 128 * b;
+            float top = -INFINITY;
+            u64 v[2][16];
+            if (ok) {
+                uint32_t r[2][32];
+                tc_ld32_issue(sS + 64 * half, r[0]);
+                tc_ld32_issue(sS + 64 * half + 32, r[1]);
+                tc_ld_wait(r[0]);
+                tc_ld_wait(r[1]);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 c = *reinterpret_cast<const float4 *>(terms + 128 * b + 64 * half + 32 * h + i);
+                        v[h][i / 2] = fma2(pack2(__uint_as_float(r[h][i]), __uint_as_float(r[h][i + 1])), k2, pack2(c.x, c.y));
+                        v[h][i / 2 + 1] = fma2(pack2(__uint_as_float(r[h][i + 2]), __uint_as_float(r[h][i + 3])), k2, pack2(c.z, c.w));
+                        float a0, a1, a2, a3;
+                        unpack2(v[h][i / 2], a0, a1);
+                        unpack2(v[h][i / 2 + 1], a2, a3);
+                        top = fmaxf(fmaxf(top, fmaxf(a0, a1)), fmaxf(a2, a3));
+                    }
+            }
+            tops[128 * half + q] = top;
+            // both halves have read S (its place is P's next) and know the query's maximum, and whether either has given up
+            ok = both(ok, 1 + (warp & 3));
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(bar(TEMPTY + b));
+            top = fmaxf(top, tops[128 * (1 - half) + q]);
+            // (read before either half writes the next tile's)
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
+            float fac = 1.f;
+            if (top > ref + MT_SLACK || (ref == -INFINITY && top > -INFINITY)) {
+                const float up = ceilf(top);
+                fac = ex2_fast(ref - up);
+                ref = up;
+            }
+            const bool raise = __any_sync(0xffffffffu, fac != 1.f);
+            if (raise) {
+                sum *= (double)fac;
+                if (t > 0) {
+                    // (O of the tile before the last is there: S of this tile was issued after it)
+                    // (where that wait runs out the halves part only at the next tile's barrier)
+                    ok = mbar_wait(bar(ODONE), (uint32_t)(t - 1) & 1u, ab);
+                    ok = __all_sync(0xffffffffu, ok);
+                    tc_fence_after();
+                    for (int c = 0; c < DVC / 2; c += 32) {
+                        const uint32_t at = tO + lanes + half * (DVC / 2) + c;
+                        uint32_t o[32];
+                        tc_ld32_issue(at, o);
+                        tc_ld_wait(o);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fac);
+                        tc_st32_issue(at, o);
+                    }
+                }
+            }
+            const float at = ref == -INFINITY ? 0.f : ref;
+            const u64 at2 = pack2(-at, -at);
+            u64 acc[2] = {0ull, 0ull};
+            uint32_t p[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                float a, c;
+                unpack2(add2(v[i / 16][i % 16], at2), a, c);
+                a = ex2_fast(a);
+                c = ex2_fast(c);
+                acc[i & 1] = add2(acc[i & 1], pack2(a, c));
+                p[i] = bf16_pair(a, c);
+            }
+            tc_st32_issue(sS + 32 * half, p);
+            float a, c;
+            unpack2(add2(acc[0], acc[1]), a, c);
+            sum += (double)(a + c);
+            tc_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(PFULL + b));
+        }
+        if (ok && nt > 0) {
+            // (one phase after the other: the wait for a phase is over as well while the one before it has yet to end)
+            if (nt > 1) ok = mbar_wait(bar(ODONE), (uint32_t)(nt - 2) & 1u, ab);
+            ok = ok && mbar_wait(bar(ODONE), (uint32_t)(nt - 1) & 1u, ab);
+            tc_fence_after();
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        const float nan = __uint_as_float(0x7fffffffu);
+        float total = ok ? (float)sum : nan;
+        // (both halves leave the loop at the same tile, after they have read its maxima, or neither has)
+        tops[128 * half + q] = total;
+        asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
+        total += tops[128 * (1 - half) + q];
+        const bool live = i0 + q < P.n;
+        const size_t row = (size_t)w * P.n + i0 + (live ? q : 0);
+        const float inv = P.splits > 1 ? (total == total ? 1.f : nan) : total == 0.f ? 0.f : 1.f / total;
+        for (int c = 0; c < DVC / 2; c += 32) {
+            const int dim = dv0 + half * (DVC / 2) + c;
+            if (dim >= P.dv) break;
+            uint32_t o[32];
+            if (nt > 0) {
+                tc_ld32_issue(tO + lanes + half * (DVC / 2) + c, o);
+                tc_ld_wait(o);
+            } else
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0u;
+            if (!live) continue;
+            if (P.splits > 1) {
+                float *dst = P.part_out + (row * P.splits + split) * P.dv + dim;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (dim + i < P.dv) dst[i] = __uint_as_float(o[i]) * inv;
+                continue;
+            }
+            uint16_t *dst = P.out + row * P.dv + dim;
+            const bool wide = P.dv % 8 == 0 && (uintptr_t)P.out % 16 == 0;
+#pragma unroll
+            for (int i = 0; i < 32; i += 8) {
+                uint32_t h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) h[e] = bf16_pair(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
+                if (wide && dim + i < P.dv) *reinterpret_cast<uint4 *>(dst + i) = make_uint4(h[0], h[1], h[2], h[3]);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (dim + i + e < P.dv) dst[i + e] = (uint16_t)(h[e / 2] >> (16 * (e & 1)));
+            }
+        }
+        if (live && half == 0 && z == 0) {
+            if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[row * P.splits + split] = make_float2(ref, total);
+            else if (P.lse) {
+                // |x|^2 from the staged query, eight dimensions at a time
+                double xx = 0.0;
+                for (int ch = 0; ch < 8 * nkc; ++ch) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(smem_dyn + (size_t)(ch / 8) * MT_CHUNK + q * 128 + (((ch & 7) ^ (q & 7)) << 4));
+                    const uint32_t h[4] = {u.x, u.y, u.z, u.w};
+                    float s = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float lo = __uint_as_float(h[e] << 16), hi = __uint_as_float(h[e] & 0xffff0000u);
+                        s = fmaf(lo, lo, fmaf(hi, hi, s));
+                    }
+                    xx += (double)s;
+                }
+                P.lse[row] = map_lse(ref, total, k, xx);
+            }
+        }
+    } else if (warp < MT_SOFT + MT_CONV) {
+        // rows i * 16 + r0 of a stage, 16 codes of each
+        const int ct = tid - MT_SOFT * 32, r0 = ct >> 3, c16 = ct & 7;
+        struct Item {
+            uint4 codes[8];
+            uint32_t scale[8];
+        };
+        // stages in the order of the matrix instructions: scores of tile t, then values of tile t - 1
+        const int per_tile = nby + nbv, items = nt * per_tile;
+        auto place = [&](int i, int &t, int &b, bool &value) {
+            // S_0 | S_1 V_0 | S_2 V_1 | ... | V_last
+            if (i < nby) { t = 0; b = i; value = false; return; }
+            const int s = (i - nby) / per_tile, o = (i - nby) % per_tile;
+            if (s == nt - 1) { t = s; b = o; value = true; return; }
+            value = o >= nby;
+            t = value ? s : s + 1;
+            b = value ? o - nby : o;
+        };
+        auto load = [&](int i, Item &it) {
+            int t, b;
+            bool value;
+            place(i, t, b, value);
+            if (value) b += dv0 / 128;
+            const Cloud8 &cl = value ? P.v : P.y;
+#pragma unroll
+            for (int a = 0; a < 8; ++a) {
+                const int j = (t0 + t) * 128 + a * 16 + r0, byte = b * 128 + c16 * 16;
+                it.codes[a] = make_uint4(0u, 0u, 0u, 0u);
+                it.scale[a] = 0u;
+                if (j < len) {
+                    const size_t at = (size_t)w * P.m + j;
+                    it.scale[a] = cl.scales[at * cl.sb + b];
+                    if (byte < cl.cb) it.codes[a] = *reinterpret_cast<const uint4 *>(cl.codes + at * cl.cb + byte);
+                }
+            }
+        };
+        Item now, next;
+        bool ok = *ab == 0;
+        if (items > 0) load(0, next);
+        for (int i = 0; i < items && ok; ++i) {
+            now = next;
+            if (i + 1 < items) load(i + 1, next);
+            int t, b;
+            bool value;
+            place(i, t, b, value);
+            const int s = i % stages;
+            ok = mbar_wait(bar(TFULL + (t & 1)), (uint32_t)(t >> 1) & 1u, ab) && mbar_wait(bar(EMPTY + s), ((uint32_t)(i / stages) & 1u) ^ 1u, ab);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            unsigned char *stage = smem_dyn + (size_t)nkc * MT_CHUNK + (size_t)s * MT_STAGE + (c16 >> 2) * MT_CHUNK;
+#pragma unroll
+            for (int a = 0; a < 8; ++a) {
+                const int r = a * 16 + r0;
+                // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
+                const bool masked = terms[128 * (t & 1) + r] == -INFINITY;
+                const uint32_t e = now.scale[a], e1 = min(e, 134u);
+                uint32_t f = masked ? 0u : e == 255u ? 0x7fffu : (e1 + 120u) << 7;
+                f |= f << 16;
+                const uint32_t wd[4] = {now.codes[a].x, now.codes[a].y, now.codes[a].z, now.codes[a].w};
+                uint32_t h[8];
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    h[2 * x] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x1404)), f);
+                    h[2 * x + 1] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x3424)), f);
+                }
+                if (!masked && e > 134u && e != 255u) {
+                    uint32_t g = (e - 134u + 127u) << 7;
+                    g |= g << 16;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) h[x] = mul_bf16x2(h[x], g);
+                }
+                const int c0 = 2 * (c16 & 3), first = c16 >> 2;             // (the two halves of a quarter-warp store their pairs in opposite order)
+                uint4 p0 = make_uint4(h[0], h[1], h[2], h[3]), p1 = make_uint4(h[4], h[5], h[6], h[7]);
+                *reinterpret_cast<uint4 *>(stage + r * 128 + (((c0 + first) ^ (r & 7)) << 4)) = first ? p1 : p0;
+                *reinterpret_cast<uint4 *>(stage + r * 128 + (((c0 + 1 - first) ^ (r & 7)) << 4)) = first ? p0 : p1;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bar(FULL + s));
+                if (value && b == nbv - 1) mbar_arrive(bar(TEMPTY + (t & 1)));
+            }
+        }
+    } else if (warp == MT_SOFT + MT_CONV) {
+        if (lane == 0) {
+            bool ok = *ab == 0;
+            int i = 0;
+            for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
+                if (t < nt)
+                    for (int b = 0; b < nby && ok; ++b, ++i) {
+                        const int s = i % stages;
+                        if (!(ok = mbar_wait(bar(FULL + s), (uint32_t)(i / stages) & 1u, ab))) break;
+                        tc_fence_after();
+                        const int steps = min(8, (P.d - 128 * b + 15) / 16);
+                        for (int q = 0; q < steps; ++q)
+                            tc_mma(tmem + 128 * (t & 1), tc_desc(sX + (2 * b + (q >> 2)) * MT_CHUNK + (q & 3) * 32),
+                                   tc_desc(sR + s * MT_STAGE + (q >> 2) * MT_CHUNK + (q & 3) * 32), MT_IDESC, b | q ? 1u : 0u);
+                        tc_commit(bar(EMPTY + s));
+                        if (b == nby - 1) tc_commit(bar(SFULL + (t & 1)));
+                    }
+                if (t == 0 || !ok) continue;
+                const int u = t - 1;
+                if (!(ok = mbar_wait(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab))) break;
+                tc_fence_after();
+                for (int b = 0; b < nbv && ok; ++b, ++i) {
+                    const int s = i % stages;
+                    if (!(ok = mbar_wait(bar(FULL + s), (uint32_t)(i / stages) & 1u, ab))) break;
+                    tc_fence_after();
+                    for (int q = 0; q < 8; ++q)
+                        mma_tmem(tO + 128 * b, tmem + 128 * (u & 1) + 8 * q, desc_columns(sR + s * MT_STAGE + q * 2048), MT_IDESC_V, u | q ? 1u : 0u);
+                    tc_commit(bar(EMPTY + s));
+                }
+                if (ok) tc_commit(bar(ODONE));
+            }
+            // what was issued is over before tensor memory is given back
+            tc_commit(bar(LAST));
+            int unused = 0;
+            mbar_wait(bar(LAST), 0, &unused);
+        }
+    } else {
+        float next[4];
+        auto fetch = [&](int t) {
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const int j = (t0 + t) * 128 + lane + 32 * a;
+                next[a] = -INFINITY;
+                if (j < len) {
+                    const size_t at = (size_t)w * P.m + j;
+                    next[a] = map_term(k, P.g ? P.g[at] : 0.0, P.y.norms[at]);
+                }
+            }
+        };
+        bool ok = *ab == 0;
+        if (nt > 0) fetch(0);
+        for (int t = 0; t < nt && ok; ++t) {
+            ok = mbar_wait(bar(TEMPTY + (t & 1)), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+#pragma unroll
+            for (int a = 0; a < 4; ++a) terms[128 * (t & 1) + lane + 32 * a] = next[a];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(TFULL + (t & 1)));
+            if (t + 1 < nt) fetch(t + 1);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == MT_SOFT + MT_CONV) tc_dealloc<512>(tmem);
+}
+
+template <int DVC>
+skb_status launch(const Map &P, cudaStream_t st)
+{
+    const int nkc = (P.d + 63) / 64, nrt = (P.n + 127) / 128, nz = (P.dv + DVC - 1) / DVC;
+    const int room = MAP_TILES_SMEM - (int)MT_MISC - nkc * (int)MT_CHUNK, stages = min(MT_MAX_STAGES, room / (int)MT_STAGE);
+    const int smem = nkc * (int)MT_CHUNK + stages * (int)MT_STAGE + (int)MT_MISC;
+    cudaFuncSetAttribute(map_tiles_kernel<DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    map_tiles_kernel<DVC><<<dim3(nrt * nz, P.splits, P.W), MT_THREADS, smem, st>>>(P, nrt, stages);
+    return op_launched("map");
+}
+
+}  // namespace
+
+skb_status launch_map_tiles(const Map &P, cudaStream_t st)
+{
+    return P.dv <= 128 ? launch<128>(P, st) : launch<256>(P, st);
+}
+
+}  // namespace skb
