@@ -546,8 +546,8 @@ skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int 
  * the product with the values, are rounded to 11 bits, sums are fp32.  A value below 2^-25 of the largest of its 128
  * dimensions among 64 targets next to it may count as zero.
  * d and dv <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on `stream` of the current device and returns; the workspace of
- * sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv) bytes (0: a bad shape; dv = 0: d; device, 256-byte aligned) is in use until they are
- * done: calls that may overlap need one each.
+ * sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv) bytes (0: a bad shape; dv = 0: v is null; device, 256-byte aligned) is in use until
+ * they are done: calls that may overlap need one each.
  */
 size_t sinkhorn_cloud8_map_workspace_bytes(int W, int n, int m, int d, int dv);
 skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, const float *eps, const void *v, const int *lengths, int W, int n, int m,

@@ -430,7 +430,7 @@ def cloud8_map(x, y, g, eps, v=None, *, lengths=None, lse=False, out=None):
         raise ValueError("out must be a contiguous bfloat16 tensor [W, n, dv] on the queries' device")
     x, eps = x.contiguous(), eps.contiguous()
     g, lengths = (None if t is None else t.contiguous() for t in (g, lengths))
-    need = lib.sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv)
+    need = lib.sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, 0 if v is None else dv)
     if need == 0:
         raise SkbError(2, "shape not supported: W, n, m, d >= 1, d and dv <= 1024, n and m <= 262143, W <= 65535")
     with _on(device):

@@ -476,9 +476,9 @@ MapPlan map_plan(int W, int n, int m, int d, int dv, int sms)
     return p;
 }
 size_t pad256(size_t b) { return (b + 255) / 256 * 256; }
-size_t map_workspace(int W, int n, int dv, int splits)
+size_t map_parts_bytes(int W, int n, int dv, int splits)
 {
-    return splits == 1 ? 256 : pad256((size_t)W * n * splits * 8) + pad256((size_t)W * n * splits * dv * 4);
+    return splits == 1 ? 0 : pad256((size_t)W * n * splits * 8) + pad256((size_t)W * n * splits * dv * 4);
 }
 
 }  // namespace
@@ -486,11 +486,17 @@ size_t map_workspace(int W, int n, int dv, int splits)
 
 using namespace skb;
 
+// own_values: dv is that of a cloud of its own
+static size_t map_workspace(int W, int n, int m, int d, int dv, bool own_values)
+{
+    // (what any device may split into: the workspace does not depend on the current one)
+    const MapPlan p = map_plan(W, n, m, d, dv, MAP_MAX_SMS);
+    return 256 + map_parts_bytes(W, n, dv, p.splits) + (p.tiles ? pad256(map_staged_bytes(W, m, d, dv, own_values)) : 0);
+}
+
 extern "C" size_t sinkhorn_cloud8_map_workspace_bytes(int W, int n, int m, int d, int dv)
 {
-    if (map_refused(W, n, m, d, dv)) return 0;
-    // (what any device may split into: the workspace does not depend on the current one)
-    return map_workspace(W, n, dv ? dv : d, map_plan(W, n, m, d, dv ? dv : d, MAP_MAX_SMS).splits);
+    return map_refused(W, n, m, d, dv) ? 0 : map_workspace(W, n, m, d, dv ? dv : d, dv != 0);
 }
 
 extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, const float *eps, const void *v, const int *lengths, int W, int n, int m,
@@ -504,7 +510,7 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     if ((uintptr_t)x % 2 || (uintptr_t)out % 2 || (uintptr_t)g % 8 || (uintptr_t)eps % 4 || (uintptr_t)lse % 4 || (uintptr_t)lengths % 4)
         return op_fail(SKB_ERR_WORKSPACE, "arrays must be aligned to their types");
     const int depth = v ? dv : d;
-    if (workspace_bytes < sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, depth)) return op_fail(SKB_ERR_WORKSPACE, "workspace too small");
+    if (workspace_bytes < map_workspace(W, n, m, d, depth, v != nullptr)) return op_fail(SKB_ERR_WORKSPACE, "workspace too small");
     int dev = 0, sms = 0;
     cudaGetDevice(&dev);
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");
@@ -518,10 +524,11 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     P.splits = plan.splits;
     P.part_ml = (float *)workspace;
     P.part_out = (float *)((char *)workspace + pad256((size_t)W * n * P.splits * 8));
+    void *room = (char *)workspace + map_parts_bytes(W, n, depth, P.splits);
     CUtensorMap ty, tv;
     if (!plan.tiles && (!points_map(&ty, P.y.codes, P.y.cb, m, W, MR_T) || !points_map(&tv, P.v.codes, P.v.cb, m, W, MR_T)))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    const skb_status rc = plan.tiles ? launch_map_tiles(P, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
+    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
     if (rc != SKB_OK || P.splits == 1) return rc;
     map_join_kernel<<<W * n, 128, 0, (cudaStream_t)stream>>>(P);
     return op_launched("map");

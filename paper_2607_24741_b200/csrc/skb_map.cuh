@@ -23,10 +23,13 @@ struct Map {
     float *part_ml, *part_out;                // splits > 1: [W, n, splits] pairs, [W, n, splits, dv]
     int W, n, m, d, dv, splits;
     int own_values;                           // v is not y
+    unsigned char *staged_y, *staged_v;       // many queries: bank and values as bf16 (the same where v is y)
+    float *terms;                             // ... and what targets add to exponents, [W, tiles, 128]
 };
 
-// Many queries (skb_map_tc.cu): d <= MAP_TILES_MAX_D, P.splits parts of a lane's bank.
-skb_status launch_map_tiles(const Map &P, cudaStream_t st);
+// Many queries (skb_map_tc.cu): d <= MAP_TILES_MAX_D, P.splits parts of a lane's bank, room for the bank in bf16 (256-byte aligned).
+size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values);
+skb_status launch_map_tiles(Map &P, void *room, cudaStream_t st);
 
 __device__ __forceinline__ int map_length(const Map &P, int w) { return P.lengths ? min(max(P.lengths[w], 0), P.m) : P.m; }
 // log2(e) / eps; NaN, and so are the lane's images, where eps is not a positive number

@@ -1,21 +1,24 @@
 // Images under the entropic map of a stored cloud for many queries (see skb_map.cu for the mathematics): both products on tcgen05.
 //
-// A block takes 128 queries, a part of the bank, and up to 256 dimensions of the values (deeper ones: further blocks, which form the scores again).
-// Per tile of 128 targets
+// map_stage_kernel writes the bank once as bf16 into the workspace, in the order in which the matrix unit wants it in shared memory (blocks of 128 targets by
+// 128 dimensions, 32 KB, 128-byte swizzle; the same layout is K-major for the scores and MN-major for the images, so values are not
+// transposed), masked targets and what is past the ends as zeros, and the targets' terms.  A value is four bits times a power of two, which
+// bf16 holds over all of the clouds' range, so products are those of the values, exactly; f16 would round weights to 11 bits instead of 8, but
+// cannot hold values of a bank whose scales differ.  Codes made into bf16 by warps of every block of queries cost more than all else: 64 lanes
+// of 1024 x 1024 x 512 took 858 us that way.
+//
+// map_tiles_kernel: a block takes 128 queries, a part of the bank, and up to 256 dimensions of the values (deeper ones: further blocks, which form the
+// scores again).  Per tile of 128 targets
 //      S = X . Y^T       bf16, fp32 in tensor memory, two buffers
 //      P = exp2(2k S + term - reference) in bf16, into S's place in tensor memory
 //      O += P . V        bf16, fp32 in tensor memory
-// so that the scores of the next tile are formed while this one's exponentials are.  Codes become bf16 on their way into shared memory: a value is four
-// bits times a power of two, which bf16 holds over all of the clouds' range, so products are those of the values, exactly; f16 would
-// round weights to 11 bits instead of 8, but cannot hold values of a bank whose scales differ.  Outputs are bf16.
-// The weights are summed in fp32 before they are rounded.
+// so that the scores of the next tile are formed while this one's exponentials are.  Outputs are bf16; the weights are summed in fp32 before they
+// are rounded.
 //   warps 0-7    softmax: a thread to a query and half of a tile's targets; the two halves of a query exchange their maxima.  The reference is a
 //                whole number, raised only when a tile's maximum passes it by more than 8 (weights up to 2^8 are as good in bf16 as those
 //                below 1): O is then multiplied by a power of two, exactly
-//   warps 8-11   codes -> bf16 in the matrix unit's layout (128-byte swizzle), 128 targets by 128 dimensions a stage of 32 KB, the next stage's
-//                codes on their way to registers meanwhile.  The same layout is K-major for S and MN-major for O: values are not transposed
-//   warp 12      matrix instructions, one thread: S of tile t + 1 before O of tile t
-//   warp 13      the targets' terms
+//   warp 8       loads: bulk copies of 32 KB and of a tile's terms
+//   warp 9       matrix instructions, one thread: S of tile t + 1 before O of tile t
 // What bounds it: at 128 dimensions the exponentials (128 x 128 of a tile at 16 a clock take as long as its products), deeper the products.
 // Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and the block's images are NaN.
 #include <cuda.h>
@@ -30,7 +33,7 @@
 namespace skb {
 namespace {
 
-constexpr int MT_SOFT = 8, MT_CONV = 4, MT_THREADS = (MT_SOFT + MT_CONV + 2) * 32;
+constexpr int MT_SOFT = 8, MT_LOAD = MT_SOFT, MT_MMA = MT_SOFT + 1, MT_THREADS = (MT_SOFT + 2) * 32;
 constexpr uint32_t MT_CHUNK = 128 * 128, MT_STAGE = 2 * MT_CHUNK;         // 128 points by 64, 128 dimensions of bf16
 constexpr int MT_MAX_STAGES = 5;
 constexpr uint32_t MT_MISC = 3072;
@@ -75,8 +78,61 @@ __device__ __forceinline__ bool both(bool ok, int barrier)
     return r != 0;
 }
 
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t mbar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(mbar) : "memory");
+}
+
+// The bank as bf16.  A thread takes 16 codes of a target; eight to a target's block of 128 dimensions.
+__global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ Map P, const int tiles, const int nby, const int nbv)
+{
+    const int nb = nby + nbv, c16 = threadIdx.x & 7;
+    const long long item = (long long)blockIdx.x * 32 + (threadIdx.x >> 3);     // (lane, tile, block, target)
+    const int r = (int)(item & 127), b0 = (int)((item >> 7) % nb), t = (int)((item >> 7) / nb % tiles);
+    const long long w = (item >> 7) / nb / tiles;
+    if (w >= P.W) return;
+    const int len = map_length(P, (int)w), j = t * 128 + r;
+    if (t * 128 >= len) return;                                                // (a tile that no one reads)
+    const bool value = b0 >= nby;
+    const int b = value ? b0 - nby : b0;
+    const Cloud8 &cl = value ? P.v : P.y;
+    float term = -INFINITY;
+    uint4 codes = make_uint4(0u, 0u, 0u, 0u);
+    uint32_t e = 0;
+    if (j < len) {
+        const size_t at = (size_t)w * P.m + j;
+        e = cl.scales[at * cl.sb + b];
+        if (b * 128 + c16 * 16 < cl.cb) codes = *reinterpret_cast<const uint4 *>(cl.codes + at * cl.cb + b * 128 + c16 * 16);
+        term = map_term(map_scale(P, (int)w), P.g ? P.g[at] : 0.0, P.y.norms[at]);
+    }
+    if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = term;
+    // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
+    const bool masked = term == -INFINITY;
+    const uint32_t e1 = min(e, 134u);
+    uint32_t f = masked ? 0u : e == 255u ? 0x7fffu : (e1 + 120u) << 7;
+    f |= f << 16;
+    const uint32_t wd[4] = {codes.x, codes.y, codes.z, codes.w};
+    uint32_t h[8];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        h[2 * x] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x1404)), f);
+        h[2 * x + 1] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x3424)), f);
+    }
+    if (!masked && e > 134u && e != 255u) {
+        uint32_t g = (e - 134u + 127u) << 7;
+        g |= g << 16;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) h[x] = mul_bf16x2(h[x], g);
+    }
+    unsigned char *dst = (value ? P.staged_v : P.staged_y) + (((size_t)w * tiles + t) * (value ? nbv : nby) + b) * MT_STAGE + (c16 >> 2) * MT_CHUNK + r * 128;
+    const int c0 = 2 * (c16 & 3);
+    *reinterpret_cast<uint4 *>(dst + ((c0 ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4 *>(dst + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+}
+
 template <int DVC>
-__global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ Map P, const int nrt, const int stages)
+__global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ Map P, const int nrt, const int stages, const int lane_tiles)
 {
     extern __shared__ __align__(1024) unsigned char smem_dyn[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -100,19 +156,19 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
     const int len = map_length(P, w), tiles = (len + 127) / 128;
     const int t0 = (int)((long long)tiles * split / P.splits), t1 = (int)((long long)tiles * (split + 1) / P.splits), nt = t1 - t0;
     if (tid == 0) {
-        for (int s = 0; s < stages; ++s) { mbar_init(bar(FULL + s), MT_CONV); mbar_init(bar(EMPTY + s), 1); }
+        for (int s = 0; s < stages; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(EMPTY + s), 1); }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar(SFULL + b), 1);
             mbar_init(bar(PFULL + b), MT_SOFT);
             mbar_init(bar(TFULL + b), 1);
-            mbar_init(bar(TEMPTY + b), MT_SOFT + MT_CONV);
+            mbar_init(bar(TEMPTY + b), MT_SOFT);
         }
         mbar_init(bar(ODONE), 1);
         mbar_init(bar(LAST), 1);
         *abort_flag = (base & 1023u) ? 1 : 0;                              // (the swizzle counts from 1024-byte boundaries)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == MT_SOFT + MT_CONV) tc_alloc<512>(tmem_holder);
+    if (warp == MT_MMA) tc_alloc<512>(tmem_holder);
     // the queries
     {
         const bool wide = P.d % 8 == 0 && (uintptr_t)P.x % 16 == 0;
@@ -300,90 +356,40 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                 P.lse[row] = map_lse(ref, total, k, xx);
             }
         }
-    } else if (warp < MT_SOFT + MT_CONV) {
-        // rows i * 16 + r0 of a stage, 16 codes of each
-        const int ct = tid - MT_SOFT * 32, r0 = ct >> 3, c16 = ct & 7;
-        struct Item {
-            uint4 codes[8];
-            uint32_t scale[8];
-        };
-        // stages in the order of the matrix instructions: scores of tile t, then values of tile t - 1
-        const int per_tile = nby + nbv, items = nt * per_tile;
-        auto place = [&](int i, int &t, int &b, bool &value) {
-            // S_0 | S_1 V_0 | S_2 V_1 | ... | V_last
-            if (i < nby) { t = 0; b = i; value = false; return; }
-            const int s = (i - nby) / per_tile, o = (i - nby) % per_tile;
-            if (s == nt - 1) { t = s; b = o; value = true; return; }
-            value = o >= nby;
-            t = value ? s : s + 1;
-            b = value ? o - nby : o;
-        };
-        auto load = [&](int i, Item &it) {
-            int t, b;
-            bool value;
-            place(i, t, b, value);
-            if (value) b += dv0 / 128;
-            const Cloud8 &cl = value ? P.v : P.y;
-#pragma unroll
-            for (int a = 0; a < 8; ++a) {
-                const int j = (t0 + t) * 128 + a * 16 + r0, byte = b * 128 + c16 * 16;
-                it.codes[a] = make_uint4(0u, 0u, 0u, 0u);
-                it.scale[a] = 0u;
-                if (j < len) {
-                    const size_t at = (size_t)w * P.m + j;
-                    it.scale[a] = cl.scales[at * cl.sb + b];
-                    if (byte < cl.cb) it.codes[a] = *reinterpret_cast<const uint4 *>(cl.codes + at * cl.cb + byte);
+    } else if (warp == MT_LOAD) {
+        if (lane == 0) {
+            const unsigned char *ys = P.staged_y + ((size_t)w * lane_tiles + t0) * nby * MT_STAGE;
+            const int all_v = (P.dv + 127) / 128;
+            const unsigned char *vs = P.staged_v + (((size_t)w * lane_tiles + t0) * all_v + dv0 / 128) * MT_STAGE;
+            const float *term = P.terms + ((size_t)w * lane_tiles + t0) * 128;
+            bool ok = *ab == 0;
+            int i = 0;
+            auto stage = [&](const unsigned char *src) {
+                const int s = i % stages;
+                if (!(ok = mbar_wait(bar(EMPTY + s), ((uint32_t)(i / stages) & 1u) ^ 1u, ab))) return;
+                mbar_expect_tx(bar(FULL + s), MT_STAGE);
+                bulk_load(sR + s * MT_STAGE, src, MT_STAGE, bar(FULL + s));
+                ++i;
+            };
+            int terms_issued = 0;
+            // in the order of the matrix instructions: scores of tile t, then images of tile t - 1
+            for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
+                if (t < nt) {
+                    if (!(ok = mbar_wait(bar(TEMPTY + (t & 1)), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab))) break;
+                    mbar_expect_tx(bar(TFULL + (t & 1)), 512);
+                    bulk_load(smem_u32(terms) + 512 * (t & 1), term + (size_t)t * 128, 512, bar(TFULL + (t & 1)));
+                    ++terms_issued;
+                    for (int b = 0; b < nby && ok; ++b) stage(ys + ((size_t)t * nby + b) * MT_STAGE);
                 }
+                if (t > 0)
+                    for (int b = 0; b < nbv && ok; ++b) stage(vs + ((size_t)(t - 1) * all_v + b) * MT_STAGE);
             }
-        };
-        Item now, next;
-        bool ok = *ab == 0;
-        if (items > 0) load(0, next);
-        for (int i = 0; i < items && ok; ++i) {
-            now = next;
-            if (i + 1 < items) load(i + 1, next);
-            int t, b;
-            bool value;
-            place(i, t, b, value);
-            const int s = i % stages;
-            ok = mbar_wait(bar(TFULL + (t & 1)), (uint32_t)(t >> 1) & 1u, ab) && mbar_wait(bar(EMPTY + s), ((uint32_t)(i / stages) & 1u) ^ 1u, ab);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            unsigned char *stage = smem_dyn + (size_t)nkc * MT_CHUNK + (size_t)s * MT_STAGE + (c16 >> 2) * MT_CHUNK;
-#pragma unroll
-            for (int a = 0; a < 8; ++a) {
-                const int r = a * 16 + r0;
-                // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
-                const bool masked = terms[128 * (t & 1) + r] == -INFINITY;
-                const uint32_t e = now.scale[a], e1 = min(e, 134u);
-                uint32_t f = masked ? 0u : e == 255u ? 0x7fffu : (e1 + 120u) << 7;
-                f |= f << 16;
-                const uint32_t wd[4] = {now.codes[a].x, now.codes[a].y, now.codes[a].z, now.codes[a].w};
-                uint32_t h[8];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    h[2 * x] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x1404)), f);
-                    h[2 * x + 1] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x3424)), f);
-                }
-                if (!masked && e > 134u && e != 255u) {
-                    uint32_t g = (e - 134u + 127u) << 7;
-                    g |= g << 16;
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) h[x] = mul_bf16x2(h[x], g);
-                }
-                const int c0 = 2 * (c16 & 3), first = c16 >> 2;             // (the two halves of a quarter-warp store their pairs in opposite order)
-                uint4 p0 = make_uint4(h[0], h[1], h[2], h[3]), p1 = make_uint4(h[4], h[5], h[6], h[7]);
-                *reinterpret_cast<uint4 *>(stage + r * 128 + (((c0 + first) ^ (r & 7)) << 4)) = first ? p1 : p0;
-                *reinterpret_cast<uint4 *>(stage + r * 128 + (((c0 + 1 - first) ^ (r & 7)) << 4)) = first ? p0 : p1;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(bar(FULL + s));
-                if (value && b == nbv - 1) mbar_arrive(bar(TEMPTY + (t & 1)));
-            }
+            // nothing may land in shared memory after the block has gone: the last load of every buffer, with a bound of its own
+            int unused = 0;
+            for (int q = max(0, i - stages); q < i; ++q) mbar_wait(bar(FULL + q % stages), (uint32_t)(q / stages) & 1u, &unused);
+            for (int q = max(0, terms_issued - 2); q < terms_issued; ++q) mbar_wait(bar(TFULL + (q & 1)), (uint32_t)(q >> 1) & 1u, &unused);
         }
-    } else if (warp == MT_SOFT + MT_CONV) {
+    } else {
         if (lane == 0) {
             bool ok = *ab == 0;
             int i = 0;
@@ -419,36 +425,11 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             int unused = 0;
             mbar_wait(bar(LAST), 0, &unused);
         }
-    } else {
-        float next[4];
-        auto fetch = [&](int t) {
-#pragma unroll
-            for (int a = 0; a < 4; ++a) {
-                const int j = (t0 + t) * 128 + lane + 32 * a;
-                next[a] = -INFINITY;
-                if (j < len) {
-                    const size_t at = (size_t)w * P.m + j;
-                    next[a] = map_term(k, P.g ? P.g[at] : 0.0, P.y.norms[at]);
-                }
-            }
-        };
-        bool ok = *ab == 0;
-        if (nt > 0) fetch(0);
-        for (int t = 0; t < nt && ok; ++t) {
-            ok = mbar_wait(bar(TEMPTY + (t & 1)), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-#pragma unroll
-            for (int a = 0; a < 4; ++a) terms[128 * (t & 1) + lane + 32 * a] = next[a];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(TFULL + (t & 1)));
-            if (t + 1 < nt) fetch(t + 1);
-        }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == MT_SOFT + MT_CONV) tc_dealloc<512>(tmem);
+    if (warp == MT_MMA) tc_dealloc<512>(tmem);
 }
 
 template <int DVC>
@@ -458,14 +439,29 @@ skb_status launch(const Map &P, cudaStream_t st)
     const int room = MAP_TILES_SMEM - (int)MT_MISC - nkc * (int)MT_CHUNK, stages = min(MT_MAX_STAGES, room / (int)MT_STAGE);
     const int smem = nkc * (int)MT_CHUNK + stages * (int)MT_STAGE + (int)MT_MISC;
     cudaFuncSetAttribute(map_tiles_kernel<DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    map_tiles_kernel<DVC><<<dim3(nrt * nz, P.splits, P.W), MT_THREADS, smem, st>>>(P, nrt, stages);
+    map_tiles_kernel<DVC><<<dim3(nrt * nz, P.splits, P.W), MT_THREADS, smem, st>>>(P, nrt, stages, (P.m + 127) / 128);
     return op_launched("map");
 }
 
 }  // namespace
 
-skb_status launch_map_tiles(const Map &P, cudaStream_t st)
+size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values)
 {
+    const size_t tiles = (size_t)W * ((m + 127) / 128);
+    return tiles * 512 + tiles * MT_STAGE * ((d + 127) / 128 + (own_values ? (dv + 127) / 128 : 0));
+}
+
+skb_status launch_map_tiles(Map &P, void *room, cudaStream_t st)
+{
+    const int tiles = (P.m + 127) / 128, nby = (P.d + 127) / 128, nbv = P.own_values ? (P.dv + 127) / 128 : 0;
+    P.staged_y = (unsigned char *)room;
+    P.staged_v = P.own_values ? P.staged_y + (size_t)P.W * tiles * nby * MT_STAGE : P.staged_y;
+    P.terms = (float *)(P.staged_y + (size_t)P.W * tiles * (nby + nbv) * MT_STAGE);
+    const long long blocks = (long long)P.W * tiles * (nby + nbv) * 4;
+    if (blocks > 0x7fffffffLL) return op_fail(SKB_ERR_SHAPE, "bank too large");
+    map_stage_kernel<<<(unsigned)blocks, 256, 0, st>>>(P, tiles, nby, nbv);
+    const skb_status rc = op_launched("map");
+    if (rc != SKB_OK) return rc;
     return P.dv <= 128 ? launch<128>(P, st) : launch<256>(P, st);
 }
 
