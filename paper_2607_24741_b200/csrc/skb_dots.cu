@@ -473,6 +473,20 @@ bool points_map(CUtensorMap *tm, const void *codes, int row_bytes, int npts, int
     return encoder() && make_map(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, rb, npts, W, rb, rb * npts, 128, box_points);
 }
 
+bool staged_map(CUtensorMap *tm, const void *base, size_t rows)
+{
+    const cuuint64_t dims[2] = {64, rows}, strides[1] = {128};
+    const cuuint32_t box[2] = {64, 64}, step[2] = {1, 1};
+    return encoder() && encoder()(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool queries_map(CUtensorMap *tm, const void *x, int d, int n, int W)
+{
+    const size_t rb = 2 * (size_t)d;
+    return encoder() && make_map(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, x, d, n, W, rb, rb * n, 64, 128);
+}
+
 DotsCloud dots_cloud(const void *base, const Cloud4 &c, int dtype, int d, size_t row)
 {
     if (dtype == SKB_BF16) return {(const uint16_t *)base + row * d, nullptr, nullptr, 2 * d, 0};

@@ -468,7 +468,7 @@ MapPlan map_plan(int W, int n, int m, int d, int dv, int sms)
 {
     MapPlan p;
     p.tiles = n > MAP_ROWS_MAX && d <= MAP_TILES_MAX_D;
-    const long long blocks = p.tiles ? (long long)W * ((n + 127) / 128) * ((dv + 255) / 256) : (long long)W * ((n + 7) / 8);
+    const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * ((n + 7) / 8);
     const long long tiles = p.tiles ? (m + 127) / 128 : (m + MR_T - 1) / MR_T;
     long long s = p.tiles ? sms / blocks : (2LL * sms + blocks - 1) / blocks;
     if (s > tiles / 2) s = tiles / 2;

@@ -34,19 +34,72 @@ namespace skb {
 namespace {
 
 constexpr int MT_SOFT = 8, MT_LOAD = MT_SOFT, MT_MMA = MT_SOFT + 1, MT_THREADS = (MT_SOFT + 2) * 32;
-constexpr uint32_t MT_CHUNK = 128 * 128, MT_STAGE = 2 * MT_CHUNK;         // 128 points by 64, 128 dimensions of bf16
-constexpr int MT_MAX_STAGES = 5;
+constexpr uint32_t MT_CHUNK = 128 * 128, MT_BLOCK = 2 * MT_CHUNK;         // 128 points by 64, 128 dimensions of bf16
+constexpr int MT_MAX_STAGES = 8;
 constexpr uint32_t MT_MISC = 3072;
 constexpr float MT_SLACK = 8.f;
 
-constexpr uint32_t MT_IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);   // D fp32, A and B bf16, 128 x 128
-constexpr uint32_t MT_IDESC_V = MT_IDESC | (1u << 16);                    // B with its columns next to each other
+// D fp32, A and B bf16, 128 queries (a pair of blocks: 256) by 128
+template <bool PAIR> constexpr uint32_t MT_IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | (((PAIR ? 256u : 128u) >> 4) << 24);
+template <bool PAIR> constexpr uint32_t MT_IDESC_V = MT_IDESC<PAIR> | (1u << 16);     // B with its columns next to each other
 
-// D += A . B with A in tensor memory
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+template <bool PAIR> __device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    if constexpr (!PAIR) tc_mma(d, a, b, MT_IDESC<PAIR>, accumulate);
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(MT_IDESC<PAIR>), "r"(accumulate) : "memory");
+}
+// ... with A in tensor memory
+template <bool PAIR> __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t accumulate)
+{
+    if constexpr (PAIR)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(MT_IDESC_V<PAIR>), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                     ::"r"(d), "r"(a), "l"(b), "r"(MT_IDESC_V<PAIR>), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t a, uint32_t rank)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// an arrival once the matrix instructions so far are done; a pair's, at both blocks' barriers (or at the first `at` of them)
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t mbar, uint32_t at = 2)
+{
+    if constexpr (!PAIR) tc_commit(mbar);
+    else
+        for (uint32_t r = 0; r < at; ++r)
+            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(in_block(mbar, r)) : "memory");
+}
+// 64 rows of 128 bytes; the barrier may be the other block's of a pair
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap *tm, int row, uint32_t mbar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(0), "r"(row), "r"(mbar) : "memory");
+}
+// 128 queries by 64 dimensions
+template <bool PAIR> __device__ __forceinline__ void load_queries(uint32_t dst, const CUtensorMap *tm, int dim, int query, int lane, uint32_t mbar)
+{
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(dim), "r"(query), "r"(lane), "r"(mbar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(dim), "r"(query), "r"(lane), "r"(mbar) : "memory");
+}
+// as mbar_wait, for what a pair's other block has done before it arrived
+__device__ __forceinline__ bool wait_cluster(uint32_t a, uint32_t parity, volatile int *abort_flag)
+{
+    if (!mbar_wait(a, parity, abort_flag)) return false;
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    return true;
 }
 // rows of 64 columns (128 bytes), 8-row groups 1024 bytes apart, the next 64 columns a chunk further
 __device__ __forceinline__ uint64_t desc_columns(uint32_t saddr)
@@ -125,24 +178,30 @@ __global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ 
 #pragma unroll
         for (int x = 0; x < 8; ++x) h[x] = mul_bf16x2(h[x], g);
     }
-    unsigned char *dst = (value ? P.staged_v : P.staged_y) + (((size_t)w * tiles + t) * (value ? nbv : nby) + b) * MT_STAGE + (c16 >> 2) * MT_CHUNK + r * 128;
+    unsigned char *dst = (value ? P.staged_v : P.staged_y) + (((size_t)w * tiles + t) * (value ? nbv : nby) + b) * MT_BLOCK + (c16 >> 2) * MT_CHUNK + r * 128;
     const int c0 = 2 * (c16 & 3);
     *reinterpret_cast<uint4 *>(dst + ((c0 ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
     *reinterpret_cast<uint4 *>(dst + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
 }
 
-template <int DVC>
-__global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ Map P, const int nrt, const int stages, const int lane_tiles)
+// PAIR: two blocks of a cluster share what they read, half of the targets (scores) or of the dimensions (images) of a stage each; the first issues
+// the instructions of both, on 256 queries.
+template <int DVC, bool PAIR>
+__global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmy,
+                                                                  const __grid_constant__ CUtensorMap tmv, const __grid_constant__ Map P, const int nrt,
+                                                                  const int stages, const int lane_tiles, const int tma_x)
 {
+    constexpr uint32_t STAGE = PAIR ? MT_BLOCK / 2 : MT_BLOCK;
     extern __shared__ __align__(1024) unsigned char smem_dyn[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rt = blockIdx.x % nrt, z = blockIdx.x / nrt, split = blockIdx.y, w = blockIdx.z;
+    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u;
     const int i0 = rt * 128, dv0 = z * DVC;
     const int nkc = (P.d + 63) / 64, nby = (P.d + 127) / 128, nbv = (min(DVC, P.dv - dv0) + 127) / 128;
 
     // shared memory: the queries' chunks, the ring, and what is small
     const uint32_t base = smem_u32(smem_dyn), sX = base, sR = base + (uint32_t)nkc * MT_CHUNK;
-    unsigned char *misc = smem_dyn + (size_t)nkc * MT_CHUNK + (size_t)stages * MT_STAGE;
+    unsigned char *misc = smem_dyn + (size_t)nkc * MT_CHUNK + (size_t)stages * STAGE;
     float *terms = reinterpret_cast<float *>(misc);                        // [2][128]
     float *tops = terms + 256;                                             // [2][128]: halves' maxima, and their sums at the end
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(tops + 256);
@@ -150,8 +209,8 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
     int *abort_flag = reinterpret_cast<int *>(tmem_holder + 1);
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     constexpr int FULL = 0, EMPTY = MT_MAX_STAGES, SFULL = 2 * MT_MAX_STAGES, PFULL = SFULL + 2, ODONE = PFULL + 2, TFULL = ODONE + 1, TEMPTY = TFULL + 2,
-                  LAST = TEMPTY + 2;
-    static_assert(LAST < 32, "barriers");
+                  LAST = TEMPTY + 2, XFULL = LAST + 1;
+    static_assert(XFULL < 32, "barriers");
 
     const int len = map_length(P, w), tiles = (len + 127) / 128;
     const int t0 = (int)((long long)tiles * split / P.splits), t1 = (int)((long long)tiles * (split + 1) / P.splits), nt = t1 - t0;
@@ -159,38 +218,41 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         for (int s = 0; s < stages; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(EMPTY + s), 1); }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar(SFULL + b), 1);
-            mbar_init(bar(PFULL + b), MT_SOFT);
+            mbar_init(bar(PFULL + b), PAIR ? 2 * MT_SOFT : MT_SOFT);
             mbar_init(bar(TFULL + b), 1);
             mbar_init(bar(TEMPTY + b), MT_SOFT);
         }
         mbar_init(bar(ODONE), 1);
         mbar_init(bar(LAST), 1);
+        mbar_init(bar(XFULL), 1);
         *abort_flag = (base & 1023u) ? 1 : 0;                              // (the swizzle counts from 1024-byte boundaries)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == MT_MMA) tc_alloc<512>(tmem_holder);
-    // the queries
-    {
-        const bool wide = P.d % 8 == 0 && (uintptr_t)P.x % 16 == 0;
+    if (warp == MT_MMA) {
+        if constexpr (!PAIR) tc_alloc<512>(tmem_holder);
+        else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_holder)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+    }
+    // the queries: by TMA (below), or where their rows are no whole number of 16 bytes by the threads, one value after the other
+    if (!tma_x)
         for (int i = tid; i < 128 * 8 * nkc; i += MT_THREADS) {
             const int r = i / (8 * nkc), ch = i % (8 * nkc), k0 = 8 * ch;
             uint32_t v[4] = {0u, 0u, 0u, 0u};
             if (i0 + r < P.n) {
                 const uint16_t *src = P.x + ((size_t)w * P.n + i0 + r) * P.d + k0;
-                if (wide && k0 < P.d) {
-                    const uint4 u = *reinterpret_cast<const uint4 *>(src);
-                    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-                } else
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (k0 + e < P.d) v[e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
+                for (int e = 0; e < 8; ++e)
+                    if (k0 + e < P.d) v[e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
             }
             *reinterpret_cast<uint4 *>(smem_dyn + (size_t)(ch / 8) * MT_CHUNK + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
         }
-    }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_sync_all();                                // both blocks' barriers are there, and their queries
     tc_fence_after();
     const uint32_t tmem = *tmem_holder, tO = tmem + 256;
     volatile int *ab = abort_flag;
@@ -287,7 +349,11 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             tc_st_wait();
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(PFULL + b));
+            if (lane == 0) {
+                if constexpr (PAIR)
+                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_block(bar(PFULL + b), 0)) : "memory");
+                else mbar_arrive(bar(PFULL + b));
+            }
         }
         if (ok && nt > 0) {
             // (one phase after the other: the wait for a phase is over as well while the one before it has yet to end)
@@ -340,9 +406,9 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         if (live && half == 0 && z == 0) {
             if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[row * P.splits + split] = make_float2(ref, total);
             else if (P.lse) {
-                // |x|^2 from the staged query, eight dimensions at a time
+                // |x|^2 from the staged query, eight dimensions at a time.  (Scores were made of it, so it is there; without targets it does not matter.)
                 double xx = 0.0;
-                for (int ch = 0; ch < 8 * nkc; ++ch) {
+                for (int ch = 0; ch < 8 * nkc && nt > 0; ++ch) {
                     const uint4 u = *reinterpret_cast<const uint4 *>(smem_dyn + (size_t)(ch / 8) * MT_CHUNK + q * 128 + (((ch & 7) ^ (q & 7)) << 4));
                     const uint32_t h[4] = {u.x, u.y, u.z, u.w};
                     float s = 0.f;
@@ -358,20 +424,33 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         }
     } else if (warp == MT_LOAD) {
         if (lane == 0) {
-            const unsigned char *ys = P.staged_y + ((size_t)w * lane_tiles + t0) * nby * MT_STAGE;
-            const int all_v = (P.dv + 127) / 128;
-            const unsigned char *vs = P.staged_v + (((size_t)w * lane_tiles + t0) * all_v + dv0 / 128) * MT_STAGE;
+            const long long y0 = ((long long)w * lane_tiles + t0) * nby, all_v = (P.dv + 127) / 128;
+            const long long v0 = ((long long)w * lane_tiles + t0) * all_v + dv0 / 128;     // blocks of 128 targets by 128 dimensions
             const float *term = P.terms + ((size_t)w * lane_tiles + t0) * 128;
             bool ok = *ab == 0;
             int i = 0;
-            auto stage = [&](const unsigned char *src) {
+            auto stage = [&](bool value, long long block) {
                 const int s = i % stages;
                 if (!(ok = mbar_wait(bar(EMPTY + s), ((uint32_t)(i / stages) & 1u) ^ 1u, ab))) return;
-                mbar_expect_tx(bar(FULL + s), MT_STAGE);
-                bulk_load(sR + s * MT_STAGE, src, MT_STAGE, bar(FULL + s));
+                const uint32_t dst = sR + s * STAGE;
+                if constexpr (!PAIR) {
+                    mbar_expect_tx(bar(FULL + s), STAGE);
+                    bulk_load(dst, (value ? P.staged_v : P.staged_y) + (size_t)block * MT_BLOCK, STAGE, bar(FULL + s));
+                } else {
+                    // scores: both halves of 64 dimensions of this block's 64 targets; images: all targets of its 64 dimensions
+                    if (rank == 0) mbar_expect_tx(bar(FULL + s), 2 * STAGE);
+                    const uint32_t full = in_block(bar(FULL + s), 0);
+                    const int row = (int)(block * 256) + (value ? 128 : 64) * (int)rank;
+                    load_rows(dst, value ? &tmv : &tmy, row, full);
+                    load_rows(dst + STAGE / 2, value ? &tmv : &tmy, row + (value ? 64 : 128), full);
+                }
                 ++i;
             };
             int terms_issued = 0;
+            if (tma_x && ok && nt > 0) {
+                if (rank == 0) mbar_expect_tx(bar(XFULL), (PAIR ? 2 : 1) * nkc * MT_CHUNK);
+                for (int c = 0; c < nkc; ++c) load_queries<PAIR>(sX + c * MT_CHUNK, &tmx, 64 * c, i0, w, PAIR ? in_block(bar(XFULL), 0) : bar(XFULL));
+            }
             // in the order of the matrix instructions: scores of tile t, then images of tile t - 1
             for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
                 if (t < nt) {
@@ -379,20 +458,26 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                     mbar_expect_tx(bar(TFULL + (t & 1)), 512);
                     bulk_load(smem_u32(terms) + 512 * (t & 1), term + (size_t)t * 128, 512, bar(TFULL + (t & 1)));
                     ++terms_issued;
-                    for (int b = 0; b < nby && ok; ++b) stage(ys + ((size_t)t * nby + b) * MT_STAGE);
+                    for (int b = 0; b < nby && ok; ++b) stage(false, y0 + (long long)t * nby + b);
                 }
                 if (t > 0)
-                    for (int b = 0; b < nbv && ok; ++b) stage(vs + ((size_t)(t - 1) * all_v + b) * MT_STAGE);
+                    for (int b = 0; b < nbv && ok; ++b) stage(true, v0 + (t - 1) * all_v + b);
             }
-            // nothing may land in shared memory after the block has gone: the last load of every buffer, with a bound of its own
+            // nothing may land in shared memory after the block has gone: the last load of every buffer, with a bound of its own.  (A pair's loads
+            // are counted at the first block, which waits for both.)
             int unused = 0;
-            for (int q = max(0, i - stages); q < i; ++q) mbar_wait(bar(FULL + q % stages), (uint32_t)(q / stages) & 1u, &unused);
+            if (tma_x && nt > 0 && rank == 0) mbar_wait(bar(XFULL), 0, &unused);
+            for (int q = max(0, i - stages); q < i && rank == 0; ++q) mbar_wait(bar(FULL + q % stages), (uint32_t)(q / stages) & 1u, &unused);
+            // (and no arrival of the other block's instructions)
+            for (int q = max(0, i - stages); q < i && PAIR; ++q) mbar_wait(bar(EMPTY + q % stages), (uint32_t)(q / stages) & 1u, &unused);
             for (int q = max(0, terms_issued - 2); q < terms_issued; ++q) mbar_wait(bar(TFULL + (q & 1)), (uint32_t)(q >> 1) & 1u, &unused);
         }
     } else {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             bool ok = *ab == 0;
             int i = 0;
+            if (tma_x && nt > 0 && ok) ok = mbar_wait(bar(XFULL), 0, ab);
+            tc_fence_after();
             for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
                 if (t < nt)
                     for (int b = 0; b < nby && ok; ++b, ++i) {
@@ -401,27 +486,27 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                         tc_fence_after();
                         const int steps = min(8, (P.d - 128 * b + 15) / 16);
                         for (int q = 0; q < steps; ++q)
-                            tc_mma(tmem + 128 * (t & 1), tc_desc(sX + (2 * b + (q >> 2)) * MT_CHUNK + (q & 3) * 32),
-                                   tc_desc(sR + s * MT_STAGE + (q >> 2) * MT_CHUNK + (q & 3) * 32), MT_IDESC, b | q ? 1u : 0u);
-                        tc_commit(bar(EMPTY + s));
-                        if (b == nby - 1) tc_commit(bar(SFULL + (t & 1)));
+                            mma_smem<PAIR>(tmem + 128 * (t & 1), tc_desc(sX + (2 * b + (q >> 2)) * MT_CHUNK + (q & 3) * 32),
+                                           tc_desc(sR + s * STAGE + (q >> 2) * (STAGE / 2) + (q & 3) * 32), b | q ? 1u : 0u);
+                        commit<PAIR>(bar(EMPTY + s));
+                        if (b == nby - 1) commit<PAIR>(bar(SFULL + (t & 1)));
                     }
                 if (t == 0 || !ok) continue;
                 const int u = t - 1;
-                if (!(ok = mbar_wait(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab))) break;
+                if (!(ok = wait_cluster(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab))) break;
                 tc_fence_after();
                 for (int b = 0; b < nbv && ok; ++b, ++i) {
                     const int s = i % stages;
                     if (!(ok = mbar_wait(bar(FULL + s), (uint32_t)(i / stages) & 1u, ab))) break;
                     tc_fence_after();
                     for (int q = 0; q < 8; ++q)
-                        mma_tmem(tO + 128 * b, tmem + 128 * (u & 1) + 8 * q, desc_columns(sR + s * MT_STAGE + q * 2048), MT_IDESC_V, u | q ? 1u : 0u);
-                    tc_commit(bar(EMPTY + s));
+                        mma_tmem<PAIR>(tO + 128 * b, tmem + 128 * (u & 1) + 8 * q, desc_columns(sR + s * STAGE + q * 2048), u | q ? 1u : 0u);
+                    commit<PAIR>(bar(EMPTY + s));
                 }
-                if (ok) tc_commit(bar(ODONE));
+                if (ok) commit<PAIR>(bar(ODONE));
             }
             // what was issued is over before tensor memory is given back
-            tc_commit(bar(LAST));
+            commit<PAIR>(bar(LAST), 1);
             int unused = 0;
             mbar_wait(bar(LAST), 0, &unused);
         }
@@ -429,17 +514,34 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (warp == MT_MMA) tc_dealloc<512>(tmem);
+    // (neither block of a pair goes while the other's instructions and loads may still use its memory)
+    if constexpr (PAIR) cluster_sync_all();
+    if (warp == MT_MMA) {
+        if constexpr (!PAIR) tc_dealloc<512>(tmem);
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
 }
 
-template <int DVC>
-skb_status launch(const Map &P, cudaStream_t st)
+template <int DVC, bool PAIR>
+skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, int tma_x, cudaStream_t st)
 {
-    const int nkc = (P.d + 63) / 64, nrt = (P.n + 127) / 128, nz = (P.dv + DVC - 1) / DVC;
-    const int room = MAP_TILES_SMEM - (int)MT_MISC - nkc * (int)MT_CHUNK, stages = min(MT_MAX_STAGES, room / (int)MT_STAGE);
-    const int smem = nkc * (int)MT_CHUNK + stages * (int)MT_STAGE + (int)MT_MISC;
-    cudaFuncSetAttribute(map_tiles_kernel<DVC>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    map_tiles_kernel<DVC><<<dim3(nrt * nz, P.splits, P.W), MT_THREADS, smem, st>>>(P, nrt, stages, (P.m + 127) / 128);
+    constexpr int stage = PAIR ? (int)MT_BLOCK / 2 : (int)MT_BLOCK;
+    const int nkc = (P.d + 63) / 64, blocks = (P.n + 127) / 128, nrt = PAIR ? (blocks + 1) / 2 * 2 : blocks, nz = (P.dv + DVC - 1) / DVC;
+    const int stages = min(MT_MAX_STAGES, (MAP_TILES_SMEM - (int)MT_MISC - nkc * (int)MT_CHUNK) / stage);
+    const int smem = nkc * (int)MT_CHUNK + stages * stage + (int)MT_MISC;
+    cudaFuncSetAttribute(map_tiles_kernel<DVC, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(nrt * nz, P.splits, P.W);
+    cfg.blockDim = dim3(MT_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = 2;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = PAIR ? 1 : 0;
+    cudaLaunchKernelEx(&cfg, map_tiles_kernel<DVC, PAIR>, tx, ty, tv, P, nrt, stages, (P.m + 127) / 128, tma_x);
     return op_launched("map");
 }
 
@@ -448,21 +550,29 @@ skb_status launch(const Map &P, cudaStream_t st)
 size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values)
 {
     const size_t tiles = (size_t)W * ((m + 127) / 128);
-    return tiles * 512 + tiles * MT_STAGE * ((d + 127) / 128 + (own_values ? (dv + 127) / 128 : 0));
+    return tiles * 512 + tiles * MT_BLOCK * ((d + 127) / 128 + (own_values ? (dv + 127) / 128 : 0));
 }
 
 skb_status launch_map_tiles(Map &P, void *room, cudaStream_t st)
 {
     const int tiles = (P.m + 127) / 128, nby = (P.d + 127) / 128, nbv = P.own_values ? (P.dv + 127) / 128 : 0;
     P.staged_y = (unsigned char *)room;
-    P.staged_v = P.own_values ? P.staged_y + (size_t)P.W * tiles * nby * MT_STAGE : P.staged_y;
-    P.terms = (float *)(P.staged_y + (size_t)P.W * tiles * (nby + nbv) * MT_STAGE);
+    P.staged_v = P.own_values ? P.staged_y + (size_t)P.W * tiles * nby * MT_BLOCK : P.staged_y;
+    P.terms = (float *)(P.staged_y + (size_t)P.W * tiles * (nby + nbv) * MT_BLOCK);
     const long long blocks = (long long)P.W * tiles * (nby + nbv) * 4;
     if (blocks > 0x7fffffffLL) return op_fail(SKB_ERR_SHAPE, "bank too large");
     map_stage_kernel<<<(unsigned)blocks, 256, 0, st>>>(P, tiles, nby, nbv);
     const skb_status rc = op_launched("map");
     if (rc != SKB_OK) return rc;
-    return P.dv <= 128 ? launch<128>(P, st) : launch<256>(P, st);
+    const bool pair = P.n > 128;
+    CUtensorMap tx = {}, ty = {}, tv = {};
+    const int tma_x = P.d % 8 == 0 && (uintptr_t)P.x % 16 == 0;
+    if ((tma_x && !queries_map(&tx, P.x, P.d, P.n, P.W)) ||
+        (pair && (!staged_map(&ty, P.staged_y, (size_t)P.W * tiles * nby * 256) ||
+                 !staged_map(&tv, P.staged_v, (size_t)P.W * tiles * (P.own_values ? nbv : nby) * 256))))
+        return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
+    if (pair) return P.dv <= 128 ? launch<128, true>(tx, ty, tv, P, tma_x, st) : launch<256, true>(tx, ty, tv, P, tma_x, st);
+    return P.dv <= 128 ? launch<128, false>(tx, ty, tv, P, tma_x, st) : launch<256, false>(tx, ty, tv, P, tma_x, st);
 }
 
 }  // namespace skb

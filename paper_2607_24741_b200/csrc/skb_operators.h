@@ -30,6 +30,10 @@ skb_status launch_dots(const DotsCloud &x, const DotsCloud &y, int dtype, int W,
                        int n_out = 0, int m_out = 0);
 // The tensor map of W lanes of npts points of row_bytes (a multiple of 16, 16-byte aligned): boxes of 128 bytes of box_points points, 128-byte swizzle.
 bool points_map(CUtensorMap *tm, const void *codes, int row_bytes, int npts, int W, int box_points);
+// ... and of rows of 128 bytes that lie as shared memory is to have them: boxes of 64 rows.
+bool staged_map(CUtensorMap *tm, const void *base, size_t rows);
+// ... and of bf16 points (d a multiple of 8, 16-byte aligned): boxes of 64 dimensions of 128 points, 128-byte swizzle.
+bool queries_map(CUtensorMap *tm, const void *x, int d, int n, int W);
 constexpr int MAP_MAX_SMS = 160;                                // multiprocessors that a map's workspace is sized for
 // sinkhorn_plan_draw; lanes whose `status` (null: none) is SKB_LANE_NONFINITE give no draws.
 skb_status plan_draw(const void *x, const void *y, const double *g, const float *eps, const float *u, const skb_draw_config *cfg,
