@@ -70,13 +70,12 @@ __device__ __forceinline__ void cluster_sync_all()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// an arrival once the matrix instructions so far are done; a pair's, at both blocks' barriers (or at the first `at` of them)
-template <bool PAIR> __device__ __forceinline__ void commit(uint32_t mbar, uint32_t at = 2)
+// an arrival once the matrix instructions so far are done; a pair's, at the barriers of the blocks in the mask
+template <bool PAIR> __device__ __forceinline__ void commit(uint32_t mbar, uint16_t mask = 3)
 {
     if constexpr (!PAIR) tc_commit(mbar);
     else
-        for (uint32_t r = 0; r < at; ++r)
-            asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(in_block(mbar, r)) : "memory");
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(mbar), "h"(mask) : "memory");
 }
 // 64 rows of 128 bytes; the barrier may be the other block's of a pair
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap *tm, int row, uint32_t mbar)
@@ -97,9 +96,23 @@ template <bool PAIR> __device__ __forceinline__ void load_queries(uint32_t dst, 
 // as mbar_wait, for what a pair's other block has done before it arrived
 __device__ __forceinline__ bool wait_cluster(uint32_t a, uint32_t parity, volatile int *abort_flag)
 {
-    if (!mbar_wait(a, parity, abort_flag)) return false;
-    asm volatile("fence.acq_rel.cluster;" ::: "memory");
-    return true;
+    long long since = 0;
+    for (;;) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(ok) : "r"(a), "r"(parity) : "memory");
+        if (ok) return true;
+        if (*abort_flag) return false;
+        if (since == 0) since = clock64();
+        else if (clock64() - since > TC_WAIT_CLOCKS) { *abort_flag = 1; return false; }
+    }
+}
+// one thread of a warp, the same one each time
+__device__ __forceinline__ bool elected()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 // rows of 64 columns (128 bytes), 8-row groups 1024 bytes apart, the next 64 columns a chunk further
 __device__ __forceinline__ uint64_t desc_columns(uint32_t saddr)
@@ -428,10 +441,11 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             const long long v0 = ((long long)w * lane_tiles + t0) * all_v + dv0 / 128;     // blocks of 128 targets by 128 dimensions
             const float *term = P.terms + ((size_t)w * lane_tiles + t0) * 128;
             bool ok = *ab == 0;
-            int i = 0;
+            // (a stage's number and its phase are counted, not divided out: a division is longer than a stage's instructions take to issue)
+            int i = 0, s = 0;
+            uint32_t ph = 0;
             auto stage = [&](bool value, long long block) {
-                const int s = i % stages;
-                if (!(ok = mbar_wait(bar(EMPTY + s), ((uint32_t)(i / stages) & 1u) ^ 1u, ab))) return;
+                if (!(ok = mbar_wait(bar(EMPTY + s), ph ^ 1u, ab))) return;
                 const uint32_t dst = sR + s * STAGE;
                 if constexpr (!PAIR) {
                     mbar_expect_tx(bar(FULL + s), STAGE);
@@ -445,6 +459,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                     load_rows(dst + STAGE / 2, value ? &tmv : &tmy, row + (value ? 64 : 128), full);
                 }
                 ++i;
+                if (++s == stages) { s = 0; ph ^= 1u; }
             };
             int terms_issued = 0;
             if (tma_x && ok && nt > 0) {
@@ -473,42 +488,62 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             for (int q = max(0, terms_issued - 2); q < terms_issued; ++q) mbar_wait(bar(TFULL + (q & 1)), (uint32_t)(q >> 1) & 1u, &unused);
         }
     } else {
-        if (lane == 0 && rank == 0) {
+        // (the whole warp walks through the stages, so that descriptors are uniform; one thread issues)
+        if (rank == 0) {
             bool ok = *ab == 0;
-            int i = 0;
-            if (tma_x && nt > 0 && ok) ok = mbar_wait(bar(XFULL), 0, ab);
+            int s = 0;
+            uint32_t ph = 0;
+            auto next = [&] { if (++s == stages) { s = 0; ph ^= 1u; } };
+            const uint64_t x0 = tc_desc(sX), r0 = tc_desc(sR), v0 = desc_columns(sR);     // (an address counts units of 16 bytes)
+            if (tma_x && nt > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(XFULL), 0, ab));
             tc_fence_after();
             for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
                 if (t < nt)
-                    for (int b = 0; b < nby && ok; ++b, ++i) {
-                        const int s = i % stages;
-                        if (!(ok = mbar_wait(bar(FULL + s), (uint32_t)(i / stages) & 1u, ab))) break;
+                    for (int b = 0; b < nby; ++b, next()) {
+                        if (!(ok = __all_sync(0xffffffffu, mbar_wait(bar(FULL + s), ph, ab)))) break;
                         tc_fence_after();
-                        const int steps = min(8, (P.d - 128 * b + 15) / 16);
-                        for (int q = 0; q < steps; ++q)
-                            mma_smem<PAIR>(tmem + 128 * (t & 1), tc_desc(sX + (2 * b + (q >> 2)) * MT_CHUNK + (q & 3) * 32),
-                                           tc_desc(sR + s * STAGE + (q >> 2) * (STAGE / 2) + (q & 3) * 32), b | q ? 1u : 0u);
-                        commit<PAIR>(bar(EMPTY + s));
-                        if (b == nby - 1) commit<PAIR>(bar(SFULL + (t & 1)));
+                        const uint64_t xd = x0 + (uint64_t)(b * 2 * (int)(MT_CHUNK >> 4)), yd = r0 + (uint64_t)(s * (int)(STAGE >> 4));
+                        const uint32_t acc = tmem + 128 * (t & 1);
+                        const int left = P.d - 128 * b;
+                        if (elected()) {
+                            mma_smem<PAIR>(acc, xd, yd, b ? 1u : 0u);
+                            if (left > 112) {
+#pragma unroll
+                                for (int q = 1; q < 8; ++q)
+                                    mma_smem<PAIR>(acc, xd + (q >> 2) * (MT_CHUNK >> 4) + (q & 3) * 2, yd + (q >> 2) * (STAGE >> 5) + (q & 3) * 2, 1u);
+                            } else
+                                for (int q = 1; 16 * q < left; ++q)
+                                    mma_smem<PAIR>(acc, xd + (q >> 2) * (MT_CHUNK >> 4) + (q & 3) * 2, yd + (q >> 2) * (STAGE >> 5) + (q & 3) * 2, 1u);
+                            commit<PAIR>(bar(EMPTY + s));
+                            if (b == nby - 1) commit<PAIR>(bar(SFULL + (t & 1)));
+                        }
+                        __syncwarp();
                     }
                 if (t == 0 || !ok) continue;
                 const int u = t - 1;
-                if (!(ok = wait_cluster(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab))) break;
+                if (!(ok = __all_sync(0xffffffffu, wait_cluster(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab)))) break;
                 tc_fence_after();
-                for (int b = 0; b < nbv && ok; ++b, ++i) {
-                    const int s = i % stages;
-                    if (!(ok = mbar_wait(bar(FULL + s), (uint32_t)(i / stages) & 1u, ab))) break;
+                for (int b = 0; b < nbv; ++b, next()) {
+                    if (!(ok = __all_sync(0xffffffffu, mbar_wait(bar(FULL + s), ph, ab)))) break;
                     tc_fence_after();
-                    for (int q = 0; q < 8; ++q)
-                        mma_tmem<PAIR>(tO + 128 * b, tmem + 128 * (u & 1) + 8 * q, desc_columns(sR + s * STAGE + q * 2048), u | q ? 1u : 0u);
-                    commit<PAIR>(bar(EMPTY + s));
+                    const uint64_t vd = v0 + (uint64_t)(s * (int)(STAGE >> 4));
+                    const uint32_t out = tO + 128 * b, weights = tmem + 128 * (u & 1);
+                    if (elected()) {
+                        mma_tmem<PAIR>(out, weights, vd, u ? 1u : 0u);
+#pragma unroll
+                        for (int q = 1; q < 8; ++q) mma_tmem<PAIR>(out, weights + 8 * q, vd + q * (2048 >> 4), 1u);
+                        commit<PAIR>(bar(EMPTY + s));
+                        if (b == nbv - 1) commit<PAIR>(bar(ODONE));
+                    }
+                    __syncwarp();
                 }
-                if (ok) commit<PAIR>(bar(ODONE));
             }
             // what was issued is over before tensor memory is given back
-            commit<PAIR>(bar(LAST), 1);
-            int unused = 0;
-            mbar_wait(bar(LAST), 0, &unused);
+            if (elected()) {
+                commit<PAIR>(bar(LAST), 1);
+                int unused = 0;
+                mbar_wait(bar(LAST), 0, &unused);
+            }
         }
     }
     __syncwarp();
