@@ -93,20 +93,6 @@ template <bool PAIR> __device__ __forceinline__ void load_queries(uint32_t dst, 
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(dim), "r"(query), "r"(lane), "r"(mbar) : "memory");
 }
-// as mbar_wait, for what a pair's other block has done before it arrived
-__device__ __forceinline__ bool wait_cluster(uint32_t a, uint32_t parity, volatile int *abort_flag)
-{
-    long long since = 0;
-    for (;;) {
-        uint32_t ok;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(ok) : "r"(a), "r"(parity) : "memory");
-        if (ok) return true;
-        if (*abort_flag) return false;
-        if (since == 0) since = clock64();
-        else if (clock64() - since > TC_WAIT_CLOCKS) { *abort_flag = 1; return false; }
-    }
-}
 // one thread of a warp, the same one each time
 __device__ __forceinline__ bool elected()
 {
@@ -363,8 +349,10 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
+                // (what the instructions read of this thread's is in tensor memory, ordered by the fence above; a release of all else to the cluster
+                // takes as long as half a tile)
                 if constexpr (PAIR)
-                    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(in_block(bar(PFULL + b), 0)) : "memory");
+                    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_block(bar(PFULL + b), 0)) : "memory");
                 else mbar_arrive(bar(PFULL + b));
             }
         }
@@ -521,7 +509,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                     }
                 if (t == 0 || !ok) continue;
                 const int u = t - 1;
-                if (!(ok = __all_sync(0xffffffffu, wait_cluster(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab)))) break;
+                if (!(ok = __all_sync(0xffffffffu, mbar_wait(bar(PFULL + (u & 1)), (uint32_t)(u >> 1) & 1u, ab)))) break;
                 tc_fence_after();
                 for (int b = 0; b < nbv; ++b, next()) {
                     if (!(ok = __all_sync(0xffffffffu, mbar_wait(bar(FULL + s), ph, ab)))) break;
