@@ -528,7 +528,7 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     CUtensorMap ty, tv;
     if (!plan.tiles && (!points_map(&ty, P.y.codes, P.y.cb, m, W, MR_T) || !points_map(&tv, P.v.codes, P.v.cb, m, W, MR_T)))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
+    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, sms, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
     if (rc != SKB_OK || P.splits == 1) return rc;
     map_join_kernel<<<W * n, 128, 0, (cudaStream_t)stream>>>(P);
     return op_launched("map");

@@ -29,7 +29,7 @@ struct Map {
 
 // Many queries (skb_map_tc.cu): d <= MAP_TILES_MAX_D, P.splits parts of a lane's bank, room for the bank in bf16 (256-byte aligned).
 size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values);
-skb_status launch_map_tiles(Map &P, void *room, cudaStream_t st);
+skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st);
 
 __device__ __forceinline__ int map_length(const Map &P, int w) { return P.lengths ? min(max(P.lengths[w], 0), P.m) : P.m; }
 // log2(e) / eps; NaN, and so are the lane's images, where eps is not a positive number

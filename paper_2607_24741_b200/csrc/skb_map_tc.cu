@@ -121,12 +121,12 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 // lowest of bf16's eight and the highest of its seven, subnormals among them.
 __device__ __forceinline__ uint32_t codes_bf16(uint32_t p) { return ((p >> 4) & 0x07f007f0u) | (p & 0x80008000u); }
 
-// whether all 64 threads of a barrier say so
-__device__ __forceinline__ bool both(bool ok, int barrier)
+// whether all COUNT threads of a barrier say so
+template <int COUNT> __device__ __forceinline__ bool all_of(bool ok, int barrier)
 {
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.and.pred q, %1, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"(barrier), "r"((uint32_t)ok) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %2, 0;\n\tbarrier.cta.red.and.pred q, %1, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"(barrier), "r"((uint32_t)ok), "n"(COUNT) : "memory");
     return r != 0;
 }
 
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ 
 template <int DVC, bool PAIR>
 __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmy,
                                                                   const __grid_constant__ CUtensorMap tmv, const __grid_constant__ Map P, const int nrt,
-                                                                  const int stages, const int lane_tiles, const int tma_x)
+                                                                  const int stages, const int lane_tiles, const int tma_x, const int wave)
 {
     constexpr uint32_t STAGE = PAIR ? MT_BLOCK / 2 : MT_BLOCK;
     extern __shared__ __align__(1024) unsigned char smem_dyn[];
@@ -266,6 +266,8 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         double sum = 0.0;
         bool ok = *ab == 0;
         const bool starts = ok;
+        const bool want_xx = P.lse && z == 0 && P.splits == 1;
+        double xx = 0.0;
         for (int t = 0; t < nt && starts; ++t) {
             const int b = t & 1;
             const uint32_t ph = (uint32_t)(t >> 1) & 1u;
@@ -296,7 +298,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             }
             tops[128 * half + q] = top;
             // both halves have read S (its place is P's next) and know the query's maximum, and whether either has given up
-            ok = both(ok, 1 + (warp & 3));
+            ok = all_of<64>(ok, 1 + (warp & 3));
             if (!ok) break;
             if (lane == 0) mbar_arrive(bar(TEMPTY + b));
             top = fmaxf(top, tops[128 * (1 - half) + q]);
@@ -355,6 +357,27 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                     asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_block(bar(PFULL + b), 0)) : "memory");
                 else mbar_arrive(bar(PFULL + b));
             }
+            if (t == 0 && want_xx) {
+                // |x|^2 of this half of the query's dimensions, while there is time: eight sums in fp32 of a value of every eight, added up in double every 64.
+                // (The queries are there: scores were made of them.)
+                for (int c = half; c < nkc; c += 2) {
+                    float part[8];
+    #pragma unroll
+                    for (int e = 0; e < 8; ++e) part[e] = 0.f;
+    #pragma unroll
+                    for (int ch = 0; ch < 8; ++ch) {
+                        const uint4 u = *reinterpret_cast<const uint4 *>(smem_dyn + (size_t)c * MT_CHUNK + q * 128 + ((ch ^ (q & 7)) << 4));
+                        const uint32_t h[4] = {u.x, u.y, u.z, u.w};
+    #pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float lo = __uint_as_float(h[e] << 16), hi = __uint_as_float(h[e] & 0xffff0000u);
+                            part[2 * e] = fmaf(lo, lo, part[2 * e]);
+                            part[2 * e + 1] = fmaf(hi, hi, part[2 * e + 1]);
+                        }
+                    }
+                    xx += (double)(((part[0] + part[1]) + (part[2] + part[3])) + ((part[4] + part[5]) + (part[6] + part[7])));
+                }
+            }
         }
         if (ok && nt > 0) {
             // (one phase after the other: the wait for a phase is over as well while the one before it has yet to end)
@@ -372,6 +395,9 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         const bool live = i0 + q < P.n;
         const size_t row = (size_t)w * P.n + i0 + (live ? q : 0);
         const float inv = P.splits > 1 ? (total == total ? 1.f : nan) : total == 0.f ? 0.f : 1.f / total;
+        // images by way of shared memory, which queries and stages need no more, so that rows are written whole
+        const bool whole = all_of<32 * MT_SOFT>(ok, 5) && P.splits == 1 && P.dv % 8 == 0 && (uintptr_t)P.out % 16 == 0;
+        constexpr int ROW = 2 * DVC;                                       // bytes
         for (int c = 0; c < DVC / 2; c += 32) {
             const int dim = dv0 + half * (DVC / 2) + c;
             if (dim >= P.dv) break;
@@ -382,45 +408,43 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             } else
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = 0u;
-            if (!live) continue;
             if (P.splits > 1) {
                 float *dst = P.part_out + (row * P.splits + split) * P.dv + dim;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
-                    if (dim + i < P.dv) dst[i] = __uint_as_float(o[i]) * inv;
+                    if (live && dim + i < P.dv) dst[i] = __uint_as_float(o[i]) * inv;
                 continue;
             }
-            uint16_t *dst = P.out + row * P.dv + dim;
-            const bool wide = P.dv % 8 == 0 && (uintptr_t)P.out % 16 == 0;
 #pragma unroll
             for (int i = 0; i < 32; i += 8) {
                 uint32_t h[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) h[e] = bf16_pair(__uint_as_float(o[i + 2 * e]) * inv, __uint_as_float(o[i + 2 * e + 1]) * inv);
-                if (wide && dim + i < P.dv) *reinterpret_cast<uint4 *>(dst + i) = make_uint4(h[0], h[1], h[2], h[3]);
-                else
+                if (whole) {
+                    const int ch = (half * (DVC / 2) + c + i) / 8;
+                    *reinterpret_cast<uint4 *>(smem_dyn + q * ROW + ((ch ^ (q & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                } else if (live)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
-                        if (dim + i + e < P.dv) dst[i + e] = (uint16_t)(h[e / 2] >> (16 * (e & 1)));
+                        if (dim + i + e < P.dv) P.out[row * P.dv + dim + i + e] = (uint16_t)(h[e / 2] >> (16 * (e & 1)));
             }
         }
-        if (live && half == 0 && z == 0) {
-            if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[row * P.splits + split] = make_float2(ref, total);
-            else if (P.lse) {
-                // |x|^2 from the staged query, eight dimensions at a time.  (Scores were made of it, so it is there; without targets it does not matter.)
-                double xx = 0.0;
-                for (int ch = 0; ch < 8 * nkc && nt > 0; ++ch) {
-                    const uint4 u = *reinterpret_cast<const uint4 *>(smem_dyn + (size_t)(ch / 8) * MT_CHUNK + q * 128 + (((ch & 7) ^ (q & 7)) << 4));
-                    const uint32_t h[4] = {u.x, u.y, u.z, u.w};
-                    float s = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float lo = __uint_as_float(h[e] << 16), hi = __uint_as_float(h[e] & 0xffff0000u);
-                        s = fmaf(lo, lo, fmaf(hi, hi, s));
-                    }
-                    xx += (double)s;
-                }
-                P.lse[row] = map_lse(ref, total, k, xx);
+        if (P.splits == 1 && P.lse && z == 0) {
+            // (the sums have been read: the barrier of all eight warps came after)
+            double *halves = reinterpret_cast<double *>(terms);
+            if (half) halves[q] = xx;
+            asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
+            if (live && half == 0) P.lse[row] = map_lse(ref, total, k, xx + halves[q]);
+        }
+        if (P.splits > 1 && live && half == 0 && z == 0) reinterpret_cast<float2 *>(P.part_ml)[row * P.splits + split] = make_float2(ref, total);
+        if (whole) {
+            asm volatile("bar.sync 5, %0;" ::"n"(32 * MT_SOFT) : "memory");
+            constexpr int PER = ROW / 16;                                  // 16-byte pieces of a row
+            for (int i = tid; i < 128 * PER; i += 32 * MT_SOFT) {
+                const int r = i / PER, ch = i % PER, dim = dv0 + 8 * ch;
+                if (i0 + r < P.n && dim < P.dv)
+                    *reinterpret_cast<uint4 *>(P.out + ((size_t)w * P.n + i0 + r) * P.dv + dim) =
+                        *reinterpret_cast<const uint4 *>(smem_dyn + r * ROW + ((ch ^ (r & 7)) << 4));
             }
         }
     } else if (warp == MT_LOAD) {
@@ -453,6 +477,16 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             if (tma_x && ok && nt > 0) {
                 if (rank == 0) mbar_expect_tx(bar(XFULL), (PAIR ? 2 : 1) * nkc * MT_CHUNK);
                 for (int c = 0; c < nkc; ++c) load_queries<PAIR>(sX + c * MT_CHUNK, &tmx, 64 * c, i0, w, PAIR ? in_block(bar(XFULL), 0) : bar(XFULL));
+            }
+            // the queries of the block that follows on this SM, about, into L2
+            if (tma_x) {
+                const long long later = (long long)blockIdx.x + (long long)gridDim.x * ((long long)blockIdx.y + (long long)gridDim.y * blockIdx.z) + wave;
+                const long long lw = later / ((long long)gridDim.x * gridDim.y);
+                const int lrt = (int)(later % gridDim.x) % nrt;
+                if (lw < P.W)
+                    for (int c = 0; c < nkc; ++c)
+                        asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
+                                     ::"l"(reinterpret_cast<uint64_t>(&tmx)), "r"(64 * c), "r"(lrt * 128), "r"((int)lw) : "memory");
             }
             // in the order of the matrix instructions: scores of tile t, then images of tile t - 1
             for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
@@ -546,7 +580,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
 }
 
 template <int DVC, bool PAIR>
-skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, int tma_x, cudaStream_t st)
+skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, int tma_x, int sms, cudaStream_t st)
 {
     constexpr int stage = PAIR ? (int)MT_BLOCK / 2 : (int)MT_BLOCK;
     const int nkc = (P.d + 63) / 64, blocks = (P.n + 127) / 128, nrt = PAIR ? (blocks + 1) / 2 * 2 : blocks, nz = (P.dv + DVC - 1) / DVC;
@@ -564,7 +598,7 @@ skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMa
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = PAIR ? 1 : 0;
-    cudaLaunchKernelEx(&cfg, map_tiles_kernel<DVC, PAIR>, tx, ty, tv, P, nrt, stages, (P.m + 127) / 128, tma_x);
+    cudaLaunchKernelEx(&cfg, map_tiles_kernel<DVC, PAIR>, tx, ty, tv, P, nrt, stages, (P.m + 127) / 128, tma_x, sms);
     return op_launched("map");
 }
 
@@ -576,7 +610,7 @@ size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values)
     return tiles * 512 + tiles * MT_BLOCK * ((d + 127) / 128 + (own_values ? (dv + 127) / 128 : 0));
 }
 
-skb_status launch_map_tiles(Map &P, void *room, cudaStream_t st)
+skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st)
 {
     const int tiles = (P.m + 127) / 128, nby = (P.d + 127) / 128, nbv = P.own_values ? (P.dv + 127) / 128 : 0;
     P.staged_y = (unsigned char *)room;
@@ -594,8 +628,8 @@ skb_status launch_map_tiles(Map &P, void *room, cudaStream_t st)
         (pair && (!staged_map(&ty, P.staged_y, (size_t)P.W * tiles * nby * 256) ||
                  !staged_map(&tv, P.staged_v, (size_t)P.W * tiles * (P.own_values ? nbv : nby) * 256))))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    if (pair) return P.dv <= 128 ? launch<128, true>(tx, ty, tv, P, tma_x, st) : launch<256, true>(tx, ty, tv, P, tma_x, st);
-    return P.dv <= 128 ? launch<128, false>(tx, ty, tv, P, tma_x, st) : launch<256, false>(tx, ty, tv, P, tma_x, st);
+    if (pair) return P.dv <= 128 ? launch<128, true>(tx, ty, tv, P, tma_x, sms, st) : launch<256, true>(tx, ty, tv, P, tma_x, sms, st);
+    return P.dv <= 128 ? launch<128, false>(tx, ty, tv, P, tma_x, sms, st) : launch<256, false>(tx, ty, tv, P, tma_x, sms, st);
 }
 
 }  // namespace skb
