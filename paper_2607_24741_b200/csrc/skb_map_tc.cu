@@ -136,31 +136,28 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(mbar) : "memory");
 }
 
-// The bank as bf16.  A thread takes 16 codes of a target; eight to a target's block of 128 dimensions.
-__global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ Map P, const int tiles, const int nby, const int nbv)
+// The bank as bf16.  A thread takes 16 codes of a target, eight to its block of 128 dimensions; 32 targets to a block of threads.
+__global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ Map P, const int nby, const int nbv)
 {
-    const int nb = nby + nbv, c16 = threadIdx.x & 7;
-    const long long item = (long long)blockIdx.x * 32 + (threadIdx.x >> 3);     // (lane, tile, block, target)
-    const int r = (int)(item & 127), b0 = (int)((item >> 7) % nb), t = (int)((item >> 7) / nb % tiles);
-    const long long w = (item >> 7) / nb / tiles;
-    if (w >= P.W) return;
-    const int len = map_length(P, (int)w), j = t * 128 + r;
+    const int c16 = threadIdx.x & 7, r = (int)(blockIdx.x & 3) * 32 + (threadIdx.x >> 3), b0 = blockIdx.x >> 2, t = blockIdx.y, w = blockIdx.z;
+    const int tiles = gridDim.y, len = map_length(P, w), j = t * 128 + r;
     if (t * 128 >= len) return;                                                // (a tile that no one reads)
     const bool value = b0 >= nby;
     const int b = value ? b0 - nby : b0;
     const Cloud8 &cl = value ? P.v : P.y;
-    float term = -INFINITY;
+    bool masked = true;
     uint4 codes = make_uint4(0u, 0u, 0u, 0u);
     uint32_t e = 0;
     if (j < len) {
         const size_t at = (size_t)w * P.m + j;
         e = cl.scales[at * cl.sb + b];
         if (b * 128 + c16 * 16 < cl.cb) codes = *reinterpret_cast<const uint4 *>(cl.codes + at * cl.cb + b * 128 + c16 * 16);
-        term = map_term(map_scale(P, (int)w), P.g ? P.g[at] : 0.0, P.y.norms[at]);
-    }
-    if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = term;
+        const double g = P.g ? P.g[at] : 0.0;
+        const float norm = P.y.norms[at];
+        masked = g == -INFINITY || norm == INFINITY;
+        if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = masked ? -INFINITY : map_term(map_scale(P, w), g, norm);
+    } else if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = -INFINITY;
     // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
-    const bool masked = term == -INFINITY;
     const uint32_t e1 = min(e, 134u);
     uint32_t f = masked ? 0u : e == 255u ? 0x7fffu : (e1 + 120u) << 7;
     f |= f << 16;
@@ -616,9 +613,7 @@ skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st)
     P.staged_y = (unsigned char *)room;
     P.staged_v = P.own_values ? P.staged_y + (size_t)P.W * tiles * nby * MT_BLOCK : P.staged_y;
     P.terms = (float *)(P.staged_y + (size_t)P.W * tiles * (nby + nbv) * MT_BLOCK);
-    const long long blocks = (long long)P.W * tiles * (nby + nbv) * 4;
-    if (blocks > 0x7fffffffLL) return op_fail(SKB_ERR_SHAPE, "bank too large");
-    map_stage_kernel<<<(unsigned)blocks, 256, 0, st>>>(P, tiles, nby, nbv);
+    map_stage_kernel<<<dim3(4 * (nby + nbv), tiles, P.W), 256, 0, st>>>(P, nby, nbv);
     const skb_status rc = op_launched("map");
     if (rc != SKB_OK) return rc;
     const bool pair = P.n > 128;
