@@ -74,9 +74,12 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return r;
 }
 
+// blocks that an SM is to hold: their waits, for barriers as for memory, are each other's time
+template <int NG, int UNITS> constexpr int MR_BLOCKS = NG * UNITS <= 4 ? 4 : NG * UNITS <= 8 ? 3 : 2;
+
 // NG groups of eight queries; UNITS blocks of 128 dimensions of values
 template <int NG, int UNITS>
-__global__ void __launch_bounds__(MR_THREADS) map_rows_kernel(const __grid_constant__ CUtensorMap tmy, const __grid_constant__ CUtensorMap tmv,
+__global__ void __launch_bounds__(MR_THREADS, MR_BLOCKS<NG, UNITS>) map_rows_kernel(const __grid_constant__ CUtensorMap tmy, const __grid_constant__ CUtensorMap tmv,
                                                               const __grid_constant__ Map P, const int slots)
 {
     constexpr int Q = 8 * NG;
@@ -106,15 +109,16 @@ __global__ void __launch_bounds__(MR_THREADS) map_rows_kernel(const __grid_const
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    // slots are filled in the order of tiles and their blocks: the bank's, then those of values of their own
-    const long long total = (long long)(t1 - t0) * per_tile;
-    long long issued = 0;                                                     // (thread 0)
-    auto issue = [&](long long until) {
-        for (; issued < until && issued < total; ++issued) {
-            const int s = (int)(issued % slots), b = (int)(issued % per_tile), t = t0 + (int)(issued / per_tile);
-            mbar_expect_tx(bar(s), MR_SLOT);
-            if (b < nby) tma_points(base + s * MR_SLOT, &tmy, b * 128, t * MR_T, w, bar(s));
-            else tma_points(base + s * MR_SLOT, &tmv, (b - nby) * 128, t * MR_T, w, bar(s));
+    // slots are filled in the order of tiles and their blocks: the bank's, then those of values of their own.  (Slots, tiles and phases are counted
+    // on: divisions would be half of the instructions.)
+    int in_tile = t0, in_block = 0, in_slot = 0;                              // (thread 0) what comes into a slot next
+    auto issue = [&](int count) {
+        for (; count > 0 && in_tile < t1; --count) {
+            mbar_expect_tx(bar(in_slot), MR_SLOT);
+            if (in_block < nby) tma_points(base + in_slot * MR_SLOT, &tmy, in_block * 128, in_tile * MR_T, w, bar(in_slot));
+            else tma_points(base + in_slot * MR_SLOT, &tmv, (in_block - nby) * 128, in_tile * MR_T, w, bar(in_slot));
+            if (++in_block == per_tile) { in_block = 0; ++in_tile; }
+            if (++in_slot == slots) in_slot = 0;
         }
     };
     if (tid == 0) issue(slots);
@@ -199,15 +203,17 @@ __global__ void __launch_bounds__(MR_THREADS) map_rows_kernel(const __grid_const
     if (t0 < t1) { na = fetch(t0, pa); nb = fetch(t0, pb); }
     __syncthreads();
 
-    long long at = 0;                                                         // slots used up so far
+    int slot0 = 0;                                                            // of a tile's first block, and the phase it is filled in
+    uint32_t phase = 0;
     bool ok = true;
-    for (int t = t0; t < t1; ++t, at += per_tile) {
+    for (int t = t0; t < t1; ++t) {
         const Point A = na, Bp = nb;
         if (t + 1 < t1) { na = fetch(t + 1, pa); nb = fetch(t + 1, pb); }
+        auto slot_of = [&](int b) { return slot0 + b < slots ? slot0 + b : slot0 + b - slots; };
         auto wait = [&](int b) {
-            const long long i = at + b;
-            ok = mbar_wait(bar((int)(i % slots)), (uint32_t)(i / slots) & 1u, &abort_flag) && ok;
-            return gen + (size_t)(i % slots) * MR_SLOT;
+            const int i = slot_of(b);
+            ok = mbar_wait(bar(i), phase ^ (slot0 + b < slots ? 0u : 1u), &abort_flag) && ok;
+            return gen + i * MR_SLOT;
         };
         // ---- scores
         float s[NG][4];
@@ -310,7 +316,7 @@ __global__ void __launch_bounds__(MR_THREADS) map_rows_kernel(const __grid_const
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
             if (128 * u + 32 * warp >= P.dv) break;
-            const unsigned char *slot = nbv ? wait(nby + u) : gen + (size_t)((at + u) % slots) * MR_SLOT;
+            const unsigned char *slot = nbv ? wait(nby + u) : gen + slot_of(u) * MR_SLOT;
             float acc[NG][2][4];
 #pragma unroll
             for (int a = 0; a < NG; ++a)
@@ -342,12 +348,18 @@ __global__ void __launch_bounds__(MR_THREADS) map_rows_kernel(const __grid_const
         }
         ok = __syncthreads_and(ok);
         if (!ok) break;
-        if (tid == 0) issue(at + per_tile + slots);
+        if (tid == 0) issue(per_tile);
+        slot0 += per_tile;
+        if (slot0 >= slots) { slot0 -= slots; phase ^= 1u; }
     }
-    // nothing may land in shared memory after the block has gone (a wait that ran out: the loads that are still on their way)
+    // nothing may land in shared memory after the block has gone: where a wait ran out, every load that may still be on its way
     if (!ok && tid == 0) {
-        int unused = 0;
-        for (long long i = issued > slots ? issued - slots : 0; i < issued; ++i) mbar_wait(bar((int)(i % slots)), (uint32_t)(i / slots) & 1u, &unused);
+        int unused = 0, s = slot0;
+        uint32_t ph = phase;
+        for (int i = 0; i < slots && (s != in_slot || i == 0); ++i) {
+            mbar_wait(bar(s), ph, &unused);
+            if (++s == slots) { s = 0; ph ^= 1u; }
+        }
     }
     // ---- the sums, over points
 #pragma unroll
@@ -396,36 +408,60 @@ __global__ void __launch_bounds__(MR_THREADS) map_rows_kernel(const __grid_const
         }
 }
 
-// The parts of a query's image, in their order; a warp to 32 dimensions of a query.
-__global__ void __launch_bounds__(128) map_join_kernel(const __grid_constant__ Map P)
+// The parts of a query's image, added up: a block to 128 dimensions of a query, a warp to every eighth part, in an order that does not change.
+__global__ void __launch_bounds__(256) map_join_kernel(const __grid_constant__ Map P)
 {
-    const int lane = threadIdx.x & 31;
+    __shared__ float s_out[8][128], s_sum[8];
+    __shared__ double s_xx[8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, dim0 = blockIdx.y * 128;
     const long long r = blockIdx.x;
+    const bool sums = P.lse && dim0 == 0;
+    double xx = 0.0;
+    if (sums)                                                                // (the query does not wait for the parts)
+        for (int i = threadIdx.x; i < P.d; i += 256) {
+            const double v = __uint_as_float((uint32_t)P.x[r * P.d + i] << 16);
+            xx += v * v;
+        }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const float2 *ml = reinterpret_cast<const float2 *>(P.part_ml) + r * P.splits;
     float top = -INFINITY;
     for (int s = lane; s < P.splits; s += 32) top = fmaxf(top, ml[s].x);
 #pragma unroll
     for (int off = 16; off; off /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
-    for (int s = 0; s < P.splits; ++s) sum = fmaf(ml[s].y, ex2f(ml[s].x - ref), sum);
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    for (int dim = threadIdx.x; dim < P.dv; dim += 128) {
-        const float *src = P.part_out + r * P.splits * P.dv + dim;
-        float v = 0.f;
-        for (int s = 0; s < P.splits; ++s) v = fmaf(src[(size_t)s * P.dv], ex2f(ml[s].x - ref), v);
-        P.out[r * P.dv + dim] = (uint16_t)bf16_pair(v * inv, 0.f);
-    }
-    if (P.lse && threadIdx.x < 32) {
-        const int w = (int)(r / P.n);
-        double xx = 0.0;
-        for (int i = lane; i < P.d; i += 32) {
-            const double v = __uint_as_float((uint32_t)P.x[r * P.d + i] << 16);
-            xx += v * v;
-        }
+    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = warp; s < P.splits; s += 8) {
+        const float2 one = ml[s];
+        const float f = ex2f(one.x - ref);
+        const float *src = P.part_out + (r * P.splits + s) * P.dv + dim0 + lane;
+        sum = fmaf(one.y, f, sum);
 #pragma unroll
-        for (int off = 16; off; off /= 2) xx += __shfl_xor_sync(0xffffffffu, xx, off);
-        if (lane == 0) P.lse[r] = map_lse(top, sum, map_scale(P, w), xx);
+        for (int e = 0; e < 4; ++e)
+            if (dim0 + lane + 32 * e < P.dv) v[e] = fmaf(src[32 * e], f, v[e]);
+    }
+#pragma unroll
+    for (int off = 16; off; off /= 2) xx += __shfl_xor_sync(0xffffffffu, xx, off);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s_out[warp][lane + 32 * e] = v[e];
+    if (lane == 0) { s_sum[warp] = sum; s_xx[warp] = xx; }
+    __syncthreads();
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += s_sum[i];
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const int dim = dim0 + threadIdx.x;
+    if (threadIdx.x < 128 && dim < P.dv) {
+        float o = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o += s_out[i][threadIdx.x];
+        P.out[r * P.dv + dim] = (uint16_t)bf16_pair(o * inv, 0.f);
+    }
+    if (sums && threadIdx.x == 0) {
+        xx = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) xx += s_xx[i];
+        P.lse[r] = map_lse(top, sum, map_scale(P, (int)(r / P.n)), xx);
     }
 }
 
@@ -433,9 +469,12 @@ template <int NG, int UNITS>
 skb_status launch_rows(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, cudaStream_t st)
 {
     const int nby = (P.d + 127) / 128, per_tile = nby + (P.own_values ? (P.dv + 127) / 128 : 0);
-    // two tiles at least, and about 80 KB, so that two blocks share an SM
-    const int slots = min(MR_MAX_SLOTS, max(2 * per_tile, 10));
-    const int smem = slots * (int)MR_SLOT + NG * 8 * nby * 256 + 1024;
+    // as many slots as leave room for the blocks that registers allow, a tile at least
+    cudaFuncAttributes fa;
+    if (cudaFuncGetAttributes(&fa, map_rows_kernel<NG, UNITS>) != cudaSuccess) return op_launched("map");
+    const int rest = NG * 8 * nby * 256 + 1024, room = MAP_SM_SMEM / MR_BLOCKS<NG, UNITS> - 1024 - (int)fa.sharedSizeBytes - rest;
+    const int slots = min(MR_MAX_SLOTS, max(per_tile, room / (int)MR_SLOT));
+    const int smem = slots * (int)MR_SLOT + rest;
     cudaFuncSetAttribute(map_rows_kernel<NG, UNITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     map_rows_kernel<NG, UNITS><<<dim3(P.splits, (P.n + 8 * NG - 1) / (8 * NG), P.W), MR_THREADS, smem, st>>>(ty, tv, P, slots);
     return op_launched("map");
@@ -464,13 +503,18 @@ struct MapPlan {
     bool tiles;
     int splits;
 };
+int rows_blocks(int n, int dv)
+{
+    const int units = dv <= 128 ? 1 : dv <= 256 ? 2 : dv <= 512 ? 4 : 8, work = (n <= 8 ? 1 : 2) * units;
+    return work <= 4 ? 4 : work <= 8 ? 3 : 2;                     // MR_BLOCKS
+}
 MapPlan map_plan(int W, int n, int m, int d, int dv, int sms)
 {
     MapPlan p;
     p.tiles = n > MAP_ROWS_MAX && d <= MAP_TILES_MAX_D;
-    const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * ((n + 7) / 8);
+    const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * (n <= 8 ? 1 : (n + 15) / 16);
     const long long tiles = p.tiles ? (m + 127) / 128 : (m + MR_T - 1) / MR_T;
-    long long s = p.tiles ? sms / blocks : (2LL * sms + blocks - 1) / blocks;
+    long long s = p.tiles ? sms / blocks : (long long)rows_blocks(n, dv) * sms / blocks;
     if (s > tiles / 2) s = tiles / 2;
     p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
     return p;
@@ -530,6 +574,16 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
     const skb_status rc = plan.tiles ? launch_map_tiles(P, room, sms, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
     if (rc != SKB_OK || P.splits == 1) return rc;
-    map_join_kernel<<<W * n, 128, 0, (cudaStream_t)stream>>>(P);
+    // (it may start, and wait, before the parts are all there)
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(W * n, (depth + 127) / 128);
+    cfg.blockDim = dim3(256);
+    cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    cudaLaunchKernelEx(&cfg, map_join_kernel, P);
     return op_launched("map");
 }
