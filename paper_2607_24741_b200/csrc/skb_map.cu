@@ -2,20 +2,25 @@
 //      out_i = sum_j w_ij v_j,   w_i = softmax over j of (g_j - |x_i - y_j|^2) / eps,
 // in one pass over the bank: exponents as k (2 x.y + g_j - |y_j|^2), k = log2(e) / eps, against a running maximum (|x_i|^2 is the same for all j).
 //
-// map_rows_kernel, here: few queries, the serving form.  Eight or sixteen queries and a part of a lane's bank to a block of four warps, two
-// to three blocks an SM.  Bounded by memory: every code is read once (by one block of queries), n <= 16 makes at most 64 flop of a byte.
-//   load     64 points at a time, 128 dimensions of them a slot of 8 KB, by TMA (128-byte swizzle, points past the end are zeros) into a ring
-//            of slots that holds two to eight tiles
-//   scores   a warp takes 16 points: codes to f16 in registers (exact), mma.sync with the queries' f16 (a power of two for each query: its
-//            largest value is 2^14, so nothing of bf16's eight bits is lost above 2^-38 of it), 128 dimensions at a time, whose sums are multiplied
-//            by the block's power of two in fp32
-//   softmax  all threads: exponentials in fp32 against the running maximum of the query, sums in fp32
-//   images   weights times the values' powers of two, less the tile's largest, in f16 (11 bits; what is below 2^-25 of the largest value of
-//            a tile's 64 points is lost), a warp takes 32 dimensions of every 128: bytes of two points side by side by prmt, to f16, mma.sync; sums of a
-//            tile are added in fp32
-// Several blocks that share a lane's bank leave (maximum, sum, image), which map_join_kernel adds up in the order of the parts.
-// The matrix instructions are mma.sync, whose operands come from registers: eight queries are an eighth of a tcgen05 tile, and codes
-// would have to go back to shared memory as f16 first.
+// map_rows_kernel, here: few queries, the serving form.  Eight or sixteen queries and a part of a lane's bank to a block.  Bounded by memory: every code is
+// read once (by one block of queries), and the tensor cores take the codes as they are:
+//   scores   S^T = Y . X^T, 128 targets of a tile by the queries: kind::mxf8f6f4 on the codes with the blocks' powers of two as scales.  A query is a sum
+//            of three e4m3 numbers a value, each a sixteenth of the one before it, with a power of two for each 128 dimensions: rounded to four bits, what is
+//            left of bf16's eight, and what is left of that for values below 2^-14 of the block's largest; what remains is below 2^-26 of that.  The three are
+//            rows of their own, added in fp32
+//   softmax  a thread to a target: exponentials in fp32 against the tile's maximum of the query, which carries over to a running one in fp32
+//   images   O^T = V^T . P^T, 128 dimensions by the queries: kind::f8f6f4 on the codes, in the same place of shared memory, now the operand whose rows lie
+//            next to each other (M-major).  Weights times the values' powers of two, less the tile's largest, are two e4m3 numbers (eight bits; what is below
+//            2^-22 of the tile's largest is lost), rows of their own again
+// so that nothing of a code passes through a register.  The same work by mma.sync, codes made f16 in registers, was bound by its instructions: one query
+// to each of 8 banks of 16384 x 512 took 35 us.
+//   warps 0-3   softmax
+//   warps 4-7   images: tensor memory -> fp32 sums in registers, a thread to a dimension of every 128
+//   warp 8      loads by TMA: slots of 128 targets by 128 dimensions (16 KB, 128-byte swizzle, targets past the end are zeros)
+//   warp 9      scores' matrix instructions, warp 11 the images': either waits for what it needs
+//   warp 10     targets' scales and terms, a tile ahead
+// Several blocks that share a lane's bank leave (maximum, sum, image), which map_join_kernel adds up.  Every wait is bounded (skb_tmem.cuh): one that
+// runs out ends all roles, and the block's images are NaN.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <string>
@@ -28,9 +33,12 @@
 namespace skb {
 namespace {
 
-constexpr int MR_THREADS = 128, MR_T = 64;                    // points of a tile
+constexpr int MR_THREADS = 12 * 32, MR_T = 128;               // points of a tile
 constexpr uint32_t MR_SLOT = MR_T * 128;
-constexpr int MR_MAX_SLOTS = 20, MR_PSTRIDE = 72;             // f16 from query to query: rows end up four banks apart
+constexpr int MR_MAX_SLOTS = 16, MR_MAX_BLOCKS = 8, MR_AHEAD = 4;     // MR_AHEAD: tiles whose scales and terms are there at once
+// rows of the queries' operand: three numbers of each query, and how many rows the instruction takes
+template <int NQ> constexpr int MR_ROWS = NQ == 8 ? 32 : 48;
+template <int NQ> constexpr int MR_SCOLS = NQ == 8 ? 32 : 64;  // columns of tensor memory that its result takes
 
 __device__ __forceinline__ float ex2f(float v)
 {
@@ -38,34 +46,11 @@ __device__ __forceinline__ float ex2f(float v)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// codes of the low or high half of a word as f16
-__device__ __forceinline__ uint32_t half_lo(uint32_t w)
+__device__ __forceinline__ uint32_t e4m3_two(float lo, float hi)
 {
     uint32_t r;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
+    asm("{\n\t.reg .b16 p;\n\tcvt.rn.satfinite.e4m3x2.f32 p, %2, %1;\n\tcvt.u32.u16 %0, p;\n\t}" : "=r"(r) : "f"(lo), "f"(hi));
     return r;
-}
-__device__ __forceinline__ uint32_t half_hi(uint32_t w)
-{
-    uint32_t r;
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
-    return r;
-}
-__device__ __forceinline__ uint16_t f16_bits(float v)
-{
-    uint16_t r;
-    asm("cvt.rn.f16.f32 %0, %1;" : "=h"(r) : "f"(v));
-    return r;
-}
-__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
-{
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ void tma_points(uint32_t dst, const CUtensorMap *tm, int byte, int point, int lane, uint32_t mbar)
-{
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(byte), "r"(point), "r"(lane), "r"(mbar) : "memory");
 }
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
 {
@@ -73,339 +58,587 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-
-// blocks that an SM is to hold: their waits, for barriers as for memory, are each other's time
-template <int NG, int UNITS> constexpr int MR_BLOCKS = NG * UNITS <= 4 ? 4 : NG * UNITS <= 8 ? 3 : 2;
-
-// NG groups of eight queries; UNITS blocks of 128 dimensions of values
-template <int NG, int UNITS>
-__global__ void __launch_bounds__(MR_THREADS, MR_BLOCKS<NG, UNITS>) map_rows_kernel(const __grid_constant__ CUtensorMap tmy, const __grid_constant__ CUtensorMap tmv,
-                                                              const __grid_constant__ Map P, const int slots)
+__device__ __forceinline__ float warp_max(float v)
 {
-    constexpr int Q = 8 * NG;
-    extern __shared__ __align__(1024) unsigned char smem_dyn[];
-    __shared__ __align__(8) unsigned long long bars[MR_MAX_SLOTS];
-    __shared__ __align__(16) float s_arg[Q][MR_T];
-    __shared__ __align__(16) uint16_t s_p[UNITS][Q][MR_PSTRIDE];
-    __shared__ float s_max[4][Q], s_run[Q], s_fac[Q], s_kx[Q], s_sum[MR_THREADS / 32][Q];
-    __shared__ __align__(8) uint8_t s_scale[MR_T][8];
-    __shared__ int s_top[4][UNITS];
-    __shared__ double s_xx[Q];
-    __shared__ int abort_flag;
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ void tma_points(uint32_t dst, const CUtensorMap *tm, int byte, int point, int lane, uint32_t mbar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(byte), "r"(point), "r"(lane), "r"(mbar) : "memory");
+}
+// 128 rows' words of four scales, 512 bytes of shared memory, into four columns of tensor memory
+__device__ __forceinline__ void scales_in(uint32_t taddr, uint32_t saddr)
+{
+    const uint64_t desc = (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(128u >> 4) << 32) | (1ull << 46);
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sfa, uint32_t sfb, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
+}
+__device__ __forceinline__ void mma_codes(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ bool elected()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// whether all 128 threads of the softmax say so
+__device__ __forceinline__ bool all_softmax(bool ok)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    return r != 0;
+}
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = lane >> 2, c = lane & 3;
-    const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-    unsigned char *gen = smem_dyn + (base - smem_u32(smem_dyn));
-    const int split = blockIdx.x, q0 = blockIdx.y * Q, w = blockIdx.z;
-    const int nby = (P.d + 127) / 128, nbv = P.own_values ? (P.dv + 127) / 128 : 0, per_tile = nby + nbv;
-    uint2 *xf = reinterpret_cast<uint2 *>(gen + (size_t)slots * MR_SLOT);      // [NG][8 nby][32] fragments of the queries
-    auto bar = [&](int s) { return smem_u32(&bars[s]); };
+// How a block's shared and tensor memory are laid out (the host's as well: it sizes them).
+struct MapRows {
+    int nby, nb;                              // blocks of 128 dimensions: of the bank, of the images
+    int yslots, vslots;                       // of the bank, of values of their own
+    int words;                                // words of scales of a point of the bank
+    uint32_t x, p, scales, small;             // offsets: queries, weights (two buffers), scales (MR_AHEAD tiles', then the queries'), the rest
+    uint32_t bytes, columns;
+};
+template <int NQ>
+__host__ __device__ inline MapRows map_rows_layout(int d, int nb, int yslots, int vslots)
+{
+    MapRows L;
+    L.nby = (d + 127) / 128;
+    L.nb = nb;
+    L.yslots = yslots;
+    L.vslots = vslots;
+    L.words = (L.nby + 3) / 4;
+    L.x = (uint32_t)(yslots + vslots) * MR_SLOT;
+    L.p = L.x + (uint32_t)(L.nby * MR_ROWS<NQ>) * 128;
+    L.scales = L.p + 2 * (uint32_t)(L.nb * 2 * NQ) * 128;
+    L.small = L.scales + (MR_AHEAD + 1) * (uint32_t)L.words * 512;
+    // terms, values' scales, tops, maxima, sums, lengths, barriers
+    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4) + 2 * 4 * NQ * 4 + 4 * NQ * 4 + NQ * 4 + NQ * 8 + 64 * 8 + 16;
+    const uint32_t used = 2 * MR_SCOLS<NQ> + 2 * (uint32_t)(L.nb * 2 * NQ) + 12 * (uint32_t)L.words;
+    L.columns = 32;
+    while (L.columns < used) L.columns *= 2;
+    return L;
+}
+
+template <int NQ, int UNITS>
+__global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_kernel(const __grid_constant__ CUtensorMap tmy, const __grid_constant__ CUtensorMap tmv,
+                                                              const __grid_constant__ Map P, const int yslots, const int vslots, const int vblocks)
+{
+    constexpr int ROWS = MR_ROWS<NQ>, SCOLS = MR_SCOLS<NQ>;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");               // (the parts' join waits for all of this grid's writes itself)
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    // (values deeper than what a block has room for: further blocks, which form the scores again)
+    const int qgroups = (P.n + NQ - 1) / NQ, z = blockIdx.y / qgroups, v0 = z * vblocks;
+    const int split = blockIdx.x, q0 = (blockIdx.y - z * qgroups) * NQ, w = blockIdx.z, nq = min(NQ, P.n - q0);
+    const MapRows L = map_rows_layout<NQ>(P.d, vblocks, yslots, vslots);
+    const int nby = L.nby, nb = min(vblocks, (P.dv + 127) / 128 - v0);
+    const uint32_t base = smem_u32(smem);
+    float *terms = reinterpret_cast<float *>(smem + L.small);                        // [MR_AHEAD][128]
+    uint2 *vscales = reinterpret_cast<uint2 *>(terms + MR_AHEAD * 128);              // [MR_AHEAD][128]
+    float *maxima = reinterpret_cast<float *>(vscales + MR_AHEAD * 128);             // [2][4][NQ]
+    uint32_t *tops = reinterpret_cast<uint32_t *>(maxima + 8 * NQ);                  // [MR_AHEAD][8]
+    float *sums = reinterpret_cast<float *>(tops + MR_AHEAD * MR_MAX_BLOCKS);                                                  // [4][NQ]
+    float *runs = sums + 4 * NQ;                                                     // [NQ]
+    double *lengths2 = reinterpret_cast<double *>(runs + NQ);                        // [NQ]
+    unsigned long long *bars = reinterpret_cast<unsigned long long *>(lengths2 + NQ);
+    uint32_t *holder = reinterpret_cast<uint32_t *>(bars + 64);
+    int *abort_flag = reinterpret_cast<int *>(holder + 1);
+    volatile int *ab = abort_flag;
+    auto bar = [&](int i) { return smem_u32(&bars[i]); };
+    constexpr int FULL = 0, EMPTY = MR_MAX_SLOTS, CFULL = 2 * MR_MAX_SLOTS, CEMPTY = CFULL + MR_AHEAD, SFULL = CEMPTY + MR_AHEAD, PFULL = SFULL + 2, DFULL = PFULL + 2,
+                  DFREE = DFULL + 2, LAST = DFREE + 2;
+    static_assert(LAST + 1 < 64, "barriers");
 
     const int len = map_length(P, w), tiles = (len + MR_T - 1) / MR_T;
-    const int t0 = (int)((long long)tiles * split / P.splits), t1 = (int)((long long)tiles * (split + 1) / P.splits);
+    const int t0 = (int)((long long)tiles * split / P.splits), nt = (int)((long long)tiles * (split + 1) / P.splits) - t0;
     if (tid == 0) {
-        for (int s = 0; s < slots; ++s) mbar_init(bar(s), 1);
-        abort_flag = 0;
+        for (int s = 0; s < yslots + vslots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(EMPTY + s), 1); }
+        for (int c = 0; c < MR_AHEAD; ++c) { mbar_init(bar(CFULL + c), 1); mbar_init(bar(CEMPTY + c), 8); }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(bar(SFULL + b), 1);
+            mbar_init(bar(PFULL + b), 4);
+            mbar_init(bar(DFULL + b), 1);
+            mbar_init(bar(DFREE + b), 4);
+        }
+        mbar_init(bar(LAST), 1);
+        mbar_init(bar(LAST + 1), 1);
+        *abort_flag = (base & 1023u) ? 1 : 0;                                        // (the swizzle counts from 1024-byte boundaries)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(holder)), "r"(L.columns) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    __syncwarp();
+    tc_fence_before();
     __syncthreads();
-    // slots are filled in the order of tiles and their blocks: the bank's, then those of values of their own.  (Slots, tiles and phases are counted
-    // on: divisions would be half of the instructions.)
-    int in_tile = t0, in_block = 0, in_slot = 0;                              // (thread 0) what comes into a slot next
-    auto issue = [&](int count) {
-        for (; count > 0 && in_tile < t1; --count) {
-            mbar_expect_tx(bar(in_slot), MR_SLOT);
-            if (in_block < nby) tma_points(base + in_slot * MR_SLOT, &tmy, in_block * 128, in_tile * MR_T, w, bar(in_slot));
-            else tma_points(base + in_slot * MR_SLOT, &tmv, (in_block - nby) * 128, in_tile * MR_T, w, bar(in_slot));
-            if (++in_block == per_tile) { in_block = 0; ++in_tile; }
-            if (++in_slot == slots) in_slot = 0;
-        }
-    };
-    if (tid == 0) issue(slots);
-
-    // the queries: a power of two, the squared length, then f16 in the order of the matrix instruction's fragments.  A warp takes every fourth.
+    tc_fence_after();
     const double k = map_scale(P, w);
-    for (int q = warp; q < Q; q += 4) {
-        const bool live = q0 + q < P.n;
-        const uint16_t *x = P.x + ((size_t)w * P.n + (live ? q0 + q : 0)) * P.d;
-        float top = 0.f;
-        bool bad = false;
+    // Loads and targets' terms start at once; the others make the queries ready first.  What no query and no live weight fills stays zero: rows of
+    // queries that are not there, their weights, the queries' unused scales
+    constexpr int READY = 9 * 32;
+    const int member = warp == 9 ? 8 : warp;
+    if (warp < 8 || warp == 9) {
+        for (uint32_t i = L.x / 16 + member * 32 + lane; i < L.scales / 16; i += READY) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (uint32_t i = (L.scales + MR_AHEAD * L.words * 512) / 16 + member * 32 + lane; i < L.small / 16; i += READY) reinterpret_cast<uint4 *>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        asm volatile("bar.sync 3, %0;" ::"n"(READY) : "memory");
+    }
+    // the queries, a warp to each: blocks' powers of two, three numbers of a value, the squared length
+    for (int q = member; q < nq && (warp < 8 || warp == 9); q += READY / 32) {
+        const uint16_t *x = P.x + ((size_t)w * P.n + q0 + q) * P.d;
         double xx = 0.0;
-        if (live)
-            for (int i = lane; i < P.d; i += 32) {
-                const float v = __uint_as_float((uint32_t)x[i] << 16);
-                bad |= !(fabsf(v) <= 3.402823466e38f);
-                top = fmaxf(top, fabsf(v));
-                xx += (double)v * (double)v;
-            }
-#pragma unroll
-        for (int off = 16; off; off /= 2) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            xx += __shfl_xor_sync(0xffffffffu, xx, off);
-        }
-        bad = __any_sync(0xffffffffu, bad);
-        const int ex = top > 0.f && !bad ? max(exponent_of(top) - 14, -126) : 0;
-        const float inv = power_of_two(-ex);
-        // fragment of eight dimensions 64 b + 16 c + 4 s .. + 3: lane (query, c) of step 4 b + s
-        for (int i = lane; i < 32 * nby; i += 32) {                            // words of four dimensions
-            uint32_t h[2] = {0u, 0u};
+        bool bad = false;
+#pragma unroll 4
+        for (int b = 0; b < nby; ++b) {
+            float v[4], top = 0.f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int dim = 4 * i + e;
-                uint32_t bits = 0;
-                if (live && dim < P.d) bits = bad ? 0x7fffu : f16_bits(__uint_as_float((uint32_t)x[dim] << 16) * inv);
-                h[e / 2] |= bits << (16 * (e & 1));
+                const int dim = 128 * b + 4 * lane + e;
+                v[e] = dim < P.d ? __uint_as_float((uint32_t)x[dim] << 16) : 0.f;
             }
-            const int b = i / 16, cc = i / 4 % 4, s = i % 4;
-            xf[((q >> 3) * 8 * nby + 4 * b + s) * 32 + 4 * (q & 7) + cc] = make_uint2(h[0], h[1]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                bad |= !(fabsf(v[e]) <= 3.402823466e38f);
+                top = fmaxf(top, fabsf(v[e]));
+                xx += (double)v[e] * (double)v[e];
+            }
+            top = warp_max(top);
+            int ex = CLOUD8_MIN_E;
+            if (top > 0.f && top <= 3.402823466e38f) {
+                ex = max(exponent_of(top) - 8, CLOUD8_MIN_E);
+                if (top > 448.f * power_of_two(ex)) ++ex;
+            }
+            const float inv = power_of_two(-ex);
+            float u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = v[e] * inv;
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+                const int r = part * NQ + q;
+                const uint32_t lo = e4m3_two(u[0], u[1]), hi = e4m3_two(u[2], u[3]);
+                *reinterpret_cast<uint32_t *>(smem + L.x + (b * ROWS + r) * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4) = lo | hi << 16;
+                const float2 a = e4m3_pair(lo), c = e4m3_pair(hi);
+                u[0] = (u[0] - a.x) * 16.f;
+                u[1] = (u[1] - a.y) * 16.f;
+                u[2] = (u[2] - c.x) * 16.f;
+                u[3] = (u[3] - c.y) * 16.f;
+                if (lane == 0) smem[L.scales + (MR_AHEAD * L.words + b / 4) * 512 + (r & 31) * 16 + (r >> 5) * 4 + (b & 3)] = (uint8_t)(ex - 4 * part + 127);
+            }
         }
-        if (lane == 0) {
-            s_kx[q] = (float)(2.0 * k * (double)power_of_two(ex));
-            s_xx[q] = xx;
-            s_run[q] = -INFINITY;
-        }
+        bad = __any_sync(0xffffffffu, bad);
+        __syncwarp();
+        // (a query that is not finite: scales that are NaN)
+        if (bad && lane < nby)
+            for (int part = 0; part < 3; ++part) {
+                const int r = part * NQ + q;
+                smem[L.scales + (MR_AHEAD * L.words + lane / 4) * 512 + (r & 31) * 16 + (r >> 5) * 4 + (lane & 3)] = 255;
+            }
+#pragma unroll
+        for (int off = 16; off; off /= 2) xx += __shfl_xor_sync(0xffffffffu, xx, off);
+        if (lane == 0) lengths2[q] = xx;
+        __syncwarp();
     }
-
-    float out[UNITS][NG][2][4];
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u)
-#pragma unroll
-        for (int a = 0; a < NG; ++a)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) out[u][a][i / 4][i & 3] = 0.f;
-    float sum[Q / 2];                                                          // of this thread's point of a tile, for every other query
-#pragma unroll
-    for (int i = 0; i < Q / 2; ++i) sum[i] = 0.f;
-
-    // this lane's two points of a tile (rows of the fragment are points in an order that keeps shared memory's banks apart)
-    const int pa = 16 * warp + ((row >> 1) | ((row & 1) << 2)), pb = pa + 8;
-    const uint2 none = make_uint2(0u, 0u);
-    struct Point {
-        float term;
-        uint2 sy, sv;
-    };
-    auto fetch = [&](int t, int p) {
-        Point r = {-INFINITY, none, none};
-        const int j = t * MR_T + p;
-        if (j >= len) return r;
-        const size_t at = (size_t)w * P.m + j;
-        r.term = map_term(k, P.g ? P.g[at] : 0.0, P.y.norms[at]);
-        const uint32_t *sy = reinterpret_cast<const uint32_t *>(P.y.scales + at * P.y.sb);
-        r.sy = make_uint2(sy[0], P.y.sb > 4 ? sy[1] : 0u);
-        if (P.own_values) {
-            const uint32_t *sv = reinterpret_cast<const uint32_t *>(P.v.scales + at * P.v.sb);
-            r.sv = make_uint2(sv[0], P.v.sb > 4 ? sv[1] : 0u);
-        } else r.sv = r.sy;
-        return r;
-    };
-    auto byte_of = [](uint2 s, int b) { return ((b < 4 ? s.x : s.y) >> (8 * (b & 3))) & 255u; };
-    Point na, nb;
-    if (t0 < t1) { na = fetch(t0, pa); nb = fetch(t0, pb); }
-    __syncthreads();
-
-    int slot0 = 0;                                                            // of a tile's first block, and the phase it is filled in
-    uint32_t phase = 0;
-    bool ok = true;
-    for (int t = t0; t < t1; ++t) {
-        const Point A = na, Bp = nb;
-        if (t + 1 < t1) { na = fetch(t + 1, pa); nb = fetch(t + 1, pb); }
-        auto slot_of = [&](int b) { return slot0 + b < slots ? slot0 + b : slot0 + b - slots; };
-        auto wait = [&](int b) {
-            const int i = slot_of(b);
-            ok = mbar_wait(bar(i), phase ^ (slot0 + b < slots ? 0u : 1u), &abort_flag) && ok;
-            return gen + i * MR_SLOT;
-        };
-        // ---- scores
-        float s[NG][4];
-#pragma unroll
-        for (int a = 0; a < NG; ++a)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[a][i] = 0.f;
-        for (int b = 0; b < nby; ++b) {
-            const unsigned char *slot = wait(b);
-            float acc[NG][4];
-#pragma unroll
-            for (int a = 0; a < NG; ++a)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[a][i] = 0.f;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 ra = *reinterpret_cast<const uint4 *>(slot + pa * 128 + (((4 * h + c) ^ (pa & 7)) << 4));
-                const uint4 rb = *reinterpret_cast<const uint4 *>(slot + pb * 128 + (((4 * h + c) ^ (pb & 7)) << 4));
-                const uint32_t wa[4] = {ra.x, ra.y, ra.z, ra.w}, wb[4] = {rb.x, rb.y, rb.z, rb.w};
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t a0 = half_lo(wa[q]), a1 = half_lo(wb[q]), a2 = half_hi(wa[q]), a3 = half_hi(wb[q]);
-#pragma unroll
-                    for (int a = 0; a < NG; ++a) {
-                        const uint2 x = xf[(a * 8 * nby + 8 * b + 4 * h + q) * 32 + lane];
-                        mma16816(acc[a], a0, a1, a2, a3, x.x, x.y);
-                    }
-                }
-            }
-            const float fa = e8m0_value(byte_of(A.sy, b)), fb = e8m0_value(byte_of(Bp.sy, b));
-#pragma unroll
-            for (int a = 0; a < NG; ++a) {
-                s[a][0] = fmaf(acc[a][0], fa, s[a][0]);
-                s[a][1] = fmaf(acc[a][1], fa, s[a][1]);
-                s[a][2] = fmaf(acc[a][2], fb, s[a][2]);
-                s[a][3] = fmaf(acc[a][3], fb, s[a][3]);
-            }
-        }
-#pragma unroll
-        for (int a = 0; a < NG; ++a)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int q = 8 * a + 2 * c + i;
-                const float kx = s_kx[q];
-                // (what a masked point's codes hold does not matter)
-                const float va = A.term == -INFINITY ? -INFINITY : fmaf(s[a][i], kx, A.term), vb = Bp.term == -INFINITY ? -INFINITY : fmaf(s[a][2 + i], kx, Bp.term);
-                s_arg[q][pa] = va;
-                s_arg[q][pb] = vb;
-                float top = fmaxf(va, vb);
-#pragma unroll
-                for (int off = 4; off < 32; off *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-                if (row == 0) s_max[warp][q] = top;
-            }
-        // the values' scales, and the largest exponent of the tile in each block (of points that are masked or NaN: none)
-        if (c == 0) {
-            *reinterpret_cast<uint2 *>(s_scale[pa]) = A.sv;
-            *reinterpret_cast<uint2 *>(s_scale[pb]) = Bp.sv;
-        }
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            const uint32_t ea = byte_of(A.sv, u), eb = byte_of(Bp.sv, u);
-            const uint32_t one = max(A.term == -INFINITY || ea == 255u ? 0u : ea, Bp.term == -INFINITY || eb == 255u ? 0u : eb);
-            const uint32_t top = __reduce_max_sync(0xffffffffu, one);
-            if (lane == 0) s_top[warp][u] = (int)top;
-        }
-        __syncthreads();
-        // ---- softmax: thread = point and every other query
-        {
-            const int p = tid & 63, other = tid >> 6;
-            uint32_t scale[UNITS];
-            const uint2 sv = *reinterpret_cast<const uint2 *>(s_scale[p]);
-#pragma unroll
-            for (int u = 0; u < UNITS; ++u) {
-                const int e = (int)byte_of(sv, u), top = max(max(s_top[0][u], s_top[1][u]), max(s_top[2][u], s_top[3][u]));
-                // a power of two (0: below fp32's), or NaN; masked points have weights of zero
-                scale[u] = e == 255 ? 0x7fffffffu : e > top ? 0u : e - top + 127 <= 0 ? 0u : (uint32_t)(e - top + 127) << 23;
-            }
-#pragma unroll
-            for (int i = 0; i < Q / 2; ++i) {
-                const int q = 2 * i + other;
-                const float run = s_run[q], top = fmaxf(fmaxf(fmaxf(s_max[0][q], s_max[1][q]), fmaxf(s_max[2][q], s_max[3][q])), run);
-                const float ref = top == -INFINITY ? 0.f : top, arg = s_arg[q][p], fac = ex2f(run - ref);
-                const float e = ex2f(arg - ref);
-                sum[i] = fmaf(sum[i], fac, e);
-                if (p == 0) s_fac[q] = fac;
-                const bool masked = arg == -INFINITY;
-#pragma unroll
-                for (int u = 0; u < UNITS; ++u) s_p[u][q][p] = masked ? (uint16_t)0 : f16_bits(e * __uint_as_float(scale[u]));
-            }
-        }
-        __syncthreads();
-        if (tid < Q) {
-            const float top = fmaxf(fmaxf(s_max[0][tid], s_max[1][tid]), fmaxf(s_max[2][tid], s_max[3][tid]));
-            s_run[tid] = fmaxf(s_run[tid], top);
-        }
-        // ---- images
-        float fac[NG][2];
-#pragma unroll
-        for (int a = 0; a < NG; ++a) { fac[a][0] = s_fac[8 * a + 2 * c]; fac[a][1] = s_fac[8 * a + 2 * c + 1]; }
-#pragma unroll
-        for (int u = 0; u < UNITS; ++u) {
-            if (128 * u + 32 * warp >= P.dv) break;
-            const unsigned char *slot = nbv ? wait(nby + u) : gen + slot_of(u) * MR_SLOT;
-            float acc[NG][2][4];
-#pragma unroll
-            for (int a = 0; a < NG; ++a)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) acc[a][i / 4][i & 3] = 0.f;
-#pragma unroll
-            for (int kk = 0; kk < MR_T / 16; ++kk) {
-                auto word = [&](int p) { return *reinterpret_cast<const uint32_t *>(slot + p * 128 + (((2 * warp + (row >> 2)) ^ (p & 7)) << 4) + (row & 3) * 4); };
-                const int p = 16 * kk + 2 * c;
-                const uint32_t w0 = word(p), w1 = word(p + 1), w2 = word(p + 8), w3 = word(p + 9);
-                const uint32_t l01 = __byte_perm(w0, w1, 0x5140), h01 = __byte_perm(w0, w1, 0x7362);
-                const uint32_t l23 = __byte_perm(w2, w3, 0x5140), h23 = __byte_perm(w2, w3, 0x7362);
-                const uint32_t a00 = half_lo(l01), a01 = half_hi(l01), a02 = half_lo(l23), a03 = half_hi(l23);
-                const uint32_t a10 = half_lo(h01), a11 = half_hi(h01), a12 = half_lo(h23), a13 = half_hi(h23);
-#pragma unroll
-                for (int a = 0; a < NG; ++a) {
-                    const uint16_t *pq = s_p[u][8 * a + row] + p;
-                    const uint32_t b0 = *reinterpret_cast<const uint32_t *>(pq), b1 = *reinterpret_cast<const uint32_t *>(pq + 8);
-                    mma16816(acc[a][0], a00, a01, a02, a03, b0, b1);
-                    mma16816(acc[a][1], a10, a11, a12, a13, b0, b1);
-                }
-            }
-            const int top = max(max(s_top[0][u], s_top[1][u]), max(s_top[2][u], s_top[3][u]));
-            const float unit = e8m0_value((uint32_t)top);
-#pragma unroll
-            for (int a = 0; a < NG; ++a)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) out[u][a][i / 4][i & 3] = fmaf(out[u][a][i / 4][i & 3], fac[a][i & 1], acc[a][i / 4][i & 3] * unit);
-        }
-        ok = __syncthreads_and(ok);
-        if (!ok) break;
-        if (tid == 0) issue(per_tile);
-        slot0 += per_tile;
-        if (slot0 >= slots) { slot0 -= slots; phase ^= 1u; }
+    if (warp < 8 || warp == 9) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("bar.sync 3, %0;" ::"n"(READY) : "memory");
     }
-    // nothing may land in shared memory after the block has gone: where a wait ran out, every load that may still be on its way
-    if (!ok && tid == 0) {
-        int unused = 0, s = slot0;
-        uint32_t ph = phase;
-        for (int i = 0; i < slots && (s != in_slot || i == 0); ++i) {
-            mbar_wait(bar(s), ph, &unused);
+    const uint32_t tmem = *holder;
+    // tensor memory: scores (two buffers), images (two), the bank's scales (two), the queries'
+    const uint32_t tD = tmem + 2 * SCOLS, dcols = (uint32_t)(vblocks * 2 * NQ), tA = tD + 2 * dcols, tB = tA + 8 * L.words;
+    const bool starts = *ab == 0;
+    auto there = [&](uint32_t a, uint32_t parity) {
+        uint32_t r;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(r) : "r"(a), "r"(parity) : "memory");
+        return r != 0;
+    };
+    // a tile's slots of a ring
+    auto filled = [&](int first, int slots, int s, uint32_t ph, int count) {
+        for (int c = 0; c < count; ++c) {
+            if (!mbar_wait(bar(FULL + first + s), ph, ab)) return false;
             if (++s == slots) { s = 0; ph ^= 1u; }
         }
-    }
-    // ---- the sums, over points
+        return true;
+    };
+    // what a warp has issued is over before tensor memory is given back
+    auto finish = [&](int barrier) {
+        if (elected()) {
+            tc_commit(bar(barrier));
+            int unused = 0;
+            mbar_wait(bar(barrier), 0, &unused);
+        }
+        __syncwarp();
+    };
+
+    if (warp < 4) {
+        // ---- softmax: a thread to a target, which is a lane of tensor memory
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const float kx = (float)(2.0 * k);
+        float run[NQ], sum[NQ];
 #pragma unroll
-    for (int i = 0; i < Q / 2; ++i) {
-#pragma unroll
-        for (int off = 16; off; off /= 2) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], off);
-        if (lane == 0) s_sum[warp][2 * i + (warp >> 1)] = sum[i];
-    }
-    __syncthreads();
-    const float nan = __uint_as_float(0x7fffffffu);
-    auto sum_of = [&](int q) { return !ok ? nan : (q & 1) ? s_sum[2][q] + s_sum[3][q] : s_sum[0][q] + s_sum[1][q]; };
-    if (tid < Q && q0 + tid < P.n) {
-        const size_t r = (size_t)w * P.n + q0 + tid;
-        if (P.splits > 1) {
-            reinterpret_cast<float2 *>(P.part_ml)[r * P.splits + split] = make_float2(s_run[tid], sum_of(tid));
-        } else if (P.lse) P.lse[r] = map_lse(s_run[tid], sum_of(tid), k, s_xx[tid]);
-    }
-#pragma unroll
-    for (int a = 0; a < NG; ++a)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int q = 8 * a + 2 * c + i;
-            if (q0 + q >= P.n) continue;
-            const size_t r = (size_t)w * P.n + q0 + q;
-            const float total_q = sum_of(q), inv = total_q == 0.f ? 0.f : 1.f / total_q;
+        for (int q = 0; q < NQ; ++q) { run[q] = -INFINITY; sum[q] = 0.f; }
+        bool ok = starts;
+        for (int t = 0; t < nt && starts; ++t) {
+            const int b = t & 1;
+            const uint32_t ph = (uint32_t)(t >> 1) & 1u;
+            const int c4 = t % MR_AHEAD;
+            ok = ok && mbar_wait(bar(CFULL + c4), (uint32_t)(t / MR_AHEAD) & 1u, ab) && mbar_wait(bar(SFULL + b), ph, ab) && mbar_wait(bar(DFREE + b), ph ^ 1u, ab);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            const float term = terms[128 * c4 + tid];
+            const uint2 sv = vscales[128 * c4 + tid];
+            const bool masked = term == -INFINITY;
+            // 256 times the values' powers of two, less the tile's largest (0: below fp32's), or NaN; masked targets have weights of zero
+            float scale[UNITS];
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
-                const int dim = 128 * u + 32 * warp + 4 * row;
-                if (dim >= P.dv) continue;
-                const float o[4] = {out[u][a][0][i], out[u][a][0][2 + i], out[u][a][1][i], out[u][a][1][2 + i]};
-                if (P.splits > 1) {
-                    float *dst = P.part_out + (r * P.splits + split) * P.dv + dim;
+                const int e = (int)(((u < 4 ? sv.x : sv.y) >> (8 * (u & 3))) & 255u), x = e - (int)tops[c4 * MR_MAX_BLOCKS + u] + 135;
+                scale[u] = __uint_as_float(e == 255 ? 0x7fffffffu : x > 0 ? (uint32_t)x << 23 : 0u);
+            }
+            float arg[NQ];
+            if (ok) {
+                uint32_t r[MR_SCOLS<NQ>];
+                uint32_t (&r0)[32] = *reinterpret_cast<uint32_t (*)[32]>(r);
+                tc_ld32_issue(tmem + lanes + SCOLS * b, r0);
+                tc_ld_wait(r0);
+                if constexpr (NQ == 16) {
+                    uint32_t (&r1)[16] = *reinterpret_cast<uint32_t (*)[16]>(r + 32);
+                    tc_ld16_issue(tmem + lanes + SCOLS * b + 32, r1);
+                    tc_ld16_wait(r1);
+                }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (dim + e < P.dv) dst[e] = o[e];
-                } else {
-                    uint16_t *dst = P.out + r * P.dv + dim;
-                    const uint32_t lo = bf16_pair(o[0] * inv, o[1] * inv), hi = bf16_pair(o[2] * inv, o[3] * inv);
-                    if (P.dv % 4 == 0 && (uintptr_t)P.out % 8 == 0) *reinterpret_cast<uint2 *>(dst) = make_uint2(lo, hi);
-                    else
+                for (int q = 0; q < NQ; ++q) {
+                    const float s = __uint_as_float(r[q]) + (__uint_as_float(r[NQ + q]) + __uint_as_float(r[2 * NQ + q]));
+                    arg[q] = masked ? -INFINITY : fmaf(s, kx, term);
+                }
+            } else
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (dim + e < P.dv) dst[e] = (uint16_t)((e < 2 ? lo : hi) >> (16 * (e & 1)));
+                for (int q = 0; q < NQ; ++q) arg[q] = 0.f;
+            // (queries that are not there, to a whole four, have scores of zero: what becomes of them is not looked at)
+#pragma unroll
+            for (int q = 0; q < NQ; q += 4)
+                if (q < nq) {
+                    const float4 m = make_float4(warp_max(arg[q]), warp_max(arg[q + 1]), warp_max(arg[q + 2]), warp_max(arg[q + 3]));
+                    if (lane == 0) *reinterpret_cast<float4 *>(maxima + (4 * b + warp) * NQ + q) = m;
+                }
+            ok = all_softmax(ok);
+            if (!ok) break;
+            unsigned char *weights = smem + L.p + b * (vblocks * 2 * NQ) * 128 + (tid & 15);
+#pragma unroll
+            for (int q = 0; q < NQ; q += 4) {
+                if (q >= nq) break;
+                float top[4], p[4];
+                {
+                    const float4 *mp = reinterpret_cast<const float4 *>(maxima + 4 * b * NQ + q);
+                    const float4 m0 = mp[0], m1 = mp[NQ / 4], m2 = mp[NQ / 2], m3 = mp[3 * NQ / 4];
+                    top[0] = fmaxf(fmaxf(m0.x, m1.x), fmaxf(m2.x, m3.x));
+                    top[1] = fmaxf(fmaxf(m0.y, m1.y), fmaxf(m2.y, m3.y));
+                    top[2] = fmaxf(fmaxf(m0.z, m1.z), fmaxf(m2.z, m3.z));
+                    top[3] = fmaxf(fmaxf(m0.w, m1.w), fmaxf(m2.w, m3.w));
+                }
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    // (tile's maximum plus infinity: the exponential is NaN, and so is what follows from it)
+                    p[h] = ex2f(arg[q + h] - (top[h] == -INFINITY ? 0.f : top[h]));
+                    const float now = fmaxf(run[q + h], top[h]), ref = now == -INFINITY ? 0.f : now;
+                    sum[q + h] = fmaf(sum[q + h], ex2f(run[q + h] - ref), p[h] * ex2f(top[h] - ref));
+                    run[q + h] = now;
+                    if (masked) p[h] = 0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < UNITS; ++u) {
+                    if (u >= nb) break;
+                    const float a0 = masked ? 0.f : p[0] * scale[u], a1 = masked ? 0.f : p[1] * scale[u], a2 = masked ? 0.f : p[2] * scale[u],
+                                a3 = masked ? 0.f : p[3] * scale[u];
+                    const uint32_t lo = e4m3_two(a0, a1), hi = e4m3_two(a2, a3);
+                    const float2 bl = e4m3_pair(lo), bh = e4m3_pair(hi);
+                    const uint32_t lo2 = e4m3_two((a0 - bl.x) * 16.f, (a1 - bl.y) * 16.f), hi2 = e4m3_two((a2 - bh.x) * 16.f, (a3 - bh.y) * 16.f);
+                    unsigned char *block = weights + u * (2 * NQ) * 128;
+                    auto put = [&](int r, uint32_t byte) { block[r * 128 + (((tid >> 4) ^ (r & 7)) << 4)] = (unsigned char)byte; };
+                    put(q, lo); put(q + 1, lo >> 8); put(q + 2, hi); put(q + 3, hi >> 8);
+                    put(NQ + q, lo2); put(NQ + q + 1, lo2 >> 8); put(NQ + q + 2, hi2); put(NQ + q + 3, hi2 >> 8);
                 }
             }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(bar(PFULL + b)); mbar_arrive(bar(CEMPTY + c4)); }
         }
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            float s = ok ? sum[q] : __uint_as_float(0x7fffffffu);
+#pragma unroll
+            for (int off = 16; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
+            if (lane == 0) sums[warp * NQ + q] = s;
+            if (tid == 0) runs[q] = run[q];
+        }
+        asm volatile("bar.sync 2, 256;" ::: "memory");
+        if (tid < nq) {
+            const size_t r = (size_t)w * P.n + q0 + tid;
+            const float total = (sums[tid] + sums[NQ + tid]) + (sums[2 * NQ + tid] + sums[3 * NQ + tid]);
+            if (z) {}                                                               // (the first block of a query has them)
+            else if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[r * P.splits + split] = make_float2(runs[tid], total);
+            else if (P.lse) P.lse[r] = map_lse(runs[tid], total, k, lengths2[tid]);
+        }
+    } else if (warp < 8) {
+        // ---- images: a thread to a dimension of every block
+        const uint32_t lanes = (uint32_t)((warp - 4) * 32) << 16;
+        float out[UNITS][NQ], run[NQ];
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            run[q] = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) out[u][q] = 0.f;
+        }
+        bool ok = starts;
+        for (int t = 0; t < nt && ok; ++t) {
+            const int b = t & 1;
+            const uint32_t ph = (uint32_t)(t >> 1) & 1u;
+            ok = mbar_wait(bar(PFULL + b), ph, ab) && mbar_wait(bar(DFULL + b), ph, ab);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            // what the images so far and the tile's are multiplied by
+            float before[NQ], of_tile[NQ];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                const float *mp = maxima + 4 * b * NQ + q;
+                const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run[q], top), ref = now == -INFINITY ? 0.f : now;
+                before[q] = ex2f(run[q] - ref);
+                of_tile[q] = ex2f(top - ref) * 0.00390625f;
+                run[q] = now;
+            }
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                if (u >= nb) break;
+                const float unit = e8m0_value(tops[t % MR_AHEAD * MR_MAX_BLOCKS + u]);
+                uint32_t r[2 * NQ];
+                if constexpr (NQ == 8) {
+                    tc_ld16_issue(tD + lanes + b * dcols + u * 2 * NQ, r);
+                    tc_ld16_wait(r);
+                } else {
+                    tc_ld32_issue(tD + lanes + b * dcols + u * 2 * NQ, r);
+                    tc_ld_wait(r);
+                }
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    const float v = fmaf(__uint_as_float(r[NQ + q]), 0.0625f, __uint_as_float(r[q])) * unit;
+                    out[u][q] = fmaf(out[u][q], before[q], v * of_tile[q]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) { mbar_arrive(bar(DFREE + b)); mbar_arrive(bar(CEMPTY + t % MR_AHEAD)); }
+        }
+        asm volatile("bar.sync 2, 256;" ::: "memory");
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            if (q >= nq) break;
+            const size_t r = (size_t)w * P.n + q0 + q;
+            const float total = (sums[q] + sums[NQ + q]) + (sums[2 * NQ + q] + sums[3 * NQ + q]);
+            const float inv = !ok ? __uint_as_float(0x7fffffffu) : P.splits > 1 ? (total == total ? 1.f : total) : total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                const int dim = 128 * (v0 + u) + tid - 128;
+                if (u >= nb || dim >= P.dv) continue;
+                if (P.splits > 1) P.part_out[(r * P.splits + split) * P.dv + dim] = out[u][q] * inv;
+                else P.out[r * P.dv + dim] = (uint16_t)bf16_pair(out[u][q] * inv, 0.f);
+            }
+        }
+    } else if (warp == 8) {
+        // ---- loads: of the bank and of values of their own, whichever has a slot
+        if (lane == 0) {
+            bool ok = starts;
+            struct Ring {
+                int slot, block, tile, issued;
+                uint32_t ph;
+            } ring[2] = {{0, 0, 0, 0, 0u}, {0, 0, vslots ? 0 : nt, 0, 0u}};
+            auto move = [&](Ring &r, bool value) {
+                const int first = value ? yslots : 0, slots = value ? vslots : yslots;
+                if (r.tile >= nt || !there(bar(EMPTY + first + r.slot), r.ph ^ 1u)) return false;
+                const uint32_t full = bar(FULL + first + r.slot), dst = base + (first + r.slot) * MR_SLOT;
+                mbar_expect_tx(full, MR_SLOT);
+                if (value) tma_points(dst, &tmv, (v0 + r.block) * 128, (t0 + r.tile) * MR_T, w, full);
+                else tma_points(dst, &tmy, r.block * 128, (t0 + r.tile) * MR_T, w, full);
+                ++r.issued;
+                if (++r.block == (value ? nb : nby)) { r.block = 0; ++r.tile; }
+                if (++r.slot == slots) { r.slot = 0; r.ph ^= 1u; }
+                return true;
+            };
+            long long since = clock64();
+            while (ok && (ring[0].tile < nt || ring[1].tile < nt)) {
+                const bool a = move(ring[0], false), b = move(ring[1], true);
+                if (a || b) since = clock64();
+                else if (*ab || clock64() - since > TC_WAIT_CLOCKS) {
+                    *abort_flag = 1;
+                    ok = false;
+                }
+            }
+            // nothing may land in shared memory after the block has gone: the last load of every slot, with a bound of its own
+            int unused = 0;
+            for (int q = max(0, ring[0].issued - yslots); q < ring[0].issued; ++q) mbar_wait(bar(FULL + q % yslots), (uint32_t)(q / yslots) & 1u, &unused);
+            for (int q = max(0, ring[1].issued - vslots); q < ring[1].issued; ++q)
+                mbar_wait(bar(FULL + yslots + q % vslots), (uint32_t)(q / vslots) & 1u, &unused);
+        }
+    } else if (warp == 9) {
+        // ---- scores: the whole warp walks through the tiles, so that descriptors are uniform; one thread issues.  (A wait, and what follows it, takes as
+        // long as sixteen instructions: a tile's slots are waited for first, then all is issued.)
+        constexpr uint32_t shape = ((uint32_t)(ROWS >> 3) << 17) | ((uint32_t)(128 >> 4) << 24) | 1u << 23;            // e4m3, e4m3, scales e8m0
+        const uint64_t y0 = tc_desc(base), x0 = tc_desc(base + L.x);
+        const int steps_last = (P.y.cb - 128 * (nby - 1)) / 32;
+        int slot0 = 0;
+        uint32_t ph = 0;
+        bool ok = starts;
+        for (int t = 0; t < nt && ok; ++t) {
+            const int b = t & 1;
+            // (the scores of the tile before the last have been read once their weights are there)
+            ok = mbar_wait(bar(CFULL + t % MR_AHEAD), (uint32_t)(t / MR_AHEAD) & 1u, ab) && (t < 2 || mbar_wait(bar(PFULL + b), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab)) &&
+                 filled(0, yslots, slot0, ph, nby);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            tc_fence_after();
+            if (elected()) {
+                for (int a = 0; a < L.words; ++a) {
+                    scales_in(tA + (b * L.words + a) * 4, base + L.scales + (t % MR_AHEAD * L.words + a) * 512);
+                    if (t == 0) scales_in(tB + a * 4, base + L.scales + (MR_AHEAD * L.words + a) * 512);
+                }
+                const uint32_t acc = tmem + SCOLS * b;
+                int slot = slot0;
+                for (int c = 0; c < nby; ++c) {
+                    const uint64_t yd = y0 + (uint64_t)(slot * (int)(MR_SLOT >> 4)), xd = x0 + (uint64_t)(c * (ROWS * 128 >> 4));
+                    const uint32_t part = (uint32_t)(c & 3), idesc = shape | part << 29 | part << 4;
+                    const uint32_t sfa = tA + (b * L.words + c / 4) * 4, sfb = tB + (c / 4) * 4;
+                    mma_scaled(acc, yd, xd, idesc, sfa, sfb, c ? 1u : 0u);
+                    if (c < nby - 1 || steps_last == 4) {
+#pragma unroll
+                        for (int q = 1; q < 4; ++q) mma_scaled(acc, yd + 2 * q, xd + 2 * q, idesc, sfa, sfb, 1u);
+                    } else
+                        for (int q = 1; q < steps_last; ++q) mma_scaled(acc, yd + 2 * q, xd + 2 * q, idesc, sfa, sfb, 1u);
+                    if (vslots) tc_commit(bar(EMPTY + slot));
+                    if (++slot == yslots) slot = 0;
+                }
+                tc_commit(bar(SFULL + b));
+            }
+            __syncwarp();
+            slot0 += nby;
+            if (slot0 >= yslots) { slot0 -= yslots; ph ^= 1u; }
+        }
+        finish(LAST);
+    } else if (warp == 11) {
+        // ---- images
+        constexpr uint32_t shape = (1u << 4) | 1u << 15 | ((uint32_t)(2 * NQ >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);   // D fp32, A M-major
+        const uint64_t y0 = tc_desc(base), p0 = tc_desc(base + L.p);
+        const int first = vslots ? yslots : 0, slots = vslots ? vslots : yslots;
+        int slot0 = 0;
+        uint32_t ph = 0;
+        bool ok = starts;
+        for (int t = 0; t < nt && ok; ++t) {
+            const int b = t & 1;
+            // (values that are the bank are there: the weights are made of its scores.  Waited for all the same, which orders the reads.)
+            // The weights, which come last, are waited for last.
+            ok = mbar_wait(bar(DFREE + b), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab) && filled(first, slots, slot0, ph, nb) && mbar_wait(bar(PFULL + b), (uint32_t)(t >> 1) & 1u, ab);
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            tc_fence_after();
+            if (elected()) {
+                int slot = slot0;
+                for (int c = 0; c < nb; ++c) {
+                    const uint64_t vd = y0 + (uint64_t)((first + slot) * (int)(MR_SLOT >> 4)), pd = p0 + (uint64_t)((b * vblocks + c) * (2 * NQ * 128 >> 4));
+                    const uint32_t acc = tD + b * dcols + c * 2 * NQ;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) mma_codes(acc, vd + q * (4096 >> 4), pd + 2 * q, shape, q ? 1u : 0u);
+                    tc_commit(bar(EMPTY + first + slot));
+                    if (++slot == slots) slot = 0;
+                }
+                tc_commit(bar(DFULL + b));
+            }
+            __syncwarp();
+            slot0 += nb;
+            if (slot0 >= slots) { slot0 -= slots; ph ^= 1u; }
+        }
+        finish(LAST + 1);
+    } else {
+        // ---- targets' scales and terms, a lane to every 32nd target of a tile; two tiles' on their way from memory, all of a tile's loads at once
+        struct Raw {
+            double g[4];
+            float norm[4];
+            uint32_t y0[4], y1[4], v0[4], v1[4];
+        };
+        const int words_v = P.v.sb / 4, word = v0 / 4, shift = 8 * (v0 & 3);       // scales from the first block of this block's dimensions on
+        auto fetch = [&](int t, Raw &r) {
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const size_t at = (size_t)w * P.m + min((t0 + t) * MR_T + lane + 32 * a, len - 1);
+                const uint32_t *sy = reinterpret_cast<const uint32_t *>(P.y.scales + at * P.y.sb), *sv = reinterpret_cast<const uint32_t *>(P.v.scales + at * P.v.sb) + word;
+                r.g[a] = P.g ? P.g[at] : 0.0;
+                r.norm[a] = P.y.norms[at];
+                r.y0[a] = sy[0];
+                r.y1[a] = L.words > 1 ? sy[1] : 0u;
+                r.v0[a] = P.own_values ? sv[0] : 0u;
+                r.v1[a] = P.own_values && word + 1 < words_v ? sv[1] : 0u;
+            }
+        };
+        bool ok = starts;
+        auto give = [&](int t, Raw &r) {
+            const int b = t % MR_AHEAD;
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(CEMPTY + b), ((uint32_t)(t / MR_AHEAD) & 1u) ^ 1u, ab));
+            if (!ok) return;
+            uint4 *dst = reinterpret_cast<uint4 *>(smem + L.scales + b * L.words * 512) + lane;
+            dst[0] = make_uint4(r.y0[0], r.y0[1], r.y0[2], r.y0[3]);
+            if (L.words > 1) dst[32] = make_uint4(r.y1[0], r.y1[1], r.y1[2], r.y1[3]);
+            bool masked[4];
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                const int p = lane + 32 * a;
+                const float term = (t0 + t) * MR_T + p < len ? map_term(k, r.g[a], r.norm[a]) : -INFINITY;
+                masked[a] = term == -INFINITY;
+                if (P.own_values) {
+                    r.v0[a] = __funnelshift_r(r.v0[a], r.v1[a], shift);
+                    r.v1[a] >>= shift;
+                } else { r.v0[a] = r.y0[a]; r.v1[a] = r.y1[a]; }
+                terms[128 * b + p] = term;
+                vscales[128 * b + p] = make_uint2(r.v0[a], r.v1[a]);
+            }
+            // the values' largest power of two of the tile in each block (of targets that are masked or NaN: none)
+#pragma unroll
+            for (int u = 0; u < UNITS; ++u) {
+                uint32_t top = 0;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    const uint32_t e = ((u < 4 ? r.v0[a] : r.v1[a]) >> (8 * (u & 3))) & 255u;
+                    top = max(top, masked[a] || e == 255u ? 0u : e);
+                }
+                top = __reduce_max_sync(0xffffffffu, top);
+                if (lane == 0) tops[b * MR_MAX_BLOCKS + u] = top;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(CFULL + b));
+        };
+        Raw one, two;
+        if (nt > 0) fetch(0, one);
+        if (nt > 1) fetch(1, two);
+        for (int t = 0; t < nt && ok; t += 2) {
+            give(t, one);
+            if (t + 2 < nt) fetch(t + 2, one);
+            if (t + 1 >= nt || !ok) break;
+            give(t + 1, two);
+            if (t + 3 < nt) fetch(t + 3, two);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 9) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(L.columns) : "memory");
 }
 
 // The parts of a query's image, added up: a block to 128 dimensions of a query, a warp to every eighth part, in an order that does not change.
@@ -465,27 +698,61 @@ __global__ void __launch_bounds__(256) map_join_kernel(const __grid_constant__ M
     }
 }
 
-template <int NG, int UNITS>
-skb_status launch_rows(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, cudaStream_t st)
+// Slots of a block, the blocks of 128 dimensions of the values that it takes, and how many blocks an SM is to hold: two where two tiles fit in half
+// of its shared memory and the columns in half of its tensor memory, for a tile goes from one kind of work to the next.
+struct RowsShape {
+    int nq, yslots, vslots, vblocks, chunks, blocks;
+};
+template <int NQ>
+RowsShape rows_shape(int d, int dv, bool own, long long tiles)
 {
-    const int nby = (P.d + 127) / 128, per_tile = nby + (P.own_values ? (P.dv + 127) / 128 : 0);
-    // as many slots as leave room for the blocks that registers allow, a tile at least
-    cudaFuncAttributes fa;
-    if (cudaFuncGetAttributes(&fa, map_rows_kernel<NG, UNITS>) != cudaSuccess) return op_launched("map");
-    const int rest = NG * 8 * nby * 256 + 1024, room = MAP_SM_SMEM / MR_BLOCKS<NG, UNITS> - 1024 - (int)fa.sharedSizeBytes - rest;
-    const int slots = min(MR_MAX_SLOTS, max(per_tile, room / (int)MR_SLOT));
-    const int smem = slots * (int)MR_SLOT + rest;
-    cudaFuncSetAttribute(map_rows_kernel<NG, UNITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    map_rows_kernel<NG, UNITS><<<dim3(P.splits, (P.n + 8 * NG - 1) / (8 * NG), P.W), MR_THREADS, smem, st>>>(ty, tv, P, slots);
+    const int nby = (d + 127) / 128, nb = (dv + 127) / 128, most = NQ == 16 ? 4 : MR_MAX_BLOCKS;
+    RowsShape r = {};
+    r.nq = NQ;
+    // (chunks of values of their own are of four blocks, a word of scales, or whole)
+    r.vblocks = nb;
+    const auto slots = [&](int room) {
+        const MapRows L = map_rows_layout<NQ>(d, r.vblocks, 0, 0);
+        return min(MR_MAX_SLOTS, (room - (int)L.bytes) / (int)MR_SLOT);
+    };
+    if (own && slots(MAP_TILES_SMEM) < nby + nb) r.vblocks = 4;
+    if (own && slots(MAP_TILES_SMEM) < nby + r.vblocks) r.vblocks = 2;
+    if (r.vblocks > most) r.vblocks = most;
+    r.chunks = (nb + r.vblocks - 1) / r.vblocks;
+    const int per_tile = nby + (own ? r.vblocks : 0), half = slots(MAP_SM_SMEM / 2 - 1024), units = r.vblocks <= 1 ? 1 : r.vblocks <= 2 ? 2 : r.vblocks <= 4 ? 4 : 8;
+    r.blocks = NQ * units <= 8 && map_rows_layout<NQ>(d, r.vblocks, 0, 0).columns <= 256 && half >= 2 * per_tile ? 2 : 1;
+    const long long all = min((long long)(r.blocks == 2 ? half : slots(MAP_TILES_SMEM)), max(2LL, tiles) * per_tile);
+    // shares of the slots in proportion, a tile's blocks at least
+    r.vslots = own ? max(r.vblocks, min((int)all - nby, (int)(all * r.vblocks / per_tile))) : 0;
+    r.yslots = (int)all - r.vslots;
+    return r;
+}
+// (a tile's blocks have a slot each: eight queries leave room for 1024 dimensions of bank and values, sixteen do not)
+RowsShape rows_shape(int n, int d, int dv, bool own, long long tiles)
+{
+    if (n > 8 && (own || dv <= 512)) {
+        const RowsShape r = rows_shape<16>(d, dv, own, tiles);
+        if (r.yslots >= (d + 127) / 128) return r;
+    }
+    return rows_shape<8>(d, dv, own, tiles);
+}
+
+template <int NQ, int UNITS>
+skb_status launch_rows(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, const RowsShape &r, cudaStream_t st)
+{
+    const MapRows L = map_rows_layout<NQ>(P.d, r.vblocks, r.yslots, r.vslots);
+    cudaFuncSetAttribute(map_rows_kernel<NQ, UNITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.bytes);
+    map_rows_kernel<NQ, UNITS><<<dim3(P.splits, (P.n + NQ - 1) / NQ * r.chunks, P.W), MR_THREADS, L.bytes, st>>>(ty, tv, P, r.yslots, r.vslots, r.vblocks);
     return op_launched("map");
 }
-template <int NG>
 skb_status launch_rows_by_depth(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, cudaStream_t st)
 {
-    if (P.dv <= 128) return launch_rows<NG, 1>(ty, tv, P, st);
-    if (P.dv <= 256) return launch_rows<NG, 2>(ty, tv, P, st);
-    if (P.dv <= 512) return launch_rows<NG, 4>(ty, tv, P, st);
-    return launch_rows<NG, 8>(ty, tv, P, st);
+    const RowsShape r = rows_shape(P.n, P.d, P.dv, P.own_values != 0, ((P.m + MR_T - 1) / MR_T + P.splits - 1) / P.splits);
+    const bool few = r.nq == 8;
+    if (r.vblocks <= 1) return few ? launch_rows<8, 1>(ty, tv, P, r, st) : launch_rows<16, 1>(ty, tv, P, r, st);
+    if (r.vblocks <= 2) return few ? launch_rows<8, 2>(ty, tv, P, r, st) : launch_rows<16, 2>(ty, tv, P, r, st);
+    if (r.vblocks <= 4) return few ? launch_rows<8, 4>(ty, tv, P, r, st) : launch_rows<16, 4>(ty, tv, P, r, st);
+    return launch_rows<8, 8>(ty, tv, P, r, st);
 }
 
 // queries up to which the matrix unit's tiles of 128 are too empty
@@ -503,18 +770,14 @@ struct MapPlan {
     bool tiles;
     int splits;
 };
-int rows_blocks(int n, int dv)
-{
-    const int units = dv <= 128 ? 1 : dv <= 256 ? 2 : dv <= 512 ? 4 : 8, work = (n <= 8 ? 1 : 2) * units;
-    return work <= 4 ? 4 : work <= 8 ? 3 : 2;                     // MR_BLOCKS
-}
-MapPlan map_plan(int W, int n, int m, int d, int dv, int sms)
+MapPlan map_plan(int W, int n, int m, int d, int dv, bool own_values, int sms)
 {
     MapPlan p;
+    const RowsShape rows = rows_shape(n, d, dv, own_values, 1 << 20);
     p.tiles = n > MAP_ROWS_MAX && d <= MAP_TILES_MAX_D;
-    const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * (n <= 8 ? 1 : (n + 15) / 16);
+    const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * ((n + rows.nq - 1) / rows.nq) * rows.chunks;
     const long long tiles = p.tiles ? (m + 127) / 128 : (m + MR_T - 1) / MR_T;
-    long long s = p.tiles ? sms / blocks : (long long)rows_blocks(n, dv) * sms / blocks;
+    long long s = (p.tiles ? 1LL : rows.blocks) * sms / blocks;
     if (s > tiles / 2) s = tiles / 2;
     p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
     return p;
@@ -534,7 +797,7 @@ using namespace skb;
 static size_t map_workspace(int W, int n, int m, int d, int dv, bool own_values)
 {
     // (what any device may split into: the workspace does not depend on the current one)
-    const MapPlan p = map_plan(W, n, m, d, dv, MAP_MAX_SMS);
+    const MapPlan p = map_plan(W, n, m, d, dv, own_values, MAP_MAX_SMS);
     return 256 + map_parts_bytes(W, n, dv, p.splits) + (p.tiles ? pad256(map_staged_bytes(W, m, d, dv, own_values)) : 0);
 }
 
@@ -564,7 +827,7 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     P.v = v ? cloud8_view(v, (size_t)W * m, dv) : P.y;
     P.g = g; P.eps = eps; P.lengths = lengths; P.out = (uint16_t *)out; P.lse = lse;
     P.W = W; P.n = n; P.m = m; P.d = d; P.dv = depth; P.own_values = v != nullptr;
-    const MapPlan plan = map_plan(W, n, m, d, depth, sms < MAP_MAX_SMS ? sms : MAP_MAX_SMS);
+    const MapPlan plan = map_plan(W, n, m, d, depth, v != nullptr, sms < MAP_MAX_SMS ? sms : MAP_MAX_SMS);
     P.splits = plan.splits;
     P.part_ml = (float *)workspace;
     P.part_out = (float *)((char *)workspace + pad256((size_t)W * n * P.splits * 8));
@@ -572,7 +835,7 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     CUtensorMap ty, tv;
     if (!plan.tiles && (!points_map(&ty, P.y.codes, P.y.cb, m, W, MR_T) || !points_map(&tv, P.v.codes, P.v.cb, m, W, MR_T)))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, sms, (cudaStream_t)stream) : n <= 8 ? launch_rows_by_depth<1>(ty, tv, P, (cudaStream_t)stream) : launch_rows_by_depth<2>(ty, tv, P, (cudaStream_t)stream);
+    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, sms, (cudaStream_t)stream) : launch_rows_by_depth(ty, tv, P, (cudaStream_t)stream);
     if (rc != SKB_OK || P.splits == 1) return rc;
     // (it may start, and wait, before the parts are all there)
     cudaLaunchConfig_t cfg = {};
