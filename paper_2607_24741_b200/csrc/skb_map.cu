@@ -14,7 +14,7 @@
 //            2^-22 of the tile's largest is lost), rows of their own again
 // so that nothing of a code passes through a register.  The same work by mma.sync, codes made f16 in registers, was bound by its instructions: one query
 // to each of 8 banks of 16384 x 512 took 35 us.
-//   warps 0-3   softmax
+//   warps 0-3   softmax, and 12-15 where registers allow: every other tile each
 //   warps 4-7   images: tensor memory -> fp32 sums in registers, a thread to a dimension of every 128
 //   warp 8      loads by TMA: slots of 128 targets by 128 dimensions (16 KB, 128-byte swizzle, targets past the end are zeros)
 //   warp 9      scores' matrix instructions, warp 11 the images': either waits for what it needs
@@ -33,9 +33,9 @@
 namespace skb {
 namespace {
 
-constexpr int MR_THREADS = 12 * 32, MR_T = 128;               // points of a tile
+constexpr int MR_T = 128;                                     // points of a tile
 constexpr uint32_t MR_SLOT = MR_T * 128;
-constexpr int MR_MAX_SLOTS = 16, MR_MAX_BLOCKS = 8, MR_AHEAD = 4;     // MR_AHEAD: tiles whose scales and terms are there at once
+constexpr int MR_MAX_SLOTS = 16, MR_MAX_BLOCKS = 8, MR_AHEAD = 6;     // MR_AHEAD: tiles whose scales and terms are there at once
 // rows of the queries' operand: three numbers of each query, and how many rows the instruction takes
 template <int NQ> constexpr int MR_ROWS = NQ == 8 ? 32 : 48;
 template <int NQ> constexpr int MR_SCOLS = NQ == 8 ? 32 : 64;  // columns of tensor memory that its result takes
@@ -92,12 +92,16 @@ __device__ __forceinline__ bool elected()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r != 0;
 }
-// whether all 128 threads of the softmax say so
-__device__ __forceinline__ bool all_softmax(bool ok)
+// warps of the softmax: two groups of four that take turns, where registers allow
+template <int NQ, int UNITS> constexpr int MR_GROUPS = NQ * UNITS <= 32 ? 2 : 1;
+template <int NQ, int UNITS> constexpr int MR_THREADS = (8 + 4 * MR_GROUPS<NQ, UNITS>) * 32;
+
+// whether all 128 threads of a group of the softmax say so
+__device__ __forceinline__ bool all_softmax(bool ok, int barrier)
 {
     uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                 : "=r"(r) : "r"((uint32_t)ok) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)ok), "r"(barrier) : "memory");
     return r != 0;
 }
 
@@ -123,7 +127,7 @@ __host__ __device__ inline MapRows map_rows_layout(int d, int nb, int yslots, in
     L.scales = L.p + 2 * (uint32_t)(L.nb * 2 * NQ) * 128;
     L.small = L.scales + (MR_AHEAD + 1) * (uint32_t)L.words * 512;
     // terms, values' scales, tops, maxima, sums, lengths, barriers
-    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4) + 2 * 4 * NQ * 4 + 4 * NQ * 4 + NQ * 4 + NQ * 8 + 64 * 8 + 16;
+    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4 + 4 * NQ * 4) + 2 * 4 * NQ * 4 + 2 * NQ * 4 + NQ * 8 + 64 * 8 + 16;
     const uint32_t used = 2 * MR_SCOLS<NQ> + 2 * (uint32_t)(L.nb * 2 * NQ) + 12 * (uint32_t)L.words;
     L.columns = 32;
     while (L.columns < used) L.columns *= 2;
@@ -131,10 +135,10 @@ __host__ __device__ inline MapRows map_rows_layout(int d, int nb, int yslots, in
 }
 
 template <int NQ, int UNITS>
-__global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_kernel(const __grid_constant__ CUtensorMap tmy, const __grid_constant__ CUtensorMap tmv,
+__global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const __grid_constant__ CUtensorMap tmy, const __grid_constant__ CUtensorMap tmv,
                                                               const __grid_constant__ Map P, const int yslots, const int vslots, const int vblocks)
 {
-    constexpr int ROWS = MR_ROWS<NQ>, SCOLS = MR_SCOLS<NQ>;
+    constexpr int ROWS = MR_ROWS<NQ>, SCOLS = MR_SCOLS<NQ>, GROUPS = MR_GROUPS<NQ, UNITS>;
     extern __shared__ __align__(1024) unsigned char smem[];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");               // (the parts' join waits for all of this grid's writes itself)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -146,30 +150,31 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
     const uint32_t base = smem_u32(smem);
     float *terms = reinterpret_cast<float *>(smem + L.small);                        // [MR_AHEAD][128]
     uint2 *vscales = reinterpret_cast<uint2 *>(terms + MR_AHEAD * 128);              // [MR_AHEAD][128]
-    float *maxima = reinterpret_cast<float *>(vscales + MR_AHEAD * 128);             // [2][4][NQ]
-    uint32_t *tops = reinterpret_cast<uint32_t *>(maxima + 8 * NQ);                  // [MR_AHEAD][8]
-    float *sums = reinterpret_cast<float *>(tops + MR_AHEAD * MR_MAX_BLOCKS);                                                  // [4][NQ]
-    float *runs = sums + 4 * NQ;                                                     // [NQ]
-    double *lengths2 = reinterpret_cast<double *>(runs + NQ);                        // [NQ]
+    float *maxima = reinterpret_cast<float *>(vscales + MR_AHEAD * 128);             // [MR_AHEAD][4][NQ]
+    uint32_t *tops = reinterpret_cast<uint32_t *>(maxima + MR_AHEAD * 4 * NQ);                  // [MR_AHEAD][8]
+    float *sums = reinterpret_cast<float *>(tops + MR_AHEAD * MR_MAX_BLOCKS);                                                  // [2][4][NQ]
+    float *runs = sums + 8 * NQ;                                                     // [2][NQ]
+    double *lengths2 = reinterpret_cast<double *>(runs + 2 * NQ);                        // [NQ]
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(lengths2 + NQ);
     uint32_t *holder = reinterpret_cast<uint32_t *>(bars + 64);
     int *abort_flag = reinterpret_cast<int *>(holder + 1);
     volatile int *ab = abort_flag;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     constexpr int FULL = 0, EMPTY = MR_MAX_SLOTS, CFULL = 2 * MR_MAX_SLOTS, CEMPTY = CFULL + MR_AHEAD, SFULL = CEMPTY + MR_AHEAD, PFULL = SFULL + 2, DFULL = PFULL + 2,
-                  DFREE = DFULL + 2, LAST = DFREE + 2;
+                  DFREE = DFULL + 2, SFREE = DFREE + 2, MFULL = SFREE + 2, LAST = MFULL + MR_AHEAD;
     static_assert(LAST + 1 < 64, "barriers");
 
     const int len = map_length(P, w), tiles = (len + MR_T - 1) / MR_T;
     const int t0 = (int)((long long)tiles * split / P.splits), nt = (int)((long long)tiles * (split + 1) / P.splits) - t0;
     if (tid == 0) {
         for (int s = 0; s < yslots + vslots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(EMPTY + s), 1); }
-        for (int c = 0; c < MR_AHEAD; ++c) { mbar_init(bar(CFULL + c), 1); mbar_init(bar(CEMPTY + c), 8); }
+        for (int c = 0; c < MR_AHEAD; ++c) { mbar_init(bar(CFULL + c), 1); mbar_init(bar(CEMPTY + c), 8); mbar_init(bar(MFULL + c), 4); }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar(SFULL + b), 1);
             mbar_init(bar(PFULL + b), 4);
             mbar_init(bar(DFULL + b), 1);
             mbar_init(bar(DFREE + b), 4);
+            mbar_init(bar(SFREE + b), 4);
         }
         mbar_init(bar(LAST), 1);
         mbar_init(bar(LAST + 1), 1);
@@ -271,6 +276,17 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
         }
         return true;
     };
+    // a query's largest exponent and the sum against it, of all groups
+    auto total_of = [&](int q, float &top) {
+        const float one = (sums[q] + sums[NQ + q]) + (sums[2 * NQ + q] + sums[3 * NQ + q]);
+        top = runs[q];
+        if constexpr (GROUPS == 1) return one;
+        const float *more = sums + 4 * NQ;
+        const float other = runs[NQ + q], two = (more[q] + more[NQ + q]) + (more[2 * NQ + q] + more[3 * NQ + q]);
+        top = fmaxf(top, other);
+        const float ref = top == -INFINITY ? 0.f : top;
+        return one * ex2f(runs[q] - ref) + two * ex2f(other - ref);
+    };
     // what a warp has issued is over before tensor memory is given back
     auto finish = [&](int barrier) {
         if (elected()) {
@@ -281,23 +297,24 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
         __syncwarp();
     };
 
-    if (warp < 4) {
+    if (warp < 4 || warp >= 12) {
         // ---- softmax: a thread to a target, which is a lane of tensor memory
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const int group = warp >> 3, part = warp & 3, p = part * 32 + lane;          // every other tile's
+        const uint32_t lanes = (uint32_t)(part * 32) << 16;
         const float kx = (float)(2.0 * k);
         float run[NQ], sum[NQ];
 #pragma unroll
         for (int q = 0; q < NQ; ++q) { run[q] = -INFINITY; sum[q] = 0.f; }
         bool ok = starts;
-        for (int t = 0; t < nt && starts; ++t) {
+        for (int t = group; t < nt && starts; t += GROUPS) {
             const int b = t & 1;
             const uint32_t ph = (uint32_t)(t >> 1) & 1u;
             const int c4 = t % MR_AHEAD;
-            ok = ok && mbar_wait(bar(CFULL + c4), (uint32_t)(t / MR_AHEAD) & 1u, ab) && mbar_wait(bar(SFULL + b), ph, ab) && mbar_wait(bar(DFREE + b), ph ^ 1u, ab);
+            ok = ok && mbar_wait(bar(CFULL + c4), (uint32_t)(t / MR_AHEAD) & 1u, ab) && mbar_wait(bar(SFULL + b), ph, ab);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
-            const float term = terms[128 * c4 + tid];
-            const uint2 sv = vscales[128 * c4 + tid];
+            const float term = terms[128 * c4 + p];
+            const uint2 sv = vscales[128 * c4 + p];
             const bool masked = term == -INFINITY;
             // 256 times the values' powers of two, less the tile's largest (0: below fp32's), or NaN; masked targets have weights of zero
             float scale[UNITS];
@@ -330,17 +347,22 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
             for (int q = 0; q < NQ; q += 4)
                 if (q < nq) {
                     const float4 m = make_float4(warp_max(arg[q]), warp_max(arg[q + 1]), warp_max(arg[q + 2]), warp_max(arg[q + 3]));
-                    if (lane == 0) *reinterpret_cast<float4 *>(maxima + (4 * b + warp) * NQ + q) = m;
+                    if (lane == 0) *reinterpret_cast<float4 *>(maxima + (4 * c4 + part) * NQ + q) = m;
                 }
-            ok = all_softmax(ok);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(SFREE + b));                               // (the scores are in registers)
+            // the weights of the tile before the last have been used; of the maxima there are as many as tiles ahead
+            ok = ok && mbar_wait(bar(DFULL + b), ph ^ 1u, ab);
+            ok = all_softmax(ok, group ? 4 : 1);
             if (!ok) break;
-            unsigned char *weights = smem + L.p + b * (vblocks * 2 * NQ) * 128 + (tid & 15);
+            unsigned char *weights = smem + L.p + b * (vblocks * 2 * NQ) * 128 + (p & 15);
 #pragma unroll
             for (int q = 0; q < NQ; q += 4) {
                 if (q >= nq) break;
-                float top[4], p[4];
+                float top[4], e[4];
                 {
-                    const float4 *mp = reinterpret_cast<const float4 *>(maxima + 4 * b * NQ + q);
+                    const float4 *mp = reinterpret_cast<const float4 *>(maxima + 4 * c4 * NQ + q);
                     const float4 m0 = mp[0], m1 = mp[NQ / 4], m2 = mp[NQ / 2], m3 = mp[3 * NQ / 4];
                     top[0] = fmaxf(fmaxf(m0.x, m1.x), fmaxf(m2.x, m3.x));
                     top[1] = fmaxf(fmaxf(m0.y, m1.y), fmaxf(m2.y, m3.y));
@@ -350,22 +372,21 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
                     // (tile's maximum plus infinity: the exponential is NaN, and so is what follows from it)
-                    p[h] = ex2f(arg[q + h] - (top[h] == -INFINITY ? 0.f : top[h]));
+                    e[h] = ex2f(arg[q + h] - (top[h] == -INFINITY ? 0.f : top[h]));
                     const float now = fmaxf(run[q + h], top[h]), ref = now == -INFINITY ? 0.f : now;
-                    sum[q + h] = fmaf(sum[q + h], ex2f(run[q + h] - ref), p[h] * ex2f(top[h] - ref));
+                    sum[q + h] = fmaf(sum[q + h], ex2f(run[q + h] - ref), e[h] * ex2f(top[h] - ref));
                     run[q + h] = now;
-                    if (masked) p[h] = 0.f;
-                }
+                                    }
 #pragma unroll
                 for (int u = 0; u < UNITS; ++u) {
                     if (u >= nb) break;
-                    const float a0 = masked ? 0.f : p[0] * scale[u], a1 = masked ? 0.f : p[1] * scale[u], a2 = masked ? 0.f : p[2] * scale[u],
-                                a3 = masked ? 0.f : p[3] * scale[u];
+                    const float a0 = masked ? 0.f : e[0] * scale[u], a1 = masked ? 0.f : e[1] * scale[u], a2 = masked ? 0.f : e[2] * scale[u],
+                                a3 = masked ? 0.f : e[3] * scale[u];
                     const uint32_t lo = e4m3_two(a0, a1), hi = e4m3_two(a2, a3);
                     const float2 bl = e4m3_pair(lo), bh = e4m3_pair(hi);
                     const uint32_t lo2 = e4m3_two((a0 - bl.x) * 16.f, (a1 - bl.y) * 16.f), hi2 = e4m3_two((a2 - bh.x) * 16.f, (a3 - bh.y) * 16.f);
                     unsigned char *block = weights + u * (2 * NQ) * 128;
-                    auto put = [&](int r, uint32_t byte) { block[r * 128 + (((tid >> 4) ^ (r & 7)) << 4)] = (unsigned char)byte; };
+                    auto put = [&](int r, uint32_t byte) { block[r * 128 + (((p >> 4) ^ (r & 7)) << 4)] = (unsigned char)byte; };
                     put(q, lo); put(q + 1, lo >> 8); put(q + 2, hi); put(q + 3, hi >> 8);
                     put(NQ + q, lo2); put(NQ + q + 1, lo2 >> 8); put(NQ + q + 2, hi2); put(NQ + q + 3, hi2 >> 8);
                 }
@@ -373,23 +394,25 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) { mbar_arrive(bar(PFULL + b)); mbar_arrive(bar(CEMPTY + c4)); }
+            if (lane == 0) { mbar_arrive(bar(PFULL + b)); mbar_arrive(bar(MFULL + c4)); mbar_arrive(bar(CEMPTY + c4)); }
         }
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
+            if (q >= nq) break;
             float s = ok ? sum[q] : __uint_as_float(0x7fffffffu);
 #pragma unroll
             for (int off = 16; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
-            if (lane == 0) sums[warp * NQ + q] = s;
-            if (tid == 0) runs[q] = run[q];
+            if (lane == 0) sums[(4 * group + part) * NQ + q] = s;
+            if (p == 0) runs[group * NQ + q] = run[q];
         }
-        asm volatile("bar.sync 2, 256;" ::: "memory");
+        asm volatile("bar.sync 2, %0;" ::"n"(128 + 128 * GROUPS) : "memory");
         if (tid < nq) {
             const size_t r = (size_t)w * P.n + q0 + tid;
-            const float total = (sums[tid] + sums[NQ + tid]) + (sums[2 * NQ + tid] + sums[3 * NQ + tid]);
+            float top;
+            const float total = total_of(tid, top);
             if (z) {}                                                               // (the first block of a query has them)
-            else if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[r * P.splits + split] = make_float2(runs[tid], total);
-            else if (P.lse) P.lse[r] = map_lse(runs[tid], total, k, lengths2[tid]);
+            else if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[r * P.splits + split] = make_float2(top, total);
+            else if (P.lse) P.lse[r] = map_lse(top, total, k, lengths2[tid]);
         }
     } else if (warp < 8) {
         // ---- images: a thread to a dimension of every block
@@ -405,7 +428,9 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
         for (int t = 0; t < nt && ok; ++t) {
             const int b = t & 1;
             const uint32_t ph = (uint32_t)(t >> 1) & 1u;
-            ok = mbar_wait(bar(PFULL + b), ph, ab) && mbar_wait(bar(DFULL + b), ph, ab);
+            // (the maxima by a barrier of their own, of which there are as many as tiles ahead: that of the weights may be a phase further by now, and a wait
+            // for a phase that is followed by another complete one is over only with the one after that)
+            ok = mbar_wait(bar(MFULL + t % MR_AHEAD), (uint32_t)(t / MR_AHEAD) & 1u, ab) && mbar_wait(bar(DFULL + b), ph, ab);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
@@ -413,7 +438,7 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
             float before[NQ], of_tile[NQ];
 #pragma unroll
             for (int q = 0; q < NQ; ++q) {
-                const float *mp = maxima + 4 * b * NQ + q;
+                const float *mp = maxima + 4 * (t % MR_AHEAD) * NQ + q;
                 const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run[q], top), ref = now == -INFINITY ? 0.f : now;
                 before[q] = ex2f(run[q] - ref);
                 of_tile[q] = ex2f(top - ref) * 0.00390625f;
@@ -441,13 +466,18 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
             __syncwarp();
             if (lane == 0) { mbar_arrive(bar(DFREE + b)); mbar_arrive(bar(CEMPTY + t % MR_AHEAD)); }
         }
-        asm volatile("bar.sync 2, 256;" ::: "memory");
+        asm volatile("bar.sync 2, %0;" ::"n"(128 + 128 * GROUPS) : "memory");
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             if (q >= nq) break;
             const size_t r = (size_t)w * P.n + q0 + q;
-            const float total = (sums[q] + sums[NQ + q]) + (sums[2 * NQ + q] + sums[3 * NQ + q]);
-            const float inv = !ok ? __uint_as_float(0x7fffffffu) : P.splits > 1 ? (total == total ? 1.f : total) : total == 0.f ? 0.f : 1.f / total;
+            // (of parts, the join divides)
+            float inv = 1.f, top;
+            if (P.splits == 1) {
+                const float total = total_of(q, top);
+                inv = total == 0.f ? 0.f : 1.f / total;
+            }
+            if (!ok) inv = __uint_as_float(0x7fffffffu);
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
                 const int dim = 128 * (v0 + u) + tid - 128;
@@ -502,8 +532,7 @@ __global__ void __launch_bounds__(MR_THREADS, NQ * UNITS <= 8 ? 2 : 1) map_rows_
         bool ok = starts;
         for (int t = 0; t < nt && ok; ++t) {
             const int b = t & 1;
-            // (the scores of the tile before the last have been read once their weights are there)
-            ok = mbar_wait(bar(CFULL + t % MR_AHEAD), (uint32_t)(t / MR_AHEAD) & 1u, ab) && (t < 2 || mbar_wait(bar(PFULL + b), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab)) &&
+            ok = mbar_wait(bar(CFULL + t % MR_AHEAD), (uint32_t)(t / MR_AHEAD) & 1u, ab) && mbar_wait(bar(SFREE + b), ((uint32_t)(t >> 1) & 1u) ^ 1u, ab) &&
                  filled(0, yslots, slot0, ph, nby);
             if (!(ok = __all_sync(0xffffffffu, ok))) break;
             tc_fence_after();
@@ -698,10 +727,9 @@ __global__ void __launch_bounds__(256) map_join_kernel(const __grid_constant__ M
     }
 }
 
-// Slots of a block, the blocks of 128 dimensions of the values that it takes, and how many blocks an SM is to hold: two where two tiles fit in half
-// of its shared memory and the columns in half of its tensor memory, for a tile goes from one kind of work to the next.
+// Slots of a block, and the blocks of 128 dimensions of the values that it takes.
 struct RowsShape {
-    int nq, yslots, vslots, vblocks, chunks, blocks;
+    int nq, yslots, vslots, vblocks, chunks;
 };
 template <int NQ>
 RowsShape rows_shape(int d, int dv, bool own, long long tiles)
@@ -719,9 +747,8 @@ RowsShape rows_shape(int d, int dv, bool own, long long tiles)
     if (own && slots(MAP_TILES_SMEM) < nby + r.vblocks) r.vblocks = 2;
     if (r.vblocks > most) r.vblocks = most;
     r.chunks = (nb + r.vblocks - 1) / r.vblocks;
-    const int per_tile = nby + (own ? r.vblocks : 0), half = slots(MAP_SM_SMEM / 2 - 1024), units = r.vblocks <= 1 ? 1 : r.vblocks <= 2 ? 2 : r.vblocks <= 4 ? 4 : 8;
-    r.blocks = NQ * units <= 8 && map_rows_layout<NQ>(d, r.vblocks, 0, 0).columns <= 256 && half >= 2 * per_tile ? 2 : 1;
-    const long long all = min((long long)(r.blocks == 2 ? half : slots(MAP_TILES_SMEM)), max(2LL, tiles) * per_tile);
+    const int per_tile = nby + (own ? r.vblocks : 0);
+    const long long all = min((long long)slots(MAP_TILES_SMEM), max(2LL, tiles) * per_tile);
     // shares of the slots in proportion, a tile's blocks at least
     r.vslots = own ? max(r.vblocks, min((int)all - nby, (int)(all * r.vblocks / per_tile))) : 0;
     r.yslots = (int)all - r.vslots;
@@ -742,7 +769,7 @@ skb_status launch_rows(const CUtensorMap &ty, const CUtensorMap &tv, const Map &
 {
     const MapRows L = map_rows_layout<NQ>(P.d, r.vblocks, r.yslots, r.vslots);
     cudaFuncSetAttribute(map_rows_kernel<NQ, UNITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.bytes);
-    map_rows_kernel<NQ, UNITS><<<dim3(P.splits, (P.n + NQ - 1) / NQ * r.chunks, P.W), MR_THREADS, L.bytes, st>>>(ty, tv, P, r.yslots, r.vslots, r.vblocks);
+    map_rows_kernel<NQ, UNITS><<<dim3(P.splits, (P.n + NQ - 1) / NQ * r.chunks, P.W), MR_THREADS<NQ, UNITS>, L.bytes, st>>>(ty, tv, P, r.yslots, r.vslots, r.vblocks);
     return op_launched("map");
 }
 skb_status launch_rows_by_depth(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, cudaStream_t st)
@@ -777,7 +804,7 @@ MapPlan map_plan(int W, int n, int m, int d, int dv, bool own_values, int sms)
     p.tiles = n > MAP_ROWS_MAX && d <= MAP_TILES_MAX_D;
     const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * ((n + rows.nq - 1) / rows.nq) * rows.chunks;
     const long long tiles = p.tiles ? (m + 127) / 128 : (m + MR_T - 1) / MR_T;
-    long long s = (p.tiles ? 1LL : rows.blocks) * sms / blocks;
+    long long s = sms / blocks;
     if (s > tiles / 2) s = tiles / 2;
     p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
     return p;

@@ -211,6 +211,22 @@ def test_results_do_not_change_from_call_to_call_stream_graph_and_offset(B, n):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(8, 1, 6000, 512, 0), (32, 12, 4000, 128, 64), (40, 16, 900, 300, 0), (5, 3, 9000, 1024, 0), (6, 9, 3000, 600, 700), (3, 700, 1500, 512, 0), (9, 100, 2000, 96, 40)])
+def test_calls_one_after_the_other_without_a_wait(B, shape):
+    # roles of a block that get out of step would show as images that differ, or as NaN where a wait ran out
+    import torch
+    W, n, m, d, dv = shape
+    x, y, g, eps, v = inputs(*shape)
+    y8, v8 = B.cloud8_pack(y.cuda()), None if v is None else B.cloud8_pack(v.cuda())
+    x, g, eps = x.cuda(), g.cuda(), eps.cuda()
+    want, wl = B.cloud8_map(x, y8, g, eps, v8, lse=True)
+    outs = [B.cloud8_map(x, y8, g, eps, v8, lse=True) for _ in range(40)]
+    assert not torch.isnan(want).any()
+    for out, lse in outs:
+        assert torch.equal(out, want) and torch.equal(lse, wl)
+
+
+@pytest.mark.gpu
 def test_images_of_a_solved_plan(B):
     # 8-bit clouds, solved, then the images of the source points against the plan applied to the targets
     import torch
