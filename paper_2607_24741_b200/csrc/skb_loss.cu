@@ -108,21 +108,22 @@ __device__ __forceinline__ Part join(Part a, Part b, float c)
     return {m, a.s * ex2f((a.m - at) * c) + b.s * ex2f((b.m - at) * c)};
 }
 
-// TPR threads of each of C blocks to a row, V vectors in each thread's registers; V = 0: the row is read twice.
-template <bool BF16, int TPR, int V, int C>
-__global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) loss_kernel(const __grid_constant__ Loss P)
+// TPR threads of each of C blocks to a row, V vectors in each thread's registers; V = 0: the row is read twice.  EVEN: rows and gradients are whole vectors.
+template <bool BF16, int TPR, int V, int C, bool EVEN>
+__global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) loss_kernel(const __grid_constant__ Loss P)
 {
-    constexpr int THREADS = TPR <= 128 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR / 32;
+    constexpr int THREADS = TPR <= 256 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR / 32, AHEAD = 2;
     constexpr int E = BF16 ? 8 : 4;
     using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
-    __shared__ int s_index[GROUPS][LS_MAX_K];
-    __shared__ float s_q[GROUPS][LS_MAX_K], s_log[GROUPS][LS_MAX_K], s_score[GROUPS][LS_MAX_K];
+    extern __shared__ float s_entries[];                          // [GROUPS][4][k]: index, q, log q, score
     __shared__ float s_total[GROUPS];
     __shared__ Part s_part[GROUPS][WARPS], s_rank[C];
     const int tid = threadIdx.x, group = tid / TPR, t = tid % TPR, lane = tid & 31, warp = t >> 5;
     const int rank = C > 1 ? (int)(blockIdx.x % C) : 0;
     const long long row = (long long)(blockIdx.x / C) * GROUPS + group;
     if (row >= P.rows) return;                                   // whole groups: barriers below are a group's
+    int *s_index = reinterpret_cast<int *>(s_entries) + (size_t)group * 4 * P.k;
+    float *s_q = reinterpret_cast<float *>(s_index) + P.k, *s_log = s_q + P.k, *s_score = s_log + P.k;
     auto group_sync = [&] {
         if constexpr (TPR == 32) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
@@ -130,11 +131,11 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
     // (a block's shared memory may be written by another of its cluster once it has started)
     if constexpr (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     const T *src = (const T *)P.scores + (size_t)row * P.ld;
-    const int head = (int)((uintptr_t)src % 16 / sizeof(T)), end = head + P.m;      // the row, in elements from a 16-byte boundary on
+    const int head = EVEN ? 0 : (int)((uintptr_t)src % 16 / sizeof(T)), end = head + P.m;      // the row, in elements from a 16-byte boundary on
     const T *base = src - head;
     const int nvec = (end + E - 1) / E;
     auto load = [&](int j) {
-        if (j * E >= head && (j + 1) * E <= end) return *reinterpret_cast<const uint4 *>(base + (size_t)j * E);
+        if (EVEN || (j * E >= head && (j + 1) * E <= end)) return *reinterpret_cast<const uint4 *>(base + (size_t)j * E);
         uint4 r = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
                        : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
         uint32_t w[4] = {r.x, r.y, r.z, r.w};
@@ -148,15 +149,17 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
     };
-    // the first entries are on their way while the row is: what follows from them waits for neither
-    constexpr int AHEAD = 2;
-    int named_ahead[AHEAD];
-    float logit_ahead[AHEAD];
+    auto score_at = [&](int j) { return BF16 ? __uint_as_float((uint32_t)src[j] << 16) : __uint_as_float((uint32_t)src[j]); };
+    // the first entries are on their way before the row is
+    int named[AHEAD];
+    float logit[AHEAD], score[AHEAD];
+    if (warp == 0) {
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-        const int k = 32 * a + lane;
-        named_ahead[a] = warp == 0 && k < P.k ? P.index[(size_t)row * P.k + k] : -1;
-        logit_ahead[a] = warp == 0 && k < P.k && P.logits ? P.logits[(size_t)row * P.k + k] : 0.f;
+        for (int a = 0; a < AHEAD; ++a) {
+            const int k = 32 * a + lane;
+            named[a] = k < P.k ? P.index[(size_t)row * P.k + k] : -1;
+            logit[a] = k < P.k && P.logits ? P.logits[(size_t)row * P.k + k] : 0.f;
+        }
     }
     uint4 held[V ? V : 1];
     if constexpr (V > 0) {
@@ -167,6 +170,43 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
                            : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
             if (j < nvec) held[v] = load(j);
         }
+    }
+    // the teacher: the first warp's, while the row is on its way; so are the scores that it names
+    if (warp == 0) {
+        float top = -INFINITY, total = 0.f;
+        auto entry = [&](int k, int j, float l) {
+            const bool there = j >= 0 && j < P.m;
+            l = there ? l * P.inv_t : -INFINITY;
+            s_index[k] = there ? j : -1;
+            s_log[k] = l;
+            top = fmaxf(top, l);
+            return there;
+        };
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            score[a] = 0.f;
+            if (32 * a + lane < P.k && entry(32 * a + lane, named[a], logit[a])) score[a] = score_at(named[a]);
+        }
+        for (int k = 32 * AHEAD + lane; k < P.k; k += 32) {
+            const int j = P.index[(size_t)row * P.k + k];
+            s_score[k] = entry(k, j, P.logits ? P.logits[(size_t)row * P.k + k] : 0.f) ? score_at(j) : 0.f;
+        }
+        const float at = finite_max(warp_max(top));
+        // (a thread reads back what it wrote)
+        for (int k = lane; k < P.k; k += 32) {
+            const float l = s_log[k] - at, e = ex2f(l * 1.44269504f);
+            s_log[k] = l;
+            s_q[k] = e;
+            total += e;
+        }
+#pragma unroll
+        for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
+        const float log_total = logf(total), inv = total == 0.f ? 0.f : 1.f / total;
+        for (int k = lane; k < P.k; k += 32) {
+            s_log[k] -= log_total;
+            s_q[k] *= inv;
+        }
+        if (lane == 0) s_total[group] = total;
     }
     // maximum and sum of what this thread has seen
     constexpr bool KEEP = V > 0 && (!BF16 || V <= 4);            // exponentials stay in registers
@@ -203,35 +243,10 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
             part = join(part, one, P.c);
         }
     }
-    // the teacher: the first warp's; the scores that it names are in the first-level cache by now
-    if (warp == 0) {
-        float top = -INFINITY, total = 0.f;
-        auto entry = [&](int k, int j, float logit) {
-            const bool named = j >= 0 && j < P.m;
-            const float l = named ? logit * P.inv_t : -INFINITY;
-            s_index[group][k] = named ? j : -1;
-            s_score[group][k] = !named ? 0.f : BF16 ? __uint_as_float((uint32_t)src[j] << 16) : __uint_as_float((uint32_t)src[j]);
-            s_log[group][k] = l;
-            top = fmaxf(top, l);
-        };
+    if (warp == 0)
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a)
-            if (32 * a + lane < P.k) entry(32 * a + lane, named_ahead[a], logit_ahead[a]);
-        for (int k = 32 * AHEAD + lane; k < P.k; k += 32)
-            entry(k, P.index[(size_t)row * P.k + k], P.logits ? P.logits[(size_t)row * P.k + k] : 0.f);
-        const float at = finite_max(warp_max(top));
-        // (a thread reads back what it wrote)
-        for (int k = lane; k < P.k; k += 32) total += expf(s_log[group][k] - at);
-#pragma unroll
-        for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
-        const float log_total = logf(total);
-        for (int k = lane; k < P.k; k += 32) {
-            const float l = s_log[group][k] - at;
-            s_log[group][k] = l - log_total;
-            s_q[group][k] = total == 0.f ? 0.f : expf(l) / total;
-        }
-        if (lane == 0) s_total[group] = total;
-    }
+            if (32 * a + lane < P.k) s_score[32 * a + lane] = score[a];
     const float own = part.m;
     part = join<32>(part, P.c);
     if constexpr (WARPS > 1) {
@@ -259,8 +274,8 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
         const float log_sum = logf(part.s);
         float sum = 0.f;
         for (int k = lane; k < P.k; k += 32) {
-            const float q = s_q[group][k];
-            if (q != 0.f) sum += q * (s_log[group][k] - ((s_score[group][k] - part.m) * P.inv_t - log_sum));
+            const float q = s_q[k];
+            if (q != 0.f) sum += q * (s_log[k] - ((s_score[k] - part.m) * P.inv_t - log_sum));
         }
 #pragma unroll
         for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
@@ -269,7 +284,7 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
     if (!P.grad) return;
     const float w = (P.weight ? P.weight[row] : 1.f) * P.inv_t, a = w / part.s;
     T *out = (T *)P.grad + (size_t)row * P.ldg - head;
-    const bool wide = (uintptr_t)out % 16 == 0;
+    const bool wide = EVEN || (uintptr_t)out % 16 == 0;
     // what an exponential is multiplied by: kept ones are against this thread's own maximum
     const float factor = (KEEP ? ex2f((finite_max(own) - finite_max(part.m)) * P.c) : 1.f) * a;
     const u64 at2 = pack2(part.m, part.m), f2 = pack2(factor, factor);
@@ -283,18 +298,20 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
         for (int i = 0; i < E / 2; ++i) {
             float p, q;
             unpack2(mul2(e[i], f2), p, q);
-            if (!live) p = q = 0.f;
             if constexpr (BF16) r[i] = bf16x2(p, q);
             else { r[2 * i] = __float_as_uint(p); r[2 * i + 1] = __float_as_uint(q); }
         }
-        if (wide && j * E >= head && (j + 1) * E <= end) {
+        if (!live) r[0] = r[1] = r[2] = r[3] = 0u;
+        if (EVEN || (wide && j * E >= head && (j + 1) * E <= end)) {
             *reinterpret_cast<uint4 *>(out + (size_t)j * E) = make_uint4(r[0], r[1], r[2], r[3]);
             return;
         }
+        if constexpr (!EVEN) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int at = j * E + e;
-            if (at >= head && at < end) out[at] = (T)(BF16 ? r[e / 2] >> (16 * (e & 1)) : r[e]);
+            for (int e1 = 0; e1 < E; ++e1) {
+                const int at = j * E + e1;
+                if (at >= head && at < end) out[at] = (T)(BF16 ? r[e1 / 2] >> (16 * (e1 & 1)) : r[e1]);
+            }
         }
     };
     if constexpr (V > 0) {
@@ -317,31 +334,44 @@ __global__ void __launch_bounds__(TPR <= 128 ? 256 : TPR, TPR <= 128 ? 4 : 2) lo
     }
     if (!live) return;
     group_sync();
+    // named entries: the first warp's, or a long list's by all
+    if (P.k <= 32) {
+        if (warp) return;
+        const int j = lane < P.k ? s_index[lane] : -1;
+        const unsigned alike = __match_any_sync(0xffffffffu, j);
+        if (j < 0 || (alike & ((1u << lane) - 1u)) || (C > 1 && (head + j) / E / TPR % C != rank)) return;
+        float q = 0.f;
+        for (unsigned left = alike; left; left &= left - 1u) q += s_q[__ffs(left) - 1];
+        const float g = ex2f((s_score[lane] - part.m) * P.c) / part.s * w - q * w;
+        out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+        return;
+    }
     for (int k = t; k < P.k; k += TPR) {
-        const int j = s_index[group][k];
+        const int j = s_index[k];
         if (j < 0 || (C > 1 && (head + j) / E / TPR % C != rank)) continue;
         float q = 0.f;
         bool first = true;
         for (int o = 0; o < P.k; ++o)
-            if (s_index[group][o] == j) {
+            if (s_index[o] == j) {
                 first &= o >= k;
-                q += s_q[group][o];
+                q += s_q[o];
             }
         if (!first) continue;
-        const float g = ex2f((s_score[group][k] - part.m) * P.c) / part.s * w - q * w;
+        const float g = ex2f((s_score[k] - part.m) * P.c) / part.s * w - q * w;
         out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
     }
 }
 
-template <bool BF16, int TPR, int V, int C>
+template <bool BF16, int TPR, int V, int C, bool EVEN>
 skb_status launch(const Loss &P, cudaStream_t st)
 {
-    constexpr int threads = TPR <= 128 ? 256 : TPR, groups = threads / TPR;
+    constexpr int threads = TPR <= 256 ? 256 : TPR, groups = threads / TPR;
     const long long blocks = (P.rows + groups - 1) / groups * C;
     if (blocks > 0x7fffffffLL) return op_fail(SKB_ERR_SHAPE, "too many rows");
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = (size_t)groups * 4 * P.k * sizeof(float);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -349,34 +379,41 @@ skb_status launch(const Loss &P, cudaStream_t st)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = C > 1 ? 1 : 0;
-    cudaLaunchKernelEx(&cfg, loss_kernel<BF16, TPR, V, C>, P);
+    cudaLaunchKernelEx(&cfg, loss_kernel<BF16, TPR, V, C, EVEN>, P);
     return op_launched("plan_loss");
 }
 
-template <bool BF16>
-skb_status launch_by_length(const Loss &P, int sms, cudaStream_t st)
+template <bool BF16, bool EVEN>
+skb_status launch_by_length(const Loss &P, long long vec, int sms, cudaStream_t st)
 {
-    constexpr int E = BF16 ? 8 : 4;
-    // vectors that a row may touch: one more than it fills where rows do not all start on a 16-byte boundary
-    const bool even = (uintptr_t)P.scores % 16 == 0 && P.ld % E == 0;
-    const long long vec = ((long long)P.m + (even ? E - 1 : 2 * E - 2)) / E;
     // more blocks to a row than it needs where there are too few rows to fill the device
     const auto blocks = [&](int least) {
         int c = least;
         while (c < 8 && P.rows * c < 2 * sms && vec / (2 * c) >= 512) c *= 2;
         return c;
     };
-    if (vec <= 32 * 4) return launch<BF16, 32, 4, 1>(P, st);
-    if (vec <= 128 * 4) return launch<BF16, 128, 4, 1>(P, st);
-    if (vec <= 128 * 8 && P.rows >= sms) return launch<BF16, 128, 8, 1>(P, st);
-    if (vec <= 512 * 8 * 8) {
-        const int c = blocks(vec <= 512 * 8 ? 1 : vec <= 512 * 16 ? 2 : vec <= 512 * 32 ? 4 : 8);
-        if (c == 1) return launch<BF16, 512, 8, 1>(P, st);
-        if (c == 2) return launch<BF16, 512, 8, 2>(P, st);
-        if (c == 4) return launch<BF16, 512, 8, 4>(P, st);
-        return launch<BF16, 512, 8, 8>(P, st);
+    if (vec <= 32 * 4) return launch<BF16, 32, 4, 1, EVEN>(P, st);
+    if (vec <= 32 * 8 && P.rows >= 8 * sms) return launch<BF16, 32, 8, 1, EVEN>(P, st);
+    if (vec <= 128 * 4) return launch<BF16, 128, 4, 1, EVEN>(P, st);
+    if (vec <= 256 * 8 * 8) {
+        const int c = blocks(vec <= 256 * 8 ? 1 : vec <= 256 * 16 ? 2 : vec <= 256 * 32 ? 4 : 8);
+        if (c == 1) return vec <= 256 * 4 ? launch<BF16, 256, 4, 1, EVEN>(P, st) : launch<BF16, 256, 8, 1, EVEN>(P, st);
+        if (c == 2) return launch<BF16, 256, 8, 2, EVEN>(P, st);
+        if (c == 4) return launch<BF16, 256, 8, 4, EVEN>(P, st);
+        return launch<BF16, 256, 8, 8, EVEN>(P, st);
     }
-    return launch<BF16, 512, 0, 8>(P, st);
+    if (vec <= 512 * 8 * 8) return launch<BF16, 512, 8, 8, EVEN>(P, st);
+    return launch<BF16, 512, 0, 8, EVEN>(P, st);
+}
+template <bool BF16>
+skb_status launch_loss(const Loss &P, int sms, cudaStream_t st)
+{
+    constexpr int E = BF16 ? 8 : 4;
+    // vectors that a row may touch: one more than it fills where rows do not all start on a 16-byte boundary
+    const bool aligned = (uintptr_t)P.scores % 16 == 0 && P.ld % E == 0;
+    const long long vec = ((long long)P.m + (aligned ? E - 1 : 2 * E - 2)) / E;
+    const bool even = aligned && P.m % E == 0 && (!P.grad || ((uintptr_t)P.grad % 16 == 0 && P.ldg % E == 0));
+    return even ? launch_by_length<BF16, true>(P, vec, sms, st) : launch_by_length<BF16, false>(P, vec, sms, st);
 }
 
 }  // namespace
@@ -401,5 +438,5 @@ extern "C" skb_status sinkhorn_plan_loss(const void *scores, int dtype, long lon
     cudaGetDevice(&dev);
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");
     const Loss P = {scores, index, logits, weight, loss, grad, rows, ld, ldg, m, k, 1.f / temperature, (float)(1.4426950408889634 / (double)temperature)};
-    return dtype == SKB_BF16 ? launch_by_length<true>(P, sms, (cudaStream_t)stream) : launch_by_length<false>(P, sms, (cudaStream_t)stream);
+    return dtype == SKB_BF16 ? launch_loss<true>(P, sms, (cudaStream_t)stream) : launch_loss<false>(P, sms, (cudaStream_t)stream);
 }
