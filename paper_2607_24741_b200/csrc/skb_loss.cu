@@ -112,7 +112,7 @@ __device__ __forceinline__ Part join(Part a, Part b, float c)
 template <bool BF16, int TPR, int V, int C, bool EVEN>
 __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) loss_kernel(const __grid_constant__ Loss P)
 {
-    constexpr int THREADS = TPR <= 256 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR / 32, AHEAD = 2;
+    constexpr int THREADS = TPR <= 256 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR / 32;
     constexpr int E = BF16 ? 8 : 4;
     using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
     extern __shared__ float s_entries[];                          // [GROUPS][4][k]: index, q, log q, score
@@ -134,11 +134,11 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     const int head = EVEN ? 0 : (int)((uintptr_t)src % 16 / sizeof(T)), end = head + P.m;      // the row, in elements from a 16-byte boundary on
     const T *base = src - head;
     const int nvec = (end + E - 1) / E;
+    const uint4 nothing = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
+                               : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);           // minus infinity
     auto load = [&](int j) {
         if (EVEN || (j * E >= head && (j + 1) * E <= end)) return *reinterpret_cast<const uint4 *>(base + (size_t)j * E);
-        uint4 r = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
-                       : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
-        uint32_t w[4] = {r.x, r.y, r.z, r.w};
+        uint32_t w[4] = {nothing.x, nothing.y, nothing.z, nothing.w};
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const int at = j * E + e;
@@ -150,60 +150,54 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         return make_uint4(w[0], w[1], w[2], w[3]);
     };
     auto score_at = [&](int j) { return BF16 ? __uint_as_float((uint32_t)src[j] << 16) : __uint_as_float((uint32_t)src[j]); };
-    // the first entries are on their way before the row is
-    int named[AHEAD];
-    float logit[AHEAD], score[AHEAD];
-    if (warp == 0) {
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            const int k = 32 * a + lane;
-            named[a] = k < P.k ? P.index[(size_t)row * P.k + k] : -1;
-            logit[a] = k < P.k && P.logits ? P.logits[(size_t)row * P.k + k] : 0.f;
-        }
+    // the first entries and the weight are on their way before the row is
+    const float weight = P.weight ? P.weight[row] : 1.f;
+    int named = -1;
+    float logit = 0.f, score = 0.f, own_q = 0.f, own_log = 0.f;   // of the first 32 entries, a lane of the first warp to each
+    if (warp == 0 && lane < P.k) {
+        named = P.index[(size_t)row * P.k + lane];
+        if (P.logits) logit = P.logits[(size_t)row * P.k + lane];
     }
     uint4 held[V ? V : 1];
     if constexpr (V > 0) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int j = (v * C + rank) * TPR + t;
-            held[v] = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u)
-                           : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+            held[v] = nothing;
             if (j < nvec) held[v] = load(j);
         }
     }
     // the teacher: the first warp's, while the row is on its way; so are the scores that it names
     if (warp == 0) {
-        float top = -INFINITY, total = 0.f;
-        auto entry = [&](int k, int j, float l) {
-            const bool there = j >= 0 && j < P.m;
-            l = there ? l * P.inv_t : -INFINITY;
-            s_index[k] = there ? j : -1;
+        if (named < 0 || named >= P.m) named = -1;
+        const float l0 = named >= 0 ? logit * P.inv_t : -INFINITY;
+        if (named >= 0) score = score_at(named);
+        float top = l0;
+        for (int k = 32 + lane; k < P.k; k += 32) {
+            int j = P.index[(size_t)row * P.k + k];
+            if (j < 0 || j >= P.m) j = -1;
+            const float l = j >= 0 ? (P.logits ? P.logits[(size_t)row * P.k + k] * P.inv_t : 0.f) : -INFINITY;
+            s_index[k] = j;
             s_log[k] = l;
+            s_score[k] = j >= 0 ? score_at(j) : 0.f;
             top = fmaxf(top, l);
-            return there;
-        };
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-            score[a] = 0.f;
-            if (32 * a + lane < P.k && entry(32 * a + lane, named[a], logit[a])) score[a] = score_at(named[a]);
-        }
-        for (int k = 32 * AHEAD + lane; k < P.k; k += 32) {
-            const int j = P.index[(size_t)row * P.k + k];
-            s_score[k] = entry(k, j, P.logits ? P.logits[(size_t)row * P.k + k] : 0.f) ? score_at(j) : 0.f;
         }
         const float at = finite_max(warp_max(top));
+        own_q = ex2f((l0 - at) * 1.44269504f);
+        float total = own_q;
         // (a thread reads back what it wrote)
-        for (int k = lane; k < P.k; k += 32) {
-            const float l = s_log[k] - at, e = ex2f(l * 1.44269504f);
-            s_log[k] = l;
-            s_q[k] = e;
-            total += e;
-        }
+        for (int k = 32 + lane; k < P.k; k += 32) total += s_q[k] = ex2f((s_log[k] - at) * 1.44269504f);
 #pragma unroll
         for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
-        const float log_total = logf(total), inv = total == 0.f ? 0.f : 1.f / total;
-        for (int k = lane; k < P.k; k += 32) {
-            s_log[k] -= log_total;
+        const float log_total = __logf(total), inv = total == 0.f ? 0.f : 1.f / total;
+        own_q *= inv;
+        own_log = l0 - at - log_total;
+        if (lane < P.k) {
+            s_index[lane] = named;
+            s_q[lane] = own_q;
+        }
+        for (int k = 32 + lane; k < P.k; k += 32) {
+            s_log[k] = s_log[k] - at - log_total;
             s_q[k] *= inv;
         }
         if (lane == 0) s_total[group] = total;
@@ -231,22 +225,19 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         part.s = a + b;
     } else {
         for (int j = rank * TPR + t; j < nvec; j += C * TPR) {
-            const uint4 x = load(j);
-            Part one = {largest<BF16>(x), 0.f};
+            const uint4 y = load(j);
+            Part one = {largest<BF16>(y), 0.f};
             const u64 at2 = pack2(finite_max(one.m), finite_max(one.m));
             u64 sum = 0ull;
 #pragma unroll
-            for (int i = 0; i < E / 2; ++i) sum = add2(sum, exponentials(two<BF16>(x, i), at2, c2));
+            for (int i = 0; i < E / 2; ++i) sum = add2(sum, exponentials(two<BF16>(y, i), at2, c2));
             float a, b;
             unpack2(sum, a, b);
             one.s = a + b;
             part = join(part, one, P.c);
         }
     }
-    if (warp == 0)
-#pragma unroll
-        for (int a = 0; a < AHEAD; ++a)
-            if (32 * a + lane < P.k) s_score[32 * a + lane] = score[a];
+    if (warp == 0 && lane < P.k) s_score[lane] = score;
     const float own = part.m;
     part = join<32>(part, P.c);
     if constexpr (WARPS > 1) {
@@ -271,26 +262,24 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     }
     const bool live = s_total[group] != 0.f;                     // (NaN, too)
     if (warp == 0 && rank == 0) {
-        const float log_sum = logf(part.s);
-        float sum = 0.f;
-        for (int k = lane; k < P.k; k += 32) {
-            const float q = s_q[k];
-            if (q != 0.f) sum += q * (s_log[k] - ((s_score[k] - part.m) * P.inv_t - log_sum));
-        }
+        const float log_sum = __logf(part.s);
+        auto term = [&](float q, float log_q, float at) { return q != 0.f ? q * (log_q - ((at - part.m) * P.inv_t - log_sum)) : 0.f; };
+        float sum = term(own_q, own_log, score);
+        for (int k = 32 + lane; k < P.k; k += 32) sum += term(s_q[k], s_log[k], s_score[k]);
 #pragma unroll
         for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         if (lane == 0) P.loss[row] = live ? sum : 0.f;
     }
     if (!P.grad) return;
-    const float w = (P.weight ? P.weight[row] : 1.f) * P.inv_t, a = w / part.s;
+    const float w = weight * P.inv_t, a = w / part.s;
     T *out = (T *)P.grad + (size_t)row * P.ldg - head;
     const bool wide = EVEN || (uintptr_t)out % 16 == 0;
     // what an exponential is multiplied by: kept ones are against this thread's own maximum
     const float factor = (KEEP ? ex2f((finite_max(own) - finite_max(part.m)) * P.c) : 1.f) * a;
     const u64 at2 = pack2(part.m, part.m), f2 = pack2(factor, factor);
-    auto again = [&](const uint4 &x, u64 (&e)[E / 2]) {
+    auto again = [&](const uint4 &y, u64 (&e)[E / 2]) {
 #pragma unroll
-        for (int i = 0; i < E / 2; ++i) e[i] = exponentials(two<BF16>(x, i), at2, c2);
+        for (int i = 0; i < E / 2; ++i) e[i] = exponentials(two<BF16>(y, i), at2, c2);
     };
     auto store = [&](int j, const u64 (&e)[E / 2]) {
         uint32_t r[4];
@@ -337,13 +326,12 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     // named entries: the first warp's, or a long list's by all
     if (P.k <= 32) {
         if (warp) return;
-        const int j = lane < P.k ? s_index[lane] : -1;
-        const unsigned alike = __match_any_sync(0xffffffffu, j);
-        if (j < 0 || (alike & ((1u << lane) - 1u)) || (C > 1 && (head + j) / E / TPR % C != rank)) return;
+        const unsigned alike = __match_any_sync(0xffffffffu, named);
+        if (named < 0 || (alike & ((1u << lane) - 1u)) || (C > 1 && (head + named) / E / TPR % C != rank)) return;
         float q = 0.f;
         for (unsigned left = alike; left; left &= left - 1u) q += s_q[__ffs(left) - 1];
-        const float g = ex2f((s_score[lane] - part.m) * P.c) / part.s * w - q * w;
-        out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+        const float g = ex2f((score - part.m) * P.c) * a - q * w;
+        out[head + named] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
         return;
     }
     for (int k = t; k < P.k; k += TPR) {
@@ -357,7 +345,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
                 q += s_q[o];
             }
         if (!first) continue;
-        const float g = ex2f((s_score[k] - part.m) * P.c) / part.s * w - q * w;
+        const float g = ex2f((s_score[k] - part.m) * P.c) * a - q * w;
         out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
     }
 }
