@@ -116,8 +116,8 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     constexpr int E = BF16 ? 8 : 4;
     using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
     extern __shared__ float s_entries[];                          // [GROUPS][4][k]: index, q, log q, score
-    __shared__ float s_total[GROUPS];
-    __shared__ Part s_part[GROUPS][WARPS], s_rank[C];
+    __shared__ float s_loss[GROUPS][WARPS];
+    __shared__ Part s_part[GROUPS][WARPS], s_teach[GROUPS][WARPS], s_rank[C];
     const int tid = threadIdx.x, group = tid / TPR, t = tid % TPR, lane = tid & 31, warp = t >> 5;
     const int rank = C > 1 ? (int)(blockIdx.x % C) : 0;
     const long long row = (long long)(blockIdx.x / C) * GROUPS + group;
@@ -153,10 +153,10 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     // the first entries and the weight are on their way before the row is
     const float weight = P.weight ? P.weight[row] : 1.f;
     int named = -1;
-    float logit = 0.f, score = 0.f, own_q = 0.f, own_log = 0.f;   // of the first 32 entries, a lane of the first warp to each
-    if (warp == 0 && lane < P.k) {
-        named = P.index[(size_t)row * P.k + lane];
-        if (P.logits) logit = P.logits[(size_t)row * P.k + lane];
+    float logit = 0.f, score = 0.f;                              // of this thread's entry: one to each, a warp's to a row may be more
+    if (t < P.k) {
+        named = P.index[(size_t)row * P.k + t];
+        if (P.logits) logit = P.logits[(size_t)row * P.k + t];
     }
     uint4 held[V ? V : 1];
     if constexpr (V > 0) {
@@ -167,40 +167,32 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             if (j < nvec) held[v] = load(j);
         }
     }
-    // the teacher: the first warp's, while the row is on its way; so are the scores that it names
-    if (warp == 0) {
-        if (named < 0 || named >= P.m) named = -1;
-        const float l0 = named >= 0 ? logit * P.inv_t : -INFINITY;
+    // the teacher, and the scores that it names, while the row is on its way
+    constexpr float LOG2E = 1.44269504f;
+    Part teach = {-INFINITY, 0.f};
+    if (named < 0 || named >= P.m) named = -1;
+    const float l0 = named >= 0 ? logit * P.inv_t : -INFINITY;
+    if (warp * 32 < P.k) {
         if (named >= 0) score = score_at(named);
-        float top = l0;
-        for (int k = 32 + lane; k < P.k; k += 32) {
-            int j = P.index[(size_t)row * P.k + k];
-            if (j < 0 || j >= P.m) j = -1;
-            const float l = j >= 0 ? (P.logits ? P.logits[(size_t)row * P.k + k] * P.inv_t : 0.f) : -INFINITY;
-            s_index[k] = j;
-            s_log[k] = l;
-            s_score[k] = j >= 0 ? score_at(j) : 0.f;
-            top = fmaxf(top, l);
-        }
-        const float at = finite_max(warp_max(top));
-        own_q = ex2f((l0 - at) * 1.44269504f);
-        float total = own_q;
+        teach.m = l0;
+        if constexpr (TPR < LS_MAX_K)
+            for (int k = t + TPR; k < P.k; k += TPR) {
+                int j = P.index[(size_t)row * P.k + k];
+                if (j < 0 || j >= P.m) j = -1;
+                const float l = j >= 0 ? (P.logits ? P.logits[(size_t)row * P.k + k] * P.inv_t : 0.f) : -INFINITY;
+                s_index[k] = j;
+                s_log[k] = l;
+                s_score[k] = j >= 0 ? score_at(j) : 0.f;
+                teach.m = fmaxf(teach.m, l);
+            }
+        teach.m = warp_max(teach.m);
+        const float at = finite_max(teach.m);
+        teach.s = ex2f((l0 - at) * LOG2E);
         // (a thread reads back what it wrote)
-        for (int k = 32 + lane; k < P.k; k += 32) total += s_q[k] = ex2f((s_log[k] - at) * 1.44269504f);
+        if constexpr (TPR < LS_MAX_K)
+            for (int k = t + TPR; k < P.k; k += TPR) teach.s += ex2f((s_log[k] - at) * LOG2E);
 #pragma unroll
-        for (int off = 16; off; off /= 2) total += __shfl_xor_sync(0xffffffffu, total, off);
-        const float log_total = __logf(total), inv = total == 0.f ? 0.f : 1.f / total;
-        own_q *= inv;
-        own_log = l0 - at - log_total;
-        if (lane < P.k) {
-            s_index[lane] = named;
-            s_q[lane] = own_q;
-        }
-        for (int k = 32 + lane; k < P.k; k += 32) {
-            s_log[k] = s_log[k] - at - log_total;
-            s_q[k] *= inv;
-        }
-        if (lane == 0) s_total[group] = total;
+        for (int off = 16; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
     }
     // maximum and sum of what this thread has seen
     constexpr bool KEEP = V > 0 && (!BF16 || V <= 4);            // exponentials stay in registers
@@ -237,12 +229,13 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             part = join(part, one, P.c);
         }
     }
-    if (warp == 0 && lane < P.k) s_score[lane] = score;
     const float own = part.m;
     part = join<32>(part, P.c);
     if constexpr (WARPS > 1) {
-        if (lane == 0) s_part[group][warp] = part;
+        if (lane == 0) { s_part[group][warp] = part; s_teach[group][warp] = teach; }
         group_sync();
+        teach = join<WARPS>(lane < WARPS ? s_teach[group][lane] : Part{-INFINITY, 0.f}, LOG2E);
+        teach.s = __shfl_sync(0xffffffffu, teach.s, 0);
         part = join<WARPS>(lane < WARPS ? s_part[group][lane] : Part{-INFINITY, 0.f}, P.c);
         part.s = __shfl_sync(0xffffffffu, part.s, 0);
     } else __syncwarp();
@@ -260,17 +253,40 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         part = join<C>(lane < C ? s_rank[lane] : Part{-INFINITY, 0.f}, P.c);
         part.s = __shfl_sync(0xffffffffu, part.s, 0);
     }
-    const bool live = s_total[group] != 0.f;                     // (NaN, too)
-    if (warp == 0 && rank == 0) {
-        const float log_sum = __logf(part.s);
-        auto term = [&](float q, float log_q, float at) { return q != 0.f ? q * (log_q - ((at - part.m) * P.inv_t - log_sum)) : 0.f; };
-        float sum = term(own_q, own_log, score);
-        for (int k = 32 + lane; k < P.k; k += 32) sum += term(s_q[k], s_log[k], s_score[k]);
+    const bool live = teach.s != 0.f;                             // (NaN, too)
+    const float teach_at = finite_max(teach.m), teach_inv = live ? 1.f / teach.s : 0.f;
+    float own_q = 0.f, sum = 0.f;
+    if (warp * 32 < P.k) {
+        const float log_all = __logf(teach.s) - __logf(part.s);
+        // (q log q - q log p)
+        auto term = [&](float q, float l, float at) { return q != 0.f ? q * ((l - teach_at) - (at - part.m) * P.inv_t - log_all) : 0.f; };
+        own_q = ex2f((l0 - teach_at) * LOG2E) * teach_inv;
+        sum = term(own_q, l0, score);
+        if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
+        if constexpr (TPR < LS_MAX_K)
+            for (int k = t + TPR; k < P.k; k += TPR) {
+                s_q[k] = ex2f((s_log[k] - teach_at) * LOG2E) * teach_inv;
+                sum += term(s_q[k], s_log[k], s_score[k]);
+            }
+        if (rank == 0) {
 #pragma unroll
-        for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        if (lane == 0) P.loss[row] = live ? sum : 0.f;
+            for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        }
     }
-    if (!P.grad) return;
+    if (WARPS > 1 && lane == 0) s_loss[group][warp] = sum;
+    // of all warps, in their order
+    auto give_loss = [&] {
+        if (rank != 0 || t != 0) return;
+        if constexpr (WARPS > 1)
+#pragma unroll
+            for (int i = 1; i < WARPS; ++i) sum += s_loss[group][i];
+        P.loss[row] = live ? sum : 0.f;
+    };
+    if (!P.grad) {
+        group_sync();
+        give_loss();
+        return;
+    }
     const float w = weight * P.inv_t, a = w / part.s;
     T *out = (T *)P.grad + (size_t)row * P.ldg - head;
     const bool wide = EVEN || (uintptr_t)out % 16 == 0;
@@ -321,11 +337,11 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             store(j, kept[0]);
         }
     }
-    if (!live) return;
     group_sync();
-    // named entries: the first warp's, or a long list's by all
+    give_loss();
+    if (!live || warp * 32 >= P.k) return;
+    // named entries: each by the first of those that name its column
     if (P.k <= 32) {
-        if (warp) return;
         const unsigned alike = __match_any_sync(0xffffffffu, named);
         if (named < 0 || (alike & ((1u << lane) - 1u)) || (C > 1 && (head + named) / E / TPR % C != rank)) return;
         float q = 0.f;
@@ -335,7 +351,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         return;
     }
     for (int k = t; k < P.k; k += TPR) {
-        const int j = s_index[k];
+        const int j = k == t ? named : s_index[k];
         if (j < 0 || (C > 1 && (head + j) / E / TPR % C != rank)) continue;
         float q = 0.f;
         bool first = true;
@@ -345,7 +361,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
                 q += s_q[o];
             }
         if (!first) continue;
-        const float g = ex2f((s_score[k] - part.m) * P.c) * a - q * w;
+        const float g = ex2f(((k == t ? score : s_score[k]) - part.m) * P.c) * a - q * w;
         out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
     }
 }
