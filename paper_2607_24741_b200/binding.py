@@ -242,7 +242,11 @@ def _on(device):
 
 
 def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
+    return _raw_stream(device.index)
+
+
+# (the stream's handle without a Stream object around it, which takes as long as a small launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _cloud4_bytes(W, npts, d, format):
@@ -341,7 +345,10 @@ def _cloud8_bytes(W, npts, d):
 class Cloud8:
     """A cloud [W, npts, d] held in 8 bits: `buffer` as sinkhorn_cloud8_pack lays it out (a uint8 CUDA tensor)."""
 
-    def __init__(self, buffer, W, npts, d):
+    def __init__(self, buffer, W, npts, d, _made=False):
+        if _made:                                   # (by cloud8_pack, which has checked it all)
+            self.buffer, self.W, self.npts, self.d, self.device = buffer, W, npts, d, buffer.device
+            return
         need = _cloud8_bytes(W, npts, d)
         if need == 0:
             raise ValueError("W, npts and d must be >= 1, d at most 1024")
@@ -349,15 +356,11 @@ class Cloud8:
             raise ValueError(f"buffer must be a contiguous uint8 CUDA tensor of at least {need} bytes")
         if buffer.data_ptr() % 256:
             raise ValueError("buffer must be 256-byte aligned")
-        self.buffer, self.W, self.npts, self.d = buffer, W, npts, d
+        self.buffer, self.W, self.npts, self.d, self.device = buffer, W, npts, d, buffer.device
 
     @property
     def shape(self):
         return (self.W, self.npts, self.d)
-
-    @property
-    def device(self):
-        return self.buffer.device
 
     def values(self, dtype=torch.float32):
         """What the cloud stands for, [W, npts, d] float32 or bfloat16 (both exact)."""
@@ -379,14 +382,15 @@ def cloud8_pack(v, values=None):
         raise ValueError("values must be torch.float32 or torch.bfloat16")
     v = v.contiguous()
     W, npts, d = v.shape
-    need = _cloud8_bytes(W, npts, d)
+    need, device = _cloud8_bytes(W, npts, d), v.device
     if need == 0:
         raise ValueError("W, npts and d must be >= 1, d at most 1024")
-    with _on(v.device):
-        buffer = torch.empty(need, dtype=torch.uint8, device=v.device)
-        out = None if values is None else torch.empty(v.shape, dtype=values, device=v.device)
-        _check_op(lib.sinkhorn_cloud8_pack(_ptr(v), DTYPES[v.dtype], W, npts, d, _ptr(buffer), _ptr(out), DTYPES.get(values, 0), _stream(v.device)))
-    cloud = Cloud8(buffer, W, npts, d)
+    with _on(device):
+        buffer = torch.empty(need, dtype=torch.uint8, device=device)
+        out = None if values is None else torch.empty_like(v, dtype=values)
+        _check_op(lib.sinkhorn_cloud8_pack(v.data_ptr(), DTYPES[v.dtype], W, npts, d, buffer.data_ptr(), None if out is None else out.data_ptr(),
+                                           DTYPES.get(values, 0), _stream(device)))
+    cloud = Cloud8(buffer, W, npts, d, True)
     return cloud if values is None else (cloud, out)
 
 
@@ -402,7 +406,7 @@ def cloud8_dots(x, y, out=None):
     with _on(x.device):
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=x.device)
-        _check_op(lib.sinkhorn_cloud8_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, _ptr(out), _stream(x.device)))
+        _check_op(lib.sinkhorn_cloud8_dots(x.buffer.data_ptr(), y.buffer.data_ptr(), x.W, x.npts, y.npts, x.d, out.data_ptr(), _stream(x.device)))
     return out
 
 
@@ -435,10 +439,12 @@ def cloud8_map(x, y, g, eps, v=None, *, lengths=None, lse=False, out=None):
         raise SkbError(2, "shape not supported: W, n, m, d >= 1, d and dv <= 1024, n and m <= 262143, W <= 65535")
     with _on(device):
         ws = torch.empty(need, dtype=torch.uint8, device=device)
-        out = torch.empty(W, n, dv, dtype=torch.bfloat16, device=device) if out is None else out
+        if out is None:
+            out = torch.empty_like(x) if dv == d else torch.empty(W, n, dv, dtype=torch.bfloat16, device=device)
         sums = torch.empty(W, n, dtype=torch.float32, device=device) if lse else None
-        _check_op(lib.sinkhorn_cloud8_map(_ptr(x), _ptr(y.buffer), _ptr(g), _ptr(eps), None if v is None else _ptr(v.buffer), _ptr(lengths), W, n, m, d, dv,
-                                          _ptr(out), _ptr(sums), _ptr(ws), need, _stream(device)))
+        _check_op(lib.sinkhorn_cloud8_map(x.data_ptr(), y.buffer.data_ptr(), None if g is None else g.data_ptr(), eps.data_ptr(),
+                                          None if v is None else v.buffer.data_ptr(), None if lengths is None else lengths.data_ptr(), W, n, m, d, dv,
+                                          out.data_ptr(), None if sums is None else sums.data_ptr(), ws.data_ptr(), need, _stream(device)))
     return (out, sums) if lse else out
 
 
@@ -470,10 +476,11 @@ def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=
     continues from it."""
     if not torch.is_tensor(scores) or not scores.is_cuda or scores.dtype not in DTYPES or scores.dim() < 1:
         raise ValueError("scores must be a float32 or bfloat16 CUDA tensor [..., m]")
-    lead, m, device = scores.shape[:-1], scores.shape[-1], scores.device
+    shape, device = scores.shape, scores.device
+    lead, m = shape[:-1], shape[-1]
     if torch.is_tensor(index) and index.shape == lead:              # one entry a row
         index, logits = index.unsqueeze(-1), logits.unsqueeze(-1) if torch.is_tensor(logits) and logits.shape == lead else logits
-    if not torch.is_tensor(index) or index.dtype != torch.int32 or index.device != device or index.dim() != scores.dim() or index.shape[:-1] != lead:
+    if not torch.is_tensor(index) or index.dtype != torch.int32 or index.device != device or index.dim() != len(shape) or index.shape[:-1] != lead:
         raise ValueError("index must be an int32 tensor [..., k] on the scores' device")
     if logits is not None and (not torch.is_tensor(logits) or logits.dtype != torch.float32 or logits.device != device or logits.shape != index.shape):
         raise ValueError("logits must be a float32 tensor of index's shape on the scores' device")
@@ -483,9 +490,12 @@ def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=
     if rows < 1 or not 1 <= m <= 262143 or not 1 <= k <= 256:
         raise ValueError("at least one row, m from 1 to 262143 and k from 1 to 256 are supported")
     in_place = torch.is_tensor(grad)
-    if in_place and (grad.dtype != scores.dtype or grad.device != device or grad.shape != scores.shape or _rows_of(grad) is None):
-        raise ValueError("grad must be a tensor like the scores with evenly spaced rows")
-    ld = _rows_of(scores)
+    ldg = m
+    if in_place:
+        ldg = _rows_of(grad) if grad.shape == shape else None
+        if ldg is None or grad.dtype != scores.dtype or grad.device != device:
+            raise ValueError("grad must be a tensor like the scores with evenly spaced rows")
+    ld = m if scores.is_contiguous() else _rows_of(scores)
     if ld is None:
         if in_place and grad.data_ptr() == scores.data_ptr():
             raise ValueError("scores whose rows are not evenly spaced cannot take the gradient")
@@ -495,10 +505,13 @@ def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=
     logits = None if logits is None else logits.contiguous()
     weight = None if weight is None else weight.contiguous()
     with _on(device):
-        loss = torch.empty(lead, dtype=torch.float32, device=device)
-        out = grad if in_place else torch.empty(scores.shape, dtype=scores.dtype, device=device) if grad else None
-        _check_op(lib.sinkhorn_plan_loss(_ptr(scores), DTYPES[scores.dtype], rows, m, ld, _ptr(index), _ptr(logits), k, float(temperature), _ptr(weight),
-                                         _ptr(loss), _ptr(out), m if out is None or not in_place else _rows_of(out), _stream(device)))
+        loss = torch.empty(lead, dtype=torch.float32, device=device) if weight is None else torch.empty_like(weight)
+        out = grad if in_place else None
+        if grad is True:
+            out = torch.empty_like(scores.detach(), memory_format=torch.contiguous_format)
+        _check_op(lib.sinkhorn_plan_loss(scores.data_ptr(), DTYPES[scores.dtype], rows, m, ld, index.data_ptr(), None if logits is None else logits.data_ptr(), k,
+                                         float(temperature), None if weight is None else weight.data_ptr(), loss.data_ptr(), None if out is None else out.data_ptr(),
+                                         ldg, _stream(device)))
     return loss if out is None else (loss, out)
 
 
