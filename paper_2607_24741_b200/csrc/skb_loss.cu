@@ -5,19 +5,23 @@
 //      d loss_i / d s_ij = (p_ij - sum of q_k over the k with j(k) = j) / T.
 //
 // One pass: a row is read once, 16 bytes a thread and vector, and stays in registers (up to 64 scores of bf16 or 32 of fp32 a
-// thread, raw) until its maximum and sum are known; then the gradient is written.  So memory bounds it.  Exponentials are taken twice,
-// against the thread's own maximum for the sum and the row's for the gradient: that is one barrier a row instead of two, and no fp32
-// copies in registers.  What a row is given goes by its length: a warp, four warps, 16 warps, or a cluster of up to eight blocks of
-// 16 warps, whose maxima and sums meet in distributed shared memory; rows longer than what a cluster's registers hold are read twice, the second time
-// from L2 (a row is at most 1 MB).  A row is reduced in a fixed order, so results do not change from call to call.
+// thread, raw) until its maximum and sum are known; then the gradient is written.  So memory bounds it, and the latencies of what a row
+// needs besides: 65536 rows of 1024 in bf16 take 53 us for 270 MB (78 % of the measured copy rate), of 64 still 43.  Exponentials are taken against the
+// thread's own maximum for the sum; short rows keep them, others take them again against the row's: that is one barrier a row instead of two, and no fp32
+// copies in registers.  What a row is given goes by its length: a warp (up to 128 vectors, or 256 where there are many rows: 32768 rows of 2048 in bf16 99 us
+// with four warps to a row, 50 so), four, eight or 16 warps, or a cluster of up to eight blocks, whose maxima and sums meet in distributed shared memory; many
+// long rows stay in shared memory (loss_long_kernel); rows longer than what a cluster's registers hold are read twice, the second time from L2 (a row
+// is at most 1 MB).  A row is reduced in a fixed order, so results do not change from call to call.
 //
-// The named entries' gradients are written after all others of the row, by the first of the entries that name a column, which adds up
-// the q of all that do: no atomics, any entry may be named any number of times.
+// The named entries, a thread to each, are fetched before the row and their softmax is made while it is on its way.  Their gradients are written after
+// all others of the row, by the first of the entries that name a column, which adds up the q of all that do: no atomics, any entry may be named
+// any number of times.
 #include <cuda_runtime.h>
 #include <string>
 
 #include "skb_f32x2.cuh"
 #include "skb_operators.h"
+#include "skb_tmem.cuh"
 
 namespace skb {
 namespace {
@@ -366,6 +370,184 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     }
 }
 
+// Long rows of whole vectors, many of them: a block an SM takes row after row.  A row comes into a ring of 32 KB pieces in shared memory by bulk copies; its
+// maximum and sum are made of the pieces as they arrive, the gradient of the same pieces, which go back one by one to the next row's
+// copies: reads and writes never stop for the barrier between the two passes.  (In registers of a cluster of four blocks a row of 65536
+// in bf16 waits for its slowest block twice: 4096 rows took 249 us, so 211; pieces of 16 KB 231, with 24 warps and 12 KB 252.)
+constexpr int LL_WARPS = 16, LL_THREADS = LL_WARPS * 32, LL_PIECE = 32768, LL_PIECES = 6;
+template <bool BF16>
+__global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __grid_constant__ Loss P)
+{
+    constexpr int E = BF16 ? 8 : 4, PER = LL_PIECE / 16 / LL_THREADS;                 // vectors of a piece to a thread
+    constexpr float LOG2E = 1.44269504f;
+    using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
+    extern __shared__ __align__(128) unsigned char ring[];
+    __shared__ __align__(8) unsigned long long bars[2 * LL_PIECES];
+    __shared__ int s_index[LS_MAX_K], abort_flag;
+    __shared__ float s_q[LS_MAX_K], s_loss[LL_WARPS];
+    __shared__ Part s_part[LL_WARPS], s_teach[LL_WARPS];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int nvec = P.m / E, pieces = (nvec * 16 + LL_PIECE - 1) / LL_PIECE;
+    auto full = [&](int s) { return smem_u32(&bars[s]); };
+    auto empty = [&](int s) { return smem_u32(&bars[LL_PIECES + s]); };
+    if (t == 0) {
+        for (int s = 0; s < LL_PIECES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), LL_WARPS); }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncthreads();
+    int slot = 0;
+    uint32_t ph = 0;
+    auto advance = [&] { if (++slot == LL_PIECES) { slot = 0; ph ^= 1u; } };
+    if (warp == LL_WARPS) {
+        if (lane == 0) {
+            bool ok = true;
+            int issued = 0;
+            for (long long row = blockIdx.x; row < P.rows && ok; row += gridDim.x) {
+                const unsigned char *src = (const unsigned char *)((const T *)P.scores + (size_t)row * P.ld);
+                for (int c = 0; c < pieces; ++c, advance()) {
+                    if (!(ok = mbar_wait(empty(slot), ph ^ 1u, &abort_flag))) break;
+                    const uint32_t bytes = (uint32_t)min(LL_PIECE, nvec * 16 - c * LL_PIECE);
+                    mbar_expect_tx(full(slot), bytes);
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(smem_u32(ring) + slot * LL_PIECE), "l"(src + (size_t)c * LL_PIECE), "r"(bytes), "r"(full(slot)) : "memory");
+                    if (issued < LL_PIECES) ++issued;
+                }
+            }
+            // nothing may land in shared memory after the block has gone: the last copy into every piece, with a bound of its own
+            int unused = 0, s = slot;
+            for (int q = 0; q < issued; ++q) {
+                if (--s < 0) { s = LL_PIECES - 1; ph ^= 1u; }
+                mbar_wait(full(s), ph, &unused);
+            }
+        }
+        return;
+    }
+    auto block_sync = [&] { asm volatile("bar.sync 1, %0;" ::"n"(LL_THREADS) : "memory"); };
+    bool ok = true;
+    const u64 c2 = pack2(P.c, P.c);
+    for (long long row = blockIdx.x; row < P.rows; row += gridDim.x) {
+        const float weight = P.weight ? P.weight[row] : 1.f;
+        int named = -1;
+        float logit = 0.f, score = 0.f;
+        if (t < P.k) {
+            named = P.index[(size_t)row * P.k + t];
+            if (P.logits) logit = P.logits[(size_t)row * P.k + t];
+        }
+        // ---- maximum and sum
+        const int slot0 = slot;
+        const uint32_t ph0 = ph;
+        Part part = {-INFINITY, 0.f};
+        for (int c = 0; c < pieces; ++c, advance()) {
+            ok = mbar_wait(full(slot), ph, &abort_flag) && ok;
+            uint4 x[PER];
+#pragma unroll
+            for (int v = 0; v < PER; ++v) {
+                const int j = v * LL_THREADS + t;
+                x[v] = BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u) : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+                if (c * (LL_PIECE / 16) + j < nvec) x[v] = *reinterpret_cast<const uint4 *>(ring + slot * LL_PIECE + j * 16);
+            }
+            float top = largest<BF16>(x[0]);
+#pragma unroll
+            for (int v = 1; v < PER; ++v) top = fmaxf(top, largest<BF16>(x[v]));
+            if (top > part.m) {
+                part.s *= ex2f((part.m - top) * P.c);                                // (of minus infinity: 0 times 0)
+                part.m = top;
+            }
+            const u64 at2 = pack2(finite_max(part.m), finite_max(part.m));
+            u64 sum[2] = {0ull, 0ull};
+#pragma unroll
+            for (int v = 0; v < PER; ++v)
+#pragma unroll
+                for (int i = 0; i < E / 2; ++i) sum[i & 1] = add2(sum[i & 1], exponentials(two<BF16>(x[v], i), at2, c2));
+            float a, b;
+            unpack2(add2(sum[0], sum[1]), a, b);
+            part.s += a + b;
+        }
+        part = join<32>(part, P.c);
+        // ---- the teacher
+        Part teach = {-INFINITY, 0.f};
+        if (named < 0 || named >= P.m) named = -1;
+        const float l0 = named >= 0 ? logit * P.inv_t : -INFINITY;
+        if (warp * 32 < P.k) {
+            teach.m = warp_max(l0);
+            teach.s = ex2f((l0 - finite_max(teach.m)) * LOG2E);
+#pragma unroll
+            for (int off = 16; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
+        }
+        if (lane == 0) { s_part[warp] = part; s_teach[warp] = teach; }
+        block_sync();
+        if (named >= 0) {
+            const int piece = slot0 + named / (LL_PIECE / (int)sizeof(T));
+            const T *at = reinterpret_cast<const T *>(ring + (piece < LL_PIECES ? piece : piece - LL_PIECES) * LL_PIECE) + named % (LL_PIECE / (int)sizeof(T));
+            score = BF16 ? __uint_as_float((uint32_t)*at << 16) : __uint_as_float((uint32_t)*at);
+        }
+        part = join<32>(lane < LL_WARPS ? s_part[lane] : Part{-INFINITY, 0.f}, P.c);
+        part.s = __shfl_sync(0xffffffffu, part.s, 0);
+        teach = join<32>(lane < LL_WARPS ? s_teach[lane] : Part{-INFINITY, 0.f}, LOG2E);
+        teach.s = __shfl_sync(0xffffffffu, teach.s, 0);
+        const bool live = teach.s != 0.f;                                             // (NaN, too)
+        const float teach_at = finite_max(teach.m), teach_inv = live ? 1.f / teach.s : 0.f;
+        float own_q = 0.f, sum = 0.f;
+        if (warp * 32 < P.k) {
+            const float log_all = __logf(teach.s) - __logf(part.s);
+            own_q = ex2f((l0 - teach_at) * LOG2E) * teach_inv;
+            if (own_q != 0.f) sum = own_q * ((l0 - teach_at) - (score - part.m) * P.inv_t - log_all);
+            if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
+#pragma unroll
+            for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        }
+        if (lane == 0) s_loss[warp] = ok ? sum : __uint_as_float(0x7fffffffu);
+        // ---- the gradient
+        const float w = weight * P.inv_t, a = w / part.s;
+        T *out = (T *)P.grad + (size_t)row * P.ldg;
+        const u64 at2 = pack2(part.m, part.m), f2 = pack2(a, a);
+        slot = slot0;
+        ph = ph0;
+        for (int c = 0; c < pieces; ++c, advance()) {
+            if (P.grad)
+#pragma unroll
+                for (int v = 0; v < PER; ++v) {
+                    const int j = v * LL_THREADS + t, at = c * (LL_PIECE / 16) + j;
+                    if (at >= nvec) break;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(ring + slot * LL_PIECE + j * 16);
+                    uint32_t r[4];
+#pragma unroll
+                    for (int i = 0; i < E / 2; ++i) {
+                        float p, q;
+                        unpack2(mul2(exponentials(two<BF16>(x, i), at2, c2), f2), p, q);
+                        if constexpr (BF16) r[i] = bf16x2(p, q);
+                        else { r[2 * i] = __float_as_uint(p); r[2 * i + 1] = __float_as_uint(q); }
+                    }
+                    if (!live) r[0] = r[1] = r[2] = r[3] = 0u;
+                    *reinterpret_cast<uint4 *>(out + (size_t)at * E) = make_uint4(r[0], r[1], r[2], r[3]);
+                }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty(slot));
+        }
+        block_sync();
+        if (t == 0) {
+#pragma unroll
+            for (int i = 1; i < LL_WARPS; ++i) sum += s_loss[i];
+            P.loss[row] = live ? sum : 0.f;
+        }
+        // named entries: each by the first of those that name its column
+        if (P.grad && live && named >= 0) {
+            float q = 0.f;
+            bool first = true;
+            for (int o = 0; o < P.k; ++o)
+                if (s_index[o] == named) {
+                    first &= o >= t;
+                    q += s_q[o];
+                }
+            if (first) {
+                const float g = ex2f((score - part.m) * P.c) * a - q * w;
+                out[named] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+            }
+        }
+    }
+}
+
 template <bool BF16, int TPR, int V, int C, bool EVEN>
 skb_status launch(const Loss &P, cudaStream_t st)
 {
@@ -399,6 +581,13 @@ skb_status launch_by_length(const Loss &P, long long vec, int sms, cudaStream_t 
     if (vec <= 32 * 4) return launch<BF16, 32, 4, 1, EVEN>(P, st);
     if (vec <= 32 * 8 && P.rows >= 8 * sms) return launch<BF16, 32, 8, 1, EVEN>(P, st);
     if (vec <= 128 * 4) return launch<BF16, 128, 4, 1, EVEN>(P, st);
+    if (vec > 256 * 8 && vec <= 512 * 8 && P.rows >= 2 * sms) return launch<BF16, 512, 8, 1, EVEN>(P, st);
+    if (EVEN && vec > 512 * 8 && vec <= LL_PIECES * (LL_PIECE / 16) && P.rows >= 4 * sms) {
+        constexpr int smem = LL_PIECES * LL_PIECE;
+        cudaFuncSetAttribute(loss_long_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        loss_long_kernel<BF16><<<sms, LL_THREADS + 32, smem, st>>>(P);
+        return op_launched("plan_loss");
+    }
     if (vec <= 256 * 8 * 8) {
         const int c = blocks(vec <= 256 * 8 ? 1 : vec <= 256 * 16 ? 2 : vec <= 256 * 32 ? 4 : 8);
         if (c == 1) return vec <= 256 * 4 ? launch<BF16, 256, 4, 1, EVEN>(P, st) : launch<BF16, 256, 8, 1, EVEN>(P, st);

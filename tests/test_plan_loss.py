@@ -104,6 +104,38 @@ def test_many_rows_of_middle_length(B, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,m", [("bfloat16", 32776), ("bfloat16", 40000), ("bfloat16", 98304), ("float32", 16388), ("float32", 20480), ("float32", 49152)])
+def test_many_long_rows_of_whole_vectors(B, dtype, m):
+    # more rows than blocks take at once, pieces that the last of them does not fill; every kind of entry among them
+    import torch
+    rows, k = 700, 40
+    scores, index, t, weight = inputs(rows, m, k, getattr(torch, dtype), m)
+    index[1] = 3
+    index[2] = -1
+    index[3, 5:] = -1
+    t[4] = -float("inf")
+    scores[5, 10:] = -float("inf")
+    index[5] %= 10
+    scores[6] = torch.finfo(scores.dtype).min
+    want, wgrad = B.plan_loss(scores.cuda(), index.cuda(), t.cuda(), weight=weight.cuda(), grad=True)
+    pick = torch.cat((torch.arange(16), torch.arange(rows - 160, rows)))
+    compare(want[pick], wgrad[pick], scores[pick], index[pick], t[pick], 1.0, weight[pick])
+    assert not torch.isnan(want).any() and not torch.isnan(wgrad).any()
+    assert torch.equal(B.plan_loss(scores.cuda(), index.cuda(), t.cuda()), want)
+    s = scores.cuda()
+    loss, g = B.plan_loss(s, index.cuda(), t.cuda(), weight=weight.cuda(), grad=s)
+    assert torch.equal(loss, want) and torch.equal(g, wgrad)
+    # a NaN, plus infinity, nothing but minus infinity: their rows alone
+    scores[8, m - 1], scores[9, 0], scores[11] = float("nan"), float("inf"), -float("inf")
+    loss, g = B.plan_loss(scores.cuda(), index.cuda(), t.cuda(), weight=weight.cuda(), grad=True)
+    bad = torch.tensor([8, 9, 11])
+    assert torch.isnan(loss[bad]).all() and torch.isnan(g[bad]).all()
+    rest = torch.ones(rows, dtype=torch.bool)
+    rest[bad] = False
+    assert torch.equal(loss[rest], want[rest]) and torch.equal(g[rest], wgrad[rest])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("k", [1, 2, 31, 32, 33, 64, 100, 255, 256])
 @pytest.mark.parametrize("m", [300, 1500, 40000])
 def test_numbers_of_named_entries(B, k, m):
