@@ -77,6 +77,13 @@ __device__ __forceinline__ void dots_mma(uint32_t acc, uint64_t a, uint64_t b, u
                      "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
                      ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
 }
+// one thread of a warp, the same one each time
+__device__ __forceinline__ bool one_thread()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 // 128 points' words of four scales, 512 bytes of shared memory, into four columns of tensor memory, the same for all four
 // quarters of the lanes.  Rows of 16 bytes, eight to a group of 128 bytes, no swizzle.
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr)
@@ -207,53 +214,65 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 if (issued >> q & 1u) mbar_wait(bar(FULL + q), issued >> (q + 16) & 1u, &unused);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int s = 0, ph = 0, b = 0, bph = 1;
-            bool ok = true;
-            for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-                for (int c = 0; c < chunks; ++c) {
-                    const bool starts = c % DT_PART<KIND> == 0, ends = (c + 1) % DT_PART<KIND> == 0 || c + 1 == chunks;
-                    if (starts) {
-                        if (!(ok = mbar_wait(bar(ACC_FREE + b), bph, &abort_flag))) break;
-                        tc_fence_after();
-                    }
-                    const uint32_t acc = tmem + b * DT_BN;
-                    if (!(ok = mbar_wait(bar(FULL + s), ph, &abort_flag))) break;
-                    const uint32_t sf = tmem + DT_SF_COL + s * DT_SF_STRIDE;
+        // (the whole warp walks through the chunks, so that descriptors are uniform; one thread issues: a thread by itself takes longer to form them than the
+        // instructions take)
+        int s = 0, ph = 0, b = 0, bph = 1;
+        bool ok = true;
+        for (long long t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+            for (int c = 0; c < chunks; ++c) {
+                const bool starts = c % DT_PART<KIND> == 0, ends = (c + 1) % DT_PART<KIND> == 0 || c + 1 == chunks;
+                if (starts) {
+                    ok = mbar_wait(bar(ACC_FREE + b), bph, &abort_flag);
+                    if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                }
+                ok = mbar_wait(bar(FULL + s), ph, &abort_flag);
+                if constexpr (SCALED) ok = ok && mbar_wait(bar(SCALES + s), ph, &abort_flag);
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                tc_fence_after();
+                const uint32_t acc = tmem + b * DT_BN, sf = tmem + DT_SF_COL + s * DT_SF_STRIDE;
+                const uint64_t da = tc_desc(tile_a(s)), db = tc_desc(tile_a(s) + DT_TILE);
+                const int left = P.row_bytes - c * 128;           // 32 bytes of a point to an instruction
+                if (one_thread()) {
                     if constexpr (SCALED) {
-                        if (!(ok = mbar_wait(bar(SCALES + s), ph, &abort_flag))) break;
-                        tc_fence_after();
 #pragma unroll
                         for (int q = 0; q < WORDS; ++q) {
                             scales_to_tmem(sf + 4 * q, sf_a(s) + 512 * q);
                             scales_to_tmem(sf + 16 + 4 * q, sf_a(s) + SF + 512 * q);
                         }
-                    } else tc_fence_after();
-                    const uint64_t da = tc_desc(tile_a(s)), db = tc_desc(tile_a(s) + DT_TILE);
-                    const int left = P.row_bytes - c * 128;       // 32 bytes of a point to an instruction
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (32 * q >= left) break;
+                    }
+                    auto one = [&](int q, uint32_t accumulate) {
                         const int word = KIND == SKB_NV4 ? q : KIND == FMT_MX8 ? 0 : q / 2;
                         // which of a word's four scales: the first or second two, or the chunk's
                         const uint32_t part = KIND == SKB_MX4 ? (uint32_t)(q & 1) * 2u : KIND == FMT_MX8 ? (uint32_t)(c & 3) : 0u;
-                        dots_mma<KIND>(acc, da + 2 * q, db + 2 * q, dots_idesc<KIND>() | part << 29 | part << 4, sf + 4 * word, sf + 16 + 4 * word,
-                                       !starts || q != 0);
+                        dots_mma<KIND>(acc, da + 2 * q, db + 2 * q, dots_idesc<KIND>() | part << 29 | part << 4, sf + 4 * word, sf + 16 + 4 * word, accumulate);
+                    };
+                    one(0, !starts);
+                    if (left >= 128) {
+#pragma unroll
+                        for (int q = 1; q < 4; ++q) one(q, 1u);
+                    } else {
+#pragma unroll
+                        for (int q = 1; q < 4; ++q)
+                            if (32 * q < left) one(q, 1u);
                     }
                     tc_commit(bar(EMPTY + s));
-                    if (++s == DT_STAGES) { s = 0; ph ^= 1; }
-                    if (ends) {
-                        tc_commit(bar(ACC + b));
-                        b ^= 1;
-                        if (b == 0) bph ^= 1;
-                    }
+                    if (ends) tc_commit(bar(ACC + b));
+                }
+                __syncwarp();
+                if (++s == DT_STAGES) { s = 0; ph ^= 1; }
+                if (ends) {
+                    b ^= 1;
+                    if (b == 0) bph ^= 1;
                 }
             }
-            // what was issued is over before tensor memory is given back
+        }
+        // what was issued is over before tensor memory is given back
+        if (one_thread()) {
             tc_commit(bar(LAST));
             int unused = 0;
             mbar_wait(bar(LAST), 0, &unused);
         }
+        __syncwarp();
     } else if (warp < 6) {
         if constexpr (SCALED) {
             const int op = (warp - 2) & 1, turn = (warp - 2) >> 1;     // operand; every other chunk
