@@ -8,9 +8,8 @@
 // thread, raw) until its maximum and sum are known; then the gradient is written.  So memory bounds it, and the latencies of what a row
 // needs besides: 65536 rows of 1024 in bf16 take 53 us for 270 MB (78 % of the measured copy rate), of 64 still 43.  Exponentials are taken against the
 // thread's own maximum for the sum; short rows keep them, others take them again against the row's: that is one barrier a row instead of two, and no fp32
-// copies in registers.  What a row is given goes by its length: a warp (up to 128 vectors, or 256 where there are many rows: 32768 rows of 2048 in bf16 99 us
-// with four warps to a row, 50 so), four, eight or 16 warps, or a cluster of up to eight blocks, whose maxima and sums meet in distributed shared memory; many
-// long rows stay in shared memory (loss_long_kernel); rows longer than what a cluster's registers hold are read twice, the second time from L2 (a row
+// copies in registers.  What a row is given goes by its length (launch_by_length): a warp, four, eight or 16 warps, or a cluster of up to eight blocks, whose
+// maxima and sums meet in distributed shared memory; long rows, a device full of them, stay in shared memory (loss_long_kernel); rows longer than what a cluster's registers hold are read twice, the second time from L2 (a row
 // is at most 1 MB).  A row is reduced in a fixed order, so results do not change from call to call.
 //
 // The named entries, a thread to each, are fetched before the row and their softmax is made while it is on its way.  Their gradients are written after
@@ -578,11 +577,14 @@ skb_status launch_by_length(const Loss &P, long long vec, int sms, cudaStream_t 
         while (c < 8 && P.rows * c < 2 * sms && vec / (2 * c) >= 512) c *= 2;
         return c;
     };
+    // (us, rows of bf16 as the line says / as the next ones would: 256 vectors by a warp or by four, 1184 rows 10 / 10, 8192 20 / 28, 32768 51 / 89; 4096 vectors by a
+    // block or by two and more, 148 rows 11 / 13, 592 21 / 26, 4096 92 / 110; 8192 vectors through shared memory or by a cluster, 100 rows 16 / 14, 148 rows
+    // 16 / 19, 592 39 / 43, 4096 199 / 218; 12288 vectors, 1184 rows 92 / 113)
     if (vec <= 32 * 4) return launch<BF16, 32, 4, 1, EVEN>(P, st);
     if (vec <= 32 * 8 && P.rows >= 8 * sms) return launch<BF16, 32, 8, 1, EVEN>(P, st);
     if (vec <= 128 * 4) return launch<BF16, 128, 4, 1, EVEN>(P, st);
-    if (vec > 256 * 8 && vec <= 512 * 8 && P.rows >= 2 * sms) return launch<BF16, 512, 8, 1, EVEN>(P, st);
-    if (EVEN && vec > 512 * 8 && vec <= LL_PIECES * (LL_PIECE / 16) && P.rows >= 4 * sms) {
+    if (vec > 256 * 8 && vec <= 512 * 8 && P.rows >= sms) return launch<BF16, 512, 8, 1, EVEN>(P, st);
+    if (EVEN && vec > 512 * 8 && vec <= LL_PIECES * (LL_PIECE / 16) && P.rows >= sms) {
         constexpr int smem = LL_PIECES * LL_PIECE;
         cudaFuncSetAttribute(loss_long_kernel<BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         loss_long_kernel<BF16><<<sms, LL_THREADS + 32, smem, st>>>(P);

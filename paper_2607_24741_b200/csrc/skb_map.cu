@@ -18,7 +18,7 @@
 //   warps 4-7   images: tensor memory -> fp32 sums in registers, a thread to a dimension of every 128
 //   warp 8      loads by TMA: slots of 128 targets by 128 dimensions (16 KB, 128-byte swizzle, targets past the end are zeros)
 //   warp 9      scores' matrix instructions, warp 11 the images': either waits for what it needs
-//   warp 10     targets' scales and terms, a tile ahead
+//   warp 10     targets' scales and terms, up to six tiles ahead
 // Several blocks that share a lane's bank leave (maximum, sum, image), which map_join_kernel adds up.  Every wait is bounded (skb_tmem.cuh): one that
 // runs out ends all roles, and the block's images are NaN.
 #include <cuda.h>
@@ -143,8 +143,8 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");               // (the parts' join waits for all of this grid's writes itself)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     // (values deeper than what a block has room for: further blocks, which form the scores again)
-    const int qgroups = (P.n + NQ - 1) / NQ, z = blockIdx.y / qgroups, v0 = z * vblocks;
-    const int split = blockIdx.x, q0 = (blockIdx.y - z * qgroups) * NQ, w = blockIdx.z, nq = min(NQ, P.n - q0);
+    const int qgroups = (P.n + NQ - 1) / NQ, z = blockIdx.x / qgroups, v0 = z * vblocks;
+    const int split = blockIdx.y, q0 = (blockIdx.x - z * qgroups) * NQ, w = blockIdx.z, nq = min(NQ, P.n - q0);
     const MapRows L = map_rows_layout<NQ>(P.d, vblocks, yslots, vslots);
     const int nby = L.nby, nb = min(vblocks, (P.dv + 127) / 128 - v0);
     const uint32_t base = smem_u32(smem);
@@ -734,7 +734,7 @@ struct RowsShape {
 template <int NQ>
 RowsShape rows_shape(int d, int dv, bool own, long long tiles)
 {
-    const int nby = (d + 127) / 128, nb = (dv + 127) / 128, most = NQ == 16 ? 4 : MR_MAX_BLOCKS;
+    const int nby = (d + 127) / 128, nb = (dv + 127) / 128, most = NQ == 16 ? 2 : MR_MAX_BLOCKS;
     RowsShape r = {};
     r.nq = NQ;
     // (chunks of values of their own are of four blocks, a word of scales, or whole)
@@ -754,36 +754,41 @@ RowsShape rows_shape(int d, int dv, bool own, long long tiles)
     r.yslots = (int)all - r.vslots;
     return r;
 }
-// (a tile's blocks have a slot each: eight queries leave room for 1024 dimensions of bank and values, sixteen do not)
-RowsShape rows_shape(int n, int d, int dv, bool own, long long tiles)
-{
-    if (n > 8 && (own || dv <= 512)) {
-        const RowsShape r = rows_shape<16>(d, dv, own, tiles);
-        if (r.yslots >= (d + 127) / 128) return r;
-    }
-    return rows_shape<8>(d, dv, own, tiles);
-}
-
 template <int NQ, int UNITS>
 skb_status launch_rows(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, const RowsShape &r, cudaStream_t st)
 {
     const MapRows L = map_rows_layout<NQ>(P.d, r.vblocks, r.yslots, r.vslots);
     cudaFuncSetAttribute(map_rows_kernel<NQ, UNITS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L.bytes);
-    map_rows_kernel<NQ, UNITS><<<dim3(P.splits, (P.n + NQ - 1) / NQ * r.chunks, P.W), MR_THREADS<NQ, UNITS>, L.bytes, st>>>(ty, tv, P, r.yslots, r.vslots, r.vblocks);
+    map_rows_kernel<NQ, UNITS><<<dim3((P.n + NQ - 1) / NQ * r.chunks, P.splits, P.W), MR_THREADS<NQ, UNITS>, L.bytes, st>>>(ty, tv, P, r.yslots, r.vslots, r.vblocks);
     return op_launched("map");
 }
-skb_status launch_rows_by_depth(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, cudaStream_t st)
+skb_status launch_rows_by_depth(const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, int nq, cudaStream_t st)
 {
-    const RowsShape r = rows_shape(P.n, P.d, P.dv, P.own_values != 0, ((P.m + MR_T - 1) / MR_T + P.splits - 1) / P.splits);
-    const bool few = r.nq == 8;
-    if (r.vblocks <= 1) return few ? launch_rows<8, 1>(ty, tv, P, r, st) : launch_rows<16, 1>(ty, tv, P, r, st);
-    if (r.vblocks <= 2) return few ? launch_rows<8, 2>(ty, tv, P, r, st) : launch_rows<16, 2>(ty, tv, P, r, st);
-    if (r.vblocks <= 4) return few ? launch_rows<8, 4>(ty, tv, P, r, st) : launch_rows<16, 4>(ty, tv, P, r, st);
+    const long long tiles = ((P.m + MR_T - 1) / MR_T + P.splits - 1) / P.splits;
+    if (nq == 16) {
+        const RowsShape r = rows_shape<16>(P.d, P.dv, P.own_values != 0, tiles);
+        return r.vblocks <= 1 ? launch_rows<16, 1>(ty, tv, P, r, st) : launch_rows<16, 2>(ty, tv, P, r, st);
+    }
+    const RowsShape r = rows_shape<8>(P.d, P.dv, P.own_values != 0, tiles);
+    if (r.vblocks <= 1) return launch_rows<8, 1>(ty, tv, P, r, st);
+    if (r.vblocks <= 2) return launch_rows<8, 2>(ty, tv, P, r, st);
+    if (r.vblocks <= 4) return launch_rows<8, 4>(ty, tv, P, r, st);
     return launch_rows<8, 8>(ty, tv, P, r, st);
 }
 
-// queries up to which the matrix unit's tiles of 128 are too empty
+// What a call is shared out by: the kernel, queries to a block of map_rows_kernel, parts of a lane's bank.  The first two go by the sizes alone, as a
+// B200's SMs take them, so that the workspace does not depend on the device.
+constexpr int MAP_SMS = 148;
+// Queries up to which the tiles of 128 queries are too empty to be worth the staging (us, here / with tiles; W, m, d, dv):
+//      queries                     16          32          33          48          64
+//      8, 16384, 512           50 / 105    83 / 112   120 / 112   114 / 114   155 / 120
+//      32, 8192, 128, 64       42 / 79     60 / 81     95 / 83     90 / 83     95 / 85
+//      64, 1024, 512           32 / 56     56 / 58     76 / 58     80 / 58    103 / 58
+//      64, 1024, 128           24 / 32     25 / 34     40 / 34     42 / 38     43 / 40
 constexpr int MAP_ROWS_MAX = 32;
+// ... and beyond them while a block has no more than so many tiles (24, 333, 200, 96: 48 queries, three tiles, 16 / 22; with eight queries to a block 64 would
+// be six tiles, 25 / 22; 1, 2000, 64: 128 queries, two tiles, 15 / 24)
+constexpr int MAP_ROWS_STEPS = 4;
 
 const char *map_refused(int W, int n, int m, int d, int dv)
 {
@@ -792,21 +797,37 @@ const char *map_refused(int W, int n, int m, int d, int dv)
     if (d > CLOUD8_MAX_D || dv > CLOUD8_MAX_D || dv < 0) return "d and dv must be at most 1024";
     return nullptr;
 }
-// Which kernel, and into how many parts a lane's bank goes: enough to fill the device, of a few tiles at least.
 struct MapPlan {
     bool tiles;
-    int splits;
+    int nq, splits;
 };
+// enough parts to fill the device, of a few tiles at least
+int map_splits(long long blocks, long long tiles, int sms)
+{
+    const long long s = min(sms / blocks, tiles / 2);
+    return (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+}
+long long rows_blocks(const RowsShape &r, int W, int n) { return (long long)W * ((n + r.nq - 1) / r.nq) * r.chunks; }
+// tiles that an SM gets through, one after the other
+long long rows_steps(const RowsShape &r, int W, int n, long long tiles)
+{
+    const long long blocks = rows_blocks(r, W, n), splits = map_splits(blocks, tiles, MAP_SMS);
+    return (blocks * splits + MAP_SMS - 1) / MAP_SMS * ((tiles + splits - 1) / splits);
+}
 MapPlan map_plan(int W, int n, int m, int d, int dv, bool own_values, int sms)
 {
+    const long long tiles = (m + MR_T - 1) / MR_T;
+    RowsShape r = rows_shape<8>(d, dv, own_values, tiles);
+    // A tile of sixteen queries takes half as long again as one of eight, of images above 256 dimensions, for which registers leave one group of warps to the
+    // softmax, twice as long: those have eight.  (32 x 8192 x 128, 12 queries: 40 us with sixteen, 50 with eight; 24 x 333 x 200, 24 queries: 20 and 16.)
+    if (n > 8 && dv <= 256) {
+        const RowsShape r16 = rows_shape<16>(d, dv, own_values, tiles);
+        if (r16.yslots >= (d + 127) / 128 && 3 * rows_steps(r16, W, n, tiles) <= 2 * rows_steps(r, W, n, tiles)) r = r16;
+    }
     MapPlan p;
-    const RowsShape rows = rows_shape(n, d, dv, own_values, 1 << 20);
-    p.tiles = n > MAP_ROWS_MAX && d <= MAP_TILES_MAX_D;
-    const long long blocks = p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : (long long)W * ((n + rows.nq - 1) / rows.nq) * rows.chunks;
-    const long long tiles = p.tiles ? (m + 127) / 128 : (m + MR_T - 1) / MR_T;
-    long long s = sms / blocks;
-    if (s > tiles / 2) s = tiles / 2;
-    p.splits = (int)(s < 1 ? 1 : s > 128 ? 128 : s);
+    p.nq = r.nq;
+    p.tiles = d <= MAP_TILES_MAX_D && n > MAP_ROWS_MAX && rows_steps(r, W, n, tiles) > MAP_ROWS_STEPS;
+    p.splits = map_splits(p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : rows_blocks(r, W, n), tiles, sms);
     return p;
 }
 size_t pad256(size_t b) { return (b + 255) / 256 * 256; }
@@ -845,6 +866,9 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
         return op_fail(SKB_ERR_WORKSPACE, "arrays must be aligned to their types");
     const int depth = v ? dv : d;
     if (workspace_bytes < map_workspace(W, n, m, d, depth, v != nullptr)) return op_fail(SKB_ERR_WORKSPACE, "workspace too small");
+    // (a block's queries may be read after another block has written images)
+    const uintptr_t x0 = (uintptr_t)x, out0 = (uintptr_t)out, queries = (uintptr_t)W * n;
+    if (x0 < out0 + 2 * queries * depth && out0 < x0 + 2 * queries * d) return op_fail(SKB_ERR_VALUE, "images cannot take the place of the queries");
     int dev = 0, sms = 0;
     cudaGetDevice(&dev);
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");
@@ -862,7 +886,7 @@ extern "C" skb_status sinkhorn_cloud8_map(const void *x, const void *y, const do
     CUtensorMap ty, tv;
     if (!plan.tiles && (!points_map(&ty, P.y.codes, P.y.cb, m, W, MR_T) || !points_map(&tv, P.v.codes, P.v.cb, m, W, MR_T)))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, sms, (cudaStream_t)stream) : launch_rows_by_depth(ty, tv, P, (cudaStream_t)stream);
+    const skb_status rc = plan.tiles ? launch_map_tiles(P, room, sms, (cudaStream_t)stream) : launch_rows_by_depth(ty, tv, P, plan.nq, (cudaStream_t)stream);
     if (rc != SKB_OK || P.splits == 1) return rc;
     // (it may start, and wait, before the parts are all there)
     cudaLaunchConfig_t cfg = {};

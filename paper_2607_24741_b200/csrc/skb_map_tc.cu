@@ -36,7 +36,7 @@ namespace {
 constexpr int MT_SOFT = 8, MT_LOAD = MT_SOFT, MT_MMA = MT_SOFT + 1, MT_THREADS = (MT_SOFT + 2) * 32;
 constexpr uint32_t MT_CHUNK = 128 * 128, MT_BLOCK = 2 * MT_CHUNK;         // 128 points by 64, 128 dimensions of bf16
 constexpr int MT_MAX_STAGES = 8;
-constexpr uint32_t MT_MISC = 3072;
+constexpr uint32_t MT_MISC = 3 * 1024;
 constexpr float MT_SLACK = 8.f;
 
 // D fp32, A and B bf16, 128 queries (a pair of blocks: 256) by 128

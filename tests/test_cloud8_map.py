@@ -19,7 +19,13 @@ def formula(x, y, g, eps, v, lengths):
 
     An exponent is off by (d/32 + 8) U of what it is made of; a weight by that (twice: itself and the sum), by what its rounding to eight
     bits loses, 2^-9 (half a step of bf16's is 2^-9 of the upper end of a binade, 2^-8 of the lower: 2^-8), and by 2^-16 for sums and
-    exponentials in fp32; what a tile's values lose is 2^-24 of the largest; the result is rounded to bf16, 2^-8 of itself."""
+    exponentials in fp32; the result is rounded to bf16, 2^-8 of itself.
+
+    Where weights are two e4m3 numbers, a weight w <= 1 (of the tile's largest) times its value's power of two 2^e is 256 w 2^(e - E), E the largest e of
+    the 128 targets of the tile.  The second number has steps of 2^-9, a sixteenth each, so what is left of it is off by up to 2^-14 whatever its size,
+    and by no more than itself.  Times the code (448 at most) and 2^E / 256 that is 448 2^-22 2^E; the tile's largest value of these 128 dimensions is above
+    224 2^E: 2^-21 of it, and no more than the weight times the value; both times the tile's largest weight of all.  (Blocks' powers of two end at
+    2^-100; the values here are far above.)"""
     import torch
     x, y, v = x.double(), y.double(), v.double()
     W, n, d = x.shape
@@ -39,7 +45,13 @@ def formula(x, y, g, eps, v, lengths):
     size = (d / 32 + 8) * U * (x.square().sum(2)[:, :, None] + y.square().sum(2)[:, None, :] + gz.abs()[:, None, :]) / e
     size = torch.where(masked[:, None, :], 0.0, size)
     mean = (p * size).sum(2)
-    err = ((p * (size + mean[:, :, None] + 2.0 ** -8 + 2.0 ** -16)) @ v.abs() + 2.0 ** -24 * v.abs().amax((1, 2), keepdim=True) + 2.0 ** -8 * out.abs())
+    err = (p * (size + mean[:, :, None] + 2.0 ** -8 + 2.0 ** -16)) @ v.abs() + 2.0 ** -8 * out.abs()
+    for j in range(0, m, 128):
+        pt = p[:, :, j:j + 128]
+        for k in range(0, v.shape[2], 128):
+            most = v[:, j:j + 128, k:k + 128].abs().amax(2)                                    # of each target
+            cut = 2.0 ** -21 * most.amax(1)[:, None, None] * pt.amax(2, keepdim=True)
+            err[:, :, k:k + 128] += torch.minimum(cut, pt * most[:, None, :]).sum(2, keepdim=True)
     lerr = mean + 2.0 ** -16 + 2 * U * lse.abs() + size.amax(2) * 2.0 ** -3
     return out, lse, err, lerr
 
@@ -168,6 +180,20 @@ def test_scales_far_apart_sharp_rows_and_far_reference_points(B, n):
 
 
 @pytest.mark.gpu
+def test_the_most_queries_of_the_deepest_points(B):
+    # more blocks of queries and values than a grid's second dimension takes
+    import torch
+    x, y, g, eps, v = inputs(1, 5, 3, 1024, 1024)
+    y8, v8 = B.cloud8_pack(y.cuda()), B.cloud8_pack(v.cuda())
+    want, wl = B.cloud8_map(x.cuda(), y8, g.cuda(), eps.cuda(), v8, lse=True)
+    n = 262143
+    many = x.cuda()[:, torch.arange(n, device="cuda") % 5]
+    out, lse = B.cloud8_map(many, y8, g.cuda(), eps.cuda(), v8, lse=True)
+    for i in range(5):
+        assert torch.equal(out[0, i::5], want[0, i].expand(out[0, i::5].shape)) and (lse[0, i::5] == wl[0, i]).all()
+
+
+@pytest.mark.gpu
 def test_long_banks_are_split_and_every_part_counts(B):
     import torch
     for n, m, d, dv in ((1, 40000, 64, 0), (5, 20011, 128, 32), (20, 9000, 40, 0), (130, 12001, 64, 16)):
@@ -265,6 +291,9 @@ def test_sizes_and_refusals_without_a_gpu(B):
     for bad in (dict(y=p(128)), dict(v=p(128), dv=4), dict(work=p(16)), dict(x=p(257)), dict(out=p(257)), dict(g=p(260)), dict(eps=p(258)), dict(lse=p(258)),
                 dict(lengths=p(258)), dict(size=0)):
         assert call(**bad) == 4, bad
+    # images over the queries, or over some of them
+    for bad in (dict(), dict(x=p(1024), out=p(1024 + 2 * 16 - 2)), dict(x=p(1024), out=p(1024 - 2 * 16 + 2)), dict(n=4, x=p(1024), v=one, dv=8, out=p(1024 - 2 * 4 * 8 + 2))):
+        assert call(**bad) == 3, bad
     with pytest.raises(ValueError):
         B.cloud8_map(torch.zeros(1, 1, 16, dtype=torch.bfloat16), torch.zeros(1, 8, 16), None, torch.ones(1))
 
@@ -283,5 +312,7 @@ def test_refusals_on_the_device(B):
                dict(out=torch.zeros(2, 3, 8, device="cuda")), dict(out=torch.zeros(2, 3, 9, dtype=torch.bfloat16, device="cuda"))):
         with pytest.raises(ValueError):
             B.cloud8_map(x, y8, g, eps, v8, **kw)
+    with pytest.raises(B.SkbError):
+        B.cloud8_map(x, y8, g, eps, out=x)
     with pytest.raises(B.SkbError):
         B.cloud8_map(torch.zeros(1, 0, 32, dtype=torch.bfloat16, device="cuda"), B.cloud8_pack(y[:1]), g[:1], eps[:1])
