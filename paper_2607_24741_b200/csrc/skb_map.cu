@@ -126,8 +126,8 @@ __host__ __device__ inline MapRows map_rows_layout(int d, int nb, int yslots, in
     L.p = L.x + (uint32_t)(L.nby * MR_ROWS<NQ>) * 128;
     L.scales = L.p + 2 * (uint32_t)(L.nb * 2 * NQ) * 128;
     L.small = L.scales + (MR_AHEAD + 1) * (uint32_t)L.words * 512;
-    // terms, values' scales, tops, maxima, sums, lengths, barriers
-    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4 + 4 * NQ * 4) + 2 * 4 * NQ * 4 + 2 * NQ * 4 + NQ * 8 + 64 * 8 + 16;
+    // terms, values' scales, maxima, factors, tops, sums, runs, lengths, barriers
+    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4 + 4 * NQ * 4) + 12 * NQ * 16 + 2 * 4 * NQ * 4 + 2 * NQ * 4 + NQ * 8 + 64 * 8 + 16;
     const uint32_t used = 2 * MR_SCOLS<NQ> + 2 * (uint32_t)(L.nb * 2 * NQ) + 12 * (uint32_t)L.words;
     L.columns = 32;
     while (L.columns < used) L.columns *= 2;
@@ -151,8 +151,9 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
     float *terms = reinterpret_cast<float *>(smem + L.small);                        // [MR_AHEAD][128]
     uint2 *vscales = reinterpret_cast<uint2 *>(terms + MR_AHEAD * 128);              // [MR_AHEAD][128]
     float *maxima = reinterpret_cast<float *>(vscales + MR_AHEAD * 128);             // [MR_AHEAD][4][NQ]
-    uint32_t *tops = reinterpret_cast<uint32_t *>(maxima + MR_AHEAD * 4 * NQ);                  // [MR_AHEAD][8]
-    float *sums = reinterpret_cast<float *>(tops + MR_AHEAD * MR_MAX_BLOCKS);                                                  // [2][4][NQ]
+    float4 *factors = reinterpret_cast<float4 *>(maxima + MR_AHEAD * 4 * NQ);        // [12][NQ]: each warp's own
+    uint32_t *tops = reinterpret_cast<uint32_t *>(factors + 12 * NQ);                // [MR_AHEAD][8]
+    float *sums = reinterpret_cast<float *>(tops + MR_AHEAD * MR_MAX_BLOCKS);        // [2][4][NQ]
     float *runs = sums + 8 * NQ;                                                     // [2][NQ]
     double *lengths2 = reinterpret_cast<double *>(runs + 2 * NQ);                        // [NQ]
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(lengths2 + NQ);
@@ -302,9 +303,10 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
         const int group = warp >> 3, part = warp & 3, p = part * 32 + lane;          // every other tile's
         const uint32_t lanes = (uint32_t)(part * 32) << 16;
         const float kx = (float)(2.0 * k);
-        float run[NQ], sum[NQ];
+        float4 *own = factors + (4 * group + part) * NQ;
+        float run = -INFINITY, sum[NQ];                                              // run: of the query that is the lane's number
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) { run[q] = -INFINITY; sum[q] = 0.f; }
+        for (int q = 0; q < NQ; ++q) sum[q] = 0.f;
         bool ok = starts;
         for (int t = group; t < nt && starts; t += GROUPS) {
             const int b = t & 1;
@@ -356,27 +358,26 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             ok = ok && mbar_wait(bar(DFULL + b), ph ^ 1u, ab);
             ok = all_softmax(ok, group ? 4 : 1);
             if (!ok) break;
+            // a lane to a query: the tile's largest exponent, and what the sums so far and the tile's are multiplied by
+            if (lane < NQ) {
+                const float *mp = maxima + 4 * c4 * NQ + lane;
+                const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run, top), ref = now == -INFINITY ? 0.f : now;
+                own[lane] = make_float4(top == -INFINITY ? 0.f : top, ex2f(run - ref), ex2f(top - ref), 0.f);
+                run = now;
+            }
+            __syncwarp();
             unsigned char *weights = smem + L.p + b * (vblocks * 2 * NQ) * 128 + (p & 15);
 #pragma unroll
             for (int q = 0; q < NQ; q += 4) {
                 if (q >= nq) break;
-                float top[4], e[4];
-                {
-                    const float4 *mp = reinterpret_cast<const float4 *>(maxima + 4 * c4 * NQ + q);
-                    const float4 m0 = mp[0], m1 = mp[NQ / 4], m2 = mp[NQ / 2], m3 = mp[3 * NQ / 4];
-                    top[0] = fmaxf(fmaxf(m0.x, m1.x), fmaxf(m2.x, m3.x));
-                    top[1] = fmaxf(fmaxf(m0.y, m1.y), fmaxf(m2.y, m3.y));
-                    top[2] = fmaxf(fmaxf(m0.z, m1.z), fmaxf(m2.z, m3.z));
-                    top[3] = fmaxf(fmaxf(m0.w, m1.w), fmaxf(m2.w, m3.w));
-                }
+                float e[4];
 #pragma unroll
                 for (int h = 0; h < 4; ++h) {
+                    const float4 f = own[q + h];
                     // (tile's maximum plus infinity: the exponential is NaN, and so is what follows from it)
-                    e[h] = ex2f(arg[q + h] - (top[h] == -INFINITY ? 0.f : top[h]));
-                    const float now = fmaxf(run[q + h], top[h]), ref = now == -INFINITY ? 0.f : now;
-                    sum[q + h] = fmaf(sum[q + h], ex2f(run[q + h] - ref), e[h] * ex2f(top[h] - ref));
-                    run[q + h] = now;
-                                    }
+                    e[h] = ex2f(arg[q + h] - f.x);
+                    sum[q + h] = fmaf(sum[q + h], f.y, e[h] * f.z);
+                }
 #pragma unroll
                 for (int u = 0; u < UNITS; ++u) {
                     if (u >= nb) break;
@@ -403,8 +404,8 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
 #pragma unroll
             for (int off = 16; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
             if (lane == 0) sums[(4 * group + part) * NQ + q] = s;
-            if (p == 0) runs[group * NQ + q] = run[q];
         }
+        if (p < NQ) runs[group * NQ + p] = run;
         asm volatile("bar.sync 2, %0;" ::"n"(128 + 128 * GROUPS) : "memory");
         if (tid < nq) {
             const size_t r = (size_t)w * P.n + q0 + tid;
@@ -417,13 +418,12 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
     } else if (warp < 8) {
         // ---- images: a thread to a dimension of every block
         const uint32_t lanes = (uint32_t)((warp - 4) * 32) << 16;
-        float out[UNITS][NQ], run[NQ];
+        float4 *own = factors + (4 + warp) * NQ;
+        float out[UNITS][NQ], run = -INFINITY;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            run[q] = -INFINITY;
+        for (int u = 0; u < UNITS; ++u)
 #pragma unroll
-            for (int u = 0; u < UNITS; ++u) out[u][q] = 0.f;
-        }
+            for (int q = 0; q < NQ; ++q) out[u][q] = 0.f;
         bool ok = starts;
         for (int t = 0; t < nt && ok; ++t) {
             const int b = t & 1;
@@ -435,14 +435,22 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             if (!ok) break;
             tc_fence_after();
             // what the images so far and the tile's are multiplied by
+            __syncwarp();
+            if (lane < NQ) {
+                const float *mp = maxima + 4 * (t % MR_AHEAD) * NQ + lane;
+                const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run, top), ref = now == -INFINITY ? 0.f : now;
+                reinterpret_cast<float2 *>(own)[lane] = make_float2(ex2f(run - ref), ex2f(top - ref) * 0.00390625f);
+                run = now;
+            }
+            __syncwarp();
             float before[NQ], of_tile[NQ];
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                const float *mp = maxima + 4 * (t % MR_AHEAD) * NQ + q;
-                const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run[q], top), ref = now == -INFINITY ? 0.f : now;
-                before[q] = ex2f(run[q] - ref);
-                of_tile[q] = ex2f(top - ref) * 0.00390625f;
-                run[q] = now;
+            for (int q = 0; q < NQ; q += 2) {
+                const float4 f = own[q / 2];
+                before[q] = f.x;
+                of_tile[q] = f.y;
+                before[q + 1] = f.z;
+                of_tile[q + 1] = f.w;
             }
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
