@@ -136,48 +136,58 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
                  ::"r"(dst), "l"(src), "r"(bytes), "r"(mbar) : "memory");
 }
 
-// The bank as bf16.  A thread takes 16 codes of a target, eight to its block of 128 dimensions; 32 targets to a block of threads.
+// The bank as bf16.  A thread takes 16 codes of four targets, whose loads are on their way at once; eight threads to a target's block of 128 dimensions.
 __global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ Map P, const int nby, const int nbv)
 {
-    const int c16 = threadIdx.x & 7, r = (int)(blockIdx.x & 3) * 32 + (threadIdx.x >> 3), b0 = blockIdx.x >> 2, t = blockIdx.y, w = blockIdx.z;
-    const int tiles = gridDim.y, len = map_length(P, w), j = t * 128 + r;
+    constexpr int PER = 4;
+    const int c16 = threadIdx.x & 7, r0 = threadIdx.x >> 3, b0 = blockIdx.x, t = blockIdx.y, w = blockIdx.z;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");               // (which waits for all of this grid's writes)
+    const int tiles = gridDim.y, len = map_length(P, w);
     if (t * 128 >= len) return;                                                // (a tile that no one reads)
     const bool value = b0 >= nby;
     const int b = value ? b0 - nby : b0;
     const Cloud8 &cl = value ? P.v : P.y;
-    bool masked = true;
-    uint4 codes = make_uint4(0u, 0u, 0u, 0u);
-    uint32_t e = 0;
-    if (j < len) {
-        const size_t at = (size_t)w * P.m + j;
-        e = cl.scales[at * cl.sb + b];
-        if (b * 128 + c16 * 16 < cl.cb) codes = *reinterpret_cast<const uint4 *>(cl.codes + at * cl.cb + b * 128 + c16 * 16);
-        const double g = P.g ? P.g[at] : 0.0;
-        const float norm = P.y.norms[at];
-        masked = g == -INFINITY || norm == INFINITY;
-        if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = masked ? -INFINITY : map_term(map_scale(P, w), g, norm);
-    } else if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = -INFINITY;
-    // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
-    const uint32_t e1 = min(e, 134u);
-    uint32_t f = masked ? 0u : e == 255u ? 0x7fffu : (e1 + 120u) << 7;
-    f |= f << 16;
-    const uint32_t wd[4] = {codes.x, codes.y, codes.z, codes.w};
-    uint32_t h[8];
+    uint4 codes[PER];
+    uint32_t e[PER];
+    double g[PER];
+    float norm[PER];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        h[2 * x] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x1404)), f);
-        h[2 * x + 1] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x3424)), f);
+    for (int a = 0; a < PER; ++a) {
+        const size_t at = (size_t)w * P.m + min(t * 128 + r0 + 32 * a, len - 1);
+        e[a] = cl.scales[at * cl.sb + b];
+        codes[a] = make_uint4(0u, 0u, 0u, 0u);
+        if (b * 128 + c16 * 16 < cl.cb) codes[a] = *reinterpret_cast<const uint4 *>(cl.codes + at * cl.cb + b * 128 + c16 * 16);
+        g[a] = P.g ? P.g[at] : 0.0;
+        norm[a] = P.y.norms[at];
     }
-    if (!masked && e > 134u && e != 255u) {
-        uint32_t g = (e - 134u + 127u) << 7;
-        g |= g << 16;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) h[x] = mul_bf16x2(h[x], g);
-    }
-    unsigned char *dst = (value ? P.staged_v : P.staged_y) + (((size_t)w * tiles + t) * (value ? nbv : nby) + b) * MT_BLOCK + (c16 >> 2) * MT_CHUNK + r * 128;
+    unsigned char *dst0 = (value ? P.staged_v : P.staged_y) + (((size_t)w * tiles + t) * (value ? nbv : nby) + b) * MT_BLOCK + (c16 >> 2) * MT_CHUNK;
     const int c0 = 2 * (c16 & 3);
-    *reinterpret_cast<uint4 *>(dst + ((c0 ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
-    *reinterpret_cast<uint4 *>(dst + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+#pragma unroll
+    for (int a = 0; a < PER; ++a) {
+        const int r = r0 + 32 * a;
+        const bool masked = t * 128 + r >= len || g[a] == -INFINITY || norm[a] == INFINITY;
+        if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = masked ? -INFINITY : map_term(map_scale(P, w), g[a], norm[a]);
+        // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
+        const uint32_t e1 = min(e[a], 134u);
+        uint32_t f = masked ? 0u : e[a] == 255u ? 0x7fffu : (e1 + 120u) << 7;
+        f |= f << 16;
+        const uint32_t wd[4] = {codes[a].x, codes[a].y, codes[a].z, codes[a].w};
+        uint32_t h[8];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            h[2 * x] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x1404)), f);
+            h[2 * x + 1] = mul_bf16x2(codes_bf16(__byte_perm(wd[x], 0u, 0x3424)), f);
+        }
+        if (!masked && e[a] > 134u && e[a] != 255u) {
+            uint32_t more = (e[a] - 134u + 127u) << 7;
+            more |= more << 16;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) h[x] = mul_bf16x2(h[x], more);
+        }
+        unsigned char *dst = dst0 + r * 128;
+        *reinterpret_cast<uint4 *>(dst + ((c0 ^ (r & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+        *reinterpret_cast<uint4 *>(dst + (((c0 + 1) ^ (r & 7)) << 4)) = make_uint4(h[4], h[5], h[6], h[7]);
+    }
 }
 
 // PAIR: two blocks of a cluster share what they read, half of the targets (scores) or of the dimensions (images) of a stage each; the first issues
@@ -485,6 +495,8 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                         asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
                                      ::"l"(reinterpret_cast<uint64_t>(&tmx)), "r"(64 * c), "r"(lrt * 128), "r"((int)lw) : "memory");
             }
+            // (the bank as bf16 is there: up to here nothing of it was read)
+            asm volatile("griddepcontrol.wait;\n\tfence.proxy.async.global;" ::: "memory");
             // in the order of the matrix instructions: scores of tile t, then images of tile t - 1
             for (int t = 0; t <= nt && nt > 0 && ok; ++t) {
                 if (t < nt) {
@@ -589,12 +601,15 @@ skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMa
     cfg.blockDim = dim3(MT_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = 2;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    // (it may start before the bank is staged, and waits for that)
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = PAIR ? 1 : 0;
+    cfg.numAttrs = PAIR ? 2 : 1;
     cudaLaunchKernelEx(&cfg, map_tiles_kernel<DVC, PAIR>, tx, ty, tv, P, nrt, stages, (P.m + 127) / 128, tma_x, sms);
     return op_launched("map");
 }
@@ -613,7 +628,7 @@ skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st)
     P.staged_y = (unsigned char *)room;
     P.staged_v = P.own_values ? P.staged_y + (size_t)P.W * tiles * nby * MT_BLOCK : P.staged_y;
     P.terms = (float *)(P.staged_y + (size_t)P.W * tiles * (nby + nbv) * MT_BLOCK);
-    map_stage_kernel<<<dim3(4 * (nby + nbv), tiles, P.W), 256, 0, st>>>(P, nby, nbv);
+    map_stage_kernel<<<dim3(nby + nbv, tiles, P.W), 256, 0, st>>>(P, nby, nbv);
     const skb_status rc = op_launched("map");
     if (rc != SKB_OK) return rc;
     const bool pair = P.n > 128;
