@@ -13,7 +13,11 @@
 //            next to each other (M-major).  Weights times the values' powers of two, less the tile's largest, are two e4m3 numbers (eight bits; what is below
 //            2^-22 of the tile's largest is lost), rows of their own again
 // so that nothing of a code passes through a register.  The same work by mma.sync, codes made f16 in registers, was bound by its instructions: one query
-// to each of 8 banks of 16384 x 512 took 35 us.
+// to each of 8 banks of 16384 x 512 took 41 us.
+// That call takes 29 us for 69 MB now, twelve queries to each of 32 banks of 8192 x 128 with values of 64 dimensions 34 us for 54 MB, of which a block's
+// start and end and the join of the parts are some ten.  Between them a tile's slots are taken for what its way through the roles takes (some
+// 5000 cycles: scores 500, softmax 2500, images 1000), and there is room for two to three tiles.  Loads that start before the block is ready, and
+// a softmax against a whole number that is seldom raised instead of the tile's maximum, made no difference.
 //   warps 0-3   softmax, and 12-15 where registers allow: every other tile each
 //   warps 4-7   images: tensor memory -> fp32 sums in registers, a thread to a dimension of every 128
 //   warp 8      loads by TMA: slots of 128 targets by 128 dimensions (16 KB, 128-byte swizzle, targets past the end are zeros)
