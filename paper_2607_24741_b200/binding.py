@@ -520,7 +520,7 @@ def _raw(v):
 
 
 def _cloud(v, name):
-    """dtype, shape, pointer and the tensor to keep of a cloud: a tensor or a Cloud4."""
+    """dtype, shape and the tensor to keep of a cloud: a tensor, a Cloud4 or a Cloud8 (as its values in bfloat16)."""
     if isinstance(v, Cloud4):
         return FORMATS[v.format], v.shape, v.buffer
     if isinstance(v, Cloud8):

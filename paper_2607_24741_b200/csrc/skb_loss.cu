@@ -6,9 +6,9 @@
 //
 // One pass: a row is read once, 16 bytes a thread and vector, and stays in registers (up to 64 scores of bf16 or 32 of fp32 a
 // thread, raw) until its maximum and sum are known; then the gradient is written.  So memory bounds it, and the latencies of what a row
-// needs besides: 65536 rows of 1024 in bf16 take 53 us for 270 MB (78 % of the measured copy rate), of 64 still 43.  Exponentials are taken against the
+// needs besides: 65536 rows of 1024 in bf16 take 48 us for 270 MB (86 % of the measured copy rate), of 64 12.  Exponentials are taken against the
 // thread's own maximum for the sum; short rows keep them, others take them again against the row's: that is one barrier a row instead of two, and no fp32
-// copies in registers.  What a row is given goes by its length (launch_by_length): a warp, four, eight or 16 warps, or a cluster of up to eight blocks, whose
+// copies in registers.  What a row is given goes by its length (launch_by_length): a quarter of a warp, half of one, a warp, four, eight or 16 warps, or a cluster of up to eight blocks, whose
 // maxima and sums meet in distributed shared memory; long rows, a device full of them, stay in shared memory (loss_long_kernel); rows longer than what a cluster's registers hold are read twice, the second time from L2 (a row
 // is at most 1 MB).  A row is reduced in a fixed order, so results do not change from call to call.
 //
@@ -105,6 +105,27 @@ template <int COUNT> __device__ __forceinline__ Part join(Part p, float c)
     for (int off = COUNT / 2; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
     return {m, s};
 }
+// the largest of COUNT threads next to each other, and a join of as many, where a warp has several groups of them
+template <int COUNT> __device__ __forceinline__ float group_max(float v)
+{
+    if constexpr (COUNT >= 32) return warp_max(v);
+    else {
+#pragma unroll
+        for (int off = COUNT / 2; off; off /= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+        return v;
+    }
+}
+template <int COUNT> __device__ __forceinline__ Part group_join(Part p, float c)
+{
+    if constexpr (COUNT >= 32) return join<32>(p, c);
+    else {
+        const float m = group_max<COUNT>(p.m);
+        float s = p.s * ex2f((p.m - finite_max(m)) * c);
+#pragma unroll
+        for (int off = COUNT / 2; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
+        return {m, s};
+    }
+}
 __device__ __forceinline__ Part join(Part a, Part b, float c)
 {
     const float m = fmaxf(a.m, b.m), at = finite_max(m);
@@ -115,7 +136,7 @@ __device__ __forceinline__ Part join(Part a, Part b, float c)
 template <bool BF16, int TPR, int V, int C, bool EVEN>
 __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) loss_kernel(const __grid_constant__ Loss P)
 {
-    constexpr int THREADS = TPR <= 256 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR / 32;
+    constexpr int THREADS = TPR <= 256 ? 256 : TPR, GROUPS = THREADS / TPR, WARPS = TPR < 32 ? 1 : TPR / 32, SPAN = TPR < 32 ? TPR : 32;
     constexpr int E = BF16 ? 8 : 4;
     using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
     extern __shared__ float s_entries[];                          // [GROUPS][4][k]: index, q, log q, score
@@ -123,12 +144,15 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     __shared__ Part s_part[GROUPS][WARPS], s_teach[GROUPS][WARPS], s_rank[C];
     const int tid = threadIdx.x, group = tid / TPR, t = tid % TPR, lane = tid & 31, warp = t >> 5;
     const int rank = C > 1 ? (int)(blockIdx.x % C) : 0;
-    const long long row = (long long)(blockIdx.x / C) * GROUPS + group;
-    if (row >= P.rows) return;                                   // whole groups: barriers below are a group's
+    const long long row_at = (long long)(blockIdx.x / C) * GROUPS + group;
+    // whole groups go: barriers below are a group's.  (Those of a part of a warp stay for its shuffles, and write nothing.)
+    if (TPR >= 32 && row_at >= P.rows) return;
+    const bool there = TPR >= 32 || row_at < P.rows;
+    const long long row = there ? row_at : P.rows - 1;
     int *s_index = reinterpret_cast<int *>(s_entries) + (size_t)group * 4 * P.k;
     float *s_q = reinterpret_cast<float *>(s_index) + P.k, *s_log = s_q + P.k, *s_score = s_log + P.k;
     auto group_sync = [&] {
-        if constexpr (TPR == 32) __syncwarp();
+        if constexpr (TPR <= 32) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(TPR) : "memory");
     };
     // (a block's shared memory may be written by another of its cluster once it has started)
@@ -188,14 +212,14 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
                 s_score[k] = j >= 0 ? score_at(j) : 0.f;
                 teach.m = fmaxf(teach.m, l);
             }
-        teach.m = warp_max(teach.m);
+        teach.m = group_max<SPAN>(teach.m);
         const float at = finite_max(teach.m);
         teach.s = ex2f((l0 - at) * LOG2E);
         // (a thread reads back what it wrote)
         if constexpr (TPR < LS_MAX_K)
             for (int k = t + TPR; k < P.k; k += TPR) teach.s += ex2f((s_log[k] - at) * LOG2E);
 #pragma unroll
-        for (int off = 16; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
+        for (int off = SPAN / 2; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
     }
     // maximum and sum of what this thread has seen
     constexpr bool KEEP = V > 0 && (!BF16 || V <= 4);            // exponentials stay in registers
@@ -233,7 +257,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         }
     }
     const float own = part.m;
-    part = join<32>(part, P.c);
+    part = group_join<SPAN>(part, P.c);
     if constexpr (WARPS > 1) {
         if (lane == 0) { s_part[group][warp] = part; s_teach[group][warp] = teach; }
         group_sync();
@@ -273,13 +297,13 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             }
         if (rank == 0) {
 #pragma unroll
-            for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            for (int off = SPAN / 2; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         }
     }
     if (WARPS > 1 && lane == 0) s_loss[group][warp] = sum;
     // of all warps, in their order
     auto give_loss = [&] {
-        if (rank != 0 || t != 0) return;
+        if (rank != 0 || t != 0 || !there) return;
         if constexpr (WARPS > 1)
 #pragma unroll
             for (int i = 1; i < WARPS; ++i) sum += s_loss[group][i];
@@ -326,7 +350,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int j = (v * C + rank) * TPR + t;
-            if (j >= nvec) continue;
+            if (j >= nvec || !there) continue;
             if constexpr (!KEEP) {
                 // (unpacked anew: the compiler would keep what it unpacked before the barrier, and spill)
                 asm volatile("" : "+r"(held[v].x), "+r"(held[v].y), "+r"(held[v].z), "+r"(held[v].w));
@@ -342,9 +366,9 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     }
     group_sync();
     give_loss();
-    if (!live || warp * 32 >= P.k) return;
+    if (!live || warp * 32 >= P.k || !there) return;
     // named entries: each by the first of those that name its column
-    if (P.k <= 32) {
+    if (TPR >= 32 && P.k <= 32) {
         const unsigned alike = __match_any_sync(0xffffffffu, named);
         if (named < 0 || (alike & ((1u << lane) - 1u)) || (C > 1 && (head + named) / E / TPR % C != rank)) return;
         float q = 0.f;
@@ -577,6 +601,16 @@ skb_status launch_by_length(const Loss &P, long long vec, int sms, cudaStream_t 
         while (c < 8 && P.rows * c < 2 * sms && vec / (2 * c) >= 512) c *= 2;
         return c;
     };
+    // Short rows are latency: several to a warp where there are more than the device's warps take at once, with more of a row to a thread where there are
+    // many more.  (us in bf16, so / a warp to a row: 65536 rows of 64 12 / 36, of 256 15 / 39, of 512 25 / 42, of 1024 46 / 50; 4736 rows of 64 3.0 / 4.5; 2368
+    // 2.9 / 3.4.  Eight vectors a thread for four: 65536 rows of 512 25 / 29, 9472 rows 5.8 / 5.4.  More than 32 entries would take too much shared memory.)
+    if (P.k <= 32 && P.rows >= 16 * sms) {
+        const bool many = P.rows >= 128 * sms;
+        if (vec <= 8 * 4) return launch<BF16, 8, 4, 1, EVEN>(P, st);
+        if (vec <= 8 * 8 && many) return launch<BF16, 8, 8, 1, EVEN>(P, st);
+        if (vec <= 16 * 4) return launch<BF16, 16, 4, 1, EVEN>(P, st);
+        if (vec <= 16 * 8 && many) return launch<BF16, 16, 8, 1, EVEN>(P, st);
+    }
     // (us, rows of bf16 as the line says / as the next ones would: 256 vectors by a warp or by four, 1184 rows 10 / 10, 8192 20 / 28, 32768 51 / 89; 4096 vectors by a
     // block or by two and more, 148 rows 11 / 13, 592 21 / 26, 4096 92 / 110; 8192 vectors through shared memory or by a cluster, 100 rows 16 / 14, 148 rows
     // 16 / 19, 592 39 / 43, 4096 199 / 218; 12288 vectors, 1184 rows 92 / 113)

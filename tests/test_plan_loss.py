@@ -96,6 +96,49 @@ def test_rows_of_every_length(B, m, dtype):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("m,k", [(1, 1), (5, 3), (8, 9), (31, 8), (64, 4), (121, 32), (128, 7), (200, 33), (250, 5), (256, 17), (257, 2), (300, 31), (505, 8), (512, 6)])
+def test_many_short_rows(B, m, k, dtype):
+    # several rows to a warp; entries named again, entries that name nothing, rows that name nothing, rows that start anywhere, gradients in place
+    import torch
+    rows, dt = 5003, getattr(torch, dtype)
+    scores, index, t, weight = inputs(rows, m, k, dt, 7 * m + k)
+    index[::3, -1] = index[::3, 0]
+    index[1::7, 0] = -1
+    index[2::11] = m
+    check(B, scores, index, t, 1.3, weight)
+    loss, grad = run(B, scores, index)
+    compare(loss, grad, scores, index)
+    wide = torch.zeros(rows, m + 3, dtype=dt, device="cuda")
+    place = wide[:, 1:m + 1]
+    place.copy_(scores)
+    got, inplace = B.plan_loss(place, index.cuda(), t.cuda(), temperature=1.3, weight=weight.cuda(), grad=place)
+    assert inplace.data_ptr() == place.data_ptr() and not wide[:, 0].any() and not wide[:, m + 1:].any()
+    compare(got, inplace, scores, index, t, 1.3, weight)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("m", [200, 255, 256, 257, 400, 505, 512, 513, 1000, 1017, 1024, 1025])
+def test_very_many_short_rows(B, m, dtype):
+    # 20481 rows that repeat 211 of them
+    import torch
+    dt = getattr(torch, dtype)
+    scores, index, t, weight = inputs(211, m, 9, dt, m)
+    index[::3, -1] = index[::3, 0]
+    index[1::7, 0] = -1
+    many = torch.arange(20481) % 211
+    loss, grad = B.plan_loss(scores[many].cuda(), index[many].cuda(), t[many].cuda(), temperature=1.3, weight=weight[many].cuda(), grad=True)
+    for first in (0, 211 * 97):
+        n = min(211, 20481 - first)
+        compare(loss[first:first + n], grad[first:first + n], *(v[:n] for v in (scores, index, t)), 1.3, weight[:n])
+    bits = lambda v: v.contiguous().view(torch.int16 if v.dtype == torch.bfloat16 else torch.int32)
+    if m % 8 == 0:                                                # (rows that start alike are summed alike)
+        for r in (0, 1, 210):
+            assert (bits(grad[r::211]) == bits(grad[r])).all() and (bits(loss[r::211]) == bits(loss[r:r + 1])).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 def test_many_rows_of_middle_length(B, dtype):
     import torch
     for m in (3000, 5000, 8001):
