@@ -22,7 +22,7 @@
 //   warps 4-7   images: tensor memory -> fp32 sums in registers, a thread to a dimension of every 128
 //   warp 8      loads by TMA: slots of 128 targets by 128 dimensions (16 KB, 128-byte swizzle, targets past the end are zeros)
 //   warp 9      scores' matrix instructions, warp 11 the images': either waits for what it needs
-//   warp 10     targets' scales and terms, up to six tiles ahead
+//   warp 10     targets' scales and terms, up to six tiles ahead; a second such warp, where registers allow, every other tile each
 // Several blocks that share a lane's bank leave (maximum, sum, image), which map_join_kernel adds up.  Every wait is bounded (skb_tmem.cuh): one that
 // runs out ends all roles, and the block's images are NaN.
 #include <cuda.h>
@@ -98,7 +98,10 @@ __device__ __forceinline__ bool elected()
 }
 // warps of the softmax: two groups of four that take turns, where registers allow
 template <int NQ, int UNITS> constexpr int MR_GROUPS = NQ * UNITS <= 32 ? 2 : 1;
-template <int NQ, int UNITS> constexpr int MR_THREADS = (8 + 4 * MR_GROUPS<NQ, UNITS>) * 32;
+// warps for the targets' terms: one takes as long for a tile as all else of it (two: one query to 8 banks of 16384 x 512 29.1 -> 27.3 us, twelve to 32 of
+// 8192 x 128 33.9 -> 31.1); a seventeenth warp costs registers, which 16 queries and 256 dimensions do not have (24 queries to 64 of 2000 x 256 36.7 -> 38.9)
+template <int NQ, int UNITS> constexpr int MR_HELPERS = NQ * UNITS > 16 && NQ == 16 ? 1 : 2;
+template <int NQ, int UNITS> constexpr int MR_THREADS = (7 + MR_HELPERS<NQ, UNITS> + 4 * MR_GROUPS<NQ, UNITS>) * 32;
 
 // whether all 128 threads of a group of the softmax say so
 __device__ __forceinline__ bool all_softmax(bool ok, int barrier)
@@ -302,7 +305,8 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
         __syncwarp();
     };
 
-    if (warp < 4 || warp >= 12) {
+    constexpr int HELPERS = MR_HELPERS<NQ, UNITS>, SECOND = 8 + 4 * GROUPS;           // SECOND: the second of them, the last warp
+    if (warp < 4 || (warp >= 12 && warp < SECOND)) {
         // ---- softmax: a thread to a target, which is a lane of tensor memory
         const int group = warp >> 3, part = warp & 3, p = part * 32 + lane;          // every other tile's
         const uint32_t lanes = (uint32_t)(part * 32) << 16;
@@ -608,7 +612,8 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
         }
         finish(LAST + 1);
     } else {
-        // ---- targets' scales and terms, a lane to every 32nd target of a tile; two tiles' on their way from memory, all of a tile's loads at once
+        // ---- targets' scales and terms, a lane to every 32nd target of a tile; two tiles' of a warp on their way from memory, all of a tile's
+        // loads at once
         struct Raw {
             double g[4];
             float norm[4];
@@ -666,14 +671,15 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             if (lane == 0) mbar_arrive(bar(CFULL + b));
         };
         Raw one, two;
-        if (nt > 0) fetch(0, one);
-        if (nt > 1) fetch(1, two);
-        for (int t = 0; t < nt && ok; t += 2) {
+        const int turn = HELPERS == 2 && warp == SECOND;
+        if (turn < nt) fetch(turn, one);
+        if (turn + HELPERS < nt) fetch(turn + HELPERS, two);
+        for (int t = turn; t < nt && ok; t += 2 * HELPERS) {
             give(t, one);
-            if (t + 2 < nt) fetch(t + 2, one);
-            if (t + 1 >= nt || !ok) break;
-            give(t + 1, two);
-            if (t + 3 < nt) fetch(t + 3, two);
+            if (t + 2 * HELPERS < nt) fetch(t + 2 * HELPERS, one);
+            if (t + HELPERS >= nt || !ok) break;
+            give(t + HELPERS, two);
+            if (t + 3 * HELPERS < nt) fetch(t + 3 * HELPERS, two);
         }
     }
     __syncwarp();
