@@ -14,10 +14,11 @@
 //            2^-22 of the tile's largest is lost), rows of their own again
 // so that nothing of a code passes through a register.  The same work by mma.sync, codes made f16 in registers, was bound by its instructions: one query
 // to each of 8 banks of 16384 x 512 took 41 us.
-// That call takes 29 us for 69 MB now, twelve queries to each of 32 banks of 8192 x 128 with values of 64 dimensions 34 us for 54 MB, of which a block's
-// start and end and the join of the parts are some ten.  Between them a tile's slots are taken for what its way through the roles takes (some
-// 5000 cycles: scores 500, softmax 2500, images 1000), and there is room for two to three tiles.  Loads that start before the block is ready, and
-// a softmax against a whole number that is seldom raised instead of the tile's maximum, made no difference.
+// That call takes 27 us for 69 MB now, twelve queries to each of 32 banks of 8192 x 128 with values of 64 dimensions 31 us for 54 MB.  Of the first some
+// 17 us are a block's time, whose tiles go by at the rate of the memory (2600 cycles for 64 KB) between the first one's arrival (some 8000, as all of a
+// block's slots are asked for at once) and the last one's way through the roles (scores 500, softmax 2000, images 1000, results 2000); with twelve queries
+// the softmax takes 1.5 times as long as the memory.  Made no difference: loads that start before the block is ready, a softmax
+// against a whole number that is seldom raised instead of the tile's maximum, a third group of warps for it, terms brought into L2 ahead.
 //   warps 0-3   softmax, and 12-15 where registers allow: every other tile each
 //   warps 4-7   images: tensor memory -> fp32 sums in registers, a thread to a dimension of every 128
 //   warp 8      loads by TMA: slots of 128 targets by 128 dimensions (16 KB, 128-byte swizzle, targets past the end are zeros)
