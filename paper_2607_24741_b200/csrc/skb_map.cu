@@ -800,13 +800,13 @@ skb_status launch_rows_by_depth(const CUtensorMap &ty, const CUtensorMap &tv, co
 constexpr int MAP_SMS = 148;
 // Queries up to which the tiles of 128 queries are too empty to be worth the staging (us, here / with tiles; W, m, d, dv):
 //      queries                     16          32          33          48          64
-//      8, 16384, 512           50 / 105    83 / 112   120 / 112   114 / 114   155 / 120
-//      32, 8192, 128, 64       42 / 79     60 / 81     95 / 83     90 / 83     95 / 85
-//      64, 1024, 512           32 / 56     56 / 58     76 / 58     80 / 58    103 / 58
-//      64, 1024, 128           24 / 32     25 / 34     40 / 34     42 / 38     43 / 40
+//      8, 16384, 512            41 / 92     72 / 98     94 / 99     95 / 100   131 / 109
+//      32, 8192, 128, 64        30 / 66     49 / 67     82 / 68     71 / 69     82 / 70
+//      64, 1024, 512            24 / 46     46 / 46     65 / 46     67 / 46     89 / 46
+//      64, 1024, 128            14 / 22     18 / 24     31 / 24     34 / 27     35 / 30
 constexpr int MAP_ROWS_MAX = 32;
-// ... and beyond them while a block has no more than so many tiles (24, 333, 200, 96: 48 queries, three tiles, 16 / 22; with eight queries to a block 64 would
-// be six tiles, 25 / 22; 1, 2000, 64: 128 queries, two tiles, 15 / 24)
+// ... and beyond them while an SM has no more than so many tiles of eight queries (24, 333, 200, 96: 48 queries, three tiles, 11 / 13; 64, three tiles of sixteen,
+// 15 / 13; 1, 2000, 64: 128 queries, two tiles, 11 / 15)
 constexpr int MAP_ROWS_STEPS = 4;
 
 const char *map_refused(int W, int n, int m, int d, int dv)
@@ -827,25 +827,30 @@ int map_splits(long long blocks, long long tiles, int sms)
     return (int)(s < 1 ? 1 : s > 128 ? 128 : s);
 }
 long long rows_blocks(const RowsShape &r, int W, int n) { return (long long)W * ((n + r.nq - 1) / r.nq) * r.chunks; }
-// tiles that an SM gets through, one after the other
-long long rows_steps(const RowsShape &r, int W, int n, long long tiles)
+// What an SM gets through one after the other, in halves of a tile of eight queries: a tile of sixteen takes half as long again, and the join of parts as long as two
+struct RowsCost {
+    long long tiles, all;
+};
+RowsCost rows_cost(const RowsShape &r, int W, int n, long long tiles)
 {
     const long long blocks = rows_blocks(r, W, n), splits = map_splits(blocks, tiles, MAP_SMS);
-    return (blocks * splits + MAP_SMS - 1) / MAP_SMS * ((tiles + splits - 1) / splits);
+    const long long steps = (blocks * splits + MAP_SMS - 1) / MAP_SMS * ((tiles + splits - 1) / splits) * (r.nq == 16 ? 3 : 2);
+    return {steps, steps + (splits > 1 ? 4 : 0)};
 }
 MapPlan map_plan(int W, int n, int m, int d, int dv, bool own_values, int sms)
 {
     const long long tiles = (m + MR_T - 1) / MR_T;
     RowsShape r = rows_shape<8>(d, dv, own_values, tiles);
-    // A tile of sixteen queries takes half as long again as one of eight, of images above 256 dimensions, for which registers leave one group of warps to the
-    // softmax, twice as long: those have eight.  (32 x 8192 x 128, 12 queries: 40 us with sixteen, 50 with eight; 24 x 333 x 200, 24 queries: 20 and 16.)
+    // Images above 256 dimensions have eight: registers leave one group of warps to the softmax of sixteen, which takes twice as long.  (us, with eight / sixteen: 32 x
+    // 8192 x 128 with values of 64, 12 queries 33 / 28, 32 queries 55 / 48; 64 x 1024 x 128, 16 queries 14 / 17, 32 queries 26 / 18; 24 x 333 x 200, 24
+    // queries 11 / 15)
     if (n > 8 && dv <= 256) {
         const RowsShape r16 = rows_shape<16>(d, dv, own_values, tiles);
-        if (r16.yslots >= (d + 127) / 128 && 3 * rows_steps(r16, W, n, tiles) <= 2 * rows_steps(r, W, n, tiles)) r = r16;
+        if (r16.yslots >= (d + 127) / 128 && rows_cost(r16, W, n, tiles).all < rows_cost(r, W, n, tiles).all) r = r16;
     }
     MapPlan p;
     p.nq = r.nq;
-    p.tiles = d <= MAP_TILES_MAX_D && n > MAP_ROWS_MAX && rows_steps(r, W, n, tiles) > MAP_ROWS_STEPS;
+    p.tiles = d <= MAP_TILES_MAX_D && n > MAP_ROWS_MAX && rows_cost(r, W, n, tiles).tiles > 2 * MAP_ROWS_STEPS;
     p.splits = map_splits(p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : rows_blocks(r, W, n), tiles, sms);
     return p;
 }
