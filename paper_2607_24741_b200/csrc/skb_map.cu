@@ -805,8 +805,8 @@ constexpr int MAP_SMS = 148;
 //      64, 1024, 512            24 / 46     46 / 46     65 / 46     67 / 46     89 / 46
 //      64, 1024, 128            14 / 22     18 / 24     31 / 24     34 / 27     35 / 30
 constexpr int MAP_ROWS_MAX = 32;
-// ... and beyond them while an SM has no more than so many tiles of eight queries (24, 333, 200, 96: 48 queries, three tiles, 11 / 13; 64, three tiles of sixteen,
-// 15 / 13; 1, 2000, 64: 128 queries, two tiles, 11 / 15)
+// ... and beyond them while an SM has no more than so many tiles, for one launch less (24, 333, 200, 96: 48 queries, three tiles of eight, 11 / 13; 77, three
+// of sixteen, 15 / 13, with the host's time 20 / 23; 128, six, 28 / 13; 1, 2000, 64: 128 queries, two tiles, 11 / 15)
 constexpr int MAP_ROWS_STEPS = 4;
 
 const char *map_refused(int W, int n, int m, int d, int dv)
@@ -827,15 +827,16 @@ int map_splits(long long blocks, long long tiles, int sms)
     return (int)(s < 1 ? 1 : s > 128 ? 128 : s);
 }
 long long rows_blocks(const RowsShape &r, int W, int n) { return (long long)W * ((n + r.nq - 1) / r.nq) * r.chunks; }
-// What an SM gets through one after the other, in halves of a tile of eight queries: a tile of sixteen takes half as long again, and the join of parts as long as two
+// Tiles that an SM gets through one after the other, and what they take, in halves of a tile of eight queries: a tile of sixteen takes half as long again, the
+// join of parts as long as two
 struct RowsCost {
-    long long tiles, all;
+    long long tiles, time;
 };
 RowsCost rows_cost(const RowsShape &r, int W, int n, long long tiles)
 {
     const long long blocks = rows_blocks(r, W, n), splits = map_splits(blocks, tiles, MAP_SMS);
-    const long long steps = (blocks * splits + MAP_SMS - 1) / MAP_SMS * ((tiles + splits - 1) / splits) * (r.nq == 16 ? 3 : 2);
-    return {steps, steps + (splits > 1 ? 4 : 0)};
+    const long long steps = (blocks * splits + MAP_SMS - 1) / MAP_SMS * ((tiles + splits - 1) / splits);
+    return {steps, steps * (r.nq == 16 ? 3 : 2) + (splits > 1 ? 4 : 0)};
 }
 MapPlan map_plan(int W, int n, int m, int d, int dv, bool own_values, int sms)
 {
@@ -846,11 +847,11 @@ MapPlan map_plan(int W, int n, int m, int d, int dv, bool own_values, int sms)
     // queries 11 / 15)
     if (n > 8 && dv <= 256) {
         const RowsShape r16 = rows_shape<16>(d, dv, own_values, tiles);
-        if (r16.yslots >= (d + 127) / 128 && rows_cost(r16, W, n, tiles).all < rows_cost(r, W, n, tiles).all) r = r16;
+        if (r16.yslots >= (d + 127) / 128 && rows_cost(r16, W, n, tiles).time < rows_cost(r, W, n, tiles).time) r = r16;
     }
     MapPlan p;
     p.nq = r.nq;
-    p.tiles = d <= MAP_TILES_MAX_D && n > MAP_ROWS_MAX && rows_cost(r, W, n, tiles).tiles > 2 * MAP_ROWS_STEPS;
+    p.tiles = d <= MAP_TILES_MAX_D && n > MAP_ROWS_MAX && rows_cost(r, W, n, tiles).tiles > MAP_ROWS_STEPS;
     p.splits = map_splits(p.tiles ? (long long)W * (n > 128 ? (n + 255) / 256 * 2 : 1) * ((dv + 255) / 256) : rows_blocks(r, W, n), tiles, sms);
     return p;
 }
