@@ -317,8 +317,9 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     const float w = weight * P.inv_t, a = w / part.s;
     T *out = (T *)P.grad + (size_t)row * P.ldg - head;
     const bool wide = EVEN || (uintptr_t)out % 16 == 0;
-    // what an exponential is multiplied by: kept ones are against this thread's own maximum
-    const float factor = (KEEP ? ex2f((finite_max(own) - finite_max(part.m)) * P.c) : 1.f) * a;
+    // what an exponential is multiplied by: kept ones are against this thread's own maximum.  (That is minus infinity where the thread has seen nothing else: its
+    // exponentials, and this, are 0; a row of nothing else has an infinite a and is NaN.)
+    const float factor = (KEEP ? ex2f((own - finite_max(part.m)) * P.c) : 1.f) * a;
     const u64 at2 = pack2(part.m, part.m), f2 = pack2(factor, factor);
     auto again = [&](const uint4 &y, u64 (&e)[E / 2]) {
 #pragma unroll

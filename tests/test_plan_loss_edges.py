@@ -1,0 +1,35 @@
+"""The loss of scores against named entries where its arithmetic has least to spare: stretches of masked scores far below zero, logits far from zero,
+sums next to one; gradients in the place of tensors that a graph or another row still needs."""
+import pytest
+
+from test_plan_loss import B, compare, inputs  # noqa: F401  (B is the fixture)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,m", [(9, 20), (9, 400), (9, 1000), (9, 3000), (9, 8000), (5, 9000), (5, 16000), (5, 30000), (5, 60000), (5, 131000), (5, 262143),
+                                    (5003, 60), (5003, 100), (5003, 250), (20480, 120), (20480, 500), (300, 40000)])
+def test_stretches_of_masked_scores_beside_scores_far_below_zero(B, rows, m, dtype):
+    # a thread that sees nothing but minus infinity has weights of 0, whatever the row's maximum: rows of every way through the kernels
+    import torch
+    scores, index, t, weight = inputs(min(rows, 211), m, min(m // 3, 4), getattr(torch, dtype), m)
+    live = m // 3
+    index %= live
+    many = torch.arange(rows) % scores.shape[0]
+    for shift, T in ((-300.0, 1.0), (-6.0, 0.05), (250.0, 1.0)):
+        s = ((scores.float() * 3 * T).clamp(-10 * T, 10 * T) + shift).to(scores.dtype)
+        s[:, live:] = -float("inf")
+        s[1], s[1, m - live:] = -float("inf"), s[0, :live]                            # the live ones at the end
+        at = index.clone()
+        at[1] += m - live
+        loss, grad = B.plan_loss(s[many].cuda(), at[many].cuda(), t[many].cuda(), temperature=T, weight=weight[many].cuda(), grad=True)
+        assert not torch.isnan(loss).any() and not torch.isnan(grad).any()
+        assert not grad[many != 1][:, live:].any() and not grad[many == 1][:, :m - live].any()
+        for first in {0, (rows - 1) // 211 * 211}:
+            n = min(211, rows - first)
+            compare(loss[first:first + n], grad[first:first + n], s[:n], at[:n], t[:n], T, weight[:n])
+        # a NaN beside them is its row's alone, and a row of nothing but masked scores is NaN
+        s[2, m - 1], s[3] = float("nan"), -float("inf")
+        loss, grad = (v[:5].cpu() for v in B.plan_loss(s[many].cuda(), at[many].cuda(), t[many].cuda(), temperature=T, grad=True))
+        bad = torch.tensor([False, False, True, True, False][:loss.shape[0]])
+        assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(grad).all(1), bad) and torch.equal(torch.isnan(grad).any(1), bad)
