@@ -245,6 +245,10 @@ def _stream(device):
     return _raw_stream(device.index)
 
 
+# What a kernel has written in a tensor that the caller gave: a graph that saved the tensor, or another view of it, must see that, as of torch's own
+# operations in place.
+_written = torch.autograd.graph.increment_version
+
 # (the stream's handle without a Stream object around it, which takes as long as a small launch)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -330,6 +334,7 @@ def cloud4_dots(x, y, out=None):
             out = torch.empty(shape, dtype=torch.float32, device=x.device)
         _check_op(lib.sinkhorn_cloud4_dots(_ptr(x.buffer), _ptr(y.buffer), x.W, x.npts, y.npts, x.d, FORMATS[x.format], _ptr(out),
                                            _stream(x.device)))
+    _written(out)
     return out
 
 
@@ -407,6 +412,7 @@ def cloud8_dots(x, y, out=None):
         if out is None:
             out = torch.empty(shape, dtype=torch.float32, device=x.device)
         _check_op(lib.sinkhorn_cloud8_dots(x.buffer.data_ptr(), y.buffer.data_ptr(), x.W, x.npts, y.npts, x.d, out.data_ptr(), _stream(x.device)))
+    _written(out)
     return out
 
 
@@ -445,6 +451,7 @@ def cloud8_map(x, y, g, eps, v=None, *, lengths=None, lse=False, out=None):
         _check_op(lib.sinkhorn_cloud8_map(x.data_ptr(), y.buffer.data_ptr(), None if g is None else g.data_ptr(), eps.data_ptr(),
                                           None if v is None else v.buffer.data_ptr(), None if lengths is None else lengths.data_ptr(), W, n, m, d, dv,
                                           out.data_ptr(), None if sums is None else sums.data_ptr(), ws.data_ptr(), need, _stream(device)))
+    _written(out)
     return (out, sums) if lse else out
 
 
@@ -473,7 +480,8 @@ def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=
     alike); see sinkhorn_plan_loss in the header.  Returns the rows' losses [...] float32; with `grad` also the gradient of the sum of
     weight [...] float32 (None: 1) times loss, [..., m] of the scores' type.  grad=scores writes it in their place, another
     tensor like them there.  Rows may be spaced out (a slice of wider ones); no autograd graph is recorded: scores.backward(gradient)
-    continues from it."""
+    continues from it.  (In their place, if the operation that made the scores does not need its result for that, as a product does not;
+    where it does, as tanh or log_softmax, backward raises an error.)"""
     if not torch.is_tensor(scores) or not scores.is_cuda or scores.dtype not in DTYPES or scores.dim() < 1:
         raise ValueError("scores must be a float32 or bfloat16 CUDA tensor [..., m]")
     shape, device = scores.shape, scores.device
@@ -512,6 +520,8 @@ def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=
         _check_op(lib.sinkhorn_plan_loss(scores.data_ptr(), DTYPES[scores.dtype], rows, m, ld, index.data_ptr(), None if logits is None else logits.data_ptr(), k,
                                          float(temperature), None if weight is None else weight.data_ptr(), loss.data_ptr(), None if out is None else out.data_ptr(),
                                          ldg, _stream(device)))
+    if in_place:
+        _written(grad)
     return loss if out is None else (loss, out)
 
 

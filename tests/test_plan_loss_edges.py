@@ -33,3 +33,43 @@ def test_stretches_of_masked_scores_beside_scores_far_below_zero(B, rows, m, dty
         loss, grad = (v[:5].cpu() for v in B.plan_loss(s[many].cuda(), at[many].cuda(), t[many].cuda(), temperature=T, grad=True))
         bad = torch.tensor([False, False, True, True, False][:loss.shape[0]])
         assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(grad).all(1), bad) and torch.equal(torch.isnan(grad).any(1), bad)
+
+
+@pytest.mark.gpu
+def test_a_gradient_in_the_place_of_what_a_graph_saved_is_seen_by_it(B):
+    import torch
+    gen = torch.Generator().manual_seed(3)
+    index = torch.randint(0, 50, (20, 3), generator=gen, dtype=torch.int32).cuda()
+    start = torch.randn(20, 50, generator=gen).cuda()
+    for act in (torch.tanh, torch.exp, torch.sigmoid, lambda h: torch.log_softmax(h, 1)):
+        h = start.clone().requires_grad_()
+        scores = act(h)
+        _, grad = B.plan_loss(scores, index, grad=scores)
+        with pytest.raises(RuntimeError):
+            scores.backward(grad)                                     # (the operation saved its result, which is gone)
+    h = start.clone().requires_grad_()
+    kept = torch.tanh(h)
+    B.plan_loss(start, index, grad=kept.detach())                     # (by way of another view of it)
+    with pytest.raises(RuntimeError):
+        kept.sum().backward()
+    # a product does not need its result: the step goes on
+    for place in (False, True):
+        lin = start[:, :50].clone()[:8].requires_grad_()
+        scores = start[:, :8] @ lin
+        _, grad = B.plan_loss(scores, index, grad=scores if place else True)
+        scores.backward(grad)
+        if place:
+            assert torch.equal(lin.grad, want)
+        want = lin.grad
+    # other tensors that are written where they are given
+    x8, y8 = B.cloud8_pack(torch.randn(1, 4, 32, generator=gen).cuda()), B.cloud8_pack(torch.randn(1, 5, 32, generator=gen).cuda())
+    dots, images, grad = torch.zeros(1, 4, 5).cuda(), torch.zeros(1, 4, 32, dtype=torch.bfloat16).cuda(), torch.zeros(20, 50).cuda()
+    x4, y4 = B.cloud4_pack(torch.randn(1, 4, 32, generator=gen).cuda(), "mx4"), B.cloud4_pack(torch.randn(1, 5, 32, generator=gen).cuda(), "mx4")
+    for t, call in ((dots, lambda: B.cloud8_dots(x8, y8, out=dots)), (images, lambda: B.cloud8_map(x8.values(torch.bfloat16), y8, None, torch.ones(1).cuda(), out=images)),
+                    (grad, lambda: B.plan_loss(start, index, grad=grad)), (dots, lambda: B.cloud4_dots(x4, y4, out=dots))):
+        before = t._version
+        call()
+        assert t._version > before
+    with torch.inference_mode():
+        s = start.clone()
+        B.plan_loss(s, index, grad=s)
