@@ -563,7 +563,8 @@ skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, co
  * minus infinity, has loss 0 and gradient 0 whatever its scores.  Scores of minus infinity have p = 0, and one that is named with
  * q > 0 makes the loss infinite (the gradient stays finite); a NaN, plus infinity or a row of minus infinity makes them NaN.
  *   weight  [rows] fp32, may be null: 1
- *   grad    may be null, of the scores' type, `ldg` elements from row to row; may be scores itself, and must not overlap them otherwise
+ *   grad    may be null, of the scores' type, `ldg` elements from row to row; may be scores itself, or lie between their rows, and is
+ *            refused where it overlaps them otherwise (rows of another stride: where their ranges meet)
  * T from 1e-30 to 1e30, k <= 256, m <= 262143, rows < 2^31.  Sums are fp32, in an order that does not change from call to call.  One kernel on `stream` of
  * the current device, which reads a row once (longer ones than 131068 of fp32 or 262136 of bf16 twice).
  */

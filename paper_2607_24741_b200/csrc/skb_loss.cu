@@ -646,6 +646,17 @@ skb_status launch_loss(const Loss &P, int sms, cudaStream_t st)
     return even ? launch_by_length<BF16, true>(P, vec, sms, st) : launch_by_length<BF16, false>(P, vec, sms, st);
 }
 
+// Whether rows of the gradient and of the scores have entries in common, delta elements apart.  (Rows of different strides whose ranges meet: taken to.)
+bool rows_overlap(long long delta, long long rows, long long m, long long ld, long long ldg)
+{
+    if (delta >= (rows - 1) * ld + m || -delta >= (rows - 1) * ldg + m) return false;
+    if (rows == 1 || ld != ldg) return true;
+    // gradient row j begins r after scores row j + q, and ld - r before the next
+    const long long q = delta >= 0 ? delta / ld : -((-delta + ld - 1) / ld), r = delta - q * ld;
+    const auto some = [&](long long apart) { return apart < rows && -apart < rows; };
+    return (r < m && some(q)) || (ld - r < m && some(q + 1));
+}
+
 }  // namespace
 }  // namespace skb
 
@@ -664,6 +675,8 @@ extern "C" skb_status sinkhorn_plan_loss(const void *scores, int dtype, long lon
     if ((uintptr_t)scores % size || (uintptr_t)grad % size || (uintptr_t)index % 4 || (uintptr_t)logits % 4 || (uintptr_t)weight % 4 || (uintptr_t)loss % 4)
         return op_fail(SKB_ERR_WORKSPACE, "arrays must be aligned to their types");
     if (grad == scores && ldg != ld) return op_fail(SKB_ERR_SHAPE, "a gradient in the place of the scores has their row stride");
+    if (grad && grad != scores && rows_overlap(((long long)(uintptr_t)grad - (long long)(uintptr_t)scores) / (long long)size, rows, m, ld, ldg))
+        return op_fail(SKB_ERR_VALUE, "a gradient that overlaps the scores must be in their place");
     int dev = 0, sms = 0;
     cudaGetDevice(&dev);
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return op_launched("device");

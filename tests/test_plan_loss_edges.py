@@ -1,5 +1,7 @@
 """The loss of scores against named entries where its arithmetic has least to spare: stretches of masked scores far below zero, logits far from zero,
 sums next to one; gradients in the place of tensors that a graph or another row still needs."""
+import ctypes
+
 import pytest
 
 from test_plan_loss import B, compare, inputs  # noqa: F401  (B is the fixture)
@@ -73,3 +75,44 @@ def test_a_gradient_in_the_place_of_what_a_graph_saved_is_seen_by_it(B):
     with torch.inference_mode():
         s = start.clone()
         B.plan_loss(s, index, grad=s)
+
+
+def overlapping(call):
+    """Calls whose gradient overlaps the scores without being in their place: (scores, grad, rows, m, ld, ldg) in elements."""
+    for grad, rows, m, ld, ldg in ((1, 4, 8, 8, 8), (-1, 4, 8, 8, 8), (8, 4, 8, 8, 8), (-8, 4, 8, 8, 8), (31, 4, 8, 8, 8), (-31, 4, 8, 8, 8), (8, 4, 8, 15, 15),
+                                   (-7, 4, 8, 16, 16), (12, 4, 8, 19, 19), (8, 4, 8, 16, 24), (24, 4, 8, 16, 8), (17, 4, 8, 16, 16), (7, 1, 8, 8, 8), (4, 2, 1, 4, 4)):
+        call(grad, rows, m, ld, ldg)
+
+
+def test_gradients_that_overlap_the_scores_are_refused(B):
+    p, base = ctypes.c_void_p, 1 << 16
+
+    def call(grad, rows, m, ld, ldg):
+        for dtype, size in ((0, 4), (1, 2)):
+            assert B.lib.sinkhorn_plan_loss(p(base), dtype, rows, m, ld, p(256), None, 1, 1.0, None, p(256), p(base + size * grad), ldg, None) == 3, (grad, ld, ldg)
+    overlapping(call)
+
+
+@pytest.mark.gpu
+def test_gradients_between_the_scores_rows_and_beside_them(B):
+    import torch
+    for dtype in (torch.float32, torch.bfloat16):
+        scores, index, t, weight = (v.cuda() for v in inputs(6, 40, 3, dtype, 1))
+        for ld, at, grad in ((80, 0, 40), (80, 40, 0), (91, 3, 47), (40, 0, 240), (40, 240, 0), (41, 0, 250)):
+            room = torch.full((2 * 6 * ld + 16,), 7.0, dtype=dtype, device="cuda")
+            s, g = (room.as_strided((6, 40), (ld, 1), first) for first in (at, grad))
+            s.copy_(scores)
+            loss, out = B.plan_loss(s, index, t, weight=weight, grad=g)
+            assert out.data_ptr() == g.data_ptr() and torch.equal(s, scores)
+            compare(loss, g, scores, index, t, 1.0, weight)
+            rest = torch.ones_like(room, dtype=torch.bool)
+            for first in (at, grad):
+                rest.as_strided((6, 40), (ld, 1), first).fill_(False)
+            assert (room[rest] == 7).all()
+        room = torch.zeros(400, dtype=dtype, device="cuda")
+
+        def call(grad, rows, m, ld, ldg):
+            s, g = room.as_strided((rows, m), (ld, 1), 100), room.as_strided((rows, m), (ldg, 1), 100 + grad)
+            with pytest.raises(B.SkbError):
+                B.plan_loss(s, torch.zeros(rows, 1, dtype=torch.int32, device="cuda"), grad=g)
+        overlapping(call)
