@@ -194,11 +194,11 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             if (j < nvec) held[v] = load(j);
         }
     }
-    // the teacher, and the scores that it names, while the row is on its way
-    constexpr float LOG2E = 1.44269504f;
+    // the teacher, and the scores that it names, while the row is on its way.  (Logits as they are: as of the scores, differences are taken before anything
+    // is multiplied, so that neither a shift of all of them nor their size is felt.)
     Part teach = {-INFINITY, 0.f};
     if (named < 0 || named >= P.m) named = -1;
-    const float l0 = named >= 0 ? logit * P.inv_t : -INFINITY;
+    const float l0 = named >= 0 ? logit : -INFINITY;
     if (warp * 32 < P.k) {
         if (named >= 0) score = score_at(named);
         teach.m = l0;
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             for (int k = t + TPR; k < P.k; k += TPR) {
                 int j = P.index[(size_t)row * P.k + k];
                 if (j < 0 || j >= P.m) j = -1;
-                const float l = j >= 0 ? (P.logits ? P.logits[(size_t)row * P.k + k] * P.inv_t : 0.f) : -INFINITY;
+                const float l = j >= 0 ? (P.logits ? P.logits[(size_t)row * P.k + k] : 0.f) : -INFINITY;
                 s_index[k] = j;
                 s_log[k] = l;
                 s_score[k] = j >= 0 ? score_at(j) : 0.f;
@@ -214,10 +214,10 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             }
         teach.m = group_max<SPAN>(teach.m);
         const float at = finite_max(teach.m);
-        teach.s = ex2f((l0 - at) * LOG2E);
+        teach.s = ex2f((l0 - at) * P.c);
         // (a thread reads back what it wrote)
         if constexpr (TPR < LS_MAX_K)
-            for (int k = t + TPR; k < P.k; k += TPR) teach.s += ex2f((s_log[k] - at) * LOG2E);
+            for (int k = t + TPR; k < P.k; k += TPR) teach.s += ex2f((s_log[k] - at) * P.c);
 #pragma unroll
         for (int off = SPAN / 2; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
     }
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     if constexpr (WARPS > 1) {
         if (lane == 0) { s_part[group][warp] = part; s_teach[group][warp] = teach; }
         group_sync();
-        teach = join<WARPS>(lane < WARPS ? s_teach[group][lane] : Part{-INFINITY, 0.f}, LOG2E);
+        teach = join<WARPS>(lane < WARPS ? s_teach[group][lane] : Part{-INFINITY, 0.f}, P.c);
         teach.s = __shfl_sync(0xffffffffu, teach.s, 0);
         part = join<WARPS>(lane < WARPS ? s_part[group][lane] : Part{-INFINITY, 0.f}, P.c);
         part.s = __shfl_sync(0xffffffffu, part.s, 0);
@@ -286,13 +286,13 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     if (warp * 32 < P.k) {
         const float log_all = __logf(teach.s) - __logf(part.s);
         // (q log q - q log p)
-        auto term = [&](float q, float l, float at) { return q != 0.f ? q * ((l - teach_at) - (at - part.m) * P.inv_t - log_all) : 0.f; };
-        own_q = ex2f((l0 - teach_at) * LOG2E) * teach_inv;
+        auto term = [&](float q, float l, float at) { return q != 0.f ? q * ((l - teach_at) * P.inv_t - (at - part.m) * P.inv_t - log_all) : 0.f; };
+        own_q = ex2f((l0 - teach_at) * P.c) * teach_inv;
         sum = term(own_q, l0, score);
         if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
         if constexpr (TPR < LS_MAX_K)
             for (int k = t + TPR; k < P.k; k += TPR) {
-                s_q[k] = ex2f((s_log[k] - teach_at) * LOG2E) * teach_inv;
+                s_q[k] = ex2f((s_log[k] - teach_at) * P.c) * teach_inv;
                 sum += term(s_q[k], s_log[k], s_score[k]);
             }
         if (rank == 0) {
@@ -403,7 +403,6 @@ template <bool BF16>
 __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __grid_constant__ Loss P)
 {
     constexpr int E = BF16 ? 8 : 4, PER = LL_PIECE / 16 / LL_THREADS;                 // vectors of a piece to a thread
-    constexpr float LOG2E = 1.44269504f;
     using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
     extern __shared__ __align__(128) unsigned char ring[];
     __shared__ __align__(8) unsigned long long bars[2 * LL_PIECES];
@@ -492,10 +491,10 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
         // ---- the teacher
         Part teach = {-INFINITY, 0.f};
         if (named < 0 || named >= P.m) named = -1;
-        const float l0 = named >= 0 ? logit * P.inv_t : -INFINITY;
+        const float l0 = named >= 0 ? logit : -INFINITY;
         if (warp * 32 < P.k) {
             teach.m = warp_max(l0);
-            teach.s = ex2f((l0 - finite_max(teach.m)) * LOG2E);
+            teach.s = ex2f((l0 - finite_max(teach.m)) * P.c);
 #pragma unroll
             for (int off = 16; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
         }
@@ -508,15 +507,15 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
         }
         part = join<32>(lane < LL_WARPS ? s_part[lane] : Part{-INFINITY, 0.f}, P.c);
         part.s = __shfl_sync(0xffffffffu, part.s, 0);
-        teach = join<32>(lane < LL_WARPS ? s_teach[lane] : Part{-INFINITY, 0.f}, LOG2E);
+        teach = join<32>(lane < LL_WARPS ? s_teach[lane] : Part{-INFINITY, 0.f}, P.c);
         teach.s = __shfl_sync(0xffffffffu, teach.s, 0);
         const bool live = teach.s != 0.f;                                             // (NaN, too)
         const float teach_at = finite_max(teach.m), teach_inv = live ? 1.f / teach.s : 0.f;
         float own_q = 0.f, sum = 0.f;
         if (warp * 32 < P.k) {
             const float log_all = __logf(teach.s) - __logf(part.s);
-            own_q = ex2f((l0 - teach_at) * LOG2E) * teach_inv;
-            if (own_q != 0.f) sum = own_q * ((l0 - teach_at) - (score - part.m) * P.inv_t - log_all);
+            own_q = ex2f((l0 - teach_at) * P.c) * teach_inv;
+            if (own_q != 0.f) sum = own_q * ((l0 - teach_at) * P.inv_t - (score - part.m) * P.inv_t - log_all);
             if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
 #pragma unroll
             for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);

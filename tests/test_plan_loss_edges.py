@@ -4,7 +4,7 @@ import ctypes
 
 import pytest
 
-from test_plan_loss import B, compare, inputs  # noqa: F401  (B is the fixture)
+from test_plan_loss import B, check, compare, inputs  # noqa: F401  (B is the fixture)
 
 
 @pytest.mark.gpu
@@ -35,6 +35,27 @@ def test_stretches_of_masked_scores_beside_scores_far_below_zero(B, rows, m, dty
         loss, grad = (v[:5].cpu() for v in B.plan_loss(s[many].cuda(), at[many].cuda(), t[many].cuda(), temperature=T, grad=True))
         bad = torch.tensor([False, False, True, True, False][:loss.shape[0]])
         assert torch.equal(torch.isnan(loss), bad) and torch.equal(torch.isnan(grad).all(1), bad) and torch.equal(torch.isnan(grad).any(1), bad)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,k", [(30, 5), (300, 40), (3000, 200), (20000, 33), (40000, 64)])
+def test_a_teachers_logits_may_all_be_shifted_and_be_of_any_finite_size(B, m, k):
+    import torch
+    for rows in (12, 300):
+        scores, index, t, weight = inputs(rows, m, k, torch.float32, k)
+        lowest, most = torch.finfo(torch.float32).min, torch.finfo(torch.float32).max
+        # the softmax of differences: a shift that all logits share is nothing to it, however small the temperature
+        check(B, scores * 0.01, index, (t * 0.01 + 1000.0), 0.01, weight)
+        check(B, scores * 0.01, index, (t * 0.01 - 5e4), 0.01, weight)
+        check(B, scores, index, t * 1e30, 3.0, weight)
+        t[0] = lowest                                                 # (a mask, where it leaves nothing else: all alike)
+        t[1], t[1, 3] = lowest, 1.0
+        t[2] = most
+        t[3, ::2] = lowest
+        t[4, 1:] = -float("inf")
+        t[5] = -float("inf")                                          # nothing
+        check(B, scores, index, t, 0.25, weight)
+        check(B, scores, index, t, 1.0, weight)
 
 
 @pytest.mark.gpu
