@@ -565,8 +565,9 @@ skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, co
  *   weight  [rows] fp32, may be null: 1
  *   grad    may be null, of the scores' type, `ldg` elements from row to row; may be scores itself, or lie between their rows, and is
  *            refused where it overlaps them otherwise (rows of another stride: where their ranges meet)
- * T from 1e-30 to 1e30, k <= 256, m <= 262143, rows < 2^31.  Sums are fp32, in an order that does not change from call to call.  One kernel on `stream` of
- * the current device, which reads a row once (longer ones than 131068 of fp32 or 262136 of bf16 twice).
+ * T from 1e-30 to 1e30, k <= 256, m <= 262143, rows < 2^31.  Sums are fp32, in an order that does not change from call to call: a loss
+ * is good to 2^-15 (1 + sum_k q_k (|log q_k| + |log p_index(k)|)), a gradient to |weight / T| (p_ij + sum of its q_k) 2^-15 (1 + |log p_ij| / 128) besides
+ * its type's rounding.  One kernel on `stream` of the current device, which reads a row once (longer ones than 131068 of fp32 or 262136 of bf16 twice).
  */
 skb_status sinkhorn_plan_loss(const void *scores, int dtype, long long rows, int m, long long ld, const int *index, const float *logits, int k,
                               float temperature, const float *weight, float *loss, void *grad, long long ldg, void *stream);

@@ -284,9 +284,9 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     const float teach_at = finite_max(teach.m), teach_inv = live ? 1.f / teach.s : 0.f;
     float own_q = 0.f, sum = 0.f;
     if (warp * 32 < P.k) {
-        const float log_all = __logf(teach.s) - __logf(part.s);
+        const float log_all = logf(part.s * teach_inv);                // (next to 1 in a confident row, where a fast logarithm is not good)
         // (q log q - q log p)
-        auto term = [&](float q, float l, float at) { return q != 0.f ? q * ((l - teach_at) * P.inv_t - (at - part.m) * P.inv_t - log_all) : 0.f; };
+        auto term = [&](float q, float l, float at) { return q != 0.f ? q * (((l - teach_at) - (at - part.m)) * P.inv_t + log_all) : 0.f; };
         own_q = ex2f((l0 - teach_at) * P.c) * teach_inv;
         sum = term(own_q, l0, score);
         if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
@@ -513,9 +513,9 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
         const float teach_at = finite_max(teach.m), teach_inv = live ? 1.f / teach.s : 0.f;
         float own_q = 0.f, sum = 0.f;
         if (warp * 32 < P.k) {
-            const float log_all = __logf(teach.s) - __logf(part.s);
+            const float log_all = logf(part.s) - logf(teach.s);
             own_q = ex2f((l0 - teach_at) * P.c) * teach_inv;
-            if (own_q != 0.f) sum = own_q * ((l0 - teach_at) * P.inv_t - (score - part.m) * P.inv_t - log_all);
+            if (own_q != 0.f) sum = own_q * (((l0 - teach_at) - (score - part.m)) * P.inv_t + log_all);
             if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
 #pragma unroll
             for (int off = 16; off; off /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, off);

@@ -2,9 +2,10 @@
 sums next to one; gradients in the place of tensors that a graph or another row still needs."""
 import ctypes
 
+import numpy as np
 import pytest
 
-from test_plan_loss import B, check, compare, inputs  # noqa: F401  (B is the fixture)
+from test_plan_loss import B, U, check, compare, inputs  # noqa: F401  (B is the fixture)
 
 
 @pytest.mark.gpu
@@ -56,6 +57,25 @@ def test_a_teachers_logits_may_all_be_shifted_and_be_of_any_finite_size(B, m, k)
         t[5] = -float("inf")                                          # nothing
         check(B, scores, index, t, 0.25, weight)
         check(B, scores, index, t, 1.0, weight)
+
+
+@pytest.mark.gpu
+def test_losses_of_confident_rows(B):
+    # log(1 + e), e = exp(-x): the exponential is off by 2 x U (its argument, twice) and 4 U, the sum by U of itself, the logarithm by 2 U of itself
+    import torch
+    x = torch.cat((torch.linspace(0.01, 16, 4001), torch.linspace(1e-4, 0.5, 777)))
+    want = np.log1p(np.exp(-x.double().numpy()))
+    e = np.exp(-x.double().numpy())
+    for m in (2, 77, 700, 70000):
+        n = len(x) if m < 1000 else 40
+        scores = torch.full((n, m), -float("inf"))
+        at = torch.arange(n) % (m - 1)
+        scores[torch.arange(n), at] = 3.0
+        scores[torch.arange(n), at + 1] = 3.0 - x[:n]
+        gap = (3.0 - scores[torch.arange(n), at + 1]).double().numpy()                # (exact in fp32)
+        want, e = np.log1p(np.exp(-gap)), np.exp(-gap)
+        loss = B.plan_loss(scores.cuda(), at.int()[:, None].cuda()).cpu().double().numpy()
+        assert (np.abs(loss - want) <= U * (1 + 2 * want + e / (1 + e) * (2 * gap + 4))).all()
 
 
 @pytest.mark.gpu
