@@ -166,8 +166,8 @@ __global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ 
 #pragma unroll
     for (int a = 0; a < PER; ++a) {
         const int r = r0 + 32 * a;
-        const bool masked = t * 128 + r >= len || g[a] == -INFINITY || norm[a] == INFINITY;
-        if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = masked ? -INFINITY : map_term(map_scale(P, w), g[a], norm[a]);
+        const bool hidden = t * 128 + r >= len || g[a] == -INFINITY, masked = hidden || norm[a] == INFINITY;
+        if (b0 == 0 && c16 == 0) P.terms[((size_t)w * tiles + t) * 128 + r] = hidden ? -INFINITY : map_term(map_scale(P, w), g[a], norm[a]);
         // what codes are multiplied by, 2^(120 + E), in one step where bf16 holds it; masked targets and their values are zeros
         const uint32_t e1 = min(e[a], 134u);
         uint32_t f = masked ? 0u : e[a] == 255u ? 0x7fffu : (e1 + 120u) << 7;
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
     float *tops = terms + 256;                                             // [2][128]: halves' maxima, and their sums at the end
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(tops + 256);
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + 32);
-    int *abort_flag = reinterpret_cast<int *>(tmem_holder + 1);
+    int *abort_flag = reinterpret_cast<int *>(tmem_holder + 1), *mine = abort_flag + 1;      // mine: the first of this part's tiles, among all lanes', and how many
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     constexpr int FULL = 0, EMPTY = MT_MAX_STAGES, SFULL = 2 * MT_MAX_STAGES, PFULL = SFULL + 2, ODONE = PFULL + 2, TFULL = ODONE + 1, TEMPTY = TFULL + 2,
                   LAST = TEMPTY + 2, XFULL = LAST + 1;
@@ -232,6 +232,8 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         mbar_init(bar(ODONE), 1);
         mbar_init(bar(LAST), 1);
         mbar_init(bar(XFULL), 1);
+        mine[0] = w * lane_tiles + t0;                                     // (here, as they take registers of the softmax else, which has none left)
+        mine[1] = nt;
         *abort_flag = (base & 1023u) ? 1 : 0;                              // (the swizzle counts from 1024-byte boundaries)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -396,10 +398,22 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         ok = __all_sync(0xffffffffu, ok);
         const float nan = __uint_as_float(0x7fffffffu);
         float total = ok ? (float)sum : nan;
+        // Where a query or eps is no number, scores of masked targets are NaN like others: a sum that is NaN is one of nothing if no target of this part counts.
+        // (The terms once more, for such sums alone: a comparison in the softmax takes one percent of the whole.)
+        if (!all_of<32 * MT_SOFT>(total == total, 5)) {
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            const volatile int *own = mine;
+            const float *term = P.terms + (size_t)own[0] * 128;
+            const int count = own[1] * 128;
+            bool any = !ok;
+            for (int i = tid; i < count; i += 32 * MT_SOFT) any |= term[i] != -INFINITY;
+            if (all_of<32 * MT_SOFT>(!any, 5)) { total = 0.f; ref = -INFINITY; }
+        }
         // (both halves leave the loop at the same tile, after they have read its maxima, or neither has)
         tops[128 * half + q] = total;
         asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
         total += tops[128 * (1 - half) + q];
+        const bool some = __any_sync(0xffffffffu, total != 0.f);          // (else there are no images)
         const bool live = i0 + q < P.n;
         const size_t row = (size_t)w * P.n + i0 + (live ? q : 0);
         const float inv = P.splits > 1 ? (total == total ? 1.f : nan) : total == 0.f ? 0.f : 1.f / total;
@@ -410,7 +424,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             const int dim = dv0 + half * (DVC / 2) + c;
             if (dim >= P.dv) break;
             uint32_t o[32];
-            if (nt > 0) {
+            if (some) {
                 tc_ld32_issue(tO + lanes + half * (DVC / 2) + c, o);
                 tc_ld_wait(o);
             } else
