@@ -537,7 +537,8 @@ skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int 
  *      z_ij = (g_j - |x_i - y_j|^2) / eps,   lse_i = log sum_j exp z_ij,   out_i = sum_j exp(z_ij - lse_i) v_j.
  * With the target's potential g [W, m] (float64, as the solver gives it; null: zeros) this is the plan's barycentric image of a source
  * point, and of any other point its extension; -eps lse_i is the source's potential there, less eps log(1 / n).
- *   g_j = -inf masks a target whatever its point and values hold; so does an index from lengths_t on
+ *   g_j = -inf masks a target whatever its point and values hold; so does an index from lengths_t on.  (Finite ones do not, however low: exponents below
+ *            fp32's range are its lowest value)
  *   lengths  [W] int, may be null: targets of a lane that count, 0 .. m (others are cut to that)
  *   out      [W, n, dv] bf16; lse [W, n] fp32, may be null
  * A query without targets has an image of zeros and lse = -inf.  A query, an unmasked target or its value that is NaN, a potential that is

@@ -39,8 +39,13 @@ __device__ __forceinline__ double map_scale(const Map &P, int w)
     const float eps = P.eps[w];
     return eps > 0.f && eps <= 3.402823466e38f ? 1.4426950408889634 / (double)eps : __longlong_as_double(0x7ff8000000000000LL);
 }
-// What a target adds to the exponent of every query, in powers of two; minus infinity: it is masked, whatever its codes.
-__device__ __forceinline__ float map_term(double k, double g, float norm) { return g == -INFINITY ? -INFINITY : (float)(k * (g - (double)norm)); }
+// What a target adds to the exponent of every query, in powers of two; minus infinity: it is masked, whatever its codes.  (What is below fp32's range is
+// its lowest value: a finite potential masks nothing by itself.)
+__device__ __forceinline__ float map_term(double k, double g, float norm)
+{
+    const float term = (float)(k * (g - (double)norm));
+    return g == -INFINITY ? -INFINITY : term == -INFINITY && norm < INFINITY ? -3.402823466e38f : term;
+}
 // natural logarithm of the sum of exponentials, from the largest exponent and the sum against it (powers of two) and |x|^2
 __device__ __forceinline__ float map_lse(float top, float sum, double k, double xx)
 {
