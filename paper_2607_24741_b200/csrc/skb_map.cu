@@ -871,7 +871,7 @@ static size_t map_workspace(int W, int n, int m, int d, int dv, bool own_values)
 {
     // (what any device may split into: the workspace does not depend on the current one)
     const MapPlan p = map_plan(W, n, m, d, dv, own_values, MAP_MAX_SMS);
-    return 256 + map_parts_bytes(W, n, dv, p.splits) + (p.tiles ? pad256(map_staged_bytes(W, m, d, dv, own_values)) : 0);
+    return 256 + map_parts_bytes(W, n, dv, p.splits) + (p.tiles ? pad256(map_staged_bytes(W, n, m, d, dv, own_values, p.splits)) : 0);
 }
 
 extern "C" size_t sinkhorn_cloud8_map_workspace_bytes(int W, int n, int m, int d, int dv)

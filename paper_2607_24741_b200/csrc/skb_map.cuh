@@ -26,10 +26,11 @@ struct Map {
     int own_values;                           // v is not y
     unsigned char *staged_y, *staged_v;       // many queries: bank and values as bf16 (the same where v is y)
     float *terms;                             // ... and what targets add to exponents, [W, tiles, 128]
+    float *sums;                              // ... and blocks' images of what is behind them, where parts are long; null: they are not
 };
 
-// Many queries (skb_map_tc.cu): d <= MAP_TILES_MAX_D, P.splits parts of a lane's bank, room for the bank in bf16 (256-byte aligned).
-size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values);
+// Many queries (skb_map_tc.cu): d <= MAP_TILES_MAX_D, P.splits parts of a lane's bank, room for the bank in bf16 and blocks' sums (256-byte aligned).
+size_t map_staged_bytes(int W, int n, int m, int d, int dv, bool own_values, int splits);
 skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st);
 
 __device__ __forceinline__ int map_length(const Map &P, int w) { return P.lengths ? min(max(P.lengths[w], 0), P.m) : P.m; }

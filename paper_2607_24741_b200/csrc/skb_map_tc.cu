@@ -25,6 +25,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <string>
+#include <type_traits>
 
 #include "skb_f32x2.cuh"
 #include "skb_map.cuh"
@@ -39,6 +40,10 @@ constexpr uint32_t MT_CHUNK = 128 * 128, MT_BLOCK = 2 * MT_CHUNK;         // 128
 constexpr int MT_MAX_STAGES = 8;
 constexpr uint32_t MT_MISC = 3 * 1024;
 constexpr float MT_SLACK = 8.f;
+// Tiles whose images are added up in tensor memory.  The matrix unit cuts each of an instruction's 16 products and the sum so far at 2^-25 of the largest,
+// and the result at 24 bits: 17 2^-25 + 2^-23 < 2^-20.6 of the sum for every 16 targets, always towards zero.  Over a bank of 262143 that is a
+// quarter of a percent of images whose values have one sign; over 64 tiles at most 2^-11.6.
+constexpr int MT_CHAIN = 64;
 
 // D fp32, A and B bf16, 128 queries (a pair of blocks: 256) by 128
 template <bool PAIR> constexpr uint32_t MT_IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | (((PAIR ? 256u : 128u) >> 4) << 24);
@@ -192,8 +197,9 @@ __global__ void __launch_bounds__(256) map_stage_kernel(const __grid_constant__ 
 }
 
 // PAIR: two blocks of a cluster share what they read, half of the targets (scores) or of the dimensions (images) of a stage each; the first issues
-// the instructions of both, on 256 queries.
-template <int DVC, bool PAIR>
+// the instructions of both, on 256 queries.  LONG: a part may have more tiles than MT_CHAIN.  (A kernel of its own: the softmax has no registers left for what that
+// takes; 64 x 1024 x 1024 x 512 would take 1 % longer.  Parts that are long take 2 to 3 % longer for it.)
+template <int DVC, bool PAIR, bool LONG>
 __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_constant__ CUtensorMap tmx, const __grid_constant__ CUtensorMap tmy,
                                                                   const __grid_constant__ CUtensorMap tmv, const __grid_constant__ Map P, const int nrt,
                                                                   const int stages, const int lane_tiles, const int tma_x, const int wave)
@@ -213,6 +219,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
     float *tops = terms + 256;                                             // [2][128]: halves' maxima, and their sums at the end
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(tops + 256);
     uint32_t *tmem_holder = reinterpret_cast<uint32_t *>(bars + 32);
+    float *refs = reinterpret_cast<float *>(bars + 36);                    // [128]: what the images in P.sums are against
     int *abort_flag = reinterpret_cast<int *>(tmem_holder + 1), *mine = abort_flag + 1;      // mine: the first of this part's tiles, among all lanes', and how many
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     constexpr int FULL = 0, EMPTY = MT_MAX_STAGES, SFULL = 2 * MT_MAX_STAGES, PFULL = SFULL + 2, ODONE = PFULL + 2, TFULL = ODONE + 1, TEMPTY = TFULL + 2,
@@ -278,9 +285,38 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
         const bool starts = ok;
         const bool want_xx = P.lse && z == 0 && P.splits == 1;
         double xx = 0.0;
+        // images in P.sums: a block's lie together, a thread's 256 floats apart
+        auto sums_of = [&] {
+            return P.sums + (blockIdx.x + (size_t)gridDim.x * (blockIdx.y + (size_t)gridDim.y * blockIdx.z)) * (128 * DVC) + tid;
+        };
+        // ... which are multiplied by this when the reference is another
+        auto since = [&](float was) { return was == -INFINITY ? 0.f : ex2_fast(was - ref); };
+        if (LONG && half == 0) refs[q] = -INFINITY;
         for (int t = 0; t < nt && starts; ++t) {
             const int b = t & 1;
             const uint32_t ph = (uint32_t)(t >> 1) & 1u;
+            if (LONG && t && t % MT_CHAIN == 0) {
+                // what has been added up in tensor memory joins the rest in fp32; the instructions begin anew.  (One phase after the other: see the end.)
+                ok = ok && mbar_wait(bar(ODONE), (uint32_t)(t - 2) & 1u, ab) && mbar_wait(bar(ODONE), (uint32_t)(t - 1) & 1u, ab);
+                ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+                const float was = refs[q], fac = since(was);
+                asm volatile("bar.sync %0, 64;" ::"r"(1 + (warp & 3)) : "memory");
+                if (half == 0) refs[q] = ref;
+                float *at = sums_of();
+                if (ok)
+#pragma unroll 1
+                    for (int c = 0; c < DVC / 2; c += 16, at += 16 * 32 * MT_SOFT) {
+                        uint32_t o[16];
+                        float rest[16];                                    // (all loads before the first store)
+                        tc_ld16_issue(tO + lanes + half * (DVC / 2) + c, o);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) rest[i] = t > MT_CHAIN ? at[i * 32 * MT_SOFT] : 0.f;
+                        tc_ld16_wait(o);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) at[i * 32 * MT_SOFT] = fmaf(rest[i], fac, __uint_as_float(o[i]));
+                    }
+            }
             ok = ok && mbar_wait(bar(TFULL + b), ph, ab) && mbar_wait(bar(SFULL + b), ph, ab);
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
@@ -430,6 +466,12 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
             } else
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] = 0u;
+            if (LONG && some && nt > MT_CHAIN) {
+                const float fac = since(refs[q]);
+                const float *at = sums_of() + c * 32 * MT_SOFT;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(fmaf(at[i * 32 * MT_SOFT], fac, __uint_as_float(o[i])));
+            }
             if (P.splits > 1) {
                 float *dst = P.part_out + (row * P.splits + split) * P.dv + dim;
 #pragma unroll
@@ -575,7 +617,7 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
                     const uint64_t vd = v0 + (uint64_t)(s * (int)(STAGE >> 4));
                     const uint32_t out = tO + 128 * b, weights = tmem + 128 * (u & 1);
                     if (elected()) {
-                        mma_tmem<PAIR>(out, weights, vd, u ? 1u : 0u);
+                        mma_tmem<PAIR>(out, weights, vd, (LONG ? u % MT_CHAIN : u) ? 1u : 0u);
 #pragma unroll
                         for (int q = 1; q < 8; ++q) mma_tmem<PAIR>(out, weights + 8 * q, vd + q * (2048 >> 4), 1u);
                         commit<PAIR>(bar(EMPTY + s));
@@ -603,14 +645,14 @@ __global__ void __launch_bounds__(MT_THREADS, 1) map_tiles_kernel(const __grid_c
     }
 }
 
-template <int DVC, bool PAIR>
+template <int DVC, bool PAIR, bool LONG>
 skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMap &tv, const Map &P, int tma_x, int sms, cudaStream_t st)
 {
     constexpr int stage = PAIR ? (int)MT_BLOCK / 2 : (int)MT_BLOCK;
     const int nkc = (P.d + 63) / 64, blocks = (P.n + 127) / 128, nrt = PAIR ? (blocks + 1) / 2 * 2 : blocks, nz = (P.dv + DVC - 1) / DVC;
     const int stages = min(MT_MAX_STAGES, (MAP_TILES_SMEM - (int)MT_MISC - nkc * (int)MT_CHUNK) / stage);
     const int smem = nkc * (int)MT_CHUNK + stages * stage + (int)MT_MISC;
-    cudaFuncSetAttribute(map_tiles_kernel<DVC, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    cudaFuncSetAttribute(map_tiles_kernel<DVC, PAIR, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(nrt * nz, P.splits, P.W);
     cfg.blockDim = dim3(MT_THREADS);
@@ -625,16 +667,22 @@ skb_status launch(const CUtensorMap &tx, const CUtensorMap &ty, const CUtensorMa
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = PAIR ? 2 : 1;
-    cudaLaunchKernelEx(&cfg, map_tiles_kernel<DVC, PAIR>, tx, ty, tv, P, nrt, stages, (P.m + 127) / 128, tma_x, sms);
+    cudaLaunchKernelEx(&cfg, map_tiles_kernel<DVC, PAIR, LONG>, tx, ty, tv, P, nrt, stages, (P.m + 127) / 128, tma_x, sms);
     return op_launched("map");
 }
 
 }  // namespace
 
-size_t map_staged_bytes(int W, int m, int d, int dv, bool own_values)
+// rows of 128 queries, and columns of values, that a launch's blocks take
+static int row_blocks(int n) { return n > 128 ? (n + 255) / 256 * 2 : 1; }
+static int value_depth(int dv) { return dv <= 128 ? 128 : (dv + 255) / 256 * 256; }
+
+size_t map_staged_bytes(int W, int n, int m, int d, int dv, bool own_values, int splits)
 {
-    const size_t tiles = (size_t)W * ((m + 127) / 128);
-    return tiles * 512 + tiles * MT_BLOCK * ((d + 127) / 128 + (own_values ? (dv + 127) / 128 : 0));
+    const int lane_tiles = (m + 127) / 128;
+    const size_t tiles = (size_t)W * lane_tiles;
+    const size_t sums = lane_tiles > MT_CHAIN ? (size_t)W * splits * row_blocks(n) * 128 * value_depth(dv) * sizeof(float) : 0;
+    return tiles * 512 + tiles * MT_BLOCK * ((d + 127) / 128 + (own_values ? (dv + 127) / 128 : 0)) + sums;
 }
 
 skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st)
@@ -643,6 +691,7 @@ skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st)
     P.staged_y = (unsigned char *)room;
     P.staged_v = P.own_values ? P.staged_y + (size_t)P.W * tiles * nby * MT_BLOCK : P.staged_y;
     P.terms = (float *)(P.staged_y + (size_t)P.W * tiles * (nby + nbv) * MT_BLOCK);
+    P.sums = tiles > MT_CHAIN ? P.terms + (size_t)P.W * tiles * 128 : nullptr;
     map_stage_kernel<<<dim3(nby + nbv, tiles, P.W), 256, 0, st>>>(P, nby, nbv);
     const skb_status rc = op_launched("map");
     if (rc != SKB_OK) return rc;
@@ -653,8 +702,14 @@ skb_status launch_map_tiles(Map &P, void *room, int sms, cudaStream_t st)
         (pair && (!staged_map(&ty, P.staged_y, (size_t)P.W * tiles * nby * 256) ||
                  !staged_map(&tv, P.staged_v, (size_t)P.W * tiles * (P.own_values ? nbv : nby) * 256))))
         return op_fail(SKB_ERR_CUDA, "cuTensorMapEncodeTiled failed");
-    if (pair) return P.dv <= 128 ? launch<128, true>(tx, ty, tv, P, tma_x, sms, st) : launch<256, true>(tx, ty, tv, P, tma_x, sms, st);
-    return P.dv <= 128 ? launch<128, false>(tx, ty, tv, P, tma_x, sms, st) : launch<256, false>(tx, ty, tv, P, tma_x, sms, st);
+    const bool longer = (tiles + P.splits - 1) / P.splits > MT_CHAIN;
+    const auto by_depth = [&](auto two, auto chained) {
+        return P.dv <= 128 ? launch<128, two.value, chained.value>(tx, ty, tv, P, tma_x, sms, st) : launch<256, two.value, chained.value>(tx, ty, tv, P, tma_x, sms, st);
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if (pair) return longer ? by_depth(yes, yes) : by_depth(yes, no);
+    return longer ? by_depth(no, yes) : by_depth(no, no);
 }
 
 }  // namespace skb

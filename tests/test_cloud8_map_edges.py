@@ -2,7 +2,7 @@
 values of one sign, products that one dimension carries, values far larger than those that have the weights."""
 import pytest
 
-from test_cloud8_map import B, formula, inputs, run  # noqa: F401  (B is the fixture)
+from test_cloud8_map import B, U, formula, inputs, run  # noqa: F401  (B is the fixture)
 
 
 def staged(B, W, n, m, d, dv=0):
@@ -67,3 +67,57 @@ def test_potentials_of_the_lowest_finite_values_are_no_masks(B, n, m, many):
     g = torch.where(g < -1e30, -float("inf"), g)
     want, wl, err, lerr = formula(x[pick], B.cloud8_pack(y.cuda()).values().cpu()[pick], g[pick], eps[pick], vv[pick], None)
     assert ((out[pick] - want).abs() <= err).all() and ((lse[pick] - wl).abs() <= lerr).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,m,dv", [(9600, 262143, 16), (5, 262143, 16), (4864, 100001, 300), (300, 262143, 130)])
+def test_long_banks_whose_values_have_one_sign(B, n, m, dv):
+    # All points are zero, so weights are 2^(g / eps log2 e), between 1/2 and 1, and rounded to bf16 (rounding of them cancels over the bank; the second
+    # e4m3 number of the kernel for few queries leaves less).  The values are positive, but for the last targets, which take back what the others came
+    # to: what is left shows a sum's error without bf16's rounding of the image.
+    #
+    # The matrix unit cuts each of 16 products and the sum so far at 2^-25 of the largest, the result at 24 bits: 17 2^-25 + 2^-23 < 2^-20.6 of the sum
+    # for each 16 targets, and sums of at most 64 tiles of 128 are added in fp32: 512 2^-20.6 = 2^-11.6 of the sum of magnitudes, 2^-16 for the
+    # rest.
+    import torch
+    gen = torch.Generator().manual_seed(m)
+    d, last = 16, 100
+    g = -torch.rand(1, m, generator=gen, dtype=torch.float64) * 0.69
+    g[0, -last:] = 0.0
+    g[0, 0] = 0.0
+    v = 1.0 + torch.rand(1, m, dv, generator=gen)
+    v8 = B.cloud8_pack(v.cuda()).values().cpu().double()
+    w = torch.exp(g[0])
+    rounded = w.float().bfloat16().double() if staged(B, 1, n, m, d, dv) else w
+    v[0, -last:] = -(rounded[:-last] @ v8[0, :-last] / last).float()
+    v8 = B.cloud8_pack(v.cuda()).values().cpu().double()
+    x, y, eps = torch.zeros(1, n, d, dtype=torch.bfloat16), torch.zeros(1, m, d), torch.ones(1)
+    out, lse, _, _ = run(B, x, y, g, eps, v)
+    want, size = rounded @ v8[0] / w.sum(), w @ v8[0].abs() / w.sum()
+    assert ((out[0] - want).abs() <= (2.0 ** -11.6 + 2.0 ** -16) * size + 2.0 ** -8 * want.abs()).all(), float(((out[0] - want).abs() / size).max())
+    assert ((lse[0] - torch.log(w.sum())).abs() <= 2.0 ** -16 + 2 * U * 13).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("W,n,m,dv", [(38, 140, 20000, 0), (20, 140, 30000, 150), (80, 100, 17000, 40)])
+def test_long_banks_whose_exponents_rise_fall_begin_late_and_end_early(B, W, n, m, dv):
+    # sums in parts of 64 tiles meet references that have been raised since, or that were not there yet
+    import torch
+    assert staged(B, W, n, m, 32, dv)
+    x, y, g, eps, v = inputs(8, n, m, 32, dv, eps=0.3)
+    ramp = torch.linspace(0, 12, m, dtype=torch.float64)
+    g[0], g[1] = ramp, ramp.flip(0)
+    g[2, :9000] = -float("inf")
+    g[3, 8191:] = -float("inf")
+    g[4, 5:m - 5] = -float("inf")
+    g[5, 8190:8200] += 30
+    x[6, 1, 3] = float("nan")
+    lengths = torch.tensor([m, m, m, m, m, m, 8193, 8192], dtype=torch.int32)
+    more = lambda t: None if t is None else t[torch.arange(W) % 8]
+    out, lse, yv, vv = run(B, *(more(t) for t in (x, y, g, eps, v)), more(lengths))
+    for t in list(range(8)) + [W - 1]:
+        one = slice(t % 8, t % 8 + 1)
+        want, wl, err, lerr = formula(x[one], yv[one], g[one], eps[one], vv[one], lengths[one])
+        good = torch.arange(n) != (1 if t % 8 == 6 else -1)
+        assert ((out[t] - want[0]).abs() <= err[0])[good].all() and ((lse[t] - wl[0]).abs() <= lerr[0])[good].all(), t
+    assert torch.isnan(out[6, 1]).all() and torch.isnan(lse[6, 1])
