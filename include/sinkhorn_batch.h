@@ -526,9 +526,9 @@ skb_status sinkhorn_cloud8_pack(const void *v, int v_dtype, int W, int npts, int
 skb_status sinkhorn_cloud8_unpack(const void *cloud, int W, int npts, int d, void *values, int values_dtype, void *stream);
 /*
  * Products of two 8-bit clouds, out[t, i, j] = x_ti . y_tj of the values they stand for: x [W, n, d], y [W, m, d] buffers of
- * sinkhorn_cloud8_pack, out [W, n, m] fp32, on the block-scaled tensor cores with fp32 accumulation.  A point that is NaN gives NaN in its row
- * or column.  One kernel on `stream` of the current device; out is written 16 bytes at a time where m is a multiple of 4 and out
- * 16-byte aligned.
+ * sinkhorn_cloud8_pack, out [W, n, m] fp32, on the block-scaled tensor cores with fp32 accumulation: off by at most 2^-19.8 of the sum of the
+ * products' magnitudes for every 32 dimensions.  A point that is NaN gives NaN in its row or column.  One kernel on `stream` of the current device;
+ * out is written 16 bytes at a time where m is a multiple of 4 and out 16-byte aligned.
  */
 skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int m, int d, float *out, void *stream);
 /*
@@ -543,7 +543,8 @@ skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int 
  *   out      [W, n, dv] bf16; lse [W, n] fp32, may be null
  * A query without targets has an image of zeros and lse = -inf.  A query, an unmasked target or its value that is NaN, a potential that is
  * NaN or plus infinity, and an eps that is not a positive number make the images they take part in NaN.
- * Exponents are made of fp32 products of the bf16 query and the bank's values, good to (d / 32 + 8) 2^-24 (|x|^2 + |y|^2 + |g|) / eps; weights, for
+ * Exponents are made of fp32 products of the bf16 query and the bank's values, good to (0.67 d + 8) 2^-24 (|x|^2 + |y|^2 + |g|) / eps
+ * (d to a whole 32: the matrix unit cuts products and sums off, and a sum that one dimension carries loses at every instruction); weights, for
  * the product with the values, are rounded to 8 bits, sums are fp32, and one of an image loses at most 2^-11.6 of its terms' magnitudes, however long the bank is.  With few queries, short banks or d above 512 a value's part of an image is besides
  * off by up to 2^-21 of the largest value that its 128 dimensions hold among the 128 targets of a tile.  out must not overlap x.
  * d and dv <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on `stream` of the current device and returns; the workspace of

@@ -121,3 +121,31 @@ def test_long_banks_whose_exponents_rise_fall_begin_late_and_end_early(B, W, n, 
         good = torch.arange(n) != (1 if t % 8 == 6 else -1)
         assert ((out[t] - want[0]).abs() <= err[0])[good].all() and ((lse[t] - wl[0]).abs() <= lerr[0])[good].all(), t
     assert torch.isnan(out[6, 1]).all() and torch.isnan(lse[6, 1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,many", [(5, False), (300, True)])
+@pytest.mark.parametrize("d", [64, 512, 1024])
+def test_exponents_whose_products_one_dimension_carries(B, n, many, d):
+    # A large first product and small ones of one sign beside it, each cut off where the sum begins: (0.67 d + 8) U of what an exponent is made of
+    # (d to a whole 32): 17 2^-25 + 2^-23 < 2^-20.6 for each 16 dimensions in bf16, 33 2^-25 + 2^-23 < 2^-19.8 for each 32 in 8 bits, a fifteenth
+    # more for the query's three parts; 8 for the terms in fp32
+    import torch
+    W, m = 7, 1500
+    if staged(B, W, n, m, d) != many:
+        assert d > 512
+        return
+    x = torch.full((W, n, d), 255 / 128 * 2.0 ** -9).bfloat16()
+    x[:, :, 0] = 1.0
+    y = torch.full((W, m, d), 1.875 * 2.0 ** -8)
+    y[:, :, ::128] = 1.0
+    y[:, :, 128::128] = 2.0 ** -1
+    g = torch.full((W, m), -float("inf"), dtype=torch.float64)
+    g[:, 1234] = 0.0
+    eps = torch.full((W,), 1e-3)
+    out, lse, yv, _ = run(B, x, y, g, eps)
+    yv = yv[:, 1234].double()
+    z = -(x.double() - yv[:, None]).square().sum(2) / eps.double()[:, None]
+    made_of = (x.double().square().sum(2) + yv.square().sum(1)[:, None]) / eps.double()[:, None]
+    assert ((lse - z).abs() <= (0.67 * (-(-d // 32) * 32) + 8) * U * made_of).all(), float(((lse - z).abs() / made_of / U).max())
+    assert ((out - yv[:, None]).abs() <= 2.0 ** -8 * yv[:, None].abs()).all()
