@@ -546,7 +546,8 @@ skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int 
  * Exponents are made of fp32 products of the bf16 query and the bank's values, good to (0.67 d + 8) 2^-24 (|x|^2 + |y|^2 + |g|) / eps
  * (d to a whole 32: the matrix unit cuts products and sums off, and a sum that one dimension carries loses at every instruction); weights, for
  * the product with the values, are rounded to 8 bits, sums are fp32, and one of an image loses at most 2^-11.6 of its terms' magnitudes, however long the bank is.  With few queries, short banks or d above 512 a value's part of an image is besides
- * off by up to 2^-21 of the largest value that its 128 dimensions hold among the 128 targets of a tile.  out must not overlap x.
+ * off by up to 2^-18 of the largest product of a weight and a value that its 128 dimensions hold among the 128 targets of a tile.  Weights times values
+ * are added up before they are divided: values above 2^100 may pass fp32's range.  out must not overlap x.
  * d and dv <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on `stream` of the current device and returns; the workspace of
  * sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv) bytes (0: a bad shape; dv = 0: v is null; device, 256-byte aligned) is in use until
  * they are done: calls that may overlap need one each.

@@ -11,8 +11,8 @@
 //            24 bits: 33 2^-25 + 2^-23 < 2^-19.8 of the magnitudes for every 32 dimensions, which is what exponents are good to
 //   softmax  a thread to a target: exponentials in fp32 against the tile's maximum of the query, which carries over to a running one in fp32
 //   images   O^T = V^T . P^T, 128 dimensions by the queries: kind::f8f6f4 on the codes, in the same place of shared memory, now the operand whose rows lie
-//            next to each other (M-major).  Weights times the values' powers of two, less the tile's largest, are two e4m3 numbers (eight bits; what is below
-//            2^-22 of the tile's largest is lost), rows of their own again
+//            next to each other (M-major).  Weights times the values' powers of two are two e4m3 numbers (eight bits; what is below 2^-22 of the reference is
+//            lost), rows of their own again.  The reference is the tile's largest power of two, or where these are far apart the query's largest product
 // so that nothing of a code passes through a register.  The same work by mma.sync, codes made f16 in registers, was bound by its instructions: one query
 // to each of 8 banks of 16384 x 512 took 41 us.
 // That call takes 27 us for 69 MB now, twelve queries to each of 32 banks of 8192 x 128 with values of 64 dimensions 31 us for 54 MB.  Of the first some
@@ -42,6 +42,7 @@ namespace {
 constexpr int MR_T = 128;                                     // points of a tile
 constexpr uint32_t MR_SLOT = MR_T * 128;
 constexpr int MR_MAX_SLOTS = 16, MR_MAX_BLOCKS = 8, MR_AHEAD = 6;     // MR_AHEAD: tiles whose scales and terms are there at once
+constexpr int MR_SPREAD = 3;                                  // how far apart values' powers of two of a tile may be for their largest to be all weights' reference
 // rows of the queries' operand: three numbers of each query, and how many rows the instruction takes
 template <int NQ> constexpr int MR_ROWS = NQ == 8 ? 32 : 48;
 template <int NQ> constexpr int MR_SCOLS = NQ == 8 ? 32 : 64;  // columns of tensor memory that its result takes
@@ -135,12 +136,91 @@ __host__ __device__ inline MapRows map_rows_layout(int d, int nb, int yslots, in
     L.p = L.x + (uint32_t)(L.nby * MR_ROWS<NQ>) * 128;
     L.scales = L.p + 2 * (uint32_t)(L.nb * 2 * NQ) * 128;
     L.small = L.scales + (MR_AHEAD + 1) * (uint32_t)L.words * 512;
-    // terms, values' scales, maxima, factors, tops, sums, runs, lengths, barriers
-    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4 + 4 * NQ * 4) + 12 * NQ * 16 + 2 * 4 * NQ * 4 + 2 * NQ * 4 + NQ * 8 + 64 * 8 + 16;
+    // terms, values' scales, maxima, factors, tops, sums, runs, largest products, lengths, barriers
+    L.bytes = L.small + MR_AHEAD * (128 * 4 + 128 * 8 + MR_MAX_BLOCKS * 4 + 4 * NQ * 4) + 12 * NQ * 16 + 2 * 4 * NQ * 4 + 2 * NQ * 4 + 2 * 4 * (uint32_t)nb * NQ * 4 +
+              NQ * 8 + 64 * 8 + 32;
     const uint32_t used = 2 * MR_SCOLS<NQ> + 2 * (uint32_t)(L.nb * 2 * NQ) + 12 * (uint32_t)L.words;
     L.columns = 32;
     while (L.columns < used) L.columns *= 2;
     return L;
+}
+
+// four queries' weights of target p as two e4m3 numbers each, into a block of 128 dimensions' operand (from the target's byte on)
+template <int NQ> __device__ __forceinline__ void put_weights(unsigned char *block, int p, int q, float a0, float a1, float a2, float a3)
+{
+    const uint32_t lo = e4m3_two(a0, a1), hi = e4m3_two(a2, a3);
+    const float2 bl = e4m3_pair(lo), bh = e4m3_pair(hi);
+    const uint32_t lo2 = e4m3_two((a0 - bl.x) * 16.f, (a1 - bl.y) * 16.f), hi2 = e4m3_two((a2 - bh.x) * 16.f, (a3 - bh.y) * 16.f);
+    auto put = [&](int r, uint32_t byte) { block[r * 128 + (((p >> 4) ^ (r & 7)) << 4)] = (unsigned char)byte; };
+    put(q, lo); put(q + 1, lo >> 8); put(q + 2, hi); put(q + 3, hi >> 8);
+    put(NQ + q, lo2); put(NQ + q + 1, lo2 >> 8); put(NQ + q + 2, hi2); put(NQ + q + 3, hi2 >> 8);
+}
+// Values of a tile whose powers of two differ by more than MR_SPREAD: against the largest of them, weights of the others would leave the numbers' range, whatever
+// little weight the largest has.  A query's weights times the powers are taken against the largest of these products then, 2^M of each 128
+// dimensions (M - top, with weights against the tile's maximum), which takes that maximum, too, and a second barrier.  Calls, so that the usual way keeps its
+// registers (one query to 8 banks of 16384 x 512: 27.2 us without this, 27.9 with calls, 29.1 in line; twelve to 32 of 8192 x 128 31.0, 31.1, 33.2).  Where
+// every tile goes this way: twelve to 32 of 8192 x 128 with values of 64, 42; one to 8 of 16384 x 512 with values of 512, 40.7 for 38.0.
+__device__ __forceinline__ float largest_of(const float *r, int stride) { return fmaxf(fmaxf(r[0], r[stride]), fmaxf(r[2 * stride], r[3 * stride])); }
+__device__ __forceinline__ float less_top(float m, float top) { return m == -INFINITY ? 0.f : m - top; }
+template <int NQ>
+__device__ __noinline__ bool weights_apart(bool ok, const float (&arg)[NQ], const float4 *own, uint2 scales, float *reach, unsigned char *weights, int nb, int vblocks,
+                                           int p, int nq, int barrier)
+{
+    const int lane = p & 31, part = p >> 5;
+    auto power = [&](int u) { return (int)(((u < 4 ? scales.x : scales.y) >> (8 * (u & 3))) & 255u); };
+    for (int u = 0; u < nb; ++u) {
+        const float e = power(u) == 255 ? -INFINITY : (float)(power(u) - 127);
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const float m = warp_max(arg[q] + e);
+            if (lane == q) reach[(part * vblocks + u) * NQ + q] = m;
+        }
+    }
+    if (!all_softmax(ok, barrier)) return false;
+    for (int u = 0; u < nb; ++u) {
+        const float e = power(u) == 255 ? __uint_as_float(0x7fffffffu) : (float)(power(u) - 119);              // (256 times)
+#pragma unroll
+        for (int q = 0; q < NQ; q += 4) {
+            if (q >= nq) break;
+            float a[4];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const float top = own[q + h].x;
+                a[h] = arg[q + h] == -INFINITY ? 0.f : ex2f((arg[q + h] - top) + (e - less_top(largest_of(reach + u * NQ + q + h, vblocks * NQ), top)));
+            }
+            put_weights<NQ>(weights + u * (2 * NQ) * 128, p, q, a[0], a[1], a[2], a[3]);
+        }
+    }
+    return true;
+}
+// ... and the tile's images, back to the weights' reference, in their place in tensor memory
+template <int NQ>
+__device__ __noinline__ void images_apart(uint32_t at, const float *reach, const float *maxima, int nb, int vblocks, int lane)
+{
+    for (int u = 0; u < nb; ++u) {
+        float unit = 0.f;                                                            // of the query that is the lane's number
+        if (lane < NQ) {
+            const float top = largest_of(maxima + lane, NQ);
+            unit = ex2f(less_top(largest_of(reach + u * NQ + lane, vblocks * NQ), top == -INFINITY ? 0.f : top));
+        }
+        uint32_t r[2 * NQ];
+        if constexpr (NQ == 8) {
+            tc_ld16_issue(at + u * 2 * NQ, r);
+            tc_ld16_wait(r);
+        } else {
+            tc_ld32_issue(at + u * 2 * NQ, r);
+            tc_ld_wait(r);
+        }
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) {
+            const float f = __shfl_sync(0xffffffffu, unit, q);
+            r[q] = __float_as_uint(__uint_as_float(r[q]) * f);
+            r[NQ + q] = __float_as_uint(__uint_as_float(r[NQ + q]) * f);
+        }
+        if constexpr (NQ == 8) tc_st16_issue(at + u * 2 * NQ, r);
+        else tc_st32_issue(at + u * 2 * NQ, r);
+    }
+    tc_st_wait();
 }
 
 template <int NQ, int UNITS>
@@ -164,10 +244,12 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
     uint32_t *tops = reinterpret_cast<uint32_t *>(factors + 12 * NQ);                // [MR_AHEAD][8]
     float *sums = reinterpret_cast<float *>(tops + MR_AHEAD * MR_MAX_BLOCKS);        // [2][4][NQ]
     float *runs = sums + 8 * NQ;                                                     // [2][NQ]
-    double *lengths2 = reinterpret_cast<double *>(runs + 2 * NQ);                        // [NQ]
+    float *reach = runs + 2 * NQ;                                                    // [2][4][vblocks][NQ]
+    double *lengths2 = reinterpret_cast<double *>(reach + 8 * vblocks * NQ);         // [NQ]
     unsigned long long *bars = reinterpret_cast<unsigned long long *>(lengths2 + NQ);
     uint32_t *holder = reinterpret_cast<uint32_t *>(bars + 64);
     int *abort_flag = reinterpret_cast<int *>(holder + 1);
+    uint32_t *spread = reinterpret_cast<uint32_t *>(abort_flag + 1);                 // [MR_AHEAD]
     volatile int *ab = abort_flag;
     auto bar = [&](int i) { return smem_u32(&bars[i]); };
     constexpr int FULL = 0, EMPTY = MR_MAX_SLOTS, CFULL = 2 * MR_MAX_SLOTS, CEMPTY = CFULL + MR_AHEAD, SFULL = CEMPTY + MR_AHEAD, PFULL = SFULL + 2, DFULL = PFULL + 2,
@@ -330,11 +412,14 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             const bool masked = term == -INFINITY;
             // 256 times the values' powers of two, less the tile's largest (0: below fp32's), or NaN; masked targets have weights of zero
             float scale[UNITS];
+            bool far = false;
 #pragma unroll
             for (int u = 0; u < UNITS; ++u) {
                 const int e = (int)(((u < 4 ? sv.x : sv.y) >> (8 * (u & 3))) & 255u), x = e - (int)tops[c4 * MR_MAX_BLOCKS + u] + 135;
                 scale[u] = __uint_as_float(e == 255 ? 0x7fffffffu : x > 0 ? (uint32_t)x << 23 : 0u);
+                far |= x < 135 - MR_SPREAD;
             }
+            far = __any_sync(0xffffffffu, far && !masked);
             float arg[NQ];
             if (ok) {
                 uint32_t r[MR_SCOLS<NQ>];
@@ -366,6 +451,7 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             if (lane == 0) mbar_arrive(bar(SFREE + b));                               // (the scores are in registers)
             // the weights of the tile before the last have been used; of the maxima there are as many as tiles ahead
             ok = ok && mbar_wait(bar(DFULL + b), ph ^ 1u, ab);
+            if (far && lane == 0) spread[c4] = 1u;
             ok = all_softmax(ok, group ? 4 : 1);
             if (!ok) break;
             // a lane to a query: the tile's largest exponent, and what the sums so far and the tile's are multiplied by
@@ -391,16 +477,19 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
 #pragma unroll
                 for (int u = 0; u < UNITS; ++u) {
                     if (u >= nb) break;
-                    const float a0 = masked ? 0.f : e[0] * scale[u], a1 = masked ? 0.f : e[1] * scale[u], a2 = masked ? 0.f : e[2] * scale[u],
-                                a3 = masked ? 0.f : e[3] * scale[u];
-                    const uint32_t lo = e4m3_two(a0, a1), hi = e4m3_two(a2, a3);
-                    const float2 bl = e4m3_pair(lo), bh = e4m3_pair(hi);
-                    const uint32_t lo2 = e4m3_two((a0 - bl.x) * 16.f, (a1 - bl.y) * 16.f), hi2 = e4m3_two((a2 - bh.x) * 16.f, (a3 - bh.y) * 16.f);
-                    unsigned char *block = weights + u * (2 * NQ) * 128;
-                    auto put = [&](int r, uint32_t byte) { block[r * 128 + (((p >> 4) ^ (r & 7)) << 4)] = (unsigned char)byte; };
-                    put(q, lo); put(q + 1, lo >> 8); put(q + 2, hi); put(q + 3, hi >> 8);
-                    put(NQ + q, lo2); put(NQ + q + 1, lo2 >> 8); put(NQ + q + 2, hi2); put(NQ + q + 3, hi2 >> 8);
+                    put_weights<NQ>(weights + u * (2 * NQ) * 128, p, q, masked ? 0.f : e[0] * scale[u], masked ? 0.f : e[1] * scale[u], masked ? 0.f : e[2] * scale[u],
+                                    masked ? 0.f : e[3] * scale[u]);
                 }
+            }
+            if (spread[c4]) {
+                float again[NQ];
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) again[q] = arg[q];
+                // (the products of the tile before the last have been used, by the images as well)
+                ok = mbar_wait(bar(DFREE + b), ph ^ 1u, ab);
+                ok = weights_apart<NQ>(ok, again, own, sv, reach + b * 4 * vblocks * NQ, weights, nb, vblocks, p, nq, group ? 4 : 1);
+                if (!ok) break;
+                if (p < MR_MAX_BLOCKS) tops[c4 * MR_MAX_BLOCKS + p] = 127u;           // (what the images are multiplied by: they are whole as they are)
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tc_fence_before();
@@ -444,6 +533,8 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
+            const bool apart = spread[t % MR_AHEAD] != 0;
+            if (apart) images_apart<NQ>(tD + lanes + b * dcols, reach + b * 4 * vblocks * NQ, maxima + 4 * (t % MR_AHEAD) * NQ, nb, vblocks, lane);
             // what the images so far and the tile's are multiplied by
             __syncwarp();
             if (lane < NQ) {
@@ -668,6 +759,7 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
                 top = __reduce_max_sync(0xffffffffu, top);
                 if (lane == 0) tops[b * MR_MAX_BLOCKS + u] = top;
             }
+            if (lane == 0) spread[b] = 0u;
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(CFULL + b));

@@ -149,3 +149,111 @@ def test_exponents_whose_products_one_dimension_carries(B, n, many, d):
     made_of = (x.double().square().sum(2) + yv.square().sum(1)[:, None]) / eps.double()[:, None]
     assert ((lse - z).abs() <= (0.67 * (-(-d // 32) * 32) + 8) * U * made_of).all(), float(((lse - z).abs() / made_of / U).max())
     assert ((out - yv[:, None]).abs() <= 2.0 ** -8 * yv[:, None].abs()).all()
+
+
+def weighted(x, y, g, eps, v):
+    """Images, logarithms of the sums, and bounds, in float64: those of the formula beside the other tests, but for exponents, (0.67 d + 8) U, and for what two
+    e4m3 numbers leave of a weight.  Weights w times their values' powers of two 2^e are taken against the largest such product of the tile, 2^M: the second number
+    is off by up to 2^-14 of w 2^(e + 8 - M), the part of the image so by 448 2^-22 2^M, at most 2^-21 of the largest product of a weight and a value (which is above
+    224 2^e).  Powers of a tile that differ by at most 2^3 are taken against the largest of them instead: 2^-18.  Never more than the product itself."""
+    import torch
+    masked = g == -float("inf")
+    x, y, v, g = x.double(), torch.where(masked[:, :, None], 0.0, y.double()), torch.where(masked[:, :, None], 0.0, v.double()), torch.where(masked, 0.0, g)
+    d = x.shape[2]
+    e = eps.double()[:, None, None]
+    made_of = (x.square().sum(2)[:, :, None] + y.square().sum(2)[:, None, :] + g.abs()[:, None, :]) / e
+    z = (g[:, None, :] - (x.square().sum(2)[:, :, None] + y.square().sum(2)[:, None, :] - 2 * x @ y.transpose(1, 2))) / e
+    z = torch.where(masked[:, None, :], -float("inf"), z)
+    lse = torch.logsumexp(z, 2)
+    p = torch.exp(z - lse[:, :, None])
+    out = p @ v
+    size = (0.67 * (-(-d // 32) * 32) + 8) * U * made_of
+    mean = (p * size).sum(2)
+    err = (p * (size + mean[:, :, None] + 2.0 ** -8 + 2.0 ** -16)) @ v.abs() + 2.0 ** -8 * out.abs()
+    for j in range(0, v.shape[1], 128):
+        for k in range(0, v.shape[2], 128):
+            most = p[:, :, j:j + 128] * v[:, j:j + 128, k:k + 128].abs().amax(2)[:, None, :]
+            err[:, :, k:k + 128] += torch.minimum(2.0 ** -18 * most.amax(2, keepdim=True), most).sum(2, keepdim=True)
+    return out, lse, err, mean + 2.0 ** -16 + 2 * U * lse.abs()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 5, 12, 16, 31, 300])
+@pytest.mark.parametrize("d,dv", [(64, 0), (64, 40), (256, 256), (512, 0), (128, 512), (1024, 0), (1024, 1024), (100, 700)])
+def test_values_far_larger_than_those_that_have_the_weights(B, n, d, dv):
+    import torch
+    W, m = 4, 400
+    x, y, g, eps, v = inputs(W, n, m, d, dv, seed=3)
+    own = v is not None
+    v = v if own else y
+    # targets without weight whose values (their own, or far away points) are 2^20 times the others'; one of a tile, all but one, every other; blocks apart
+    far = torch.zeros(W, m, dtype=torch.bool)
+    far[0, ::128], far[1, :], far[2, ::2] = True, True, True
+    far[1, 5::128] = False
+    far[3, 200:] = True
+    v = torch.where(far[:, :, None], v * 2.0 ** 20, v)
+    if not own:
+        y = v
+    else:
+        v[3, :, 128:] *= 2.0 ** 9
+    g = torch.where(far, -1e3 * eps.double()[:, None], g)
+    if not own:                                                       # (points that far away need no potential to have no weight)
+        g[far] = 0.0
+    y8, v8 = B.cloud8_pack(y.cuda()), B.cloud8_pack(v.cuda()) if own else None
+    out, lse = B.cloud8_map(x.cuda(), y8, g.cuda(), eps.cuda(), v8, lse=True)
+    yv = y8.values().cpu()
+    want, wl, err, lerr = weighted(x, yv, g, eps, v8.values().cpu() if own else yv)
+    out, lse = out.cpu().double(), lse.cpu().double()
+    assert ((out - want).abs() <= err).all(), float(((out - want).abs() / err).max())
+    assert ((lse - wl).abs() <= lerr).all()
+    # weights of every size beside values of every size
+    gen = torch.Generator().manual_seed(9)
+    if own:
+        power = torch.randint(-30, 31, (W, m, 1), generator=gen).double()
+        v = (torch.randn(W, m, dv, generator=gen) * torch.exp2(power)).float()
+        g = 0.1 * torch.randn(W, m, generator=gen, dtype=torch.float64) - eps.double()[:, None] * power[:, :, 0] * 0.7
+        v8 = B.cloud8_pack(v.cuda())
+        out, lse = B.cloud8_map(x.cuda(), y8, g.cuda(), eps.cuda(), v8, lse=True)
+        want, wl, err, lerr = weighted(x, yv, g, eps, v8.values().cpu())
+        assert ((out.cpu().double() - want).abs() <= err).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,m", [(3, 300), (20, 300), (300, 300), (300, 3000)])
+def test_values_that_are_zeros_masked_or_not_finite_beside_large_ones(B, n, m):
+    import torch
+    W, dv = 5, 200
+    x, y, g, eps, v = inputs(W, n, m, 64, dv, seed=4)
+    v[:, ::3] *= 2.0 ** 25
+    v[0, 1::3] = 0.0                                                  # (a target's values may be nothing)
+    v[1] = 0.0
+    v[2, :128] = 0.0
+    g[3, ::3] = -float("inf")
+    g[3, 128:256] = -float("inf")                                     # a tile without targets between others
+    v[4, 131] = float("nan")
+    v8, y8 = B.cloud8_pack(v.cuda()), B.cloud8_pack(y.cuda())
+    out, lse = (t.cpu().double() for t in B.cloud8_map(x.cuda(), y8, g.cuda(), eps.cuda(), v8, lse=True))
+    assert torch.isnan(out[4]).all() and not torch.isnan(lse).any()
+    want, wl, err, lerr = weighted(x[:4], y8.values().cpu()[:4], g[:4], eps[:4], v8.values().cpu()[:4])
+    assert ((out[:4] - want).abs() <= err).all() and ((lse[:4] - wl).abs() <= lerr).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(8, 1, 6000, 512, 512), (32, 12, 4000, 128, 64), (5, 3, 9000, 1024, 1024), (6, 9, 3000, 600, 700), (40, 16, 900, 200, 256), (30, 8, 2500, 64, 1)])
+def test_calls_over_values_far_apart_one_after_the_other(B, shape):
+    # tiles of values alike between tiles of others: roles of a block that get out of step would show as images that differ
+    import torch
+    W, n, m, d, dv = shape
+    x, y, g, eps, v = inputs(*shape)
+    apart = (torch.arange(m) // 128 % 3 != 1) & (torch.arange(m) % 5 == 0)
+    v[:, apart] *= 2.0 ** 12
+    y8, v8 = B.cloud8_pack(y.cuda()), B.cloud8_pack(v.cuda())
+    x, g, eps = x.cuda(), g.cuda(), eps.cuda()
+    want, wl = B.cloud8_map(x, y8, g, eps, v8, lse=True)
+    outs = [B.cloud8_map(x, y8, g, eps, v8, lse=True) for _ in range(40)]
+    assert not torch.isnan(want).any()
+    for out, lse in outs:
+        assert torch.equal(out, want) and torch.equal(lse, wl)
+    one = slice(1, 3)
+    exact, wl2, err, lerr = weighted(x[one].cpu(), y8.values()[one].cpu(), g[one].cpu(), eps[one].cpu(), v8.values()[one].cpu())
+    assert ((want[one].cpu().double() - exact).abs() <= err).all() and ((wl[one].cpu().double() - wl2).abs() <= lerr).all()
