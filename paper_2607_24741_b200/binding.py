@@ -420,7 +420,8 @@ def cloud8_map(x, y, g, eps, v=None, *, lengths=None, lse=False, out=None):
     """Images of x [W, n, d] (bfloat16, CUDA) under the entropic map of the bank y [W, m, d], a Cloud8, with its potential g [W, m]
     (float64, or None: zeros) and eps [W] float32: the values' mean by the softmax over j of (g_j - |x_i - y_j|^2) / eps, the values being
     the bank's points or v [W, m, dv], a Cloud8.  lengths [W] int32: the targets of each lane that count; see sinkhorn_cloud8_map in
-    the header.  Returns [W, n, dv] bfloat16 (into `out`, if given), with `lse` also the logarithms of the sums [W, n] float32."""
+    the header.  Returns [W, n, dv] bfloat16 (into `out`, if given), with `lse` also the logarithms of the sums [W, n] float32.  No gradient is
+    recorded."""
     if not isinstance(y, Cloud8) or not (v is None or isinstance(v, Cloud8)):
         raise ValueError("y, and v if given, must be Cloud8")
     if not torch.is_tensor(x) or not x.is_cuda or x.dtype != torch.bfloat16 or x.dim() != 3:
