@@ -510,9 +510,8 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             const size_t r = (size_t)w * P.n + q0 + tid;
             float top;
             const float total = total_of(tid, top);
-            if (z) {}                                                               // (the first block of a query has them)
-            else if (P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[r * P.splits + split] = make_float2(top, total);
-            else if (P.lse) P.lse[r] = map_lse(top, total, k, lengths2[tid]);
+            if (z == 0 && P.splits > 1) reinterpret_cast<float2 *>(P.part_ml)[r * P.splits + split] = make_float2(top, total);
+            if (z == 0 && P.splits == 1 && P.lse) P.lse[r] = map_lse(top, total, k, lengths2[tid]);
         }
     } else if (warp < 8) {
         // ---- images: a thread to a dimension of every block

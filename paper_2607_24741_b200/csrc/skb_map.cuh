@@ -11,7 +11,6 @@ namespace skb {
 
 constexpr int MAP_TILES_MAX_D = 512;          // queries' depth up to which they stay in shared memory as tiles
 constexpr int MAP_TILES_SMEM = 232448;        // shared memory that a block may have
-constexpr int MAP_SM_SMEM = 228 * 1024;       // ... and that an SM has, 1 KB of it taken for each block
 
 struct Map {
     const uint16_t *x;                        // [W, n, d] bf16
