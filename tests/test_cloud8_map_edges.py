@@ -257,3 +257,24 @@ def test_calls_over_values_far_apart_one_after_the_other(B, shape):
     one = slice(1, 3)
     exact, wl2, err, lerr = weighted(x[one].cpu(), y8.values()[one].cpu(), g[one].cpu(), eps[one].cpu(), v8.values()[one].cpu())
     assert ((want[one].cpu().double() - exact).abs() <= err).all() and ((wl[one].cpu().double() - wl2).abs() <= lerr).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [30, 160])
+def test_images_are_the_solved_plan_applied_to_the_values(B, n):
+    # sum_j pi_ij v_j over sum_j pi_ij, which apply_plan forms in float64 and rounds to fp32
+    import torch
+    W, m, d, dv = 3, 200, 64, 15
+    x, y, _, _, v = inputs(W, n, m, d, dv, seed=6)
+    x8, y8, v8 = (B.cloud8_pack(t.float().cuda()) for t in (x, y, v))
+    a, b, eps = torch.full((W, n), 1 / n).cuda(), torch.full((W, m), 1 / m).cuda(), torch.full((W,), 0.1).cuda()
+    sb = B.SinkhornBatch(x8, y8, a, b, eps, 1e-4)
+    sb.drain()
+    g = sb.potentials(f64=True)[1]
+    applied = sb.apply_plan(torch.cat((v8.values(), torch.ones(W, m, 1, device="cuda")), 2)).cpu().double()
+    sb.close()
+    out = B.cloud8_map(x8.values(torch.bfloat16), y8, g, eps, v8).cpu().double()
+    want = applied[:, :, :dv] / applied[:, :, dv:]
+    exact, _, err, _ = weighted(x8.values().cpu(), y8.values().cpu(), g.cpu(), eps.cpu(), v8.values().cpu())
+    assert ((exact - want).abs() <= 2.0 ** -20 * v8.values().cpu().double().abs().amax(1, keepdim=True)).all()
+    assert ((out - want).abs() <= err + 2.0 ** -20 * v8.values().cpu().double().abs().amax(1, keepdim=True)).all()
