@@ -516,7 +516,7 @@ def plan_loss(scores, index, logits=None, *, temperature=1.0, weight=None, grad=
     with _on(device):
         loss = torch.empty(lead, dtype=torch.float32, device=device) if weight is None else torch.empty_like(weight)
         out = grad if in_place else None
-        if grad is True:
+        if not in_place and grad:
             out = torch.empty_like(scores.detach(), memory_format=torch.contiguous_format)
         _check_op(lib.sinkhorn_plan_loss(scores.data_ptr(), DTYPES[scores.dtype], rows, m, ld, index.data_ptr(), None if logits is None else logits.data_ptr(), k,
                                          float(temperature), None if weight is None else weight.data_ptr(), loss.data_ptr(), None if out is None else out.data_ptr(),

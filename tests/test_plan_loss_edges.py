@@ -5,7 +5,7 @@ import ctypes
 import numpy as np
 import pytest
 
-from test_plan_loss import B, U, check, compare, inputs  # noqa: F401  (B is the fixture)
+from test_plan_loss import B, U, check, compare, inputs, run  # noqa: F401  (B is the fixture)
 
 
 @pytest.mark.gpu
@@ -157,3 +157,15 @@ def test_gradients_between_the_scores_rows_and_beside_them(B):
             with pytest.raises(B.SkbError):
                 B.plan_loss(s, torch.zeros(rows, 1, dtype=torch.int32, device="cuda"), grad=g)
         overlapping(call)
+
+
+@pytest.mark.gpu
+def test_a_gradient_that_is_asked_for_by_any_true_value_is_given(B):
+    import torch
+    scores, index, t, weight = (v.cuda() for v in inputs(6, 40, 3, torch.float32, 1))
+    want = B.plan_loss(scores, index, t, weight=weight, grad=True)
+    for yes in (1, np.True_):
+        loss, grad = B.plan_loss(scores, index, t, weight=weight, grad=yes)
+        assert torch.equal(loss, want[0]) and torch.equal(grad, want[1])
+    for no in (0, None, np.False_):
+        assert torch.equal(B.plan_loss(scores, index, t, weight=weight, grad=no), want[0])
