@@ -10,6 +10,7 @@
 // Both read a cloud once and write it once.  64 x 1024 x 512 from bf16, with the values in bf16 (168 MB), take 30.8 us, 83 % of the measured copy rate
 // (34.8 with a comparison of every value for what is not finite, and one for what would saturate).  Sixteen consecutive dimensions to a thread, eight threads to a block, up to
 // a warp to a point: values stay in registers between the block's maximum and the codes, and 16 codes are one 16-byte store.
+// The way back takes 19.0 us to bf16 (101 MB, 81 % of the copy rate) and 39.9 to fp32 (168 MB, 64 %).
 #include <cuda_runtime.h>
 #include <string>
 

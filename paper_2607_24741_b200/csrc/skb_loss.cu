@@ -6,7 +6,8 @@
 //
 // One pass: a row is read once, 16 bytes a thread and vector, and stays in registers (up to 64 scores of bf16 or 32 of fp32 a
 // thread, raw) until its maximum and sum are known; then the gradient is written.  So memory bounds it, and the latencies of what a row
-// needs besides: 65536 rows of 1024 in bf16 take 47 us for 270 MB (87 % of the measured copy rate; 53 for a call by itself), of 64 12.  Exponentials are taken against the
+// needs besides: 65536 rows of 1024 in bf16 take 47 us for 270 MB (87 % of the measured copy rate; 52 for a call by itself; 28 without the
+// gradient), of 64 12.  Exponentials are taken against the
 // thread's own maximum for the sum; short rows keep them, others take them again against the row's: that is one barrier a row instead of two, and no fp32
 // copies in registers.  What a row is given goes by its length (launch_by_length): a quarter of a warp, half of one, a warp, four, eight or 16 warps, or a cluster of up to eight blocks, whose
 // maxima and sums meet in distributed shared memory; long rows, a device full of them, stay in shared memory (loss_long_kernel); rows longer than what a cluster's registers hold are read twice, the second time from L2 (a row

@@ -15,7 +15,7 @@
 //            lost), rows of their own again.  The reference is the tile's largest power of two, or where these are far apart the query's largest product
 // so that nothing of a code passes through a register.  The same work by mma.sync, codes made f16 in registers, was bound by its instructions: one query
 // to each of 8 banks of 16384 x 512 took 41 us.
-// That call takes 27 us for 69 MB now, twelve queries to each of 32 banks of 8192 x 128 with values of 64 dimensions 31 us for 54 MB.  Of the first some
+// That call takes 28 us for 69 MB now, twelve queries to each of 32 banks of 8192 x 128 with values of 64 dimensions 31 us for 54 MB.  Of the first some
 // 17 us are a block's time, whose tiles go by at the rate of the memory (2600 cycles for 64 KB) between the first one's arrival (some 8000, as all of a
 // block's slots are asked for at once) and the last one's way through the roles (scores 500, softmax 2000, images 1000, results 2000); with twelve queries
 // the softmax takes 1.5 times as long as the memory.  Made no difference: loads that start before the block is ready, a softmax

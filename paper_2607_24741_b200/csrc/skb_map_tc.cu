@@ -19,8 +19,12 @@
 //                below 1): O is then multiplied by a power of two, exactly
 //   warp 8       loads: bulk copies of 32 KB and of a tile's terms
 //   warp 9       matrix instructions, one thread: S of tile t + 1 before O of tile t
-// 64 lanes of 1024 queries to 1024 x 512 take 204 us, 22 of them the staging: 206 GFLOP of products (two thirds of them the scores, formed
-// for 256 dimensions of the images each) at 1.1 PFLOP/s.  What bounds it: at 128 dimensions the exponentials (128 x 128 of a tile at 16 a clock take as long as its products), deeper the products.
+// 64 lanes of 1024 queries to 1024 x 512 take 205 us, 22 of them the staging: 206 GFLOP of products (two thirds of them the scores, formed
+// for 256 dimensions of the images each) at 1.1 PFLOP/s.  What bounds it: at 128 dimensions the exponentials (128 x 128 of a tile at 16 a clock take as long as
+// its products); deeper no unit by itself (the tensor pipe is active for 43 % of 16 lanes' 59 us): a block's queries arrive and its images leave
+// with nothing beside them, one block an SM, every eight tiles.
+// Weights in bf16 are the choice of one pass of the matrix unit over the values: eight bits as of the images themselves.  Where values average out that
+// is felt: images of values of their own with mixed signs are off by 2.4e-3 of their size (rms) where weights in fp32 leave bf16's 1.7e-3.
 // Every wait is bounded (skb_tmem.cuh): one that runs out ends all roles, and the block's images are NaN.
 #include <cuda.h>
 #include <cuda_runtime.h>
