@@ -545,9 +545,10 @@ skb_status sinkhorn_cloud8_dots(const void *x, const void *y, int W, int n, int 
  * NaN or plus infinity, and an eps that is not a positive number make the images they take part in NaN.
  * Exponents are made of fp32 products of the bf16 query and the bank's values, good to (0.67 d + 8) 2^-24 (|x|^2 + |y|^2 + |g|) / eps
  * (d to a whole 32: the matrix unit cuts products and sums off, and a sum that one dimension carries loses at every instruction); weights, for
- * the product with the values, are rounded to 8 bits, sums are fp32, and one of an image loses at most 2^-11.6 of its terms' magnitudes, however long the bank is.  With few queries, short banks or d above 512 a value's part of an image is besides
- * off by up to 2^-18 of the largest product of a weight and a value that its 128 dimensions hold among the 128 targets of a tile.  Weights times values
- * are added up before they are divided: values above 2^100 may pass fp32's range.  out must not overlap x.
+ * the product with the values, are rounded to 8 bits (those below 2^-126 of a query's largest are none), sums are fp32, and one of an image loses at
+ * most 2^-11.6 of its terms' magnitudes, however long the bank is.  With few queries, short banks or d above 512 a value's part of an image is besides
+ * off by up to 2^-18 of the largest product of a weight and a value that its 128 dimensions hold among the 128 targets of a tile, or 2^-113.  Weights times
+ * values are added up before they are divided: values above 2^100 may pass fp32's range.  out must not overlap x.
  * d and dv <= 1024, n and m <= 262143, W <= 65535.  Enqueues kernels on `stream` of the current device and returns; the workspace of
  * sinkhorn_cloud8_map_workspace_bytes(W, n, m, d, dv) bytes (0: a bad shape; dv = 0: v is null; device, 256-byte aligned) is in use until
  * they are done: calls that may overlap need one each.
@@ -570,7 +571,8 @@ skb_status sinkhorn_cloud8_map(const void *x, const void *y, const double *g, co
  *            refused where it overlaps them otherwise (rows of another stride: where their ranges meet)
  * T from 1e-30 to 1e30, k <= 256, m <= 262143, rows < 2^31.  Sums are fp32, in an order that does not change from call to call: a loss
  * is good to 2^-15 (1 + sum_k q_k (|log q_k| + |log p_index(k)|)), a gradient to |weight / T| (p_ij + sum of its q_k) 2^-15 (1 + |log p_ij| / 128) besides
- * its type's rounding.  One kernel on `stream` of the current device, which reads a row once (longer ones than 131068 of fp32 or 262136 of bf16 twice).
+ * its type's rounding; p and q below 2^-126 of a row's largest are none.  One kernel on `stream` of the current device, which reads a row once (longer
+ * ones than 131068 of fp32 or 262136 of bf16 twice).
  */
 skb_status sinkhorn_plan_loss(const void *scores, int dtype, long long rows, int m, long long ld, const int *index, const float *logits, int k,
                               float temperature, const float *weight, float *loss, void *grad, long long ldg, void *stream);
