@@ -78,13 +78,6 @@ __device__ __forceinline__ void dots_mma(uint32_t acc, uint64_t a, uint64_t b, u
                      "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
                      ::"r"(acc), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(sfa), "r"(sfb) : "memory");
 }
-// one thread of a warp, the same one each time
-__device__ __forceinline__ bool one_thread()
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
-}
 // 128 points' words of four scales, 512 bytes of shared memory, into four columns of tensor memory, the same for all four
 // quarters of the lanes.  Rows of 16 bytes, eight to a group of 128 bytes, no swizzle.
 __device__ __forceinline__ void scales_to_tmem(uint32_t taddr, uint32_t saddr)
@@ -233,7 +226,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
                 const uint32_t acc = tmem + b * DT_BN, sf = tmem + DT_SF_COL + s * DT_SF_STRIDE;
                 const uint64_t da = tc_desc(tile_a(s)), db = tc_desc(tile_a(s) + DT_TILE);
                 const int left = P.row_bytes - c * 128;           // 32 bytes of a point to an instruction
-                if (one_thread()) {
+                if (elected()) {
                     if constexpr (SCALED) {
 #pragma unroll
                         for (int q = 0; q < WORDS; ++q) {
@@ -268,7 +261,7 @@ __global__ void __launch_bounds__(DT_THREADS, 1) dots_kernel(const __grid_consta
             }
         }
         // what was issued is over before tensor memory is given back
-        if (one_thread()) {
+        if (elected()) {
             tc_commit(bar(LAST));
             int unused = 0;
             mbar_wait(bar(LAST), 0, &unused);

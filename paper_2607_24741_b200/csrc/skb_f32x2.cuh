@@ -1,6 +1,7 @@
-// Packed fp32 arithmetic (two values to an instruction) and the fast exponential.
+// Packed fp32 arithmetic (two values to an instruction), the fast exponential, a warp's maximum, two values as bf16.
 #pragma once
 #include <cuda_runtime.h>
+#include <stdint.h>
 
 namespace skb {
 
@@ -39,6 +40,19 @@ __device__ __forceinline__ float ex2_fast(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// (NaN counts as none)
+__device__ __forceinline__ float warp_max(float v)
+{
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
+{
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
 }
 
 }  // namespace skb

@@ -39,12 +39,6 @@ struct Loss {
     float inv_t, c;                           // 1 / T and log2(e) / T
 };
 
-__device__ __forceinline__ float ex2f(float v)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 // two scores of a vector
 template <bool BF16> __device__ __forceinline__ u64 two(const uint4 &v, int i)
 {
@@ -66,12 +60,6 @@ template <bool BF16> __device__ __forceinline__ float largest(const uint4 &v)
     } else
         return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
 }
-__device__ __forceinline__ float warp_max(float v)
-{
-    float r;
-    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ u64 mul2(u64 a, u64 b)
 {
     u64 d;
@@ -83,15 +71,9 @@ __device__ __forceinline__ u64 exponentials(u64 s, u64 at2, u64 c2)
 {
     float a, b;
     unpack2(mul2(sub2(s, at2), c2), a, b);
-    return pack2(ex2f(a), ex2f(b));
+    return pack2(ex2_fast(a), ex2_fast(b));
 }
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 // (maximum, sum of exponentials against it), both of none: (-inf, 0)
 struct __align__(8) Part {                   // (written to other blocks in one 8-byte store)
     float m, s;
@@ -101,7 +83,7 @@ template <int COUNT> __device__ __forceinline__ Part join(Part p, float c)
 {
     const float m = warp_max(p.m), at = finite_max(m);
     // (a sum beside a maximum of minus infinity is 0, or NaN, which stays)
-    float s = p.s * ex2f((p.m - at) * c);
+    float s = p.s * ex2_fast((p.m - at) * c);
 #pragma unroll
     for (int off = COUNT / 2; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
     return {m, s};
@@ -121,7 +103,7 @@ template <int COUNT> __device__ __forceinline__ Part group_join(Part p, float c)
     if constexpr (COUNT >= 32) return join<32>(p, c);
     else {
         const float m = group_max<COUNT>(p.m);
-        float s = p.s * ex2f((p.m - finite_max(m)) * c);
+        float s = p.s * ex2_fast((p.m - finite_max(m)) * c);
 #pragma unroll
         for (int off = COUNT / 2; off; off /= 2) s += __shfl_xor_sync(0xffffffffu, s, off);
         return {m, s};
@@ -130,7 +112,7 @@ template <int COUNT> __device__ __forceinline__ Part group_join(Part p, float c)
 __device__ __forceinline__ Part join(Part a, Part b, float c)
 {
     const float m = fmaxf(a.m, b.m), at = finite_max(m);
-    return {m, a.s * ex2f((a.m - at) * c) + b.s * ex2f((b.m - at) * c)};
+    return {m, a.s * ex2_fast((a.m - at) * c) + b.s * ex2_fast((b.m - at) * c)};
 }
 
 // TPR threads of each of C blocks to a row, V vectors in each thread's registers; V = 0: the row is read twice.  EVEN: rows and gradients are whole vectors.
@@ -215,10 +197,10 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
             }
         teach.m = group_max<SPAN>(teach.m);
         const float at = finite_max(teach.m);
-        teach.s = ex2f((l0 - at) * P.c);
+        teach.s = ex2_fast((l0 - at) * P.c);
         // (a thread reads back what it wrote)
         if constexpr (TPR < LS_MAX_K)
-            for (int k = t + TPR; k < P.k; k += TPR) teach.s += ex2f((s_log[k] - at) * P.c);
+            for (int k = t + TPR; k < P.k; k += TPR) teach.s += ex2_fast((s_log[k] - at) * P.c);
 #pragma unroll
         for (int off = SPAN / 2; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
     }
@@ -288,12 +270,12 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         const float log_all = logf(part.s * teach_inv);                // (next to 1 in a confident row, where a fast logarithm is not good)
         // (q log q - q log p)
         auto term = [&](float q, float l, float at) { return q != 0.f ? q * (((l - teach_at) - (at - part.m)) * P.inv_t + log_all) : 0.f; };
-        own_q = ex2f((l0 - teach_at) * P.c) * teach_inv;
+        own_q = ex2_fast((l0 - teach_at) * P.c) * teach_inv;
         sum = term(own_q, l0, score);
         if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
         if constexpr (TPR < LS_MAX_K)
             for (int k = t + TPR; k < P.k; k += TPR) {
-                s_q[k] = ex2f((s_log[k] - teach_at) * P.c) * teach_inv;
+                s_q[k] = ex2_fast((s_log[k] - teach_at) * P.c) * teach_inv;
                 sum += term(s_q[k], s_log[k], s_score[k]);
             }
         if (rank == 0) {
@@ -320,7 +302,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
     const bool wide = EVEN || (uintptr_t)out % 16 == 0;
     // what an exponential is multiplied by: kept ones are against this thread's own maximum.  (That is minus infinity where the thread has seen nothing else: its
     // exponentials, and this, are 0; a row of nothing else has an infinite a and is NaN.)
-    const float factor = (KEEP ? ex2f((own - finite_max(part.m)) * P.c) : 1.f) * a;
+    const float factor = (KEEP ? ex2_fast((own - finite_max(part.m)) * P.c) : 1.f) * a;
     const u64 at2 = pack2(part.m, part.m), f2 = pack2(factor, factor);
     auto again = [&](const uint4 &y, u64 (&e)[E / 2]) {
 #pragma unroll
@@ -332,7 +314,7 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         for (int i = 0; i < E / 2; ++i) {
             float p, q;
             unpack2(mul2(e[i], f2), p, q);
-            if constexpr (BF16) r[i] = bf16x2(p, q);
+            if constexpr (BF16) r[i] = bf16_pair(p, q);
             else { r[2 * i] = __float_as_uint(p); r[2 * i + 1] = __float_as_uint(q); }
         }
         if (!live) r[0] = r[1] = r[2] = r[3] = 0u;
@@ -375,8 +357,8 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
         if (named < 0 || (alike & ((1u << lane) - 1u)) || (C > 1 && (head + named) / E / TPR % C != rank)) return;
         float q = 0.f;
         for (unsigned left = alike; left; left &= left - 1u) q += s_q[__ffs(left) - 1];
-        const float g = ex2f((score - part.m) * P.c) * a - q * w;
-        out[head + named] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+        const float g = ex2_fast((score - part.m) * P.c) * a - q * w;
+        out[head + named] = BF16 ? (T)bf16_pair(g, 0.f) : (T)__float_as_uint(g);
         return;
     }
     for (int k = t; k < P.k; k += TPR) {
@@ -390,8 +372,8 @@ __global__ void __launch_bounds__(TPR <= 256 ? 256 : TPR, TPR <= 256 ? 4 : 2) lo
                 q += s_q[o];
             }
         if (!first) continue;
-        const float g = ex2f(((k == t ? score : s_score[k]) - part.m) * P.c) * a - q * w;
-        out[head + j] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+        const float g = ex2_fast(((k == t ? score : s_score[k]) - part.m) * P.c) * a - q * w;
+        out[head + j] = BF16 ? (T)bf16_pair(g, 0.f) : (T)__float_as_uint(g);
     }
 }
 
@@ -475,7 +457,7 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
 #pragma unroll
             for (int v = 1; v < PER; ++v) top = fmaxf(top, largest<BF16>(x[v]));
             if (top > part.m) {
-                part.s *= ex2f((part.m - top) * P.c);                                // (of minus infinity: 0 times 0)
+                part.s *= ex2_fast((part.m - top) * P.c);                                // (of minus infinity: 0 times 0)
                 part.m = top;
             }
             const u64 at2 = pack2(finite_max(part.m), finite_max(part.m));
@@ -495,7 +477,7 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
         const float l0 = named >= 0 ? logit : -INFINITY;
         if (warp * 32 < P.k) {
             teach.m = warp_max(l0);
-            teach.s = ex2f((l0 - finite_max(teach.m)) * P.c);
+            teach.s = ex2_fast((l0 - finite_max(teach.m)) * P.c);
 #pragma unroll
             for (int off = 16; off; off /= 2) teach.s += __shfl_xor_sync(0xffffffffu, teach.s, off);
         }
@@ -515,7 +497,7 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
         float own_q = 0.f, sum = 0.f;
         if (warp * 32 < P.k) {
             const float log_all = logf(part.s) - logf(teach.s);
-            own_q = ex2f((l0 - teach_at) * P.c) * teach_inv;
+            own_q = ex2_fast((l0 - teach_at) * P.c) * teach_inv;
             if (own_q != 0.f) sum = own_q * (((l0 - teach_at) - (score - part.m)) * P.inv_t + log_all);
             if (t < P.k) { s_index[t] = named; s_q[t] = own_q; }
 #pragma unroll
@@ -540,7 +522,7 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
                     for (int i = 0; i < E / 2; ++i) {
                         float p, q;
                         unpack2(mul2(exponentials(two<BF16>(x, i), at2, c2), f2), p, q);
-                        if constexpr (BF16) r[i] = bf16x2(p, q);
+                        if constexpr (BF16) r[i] = bf16_pair(p, q);
                         else { r[2 * i] = __float_as_uint(p); r[2 * i + 1] = __float_as_uint(q); }
                     }
                     if (!live) r[0] = r[1] = r[2] = r[3] = 0u;
@@ -565,8 +547,8 @@ __global__ void __launch_bounds__(LL_THREADS + 32, 1) loss_long_kernel(const __g
                     q += s_q[o];
                 }
             if (first) {
-                const float g = ex2f((score - part.m) * P.c) * a - q * w;
-                out[named] = BF16 ? (T)bf16x2(g, 0.f) : (T)__float_as_uint(g);
+                const float g = ex2_fast((score - part.m) * P.c) * a - q * w;
+                out[named] = BF16 ? (T)bf16_pair(g, 0.f) : (T)__float_as_uint(g);
             }
         }
     }

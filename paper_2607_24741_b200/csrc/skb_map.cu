@@ -32,6 +32,7 @@
 #include <string>
 
 #include "skb_cloud_io.cuh"
+#include "skb_f32x2.cuh"
 #include "skb_map.cuh"
 #include "skb_operators.h"
 #include "skb_tmem.cuh"
@@ -47,28 +48,10 @@ constexpr int MR_SPREAD = 3;                                  // how far apart v
 template <int NQ> constexpr int MR_ROWS = NQ == 8 ? 32 : 48;
 template <int NQ> constexpr int MR_SCOLS = NQ == 8 ? 32 : 64;  // columns of tensor memory that its result takes
 
-__device__ __forceinline__ float ex2f(float v)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
-    return r;
-}
 __device__ __forceinline__ uint32_t e4m3_two(float lo, float hi)
 {
     uint32_t r;
     asm("{\n\t.reg .b16 p;\n\tcvt.rn.satfinite.e4m3x2.f32 p, %2, %1;\n\tcvt.u32.u16 %0, p;\n\t}" : "=r"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ float warp_max(float v)
-{
-    float r;
-    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
 }
 __device__ __forceinline__ void tma_points(uint32_t dst, const CUtensorMap *tm, int byte, int point, int lane, uint32_t mbar)
@@ -92,12 +75,6 @@ __device__ __forceinline__ void mma_codes(uint32_t d, uint64_t a, uint64_t b, ui
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ bool elected()
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
 }
 // warps of the softmax: two groups of four that take turns, where registers allow
 template <int NQ, int UNITS> constexpr int MR_GROUPS = NQ * UNITS <= 32 ? 2 : 1;
@@ -186,7 +163,7 @@ __device__ __noinline__ bool weights_apart(bool ok, const float (&arg)[NQ], cons
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 const float top = own[q + h].x;
-                a[h] = arg[q + h] == -INFINITY ? 0.f : ex2f((arg[q + h] - top) + (e - less_top(largest_of(reach + u * NQ + q + h, vblocks * NQ), top)));
+                a[h] = arg[q + h] == -INFINITY ? 0.f : ex2_fast((arg[q + h] - top) + (e - less_top(largest_of(reach + u * NQ + q + h, vblocks * NQ), top)));
             }
             put_weights<NQ>(weights + u * (2 * NQ) * 128, p, q, a[0], a[1], a[2], a[3]);
         }
@@ -201,7 +178,7 @@ __device__ __noinline__ void images_apart(uint32_t at, const float *reach, const
         float unit = 0.f;                                                            // of the query that is the lane's number
         if (lane < NQ) {
             const float top = largest_of(maxima + lane, NQ);
-            unit = ex2f(less_top(largest_of(reach + u * NQ + lane, vblocks * NQ), top == -INFINITY ? 0.f : top));
+            unit = ex2_fast(less_top(largest_of(reach + u * NQ + lane, vblocks * NQ), top == -INFINITY ? 0.f : top));
         }
         uint32_t r[2 * NQ];
         if constexpr (NQ == 8) {
@@ -377,7 +354,7 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
         const float other = runs[NQ + q], two = (more[q] + more[NQ + q]) + (more[2 * NQ + q] + more[3 * NQ + q]);
         top = fmaxf(top, other);
         const float ref = top == -INFINITY ? 0.f : top;
-        return one * ex2f(runs[q] - ref) + two * ex2f(other - ref);
+        return one * ex2_fast(runs[q] - ref) + two * ex2_fast(other - ref);
     };
     // what a warp has issued is over before tensor memory is given back
     auto finish = [&](int barrier) {
@@ -458,7 +435,7 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             if (lane < NQ) {
                 const float *mp = maxima + 4 * c4 * NQ + lane;
                 const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run, top), ref = now == -INFINITY ? 0.f : now;
-                own[lane] = make_float4(top == -INFINITY ? 0.f : top, ex2f(run - ref), ex2f(top - ref), 0.f);
+                own[lane] = make_float4(top == -INFINITY ? 0.f : top, ex2_fast(run - ref), ex2_fast(top - ref), 0.f);
                 run = now;
             }
             __syncwarp();
@@ -471,7 +448,7 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
                 for (int h = 0; h < 4; ++h) {
                     const float4 f = own[q + h];
                     // (tile's maximum plus infinity: the exponential is NaN, and so is what follows from it)
-                    e[h] = ex2f(arg[q + h] - f.x);
+                    e[h] = ex2_fast(arg[q + h] - f.x);
                     sum[q + h] = fmaf(sum[q + h], f.y, e[h] * f.z);
                 }
 #pragma unroll
@@ -539,7 +516,7 @@ __global__ void __launch_bounds__(MR_THREADS<NQ, UNITS>) map_rows_kernel(const _
             if (lane < NQ) {
                 const float *mp = maxima + 4 * (t % MR_AHEAD) * NQ + lane;
                 const float top = fmaxf(fmaxf(mp[0], mp[NQ]), fmaxf(mp[2 * NQ], mp[3 * NQ])), now = fmaxf(run, top), ref = now == -INFINITY ? 0.f : now;
-                reinterpret_cast<float2 *>(own)[lane] = make_float2(ex2f(run - ref), ex2f(top - ref) * 0.00390625f);
+                reinterpret_cast<float2 *>(own)[lane] = make_float2(ex2_fast(run - ref), ex2_fast(top - ref) * 0.00390625f);
                 run = now;
             }
             __syncwarp();
@@ -806,7 +783,7 @@ __global__ void __launch_bounds__(256) map_join_kernel(const __grid_constant__ M
 #pragma unroll 4
     for (int s = warp; s < P.splits; s += 8) {
         const float2 one = ml[s];
-        const float f = ex2f(one.x - ref);
+        const float f = ex2_fast(one.x - ref);
         const float *src = P.part_out + (r * P.splits + s) * P.dv + dim0 + lane;
         sum = fmaf(one.y, f, sum);
 #pragma unroll

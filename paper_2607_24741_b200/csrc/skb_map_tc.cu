@@ -103,23 +103,10 @@ template <bool PAIR> __device__ __forceinline__ void load_queries(uint32_t dst, 
         asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(dim), "r"(query), "r"(lane), "r"(mbar) : "memory");
 }
-// one thread of a warp, the same one each time
-__device__ __forceinline__ bool elected()
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
-    return r != 0;
-}
 // rows of 64 columns (128 bytes), 8-row groups 1024 bytes apart, the next 64 columns a chunk further
 __device__ __forceinline__ uint64_t desc_columns(uint32_t saddr)
 {
     return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(MT_CHUNK >> 4) << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
-{
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
 {
